@@ -257,7 +257,8 @@ def _prepare_experts(case, seed):
 
         s["hl"], s["stream"] = hl, torch.cuda.current_stream().cuda_stream
         s["type"] = hl.dtype_of(s["x"]) if "x" in s else 0
-        s["route"] = hl.make_route(T, s["n_tokens"], K, E, rows, s["place"], s["source"], s["counts"], s["offsets"])
+        s["route"] = hl.make_route(T, s["n_tokens"], K, E, case["align"], rows, s["place"], s["source"], s["counts"],
+                                   s["offsets"])
         s["ws_bytes"] = hl.hl_expert_workspace_bytes(T, K, E)
         s["ws"] = torch.empty(max(1, s["ws_bytes"]), dtype=torch.uint8, device=DEVICE)
         s["status"] = torch.zeros(1, dtype=torch.int32, device=DEVICE)
@@ -322,9 +323,9 @@ def _prepare_rowclip(case, seed):
 
         s["hl"], s["stream"] = hl, torch.cuda.current_stream().cuda_stream
         geom = hl.make_geometry([per_table] * T, D, case["steps"])
-        ws = hl.hl_workspace_bytes(geom, case["batch"], max(1, n), 0, 0)
+        ws = hl.hl_workspace_bytes(geom, case["batch"], max(1, n), per_table * T, 0)
         s["workspace"] = torch.empty(ws, dtype=torch.uint8, device=DEVICE)
-        s["ctx"] = _Context(hl, hl.hl_create(geom, case["batch"], max(1, n), 0, 0, s["workspace"], ws))
+        s["ctx"] = _Context(hl, hl.hl_create(geom, case["batch"], max(1, n), per_table * T, 0, s["workspace"], ws))
         s["sumsq"] = torch.zeros(1, dtype=torch.float64, device=DEVICE)
         s["tensors"] = hl.make_tensors([(s["grad"], s["grad_out"], hl.HL_TENSOR_NOT_IN_NORM), (s["dense"], s["dense_out"])])
         s["ws_bytes"] = hl.hl_grad_workspace_bytes()
@@ -350,8 +351,8 @@ def prepare(case, seed):
 def _run_sort(s):
     if not own:
         return _sorted(s["case"], s["experts"])
-    s["hl"].hl_expert_sort(s["route"], s["experts"], _expert_cap(s["case"]), s["case"]["align"], s["status"], s["ws"],
-                           s["ws_bytes"], s["stream"])
+    s["hl"].hl_expert_sort(s["route"], s["experts"], _expert_cap(s["case"]), s["status"], s["ws"], s["ws_bytes"],
+                           s["stream"])
     return s["place"], s["source"], s["counts"], s["offsets"]
 
 
