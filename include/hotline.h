@@ -565,6 +565,103 @@ HL_API int32_t hl_wide_index_cold(hl_wide* w, const int32_t* d_non_offsets, cons
                                   const int32_t* d_n_non, int32_t* d_non_slots, int64_t* d_cold_rows,
                                   int64_t* d_n_cold, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * Between the pooled rows and their gradients (no counterpart in the paper, which leaves the dense model to the GPU's
+ * framework): tokens sorted by expert and back, and the global norm of the gradients.
+ *
+ * A token is a row of `dim` values (an input's pooled rows, say) that a router sends to top_k of n_experts experts.  The
+ * calls need no context.  Rows may be fp32, bf16 or fp16 (HL_F32 ...), of any width, `ld_*` values from one row's begin
+ * to the next; sums are fp32, rounded once.  (Rows that begin at multiples of 16 bytes move fastest.)  Buffers of one call
+ * must not overlap.
+ * ------------------------------------------------------------------------------------------------------- */
+#define HL_F32  0
+#define HL_BF16 1
+#define HL_F16  2
+
+#define HL_MAX_EXPERTS 1024
+#define HL_MAX_TOP_K   64
+
+/* Where every token's rows are among the experts'.  Choice a = t * top_k + k is token t's k-th.  max_tokens * top_k < 2^30. */
+typedef struct {
+    const int32_t* n_tokens;         /* device: how many tokens there are, at most max_tokens (NULL: max_tokens).  What
+                                        belongs to the tokens behind them is neither read nor written by any call      */
+    int64_t        max_tokens;
+    int32_t        top_k;            /* 1 .. HL_MAX_TOP_K                                                               */
+    int32_t        n_experts;        /* 1 .. HL_MAX_EXPERTS                                                             */
+    int32_t        align;            /* an expert's rows are filled up to a multiple of this (1 .. 65536), for products
+                                        that work on tiles of rows                                                     */
+    int64_t        cap_rows;         /* rows of the expert-ordered buffers; max_tokens * top_k + min(n_experts, max_tokens
+                                        * top_k) * (align - 1) are always enough                                       */
+    int32_t*       place;            /* device [max_tokens * top_k]: the row of every choice, -1: none                  */
+    int32_t*       source;           /* device [cap_rows] or NULL: the choice in every row, -1 in the rows that fill an
+                                        expert up; rows behind the last expert's are left as they were                 */
+    int32_t*       counts;           /* device [n_experts]: choices of every expert that have a row                     */
+    int32_t*       offsets;          /* device [n_experts + 1]: where every expert's rows begin                         */
+} hl_route;
+
+/* Bytes of device workspace hl_expert_sort needs.  0 on invalid arguments. */
+HL_API size_t hl_expert_workspace_bytes(int64_t max_tokens, int32_t top_k, int32_t n_experts);
+
+/* Fills route->place, source, counts and offsets from the router's choices d_experts [max_tokens, top_k] (expert ids; -1:
+ * none).  An expert's rows hold its choices in ascending order, after those of the experts before it; expert_cap > 0: its
+ * first expert_cap choices, the others get no row.  d_status (device, may be NULL) receives HL_OK, HL_EBOUNDS if an id was
+ * none of -1 .. n_experts - 1 (it counts as -1), or HL_ECAPACITY if cap_rows was too small (choices that would lie behind
+ * it get no row).  The workspace (256-byte aligned) holds nothing between calls; two calls in flight need one each. */
+HL_API int32_t hl_expert_sort(const hl_route* route, const int32_t* d_experts, int64_t expert_cap, int32_t* d_status,
+                              void* d_workspace, size_t ws_bytes, void* stream);
+
+/* y[place[t, k], :] = x[t, :]; rows that fill an expert up become zeros, rows behind the last expert's are left alone.
+ * The gradient of x is hl_expert_combine of y's gradient without weights. */
+HL_API int32_t hl_expert_dispatch(const hl_route* route, int32_t dtype, int64_t dim, const void* d_x, int64_t ld_x,
+                                  void* d_y, int64_t ld_y, void* stream);
+
+/* out[t, :] = sum over k of weights[t, k] * y[place[t, k], :], in the order of k; a choice without a row adds nothing,
+ * whatever its weight.  d_weights fp32 [max_tokens, top_k], NULL: the plain sum. */
+HL_API int32_t hl_expert_combine(const hl_route* route, int32_t dtype, int64_t dim, const void* d_y, int64_t ld_y,
+                                 const float* d_weights, void* d_out, int64_t ld_out, void* stream);
+
+/* The gradients of hl_expert_combine: grad_y[place[t, k], :] = weights[t, k] * grad_out[t, :], zeros in the rows that fill
+ * an expert up; grad_weights[t, k] = <grad_out[t, :], y[place[t, k], :]>, 0 for a choice without a row.
+ * d_grad_weights fp32 [max_tokens, top_k] or NULL (d_y is then not read). */
+HL_API int32_t hl_expert_combine_bwd(const hl_route* route, int32_t dtype, int64_t dim, const void* d_grad_out,
+                                     int64_t ld_grad_out, const void* d_y, int64_t ld_y, const float* d_weights,
+                                     void* d_grad_y, int64_t ld_grad_y, float* d_grad_weights, void* stream);
+
+/* One of many gradient tensors: n values at src; hl_grad_clip writes them, scaled, to dst (dst == src: in place, with the
+ * same type; NULL: nowhere). */
+typedef struct {
+    const void* src;
+    void*       dst;
+    int64_t     n;
+    int32_t     src_dtype, dst_dtype;
+    int32_t     flags;               /* HL_TENSOR_x */
+    int32_t     reserved;            /* 0 */
+} hl_tensor;
+#define HL_TENSOR_NOT_IN_NORM 1      /* scaled, but not part of the norm (its share is given otherwise: d_further) */
+
+/* Bytes of device workspace the next two calls need (256-byte aligned; it holds nothing between calls, and two calls in
+ * flight need one each). */
+HL_API size_t hl_grad_workspace_bytes(void);
+
+/* *d_norm = sqrt(sum of the squares of all values of the tensors + d_further[0] + ... + d_further[n_further - 1]), in fp64,
+ * rounded once.  `tensors` is a HOST array of n_tensors (read during the call), d_further a device array (may be NULL). */
+HL_API int32_t hl_grad_norm(const hl_tensor* tensors, int32_t n_tensors, const double* d_further, int32_t n_further,
+                            float* d_norm, void* d_workspace, size_t ws_bytes, void* stream);
+
+/* hl_grad_norm, and every tensor scaled by min(1, max_norm / (norm + 1e-6)): dst = factor * src (fp32, rounded once to dst's
+ * type).  Tensors in place keep their bits when the factor is 1.  A norm that is infinite makes the factor 0, one that is
+ * NaN makes it NaN; *d_norm (may be NULL) shows both. */
+HL_API int32_t hl_grad_clip(const hl_tensor* tensors, int32_t n_tensors, const double* d_further, int32_t n_further,
+                            float max_norm, float* d_norm, void* d_workspace, size_t ws_bytes, void* stream);
+
+/* *d_sumsq = sum over the distinct slots u of |G_u|^2, with G_u the row gradients that hl_embbag_bwd_apply applies: the sum
+ * of d_grad_out's rows over the lookups of u.  d_sorted_slots, d_sorted_bags and *d_n_lookups as made by
+ * hl_embbag_bwd_prepare, or by hl_embbag_bwd_prepare_merged (with d_n_lookups + 2); skipped lookups add nothing.  With it as
+ * one of d_further, hl_grad_clip clips by the norm of the tables' gradients, which is not that of d_grad_out where several
+ * lookups share a row.  Scratch: the backward region (prepare's and apply's). */
+HL_API int32_t hl_embbag_grad_sumsq(hl_ctx* ctx, const int32_t* d_sorted_slots, const int32_t* d_sorted_bags,
+                                    const int32_t* d_n_lookups, const float* d_grad_out, double* d_sumsq, void* stream);
+
 /* No counterpart in the paper: an addition for callers that cannot allocate.
  *
  * Some callers have no way to hand the library a workspace: code that runs where device allocation is forbidden

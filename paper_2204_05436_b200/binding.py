@@ -28,6 +28,8 @@ EXPORTS = (
     "hl_wide_build_remap", "hl_wide_fragment", "hl_wide_index_cold",
     "hl_index_cold_begin", "hl_index_cold_end", "hl_index_cold_verdict",
     "hl_embbag_bwd_prepare_merged", "hl_pipe_set_order", "hl_step", "hl_wide_test_bounded_waits",
+    "hl_expert_workspace_bytes", "hl_expert_sort", "hl_expert_dispatch", "hl_expert_combine", "hl_expert_combine_bwd",
+    "hl_grad_workspace_bytes", "hl_grad_norm", "hl_grad_clip", "hl_embbag_grad_sumsq",
 )
 
 
@@ -72,6 +74,18 @@ class hl_pipe_options(ctypes.Structure):
 class hl_pipe_span(ctypes.Structure):
     _fields_ = [("mini_batch", ctypes.c_int32), ("what", ctypes.c_int32), ("stream", ctypes.c_int32),
                 ("begin_ms", ctypes.c_float), ("end_ms", ctypes.c_float)]
+
+
+class hl_route(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_void_p), ("max_tokens", ctypes.c_int64), ("top_k", ctypes.c_int32),
+                ("n_experts", ctypes.c_int32), ("align", ctypes.c_int32), ("cap_rows", ctypes.c_int64),
+                ("place", ctypes.c_void_p), ("source", ctypes.c_void_p), ("counts", ctypes.c_void_p),
+                ("offsets", ctypes.c_void_p)]
+
+
+class hl_tensor(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_int64), ("src_dtype", ctypes.c_int32),
+                ("dst_dtype", ctypes.c_int32), ("flags", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 def _load() -> ctypes.CDLL:
@@ -206,6 +220,25 @@ def _load() -> ctypes.CDLL:
     lib.hl_flush_hot.argtypes = [vp, vp, vp, vp, vp, vp]
     lib.hl_embbag_bwd_sgd_static.restype = i32
     lib.hl_embbag_bwd_sgd_static.argtypes = [vp, i64, i32, vp, vp, i32, i64, vp, ctypes.c_float, vp, vp]
+    rt, f32, sz = ctypes.POINTER(hl_route), ctypes.c_float, ctypes.c_size_t
+    lib.hl_expert_workspace_bytes.restype = sz
+    lib.hl_expert_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.hl_expert_sort.restype = i32
+    lib.hl_expert_sort.argtypes = [rt, vp, i64, vp, vp, sz, vp]
+    lib.hl_expert_dispatch.restype = i32
+    lib.hl_expert_dispatch.argtypes = [rt, i32, i64, vp, i64, vp, i64, vp]
+    lib.hl_expert_combine.restype = i32
+    lib.hl_expert_combine.argtypes = [rt, i32, i64, vp, i64, vp, vp, i64, vp]
+    lib.hl_expert_combine_bwd.restype = i32
+    lib.hl_expert_combine_bwd.argtypes = [rt, i32, i64, vp, i64, vp, i64, vp, vp, i64, vp, vp]
+    lib.hl_grad_workspace_bytes.restype = sz
+    lib.hl_grad_workspace_bytes.argtypes = []
+    lib.hl_grad_norm.restype = i32
+    lib.hl_grad_norm.argtypes = [ctypes.POINTER(hl_tensor), i32, vp, i32, vp, vp, sz, vp]
+    lib.hl_grad_clip.restype = i32
+    lib.hl_grad_clip.argtypes = [ctypes.POINTER(hl_tensor), i32, vp, i32, f32, vp, vp, sz, vp]
+    lib.hl_embbag_grad_sumsq.restype = i32
+    lib.hl_embbag_grad_sumsq.argtypes = [vp, vp, vp, vp, vp, vp, vp]
     return lib
 
 
@@ -668,3 +701,90 @@ def hl_embbag_bwd_prepare_merged(ctx: int, pop: hl_ubatch, d_n_pop, non: hl_ubat
 
 def hl_pipe_set_order(pipe: int, order: int) -> None:
     _check("hl_pipe_set_order", _lib.hl_pipe_set_order(pipe, int(order)))
+
+
+# ---- between the pooled rows and their gradients: experts, gradient norms ------------------------------------------------
+HL_F32, HL_BF16, HL_F16 = 0, 1, 2
+HL_MAX_EXPERTS, HL_MAX_TOP_K = 1024, 64
+HL_TENSOR_NOT_IN_NORM = 1
+
+
+def dtype_of(tensor) -> int:
+    """HL_F32, HL_BF16 or HL_F16 of a torch tensor; a TypeError for any other type."""
+    kind = str(tensor.dtype)
+    try:
+        return {"torch.float32": HL_F32, "torch.bfloat16": HL_BF16, "torch.float16": HL_F16}[kind]
+    except KeyError:
+        raise TypeError(f"rows and gradients are float32, bfloat16 or float16, not {kind}") from None
+
+
+def make_route(max_tokens: int, n_tokens, top_k: int, n_experts: int, align: int, cap_rows: int, place, source, counts,
+               offsets) -> hl_route:
+    return hl_route(_ptr(n_tokens), int(max_tokens), int(top_k), int(n_experts), int(align), int(cap_rows), _ptr(place),
+                    _ptr(source), _ptr(counts), _ptr(offsets))
+
+
+def make_tensors(pairs):
+    """The list that hl_grad_norm and hl_grad_clip take, from (src, dst) or (src, dst, flags) of contiguous torch tensors;
+    dst may be None, or src itself (in place).  It keeps their addresses, not the tensors."""
+    arr = (hl_tensor * len(pairs))()
+    for i, pair in enumerate(pairs):
+        src, dst, flags = pair if len(pair) == 3 else (*pair, 0)
+        if not src.is_contiguous() or (dst is not None and (not dst.is_contiguous() or dst.numel() != src.numel())):
+            raise ValueError("gradient tensors are contiguous, and dst has as many values as src")
+        if dst is not None and dst.device != src.device:
+            raise ValueError("src and dst are on one device")
+        arr[i] = hl_tensor(_ptr(src), _ptr(dst), src.numel(), dtype_of(src), dtype_of(src if dst is None else dst),
+                           int(flags), 0)
+    return arr
+
+
+def hl_expert_workspace_bytes(max_tokens: int, top_k: int, n_experts: int) -> int:
+    n = _lib.hl_expert_workspace_bytes(int(max_tokens), int(top_k), int(n_experts))
+    if n == 0:
+        raise HotlineError("hl_expert_workspace_bytes", HL_EINVAL)
+    return int(n)
+
+
+def hl_expert_sort(route: hl_route, d_experts, expert_cap: int, d_status, d_workspace, ws_bytes: int, stream: int) -> None:
+    _check("hl_expert_sort", _lib.hl_expert_sort(route, _ptr(d_experts), expert_cap, _ptr(d_status), _ptr(d_workspace),
+                                                 ws_bytes, stream))
+
+
+def hl_expert_dispatch(route: hl_route, dtype: int, dim: int, d_x, ld_x: int, d_y, ld_y: int, stream: int) -> None:
+    _check("hl_expert_dispatch", _lib.hl_expert_dispatch(route, dtype, dim, _ptr(d_x), ld_x, _ptr(d_y), ld_y, stream))
+
+
+def hl_expert_combine(route: hl_route, dtype: int, dim: int, d_y, ld_y: int, d_weights, d_out, ld_out: int,
+                      stream: int) -> None:
+    _check("hl_expert_combine", _lib.hl_expert_combine(route, dtype, dim, _ptr(d_y), ld_y, _ptr(d_weights), _ptr(d_out),
+                                                       ld_out, stream))
+
+
+def hl_expert_combine_bwd(route: hl_route, dtype: int, dim: int, d_grad_out, ld_grad_out: int, d_y, ld_y: int, d_weights,
+                          d_grad_y, ld_grad_y: int, d_grad_weights, stream: int) -> None:
+    _check("hl_expert_combine_bwd", _lib.hl_expert_combine_bwd(
+        route, dtype, dim, _ptr(d_grad_out), ld_grad_out, _ptr(d_y), ld_y, _ptr(d_weights), _ptr(d_grad_y), ld_grad_y,
+        _ptr(d_grad_weights), stream))
+
+
+def hl_grad_workspace_bytes() -> int:
+    return int(_lib.hl_grad_workspace_bytes())
+
+
+def hl_grad_norm(tensors, d_further, n_further: int, d_norm, d_workspace, ws_bytes: int, stream: int) -> None:
+    """``tensors``: from make_tensors."""
+    _check("hl_grad_norm", _lib.hl_grad_norm(tensors, len(tensors), _ptr(d_further), n_further, _ptr(d_norm),
+                                             _ptr(d_workspace), ws_bytes, stream))
+
+
+def hl_grad_clip(tensors, d_further, n_further: int, max_norm: float, d_norm, d_workspace, ws_bytes: int,
+                 stream: int) -> None:
+    """``tensors``: from make_tensors."""
+    _check("hl_grad_clip", _lib.hl_grad_clip(tensors, len(tensors), _ptr(d_further), n_further, max_norm, _ptr(d_norm),
+                                             _ptr(d_workspace), ws_bytes, stream))
+
+
+def hl_embbag_grad_sumsq(ctx: int, d_sorted_slots, d_sorted_bags, d_n_lookups, d_grad_out, d_sumsq, stream: int) -> None:
+    _check("hl_embbag_grad_sumsq", _lib.hl_embbag_grad_sumsq(ctx, _ptr(d_sorted_slots), _ptr(d_sorted_bags),
+                                                             _ptr(d_n_lookups), _ptr(d_grad_out), _ptr(d_sumsq), stream))

@@ -204,7 +204,7 @@ cudaError_t launch_kernel(const void* func, dim3 grid, dim3 block, size_t smem, 
                           const uint32_t* sizes, int n_args, cudaStream_t stream);
 
 template <typename... P, typename... A>
-cudaError_t launch_cluster(void (*kernel)(P...), int64_t grid, int block, size_t smem, int cluster, cudaStream_t stream,
+cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int block, size_t smem, int cluster, cudaStream_t stream,
                            A&&... a) {
     static_assert(sizeof...(P) == sizeof...(A), "one argument per parameter");
     // (arguments are compared byte by byte: LaunchCache)
@@ -214,13 +214,13 @@ cudaError_t launch_cluster(void (*kernel)(P...), int64_t grid, int block, size_t
     return std::apply(
         [&](auto&... x) {
             void* ptrs[] = {const_cast<void*>(static_cast<const void*>(&x))...};
-            return launch_kernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)grid), dim3((unsigned)block), smem,
+            return launch_kernel(reinterpret_cast<const void*>(kernel), grid, dim3((unsigned)block), smem,
                                  cluster, ptrs, sizes, (int)sizeof...(P), stream);
         },
         args);
 }
 template <typename... P, typename... A>
-cudaError_t launch(void (*kernel)(P...), int64_t grid, int block, cudaStream_t stream, A&&... a) {
+cudaError_t launch(void (*kernel)(P...), dim3 grid, int block, cudaStream_t stream, A&&... a) {
     return launch_cluster(kernel, grid, block, 0, 0, stream, std::forward<A>(a)...);
 }
 
