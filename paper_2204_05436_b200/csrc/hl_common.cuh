@@ -224,6 +224,17 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, int block, cudaStream_t stre
     return launch_cluster(kernel, grid, block, 0, 0, stream, std::forward<A>(a)...);
 }
 
+// A kernel that is put on its stream while the one before it is still at work: its CTAs come up as that one's make room, and
+// wait_for_last() holds them until it has finished and its results can be read.  The kernel before lets it by let_next_start(),
+// made by all of its CTAs (or by their end).  (In a graph of LaunchBatch it starts behind the other, as any kernel does.)
+constexpr int kAfterLast = -1;
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int block, size_t smem, cudaStream_t stream, A&&... a) {
+    return launch_cluster(kernel, grid, block, smem, kAfterLast, stream, std::forward<A>(a)...);
+}
+__device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // f() with its launches collected in `cache` (nullptr: not)
 template <typename F>
 int32_t as_graph(LaunchCache* cache, F f) {

@@ -12,13 +12,14 @@ namespace hl {
 namespace {
 
 // ---- the sort ---------------------------------------------------------------------------------------------------
-// A stable counting sort of the choices by expert.  A warp takes kItems * 32 consecutive choices, 32 at a time; the choices
-// of one expert among them rank by lane (a match over the warp) behind those the warp has counted before.  Behind that, a
-// choice's row is: rows of the experts before + choices of the expert in CTAs before + in warps before + in the warp.
+// A stable counting sort of the choices by expert.  The choices are dealt out evenly, a run of them to each CTA and of those one
+// to each warp, which takes 32 at a time: the choices of one expert among them rank by lane, behind those the warp has counted
+// before.  A choice's row is: rows of the experts before + choices of the expert in CTAs before + in warps before + in the warp.
 constexpr int kSortNT = 512, kSortWarps = kSortNT / 32, kItems = 16;
-constexpr int kSortChoices = kSortNT * kItems;       // of a CTA
+constexpr int kSortChoices = kSortNT * kItems;       // most of a CTA
 constexpr int kExpertsPerThread = HL_MAX_EXPERTS / kSortNT + 1;
 static_assert(HL_MAX_EXPERTS <= 2 * kSortNT, "place_experts: two experts a thread");
+constexpr uint32_t kNone = 0xffffu;
 
 // what the sort writes, and the words it goes by
 struct SortOut {
@@ -29,7 +30,7 @@ struct SortOut {
 
 __device__ __forceinline__ int live_choices(const int32_t* n_tokens, int max_tokens, int top_k) {
     int t = max_tokens;
-    if (n_tokens) t = min(max(*n_tokens, 0), max_tokens);
+    if (n_tokens) t = min(max(__ldg(n_tokens), 0), max_tokens);
     return t * top_k;
 }
 
@@ -52,43 +53,54 @@ __device__ __forceinline__ SortSmem sort_smem(uint32_t* base, int E) {
 }
 __device__ __forceinline__ int hist_pitch(int E) { return 2 * ((E + 1) / 2); }
 
-// Ranks the CTA's choices [first, first + kSortChoices) below n.  packed[i]: expert (16 bits; 0xffff: none), rank in the warp.
-__device__ __forceinline__ void rank_choices(const SortSmem& s, const int32_t* __restrict__ experts, int64_t first, int64_t n,
-                                             int E, uint32_t packed[kItems]) {
+// The lanes with the same value of `bits` bits, among those that are valid.  (A match over the warp does it in one instruction,
+// which takes the multiprocessor 60 cycles; a ballot a bit takes three: eight bits 24.)
+__device__ __forceinline__ unsigned same_value(unsigned v, bool valid, int bits) {
+    unsigned peers = __ballot_sync(0xffffffffu, valid);
+    for (int b = 0; b < bits; ++b) {
+        const unsigned bit = (v >> b) & 1u;
+        peers &= __ballot_sync(0xffffffffu, bit) ^ (bit - 1u);
+    }
+    return peers;
+}
+
+// Ranks the CTA's choices [first, first + rounds * kSortNT) below n.  packed[i]: expert (16 bits; kNone: none), rank in the warp.
+// s.hist and s.warp_hist as above.
+__device__ __forceinline__ void rank_choices(const SortSmem& s, const int32_t* __restrict__ experts, int64_t first, int rounds,
+                                             int64_t n, int E, uint32_t packed[kItems]) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = hist_pitch(E);
-    for (int i = threadIdx.x; i < kSortWarps * pitch / 2; i += kSortNT) reinterpret_cast<uint32_t*>(s.warp_hist)[i] = 0;
-    if (threadIdx.x == 0) s.hist[E] = 0;
-    const int64_t seg = first + warp * (kItems * 32) + lane;
+    const int64_t seg = first + warp * (rounds * 32) + lane;
     int e[kItems];
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) e[i] = seg + i * 32 < n ? __ldg(&experts[seg + i * 32]) : -1;
+    for (int i = 0; i < kItems; ++i) e[i] = i < rounds && seg + i * 32 < n ? __ldg(&experts[seg + i * 32]) : -1;
+    for (int i = threadIdx.x; i < kSortWarps * pitch / 2; i += kSortNT) reinterpret_cast<uint32_t*>(s.warp_hist)[i] = 0;
+    if (threadIdx.x == 0) s.hist[E] = 0;
     __syncthreads();
+    const int bits = 32 - __clz(E - 1);
     uint16_t* h = s.warp_hist + warp * pitch;
-    int bad = 0;
+    bool bad = false;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
+        packed[i] = kNone << 16;
+        if (i >= rounds) continue;
         const bool ok = e[i] >= 0 && e[i] < E;
-        bad += !ok && e[i] != -1;
-        packed[i] = 0xffff0000u;
-        if (first + warp * (kItems * 32) + i * 32 >= n) continue;            // (the same for the warp)
-        const unsigned peers = __match_any_sync(0xffffffffu, ok ? e[i] : -1);
-        if (ok) {
-            const unsigned mine = __popc(peers & lanemask_lt());
-            const unsigned base = h[e[i]];
-            packed[i] = ((uint32_t)e[i] << 16) | (base + mine);
-        }
+        bad = bad || (!ok && e[i] != -1);
+        const unsigned peers = same_value((unsigned)e[i], ok, bits), below = peers & lanemask_lt();
+        if (ok) packed[i] = ((uint32_t)e[i] << 16) | (h[e[i]] + __popc(below));
         __syncwarp();
-        if (ok && (peers & lanemask_lt()) == 0) h[e[i]] = (uint16_t)((packed[i] & 0xffffu) + __popc(peers));
+        if (ok && below == 0) h[e[i]] = (uint16_t)((packed[i] & 0xffffu) + __popc(peers));
         __syncwarp();
     }
-    if (__any_sync(0xffffffffu, bad != 0) && lane == 0) atomicAdd(&s.hist[E], 1);
+    if (__any_sync(0xffffffffu, bad) && lane == 0) atomicAdd(&s.hist[E], 1);
     __syncthreads();
     for (int x = threadIdx.x; x < E; x += kSortNT) {
-        int sum = 0;
+        int c[kSortWarps], sum = 0;
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) c[w] = s.warp_hist[w * pitch + x];
+#pragma unroll
         for (int w = 0; w < kSortWarps; ++w) {
-            const int c = s.warp_hist[w * pitch + x];
             s.warp_hist[w * pitch + x] = (uint16_t)sum;
-            sum += c;
+            sum += c[w];
         }
         s.hist[x] = sum;
     }
@@ -99,9 +111,7 @@ __device__ __forceinline__ void rank_choices(const SortSmem& s, const int32_t* _
 // *over: rows that did not fit.
 __device__ __forceinline__ void place_experts(const SortSmem& s, int E, const SortOut& o, bool* over) {
     __shared__ int64_t s_warp[kSortWarps];
-    __shared__ int s_over;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (threadIdx.x == 0) s_over = 0;
     int64_t rows[2], sum = 0;
     int cnt[2];
 #pragma unroll
@@ -109,7 +119,7 @@ __device__ __forceinline__ void place_experts(const SortSmem& s, int E, const So
         const int e = 2 * threadIdx.x + k;
         cnt[k] = e < E ? s.count[e] : 0;
         if (o.expert_cap > 0) cnt[k] = min(cnt[k], o.expert_cap);
-        rows[k] = ((int64_t)cnt[k] + o.align - 1) / o.align * o.align;
+        rows[k] = (int64_t)((uint32_t)(cnt[k] + o.align - 1) / (uint32_t)o.align) * o.align;
         sum += rows[k];
     }
     int64_t incl = sum;
@@ -122,37 +132,19 @@ __device__ __forceinline__ void place_experts(const SortSmem& s, int E, const So
     __syncthreads();
     int64_t at = incl - sum;
     for (int w = 0; w < warp; ++w) at += s_warp[w];
+    bool mine = false;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int e = 2 * threadIdx.x + k;
         if (e < E) {
-            if (at + cnt[k] > o.cap_rows) s_over = 1;
+            mine = mine || at + cnt[k] > o.cap_rows;
             s.offset[e] = (int32_t)min(at, o.cap_rows);
             s.count[e] = (int32_t)min((int64_t)cnt[k], max(o.cap_rows - at, (int64_t)0));
             if (e == E - 1) s.offset[E] = (int32_t)min(at + rows[k], o.cap_rows);
         }
         at += rows[k];
     }
-    __syncthreads();
-    *over = s_over != 0;
-}
-
-__device__ __forceinline__ void write_places(const SortSmem& s, const SortOut& o, int64_t first, int64_t n, int E,
-                                             const uint32_t packed[kItems]) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = hist_pitch(E);
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        const int64_t a = first + warp * (kItems * 32) + i * 32 + lane;
-        if (a >= n) continue;
-        const uint32_t e = packed[i] >> 16;
-        int32_t row = -1;
-        if (e != 0xffffu) {
-            const int r = s.hist[e] + s.warp_hist[warp * pitch + e] + (int)(packed[i] & 0xffffu);
-            if (r < s.count[e]) row = s.offset[e] + r;
-        }
-        o.place[a] = row;
-        if (row >= 0 && o.source) o.source[row] = (int32_t)a;
-    }
+    *over = __syncthreads_or(mine) != 0;
 }
 
 // The rows that fill an expert up, and the plan's words, by CTA `cta` of `ctas`.
@@ -172,6 +164,16 @@ __device__ __forceinline__ void write_plan(const SortSmem& s, const SortOut& o, 
     }
 }
 
+__device__ __forceinline__ void write_place(const SortSmem& s, const SortOut& o, int64_t a, uint32_t e, int rank) {
+    int32_t row = -1;
+    if (e != kNone) {
+        const int r = s.hist[e] + rank;
+        if (r < s.count[e]) row = s.offset[e] + r;
+    }
+    o.place[a] = row;
+    if (row >= 0 && o.source) o.source[row] = (int32_t)a;
+}
+
 // All of it in one cluster, whose CTAs read each other's counts.
 template <int CTAS>
 __global__ void __launch_bounds__(kSortNT) k_expert_sort(const int32_t* __restrict__ experts, const int32_t* n_tokens,
@@ -181,10 +183,10 @@ __global__ void __launch_bounds__(kSortNT) k_expert_sort(const int32_t* __restri
     extern __shared__ uint32_t s_base[];
     const SortSmem s = sort_smem(s_base, E);
     const SortOut o{place, source, counts, offsets, status, cap_rows, expert_cap, align};
-    const int64_t n = live_choices(n_tokens, max_tokens, top_k), first = (int64_t)blockIdx.x * kSortChoices;
+    const int n = live_choices(n_tokens, max_tokens, top_k), rounds = (n + CTAS * kSortNT - 1) / (CTAS * kSortNT);
+    const int first = (int)blockIdx.x * rounds * kSortNT;
     uint32_t packed[kItems];
-    rank_choices(s, experts, first, n, E, packed);
-    int bad = 0;
+    rank_choices(s, experts, first, rounds, n, E, packed);
     if constexpr (CTAS > 1) {
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
@@ -193,12 +195,13 @@ __global__ void __launch_bounds__(kSortNT) k_expert_sort(const int32_t* __restri
         for (int k = 0; k < kExpertsPerThread; ++k) {
             const int e = threadIdx.x + k * kSortNT;
             if (e > E) break;
-            int all = 0;
+            int v[CTAS], all = 0;
+#pragma unroll
+            for (int c = 0; c < CTAS; ++c) v[c] = *cluster.map_shared_rank(&s.hist[e], c);
 #pragma unroll
             for (int c = 0; c < CTAS; ++c) {
-                const int v = *cluster.map_shared_rank(&s.hist[e], c);
-                if (c < (int)blockIdx.x) before[k] += v;
-                all += v;
+                if (c < (int)blockIdx.x) before[k] += v[c];
+                all += v[c];
             }
             s.count[e] = all;
         }
@@ -215,67 +218,99 @@ __global__ void __launch_bounds__(kSortNT) k_expert_sort(const int32_t* __restri
         }
     }
     __syncthreads();
-    bad = s.count[E];
+    const bool bad = s.count[E] != 0;
     bool over;
     place_experts(s, E, o, &over);
-    write_places(s, o, first, n, E, packed);
-    write_plan(s, o, E, blockIdx.x, CTAS, over, bad != 0);
-}
-
-// In three kernels: every tile's counts, sums of them over the tiles before, places.
-__global__ void __launch_bounds__(kSortNT) k_expert_count(const int32_t* __restrict__ experts, const int32_t* n_tokens,
-                                                          int max_tokens, int top_k, int E, int32_t* __restrict__ tile_counts) {
-    extern __shared__ uint32_t s_base[];
-    const SortSmem s = sort_smem(s_base, E);
-    const int64_t n = live_choices(n_tokens, max_tokens, top_k), first = (int64_t)blockIdx.x * kSortChoices;
-    uint32_t packed[kItems];
-    rank_choices(s, experts, first, n, E, packed);
-    for (int e = threadIdx.x; e <= E; e += kSortNT) tile_counts[(int64_t)blockIdx.x * (E + 1) + e] = s.hist[e];
-}
-
-// tile_counts[t][e] := sum over the tiles before t; totals[e].  A CTA takes 32 experts, its warps a run of tiles each.
-__global__ void __launch_bounds__(1024) k_expert_scan(int32_t* __restrict__ tile_counts, int64_t n_tiles, int E,
-                                                      int32_t* __restrict__ totals) {
-    __shared__ int32_t s_sum[32][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
-    const int64_t per = (n_tiles + 31) / 32, t0 = warp * per, t1 = min(t0 + per, n_tiles);
-    int sum = 0;
-    if (e <= E)
-        for (int64_t t = t0; t < t1; ++t) sum += tile_counts[t * (E + 1) + e];
-    s_sum[warp][lane] = sum;
-    __syncthreads();
-    if (e > E) return;
-    int before = 0;
-    for (int w = 0; w < warp; ++w) before += s_sum[w][lane];
-    for (int64_t t = t0; t < t1; ++t) {
-        const int c = tile_counts[t * (E + 1) + e];
-        tile_counts[t * (E + 1) + e] = before;
-        before += c;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        const int a = first + (warp * rounds + i) * 32 + lane;
+        const uint32_t e = packed[i] >> 16;
+        if (i < rounds && a < n)
+            write_place(s, o, a, e, (int)(packed[i] & 0xffffu) + (e == kNone ? 0 : s.warp_hist[warp * hist_pitch(E) + e]));
     }
-    if (warp == 31) totals[e] = before;
+    write_plan(s, o, E, blockIdx.x, CTAS, over, bad);
 }
 
-__global__ void __launch_bounds__(kSortNT) k_expert_place(const int32_t* __restrict__ experts, const int32_t* n_tokens,
-                                                          int max_tokens, int top_k, int E, int expert_cap, int align,
-                                                          int64_t cap_rows, int32_t* place, int32_t* source, int32_t* counts,
-                                                          int32_t* offsets, int32_t* status,
-                                                          const int32_t* __restrict__ tile_counts,
-                                                          const int32_t* __restrict__ totals) {
+// In three kernels: every tile's choices ranked (their expert and rank in the tile, as packed above, into `ranked`) and
+// counted, sums of the counts over the tiles before, places.  tile_counts: [E + 1][tiles].
+__global__ void __launch_bounds__(kSortNT) k_expert_rank(const int32_t* __restrict__ experts, const int32_t* n_tokens,
+                                                         int max_tokens, int top_k, int E, int32_t* __restrict__ tile_counts,
+                                                         uint32_t* __restrict__ ranked) {
+    extern __shared__ uint32_t s_base[];
+    let_next_start();
+    const SortSmem s = sort_smem(s_base, E);
+    const int n = live_choices(n_tokens, max_tokens, top_k), tiles = gridDim.x;
+    const int rounds = (int)(((int64_t)n + (int64_t)tiles * kSortNT - 1) / ((int64_t)tiles * kSortNT));
+    const int64_t first = (int64_t)blockIdx.x * rounds * kSortNT;
+    uint32_t packed[kItems];
+    rank_choices(s, experts, first, rounds, n, E, packed);
+    for (int e = threadIdx.x; e <= E; e += kSortNT) tile_counts[(int64_t)e * tiles + blockIdx.x] = s.hist[e];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        const int64_t a = first + (warp * rounds + i) * 32 + lane;
+        const uint32_t e = packed[i] >> 16;
+        if (i < rounds && a < n) ranked[a] = e == kNone ? packed[i] : packed[i] + s.warp_hist[warp * hist_pitch(E) + e];
+    }
+}
+
+// tile_counts[e][t] := sum over the tiles before t; totals[e].  A warp takes an expert.
+__global__ void __launch_bounds__(256) k_expert_scan(int32_t* __restrict__ tile_counts, int tiles, int E,
+                                                     int32_t* __restrict__ totals) {
+    let_next_start();
+    wait_for_last();
+    const int lane = threadIdx.x & 31, e = (int)(blockIdx.x * 8 + (threadIdx.x >> 5));
+    if (e > E) return;
+    int32_t* row = tile_counts + (int64_t)e * tiles;
+    constexpr int kAhead = 8;
+    int before = 0;
+    for (int t0 = 0; t0 < tiles; t0 += 32 * kAhead) {
+        int c[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) c[i] = t0 + i * 32 + lane < tiles ? row[t0 + i * 32 + lane] : 0;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            int incl = c[i];
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += v;
+            }
+            if (t0 + i * 32 + lane < tiles) row[t0 + i * 32 + lane] = before + incl - c[i];
+            before += __shfl_sync(0xffffffffu, incl, 31);
+        }
+    }
+    if (lane == 0) totals[e] = before;
+}
+
+__global__ void __launch_bounds__(kSortNT) k_expert_place(const int32_t* n_tokens, int max_tokens, int top_k, int E,
+                                                          int expert_cap, int align, int64_t cap_rows, int32_t* place,
+                                                          int32_t* source, int32_t* counts, int32_t* offsets, int32_t* status,
+                                                          const int32_t* tile_counts, const int32_t* totals,
+                                                          const uint32_t* ranked) {
     extern __shared__ uint32_t s_base[];
     const SortSmem s = sort_smem(s_base, E);
     const SortOut o{place, source, counts, offsets, status, cap_rows, expert_cap, align};
-    const int64_t n = live_choices(n_tokens, max_tokens, top_k), first = (int64_t)blockIdx.x * kSortChoices;
+    const int n = live_choices(n_tokens, max_tokens, top_k), tiles = gridDim.x;
+    const int rounds = (int)(((int64_t)n + (int64_t)tiles * kSortNT - 1) / ((int64_t)tiles * kSortNT));
+    const int64_t first = (int64_t)blockIdx.x * rounds * kSortNT + threadIdx.x;
+    wait_for_last();
     uint32_t packed[kItems];
-    rank_choices(s, experts, first, n, E, packed);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) packed[i] = i < rounds && first + i * kSortNT < n ? ranked[first + i * kSortNT] : 0;
     for (int e = threadIdx.x; e <= E; e += kSortNT) {
-        s.hist[e] = tile_counts[(int64_t)blockIdx.x * (E + 1) + e];
+        s.hist[e] = tile_counts[(int64_t)e * tiles + blockIdx.x];
         s.count[e] = totals[e];
     }
     __syncthreads();
     const bool bad = s.count[E] != 0;
     bool over;
     place_experts(s, E, o, &over);
-    write_places(s, o, first, n, E, packed);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+        if (i < rounds && first + i * kSortNT < n)
+            write_place(s, o, first + i * kSortNT, packed[i] >> 16, (int)(packed[i] & 0xffffu));
     write_plan(s, o, E, blockIdx.x, gridDim.x, over, bad);
 }
 
@@ -283,10 +318,17 @@ constexpr int kClusterCtas = 8;
 constexpr int64_t kOneCluster = (int64_t)kClusterCtas * kSortChoices;
 
 // ---- rows -----------------------------------------------------------------------------------------------------------
-// N values of type T, moved as one.
-template <typename T, int N>
-struct alignas(sizeof(T) * N) Vec {
-    T v[N];
+// Values move 16 bytes at a time.  Where every row of a call begins at a multiple of 16 bytes (ANY = false), a vector is one
+// load and one store.  Elsewhere a row that is written is cut where its own 16-byte lines begin, so that all its stores but
+// those at its ends are whole lines, and what belongs there is put together from the two lines it lies in (load_any).
+template <typename T>
+struct Vec {
+    static constexpr int N = 16 / sizeof(T);
+    union {
+        uint4 raw;
+        T v[N];
+    };
+    __device__ Vec() {}
 };
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -300,154 +342,284 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { retu
 template <>
 __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 
-constexpr int kRowNT = 256, kRowWarps = kRowNT / 32;
-
-// Rows that fill experts up: CTA u of n_units x E takes every n_units-th of expert u % E's.
-template <typename V>
-__device__ __forceinline__ void zero_pads(int u, int units, int E, const int32_t* __restrict__ counts,
-                                          const int32_t* __restrict__ offsets, int64_t cap_rows, V* y, int64_t ld, int nv) {
-    const int e = u % E, part = u / E;
-    const int64_t begin = (int64_t)__ldg(&offsets[e]) + __ldg(&counts[e]), end = min((int64_t)__ldg(&offsets[e + 1]), cap_rows);
-    if (__ldg(&offsets[e]) < 0 || __ldg(&counts[e]) < 0) return;
-    for (int64_t r = begin + part; r < end; r += units)
-        for (int c = threadIdx.x; c < nv; c += kRowNT) y[r * ld + c] = V{};
+// rows x dim values, ld from one row's begin to the next
+template <typename T>
+struct Rows {
+    T* p;
+    int64_t ld;
+    __device__ __forceinline__ T* at(int64_t r) const { return p + r * ld; }
+};
+template <typename T>
+__device__ __forceinline__ int in_line(const T* p) {           // values between the 16-byte line's begin and p
+    return (int)(reinterpret_cast<uintptr_t>(p) & 15) / (int)sizeof(T);
 }
 
-// y[place[t, k]] = x[t].  A warp takes 32 * U vectors of a token's row at a time: it reads them once and writes them to the
-// token's rows, so that every row crosses memory once.
-template <typename V, int U>
-__global__ void __launch_bounds__(kRowNT) k_expert_dispatch(const V* __restrict__ x, int64_t ld_x,
-                                                            const int32_t* n_tokens, int max_tokens, int top_k, int nv,
+// 16 bytes from p on, whatever p's alignment, of a buffer [lo, hi); what lies outside of it reads as anything.
+template <typename T>
+__device__ __forceinline__ Vec<T> load_any(const T* p, const T* lo, const T* hi) {
+    Vec<T> r;
+    const int s = (int)(reinterpret_cast<uintptr_t>(p) & 15);
+    const T* line = p - s / (int)sizeof(T);
+    constexpr int N = Vec<T>::N;
+    if (line >= lo && line + (s ? 2 * N : N) <= hi) {
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(line));
+        if (s == 0) {
+            r.raw = a;
+            return r;
+        }
+        const uint4 b = __ldg(reinterpret_cast<const uint4*>(line) + 1);
+        uint32_t w[6] = {a.x, a.y, a.z, a.w, b.x, b.y};
+        uint32_t x[5];
+        const uint32_t far[2] = {b.z, b.w};
+        if (s & 8) {
+            w[0] = a.z, w[1] = a.w, w[2] = b.x, w[3] = b.y, w[4] = far[0], w[5] = far[1];
+        }
+#pragma unroll
+        for (int i = 0; i < 5; ++i) x[i] = s & 4 ? w[i + 1] : w[i];
+        const int bits = (s & 3) * 8;
+        r.raw = make_uint4(__funnelshift_r(x[0], x[1], bits), __funnelshift_r(x[1], x[2], bits),
+                           __funnelshift_r(x[2], x[3], bits), __funnelshift_r(x[3], x[4], bits));
+        return r;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (p + j >= lo && p + j < hi) r.v[j] = p[j];
+    return r;
+}
+
+// values [e, e + N) of a row of dim values, as much of them as there is; row + e is a line's begin
+template <typename T>
+__device__ __forceinline__ void store_line(T* row, int e, int dim, const Vec<T>& v) {
+    constexpr int N = Vec<T>::N;
+    if (e >= 0 && e + N <= dim) {
+        *reinterpret_cast<uint4*>(row + e) = v.raw;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (e + j >= 0 && e + j < dim) row[e + j] = v.v[j];
+}
+
+constexpr int kRowNT = 256;
+
+// Lines that a row of dim values can lie in.
+template <typename T>
+__host__ __device__ constexpr int lines_of(int64_t dim, bool any) {
+    return (int)((dim + (any ? Vec<T>::N - 1 : 0) + Vec<T>::N - 1) / Vec<T>::N);
+}
+
+// Rows that fill experts up: CTA u of units x E takes every units-th of expert u % E's.
+template <typename T>
+__device__ __forceinline__ void zero_pads(int u, int units, int E, const int32_t* __restrict__ counts,
+                                          const int32_t* __restrict__ offsets, int64_t cap_rows, Rows<T> y, int dim) {
+    const int e = u % E, part = u / E;
+    const int64_t first = __ldg(&offsets[e]), count = __ldg(&counts[e]), end = min((int64_t)__ldg(&offsets[e + 1]), cap_rows);
+    if (first < 0 || count < 0) return;
+    Vec<T> zero;
+    zero.raw = make_uint4(0, 0, 0, 0);
+    for (int64_t r = first + count + part; r < end; r += units) {
+        T* row = y.at(r);
+        for (int e0 = -in_line(row) + (int)threadIdx.x * Vec<T>::N; e0 < dim; e0 += kRowNT * Vec<T>::N) store_line(row, e0, dim, zero);
+    }
+}
+
+// Which token and line a thread's item is: items are dealt out in turn, kItemsPerCta to a CTA.
+template <int U>
+struct Items {
+    int64_t t0;
+    unsigned r0;
+    int lines;
+    __device__ __forceinline__ Items(int lines_) : lines(lines_) {
+        const int64_t first = (int64_t)blockIdx.x * (kRowNT * U);
+        t0 = first / lines;
+        r0 = (unsigned)(first - t0 * lines);
+    }
+    __device__ __forceinline__ void get(int u, int64_t* t, int* line) const {
+        const unsigned i = r0 + u * kRowNT + threadIdx.x, q = i / (unsigned)lines;
+        *t = t0 + q;
+        *line = (int)(i - q * lines);
+    }
+};
+
+// y[place[t, k]] = x[t].  A thread takes a line of a token's row, which it reads once for all of the token's rows.
+template <typename T, bool ANY, int U>
+__global__ void __launch_bounds__(kRowNT) k_expert_dispatch(const T* __restrict__ x_, int64_t ld_x, const int32_t* n_tokens,
+                                                            int max_tokens, int top_k, int dim,
                                                             const int32_t* __restrict__ place, int64_t cap_rows,
-                                                            V* __restrict__ y, int64_t ld_y, int row_ctas, int E,
+                                                            T* __restrict__ y_, int64_t ld_y, int lines, int row_ctas, int E,
                                                             int pad_units, const int32_t* __restrict__ counts,
                                                             const int32_t* __restrict__ offsets) {
+    constexpr int N = Vec<T>::N, KU = 4;
+    const Rows<const T> x{x_, ld_x};
+    const Rows<T> y{y_, ld_y};
     if ((int)blockIdx.x >= row_ctas) {
-        zero_pads(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, y, ld_y, nv);
+        zero_pads(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, y, dim);
         return;
     }
-    const int lane = threadIdx.x & 31;
-    const int tokens = live_choices(n_tokens, max_tokens, 1), blocks = (nv + 32 * U - 1) / (32 * U);
-    const int64_t items = (int64_t)tokens * blocks;
-    for (int64_t i = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5); i < items; i += (int64_t)row_ctas * kRowWarps) {
-        const int64_t t = i / blocks;
-        const int c0 = (int)(i - t * blocks) * 32 * U + lane;
-        V v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (c0 + u * 32 < nv) v[u] = x[t * ld_x + c0 + u * 32];
-        for (int k = 0; k < top_k; ++k) {
-            const int64_t row = __ldg(&place[t * top_k + k]);
-            if (row < 0 || row >= cap_rows) continue;
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (c0 + u * 32 < nv) y[row * ld_y + c0 + u * 32] = v[u];
-        }
-    }
-}
-
-// out[t] = sum over k of w[t, k] * y[place[t, k]], in fp32, in the order of k, rounded once.  (Without weights: the sum.)
-template <typename T, int N, int U>
-__global__ void __launch_bounds__(kRowNT) k_expert_combine(const Vec<T, N>* __restrict__ y, int64_t ld_y, int64_t cap_rows,
-                                                           const int32_t* n_tokens, int max_tokens, int top_k, int nv,
-                                                           const int32_t* __restrict__ place,
-                                                           const float* __restrict__ weights, Vec<T, N>* __restrict__ out,
-                                                           int64_t ld_out) {
-    const int lane = threadIdx.x & 31;
-    const int tokens = live_choices(n_tokens, max_tokens, 1), blocks = (nv + 32 * U - 1) / (32 * U);
-    const int64_t items = (int64_t)tokens * blocks;
-    for (int64_t i = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5); i < items; i += (int64_t)gridDim.x * kRowWarps) {
-        const int64_t t = i / blocks;
-        const int c0 = (int)(i - t * blocks) * 32 * U + lane;
-        float acc[U][N] = {};
-        for (int k = 0; k < top_k; ++k) {
-            const int64_t row = __ldg(&place[t * top_k + k]);
-            if (row < 0 || row >= cap_rows) continue;
-            const float w = weights ? __ldg(&weights[t * top_k + k]) : 1.f;
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (c0 + u * 32 >= nv) continue;
-                const Vec<T, N> v = y[row * ld_y + c0 + u * 32];
-#pragma unroll
-                for (int j = 0; j < N; ++j) acc[u][j] = fmaf(w, to_f32(v.v[j]), acc[u][j]);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (c0 + u * 32 >= nv) continue;
-            Vec<T, N> v;
-#pragma unroll
-            for (int j = 0; j < N; ++j) v.v[j] = from_f32<T>(acc[u][j]);
-            out[t * ld_out + c0 + u * 32] = v;
-        }
-    }
-}
-
-// grad_y[place[t, k]] = w[t, k] * grad_out[t]; grad_w[t, k] = <grad_out[t], y[place[t, k]]>.  W warps of a CTA take a token:
-// 32 * U vectors each at a time, which stay in registers for all of the token's rows.
-template <typename T, int N, int U>
-__global__ void __launch_bounds__(kRowNT) k_expert_combine_bwd(
-    const Vec<T, N>* __restrict__ grad_out, int64_t ld_go, const Vec<T, N>* __restrict__ y, int64_t ld_y, int64_t cap_rows,
-    const int32_t* n_tokens, int max_tokens, int top_k, int nv, const int32_t* __restrict__ place,
-    const float* __restrict__ weights, Vec<T, N>* __restrict__ grad_y, int64_t ld_gy, float* __restrict__ grad_w, int W,
-    int row_ctas, int E, int pad_units, const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets) {
-    if ((int)blockIdx.x >= row_ctas) {
-        zero_pads(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, grad_y, ld_gy, nv);
-        return;
-    }
-    __shared__ float s_dot[kRowWarps][HL_MAX_TOP_K];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % W, per_cta = kRowWarps / W;
     const int tokens = live_choices(n_tokens, max_tokens, 1);
-    for (int64_t t0 = (int64_t)blockIdx.x * per_cta; t0 < tokens; t0 += (int64_t)row_ctas * per_cta) {
-        const int64_t t = t0 + warp / W;
-        if (t < tokens) {
-            if (grad_w)
-                for (int k = lane; k < top_k; k += 32) s_dot[warp][k] = 0.f;
-            __syncwarp();
-            for (int c0 = part * 32 * U + lane; c0 - lane < nv; c0 += W * 32 * U) {
-                Vec<T, N> g[U];
+    const T* end = x.at((int64_t)max_tokens - 1) + dim;
+    const Items<U> items(lines);
+    Vec<T> v[U];
+    int64_t t[U];
+    int line[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) g[u] = c0 + u * 32 < nv ? grad_out[t * ld_go + c0 + u * 32] : Vec<T, N>{};
-                for (int k = 0; k < top_k; ++k) {
-                    const int64_t row = __ldg(&place[t * top_k + k]);
-                    if (row < 0 || row >= cap_rows) continue;
-                    const float w = weights ? __ldg(&weights[t * top_k + k]) : 1.f;
-                    float dot = 0.f;
-                    if (grad_w) {
-                        Vec<T, N> v[U];
+    for (int u = 0; u < U; ++u) {
+        items.get(u, &t[u], &line[u]);
+        if constexpr (!ANY)
+            if (t[u] < tokens) v[u].raw = __ldg(reinterpret_cast<const uint4*>(x.at(t[u]) + line[u] * N));
+    }
 #pragma unroll
-                        for (int u = 0; u < U; ++u) v[u] = c0 + u * 32 < nv ? y[row * ld_y + c0 + u * 32] : Vec<T, N>{};
+    for (int u = 0; u < U; ++u) {
+        if (t[u] >= tokens) continue;
+        for (int k0 = 0; k0 < top_k; k0 += KU) {
+            int64_t row[KU];
 #pragma unroll
-                        for (int u = 0; u < U; ++u)
+            for (int q = 0; q < KU; ++q) row[q] = k0 + q < top_k ? __ldg(&place[t[u] * top_k + k0 + q]) : -1;
 #pragma unroll
-                            for (int j = 0; j < N; ++j) dot = fmaf(to_f32(g[u].v[j]), to_f32(v[u].v[j]), dot);
-                    }
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        if (c0 + u * 32 >= nv) continue;
-                        Vec<T, N> r;
-#pragma unroll
-                        for (int j = 0; j < N; ++j) r.v[j] = from_f32<T>(w * to_f32(g[u].v[j]));
-                        grad_y[row * ld_gy + c0 + u * 32] = r;
-                    }
-                    if (grad_w) {
-#pragma unroll
-                        for (int d = 16; d > 0; d >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, d);
-                        if (lane == 0) s_dot[warp][k] += dot;
-                    }
+            for (int q = 0; q < KU; ++q) {
+                if (row[q] < 0 || row[q] >= cap_rows) continue;
+                T* to = y.at(row[q]);
+                if constexpr (!ANY) {
+                    *reinterpret_cast<uint4*>(to + line[u] * N) = v[u].raw;
+                } else {
+                    const int e = line[u] * N - in_line(to);
+                    if (e < dim) store_line(to, e, dim, load_any(x.at(t[u]) + e, x_, end));
                 }
             }
         }
-        if (!grad_w) continue;
-        __syncthreads();
-        for (int i = threadIdx.x; i < per_cta * top_k; i += kRowNT) {
-            const int j = i / top_k, k = i - j * top_k;
-            if (t0 + j >= tokens) continue;
-            float dot = 0.f;
-            for (int p = 0; p < W; ++p) dot += s_dot[j * W + p][k];
-            grad_w[(t0 + j) * top_k + k] = dot;
+    }
+}
+
+// out[t] = sum over k of w[t, k] * y[place[t, k]], in fp32, in the order of k, rounded once.  (Without weights: the sum.)  A
+// thread takes a line of out, and KU of the token's rows at a time.
+template <typename T, bool ANY, int KU, int U>
+__global__ void __launch_bounds__(kRowNT) k_expert_combine(const T* __restrict__ y_, int64_t ld_y, int64_t cap_rows,
+                                                           const int32_t* n_tokens, int max_tokens, int top_k, int dim,
+                                                           const int32_t* __restrict__ place,
+                                                           const float* __restrict__ weights, T* __restrict__ out_,
+                                                           int64_t ld_out, int lines) {
+    constexpr int N = Vec<T>::N;
+    const Rows<const T> y{y_, ld_y};
+    const Rows<T> out{out_, ld_out};
+    const int tokens = live_choices(n_tokens, max_tokens, 1);
+    const T* end = y.at(cap_rows - 1) + dim;
+    const Items<U> items(lines);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        int64_t t;
+        int line;
+        items.get(u, &t, &line);
+        if (t >= tokens) continue;
+        T* to = out.at(t);
+        const int e = line * N - (ANY ? in_line(to) : 0);
+        if (ANY && e >= dim) continue;
+        float acc[N] = {};
+        for (int k0 = 0; k0 < top_k; k0 += KU) {
+            Vec<T> v[KU];
+            float w[KU];
+#pragma unroll
+            for (int q = 0; q < KU; ++q) {
+                const int64_t row = k0 + q < top_k ? __ldg(&place[t * top_k + k0 + q]) : -1;
+                const bool ok = row >= 0 && row < cap_rows;
+                w[q] = ok ? (weights ? __ldg(&weights[t * top_k + k0 + q]) : 1.f) : 0.f;
+                v[q].raw = make_uint4(0, 0, 0, 0);
+                if (!ok) continue;
+                if constexpr (ANY) v[q] = load_any(y.at(row) + e, y_, end);
+                else v[q].raw = __ldg(reinterpret_cast<const uint4*>(y.at(row) + e));
+            }
+#pragma unroll
+            for (int q = 0; q < KU; ++q)
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[j] = fmaf(w[q], to_f32(v[q].v[j]), acc[j]);
         }
-        __syncthreads();
+        Vec<T> r;
+#pragma unroll
+        for (int j = 0; j < N; ++j) r.v[j] = from_f32<T>(acc[j]);
+        if constexpr (ANY) store_line(to, e, dim, r);
+        else *reinterpret_cast<uint4*>(to + e) = r.raw;
+    }
+}
+
+// grad_y[place[t, k]] = w[t, k] * grad_out[t]; grad_w[t, k] = <grad_out[t], y[place[t, k]]>.  P threads (a power of two) take a
+// token, KU of its rows at a time.
+template <typename T, bool ANY>
+__global__ void __launch_bounds__(kRowNT) k_expert_combine_bwd(
+    const T* __restrict__ go_, int64_t ld_go, const T* __restrict__ y_, int64_t ld_y, int64_t cap_rows, const int32_t* n_tokens,
+    int max_tokens, int top_k, int dim, const int32_t* __restrict__ place, const float* __restrict__ weights,
+    T* __restrict__ gy_, int64_t ld_gy, float* __restrict__ grad_w, int P, int lines, int row_ctas, int E, int pad_units,
+    const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets) {
+    constexpr int N = Vec<T>::N, KU = 4;
+    const Rows<const T> go{go_, ld_go}, y{y_, ld_y};
+    const Rows<T> gy{gy_, ld_gy};
+    if ((int)blockIdx.x >= row_ctas) {
+        zero_pads(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, gy, dim);
+        return;
+    }
+    __shared__ float s_dot[kRowNT / 32][KU];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = threadIdx.x & (P - 1);
+    const int tokens = live_choices(n_tokens, max_tokens, 1);
+    const int64_t t = (int64_t)blockIdx.x * (kRowNT / P) + threadIdx.x / P;
+    const T *go_end = go.at((int64_t)max_tokens - 1) + dim, *y_end = y.at(cap_rows - 1) + dim;
+    for (int k0 = 0; k0 < top_k; k0 += KU) {
+        int64_t row[KU];
+        float w[KU], dot[KU];
+#pragma unroll
+        for (int q = 0; q < KU; ++q) {
+            row[q] = t < tokens && k0 + q < top_k ? __ldg(&place[t * top_k + k0 + q]) : -1;
+            if (row[q] >= cap_rows) row[q] = -1;
+            w[q] = row[q] >= 0 && weights ? __ldg(&weights[t * top_k + k0 + q]) : 1.f;
+            dot[q] = 0.f;
+        }
+        for (int l = sub; l < lines; l += P) {
+            if (t >= tokens) break;
+            Vec<T> g, v[KU];
+            if constexpr (!ANY) g.raw = __ldg(reinterpret_cast<const uint4*>(go.at(t) + l * N));
+            int e[KU];
+#pragma unroll
+            for (int q = 0; q < KU; ++q) {
+                v[q].raw = make_uint4(0, 0, 0, 0);
+                if (row[q] < 0) continue;
+                e[q] = l * N - (ANY ? in_line(gy.at(row[q])) : 0);
+                if (ANY && e[q] >= dim) continue;
+                if (!grad_w) continue;
+                if constexpr (ANY) v[q] = load_any(y.at(row[q]) + e[q], y_, y_end);
+                else v[q].raw = __ldg(reinterpret_cast<const uint4*>(y.at(row[q]) + e[q]));
+            }
+#pragma unroll
+            for (int q = 0; q < KU; ++q) {
+                if (row[q] < 0 || (ANY && e[q] >= dim)) continue;
+                if constexpr (ANY) g = load_any(go.at(t) + e[q], go_, go_end);
+                Vec<T> r;
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float x = to_f32(g.v[j]);
+                    if (!ANY || (e[q] + j >= 0 && e[q] + j < dim)) dot[q] = fmaf(x, to_f32(v[q].v[j]), dot[q]);
+                    r.v[j] = from_f32<T>(w[q] * x);
+                }
+                if constexpr (ANY) store_line(gy.at(row[q]), e[q], dim, r);
+                else *reinterpret_cast<uint4*>(gy.at(row[q]) + e[q]) = r.raw;
+            }
+        }
+        if (!grad_w) continue;
+        const int in_warp = min(P, 32);
+        for (int d = in_warp / 2; d > 0; d >>= 1)
+#pragma unroll
+            for (int q = 0; q < KU; ++q) dot[q] += __shfl_xor_sync(0xffffffffu, dot[q], d);
+        if (P > 32) {
+            if (lane == 0)
+#pragma unroll
+                for (int q = 0; q < KU; ++q) s_dot[warp][q] = dot[q];
+            __syncthreads();
+            if (sub == 0)
+                for (int o = 1; o < P / 32; ++o)
+#pragma unroll
+                    for (int q = 0; q < KU; ++q) dot[q] += s_dot[warp + o][q];
+            __syncthreads();
+        }
+        if (sub == 0 && t < tokens)
+#pragma unroll
+            for (int q = 0; q < KU; ++q)
+                if (k0 + q < top_k) grad_w[t * top_k + k0 + q] = dot[q];
     }
 }
 
@@ -492,51 +664,56 @@ int pad_units(const hl_route* r) {
     return (int)(u < r->align - 1 ? u : r->align - 1);
 }
 
-template <typename V, int U>
-int32_t launch_dispatch(const hl_route* r, int64_t dim, const void* x, int64_t ld_x, void* y, int64_t ld_y, int size,
-                        cudaStream_t stream) {
-    const int per = sizeof(V) / size, nv = (int)(dim / per), units = pad_units(r);
-    const int ctas = r->max_tokens ? grid_for(r->max_tokens * div_up(nv, 32 * U), kRowWarps, 1 << 20) : 0;
+// Tiles of at most kSortChoices choices: as many CTAs as fill whole rounds of the chip.
+int64_t sort_tiles(int64_t n) { return div_up(div_up(n > 0 ? n : 1, kSortChoices), kSMsFallback) * kSMsFallback; }
+
+template <typename T, bool ANY>
+int32_t launch_dispatch(const hl_route* r, int64_t dim, const void* x, int64_t ld_x, void* y, int64_t ld_y, cudaStream_t stream) {
+    constexpr int U = ANY ? 1 : 2;
+    const int lines = lines_of<T>(dim, ANY), units = pad_units(r);
+    const int64_t ctas = div_up(r->max_tokens * lines, kRowNT * U);
     if (ctas + units == 0) return HL_OK;
-    HL_CUDA_TRY(launch(k_expert_dispatch<V, U>, ctas + units * r->n_experts, kRowNT, stream, static_cast<const V*>(x), ld_x / per,
-                       r->n_tokens, r->max_tokens, r->top_k, nv, r->place, r->cap_rows, static_cast<V*>(y), ld_y / per, ctas,
+    if (ctas + (int64_t)units * r->n_experts > 0x7fffffff) return HL_EINVAL;
+    HL_CUDA_TRY(launch(k_expert_dispatch<T, ANY, U>, ctas + units * r->n_experts, kRowNT, stream, static_cast<const T*>(x), ld_x,
+                       r->n_tokens, r->max_tokens, r->top_k, dim, r->place, r->cap_rows, static_cast<T*>(y), ld_y, lines, ctas,
                        r->n_experts, units, r->counts, r->offsets));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
 }
 
-template <typename T, int N, int U>
+template <typename T, bool ANY>
 int32_t launch_combine(const hl_route* r, int64_t dim, const void* y, int64_t ld_y, const float* w, void* out, int64_t ld_out,
                        cudaStream_t stream) {
-    using V = Vec<T, N>;
-    const int nv = (int)(dim / N);
-    HL_CUDA_TRY(launch(k_expert_combine<T, N, U>, grid_for(r->max_tokens * div_up(nv, 32 * U), kRowWarps, 1 << 20), kRowNT,
-                       stream, static_cast<const V*>(y), ld_y / N, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, nv,
-                       r->place, w, static_cast<V*>(out), ld_out / N));
+    const int lines = lines_of<T>(dim, ANY);
+    const bool few = r->top_k <= 2;
+    const int64_t ctas = div_up(r->max_tokens * lines, kRowNT * (few ? 2 : 1));
+    if (ctas > 0x7fffffff) return HL_EINVAL;
+    HL_CUDA_TRY(launch(few ? k_expert_combine<T, ANY, 2, 2> : k_expert_combine<T, ANY, 4, 1>, ctas, kRowNT, stream,
+                       static_cast<const T*>(y), ld_y, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, dim, r->place, w,
+                       static_cast<T*>(out), ld_out, lines));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
 }
 
-template <typename T, int N, int U>
+template <typename T, bool ANY>
 int32_t launch_combine_bwd(const hl_route* r, int64_t dim, const void* go, int64_t ld_go, const void* y, int64_t ld_y,
                            const float* w, void* gy, int64_t ld_gy, float* gw, cudaStream_t stream) {
-    using V = Vec<T, N>;
-    const int nv = (int)(dim / N), units = pad_units(r);
-    int W = 1;
-    while (W < kRowWarps && W * 32 * U < nv) W *= 2;
-    const int ctas = r->max_tokens ? grid_for(r->max_tokens, kRowWarps / W, 1 << 20) : 0;
+    const int lines = lines_of<T>(dim, ANY), units = pad_units(r);
+    // threads of a token: enough for a line each, at most a warp's unless there are few tokens
+    int P = 4;
+    while (P < kRowNT && P < lines && (P < 32 || r->max_tokens * P < (int64_t)kSMsFallback * 1024)) P *= 2;
+    const int64_t ctas = div_up(r->max_tokens, kRowNT / P);
     if (ctas + units == 0) return HL_OK;
-    HL_CUDA_TRY(launch(k_expert_combine_bwd<T, N, U>, ctas + units * r->n_experts, kRowNT, stream, static_cast<const V*>(go),
-                       ld_go / N, static_cast<const V*>(y), ld_y / N, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, nv,
-                       r->place, w, static_cast<V*>(gy), ld_gy / N, gw, W, ctas, r->n_experts, units, r->counts, r->offsets));
+    if (ctas + (int64_t)units * r->n_experts > 0x7fffffff) return HL_EINVAL;
+    HL_CUDA_TRY(launch(k_expert_combine_bwd<T, ANY>, ctas + units * r->n_experts, kRowNT, stream, static_cast<const T*>(go), ld_go,
+                       static_cast<const T*>(y), ld_y, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, dim, r->place, w,
+                       static_cast<T*>(gy), ld_gy, gw, P, lines, ctas, r->n_experts, units, r->counts, r->offsets));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
 }
-
-int64_t sort_tiles(int64_t n) { return div_up(n > 0 ? n : 1, kSortChoices); }
 
 }  // namespace
 }  // namespace hl
@@ -547,7 +724,9 @@ extern "C" size_t hl_expert_workspace_bytes(int64_t max_tokens, int32_t top_k, i
     if (max_tokens < 0 || max_tokens >= (int64_t(1) << 30) || top_k < 1 || top_k > HL_MAX_TOP_K || n_experts < 1 || n_experts > HL_MAX_EXPERTS ||
         max_tokens * top_k >= (int64_t(1) << 30))
         return 0;
-    return ((sort_tiles(max_tokens * top_k) + 1) * (n_experts + 1) * sizeof(int32_t) + 255) & ~size_t(255);
+    const int64_t n = max_tokens * top_k;
+    if (n <= kOneCluster) return 256;
+    return (((sort_tiles(n) + 1) * (n_experts + 1) + n) * sizeof(int32_t) + 255) & ~size_t(255);
 }
 
 extern "C" int32_t hl_expert_sort(const hl_route* route, const int32_t* d_experts, int64_t expert_cap, int32_t* d_status,
@@ -574,16 +753,24 @@ extern "C" int32_t hl_expert_sort(const hl_route* route, const int32_t* d_expert
     const int64_t tiles = sort_tiles(n);
     int32_t* totals = static_cast<int32_t*>(d_workspace);
     int32_t* tile_counts = totals + (E + 1);
-    HL_CUDA_TRY(launch_cluster(k_expert_count, tiles, kSortNT, smem, 0, stream, d_experts, route->n_tokens, route->max_tokens,
-                               route->top_k, E, tile_counts));
-    HL_CUDA_TRY(launch(k_expert_scan, div_up(E + 1, 32), 1024, stream, tile_counts, tiles, E, totals));
-    HL_CUDA_TRY(launch_cluster(k_expert_place, tiles, kSortNT, smem, 0, stream, d_experts, route->n_tokens, route->max_tokens,
-                               route->top_k, E, cap, route->align, route->cap_rows, route->place, route->source, route->counts,
-                               route->offsets, d_status, (const int32_t*)tile_counts, (const int32_t*)totals));
+    uint32_t* ranked = reinterpret_cast<uint32_t*>(tile_counts + tiles * (E + 1));
+    HL_CUDA_TRY(launch_cluster(k_expert_rank, tiles, kSortNT, smem, 0, stream, d_experts, route->n_tokens, route->max_tokens,
+                               route->top_k, E, tile_counts, ranked));
+    HL_CUDA_TRY(launch_after(k_expert_scan, div_up(E + 1, 8), 256, 0, stream, tile_counts, tiles, E, totals));
+    HL_CUDA_TRY(launch_after(k_expert_place, tiles, kSortNT, smem, stream, route->n_tokens, route->max_tokens, route->top_k, E,
+                             cap, route->align, route->cap_rows, route->place, route->source, route->counts, route->offsets,
+                             d_status, (const int32_t*)tile_counts, (const int32_t*)totals, (const uint32_t*)ranked));
     note_launches(3);
     HL_LAUNCH_CHECK();
     return HL_OK;
 }
+
+#define HL_FOR_TYPE(CALL)                                                                   \
+    do {                                                                                    \
+        if (dtype == HL_F32) return wide ? CALL(float, false) : CALL(float, true);          \
+        if (dtype == HL_BF16) return wide ? CALL(__nv_bfloat16, false) : CALL(__nv_bfloat16, true); \
+        return wide ? CALL(__half, false) : CALL(__half, true);                             \
+    } while (0)
 
 extern "C" int32_t hl_expert_dispatch(const hl_route* route, int32_t dtype, int64_t dim, const void* d_x, int64_t ld_x,
                                       void* d_y, int64_t ld_y, void* stream_) {
@@ -593,21 +780,11 @@ extern "C" int32_t hl_expert_dispatch(const hl_route* route, int32_t dtype, int6
     const Matrix x{d_x, ld_x, route->max_tokens}, y{d_y, ld_y, route->cap_rows};
     if (!matrices_ok(dtype, dim, {x, y})) return HL_EINVAL;
     if (route->cap_rows == 0) return HL_OK;
-    const int size = size_of(dtype);
-#define HL_DISPATCH(V, U) launch_dispatch<V, U>(route, dim, d_x, ld_x, d_y, ld_y, size, stream)
-    if (aligned_to(16, size, dim, {x, y})) return HL_DISPATCH(uint4, 4);
-    if (aligned_to(8, size, dim, {x, y})) return HL_DISPATCH(uint2, 4);
-    if (aligned_to(4, size, dim, {x, y})) return HL_DISPATCH(uint32_t, 8);
-    return HL_DISPATCH(uint16_t, 8);
+    const bool wide = aligned_to(16, size_of(dtype), dim, {x, y});
+#define HL_DISPATCH(T, ANY) launch_dispatch<T, ANY>(route, dim, d_x, ld_x, d_y, ld_y, stream)
+    HL_FOR_TYPE(HL_DISPATCH);
 #undef HL_DISPATCH
 }
-
-#define HL_FOR_TYPE(CALL)                                                                        \
-    do {                                                                                         \
-        if (dtype == HL_F32) return wide ? CALL(float, 4, 4) : CALL(float, 1, 8);                \
-        if (dtype == HL_BF16) return wide ? CALL(__nv_bfloat16, 8, 4) : CALL(__nv_bfloat16, 1, 8); \
-        return wide ? CALL(__half, 8, 4) : CALL(__half, 1, 8);                                   \
-    } while (0)
 
 extern "C" int32_t hl_expert_combine(const hl_route* route, int32_t dtype, int64_t dim, const void* d_y, int64_t ld_y,
                                      const float* d_weights, void* d_out, int64_t ld_out, void* stream_) {
@@ -617,7 +794,7 @@ extern "C" int32_t hl_expert_combine(const hl_route* route, int32_t dtype, int64
     if (!matrices_ok(dtype, dim, {y, out})) return HL_EINVAL;
     if (route->max_tokens == 0) return HL_OK;
     const bool wide = aligned_to(16, size_of(dtype), dim, {y, out});
-#define HL_COMBINE(T, N, U) launch_combine<T, N, U>(route, dim, d_y, ld_y, d_weights, d_out, ld_out, stream)
+#define HL_COMBINE(T, ANY) launch_combine<T, ANY>(route, dim, d_y, ld_y, d_weights, d_out, ld_out, stream)
     HL_FOR_TYPE(HL_COMBINE);
 #undef HL_COMBINE
 }
@@ -632,8 +809,8 @@ extern "C" int32_t hl_expert_combine_bwd(const hl_route* route, int32_t dtype, i
     const Matrix y{d_grad_weights ? d_y : d_grad_y, d_grad_weights ? ld_y : ld_grad_y, route->cap_rows};   // (else not read)
     if (!matrices_ok(dtype, dim, {go, y, gy})) return HL_EINVAL;
     const bool wide = aligned_to(16, size_of(dtype), dim, {go, y, gy});
-#define HL_COMBINE_BWD(T, N, U) \
-    launch_combine_bwd<T, N, U>(route, dim, d_grad_out, ld_grad_out, d_y, ld_y, d_weights, d_grad_y, ld_grad_y, d_grad_weights, stream)
+#define HL_COMBINE_BWD(T, ANY) \
+    launch_combine_bwd<T, ANY>(route, dim, d_grad_out, ld_grad_out, d_y, ld_y, d_weights, d_grad_y, ld_grad_y, d_grad_weights, stream)
     HL_FOR_TYPE(HL_COMBINE_BWD);
 #undef HL_COMBINE_BWD
 }

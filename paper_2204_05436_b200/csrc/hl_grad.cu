@@ -26,10 +26,11 @@ __device__ __forceinline__ double block_sum(double v) {        // the same in ev
 }
 
 // ---- many tensors ---------------------------------------------------------------------------------------------------
-// A call's tensors are cut into tiles of kTile values, which are dealt out to the CTAs in turn.
-constexpr int kTile = 8192;
+// A call's tensors are cut into tiles of 2^tile_bits values, and every CTA takes a run of tiles.
+constexpr int kMinTileBits = 10, kMaxTileBits = 13;
 constexpr int kGradCtas = 8;                         // CTAs per multiprocessor
 constexpr int kMaxPartials = 2048;                   // sums of squares, one per CTA
+constexpr int kAhead = 4;                            // loads of a thread on their way
 
 // N tensors and where their tiles begin, as a kernel argument.
 template <int N>
@@ -39,24 +40,51 @@ struct TensorPairArgs {
     int64_t n[N];
     int32_t first_tile[N];
     uint8_t kind[N];                                 // type of src, type of dst
-    int32_t n_tensors, n_tiles;
+    int32_t n_tensors, n_tiles, tile_bits, unused;
 };
 
 template <typename T>
-struct Wide {
-    static constexpr int N = 16 / sizeof(T);
-    union {
-        uint4 raw;
-        T v[N];
-    };
-    __device__ Wide() {}
-};
+constexpr int kWide = 16 / sizeof(T);                // values in 16 bytes
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 __device__ __forceinline__ void put(__half* p, float x) { *p = __float2half_rn(x); }
+// a word's values, and a word from values
+template <typename T>
+__device__ __forceinline__ void unpack(uint32_t w, float* x) {
+    if constexpr (sizeof(T) == 4) {
+        x[0] = __uint_as_float(w);
+    } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+        x[0] = __uint_as_float(w << 16);
+        x[1] = __uint_as_float(w & 0xffff0000u);
+    } else {
+        const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        x[0] = v.x;
+        x[1] = v.y;
+    }
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pack(const float* x) {
+    if constexpr (sizeof(T) == 4) {
+        return __float_as_uint(x[0]);
+    } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(x[0], x[1]);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+        const __half2 v = __floats2half2_rn(x[0], x[1]);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void unpack4(const uint4& r, float (&x)[kWide<T>]) {
+    constexpr int n = 4 / sizeof(T);
+    unpack<T>(r.x, x);
+    unpack<T>(r.y, x + n);
+    unpack<T>(r.z, x + 2 * n);
+    unpack<T>(r.w, x + 3 * n);
+}
 
 // values before p's next multiple of 16 bytes
 template <typename T>
@@ -67,16 +95,20 @@ __device__ __forceinline__ int head_of(const T* p, int n) {
 
 template <typename T>
 __device__ __forceinline__ double tile_squares(const T* __restrict__ p, int n) {
+    constexpr int W = kWide<T>;
     double sum = 0.0;
-    const int head = head_of(p, n), nv = (n - head) / Wide<T>::N, tail = head + nv * Wide<T>::N;
+    const int head = head_of(p, n), nv = (n - head) / W, tail = head + nv * W;
     const uint4* q = reinterpret_cast<const uint4*>(p + head);
-    for (int i = threadIdx.x; i < nv; i += kNT) {
-        Wide<T> w;
-        w.raw = __ldg(&q[i]);
+    for (int i = threadIdx.x; i < nv; i += kNT * kAhead) {
+        uint4 r[kAhead];
 #pragma unroll
-        for (int j = 0; j < Wide<T>::N; ++j) {
-            const double x = to_f32(w.v[j]);
-            sum = fma(x, x, sum);
+        for (int u = 0; u < kAhead; ++u) r[u] = i + u * kNT < nv ? __ldg(&q[i + u * kNT]) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            float x[W];
+            unpack4<T>(r[u], x);
+#pragma unroll
+            for (int j = 0; j < W; ++j) sum = fma((double)x[j], (double)x[j], sum);
         }
     }
     for (int i = threadIdx.x; i < head + n - tail; i += kNT) {
@@ -86,28 +118,41 @@ __device__ __forceinline__ double tile_squares(const T* __restrict__ p, int n) {
     return sum;
 }
 
+// (p and d may be the same)
 template <typename S, typename D>
 __device__ __forceinline__ void tile_scale(const S* p, D* d, int n, float f) {
-    constexpr int N = Wide<S>::N;
-    const int head = head_of(p, n), nv = (n - head) / N, tail = head + nv * N;
+    constexpr int W = kWide<S>, kLine = W * sizeof(D) < 16 ? W * sizeof(D) : 16;       // bytes of a store
+    const int head = head_of(p, n);
+    if (reinterpret_cast<uintptr_t>(d + head) % kLine) {       // no common lines
+#pragma unroll 4
+        for (int i = threadIdx.x; i < n; i += kNT) put(&d[i], f * to_f32(p[i]));
+        return;
+    }
+    const int nv = (n - head) / W, tail = head + nv * W;
     const uint4* q = reinterpret_cast<const uint4*>(p + head);
-    const bool wide = (reinterpret_cast<uintptr_t>(d + head) & (N * sizeof(D) < 16 ? N * sizeof(D) - 1 : 15)) == 0;
-    for (int i = threadIdx.x; i < nv; i += kNT) {
-        Wide<S> w;
-        w.raw = q[i];
-        alignas(16) D r[N];
+    for (int i = threadIdx.x; i < nv; i += kNT * kAhead) {
+        uint4 r[kAhead];
 #pragma unroll
-        for (int j = 0; j < N; ++j) put(&r[j], f * to_f32(w.v[j]));
-        D* to = d + head + i * N;
-        if (!wide) {
+        for (int u = 0; u < kAhead; ++u) r[u] = i + u * kNT < nv ? __ldcs(&q[i + u * kNT]) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int j = 0; j < N; ++j) to[j] = r[j];
-        } else if constexpr (N * sizeof(D) == 8) {
-            *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(r);
-        } else {
+        for (int u = 0; u < kAhead; ++u) {
+            if (i + u * kNT >= nv) break;
+            float x[W];
+            unpack4<S>(r[u], x);
 #pragma unroll
-            for (int j = 0; j < (int)(N * sizeof(D) / 16); ++j)
-                reinterpret_cast<uint4*>(to)[j] = reinterpret_cast<const uint4*>(r)[j];
+            for (int j = 0; j < W; ++j) x[j] *= f;
+            constexpr int kWords = W * sizeof(D) / 4, kPer = 4 / sizeof(D);
+            uint32_t w[kWords];
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) w[j] = pack<D>(x + j * kPer);
+            D* to = d + head + (int64_t)(i + u * kNT) * W;
+            if constexpr (kWords == 2) {
+                *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kWords; j += 4)
+                    *reinterpret_cast<uint4*>(to + j * kPer) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+            }
         }
     }
     for (int i = threadIdx.x; i < head + n - tail; i += kNT) {
@@ -127,17 +172,25 @@ __device__ __forceinline__ int tensor_of(const TensorPairArgs<N>& a, int tile) {
     }
     return lo;
 }
+// CTA b's tiles are [first_of(b), first_of(b + 1)).
+template <int N>
+__device__ __forceinline__ int first_of(const TensorPairArgs<N>& a, unsigned b) {
+    return (int)((int64_t)a.n_tiles * b / gridDim.x);
+}
 
 // partial[b] (+)= the squares of CTA b's tiles
 template <int N>
 __global__ void __launch_bounds__(kNT) k_grad_squares(const __grid_constant__ TensorPairArgs<N> a, int more,
                                                       double* __restrict__ partial) {
+    let_next_start();
     double sum = 0.0;
-    for (int tile = blockIdx.x; tile < a.n_tiles; tile += gridDim.x) {
-        const int t = tensor_of(a, tile);
+    const int end = first_of(a, blockIdx.x + 1);
+    int tile = first_of(a, blockIdx.x), t = tensor_of(a, tile);
+    for (; tile < end; ++tile) {
+        if (t + 1 < a.n_tensors && a.first_tile[t + 1] <= tile) ++t;
         const int kind = a.kind[t];
-        const int64_t at = (int64_t)(tile - a.first_tile[t]) * kTile;
-        const int n = (int)min((int64_t)kTile, a.n[t] - at);
+        const int64_t at = (int64_t)(tile - a.first_tile[t]) << a.tile_bits;
+        const int n = (int)min((int64_t)1 << a.tile_bits, a.n[t] - at);
         if ((kind & 3) == HL_F32) sum += tile_squares(static_cast<const float*>(a.src[t]) + at, n);
         else if ((kind & 3) == HL_BF16) sum += tile_squares(static_cast<const __nv_bfloat16*>(a.src[t]) + at, n);
         else sum += tile_squares(static_cast<const __half*>(a.src[t]) + at, n);
@@ -146,37 +199,40 @@ __global__ void __launch_bounds__(kNT) k_grad_squares(const __grid_constant__ Te
     if (threadIdx.x == 0) partial[blockIdx.x] = more ? partial[blockIdx.x] + sum : sum;
 }
 
-__device__ __forceinline__ double total_squares(const double* __restrict__ partial, int n_partials,
-                                                const double* __restrict__ further, int n_further) {
+__device__ __forceinline__ double total_squares(const double* partial, int n_partials, const double* further, int n_further) {
     double sum = 0.0;
     for (int i = threadIdx.x; i < n_partials; i += kNT) sum += partial[i];
     for (int i = threadIdx.x; i < n_further; i += kNT) sum += further[i];
     return block_sum(sum);
 }
 
-__global__ void __launch_bounds__(kNT) k_grad_norm(const double* __restrict__ partial, int n_partials,
-                                                   const double* __restrict__ further, int n_further, float* norm) {
+__global__ void __launch_bounds__(kNT) k_grad_norm(const double* partial, int n_partials, const double* further, int n_further,
+                                                   float* norm) {
+    wait_for_last();
     const double sum = total_squares(partial, n_partials, further, n_further);
     if (threadIdx.x == 0) *norm = (float)sqrt(sum);
 }
 
+// A CTA takes its tiles from the last to the first: what the sums of squares read last is still in the L2.
 template <int N>
-__global__ void __launch_bounds__(kNT) k_grad_scale(const __grid_constant__ TensorPairArgs<N> a,
-                                                    const double* __restrict__ partial, int n_partials,
-                                                    const double* __restrict__ further, int n_further, float max_norm,
+__global__ void __launch_bounds__(kNT, 4) k_grad_scale(const __grid_constant__ TensorPairArgs<N> a, const double* partial,
+                                                    int n_partials, const double* further, int n_further, float max_norm,
                                                     float* norm) {
+    const int begin = first_of(a, blockIdx.x);
+    int tile = first_of(a, blockIdx.x + 1) - 1, t = tensor_of(a, tile);
+    wait_for_last();
     const double total = sqrt(total_squares(partial, n_partials, further, n_further));
     if (blockIdx.x == 0 && threadIdx.x == 0 && norm) *norm = (float)total;
     const double c = (double)max_norm / (total + 1e-6);
     const float f = c > 1.0 ? 1.f : (float)c;        // (NaN: NaN)
-    for (int tile = blockIdx.x; tile < a.n_tiles; tile += gridDim.x) {
-        const int t = tensor_of(a, tile);
-        const int64_t at = (int64_t)(tile - a.first_tile[t]) * kTile;
-        const int n = (int)min((int64_t)kTile, a.n[t] - at);
+    for (; tile >= begin; --tile) {
+        if (a.first_tile[t] > tile) --t;
+        const int64_t at = (int64_t)(tile - a.first_tile[t]) << a.tile_bits;
+        const int n = (int)min((int64_t)1 << a.tile_bits, a.n[t] - at);
         const void* s = a.src[t];
         void* d = a.dst[t];
         const int from = a.kind[t] & 3, to = (a.kind[t] >> 2) & 3;
-        if (d == nullptr || (d == s && f == 1.f)) continue;
+        if (d == s && f == 1.f) continue;
         using B = __nv_bfloat16;
         using H = __half;
 #define HL_SCALE(S, D) tile_scale(static_cast<const S*>(s) + at, static_cast<D*>(d) + at, n, f)
@@ -222,16 +278,16 @@ int grad_grid() {
 
 // f(args) for the tensors that count (of the norm, or those to write) in groups of at most N, each a kernel's argument
 template <int N, typename F>
-int32_t in_groups(const hl_tensor* ts, int32_t n, bool norm, F f) {
+int32_t in_groups(const hl_tensor* ts, int32_t n, bool norm, int tile_bits, F f) {
     TensorPairArgs<N> a;
     int i = 0;
     while (i < n) {
-        memset(&a, 0, sizeof(a));
+        a.n_tensors = 0;
         int64_t tiles = 0;
         for (; i < n && a.n_tensors < N; ++i) {
             const hl_tensor& t = ts[i];
             if (t.n == 0 || (norm ? (t.flags & HL_TENSOR_NOT_IN_NORM) != 0 : t.dst == nullptr)) continue;
-            const int64_t more = div_up(t.n, kTile);
+            const int64_t more = div_up(t.n, int64_t(1) << tile_bits);
             if (tiles + more > 0x7fffffff) break;
             const int k = a.n_tensors++;
             a.src[k] = t.src;
@@ -242,6 +298,7 @@ int32_t in_groups(const hl_tensor* ts, int32_t n, bool norm, F f) {
             tiles += more;
         }
         a.n_tiles = (int32_t)tiles;
+        a.tile_bits = tile_bits;
         if (a.n_tensors == 0) break;
         const int32_t st = f(a);
         if (st != HL_OK) return st;
@@ -249,26 +306,40 @@ int32_t in_groups(const hl_tensor* ts, int32_t n, bool norm, F f) {
     return HL_OK;
 }
 
+int64_t tiles_of(const hl_tensor* ts, int32_t n, bool norm, int tile_bits) {
+    int64_t tiles = 0;
+    for (int i = 0; i < n; ++i)
+        if (norm ? !(ts[i].flags & HL_TENSOR_NOT_IN_NORM) : ts[i].dst != nullptr) tiles += div_up(ts[i].n, int64_t(1) << tile_bits);
+    return tiles;
+}
+
 template <int N>
 int32_t clip(const hl_tensor* ts, int32_t n, const double* further, int32_t n_further, bool scale, float max_norm, float* norm,
              double* partial, cudaStream_t stream) {
     const int most = grad_grid();
-    int64_t tiles = 0;
-    for (int i = 0; i < n; ++i) tiles += ts[i].flags & HL_TENSOR_NOT_IN_NORM ? 0 : div_up(ts[i].n, kTile);
+    // the smallest tiles that leave a CTA one
+    const auto bits = [&](bool of_norm) {
+        int b = kMinTileBits;
+        while (b < kMaxTileBits && tiles_of(ts, n, of_norm, b) > most) ++b;
+        return b;
+    };
+    const int norm_bits = bits(true);
+    const int64_t tiles = tiles_of(ts, n, true, norm_bits);
     const int n_partials = tiles ? grid_for(tiles, 1, most) : 0;
     bool more = false;
-    int32_t st = in_groups<N>(ts, n, true, [&](const TensorPairArgs<N>& a) -> int32_t {
+    int32_t st = in_groups<N>(ts, n, true, norm_bits, [&](const TensorPairArgs<N>& a) -> int32_t {
         HL_CUDA_TRY(launch(k_grad_squares<N>, n_partials, kNT, stream, a, more ? 1 : 0, partial));   // (later groups add)
         more = true;
         note_launches(1);
         return HL_OK;
     });
     if (st != HL_OK) return st;
+    const int first_after = n_partials ? kAfterLast : 0;       // (of what the caller has on the stream, all has to be over)
     bool said = false;
     if (scale) {
-        st = in_groups<N>(ts, n, false, [&](const TensorPairArgs<N>& a) -> int32_t {
-            HL_CUDA_TRY(launch(k_grad_scale<N>, grid_for(a.n_tiles, 1, most), kNT, stream, a, (const double*)partial, n_partials,
-                               further, n_further, max_norm, said ? nullptr : norm));
+        st = in_groups<N>(ts, n, false, bits(false), [&](const TensorPairArgs<N>& a) -> int32_t {
+            HL_CUDA_TRY(launch_cluster(k_grad_scale<N>, grid_for(a.n_tiles, 1, most), kNT, 0, said ? 0 : first_after, stream, a,
+                                       (const double*)partial, n_partials, further, n_further, max_norm, said ? nullptr : norm));
             said = true;
             note_launches(1);
             return HL_OK;
@@ -276,7 +347,8 @@ int32_t clip(const hl_tensor* ts, int32_t n, const double* further, int32_t n_fu
         if (st != HL_OK) return st;
     }
     if (!said && norm) {
-        HL_CUDA_TRY(launch(k_grad_norm, 1, kNT, stream, (const double*)partial, n_partials, further, n_further, norm));
+        HL_CUDA_TRY(launch_cluster(k_grad_norm, 1, kNT, 0, first_after, stream, (const double*)partial, n_partials, further,
+                                   n_further, norm));
         note_launches(1);
     }
     HL_LAUNCH_CHECK();
@@ -309,34 +381,52 @@ struct RowShape {
 __device__ __forceinline__ double square(const double a[4]) { return a[0] * a[0] + a[1] * a[1] + a[2] * a[2] + a[3] * a[3]; }
 
 template <int G>
-__global__ void __launch_bounds__(kNT) k_rows_squares(const int32_t* __restrict__ slots, const int32_t* __restrict__ bags,
+__global__ void __launch_bounds__(kNT, 4) k_rows_squares(const int32_t* __restrict__ slots, const int32_t* __restrict__ bags,
                                                       const int32_t* __restrict__ d_n, int64_t max_n, int64_t n_slots,
                                                       int64_t n_bags, const float4* __restrict__ grad, int D4,
                                                       double* __restrict__ pieces, int32_t* __restrict__ starts,
                                                       double* __restrict__ partial) {
     using Shape = RowShape<G>;
-    __shared__ double s_head[kNT][4];                // of a run that an earlier group began, by lane
-    __shared__ bool s_cont[Shape::kGroups], s_whole[Shape::kGroups];
-    const int64_t n = min((int64_t)max(*d_n, 0), max_n);
-    const int64_t windows = (n + Shape::kWindow - 1) / Shape::kWindow;
+    constexpr int kGroups = Shape::kGroups, kWindow = Shape::kWindow, kRows = 4;
+    __shared__ int32_t s_slot[kWindow + 2], s_bag[kWindow];    // s_slot[0]: the lookup before the window's
+    __shared__ double s_head[kNT][4];                          // of a run that an earlier group began, by lane
+    __shared__ bool s_cont[kGroups], s_whole[kGroups];
+    let_next_start();
+    const int64_t n = min((int64_t)max(__ldg(d_n), 0), max_n), w = blockIdx.x, begin = w * kWindow;
     const int g = threadIdx.x / G, sub = threadIdx.x % G, c = blockIdx.y * G + sub;
     const bool mine = c < D4;
-    double total = 0.0;
-    for (int64_t w = blockIdx.x; w < windows; w += gridDim.x) {
-        const int64_t first = w * Shape::kWindow + g * kRun;
-        const int len = (int)max((int64_t)0, min((int64_t)kRun, n - first));
-        double acc[4] = {}, tail[4] = {};
-        bool cont = false, whole = false, open = false;
-        if (len > 0) {
-            int32_t slot = slots[first];
-            const int32_t before = first > 0 ? slots[first - 1] : -1;
-            cont = first > 0 && before == slot;
-            bool head = cont;                        // the run at hand began before this group's lookups
-#pragma unroll 4
-            for (int i = 0; i < len; ++i) {
-                const int32_t s = slots[first + i], b = bags[first + i];
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (mine && s >= 0 && s < n_slots && b >= 0 && b < n_bags) v = __ldg(&grad[(int64_t)b * D4 + c]);
+    const int here = (int)max((int64_t)0, min((int64_t)kWindow, n - begin));       // lookups of the window
+    for (int i = threadIdx.x; i < kWindow + 2; i += kNT) {
+        const int64_t at = begin - 1 + i;
+        s_slot[i] = at >= 0 && at < n ? __ldg(&slots[at]) : 0;
+        if (i < kWindow && i < here) {
+            const int32_t b = __ldg(&bags[begin + i]);
+            s_bag[i] = b >= 0 && b < n_bags ? b : -1;
+        }
+    }
+    __syncthreads();
+    const int l0 = g * kRun, len = max(0, min(kRun, here - l0));
+    double total = 0.0, acc[4] = {};
+    bool cont = false, whole = false, open = false;
+    if (len > 0) {
+        int32_t slot = s_slot[1 + l0];
+        cont = begin + l0 > 0 && s_slot[l0] == slot;
+        bool head = cont;                            // the run at hand began before this group's lookups
+#pragma unroll 1
+        for (int i0 = 0; i0 < len; i0 += kRows) {
+            float4 v[kRows];
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+                v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (i0 + j < len && mine) {
+                    const int32_t s = s_slot[1 + l0 + i0 + j], b = s_bag[l0 + i0 + j];
+                    if (s >= 0 && s < n_slots && b >= 0) v[j] = __ldg(&grad[(int64_t)b * D4 + c]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
+                if (i0 + j >= len) break;
+                const int32_t s = s_slot[1 + l0 + i0 + j];
                 if (s != slot) {                     // a run ends
                     if (head) {
 #pragma unroll
@@ -349,122 +439,134 @@ __global__ void __launch_bounds__(kNT) k_rows_squares(const int32_t* __restrict_
 #pragma unroll
                     for (int k = 0; k < 4; ++k) acc[k] = 0.0;
                 }
-                acc[0] += v.x;
-                acc[1] += v.y;
-                acc[2] += v.z;
-                acc[3] += v.w;
-            }
-            const bool goes_on = first + len < n && slots[first + len] == slot;
-            if (head) {                              // one run, from before the first to the last of them
-                whole = goes_on;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) s_head[threadIdx.x][k] = acc[k];
-            } else if (goes_on) {
-                open = true;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) tail[k] = acc[k];
-            } else {
-                total += square(acc);
+                acc[0] += v[j].x;
+                acc[1] += v[j].y;
+                acc[2] += v[j].z;
+                acc[3] += v[j].w;
             }
         }
-        if (sub == 0) {
-            s_cont[g] = cont;
-            s_whole[g] = whole;
+        const bool goes_on = begin + l0 + len < n && s_slot[1 + l0 + len] == slot;
+        if (head) {                                  // one run, from before the first to the last of them
+            whole = goes_on;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s_head[threadIdx.x][k] = acc[k];
+        } else if (goes_on) {
+            open = true;
+        } else {
+            total += square(acc);
         }
-        __syncthreads();
-        // the group that began a run puts it together; the window's first group also what an earlier window's run left here
-        if (g == 0 && cont) {
-            double a[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) a[k] = s_head[sub][k];
-            for (int h = 1; h < Shape::kGroups && s_whole[h - 1] && s_cont[h]; ++h)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) a[k] += s_head[h * G + sub][k];
-            if (mine)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) pieces[((w * 2 + 0) * D4 + c) * 4 + k] = a[k];
-        }
-        bool out = false;
-        if (open) {
-            int h = g + 1;
-            bool more = true;
-            for (; more && h < Shape::kGroups; ++h) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) tail[k] += s_head[h * G + sub][k];
-                more = s_whole[h];
-            }
-            out = more;                              // on into the next window
-            if (!out) total += square(tail);
-            else if (mine)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) pieces[((w * 2 + 1) * D4 + c) * 4 + k] = tail[k];
-        }
-        const int any = __syncthreads_or(out);
-        if (threadIdx.x == 0 && blockIdx.y == 0) starts[w] = any;
     }
+    if (sub == 0) {
+        s_cont[g] = cont;
+        s_whole[g] = whole;
+    }
+    __syncthreads();
+    // the group that began a run puts it together; the window's first group also what an earlier window's run left here
+    if (g == 0 && cont) {
+        double a[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a[k] = s_head[sub][k];
+        for (int h = 1; h < kGroups && s_whole[h - 1] && s_cont[h]; ++h)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a[k] += s_head[h * G + sub][k];
+        if (mine)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) pieces[((w * 2 + 0) * D4 + c) * 4 + k] = a[k];
+    }
+    bool out = false;                                // on into the next window
+    if (open) {
+        out = true;
+        for (int h = g + 1; out && h < kGroups; ++h) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[k] += s_head[h * G + sub][k];
+            out = s_whole[h];
+        }
+        if (!out) total += square(acc);
+        else if (mine)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) pieces[((w * 2 + 1) * D4 + c) * 4 + k] = acc[k];
+    }
+    const int any = __syncthreads_or(out);
+    if (threadIdx.x == 0 && blockIdx.y == 0) starts[w] = any;
     total = block_sum(mine ? total : 0.0);
-    if (threadIdx.x == 0) partial[blockIdx.y * gridDim.x + blockIdx.x] = total;
+    if (threadIdx.x == 0) partial[blockIdx.y * gridDim.x + w] = total;
 }
 
-// The runs over several windows: a CTA looks for the windows in which one starts.
+// The run over several windows that starts in window blockIdx.x, if one does.
 template <int G>
-__global__ void __launch_bounds__(kNT) k_rows_long(const int32_t* __restrict__ slots, const int32_t* __restrict__ d_n,
-                                                   int64_t max_n, int D4, const double* __restrict__ pieces,
-                                                   const int32_t* __restrict__ starts, double* __restrict__ partial) {
+__global__ void __launch_bounds__(kNT) k_rows_long(const int32_t* slots, const int32_t* d_n, int64_t max_n, int D4,
+                                                   const double* pieces, const int32_t* starts, double* partial) {
     using Shape = RowShape<G>;
+    constexpr int kGroups = Shape::kGroups, kWindow = Shape::kWindow;
     __shared__ double s_sum[kNT][4];
+    __shared__ int s_first;
+    let_next_start();
+    wait_for_last();
+    const int64_t w = blockIdx.x;
+    double* to = &partial[blockIdx.y * gridDim.x + w];
+    if (!starts[w]) {
+        if (threadIdx.x == 0) *to = 0.0;
+        return;
+    }
     const int64_t n = min((int64_t)max(*d_n, 0), max_n);
-    const int64_t windows = (n + Shape::kWindow - 1) / Shape::kWindow;
     const int g = threadIdx.x / G, sub = threadIdx.x % G, c = blockIdx.y * G + sub;
     const bool mine = c < D4;
-    double total = 0.0;
-    for (int64_t w = blockIdx.x; w < windows; w += gridDim.x) {
-        if (!starts[w]) continue;
-        const int32_t slot = slots[(w + 1) * Shape::kWindow - 1];
-        int64_t last = w + 1;                        // the window in which the run ends
-        for (;;) {
-            const int64_t x = last + threadIdx.x, next = (x + 1) * Shape::kWindow;
-            const bool ends = next >= n || slots[next] != slot;
-            const int any = __syncthreads_or(ends);
-            if (any) {
-                __shared__ int s_first;
-                if (threadIdx.x == 0) s_first = kNT;
-                __syncthreads();
-                if (ends) atomicMin(&s_first, (int)threadIdx.x);
-                __syncthreads();
-                last += s_first;
-                __syncthreads();
-                break;
-            }
-            last += kNT;
-        }
-        double a[4] = {};
-        if (mine) {
-            if (g == 0)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) a[k] = pieces[((w * 2 + 1) * D4 + c) * 4 + k];
-            for (int64_t x = w + 1 + g; x <= last; x += Shape::kGroups)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) a[k] += pieces[((x * 2 + 0) * D4 + c) * 4 + k];
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) s_sum[threadIdx.x][k] = a[k];
-        __syncthreads();
-        if (g == 0) {
-            for (int h = 1; h < Shape::kGroups; ++h)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) a[k] += s_sum[h * G + sub][k];
-            total += square(a);
-        }
-        __syncthreads();
+    const int32_t slot = slots[(w + 1) * kWindow - 1];
+    if (threadIdx.x == 0) s_first = kNT;
+    __syncthreads();
+    int64_t last = w + 1;                            // the window in which the run ends
+    for (;; last += kNT) {
+        const int64_t next = (last + threadIdx.x + 1) * kWindow;
+        const bool ends = next >= n || slots[next] != slot;
+        if (ends) atomicMin(&s_first, (int)threadIdx.x);
+        if (__syncthreads_or(ends)) break;
     }
-    total = block_sum(mine ? total : 0.0);
-    if (threadIdx.x == 0) partial[blockIdx.y * gridDim.x + blockIdx.x] = total;
+    last += s_first;
+    double a[4] = {};
+    if (mine) {
+        if (g == 0)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a[k] = pieces[((w * 2 + 1) * D4 + c) * 4 + k];
+#pragma unroll 4
+        for (int64_t x = w + 1 + g; x <= last; x += kGroups) {
+            const double2* p = reinterpret_cast<const double2*>(&pieces[((x * 2 + 0) * D4 + c) * 4]);
+            const double2 lo = p[0], hi = p[1];
+            a[0] += lo.x;
+            a[1] += lo.y;
+            a[2] += hi.x;
+            a[3] += hi.y;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s_sum[threadIdx.x][k] = a[k];
+    __syncthreads();
+    double total = 0.0;
+    if (g == 0 && mine) {
+        for (int h = 1; h < kGroups; ++h)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a[k] += s_sum[h * G + sub][k];
+        total = square(a);
+    }
+    total = block_sum(total);
+    if (threadIdx.x == 0) *to = total;
 }
 
-__global__ void __launch_bounds__(kNT) k_rows_total(const double* __restrict__ partial, int n_partials, double* sumsq) {
-    const double sum = total_squares(partial, n_partials, nullptr, 0);
-    if (threadIdx.x == 0) *sumsq = sum;
+constexpr int kTotalNT = 1024;
+__global__ void __launch_bounds__(kTotalNT) k_rows_total(const double* partial, int n_partials, double* sumsq) {
+    __shared__ double s[kTotalNT / 32];
+    wait_for_last();
+    double v = 0.0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n_partials; i += kTotalNT) v += partial[i];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    v = s[threadIdx.x];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if (threadIdx.x == 0) *sumsq = v;
 }
 
 // In the backward region: the pieces of runs over several windows where hl_embbag_bwd_apply keeps its own (a call of one window
@@ -477,19 +579,17 @@ int32_t rows_squares(hl_ctx* ctx, const int32_t* slots, const int32_t* bags, con
     static_assert(Shape::kWindow >= 4 * kBwdChunk, "room for the pieces");
     const int D4 = ctx->D / 4, cols = (int)div_up(D4, G);
     const int64_t windows = div_up(ctx->max_nnz > 0 ? ctx->max_nnz : 1, Shape::kWindow);
-    const int short_ctas = grid_for(windows, 1, 4 * ctx_sms(ctx)), long_ctas = grid_for(windows, 1, ctx_sms(ctx));
-    const int n_partials = (short_ctas + long_ctas) * cols;
+    const int64_t n_partials = 2 * windows * cols;
     double* pieces = reinterpret_cast<double*>(ctx->r.bwd_part);
     double* partial = reinterpret_cast<double*>(ctx->r.bwd_hist[1]);
     int32_t* starts = reinterpret_cast<int32_t*>(partial + n_partials);
-    if ((n_partials * 2 + windows) > sort_hist_words(ctx->max_nnz)) return HL_EINVAL;        // (rows of up to 1 024 fp32: never)
-    const auto grid = [&](int ctas) { return dim3((unsigned)ctas, (unsigned)cols); };
-    HL_CUDA_TRY(launch(k_rows_squares<G>, grid(short_ctas), kNT, stream, slots, bags, d_n, ctx->max_nnz,
-                       ctx->hot_cap + ctx->staging_cap, ctx->max_bags, reinterpret_cast<const float4*>(grad), D4, pieces, starts,
-                       partial));
-    HL_CUDA_TRY(launch(k_rows_long<G>, grid(long_ctas), kNT, stream, slots, d_n, ctx->max_nnz, D4, (const double*)pieces,
-                       (const int32_t*)starts, partial + short_ctas * cols));
-    HL_CUDA_TRY(launch(k_rows_total, 1, kNT, stream, (const double*)partial, n_partials, sumsq));
+    if (n_partials * 2 + windows > sort_hist_words(ctx->max_nnz)) return HL_EINVAL;          // (rows of up to 1 024 fp32: never)
+    const dim3 grid((unsigned)windows, (unsigned)cols);
+    HL_CUDA_TRY(launch(k_rows_squares<G>, grid, kNT, stream, slots, bags, d_n, ctx->max_nnz, ctx->hot_cap + ctx->staging_cap,
+                       ctx->max_bags, reinterpret_cast<const float4*>(grad), D4, pieces, starts, partial));
+    HL_CUDA_TRY(launch_after(k_rows_long<G>, grid, kNT, 0, stream, slots, d_n, ctx->max_nnz, D4, (const double*)pieces,
+                             (const int32_t*)starts, partial + windows * cols));
+    HL_CUDA_TRY(launch_after(k_rows_total, 1, kTotalNT, 0, stream, (const double*)partial, n_partials, sumsq));
     note_launches(3);
     HL_LAUNCH_CHECK();
     return HL_OK;

@@ -85,9 +85,14 @@ cudaError_t launch_now(const void* func, dim3 grid, dim3 block, size_t smem, int
     if (cluster == 0) return cudaLaunchKernel(func, grid, block, args, smem, stream);
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = cluster;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    if (cluster == kAfterLast) {
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+    } else {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = cluster;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    }
     cfg.gridDim = grid;
     cfg.blockDim = block;
     cfg.dynamicSmemBytes = smem;
@@ -324,6 +329,7 @@ cudaError_t launch_kernel(const void* func, dim3 grid, dim3 block, size_t smem, 
                           const uint32_t* sizes, int n_args, cudaStream_t stream) {
     Collecting& c = t_now;
     if (!c.cache) return launch_now(func, grid, block, smem, cluster, args, stream);
+    if (cluster == kAfterLast) cluster = 0;
     if (c.stream != stream) {
         launch_flush();
         c.stream = stream;
