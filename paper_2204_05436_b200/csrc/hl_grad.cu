@@ -118,41 +118,42 @@ __device__ __forceinline__ double tile_squares(const T* __restrict__ p, int n) {
     return sum;
 }
 
-// (p and d may be the same)
+// As many values at a time as are 16 bytes in the wider type, so that a warp's stores are whole lines.  (p and d may be the same.)
 template <typename S, typename D>
 __device__ __forceinline__ void tile_scale(const S* p, D* d, int n, float f) {
-    constexpr int W = kWide<S>, kLine = W * sizeof(D) < 16 ? W * sizeof(D) : 16;       // bytes of a store
+    constexpr int W = sizeof(S) > sizeof(D) ? kWide<S> : kWide<D>, kIn = W * sizeof(S) / 4, kOut = W * sizeof(D) / 4;   // words
     const int head = head_of(p, n);
-    if (reinterpret_cast<uintptr_t>(d + head) % kLine) {       // no common lines
+    if (reinterpret_cast<uintptr_t>(d + head) % (kOut * 4)) {  // no common lines
 #pragma unroll 4
         for (int i = threadIdx.x; i < n; i += kNT) put(&d[i], f * to_f32(p[i]));
         return;
     }
     const int nv = (n - head) / W, tail = head + nv * W;
-    const uint4* q = reinterpret_cast<const uint4*>(p + head);
-    for (int i = threadIdx.x; i < nv; i += kNT * kAhead) {
-        uint4 r[kAhead];
+    constexpr int kFly = kIn == 4 ? kAhead : 2 * kAhead;
+    using In = std::conditional_t<kIn == 4, uint4, uint2>;
+    const In* q = reinterpret_cast<const In*>(p + head);
+    for (int i = threadIdx.x; i < nv; i += kNT * kFly) {
+        In r[kFly];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) r[u] = i + u * kNT < nv ? __ldcs(&q[i + u * kNT]) : make_uint4(0, 0, 0, 0);
+        for (int u = 0; u < kFly; ++u) r[u] = i + u * kNT < nv ? __ldcs(&q[i + u * kNT]) : In{};
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
+        for (int u = 0; u < kFly; ++u) {
             if (i + u * kNT >= nv) break;
+            constexpr int kPerIn = 4 / sizeof(S), kPerOut = 4 / sizeof(D);
             float x[W];
-            unpack4<S>(r[u], x);
+            unpack<S>(r[u].x, x);
+            unpack<S>(r[u].y, x + kPerIn);
+            if constexpr (kIn == 4) {
+                unpack<S>(r[u].z, x + 2 * kPerIn);
+                unpack<S>(r[u].w, x + 3 * kPerIn);
+            }
 #pragma unroll
             for (int j = 0; j < W; ++j) x[j] *= f;
-            constexpr int kWords = W * sizeof(D) / 4, kPer = 4 / sizeof(D);
-            uint32_t w[kWords];
-#pragma unroll
-            for (int j = 0; j < kWords; ++j) w[j] = pack<D>(x + j * kPer);
             D* to = d + head + (int64_t)(i + u * kNT) * W;
-            if constexpr (kWords == 2) {
-                *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < kWords; j += 4)
-                    *reinterpret_cast<uint4*>(to + j * kPer) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
-            }
+            if constexpr (kOut == 2)
+                *reinterpret_cast<uint2*>(to) = make_uint2(pack<D>(x), pack<D>(x + kPerOut));
+            else
+                *reinterpret_cast<uint4*>(to) = make_uint4(pack<D>(x), pack<D>(x + kPerOut), pack<D>(x + 2 * kPerOut), pack<D>(x + 3 * kPerOut));
         }
     }
     for (int i = threadIdx.x; i < head + n - tail; i += kNT) {
@@ -369,146 +370,156 @@ int32_t clip_call(const hl_tensor* ts, int32_t n, const double* further, int32_t
 
 // ---- an embedding's row gradients -----------------------------------------------------------------------------------
 // Sum over the distinct slots u of |sum over the lookups j of u of grad[bag(j)]|^2, from the (slot, bag) pairs sorted by slot.
-// A CTA takes windows of consecutive lookups, each of its groups of G lanes kRun of them and 4 * G columns; blockIdx.y: which
+// A CTA takes windows of consecutive lookups, each of its groups of G lanes a few of them and 4 * G columns; blockIdx.y: which
 // columns.  A group sums its lookups run by run in fp64; the pieces of a run over several groups meet in shared memory, and
 // those of a run over several windows go through `pieces` to k_rows_long.
-constexpr int kRun = 16;
 template <int G>
 struct RowShape {
-    static constexpr int kGroups = kNT / G, kWindow = kGroups * kRun;
+    static constexpr int kGroups = kNT / G, kRun = G < 16 ? G : 16, kWindow = kGroups * kRun;
 };
 
-__device__ __forceinline__ double square(const double a[4]) { return a[0] * a[0] + a[1] * a[1] + a[2] * a[2] + a[3] * a[3]; }
+__device__ __forceinline__ double square(const double (&a)[4]) { return a[0] * a[0] + a[1] * a[1] + a[2] * a[2] + a[3] * a[3]; }
 
 template <int G>
-__global__ void __launch_bounds__(kNT, 4) k_rows_squares(const int32_t* __restrict__ slots, const int32_t* __restrict__ bags,
+__global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int32_t* __restrict__ slots, const int32_t* __restrict__ bags,
                                                       const int32_t* __restrict__ d_n, int64_t max_n, int64_t n_slots,
                                                       int64_t n_bags, const float4* __restrict__ grad, int D4,
                                                       double* __restrict__ pieces, int32_t* __restrict__ starts,
-                                                      double* __restrict__ partial) {
+                                                      int64_t max_windows, double* __restrict__ partial) {
     using Shape = RowShape<G>;
-    constexpr int kGroups = Shape::kGroups, kWindow = Shape::kWindow, kRows = 4;
+    constexpr int kGroups = Shape::kGroups, kWindow = Shape::kWindow, kRun = Shape::kRun, kRows = kRun < 8 ? kRun : 8;
     __shared__ int32_t s_slot[kWindow + 2], s_bag[kWindow];    // s_slot[0]: the lookup before the window's
-    __shared__ double s_head[kNT][4];                          // of a run that an earlier group began, by lane
-    __shared__ bool s_cont[kGroups], s_whole[kGroups];
+    __shared__ __align__(16) double s_head[kNT][4];            // of a run that an earlier group began, by lane
+    __shared__ uint32_t s_whole[kGroups / 32 + 1];             // groups whose lookups are all of a run that goes on behind them
     let_next_start();
-    const int64_t n = min((int64_t)max(__ldg(d_n), 0), max_n), w = blockIdx.x, begin = w * kWindow;
+    const int64_t n = min((int64_t)max(__ldg(d_n), 0), max_n), windows = (n + kWindow - 1) / kWindow;
     const int g = threadIdx.x / G, sub = threadIdx.x % G, c = blockIdx.y * G + sub;
     const bool mine = c < D4;
-    const int here = (int)max((int64_t)0, min((int64_t)kWindow, n - begin));       // lookups of the window
-    for (int i = threadIdx.x; i < kWindow + 2; i += kNT) {
-        const int64_t at = begin - 1 + i;
-        s_slot[i] = at >= 0 && at < n ? __ldg(&slots[at]) : 0;
-        if (i < kWindow && i < here) {
-            const int32_t b = __ldg(&bags[begin + i]);
-            s_bag[i] = b >= 0 && b < n_bags ? b : -1;
+    double total = 0.0;
+    if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) starts[max_windows] = 0;      // (k_rows_long's tally)
+    // the next window's pairs are on their way while this one's rows are summed; two threads also take the lookups around it
+    constexpr bool kWhole = kWindow == kNT;
+    int32_t slot_ahead = 0, bag_ahead = 0, around_ahead = 0;
+    const auto ask = [&](int64_t w) {
+        const int64_t at = w * kWindow + threadIdx.x, around = threadIdx.x == 0 ? w * kWindow - 1 : (w + 1) * kWindow;
+        if ((kWhole || threadIdx.x < kWindow) && at < n) {
+            slot_ahead = __ldg(&slots[at]);
+            bag_ahead = __ldg(&bags[at]);
         }
-    }
-    __syncthreads();
-    const int l0 = g * kRun, len = max(0, min(kRun, here - l0));
-    double total = 0.0, acc[4] = {};
-    bool cont = false, whole = false, open = false;
-    if (len > 0) {
-        int32_t slot = s_slot[1 + l0];
-        cont = begin + l0 > 0 && s_slot[l0] == slot;
-        bool head = cont;                            // the run at hand began before this group's lookups
+        if (threadIdx.x < 2 && around >= 0 && around < n) around_ahead = __ldg(&slots[around]);
+    };
+    if (blockIdx.x < windows) ask(blockIdx.x);
+    for (int64_t w = blockIdx.x; w < windows; w += gridDim.x) {
+        const int64_t begin = w * kWindow;
+        const int here = (int)min((int64_t)kWindow, n - begin);    // lookups of the window
+        if (kWhole || threadIdx.x < kWindow) {
+            s_slot[1 + threadIdx.x] = slot_ahead;
+            s_bag[threadIdx.x] = bag_ahead >= 0 && bag_ahead < n_bags ? bag_ahead : -1;
+        }
+        if (threadIdx.x < 2) s_slot[threadIdx.x ? kWindow + 1 : 0] = around_ahead;
+        if (threadIdx.x <= kGroups / 32) s_whole[threadIdx.x] = 0;
+        __syncthreads();
+        if (w + gridDim.x < windows) ask(w + gridDim.x);
+        const int l0 = g * kRun, len = max(0, min(kRun, here - l0));
+        double acc[4] = {};
+        bool cont = false, whole = false, open = false;
+        if (len > 0) {
+            int32_t slot = s_slot[1 + l0];
+            cont = begin + l0 > 0 && s_slot[l0] == slot;
+            bool head = cont;                            // the run at hand began before this group's lookups
 #pragma unroll 1
-        for (int i0 = 0; i0 < len; i0 += kRows) {
-            float4 v[kRows];
+            for (int i0 = 0; i0 < len; i0 += kRows) {
+                float4 v[kRows];
 #pragma unroll
-            for (int j = 0; j < kRows; ++j) {
-                v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (i0 + j < len && mine) {
-                    const int32_t s = s_slot[1 + l0 + i0 + j], b = s_bag[l0 + i0 + j];
-                    if (s >= 0 && s < n_slots && b >= 0) v[j] = __ldg(&grad[(int64_t)b * D4 + c]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < kRows; ++j) {
-                if (i0 + j >= len) break;
-                const int32_t s = s_slot[1 + l0 + i0 + j];
-                if (s != slot) {                     // a run ends
-                    if (head) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) s_head[threadIdx.x][k] = acc[k];
-                    } else {
-                        total += square(acc);
+                for (int j = 0; j < kRows; ++j) {
+                    v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (i0 + j < len && mine) {
+                        const int32_t s = s_slot[1 + l0 + i0 + j], b = s_bag[l0 + i0 + j];
+                        if (s >= 0 && s < n_slots && b >= 0) v[j] = __ldg(&grad[(int64_t)b * D4 + c]);
                     }
-                    head = false;
-                    slot = s;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[k] = 0.0;
                 }
-                acc[0] += v[j].x;
-                acc[1] += v[j].y;
-                acc[2] += v[j].z;
-                acc[3] += v[j].w;
+#pragma unroll
+                for (int j = 0; j < kRows; ++j) {
+                    if (i0 + j >= len) break;
+                    const int32_t s = s_slot[1 + l0 + i0 + j];
+                    if (s != slot) {                     // a run ends
+                        if (head) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) s_head[threadIdx.x][k] = acc[k];
+                        } else {
+                            total += square(acc);
+                        }
+                        head = false;
+                        slot = s;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) acc[k] = 0.0;
+                    }
+                    acc[0] += v[j].x;
+                    acc[1] += v[j].y;
+                    acc[2] += v[j].z;
+                    acc[3] += v[j].w;
+                }
+            }
+            const bool goes_on = begin + l0 + len < n && s_slot[1 + l0 + len] == slot;
+            if (head) {                                  // one run, from before the first to the last of them
+                whole = goes_on;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s_head[threadIdx.x][k] = acc[k];
+            } else if (goes_on) {
+                open = true;
+            } else {
+                total += square(acc);
             }
         }
-        const bool goes_on = begin + l0 + len < n && s_slot[1 + l0 + len] == slot;
-        if (head) {                                  // one run, from before the first to the last of them
-            whole = goes_on;
+        if (sub == 0 && whole) atomicOr(&s_whole[g >> 5], 1u << (g & 31));
+        __syncthreads();
+        // The group that began a run puts it together, the window's first group also what an earlier window's run left here.  They
+        // add what groups first .. last - 1 left: those that are all the run's, and the one behind them, in which it ends.
+        const uint64_t mask = (uint64_t)s_whole[0] | (kGroups > 32 ? (uint64_t)s_whole[kGroups > 32] << 32 : 0);
+        const auto add_from = [&](int h, double (&a)[4]) {         // returns whether the run goes on into the next window
+            const uint64_t rest = h < 64 ? ~(mask >> h) : ~0ull;
+            const int last = h + (rest ? __ffsll((long long)rest) - 1 : 64);       // the group in which it ends
+#pragma unroll 4
+            for (; h <= last && h < kGroups; ++h) {
+                const double2 lo = *reinterpret_cast<const double2*>(&s_head[h * G + sub][0]);
+                const double2 hi = *reinterpret_cast<const double2*>(&s_head[h * G + sub][2]);
+                a[0] += lo.x;
+                a[1] += lo.y;
+                a[2] += hi.x;
+                a[3] += hi.y;
+            }
+            return last >= kGroups;
+        };
+        if (g == 0 && cont) {
+            double a[4] = {};
+            (void)add_from(0, a);
+            if (mine)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s_head[threadIdx.x][k] = acc[k];
-        } else if (goes_on) {
-            open = true;
-        } else {
-            total += square(acc);
+                for (int k = 0; k < 4; ++k) pieces[((w * 2 + 0) * D4 + c) * 4 + k] = a[k];
         }
-    }
-    if (sub == 0) {
-        s_cont[g] = cont;
-        s_whole[g] = whole;
-    }
-    __syncthreads();
-    // the group that began a run puts it together; the window's first group also what an earlier window's run left here
-    if (g == 0 && cont) {
-        double a[4];
+        bool out = false;
+        if (open) {
+            out = add_from(g + 1, acc);
+            if (!out) total += square(acc);
+            else if (mine)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) a[k] = s_head[sub][k];
-        for (int h = 1; h < kGroups && s_whole[h - 1] && s_cont[h]; ++h)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) a[k] += s_head[h * G + sub][k];
-        if (mine)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) pieces[((w * 2 + 0) * D4 + c) * 4 + k] = a[k];
-    }
-    bool out = false;                                // on into the next window
-    if (open) {
-        out = true;
-        for (int h = g + 1; out && h < kGroups; ++h) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) acc[k] += s_head[h * G + sub][k];
-            out = s_whole[h];
+                for (int k = 0; k < 4; ++k) pieces[((w * 2 + 1) * D4 + c) * 4 + k] = acc[k];
         }
-        if (!out) total += square(acc);
-        else if (mine)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) pieces[((w * 2 + 1) * D4 + c) * 4 + k] = acc[k];
+        const int any = __syncthreads_or(out);
+        if (threadIdx.x == 0 && blockIdx.y == 0) starts[w] = any;
     }
-    const int any = __syncthreads_or(out);
-    if (threadIdx.x == 0 && blockIdx.y == 0) starts[w] = any;
     total = block_sum(mine ? total : 0.0);
-    if (threadIdx.x == 0) partial[blockIdx.y * gridDim.x + w] = total;
+    if (threadIdx.x == 0) partial[blockIdx.y * gridDim.x + blockIdx.x] = total;
 }
 
-// The run over several windows that starts in window blockIdx.x, if one does.
+// The square of the run over several windows that starts in window w (a part of it per thread; all threads of the CTA call it).
 template <int G>
-__global__ void __launch_bounds__(kNT) k_rows_long(const int32_t* slots, const int32_t* d_n, int64_t max_n, int D4,
-                                                   const double* pieces, const int32_t* starts, double* partial) {
+__device__ __forceinline__ double long_run(const int32_t* slots, int64_t n, int D4, const double* pieces, int64_t w) {
     using Shape = RowShape<G>;
     constexpr int kGroups = Shape::kGroups, kWindow = Shape::kWindow;
     __shared__ double s_sum[kNT][4];
     __shared__ int s_first;
-    let_next_start();
-    wait_for_last();
-    const int64_t w = blockIdx.x;
-    double* to = &partial[blockIdx.y * gridDim.x + w];
-    if (!starts[w]) {
-        if (threadIdx.x == 0) *to = 0.0;
-        return;
-    }
-    const int64_t n = min((int64_t)max(*d_n, 0), max_n);
+    __syncthreads();
     const int g = threadIdx.x / G, sub = threadIdx.x % G, c = blockIdx.y * G + sub;
     const bool mine = c < D4;
     const int32_t slot = slots[(w + 1) * kWindow - 1];
@@ -540,33 +551,50 @@ __global__ void __launch_bounds__(kNT) k_rows_long(const int32_t* slots, const i
 #pragma unroll
     for (int k = 0; k < 4; ++k) s_sum[threadIdx.x][k] = a[k];
     __syncthreads();
-    double total = 0.0;
-    if (g == 0 && mine) {
-        for (int h = 1; h < kGroups; ++h)
+    if (g != 0 || !mine) return 0.0;
+    const int most = (int)min((int64_t)kGroups, last - w);     // groups that had a piece
+#pragma unroll 4
+    for (int h = 1; h < most; ++h)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) a[k] += s_sum[h * G + sub][k];
-        total = square(a);
-    }
-    total = block_sum(total);
-    if (threadIdx.x == 0) *to = total;
+        for (int k = 0; k < 4; ++k) a[k] += s_sum[h * G + sub][k];
+    return square(a);
 }
 
-constexpr int kTotalNT = 1024;
-__global__ void __launch_bounds__(kTotalNT) k_rows_total(const double* partial, int n_partials, double* sumsq) {
-    __shared__ double s[kTotalNT / 32];
+// Those runs; the last CTA to be done adds everything up.
+template <int G>
+__global__ void __launch_bounds__(kNT) k_rows_long(const int32_t* slots, const int32_t* d_n, int64_t max_n, int D4,
+                                                   const double* pieces, int32_t* starts, int64_t max_windows, double* partial,
+                                                   int n_partials, double* sumsq) {
+    __shared__ uint32_t s_starts[kWarps];
+    __shared__ bool s_last;
     wait_for_last();
-    double v = 0.0;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n_partials; i += kTotalNT) v += partial[i];
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+    const int64_t n = min((int64_t)max(*d_n, 0), max_n), windows = (n + RowShape<G>::kWindow - 1) / RowShape<G>::kWindow;
+    double total = 0.0;
+    for (int64_t w0 = blockIdx.x; w0 < windows; w0 += (int64_t)gridDim.x * kNT) {              // this CTA's windows, 256 at a time
+        const int64_t w = w0 + (int64_t)threadIdx.x * gridDim.x;
+        const uint32_t some = __ballot_sync(0xffffffffu, w < windows && starts[w] != 0);
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) s_starts[threadIdx.x >> 5] = some;
+        __syncthreads();
+        for (int i = 0; i < kWarps; ++i)
+            for (uint32_t left = s_starts[i]; left; left &= left - 1)
+                total += long_run<G>(slots, n, D4, pieces, w0 + (int64_t)(i * 32 + __ffs(left) - 1) * gridDim.x);
+    }
+    total = block_sum(total);
+    const int n_ctas = gridDim.x * gridDim.y;
+    if (threadIdx.x == 0) {
+        partial[n_partials - n_ctas + blockIdx.y * gridDim.x + blockIdx.x] = total;
+        __threadfence();
+        s_last = atomicAdd(&starts[max_windows], 1) == n_ctas - 1;
+    }
     __syncthreads();
-    if (threadIdx.x >= 32) return;
-    v = s[threadIdx.x];
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    if (threadIdx.x == 0) *sumsq = v;
+    if (!s_last) return;
+    __threadfence();
+    double sum = 0.0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n_partials; i += kNT) sum += __ldcg(&partial[i]);
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) *sumsq = sum;
 }
 
 // In the backward region: the pieces of runs over several windows where hl_embbag_bwd_apply keeps its own (a call of one window
@@ -576,21 +604,21 @@ template <int G>
 int32_t rows_squares(hl_ctx* ctx, const int32_t* slots, const int32_t* bags, const int32_t* d_n, const float* grad,
                      double* sumsq, cudaStream_t stream) {
     using Shape = RowShape<G>;
-    static_assert(Shape::kWindow >= 4 * kBwdChunk, "room for the pieces");
+    static_assert(Shape::kWindow >= 4 * kBwdChunk && Shape::kGroups <= 64, "room for the pieces");
     const int D4 = ctx->D / 4, cols = (int)div_up(D4, G);
     const int64_t windows = div_up(ctx->max_nnz > 0 ? ctx->max_nnz : 1, Shape::kWindow);
-    const int64_t n_partials = 2 * windows * cols;
+    const int rows_ctas = grid_for(windows, 1, (G < 32 ? 3 : 2) * ctx_sms(ctx)), long_ctas = grid_for(windows, 1, 2 * ctx_sms(ctx));
+    const int n_partials = (rows_ctas + long_ctas) * cols;
     double* pieces = reinterpret_cast<double*>(ctx->r.bwd_part);
     double* partial = reinterpret_cast<double*>(ctx->r.bwd_hist[1]);
     int32_t* starts = reinterpret_cast<int32_t*>(partial + n_partials);
-    if (n_partials * 2 + windows > sort_hist_words(ctx->max_nnz)) return HL_EINVAL;          // (rows of up to 1 024 fp32: never)
-    const dim3 grid((unsigned)windows, (unsigned)cols);
-    HL_CUDA_TRY(launch(k_rows_squares<G>, grid, kNT, stream, slots, bags, d_n, ctx->max_nnz, ctx->hot_cap + ctx->staging_cap,
-                       ctx->max_bags, reinterpret_cast<const float4*>(grad), D4, pieces, starts, partial));
-    HL_CUDA_TRY(launch_after(k_rows_long<G>, grid, kNT, 0, stream, slots, d_n, ctx->max_nnz, D4, (const double*)pieces,
-                             (const int32_t*)starts, partial + windows * cols));
-    HL_CUDA_TRY(launch_after(k_rows_total, 1, kTotalNT, 0, stream, (const double*)partial, n_partials, sumsq));
-    note_launches(3);
+    if (2 * n_partials + windows + 1 > sort_hist_words(ctx->max_nnz)) return HL_EINVAL;      // (rows of up to 1 024 fp32: never)
+    HL_CUDA_TRY(launch(k_rows_squares<G>, dim3((unsigned)rows_ctas, (unsigned)cols), kNT, stream, slots, bags, d_n, ctx->max_nnz,
+                       ctx->hot_cap + ctx->staging_cap, ctx->max_bags, reinterpret_cast<const float4*>(grad), D4, pieces, starts,
+                       windows, partial));
+    HL_CUDA_TRY(launch_after(k_rows_long<G>, dim3((unsigned)long_ctas, (unsigned)cols), kNT, 0, stream, slots, d_n, ctx->max_nnz,
+                             D4, (const double*)pieces, starts, windows, partial, n_partials, sumsq));
+    note_launches(2);
     HL_LAUNCH_CHECK();
     return HL_OK;
 }
