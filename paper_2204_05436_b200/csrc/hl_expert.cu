@@ -18,7 +18,7 @@ namespace {
 constexpr int kSortNT = 512, kSortWarps = kSortNT / 32, kItems = 16;
 constexpr int kSortChoices = kSortNT * kItems;       // most of a CTA
 constexpr int kExpertsPerThread = HL_MAX_EXPERTS / kSortNT + 1;
-static_assert(HL_MAX_EXPERTS <= 2 * kSortNT, "place_experts: two experts a thread");
+static_assert(HL_MAX_EXPERTS <= 1024 && HL_MAX_EXPERTS <= 2 * kSortNT, "place_experts: two experts a thread");
 constexpr uint32_t kNone = 0xffffu;
 
 // what the sort writes, and the words it goes by
@@ -53,15 +53,38 @@ __device__ __forceinline__ SortSmem sort_smem(uint32_t* base, int E) {
 }
 __device__ __forceinline__ int hist_pitch(int E) { return 2 * ((E + 1) / 2); }
 
-// The lanes with the same value of `bits` bits, among those that are valid.  (A match over the warp does it in one instruction,
+// The lanes with the same value of BITS bits, among those that are valid.  (A match over the warp does it in one instruction,
 // which takes the multiprocessor 60 cycles; a ballot a bit takes three: eight bits 24.)
-__device__ __forceinline__ unsigned same_value(unsigned v, bool valid, int bits) {
+template <int BITS>
+__device__ __forceinline__ unsigned same_value(unsigned v, bool valid) {
     unsigned peers = __ballot_sync(0xffffffffu, valid);
-    for (int b = 0; b < bits; ++b) {
-        const unsigned bit = (v >> b) & 1u;
-        peers &= __ballot_sync(0xffffffffu, bit) ^ (bit - 1u);
+#pragma unroll
+    for (int b = 0; b < BITS; ++b) {
+        const bool bit = v & (1u << b);
+        const unsigned with = __ballot_sync(0xffffffffu, bit);
+        peers &= bit ? with : ~with;
     }
     return peers;
+}
+
+// Ranks a warp's choices of `rounds` rounds: e in, packed out (expert in the upper 16 bits, kNone: none; rank in the warp), and
+// counts them into h.  Returns whether an id was no expert's.
+template <int BITS>
+__device__ __forceinline__ bool rank_rounds(const int e[kItems], int rounds, int E, uint16_t* h, uint32_t packed[kItems]) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        packed[i] = kNone << 16;
+        if (i >= rounds) continue;
+        const bool ok = (unsigned)e[i] < (unsigned)E;
+        bad = bad || (!ok && e[i] != -1);
+        const unsigned peers = same_value<BITS>((unsigned)e[i], ok), below = peers & lanemask_lt();
+        if (ok) packed[i] = ((uint32_t)e[i] << 16) | (h[e[i]] + __popc(below));
+        __syncwarp();
+        if (ok && below == 0) h[e[i]] = (uint16_t)(packed[i] + __popc(peers));
+        __syncwarp();
+    }
+    return bad;
 }
 
 // Ranks the CTA's choices [first, first + rounds * kSortNT) below n (of `most` that can be read).  packed[i]: expert (16 bits; kNone: none), rank in the warp.
@@ -76,22 +99,14 @@ __device__ __forceinline__ void rank_choices(const SortSmem& s, const int32_t* _
     for (int i = threadIdx.x; i < kSortWarps * pitch / 2; i += kSortNT) reinterpret_cast<uint32_t*>(s.warp_hist)[i] = 0;
     if (threadIdx.x == 0) s.hist[E] = 0;
     __syncthreads();
-    const int bits = 32 - __clz(E - 1);
     uint16_t* h = s.warp_hist + warp * pitch;
-    bool bad = false;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        packed[i] = kNone << 16;
-        if (i >= rounds) continue;
+    for (int i = 0; i < kItems; ++i)
         if (seg + i * 32 >= n) e[i] = -1;
-        const bool ok = e[i] >= 0 && e[i] < E;
-        bad = bad || (!ok && e[i] != -1);
-        const unsigned peers = same_value((unsigned)e[i], ok, bits), below = peers & lanemask_lt();
-        if (ok) packed[i] = ((uint32_t)e[i] << 16) | (h[e[i]] + __popc(below));
-        __syncwarp();
-        if (ok && below == 0) h[e[i]] = (uint16_t)((packed[i] & 0xffffu) + __popc(peers));
-        __syncwarp();
-    }
+    const bool bad = E <= 16    ? rank_rounds<4>(e, rounds, E, h, packed)
+                     : E <= 64  ? rank_rounds<6>(e, rounds, E, h, packed)
+                     : E <= 256 ? rank_rounds<8>(e, rounds, E, h, packed)
+                                : rank_rounds<10>(e, rounds, E, h, packed);
     if (__any_sync(0xffffffffu, bad) && lane == 0) atomicAdd(&s.hist[E], 1);
     __syncthreads();
     for (int x = threadIdx.x; x < E; x += kSortNT) {
@@ -287,9 +302,9 @@ __global__ void __launch_bounds__(256) k_expert_scan(int32_t* __restrict__ tile_
     if (lane == 0) totals[e] = before;
 }
 
-// A tile's choices are put in order of their rows in shared memory first, so that what `source` gets are runs: 32 choices of a
-// warp go to 32 places, and a multiprocessor writes about one line a cycle (2.1 M choices of 256 experts: 12.9 us without).
-__host__ __device__ constexpr size_t place_smem_bytes(int E) { return 16 * (size_t)(E + 1) + 2 * (size_t)kSortChoices; }
+// A tile's choices are put in order of their rows in shared memory first, so that what `source` gets are runs: written as they
+// come, 32 choices of a warp go to 32 lines.
+__host__ __device__ constexpr size_t place_smem_bytes(int E) { return 12 * (size_t)(E + 1) + 4 * (size_t)kSortChoices; }
 __global__ void __launch_bounds__(kSortNT) k_expert_place(const int32_t* n_tokens, int max_tokens, int top_k, int E,
                                                           int expert_cap, int align, int64_t cap_rows, int32_t* place,
                                                           int32_t* source, int32_t* counts, int32_t* offsets, int32_t* status,
@@ -300,8 +315,7 @@ __global__ void __launch_bounds__(kSortNT) k_expert_place(const int32_t* n_token
     s.hist = reinterpret_cast<int32_t*>(s_base);
     s.offset = s.hist + E + 1;
     s.count = s.offset + E + 1;
-    int32_t* s_first = s.count + E + 1;              // of an expert's choices, in the tile's order
-    uint16_t* s_choice = reinterpret_cast<uint16_t*>(s_first + E + 1);
+    uint32_t* s_order = reinterpret_cast<uint32_t*>(s.count + E + 1);      // expert (16 bits), choice of the tile
     const SortOut o{place, source, counts, offsets, status, cap_rows, expert_cap, align};
     const int n = live_choices(n_tokens, max_tokens, top_k), tiles = gridDim.x;
     const int rounds = (int)(((int64_t)n + (int64_t)tiles * kSortNT - 1) / ((int64_t)tiles * kSortNT));
@@ -314,47 +328,51 @@ __global__ void __launch_bounds__(kSortNT) k_expert_place(const int32_t* n_token
         const int j = i * kSortNT + threadIdx.x;
         packed[i] = j < here ? ranked[first + j] : kNone << 16;
     }
-    for (int e = threadIdx.x; e <= E; e += kSortNT) {
-        const int32_t* row = &tile_counts[(int64_t)e * tiles + blockIdx.x];
-        s.hist[e] = row[0];
-        s.count[e] = totals[e];
-        s_first[e] = ((int)blockIdx.x + 1 < tiles ? row[1] : s.count[e]) - s.hist[e];          // how many there are here
+    int in_tile[2], mine = 0;          // of the two experts that place_experts gives a thread
+    const int e0 = 2 * threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        in_tile[k] = 0;
+        if (e0 + k >= E) continue;
+        const int32_t* row = &tile_counts[(int64_t)(e0 + k) * tiles + blockIdx.x];
+        const int before = row[0], all = totals[e0 + k];
+        s.hist[e0 + k] = before;
+        s.count[e0 + k] = all;
+        in_tile[k] = ((int)blockIdx.x + 1 < tiles ? row[1] : all) - before;
+        mine += in_tile[k];
     }
+    const bool bad = totals[E] != 0;
     __syncthreads();
-    const bool bad = s.count[E] != 0;
     bool over;
     place_experts(s, E, o, &over);
     write_plan(s, o, E, blockIdx.x, gridDim.x, over, bad);
-    if (source) {
-        int sum[2], mine = 0;          // s_first: sums over the experts before
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        __shared__ int s_warp[kSortWarps];
+    __shared__ int s_warp[kSortWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int incl = mine;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int e = 2 * threadIdx.x + k;
-            sum[k] = e < E ? s_first[e] : 0;
-            mine += sum[k];
-        }
-        int incl = mine;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, d);
-            if (lane >= d) incl += v;
-        }
-        if (lane == 31) s_warp[warp] = incl;
-        __syncthreads();
-        int at = incl - mine;
-#pragma unroll
-        for (int w = 0; w < kSortWarps; ++w) at += w < warp ? s_warp[w] : 0;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int e = 2 * threadIdx.x + k;
-            if (e < E) s_first[e] = at;
-            at += sum[k];
-            if (e == E - 1) s_first[E] = at;
-        }
-        __syncthreads();
+    for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += v;
     }
+    if (lane == 31) s_warp[warp] = incl;
+    __syncthreads();
+    // from here on: hist: row of an expert's first choice in the tile, count: end of its rows, offset: its first choice in order
+    int at = incl - mine, in_order = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+        at += w < warp ? s_warp[w] : 0;
+        in_order += s_warp[w];
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (e0 + k >= E) continue;
+        const int off = s.offset[e0 + k];
+        s.hist[e0 + k] += off;
+        s.count[e0 + k] += off;
+        s.offset[e0 + k] = at;
+        at += in_tile[k];
+    }
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
         const int j = i * kSortNT + threadIdx.x;
@@ -362,20 +380,18 @@ __global__ void __launch_bounds__(kSortNT) k_expert_place(const int32_t* n_token
         const uint32_t e = packed[i] >> 16, rank = packed[i] & 0xffffu;
         int32_t row = -1;
         if (e != kNone) {
-            const int r = s.hist[e] + (int)rank;
-            if (r < s.count[e]) row = s.offset[e] + r;
-            if (source) s_choice[s_first[e] + rank] = (uint16_t)j;
+            row = s.hist[e] + (int)rank;
+            if (row >= s.count[e]) row = -1;
+            s_order[s.offset[e] + rank] = (e << 16) | (uint32_t)j;
         }
         place[first + j] = row;
     }
     if (!source) return;
     __syncthreads();
-    const int in_order = s_first[E];
     for (int j = threadIdx.x; j < in_order; j += kSortNT) {
-        const int64_t a = first + s_choice[j];
-        const uint32_t e = ranked[a] >> 16;
-        const int r = s.hist[e] + j - s_first[e];
-        if (r < s.count[e]) source[s.offset[e] + r] = (int32_t)a;
+        const uint32_t x = s_order[j], e = x >> 16;
+        const int row = s.hist[e] + j - s.offset[e];
+        if (row < s.count[e]) source[row] = (int32_t)first + (int32_t)(x & 0xffffu);
     }
 }
 
@@ -419,47 +435,52 @@ __device__ __forceinline__ int in_line(const T* p) {           // values between
     return (int)(reinterpret_cast<uintptr_t>(p) & 15) / (int)sizeof(T);
 }
 
-// 16 bytes from p on, whatever p's alignment, of a buffer [lo, hi); what lies outside of it reads as anything.  In two halves: the
-// two lines they lie in are asked for, into shared memory of the thread's own (registers for them would leave room for half as
-// many threads, and what bounds these kernels is how much is on its way), and what is wanted is put together from them.
+// 16 bytes from any place of a buffer on; what lies outside of it reads as anything.  In two halves: the two lines they lie in are
+// asked for, into shared memory of the thread's own (registers for them would leave room for half as many threads, and what
+// bounds these kernels is how much is on its way and how many instructions it takes), and what is wanted is put together from them.
 constexpr int kRowNT = 256;
 template <typename T>
-struct AnyLine {
-    uint4* slot;                       // two, kRowNT apart
-    const T *p, *lo, *hi;
-    __device__ __forceinline__ int shift() const { return (int)(reinterpret_cast<uintptr_t>(p) & 15); }
-    __device__ __forceinline__ bool inside() const {
-        const int s = shift();
-        const T* line = p - s / (int)sizeof(T);
-        return line >= lo && line + (s ? 2 * Vec<T>::N : Vec<T>::N) <= hi;
-    }
-    __device__ __forceinline__ void request(bool wanted) const {
-        const int s = shift();
-        const T* line = p - s / (int)sizeof(T);
-        if (!wanted || !inside()) return;
+struct Buffer {
+    const T* p;
+    int64_t values;
+    uint64_t most;                     // places N to most + N have two lines inside the buffer, whatever its alignment
+    __device__ __forceinline__ Buffer(const T* p_, int64_t values_)
+        : p(p_), values(values_), most(values_ > 3 * Vec<T>::N ? values_ - 3 * Vec<T>::N : 0) {}
+    // slot: two of the thread's, kRowNT apart.  Returns the bytes of the first line that are not wanted, or -1: to be read value
+    // by value.
+    __device__ __forceinline__ int request(int64_t at, uint4* slot) const {
+        if ((uint64_t)(at - Vec<T>::N) >= most) return -1;
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p + at), line = a & ~(uintptr_t)15;
         const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot);
         asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to), "l"(line) : "memory");
-        if (s) asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to + kRowNT * 16), "l"(line + Vec<T>::N) : "memory");
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to + kRowNT * 16), "l"(line + 16) : "memory");
+        return (int)(a & 15);
     }
-    // (wanted, and arrived)
-    __device__ __forceinline__ Vec<T> take() const {
+    __device__ __forceinline__ Vec<T> take(int s, const uint4* slot, int64_t at) const {
         Vec<T> r;
-        if (!inside()) {
+        if (s < 0) {
             r.raw = make_uint4(0, 0, 0, 0);
-#pragma unroll
+#pragma unroll 1
             for (int j = 0; j < Vec<T>::N; ++j)
-                if (p + j >= lo && p + j < hi) r.v[j] = p[j];
+                if (at + j >= 0 && at + j < values) {
+                    T x = p[at + j];
+#pragma unroll
+                    for (int i = 0; i < Vec<T>::N; ++i)
+                        if (i == j) r.v[i] = x;
+                }
             return r;
         }
-        const int s = shift();
         const uint4 a = slot[0], b = slot[kRowNT];
         const bool far = s & 8, odd = s & 4;
-        const int bits = (s & 3) * 8;
+        const int bits = s * 8;        // (a funnel shift takes it modulo 32)
         const uint32_t w0 = far ? a.z : a.x, w1 = far ? a.w : a.y, w2 = far ? b.x : a.z, w3 = far ? b.y : a.w,
                        w4 = far ? b.z : b.x, w5 = far ? b.w : b.y;
         const uint32_t x0 = odd ? w1 : w0, x1 = odd ? w2 : w1, x2 = odd ? w3 : w2, x3 = odd ? w4 : w3, x4 = odd ? w5 : w4;
-        r.raw = make_uint4(__funnelshift_r(x0, x1, bits), __funnelshift_r(x1, x2, bits), __funnelshift_r(x2, x3, bits),
-                           __funnelshift_r(x3, x4, bits));
+        if constexpr (sizeof(T) == 4)
+            r.raw = make_uint4(x0, x1, x2, x3);
+        else
+            r.raw = make_uint4(__funnelshift_r(x0, x1, bits), __funnelshift_r(x1, x2, bits), __funnelshift_r(x2, x3, bits),
+                               __funnelshift_r(x3, x4, bits));
         return r;
     }
 };
@@ -467,9 +488,11 @@ __device__ __forceinline__ void wait_lines() { asm volatile("cp.async.wait_all;"
 
 // values [e, e + N) of a row of dim values, as much of them as there is; row + e is a line's begin
 template <typename T>
+__device__ __forceinline__ bool whole_line(int e, int dim) { return e >= 0 && e + Vec<T>::N <= dim; }
+template <typename T>
 __device__ __forceinline__ void store_line(T* row, int e, int dim, const Vec<T>& v) {
     constexpr int N = Vec<T>::N;
-    if (e >= 0 && e + N <= dim) {
+    if (whole_line<T>(e, dim)) {
         *reinterpret_cast<uint4*>(row + e) = v.raw;
         return;
     }
@@ -499,19 +522,27 @@ __device__ __forceinline__ void zero_pads(int u, int units, int E, const int32_t
     }
 }
 
-// Which token and line a thread's item is: items are dealt out in turn, kItemsPerCta to a CTA.
+// Which token and line a thread's item is: items are dealt out in turn, kRowNT * U to a CTA.  (A division per thread would be a
+// good part of the kernels' instructions: the CTA's first item goes through fp64, the others are multiplied by 2^32 / lines, which
+// is right for less than 512 lines; from there on a CTA has at most two tokens.)
 template <int U>
 struct Items {
     int64_t t0;
-    unsigned r0;
+    unsigned r0, magic;
     int lines;
     __device__ __forceinline__ Items(int lines_) : lines(lines_) {
         const int64_t first = (int64_t)blockIdx.x * (kRowNT * U);
-        t0 = first / lines;
-        r0 = (unsigned)(first - t0 * lines);
+        t0 = (int64_t)((double)first * (1.0 / lines));
+        int64_t r = first - t0 * lines;
+        if (r < 0) --t0, r += lines;
+        if (r >= lines) ++t0, r -= lines;
+        r0 = (unsigned)r;
+        magic = lines < 512 ? 0xffffffffu / (unsigned)lines + 1 : 0;
     }
     __device__ __forceinline__ void get(int u, int64_t* t, int* line) const {
-        const unsigned i = r0 + u * kRowNT + threadIdx.x, q = i / (unsigned)lines;
+        const unsigned i = r0 + u * kRowNT + threadIdx.x;
+        unsigned q = lines == 1 ? i : __umulhi(i, magic);
+        if (lines >= 512) q = i >= (unsigned)lines;
         *t = t0 + q;
         *line = (int)(i - q * lines);
     }
@@ -533,7 +564,6 @@ __global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_dispatch(const T
         return;
     }
     const int tokens = live_choices(n_tokens, max_tokens, 1);
-    const T* end = x.at((int64_t)max_tokens - 1) + dim;
     const Items<U> items(lines);
     Vec<T> v[U];
     int64_t t[U];
@@ -556,22 +586,21 @@ __global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_dispatch(const T
                 for (int q = 0; q < KU; ++q)
                     if (row[q] >= 0 && row[q] < cap_rows) *reinterpret_cast<uint4*>(y.at(row[q]) + line[u] * N) = v[u].raw;
             } else {
-                __shared__ uint4 s_lines[2 * KU][kRowNT];
-                AnyLine<T> l[KU];
-                int e[KU];
-                bool ok[KU];
+                __shared__ uint4 s_lines[KU][2][kRowNT];
+                const Buffer<T> from(x_, (int64_t)(max_tokens - 1) * ld_x + dim);
+                int e[KU], s[KU];
 #pragma unroll
                 for (int q = 0; q < KU; ++q) {
-                    ok[q] = row[q] >= 0 && row[q] < cap_rows;
-                    e[q] = line[u] * N - in_line(y.at(ok[q] ? row[q] : 0));
-                    ok[q] = ok[q] && e[q] < dim;
-                    l[q] = {&s_lines[2 * q][threadIdx.x], x.at(t[u]) + e[q], x_, end};
-                    l[q].request(ok[q]);
+                    if (row[q] >= cap_rows) row[q] = -1;
+                    e[q] = line[u] * N - in_line(y.at(row[q]));
+                    if (e[q] >= dim) row[q] = -1;
+                    if (row[q] >= 0) s[q] = from.request(t[u] * ld_x + e[q], &s_lines[q][0][threadIdx.x]);
                 }
                 wait_lines();
 #pragma unroll
                 for (int q = 0; q < KU; ++q)
-                    if (ok[q]) store_line(y.at(row[q]), e[q], dim, l[q].take());
+                    if (row[q] >= 0)
+                        store_line(y.at(row[q]), e[q], dim, from.take(s[q], &s_lines[q][0][threadIdx.x], t[u] * ld_x + e[q]));
             }
         }
     }
@@ -602,22 +631,22 @@ __global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_combine(const T*
     for (int k0 = 0; k0 < top_k; k0 += KU) {
         float w[KU];
         if constexpr (ANY) {
-            __shared__ uint4 s_lines[KU * 2][kRowNT];
-            const T* end = y.at(cap_rows - 1) + dim;
-            AnyLine<T> l[KU];
+            __shared__ uint4 s_lines[KU][2][kRowNT];
+            const Buffer<T> from(y_, (cap_rows - 1) * ld_y + dim);
+            int64_t row[KU];
+            int s[KU];
 #pragma unroll
             for (int q = 0; q < KU; ++q) {
-                const int64_t row = k0 + q < top_k ? __ldg(&place[k0 + q]) : -1;
-                const bool ok = row >= 0 && row < cap_rows;
+                row[q] = k0 + q < top_k ? __ldg(&place[k0 + q]) : -1;
+                if (row[q] >= cap_rows) row[q] = -1;
                 w[q] = weights && k0 + q < top_k ? __ldg(&weights[k0 + q]) : 1.f;
-                l[q] = {&s_lines[q * 2][threadIdx.x], ok ? y.at(row) + e : nullptr, y_, end};
-                l[q].request(ok);
+                if (row[q] >= 0) s[q] = from.request(row[q] * ld_y + e, &s_lines[q][0][threadIdx.x]);
             }
             wait_lines();
 #pragma unroll
             for (int q = 0; q < KU; ++q) {
-                if (!l[q].p) continue;
-                const Vec<T> v = l[q].take();
+                if (row[q] < 0) continue;
+                const Vec<T> v = from.take(s[q], &s_lines[q][0][threadIdx.x], row[q] * ld_y + e);
 #pragma unroll
                 for (int j = 0; j < N; ++j) acc[j] = fmaf(w[q], to_f32(v.v[j]), acc[j]);
             }
@@ -663,7 +692,7 @@ __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd(
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = threadIdx.x & (P - 1);
     const int tokens = live_choices(n_tokens, max_tokens, 1);
     const int64_t t = (int64_t)blockIdx.x * (kRowNT / P) + threadIdx.x / P;
-    const T *go_end = go.at((int64_t)max_tokens - 1) + dim, *y_end = y.at(cap_rows - 1) + dim;
+    const Buffer<T> from_go(go_, (int64_t)(max_tokens - 1) * ld_go + dim), from_y(y_, (cap_rows - 1) * ld_y + dim);
     for (int k0 = 0; k0 < top_k; k0 += KU) {
         int64_t row[KU];
         float w[KU], dot[KU];
@@ -677,34 +706,32 @@ __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd(
         for (int l = sub; l < lines; l += P) {
             if (t >= tokens) break;
             if constexpr (ANY) {
-                __shared__ uint4 s_lines[4 * KU][kRowNT];
-                AnyLine<T> g[KU], v[KU];
-                int e[KU];
+                __shared__ uint4 s_lines[KU][4][kRowNT];
+                int e[KU], sg[KU], sy[KU];
                 bool ok[KU];
 #pragma unroll
                 for (int q = 0; q < KU; ++q) {
-                    const int64_t r = max(row[q], (int64_t)0);
-                    e[q] = l * N - in_line(gy.at(r));
+                    e[q] = l * N - in_line(gy.at(row[q]));
                     ok[q] = row[q] >= 0 && e[q] < dim;
-                    g[q] = {&s_lines[4 * q][threadIdx.x], go.at(t) + e[q], go_, go_end};
-                    v[q] = {&s_lines[4 * q + 2][threadIdx.x], y.at(r) + e[q], y_, y_end};
-                    g[q].request(ok[q]);
-                    v[q].request(ok[q] && grad_w);
+                    if (!ok[q]) continue;
+                    sg[q] = from_go.request(t * ld_go + e[q], &s_lines[q][0][threadIdx.x]);
+                    if (grad_w) sy[q] = from_y.request(row[q] * ld_y + e[q], &s_lines[q][2][threadIdx.x]);
                 }
                 wait_lines();
 #pragma unroll
                 for (int q = 0; q < KU; ++q) {
                     if (!ok[q]) continue;
-                    const Vec<T> a = g[q].take();
-                    Vec<T> b, r;
-                    b.raw = make_uint4(0, 0, 0, 0);
-                    if (grad_w) b = v[q].take();
+                    const Vec<T> a = from_go.take(sg[q], &s_lines[q][0][threadIdx.x], t * ld_go + e[q]);
+                    if (grad_w) {
+                        Vec<T> b = from_y.take(sy[q], &s_lines[q][2][threadIdx.x], row[q] * ld_y + e[q]);
+                        const bool whole = whole_line<T>(e[q], dim);
 #pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const float x = to_f32(a.v[j]);
-                        if (e[q] + j >= 0 && e[q] + j < dim) dot[q] = fmaf(x, to_f32(b.v[j]), dot[q]);
-                        r.v[j] = from_f32<T>(w[q] * x);
+                        for (int j = 0; j < N; ++j)
+                            if (whole || (e[q] + j >= 0 && e[q] + j < dim)) dot[q] = fmaf(to_f32(a.v[j]), to_f32(b.v[j]), dot[q]);
                     }
+                    Vec<T> r;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) r.v[j] = from_f32<T>(w[q] * to_f32(a.v[j]));
                     store_line(gy.at(row[q]), e[q], dim, r);
                 }
             } else {

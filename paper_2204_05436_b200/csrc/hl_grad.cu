@@ -388,13 +388,14 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
                                                       int64_t max_windows, double* __restrict__ partial) {
     using Shape = RowShape<G>;
     constexpr int kGroups = Shape::kGroups, kWindow = Shape::kWindow, kRun = Shape::kRun, kRows = kRun < 8 ? kRun : 8;
-    __shared__ int32_t s_slot[kWindow + 2], s_bag[kWindow];    // s_slot[0]: the lookup before the window's
+    __shared__ int32_t s_slot[kWindow + 2], s_bag[kWindow];    // s_slot[0]: the lookup before the window's; s_bag -1: none to add
     __shared__ __align__(16) double s_head[kNT][4];            // of a run that an earlier group began, by lane
     __shared__ uint32_t s_whole[kGroups / 32 + 1];             // groups whose lookups are all of a run that goes on behind them
     let_next_start();
     const int64_t n = min((int64_t)max(__ldg(d_n), 0), max_n), windows = (n + kWindow - 1) / kWindow;
     const int g = threadIdx.x / G, sub = threadIdx.x % G, c = blockIdx.y * G + sub;
     const bool mine = c < D4;
+    const int col = mine ? c : 0;
     double total = 0.0;
     if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) starts[max_windows] = 0;      // (k_rows_long's tally)
     // the next window's pairs are on their way while this one's rows are summed; two threads also take the lookups around it
@@ -414,7 +415,8 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
         const int here = (int)min((int64_t)kWindow, n - begin);    // lookups of the window
         if (kWhole || threadIdx.x < kWindow) {
             s_slot[1 + threadIdx.x] = slot_ahead;
-            s_bag[threadIdx.x] = bag_ahead >= 0 && bag_ahead < n_bags ? bag_ahead : -1;
+            const bool adds = (int)threadIdx.x < here && bag_ahead >= 0 && bag_ahead < n_bags && slot_ahead >= 0 && slot_ahead < n_slots;
+            s_bag[threadIdx.x] = adds ? bag_ahead : -1;
         }
         if (threadIdx.x < 2) s_slot[threadIdx.x ? kWindow + 1 : 0] = around_ahead;
         if (threadIdx.x <= kGroups / 32) s_whole[threadIdx.x] = 0;
@@ -429,15 +431,12 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
             bool head = cont;                            // the run at hand began before this group's lookups
 #pragma unroll 1
             for (int i0 = 0; i0 < len; i0 += kRows) {
-                float4 v[kRows];
+                float4 v[kRows];                     // (all of them asked for, whether they add anything or not: no branches)
+                int32_t b[kRows];
 #pragma unroll
-                for (int j = 0; j < kRows; ++j) {
-                    v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (i0 + j < len && mine) {
-                        const int32_t s = s_slot[1 + l0 + i0 + j], b = s_bag[l0 + i0 + j];
-                        if (s >= 0 && s < n_slots && b >= 0) v[j] = __ldg(&grad[(int64_t)b * D4 + c]);
-                    }
-                }
+                for (int j = 0; j < kRows; ++j) b[j] = s_bag[l0 + i0 + j];
+#pragma unroll
+                for (int j = 0; j < kRows; ++j) v[j] = __ldg(&grad[(int64_t)max(b[j], 0) * D4 + col]);
 #pragma unroll
                 for (int j = 0; j < kRows; ++j) {
                     if (i0 + j >= len) break;
@@ -454,10 +453,12 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
 #pragma unroll
                         for (int k = 0; k < 4; ++k) acc[k] = 0.0;
                     }
-                    acc[0] += v[j].x;
-                    acc[1] += v[j].y;
-                    acc[2] += v[j].z;
-                    acc[3] += v[j].w;
+                    if (b[j] >= 0) {
+                        acc[0] += v[j].x;
+                        acc[1] += v[j].y;
+                        acc[2] += v[j].z;
+                        acc[3] += v[j].w;
+                    }
                 }
             }
             const bool goes_on = begin + l0 + len < n && s_slot[1 + l0 + len] == slot;
@@ -512,73 +513,88 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
     if (threadIdx.x == 0) partial[blockIdx.y * gridDim.x + blockIdx.x] = total;
 }
 
-// The square of the run over several windows that starts in window w (a part of it per thread; all threads of the CTA call it).
+// The sum of a run's pieces: the one in window w, in which it starts, and those of the windows up to `last`, by P threads of which
+// this is number `i`: group i / G of P / G.
 template <int G>
-__device__ __forceinline__ double long_run(const int32_t* slots, int64_t n, int D4, const double* pieces, int64_t w) {
-    using Shape = RowShape<G>;
-    constexpr int kGroups = Shape::kGroups, kWindow = Shape::kWindow;
-    __shared__ double s_sum[kNT][4];
-    __shared__ int s_first;
-    __syncthreads();
-    const int g = threadIdx.x / G, sub = threadIdx.x % G, c = blockIdx.y * G + sub;
-    const bool mine = c < D4;
-    const int32_t slot = slots[(w + 1) * kWindow - 1];
-    if (threadIdx.x == 0) s_first = kNT;
-    __syncthreads();
-    int64_t last = w + 1;                            // the window in which the run ends
-    for (;; last += kNT) {
-        const int64_t next = (last + threadIdx.x + 1) * kWindow;
-        const bool ends = next >= n || slots[next] != slot;
-        if (ends) atomicMin(&s_first, (int)threadIdx.x);
-        if (__syncthreads_or(ends)) break;
-    }
-    last += s_first;
-    double a[4] = {};
-    if (mine) {
-        if (g == 0)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) a[k] = pieces[((w * 2 + 1) * D4 + c) * 4 + k];
-#pragma unroll 4
-        for (int64_t x = w + 1 + g; x <= last; x += kGroups) {
-            const double2* p = reinterpret_cast<const double2*>(&pieces[((x * 2 + 0) * D4 + c) * 4]);
-            const double2 lo = p[0], hi = p[1];
-            a[0] += lo.x;
-            a[1] += lo.y;
-            a[2] += hi.x;
-            a[3] += hi.y;
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) s_sum[threadIdx.x][k] = a[k];
-    __syncthreads();
-    if (g != 0 || !mine) return 0.0;
-    const int most = (int)min((int64_t)kGroups, last - w);     // groups that had a piece
-#pragma unroll 4
-    for (int h = 1; h < most; ++h)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) a[k] += s_sum[h * G + sub][k];
-    return square(a);
+__device__ __forceinline__ void add_pieces(const double* pieces, int D4, int c, int64_t w, int64_t last, int i, int P, double (&a)[4]) {
+    const auto add = [&](int64_t at) {
+        const double2* p = reinterpret_cast<const double2*>(&pieces[(at * D4 + c) * 4]);
+        const double2 lo = p[0], hi = p[1];
+        a[0] += lo.x;
+        a[1] += lo.y;
+        a[2] += hi.x;
+        a[3] += hi.y;
+    };
+    if (i / G == 0) add(w * 2 + 1);
+#pragma unroll 8
+    for (int64_t x = w + 1 + i / G; x <= last; x += P / G) add(x * 2);
 }
 
-// Those runs; the last CTA to be done adds everything up.
+// The runs over several windows, each where it starts: a warp takes a window, and a run that goes on for more than 32 others is
+// the whole CTA's.  The last CTA to be done adds everything up.
 template <int G>
 __global__ void __launch_bounds__(kNT) k_rows_long(const int32_t* slots, const int32_t* d_n, int64_t max_n, int D4,
                                                    const double* pieces, int32_t* starts, int64_t max_windows, double* partial,
                                                    int n_partials, double* sumsq) {
-    __shared__ uint32_t s_starts[kWarps];
+    using Shape = RowShape<G>;
+    constexpr int kGroups = Shape::kGroups, kWindow = Shape::kWindow;
+    __shared__ double s_sum[kNT][4];
+    __shared__ int64_t s_long[kWarps];
+    __shared__ int s_first;
     __shared__ bool s_last;
     wait_for_last();
-    const int64_t n = min((int64_t)max(*d_n, 0), max_n), windows = (n + RowShape<G>::kWindow - 1) / RowShape<G>::kWindow;
+    const int64_t n = min((int64_t)max(*d_n, 0), max_n), windows = (n + kWindow - 1) / kWindow;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % G, c = blockIdx.y * G + sub;
+    const bool mine = c < D4;
     double total = 0.0;
-    for (int64_t w0 = blockIdx.x; w0 < windows; w0 += (int64_t)gridDim.x * kNT) {              // this CTA's windows, 256 at a time
-        const int64_t w = w0 + (int64_t)threadIdx.x * gridDim.x;
-        const uint32_t some = __ballot_sync(0xffffffffu, w < windows && starts[w] != 0);
+    for (int64_t w0 = (int64_t)blockIdx.x * kWarps; w0 < windows; w0 += (int64_t)gridDim.x * kWarps) {
+        const int64_t w = w0 + warp;
+        bool too_long = false;
+        if (w < windows && starts[w]) {
+            const int32_t slot = slots[(w + 1) * kWindow - 1];
+            const int64_t next = (w + 2 + lane) * kWindow;
+            const unsigned ends = __ballot_sync(0xffffffffu, next >= n || slots[next] != slot);
+            too_long = ends == 0;
+            if (!too_long) {
+                double a[4] = {};
+                if (mine) add_pieces<G>(pieces, D4, c, w, w + __ffs(ends), lane, 32, a);
+#pragma unroll
+                for (int d = 16; d >= G; d >>= 1)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) a[k] += __shfl_xor_sync(0xffffffffu, a[k], d);
+                if (lane < G && mine) total += square(a);
+            }
+        }
+        if (lane == 0) s_long[warp] = too_long ? w : -1;
         __syncthreads();
-        if ((threadIdx.x & 31) == 0) s_starts[threadIdx.x >> 5] = some;
+        for (int i = 0; i < kWarps; ++i) {
+            const int64_t x = s_long[i];
+            if (x < 0) continue;                     // (the same for all threads)
+            const int32_t slot = slots[(x + 1) * kWindow - 1];
+            if (threadIdx.x == 0) s_first = kNT;
+            __syncthreads();
+            int64_t last = x + 33;                   // the window in which the run ends
+            for (;; last += kNT) {
+                const int64_t next = (last + threadIdx.x + 1) * kWindow;
+                const bool ends = next >= n || slots[next] != slot;
+                if (ends) atomicMin(&s_first, (int)threadIdx.x);
+                if (__syncthreads_or(ends)) break;
+            }
+            double a[4] = {};
+            if (mine) add_pieces<G>(pieces, D4, c, x, last + s_first, threadIdx.x, kNT, a);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s_sum[threadIdx.x][k] = a[k];
+            __syncthreads();
+            if (threadIdx.x < G && mine) {
+#pragma unroll 8
+                for (int h = 1; h < kGroups; ++h)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) a[k] += s_sum[h * G + sub][k];
+                total += square(a);
+            }
+            __syncthreads();
+        }
         __syncthreads();
-        for (int i = 0; i < kWarps; ++i)
-            for (uint32_t left = s_starts[i]; left; left &= left - 1)
-                total += long_run<G>(slots, n, D4, pieces, w0 + (int64_t)(i * 32 + __ffs(left) - 1) * gridDim.x);
     }
     total = block_sum(total);
     const int n_ctas = gridDim.x * gridDim.y;
@@ -607,7 +623,7 @@ int32_t rows_squares(hl_ctx* ctx, const int32_t* slots, const int32_t* bags, con
     static_assert(Shape::kWindow >= 4 * kBwdChunk && Shape::kGroups <= 64, "room for the pieces");
     const int D4 = ctx->D / 4, cols = (int)div_up(D4, G);
     const int64_t windows = div_up(ctx->max_nnz > 0 ? ctx->max_nnz : 1, Shape::kWindow);
-    const int rows_ctas = grid_for(windows, 1, (G < 32 ? 3 : 2) * ctx_sms(ctx)), long_ctas = grid_for(windows, 1, 2 * ctx_sms(ctx));
+    const int rows_ctas = grid_for(windows, 1, (G < 32 ? 3 : 2) * ctx_sms(ctx)), long_ctas = grid_for(windows, kWarps, 2 * ctx_sms(ctx));
     const int n_partials = (rows_ctas + long_ctas) * cols;
     double* pieces = reinterpret_cast<double*>(ctx->r.bwd_part);
     double* partial = reinterpret_cast<double*>(ctx->r.bwd_hist[1]);
