@@ -15,17 +15,13 @@ namespace {
 // A stable counting sort of the choices by expert.  The choices are dealt out evenly, a run of them to each CTA and of those one
 // to each warp, which takes 32 at a time: the choices of one expert among them rank by lane, behind those the warp has counted
 // before.  A choice's row is: rows of the experts before + choices of the expert in CTAs before + in warps before + in the warp.
-constexpr int kSortNT = 512, kSortWarps = kSortNT / 32, kItems = 16;
-constexpr int kSortChoices = kSortNT * kItems;       // most of a CTA
-constexpr int kExpertsPerThread = HL_MAX_EXPERTS / kSortNT + 1;
-static_assert(HL_MAX_EXPERTS <= 1024 && HL_MAX_EXPERTS <= 2 * kSortNT, "place_experts: two experts a thread");
+// (Choices are counted in 32 bits: there are less than 2^30.)
 constexpr uint32_t kNone = 0xffffu;
 
 // what the sort writes, and the words it goes by
 struct SortOut {
     int32_t *place, *source, *counts, *offsets, *status;
-    int64_t cap_rows;
-    int32_t expert_cap, align;
+    int cap_rows, expert_cap, align;
 };
 
 __device__ __forceinline__ int live_choices(const int32_t* n_tokens, int max_tokens, int top_k) {
@@ -34,184 +30,190 @@ __device__ __forceinline__ int live_choices(const int32_t* n_tokens, int max_tok
     return t * top_k;
 }
 
-struct SortSmem {
-    uint16_t* warp_hist;               // [kSortWarps][E]; then choices of the expert in the warps before
+// CTAs of NT threads with at most ITEMS rounds of 32 choices per warp.
+template <int NT, int ITEMS>
+struct Sort {
+    static constexpr int kWarps = NT / 32, kChoices = NT * ITEMS, kPer = HL_MAX_EXPERTS / NT;     // experts of a thread
+    static_assert(HL_MAX_EXPERTS == 1024 && kChoices <= 32768, "ten bits of expert, ranks of 15");
+
+    uint16_t* warp_hist;               // [kWarps][E]; then choices of the expert in the warps before
     int32_t* hist;                     // [E + 1] of this CTA, [E]: ids that are no expert's; then of the CTAs before
     int32_t* offset;                   // [E + 1]
     int32_t* count;                    // [E + 1]
+    int E, pitch;
+
+    static constexpr size_t smem_bytes(int E) { return 4 * ((size_t)kWarps * ((E + 1) / 2) + 3 * (size_t)(E + 1)); }
+
+    __device__ __forceinline__ Sort(uint32_t* base, int E_) : E(E_), pitch(2 * ((E_ + 1) / 2)) {
+        warp_hist = reinterpret_cast<uint16_t*>(base);
+        hist = reinterpret_cast<int32_t*>(base + kWarps * (pitch / 2));
+        offset = hist + E + 1;
+        count = offset + E + 1;
+    }
+
+    // The lanes with the same value of BITS bits, among those that are valid.  (A match over the warp does it in one
+    // instruction, which takes the multiprocessor 60 cycles; a ballot a bit takes three: eight bits 24.)
+    template <int BITS>
+    static __device__ __forceinline__ unsigned same_value(unsigned v, bool valid) {
+        unsigned peers = __ballot_sync(0xffffffffu, valid);
+#pragma unroll
+        for (int b = 0; b < BITS; ++b) {
+            const unsigned bit = (v >> b) & 1u;
+            peers &= __ballot_sync(0xffffffffu, bit) ^ (bit - 1u);           // those with the bit, or those without
+        }
+        return peers;
+    }
+
+    // A warp's rounds: e in, packed out (expert in the upper 16 bits, kNone: none; rank in the warp), counted into h.
+    template <int BITS>
+    __device__ __forceinline__ void rank_rounds(const int (&e)[ITEMS], int rounds, uint16_t* h, uint32_t (&packed)[ITEMS]) const {
+        const unsigned lt = lanemask_lt();
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            packed[i] = kNone << 16;
+            if (i >= rounds) continue;
+            const bool ok = e[i] >= 0;
+            const unsigned peers = same_value<BITS>((unsigned)e[i], ok), below = peers & lt;
+            if (ok) packed[i] = ((uint32_t)e[i] << 16) | (h[e[i]] + __popc(below));
+            __syncwarp();
+            if (ok && below == 0) h[e[i]] = (uint16_t)(packed[i] + __popc(peers));
+            __syncwarp();
+        }
+    }
+
+    // Ranks the CTA's choices [first, first + rounds * NT) below n, of `most` that can be read, and counts them: warp_hist, hist.
+    __device__ __forceinline__ void rank(const int32_t* __restrict__ experts, int first, int rounds, int n, int most,
+                                         uint32_t (&packed)[ITEMS]) const {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seg = first + warp * (rounds * 32) + lane;
+        int e[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) e[i] = i < rounds && seg + i * 32 < most ? __ldg(&experts[seg + i * 32]) : -1;
+        for (int i = threadIdx.x; i < kWarps * pitch / 2; i += NT) reinterpret_cast<uint32_t*>(warp_hist)[i] = 0;
+        if (threadIdx.x == 0) hist[E] = 0;
+        __syncthreads();
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (seg + i * 32 >= n) e[i] = -1;
+            if ((unsigned)e[i] >= (unsigned)E) {
+                bad = bad || e[i] != -1;
+                e[i] = -1;
+            }
+        }
+        uint16_t* h = warp_hist + warp * pitch;
+        if (E <= 16) rank_rounds<4>(e, rounds, h, packed);
+        else if (E <= 64) rank_rounds<6>(e, rounds, h, packed);
+        else if (E <= 256) rank_rounds<8>(e, rounds, h, packed);
+        else rank_rounds<10>(e, rounds, h, packed);
+        if (__any_sync(0xffffffffu, bad) && lane == 0) atomicAdd(&hist[E], 1);
+        __syncthreads();
+        for (int x = threadIdx.x; x < E; x += NT) {
+            int c[kWarps], sum = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) c[w] = warp_hist[w * pitch + x];
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                warp_hist[w * pitch + x] = (uint16_t)sum;
+                sum += c[w];
+            }
+            hist[x] = sum;
+        }
+        __syncthreads();
+    }
+
+    // Sum of v over the threads before; *all: over all of them.
+    static __device__ __forceinline__ int before(int v, int* all) {
+        __shared__ int s_warp[kWarps];
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        int incl = v;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += x;
+        }
+        __syncthreads();
+        if (lane == 31) s_warp[warp] = incl;
+        __syncthreads();
+        int at = incl - v;
+        *all = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            at += w < warp ? s_warp[w] : 0;
+            *all += s_warp[w];
+        }
+        return at;
+    }
+
+    // count holds every expert's choices: turns them into the rows it gets and their offsets, both inside cap_rows.  Returns
+    // whether some did not fit.  (All rows together, filled up: less than 2^30 + 2^26.)  A thread has kPer experts in a row.
+    __device__ __forceinline__ bool place(const SortOut& o) const {
+        int rows[kPer], cnt[kPer], sum = 0, all;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int e = kPer * threadIdx.x + k;
+            rows[k] = cnt[k] = 0;
+            if (e >= E) continue;
+            cnt[k] = count[e];
+            if (o.expert_cap > 0) cnt[k] = min(cnt[k], o.expert_cap);
+            rows[k] = o.align == 1 ? cnt[k] : (int)((uint32_t)(cnt[k] + o.align - 1) / (uint32_t)o.align) * o.align;
+            sum += rows[k];
+        }
+        int at = before(sum, &all);
+        bool mine = false;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int e = kPer * threadIdx.x + k;
+            if (e >= E) break;
+            mine = mine || at + cnt[k] > o.cap_rows;
+            offset[e] = min(at, o.cap_rows);
+            count[e] = min(cnt[k], max(o.cap_rows - at, 0));
+            at += rows[k];
+        }
+        if (threadIdx.x == 0) offset[E] = min(all, o.cap_rows);
+        return __syncthreads_or(mine) != 0;
+    }
+
+    // The rows that fill an expert up, and the plan's words, by CTA `cta` of `ctas`.
+    __device__ __forceinline__ void write_plan(const SortOut& o, int cta, int ctas, bool over, bool bad) const {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        if (o.source && o.align > 1)
+            for (int e = cta * kWarps + warp; e < E; e += ctas * kWarps)
+                for (int r = offset[e] + count[e] + lane; r < offset[e + 1]; r += 32) o.source[r] = -1;
+        if (cta != 0) return;
+        for (int e = threadIdx.x; e < E; e += NT) {
+            o.counts[e] = count[e];
+            o.offsets[e] = offset[e];
+        }
+        if (threadIdx.x == 0) {
+            o.offsets[E] = offset[E];
+            if (o.status) *o.status = bad ? HL_EBOUNDS : over ? HL_ECAPACITY : HL_OK;
+        }
+    }
 };
-__host__ __device__ constexpr size_t sort_smem_words(int E) {
-    return (size_t)kSortWarps * ((E + 1) / 2) + 3 * (size_t)(E + 1);
-}
-__device__ __forceinline__ SortSmem sort_smem(uint32_t* base, int E) {
-    SortSmem s;
-    s.warp_hist = reinterpret_cast<uint16_t*>(base);
-    s.hist = reinterpret_cast<int32_t*>(base + kSortWarps * ((E + 1) / 2));
-    s.offset = s.hist + E + 1;
-    s.count = s.offset + E + 1;
-    return s;
-}
-__device__ __forceinline__ int hist_pitch(int E) { return 2 * ((E + 1) / 2); }
-
-// The lanes with the same value of BITS bits, among those that are valid.  (A match over the warp does it in one instruction,
-// which takes the multiprocessor 60 cycles; a ballot a bit takes three: eight bits 24.)
-template <int BITS>
-__device__ __forceinline__ unsigned same_value(unsigned v, bool valid) {
-    unsigned peers = __ballot_sync(0xffffffffu, valid);
-#pragma unroll
-    for (int b = 0; b < BITS; ++b) {
-        const bool bit = v & (1u << b);
-        const unsigned with = __ballot_sync(0xffffffffu, bit);
-        peers &= bit ? with : ~with;
-    }
-    return peers;
-}
-
-// Ranks a warp's choices of `rounds` rounds: e in, packed out (expert in the upper 16 bits, kNone: none; rank in the warp), and
-// counts them into h.  Returns whether an id was no expert's.
-template <int BITS>
-__device__ __forceinline__ bool rank_rounds(const int e[kItems], int rounds, int E, uint16_t* h, uint32_t packed[kItems]) {
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        packed[i] = kNone << 16;
-        if (i >= rounds) continue;
-        const bool ok = (unsigned)e[i] < (unsigned)E;
-        bad = bad || (!ok && e[i] != -1);
-        const unsigned peers = same_value<BITS>((unsigned)e[i], ok), below = peers & lanemask_lt();
-        if (ok) packed[i] = ((uint32_t)e[i] << 16) | (h[e[i]] + __popc(below));
-        __syncwarp();
-        if (ok && below == 0) h[e[i]] = (uint16_t)(packed[i] + __popc(peers));
-        __syncwarp();
-    }
-    return bad;
-}
-
-// Ranks the CTA's choices [first, first + rounds * kSortNT) below n (of `most` that can be read).  packed[i]: expert (16 bits; kNone: none), rank in the warp.
-// s.hist and s.warp_hist as above.
-__device__ __forceinline__ void rank_choices(const SortSmem& s, const int32_t* __restrict__ experts, int64_t first, int rounds,
-                                             int64_t n, int64_t most, int E, uint32_t packed[kItems]) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = hist_pitch(E);
-    const int64_t seg = first + warp * (rounds * 32) + lane;
-    int e[kItems];
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) e[i] = i < rounds && seg + i * 32 < most ? __ldg(&experts[seg + i * 32]) : -1;
-    for (int i = threadIdx.x; i < kSortWarps * pitch / 2; i += kSortNT) reinterpret_cast<uint32_t*>(s.warp_hist)[i] = 0;
-    if (threadIdx.x == 0) s.hist[E] = 0;
-    __syncthreads();
-    uint16_t* h = s.warp_hist + warp * pitch;
-#pragma unroll
-    for (int i = 0; i < kItems; ++i)
-        if (seg + i * 32 >= n) e[i] = -1;
-    const bool bad = E <= 16    ? rank_rounds<4>(e, rounds, E, h, packed)
-                     : E <= 64  ? rank_rounds<6>(e, rounds, E, h, packed)
-                     : E <= 256 ? rank_rounds<8>(e, rounds, E, h, packed)
-                                : rank_rounds<10>(e, rounds, E, h, packed);
-    if (__any_sync(0xffffffffu, bad) && lane == 0) atomicAdd(&s.hist[E], 1);
-    __syncthreads();
-    for (int x = threadIdx.x; x < E; x += kSortNT) {
-        int c[kSortWarps], sum = 0;
-#pragma unroll
-        for (int w = 0; w < kSortWarps; ++w) c[w] = s.warp_hist[w * pitch + x];
-#pragma unroll
-        for (int w = 0; w < kSortWarps; ++w) {
-            s.warp_hist[w * pitch + x] = (uint16_t)sum;
-            sum += c[w];
-        }
-        s.hist[x] = sum;
-    }
-    __syncthreads();
-}
-
-// s.count holds every expert's choices: turns them into the rows it gets and their offsets, both inside cap_rows.
-// *over: rows that did not fit.  (All rows together, filled up: less than 2^30 + 2^26.)
-__device__ __forceinline__ void place_experts(const SortSmem& s, int E, const SortOut& o, bool* over) {
-    __shared__ int s_warp[kSortWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cap = (int)o.cap_rows;
-    int rows[2], cnt[2], sum = 0;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {      // two neighbouring experts a thread
-        const int e = 2 * threadIdx.x + k;
-        cnt[k] = e < E ? s.count[e] : 0;
-        if (o.expert_cap > 0) cnt[k] = min(cnt[k], o.expert_cap);
-        rows[k] = o.align == 1 ? cnt[k] : (int)((uint32_t)(cnt[k] + o.align - 1) / (uint32_t)o.align) * o.align;
-        sum += rows[k];
-    }
-    int incl = sum;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += v;
-    }
-    if (lane == 31) s_warp[warp] = incl;
-    __syncthreads();
-    int at = incl - sum;
-#pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) at += w < warp ? s_warp[w] : 0;
-    bool mine = false;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int e = 2 * threadIdx.x + k;
-        if (e < E) {
-            mine = mine || at + cnt[k] > cap;
-            s.offset[e] = min(at, cap);
-            s.count[e] = min(cnt[k], max(cap - at, 0));
-            if (e == E - 1) s.offset[E] = min(at + rows[k], cap);
-        }
-        at += rows[k];
-    }
-    *over = __syncthreads_or(mine) != 0;
-}
-
-// The rows that fill an expert up, and the plan's words, by CTA `cta` of `ctas`.
-__device__ __forceinline__ void write_plan(const SortSmem& s, const SortOut& o, int E, int cta, int ctas, bool over, bool bad) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (o.source && o.align > 1)
-        for (int e = cta * kSortWarps + warp; e < E; e += ctas * kSortWarps)
-            for (int r = s.offset[e] + s.count[e] + lane; r < s.offset[e + 1]; r += 32) o.source[r] = -1;
-    if (cta != 0) return;
-    for (int e = threadIdx.x; e < E; e += kSortNT) {
-        o.counts[e] = s.count[e];
-        o.offsets[e] = s.offset[e];
-    }
-    if (threadIdx.x == 0) {
-        o.offsets[E] = s.offset[E];
-        if (o.status) *o.status = bad ? HL_EBOUNDS : over ? HL_ECAPACITY : HL_OK;
-    }
-}
-
-__device__ __forceinline__ void write_place(const SortSmem& s, const SortOut& o, int64_t a, uint32_t e, int rank) {
-    int32_t row = -1;
-    if (e != kNone) {
-        const int r = s.hist[e] + rank;
-        if (r < s.count[e]) row = s.offset[e] + r;
-    }
-    o.place[a] = row;
-    if (row >= 0 && o.source) o.source[row] = (int32_t)a;
-}
 
 // All of it in one cluster, whose CTAs read each other's counts.
-template <int CTAS>
-__global__ void __launch_bounds__(kSortNT) k_expert_sort(const int32_t* __restrict__ experts, const int32_t* n_tokens,
-                                                         int max_tokens, int top_k, int E, int expert_cap, int align,
-                                                         int64_t cap_rows, int32_t* place, int32_t* source, int32_t* counts,
-                                                         int32_t* offsets, int32_t* status) {
+template <int CTAS, int NT, int ITEMS>
+__global__ void __launch_bounds__(NT) k_expert_sort(const int32_t* __restrict__ experts, const int32_t* n_tokens,
+                                                    int max_tokens, int top_k, int E, int expert_cap, int align, int cap_rows,
+                                                    int32_t* place, int32_t* source, int32_t* counts, int32_t* offsets,
+                                                    int32_t* status) {
     extern __shared__ uint32_t s_base[];
-    const SortSmem s = sort_smem(s_base, E);
+    const Sort<NT, ITEMS> s(s_base, E);
     const SortOut o{place, source, counts, offsets, status, cap_rows, expert_cap, align};
     const int n = live_choices(n_tokens, max_tokens, top_k);
     // (one CTA asks for what there can be at once, rather than wait for how many there are)
-    const int rounds = ((CTAS == 1 ? max_tokens * top_k : n) + CTAS * kSortNT - 1) / (CTAS * kSortNT);
-    const int first = (int)blockIdx.x * rounds * kSortNT;
-    uint32_t packed[kItems];
-    rank_choices(s, experts, first, rounds, n, CTAS == 1 ? max_tokens * top_k : n, E, packed);
+    const int most = CTAS == 1 ? max_tokens * top_k : n, rounds = (most + CTAS * NT - 1) / (CTAS * NT);
+    const int first = (int)blockIdx.x * rounds * NT;
+    uint32_t packed[ITEMS];
+    s.rank(experts, first, rounds, n, most, packed);
     if constexpr (CTAS > 1) {
+        constexpr int kMine = HL_MAX_EXPERTS / NT + 1;
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
-        int before[kExpertsPerThread] = {};
+        int before[kMine] = {};
 #pragma unroll
-        for (int k = 0; k < kExpertsPerThread; ++k) {
-            const int e = threadIdx.x + k * kSortNT;
+        for (int k = 0; k < kMine; ++k) {
+            const int e = threadIdx.x + k * NT;
             if (e > E) break;
             int v[CTAS], all = 0;
 #pragma unroll
@@ -225,146 +227,144 @@ __global__ void __launch_bounds__(kSortNT) k_expert_sort(const int32_t* __restri
         }
         cluster.sync();                // (nobody reads this CTA's counts any more)
 #pragma unroll
-        for (int k = 0; k < kExpertsPerThread; ++k) {
-            const int e = threadIdx.x + k * kSortNT;
+        for (int k = 0; k < kMine; ++k) {
+            const int e = threadIdx.x + k * NT;
             if (e <= E) s.hist[e] = before[k];
         }
     } else {
-        for (int e = threadIdx.x; e <= E; e += kSortNT) {
+        for (int e = threadIdx.x; e <= E; e += NT) {
             s.count[e] = s.hist[e];
             s.hist[e] = 0;
         }
     }
     __syncthreads();
     const bool bad = s.count[E] != 0;
-    bool over;
-    place_experts(s, E, o, &over);
+    const bool over = s.place(o);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
         const int a = first + (warp * rounds + i) * 32 + lane;
+        if (i >= rounds || a >= n) continue;
         const uint32_t e = packed[i] >> 16;
-        if (i < rounds && a < n)
-            write_place(s, o, a, e, (int)(packed[i] & 0xffffu) + (e == kNone ? 0 : s.warp_hist[warp * hist_pitch(E) + e]));
+        int32_t row = -1;
+        if (e != kNone) {
+            const int r = s.hist[e] + s.warp_hist[warp * s.pitch + e] + (int)(packed[i] & 0xffffu);
+            if (r < s.count[e]) row = s.offset[e] + r;
+        }
+        place[a] = row;
+        if (row >= 0 && source) source[row] = a;
     }
-    write_plan(s, o, E, blockIdx.x, CTAS, over, bad);
+    s.write_plan(o, blockIdx.x, CTAS, over, bad);
 }
 
 // In three kernels: every tile's choices ranked (their expert and rank in the tile, as packed above, into `ranked`) and
-// counted, sums of the counts over the tiles before, places.  tile_counts: [E + 1][tiles].
-__global__ void __launch_bounds__(kSortNT) k_expert_rank(const int32_t* __restrict__ experts, const int32_t* n_tokens,
+// counted, sums of the counts over the tiles before, places.  tile_counts: [tiles][E + 1].
+constexpr int kTileNT = 512, kTileItems = 16;
+using Tile = Sort<kTileNT, kTileItems>;
+__device__ __forceinline__ int tile_rounds(int n, int tiles) {
+    return (int)(((int64_t)n + (int64_t)tiles * kTileNT - 1) / ((int64_t)tiles * kTileNT));
+}
+
+__global__ void __launch_bounds__(kTileNT) k_expert_rank(const int32_t* __restrict__ experts, const int32_t* n_tokens,
                                                          int max_tokens, int top_k, int E, int32_t* __restrict__ tile_counts,
                                                          uint32_t* __restrict__ ranked) {
     extern __shared__ uint32_t s_base[];
     let_next_start();
-    const SortSmem s = sort_smem(s_base, E);
-    const int n = live_choices(n_tokens, max_tokens, top_k), tiles = gridDim.x;
-    const int rounds = (int)(((int64_t)n + (int64_t)tiles * kSortNT - 1) / ((int64_t)tiles * kSortNT));
-    const int64_t first = (int64_t)blockIdx.x * rounds * kSortNT;
-    uint32_t packed[kItems];
-    rank_choices(s, experts, first, rounds, n, n, E, packed);
-    for (int e = threadIdx.x; e <= E; e += kSortNT) tile_counts[(int64_t)e * tiles + blockIdx.x] = s.hist[e];
+    const Tile s(s_base, E);
+    const int n = live_choices(n_tokens, max_tokens, top_k), tiles = gridDim.x, rounds = tile_rounds(n, tiles);
+    const int first = min((int64_t)blockIdx.x * rounds * kTileNT, (int64_t)n);
+    uint32_t packed[kTileItems];
+    s.rank(experts, first, rounds, n, n, packed);
+    for (int e = threadIdx.x; e <= E; e += kTileNT) tile_counts[(int64_t)blockIdx.x * (E + 1) + e] = s.hist[e];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        const int64_t a = first + (warp * rounds + i) * 32 + lane;
+    for (int i = 0; i < kTileItems; ++i) {
+        const int a = first + (warp * rounds + i) * 32 + lane;
         const uint32_t e = packed[i] >> 16;
-        if (i < rounds && a < n) ranked[a] = e == kNone ? packed[i] : packed[i] + s.warp_hist[warp * hist_pitch(E) + e];
+        if (i < rounds && a < n) ranked[a] = e == kNone ? packed[i] : packed[i] + s.warp_hist[warp * s.pitch + e];
     }
 }
 
-// tile_counts[e][t] := sum over the tiles before t; totals[e].  A warp takes an expert.
-__global__ void __launch_bounds__(256) k_expert_scan(int32_t* __restrict__ tile_counts, int tiles, int E,
-                                                     int32_t* __restrict__ totals) {
+// tile_counts[t][e] := sum over the tiles before t; totals[e].  A CTA takes 32 experts, its warps a run of tiles each.
+constexpr int kScanNT = 1024;
+__global__ void __launch_bounds__(kScanNT) k_expert_scan(int32_t* __restrict__ tile_counts, int tiles, int E,
+                                                         int32_t* __restrict__ totals) {
+    constexpr int kWarps = kScanNT / 32, kAhead = 16;
+    __shared__ int s_sum[kWarps][32];
     let_next_start();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = (int)blockIdx.x * 32 + lane;
+    const int per = (tiles + kWarps - 1) / kWarps, t0 = min(warp * per, tiles), t1 = min(t0 + per, tiles);
+    int32_t* column = tile_counts + min(e, E);
     wait_for_last();
-    const int lane = threadIdx.x & 31, e = (int)(blockIdx.x * 8 + (threadIdx.x >> 5));
-    if (e > E) return;
-    int32_t* row = tile_counts + (int64_t)e * tiles;
-    constexpr int kAhead = 8;
+    int c[kAhead], sum = 0;            // the first of the run's tiles stay in registers
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) c[i] = t0 + i < t1 ? column[(int64_t)(t0 + i) * (E + 1)] : 0;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) sum += c[i];
+    for (int t = t0 + kAhead; t < t1; ++t) sum += column[(int64_t)t * (E + 1)];
+    s_sum[warp][lane] = sum;
+    __syncthreads();
     int before = 0;
-    for (int t0 = 0; t0 < tiles; t0 += 32 * kAhead) {
-        int c[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) c[i] = t0 + i * 32 + lane < tiles ? row[t0 + i * 32 + lane] : 0;
+    for (int w = 0; w < kWarps; ++w) before += w < warp ? s_sum[w][lane] : 0;
+    if (e > E) return;
+    if (warp == kWarps - 1) totals[e] = before + sum;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            int incl = c[i];
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += v;
-            }
-            if (t0 + i * 32 + lane < tiles) row[t0 + i * 32 + lane] = before + incl - c[i];
-            before += __shfl_sync(0xffffffffu, incl, 31);
-        }
+    for (int i = 0; i < kAhead; ++i) {
+        if (t0 + i < t1) column[(int64_t)(t0 + i) * (E + 1)] = before;
+        before += c[i];
     }
-    if (lane == 0) totals[e] = before;
+    for (int t = t0 + kAhead; t < t1; ++t) {
+        const int x = column[(int64_t)t * (E + 1)];
+        column[(int64_t)t * (E + 1)] = before;
+        before += x;
+    }
 }
 
 // A tile's choices are put in order of their rows in shared memory first, so that what `source` gets are runs: written as they
 // come, 32 choices of a warp go to 32 lines.
-__host__ __device__ constexpr size_t place_smem_bytes(int E) { return 12 * (size_t)(E + 1) + 4 * (size_t)kSortChoices; }
-__global__ void __launch_bounds__(kSortNT) k_expert_place(const int32_t* n_tokens, int max_tokens, int top_k, int E,
-                                                          int expert_cap, int align, int64_t cap_rows, int32_t* place,
+constexpr size_t place_smem_bytes(int E) { return 12 * (size_t)(E + 1) + 4 * (size_t)Tile::kChoices; }
+__global__ void __launch_bounds__(kTileNT) k_expert_place(const int32_t* n_tokens, int max_tokens, int top_k, int E,
+                                                          int expert_cap, int align, int cap_rows, int32_t* place,
                                                           int32_t* source, int32_t* counts, int32_t* offsets, int32_t* status,
                                                           const int32_t* tile_counts, const int32_t* totals,
                                                           const uint32_t* ranked) {
     extern __shared__ uint32_t s_base[];
-    SortSmem s{};
+    Tile s(s_base, E);
     s.hist = reinterpret_cast<int32_t*>(s_base);
     s.offset = s.hist + E + 1;
     s.count = s.offset + E + 1;
     uint32_t* s_order = reinterpret_cast<uint32_t*>(s.count + E + 1);      // expert (16 bits), choice of the tile
     const SortOut o{place, source, counts, offsets, status, cap_rows, expert_cap, align};
-    const int n = live_choices(n_tokens, max_tokens, top_k), tiles = gridDim.x;
-    const int rounds = (int)(((int64_t)n + (int64_t)tiles * kSortNT - 1) / ((int64_t)tiles * kSortNT));
-    const int64_t first = (int64_t)blockIdx.x * rounds * kSortNT;
-    const int here = (int)max((int64_t)0, min((int64_t)rounds * kSortNT, n - first));
+    const int n = live_choices(n_tokens, max_tokens, top_k), tiles = gridDim.x, rounds = tile_rounds(n, tiles);
+    const int first = min((int64_t)blockIdx.x * rounds * kTileNT, (int64_t)n), here = min(rounds * kTileNT, n - first);
     wait_for_last();
-    uint32_t packed[kItems];
+    uint32_t packed[kTileItems];
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        const int j = i * kSortNT + threadIdx.x;
+    for (int i = 0; i < kTileItems; ++i) {
+        const int j = i * kTileNT + threadIdx.x;
         packed[i] = j < here ? ranked[first + j] : kNone << 16;
     }
-    int in_tile[2], mine = 0;          // of the two experts that place_experts gives a thread
-    const int e0 = 2 * threadIdx.x;
+    int in_tile[Tile::kPer], mine = 0;                         // of the experts that place() gives a thread
+    const int e0 = Tile::kPer * threadIdx.x;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < Tile::kPer; ++k) {
         in_tile[k] = 0;
         if (e0 + k >= E) continue;
-        const int32_t* row = &tile_counts[(int64_t)(e0 + k) * tiles + blockIdx.x];
+        const int32_t* row = &tile_counts[(int64_t)blockIdx.x * (E + 1) + e0 + k];
         const int before = row[0], all = totals[e0 + k];
         s.hist[e0 + k] = before;
         s.count[e0 + k] = all;
-        in_tile[k] = ((int)blockIdx.x + 1 < tiles ? row[1] : all) - before;
+        in_tile[k] = ((int)blockIdx.x + 1 < tiles ? row[E + 1] : all) - before;
         mine += in_tile[k];
     }
     const bool bad = totals[E] != 0;
-    __syncthreads();
-    bool over;
-    place_experts(s, E, o, &over);
-    write_plan(s, o, E, blockIdx.x, gridDim.x, over, bad);
-    __shared__ int s_warp[kSortWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int incl = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += v;
-    }
-    if (lane == 31) s_warp[warp] = incl;
-    __syncthreads();
+    const bool over = s.place(o);
+    s.write_plan(o, blockIdx.x, gridDim.x, over, bad);
     // from here on: hist: row of an expert's first choice in the tile, count: end of its rows, offset: its first choice in order
-    int at = incl - mine, in_order = 0;
+    int in_order, at = Tile::before(mine, &in_order);
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) {
-        at += w < warp ? s_warp[w] : 0;
-        in_order += s_warp[w];
-    }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < Tile::kPer; ++k) {
         if (e0 + k >= E) continue;
         const int off = s.offset[e0 + k];
         s.hist[e0 + k] += off;
@@ -374,8 +374,8 @@ __global__ void __launch_bounds__(kSortNT) k_expert_place(const int32_t* n_token
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-        const int j = i * kSortNT + threadIdx.x;
+    for (int i = 0; i < kTileItems; ++i) {
+        const int j = i * kTileNT + threadIdx.x;
         if (j >= here) continue;
         const uint32_t e = packed[i] >> 16, rank = packed[i] & 0xffffu;
         int32_t row = -1;
@@ -388,15 +388,16 @@ __global__ void __launch_bounds__(kSortNT) k_expert_place(const int32_t* n_token
     }
     if (!source) return;
     __syncthreads();
-    for (int j = threadIdx.x; j < in_order; j += kSortNT) {
+    for (int j = threadIdx.x; j < in_order; j += kTileNT) {
         const uint32_t x = s_order[j], e = x >> 16;
         const int row = s.hist[e] + j - s.offset[e];
-        if (row < s.count[e]) source[row] = (int32_t)first + (int32_t)(x & 0xffffu);
+        if (row < s.count[e]) source[row] = first + (int)(x & 0xffffu);
     }
 }
 
+// Which of them sorts n choices.
 constexpr int kClusterCtas = 8;
-constexpr int64_t kOneCluster = (int64_t)kClusterCtas * kSortChoices;
+constexpr int64_t kFewChoices = 128 * 4, kSomeChoices = kClusterCtas * 512 * 4, kOneCluster = kClusterCtas * 512 * 16;
 
 // ---- rows -----------------------------------------------------------------------------------------------------------
 // Values move 16 bytes at a time.  Where every row of a call begins at a multiple of 16 bytes (ANY = false), a vector is one
@@ -427,8 +428,8 @@ __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2hal
 template <typename T>
 struct Rows {
     T* p;
-    int64_t ld;
-    __device__ __forceinline__ T* at(int64_t r) const { return p + r * ld; }
+    int ld;
+    __device__ __forceinline__ T* at(int r) const { return p + (int64_t)r * ld; }
 };
 template <typename T>
 __device__ __forceinline__ int in_line(const T* p) {           // values between the 16-byte line's begin and p
@@ -510,52 +511,50 @@ __host__ __device__ constexpr int lines_of(int64_t dim, bool any) {
 // Rows that fill experts up: CTA u of units x E takes every units-th of expert u % E's.
 template <typename T>
 __device__ __forceinline__ void zero_pads(int u, int units, int E, const int32_t* __restrict__ counts,
-                                          const int32_t* __restrict__ offsets, int64_t cap_rows, Rows<T> y, int dim) {
-    const int e = u % E, part = u / E;
-    const int64_t first = __ldg(&offsets[e]), count = __ldg(&counts[e]), end = min((int64_t)__ldg(&offsets[e + 1]), cap_rows);
+                                          const int32_t* __restrict__ offsets, int cap_rows, Rows<T> y, int dim) {
+    const int e = u % E, part = u / E, end = min(__ldg(&offsets[e + 1]), cap_rows);
+    const int64_t first = __ldg(&offsets[e]), count = __ldg(&counts[e]);
     if (first < 0 || count < 0) return;
     Vec<T> zero;
     zero.raw = make_uint4(0, 0, 0, 0);
     for (int64_t r = first + count + part; r < end; r += units) {
-        T* row = y.at(r);
+        T* row = y.at((int)r);
         for (int e0 = -in_line(row) + (int)threadIdx.x * Vec<T>::N; e0 < dim; e0 += kRowNT * Vec<T>::N) store_line(row, e0, dim, zero);
     }
 }
 
-// Which token and line a thread's item is: items are dealt out in turn, kRowNT * U to a CTA.  (A division per thread would be a
-// good part of the kernels' instructions: the CTA's first item goes through fp64, the others are multiplied by 2^32 / lines, which
-// is right for less than 512 lines; from there on a CTA has at most two tokens.)
+// Which token and line a thread's item is: items are dealt out in turn, kRowNT * U to a CTA.  Divisions would be a good part of the
+// kernels' instructions: the host gives 2^64 / lines, rounded up (exact quotients for less than 2^40 items and lines below 2^24), and
+// inside a CTA the token before is followed by at most one more from 512 lines on, below which 2^32 / lines does.
 template <int U>
 struct Items {
-    int64_t t0;
+    int t0;
     unsigned r0, magic;
     int lines;
-    __device__ __forceinline__ Items(int lines_) : lines(lines_) {
-        const int64_t first = (int64_t)blockIdx.x * (kRowNT * U);
-        t0 = (int64_t)((double)first * (1.0 / lines));
-        int64_t r = first - t0 * lines;
-        if (r < 0) --t0, r += lines;
-        if (r >= lines) ++t0, r -= lines;
-        r0 = (unsigned)r;
-        magic = lines < 512 ? 0xffffffffu / (unsigned)lines + 1 : 0;
+    __device__ __forceinline__ Items(int lines_, uint64_t inverse) : lines(lines_) {
+        const uint64_t first = (uint64_t)blockIdx.x * (kRowNT * U);
+        t0 = lines == 1 ? (int)first : (int)__umul64hi(first, inverse);
+        r0 = (unsigned)(first - (uint64_t)t0 * lines);
+        magic = (unsigned)((inverse + 0xffffffffu) >> 32);
     }
-    __device__ __forceinline__ void get(int u, int64_t* t, int* line) const {
+    __device__ __forceinline__ void get(int u, int* t, int* line) const {
         const unsigned i = r0 + u * kRowNT + threadIdx.x;
-        unsigned q = lines == 1 ? i : __umulhi(i, magic);
-        if (lines >= 512) q = i >= (unsigned)lines;
-        *t = t0 + q;
+        const unsigned q = lines == 1 ? i : lines >= 512 ? i >= (unsigned)lines : __umulhi(i, magic);
+        *t = t0 + (int)q;
         *line = (int)(i - q * lines);
     }
 };
+uint64_t inverse_of(int lines) { return lines == 1 ? 0 : ~uint64_t(0) / lines + 1; }
 
 // y[place[t, k]] = x[t].  A thread takes a line of a token's row, which it reads once for all of the token's rows.
 template <typename T, bool ANY, int U>
-__global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_dispatch(const T* __restrict__ x_, int64_t ld_x, const int32_t* n_tokens,
-                                                            int max_tokens, int top_k, int dim,
-                                                            const int32_t* __restrict__ place, int64_t cap_rows,
-                                                            T* __restrict__ y_, int64_t ld_y, int lines, int row_ctas, int E,
-                                                            int pad_units, const int32_t* __restrict__ counts,
-                                                            const int32_t* __restrict__ offsets) {
+__global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_dispatch(const T* __restrict__ x_, int ld_x,
+                                                                         const int32_t* n_tokens, int max_tokens, int top_k,
+                                                                         int dim, const int32_t* __restrict__ place,
+                                                                         int cap_rows, T* __restrict__ y_, int ld_y, int lines,
+                                                                         uint64_t inverse, int row_ctas, int E, int pad_units,
+                                                                         const int32_t* __restrict__ counts,
+                                                                         const int32_t* __restrict__ offsets) {
     constexpr int N = Vec<T>::N, KU = 4;
     const Rows<const T> x{x_, ld_x};
     const Rows<T> y{y_, ld_y};
@@ -564,10 +563,9 @@ __global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_dispatch(const T
         return;
     }
     const int tokens = live_choices(n_tokens, max_tokens, 1);
-    const Items<U> items(lines);
+    const Items<U> items(lines, inverse);
     Vec<T> v[U];
-    int64_t t[U];
-    int line[U];
+    int t[U], line[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         items.get(u, &t[u], &line[u]);
@@ -577,109 +575,118 @@ __global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_dispatch(const T
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (t[u] >= tokens) continue;
+        const int32_t* at = place + t[u] * top_k;
         for (int k0 = 0; k0 < top_k; k0 += KU) {
-            int64_t row[KU];
+            int row[KU];
 #pragma unroll
-            for (int q = 0; q < KU; ++q) row[q] = k0 + q < top_k ? __ldg(&place[t[u] * top_k + k0 + q]) : -1;
+            for (int q = 0; q < KU; ++q) {
+                row[q] = k0 + q < top_k ? __ldg(&at[k0 + q]) : -1;
+                if (row[q] >= cap_rows) row[q] = -1;
+            }
             if constexpr (!ANY) {
 #pragma unroll
                 for (int q = 0; q < KU; ++q)
-                    if (row[q] >= 0 && row[q] < cap_rows) *reinterpret_cast<uint4*>(y.at(row[q]) + line[u] * N) = v[u].raw;
+                    if (row[q] >= 0) *reinterpret_cast<uint4*>(y.at(row[q]) + line[u] * N) = v[u].raw;
             } else {
                 __shared__ uint4 s_lines[KU][2][kRowNT];
                 const Buffer<T> from(x_, (int64_t)(max_tokens - 1) * ld_x + dim);
+                const int64_t x_at = (int64_t)t[u] * ld_x;
                 int e[KU], s[KU];
 #pragma unroll
                 for (int q = 0; q < KU; ++q) {
-                    if (row[q] >= cap_rows) row[q] = -1;
                     e[q] = line[u] * N - in_line(y.at(row[q]));
                     if (e[q] >= dim) row[q] = -1;
-                    if (row[q] >= 0) s[q] = from.request(t[u] * ld_x + e[q], &s_lines[q][0][threadIdx.x]);
+                    if (row[q] >= 0) s[q] = from.request(x_at + e[q], &s_lines[q][0][threadIdx.x]);
                 }
                 wait_lines();
 #pragma unroll
                 for (int q = 0; q < KU; ++q)
                     if (row[q] >= 0)
-                        store_line(y.at(row[q]), e[q], dim, from.take(s[q], &s_lines[q][0][threadIdx.x], t[u] * ld_x + e[q]));
+                        store_line(y.at(row[q]), e[q], dim, from.take(s[q], &s_lines[q][0][threadIdx.x], x_at + e[q]));
             }
         }
     }
 }
 
 // out[t] = sum over k of w[t, k] * y[place[t, k]], in fp32, in the order of k, rounded once.  (Without weights: the sum.)  A
-// thread takes a line of out, and KU of the token's rows at a time.
-template <typename T, bool ANY, int KU>
-__global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_combine(const T* __restrict__ y_, int64_t ld_y, int64_t cap_rows,
-                                                           const int32_t* n_tokens, int max_tokens, int top_k, int dim,
-                                                           const int32_t* __restrict__ place,
-                                                           const float* __restrict__ weights, T* __restrict__ out_,
-                                                           int64_t ld_out, int lines) {
+// thread takes a line of out, or U of them one after the other, and KU of the token's rows at a time.
+template <typename T, bool ANY, int KU, int U>
+__global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_combine(const T* __restrict__ y_, int ld_y, int cap_rows,
+                                                                        const int32_t* n_tokens, int max_tokens, int top_k,
+                                                                        int dim, const int32_t* __restrict__ place,
+                                                                        const float* __restrict__ weights,
+                                                                        T* __restrict__ out_, int ld_out, int lines,
+                                                                        uint64_t inverse) {
     constexpr int N = Vec<T>::N;
     const Rows<const T> y{y_, ld_y};
     const Rows<T> out{out_, ld_out};
     const int tokens = live_choices(n_tokens, max_tokens, 1);
-    int64_t t;
-    int line;
-    Items<1>(lines).get(0, &t, &line);
-    if (t >= tokens) return;
-    T* to = out.at(t);
-    const int e = line * N - (ANY ? in_line(to) : 0);
-    if (ANY && e >= dim) return;
-    place += t * top_k;
-    if (weights) weights += t * top_k;
-    float acc[N] = {};
-    for (int k0 = 0; k0 < top_k; k0 += KU) {
-        float w[KU];
-        if constexpr (ANY) {
-            __shared__ uint4 s_lines[KU][2][kRowNT];
-            const Buffer<T> from(y_, (cap_rows - 1) * ld_y + dim);
-            int64_t row[KU];
-            int s[KU];
+    const Items<U> items(lines, inverse);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        int t, line;
+        items.get(u, &t, &line);
+        if (t >= tokens) return;
+        T* to = out.at(t);
+        const int e = line * N - (ANY ? in_line(to) : 0);
+        if (ANY && e >= dim) continue;
+        const int32_t* at = place + t * top_k;
+        const float* w_at = weights + t * top_k;
+        float acc[N] = {};
+        for (int k0 = 0; k0 < top_k; k0 += KU) {
+            int row[KU];
+            float w[KU];
 #pragma unroll
             for (int q = 0; q < KU; ++q) {
-                row[q] = k0 + q < top_k ? __ldg(&place[k0 + q]) : -1;
+                row[q] = k0 + q < top_k ? __ldg(&at[k0 + q]) : -1;
                 if (row[q] >= cap_rows) row[q] = -1;
-                w[q] = weights && k0 + q < top_k ? __ldg(&weights[k0 + q]) : 1.f;
-                if (row[q] >= 0) s[q] = from.request(row[q] * ld_y + e, &s_lines[q][0][threadIdx.x]);
+                w[q] = weights && k0 + q < top_k ? __ldg(&w_at[k0 + q]) : 1.f;
             }
-            wait_lines();
+            if constexpr (ANY) {
+                __shared__ uint4 s_lines[KU][2][kRowNT];
+                const Buffer<T> from(y_, (int64_t)(cap_rows - 1) * ld_y + dim);
+                int s[KU];
 #pragma unroll
-            for (int q = 0; q < KU; ++q) {
-                if (row[q] < 0) continue;
-                const Vec<T> v = from.take(s[q], &s_lines[q][0][threadIdx.x], row[q] * ld_y + e);
+                for (int q = 0; q < KU; ++q)
+                    if (row[q] >= 0) s[q] = from.request((int64_t)row[q] * ld_y + e, &s_lines[q][0][threadIdx.x]);
+                wait_lines();
 #pragma unroll
-                for (int j = 0; j < N; ++j) acc[j] = fmaf(w[q], to_f32(v.v[j]), acc[j]);
+                for (int q = 0; q < KU; ++q) {
+                    if (row[q] < 0) continue;
+                    const Vec<T> v = from.take(s[q], &s_lines[q][0][threadIdx.x], (int64_t)row[q] * ld_y + e);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) acc[j] = fmaf(w[q], to_f32(v.v[j]), acc[j]);
+                }
+            } else {
+                Vec<T> v[KU];
+#pragma unroll
+                for (int q = 0; q < KU; ++q) {
+                    v[q].raw = make_uint4(0, 0, 0, 0);
+                    if (row[q] >= 0) v[q].raw = __ldg(reinterpret_cast<const uint4*>(y.at(row[q]) + e));
+                }
+#pragma unroll
+                for (int q = 0; q < KU; ++q) {
+                    const float f = row[q] >= 0 ? w[q] : 0.f;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) acc[j] = fmaf(f, to_f32(v[q].v[j]), acc[j]);
+                }
             }
-        } else {
-            Vec<T> v[KU];
-#pragma unroll
-            for (int q = 0; q < KU; ++q) {
-                const int64_t row = k0 + q < top_k ? __ldg(&place[k0 + q]) : -1;
-                const bool ok = row >= 0 && row < cap_rows;
-                w[q] = ok ? (weights ? __ldg(&weights[k0 + q]) : 1.f) : 0.f;
-                v[q].raw = make_uint4(0, 0, 0, 0);
-                if (ok) v[q].raw = __ldg(reinterpret_cast<const uint4*>(y.at(row) + e));
-            }
-#pragma unroll
-            for (int q = 0; q < KU; ++q)
-#pragma unroll
-                for (int j = 0; j < N; ++j) acc[j] = fmaf(w[q], to_f32(v[q].v[j]), acc[j]);
         }
-    }
-    Vec<T> r;
+        Vec<T> r;
 #pragma unroll
-    for (int j = 0; j < N; ++j) r.v[j] = from_f32<T>(acc[j]);
-    if constexpr (ANY) store_line(to, e, dim, r);
-    else *reinterpret_cast<uint4*>(to + e) = r.raw;
+        for (int j = 0; j < N; ++j) r.v[j] = from_f32<T>(acc[j]);
+        if constexpr (ANY) store_line(to, e, dim, r);
+        else *reinterpret_cast<uint4*>(to + e) = r.raw;
+    }
 }
 
 // grad_y[place[t, k]] = w[t, k] * grad_out[t]; grad_w[t, k] = <grad_out[t], y[place[t, k]]>.  P threads (a power of two) take a
 // token, KU of its rows at a time.
 template <typename T, bool ANY>
 __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd(
-    const T* __restrict__ go_, int64_t ld_go, const T* __restrict__ y_, int64_t ld_y, int64_t cap_rows, const int32_t* n_tokens,
+    const T* __restrict__ go_, int ld_go, const T* __restrict__ y_, int ld_y, int cap_rows, const int32_t* n_tokens,
     int max_tokens, int top_k, int dim, const int32_t* __restrict__ place, const float* __restrict__ weights,
-    T* __restrict__ gy_, int64_t ld_gy, float* __restrict__ grad_w, int P, int lines, int row_ctas, int E, int pad_units,
+    T* __restrict__ gy_, int ld_gy, float* __restrict__ grad_w, int P, int lines, int row_ctas, int E, int pad_units,
     const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets) {
     constexpr int N = Vec<T>::N, KU = ANY ? 2 : 4;
     const Rows<const T> go{go_, ld_go}, y{y_, ld_y};
@@ -691,10 +698,9 @@ __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd(
     __shared__ float s_dot[kRowNT / 32][KU];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = threadIdx.x & (P - 1);
     const int tokens = live_choices(n_tokens, max_tokens, 1);
-    const int64_t t = (int64_t)blockIdx.x * (kRowNT / P) + threadIdx.x / P;
-    const Buffer<T> from_go(go_, (int64_t)(max_tokens - 1) * ld_go + dim), from_y(y_, (cap_rows - 1) * ld_y + dim);
+    const int t = (int)blockIdx.x * (kRowNT / P) + (int)threadIdx.x / P;
     for (int k0 = 0; k0 < top_k; k0 += KU) {
-        int64_t row[KU];
+        int row[KU];
         float w[KU], dot[KU];
 #pragma unroll
         for (int q = 0; q < KU; ++q) {
@@ -703,35 +709,41 @@ __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd(
             w[q] = row[q] >= 0 && weights ? __ldg(&weights[t * top_k + k0 + q]) : 1.f;
             dot[q] = 0.f;
         }
-        for (int l = sub; l < lines; l += P) {
-            if (t >= tokens) break;
+        for (int l = t < tokens ? sub : lines; l < lines; l += P) {
             if constexpr (ANY) {
                 __shared__ uint4 s_lines[KU][4][kRowNT];
+                const Buffer<T> from_go(go_, (int64_t)(max_tokens - 1) * ld_go + dim), from_y(y_, (int64_t)(cap_rows - 1) * ld_y + dim);
+                const int64_t go_at = (int64_t)t * ld_go;
                 int e[KU], sg[KU], sy[KU];
-                bool ok[KU];
 #pragma unroll
                 for (int q = 0; q < KU; ++q) {
-                    e[q] = l * N - in_line(gy.at(row[q]));
-                    ok[q] = row[q] >= 0 && e[q] < dim;
-                    if (!ok[q]) continue;
-                    sg[q] = from_go.request(t * ld_go + e[q], &s_lines[q][0][threadIdx.x]);
-                    if (grad_w) sy[q] = from_y.request(row[q] * ld_y + e[q], &s_lines[q][2][threadIdx.x]);
+                    e[q] = row[q] < 0 ? dim : l * N - in_line(gy.at(row[q]));
+                    if (e[q] >= dim) continue;
+                    sg[q] = from_go.request(go_at + e[q], &s_lines[q][0][threadIdx.x]);
+                    if (grad_w) sy[q] = from_y.request((int64_t)row[q] * ld_y + e[q], &s_lines[q][2][threadIdx.x]);
                 }
                 wait_lines();
 #pragma unroll
                 for (int q = 0; q < KU; ++q) {
-                    if (!ok[q]) continue;
-                    const Vec<T> a = from_go.take(sg[q], &s_lines[q][0][threadIdx.x], t * ld_go + e[q]);
-                    if (grad_w) {
-                        Vec<T> b = from_y.take(sy[q], &s_lines[q][2][threadIdx.x], row[q] * ld_y + e[q]);
-                        const bool whole = whole_line<T>(e[q], dim);
+                    if (e[q] >= dim) continue;
+                    const Vec<T> a = from_go.take(sg[q], &s_lines[q][0][threadIdx.x], go_at + e[q]);
+                    float g[N];
 #pragma unroll
-                        for (int j = 0; j < N; ++j)
-                            if (whole || (e[q] + j >= 0 && e[q] + j < dim)) dot[q] = fmaf(to_f32(a.v[j]), to_f32(b.v[j]), dot[q]);
+                    for (int j = 0; j < N; ++j) g[j] = to_f32(a.v[j]);
+                    if (grad_w) {
+                        const Vec<T> b = from_y.take(sy[q], &s_lines[q][2][threadIdx.x], (int64_t)row[q] * ld_y + e[q]);
+                        if (whole_line<T>(e[q], dim)) {
+#pragma unroll
+                            for (int j = 0; j < N; ++j) dot[q] = fmaf(g[j], to_f32(b.v[j]), dot[q]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < N; ++j)
+                                if ((unsigned)(e[q] + j) < (unsigned)dim) dot[q] = fmaf(g[j], to_f32(b.v[j]), dot[q]);
+                        }
                     }
                     Vec<T> r;
 #pragma unroll
-                    for (int j = 0; j < N; ++j) r.v[j] = from_f32<T>(w[q] * to_f32(a.v[j]));
+                    for (int j = 0; j < N; ++j) r.v[j] = from_f32<T>(w[q] * g[j]);
                     store_line(gy.at(row[q]), e[q], dim, r);
                 }
             } else {
@@ -803,7 +815,7 @@ bool matrices_ok(int32_t dtype, int64_t dim, std::initializer_list<Matrix> ms) {
     const int size = size_of(dtype);
     if (!size || dim < 1 || dim > (int64_t(1) << 24)) return false;
     for (const Matrix& m : ms)
-        if ((!m.p && m.rows > 0) || m.ld < dim || m.ld > (int64_t(1) << 31) || reinterpret_cast<uintptr_t>(m.p) % size)
+        if ((!m.p && m.rows > 0) || m.ld < dim || m.ld >= (int64_t(1) << 31) || reinterpret_cast<uintptr_t>(m.p) % size)
             return false;
     return true;
 }
@@ -820,8 +832,8 @@ int pad_units(const hl_route* r) {
     return (int)(u < r->align - 1 ? u : r->align - 1);
 }
 
-// Tiles of at most kSortChoices choices: as many CTAs as fill whole rounds of the chip.
-int64_t sort_tiles(int64_t n) { return div_up(div_up(n > 0 ? n : 1, kSortChoices), kSMsFallback) * kSMsFallback; }
+// Tiles of at most Tile::kChoices choices: as many CTAs as fill whole rounds of the chip.
+int64_t sort_tiles(int64_t n) { return div_up(div_up(n > 0 ? n : 1, Tile::kChoices), kSMsFallback) * kSMsFallback; }
 
 template <typename T, bool ANY>
 int32_t launch_dispatch(const hl_route* r, int64_t dim, const void* x, int64_t ld_x, void* y, int64_t ld_y, cudaStream_t stream) {
@@ -831,8 +843,8 @@ int32_t launch_dispatch(const hl_route* r, int64_t dim, const void* x, int64_t l
     if (ctas + units == 0) return HL_OK;
     if (ctas + (int64_t)units * r->n_experts > 0x7fffffff) return HL_EINVAL;
     HL_CUDA_TRY(launch(k_expert_dispatch<T, ANY, U>, ctas + units * r->n_experts, kRowNT, stream, static_cast<const T*>(x), ld_x,
-                       r->n_tokens, r->max_tokens, r->top_k, dim, r->place, r->cap_rows, static_cast<T*>(y), ld_y, lines, ctas,
-                       r->n_experts, units, r->counts, r->offsets));
+                       r->n_tokens, r->max_tokens, r->top_k, dim, r->place, r->cap_rows, static_cast<T*>(y), ld_y, lines,
+                       inverse_of(lines), ctas, r->n_experts, units, r->counts, r->offsets));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
@@ -843,11 +855,11 @@ int32_t launch_combine(const hl_route* r, int64_t dim, const void* y, int64_t ld
                        cudaStream_t stream) {
     const int lines = lines_of<T>(dim, ANY);
     const bool few = r->top_k <= 2;
-    const int64_t ctas = div_up(r->max_tokens * lines, kRowNT);
+    const int64_t ctas = div_up(r->max_tokens * lines, kRowNT * (few && !ANY ? 2 : 1));
     if (ctas > 0x7fffffff) return HL_EINVAL;
-    HL_CUDA_TRY(launch(few ? k_expert_combine<T, ANY, 2> : k_expert_combine<T, ANY, 4>, ctas, kRowNT, stream,
+    HL_CUDA_TRY(launch(few ? k_expert_combine<T, ANY, 2, ANY ? 1 : 2> : k_expert_combine<T, ANY, 4, 1>, ctas, kRowNT, stream,
                        static_cast<const T*>(y), ld_y, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, dim, r->place, w,
-                       static_cast<T*>(out), ld_out, lines));
+                       static_cast<T*>(out), ld_out, lines, inverse_of(lines)));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
@@ -901,13 +913,15 @@ extern "C" int32_t hl_expert_sort(const hl_route* route, const int32_t* d_expert
     if (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255)) return HL_EINVAL;
     if (ws_bytes < hl_expert_workspace_bytes(route->max_tokens, route->top_k, E)) return HL_ECAPACITY;
     const int32_t cap = (int32_t)(expert_cap < (int64_t(1) << 30) ? expert_cap : 0);
-    const size_t smem = sort_smem_words(E) * 4;
     if (n <= kOneCluster) {
-        const bool one = n <= kSortChoices;
-        HL_CUDA_TRY(launch_cluster(one ? k_expert_sort<1> : k_expert_sort<kClusterCtas>, one ? 1 : kClusterCtas, kSortNT, smem,
-                                   one ? 0 : kClusterCtas, stream, d_experts, route->n_tokens, route->max_tokens, route->top_k,
-                                   E, cap, route->align, route->cap_rows, route->place, route->source, route->counts,
-                                   route->offsets, d_status));
+#define HL_SORT(CTAS, NT, ITEMS)                                                                                              \
+    launch_cluster(k_expert_sort<CTAS, NT, ITEMS>, CTAS, NT, (Sort<NT, ITEMS>::smem_bytes(E)), CTAS > 1 ? CTAS : 0, stream,   \
+                   d_experts, route->n_tokens, route->max_tokens, route->top_k, E, cap, route->align, route->cap_rows,         \
+                   route->place, route->source, route->counts, route->offsets, d_status)
+        HL_CUDA_TRY(n <= kFewChoices    ? HL_SORT(1, 128, 4)
+                    : n <= kSomeChoices ? HL_SORT(kClusterCtas, 512, 4)
+                                        : HL_SORT(kClusterCtas, 512, 16));
+#undef HL_SORT
         note_launches(1);
         HL_LAUNCH_CHECK();
         return HL_OK;
@@ -916,12 +930,13 @@ extern "C" int32_t hl_expert_sort(const hl_route* route, const int32_t* d_expert
     int32_t* totals = static_cast<int32_t*>(d_workspace);
     int32_t* tile_counts = totals + (E + 1);
     uint32_t* ranked = reinterpret_cast<uint32_t*>(tile_counts + tiles * (E + 1));
-    HL_CUDA_TRY(launch_cluster(k_expert_rank, tiles, kSortNT, smem, 0, stream, d_experts, route->n_tokens, route->max_tokens,
-                               route->top_k, E, tile_counts, ranked));
-    HL_CUDA_TRY(launch_after(k_expert_scan, div_up(E + 1, 8), 256, 0, stream, tile_counts, tiles, E, totals));
-    HL_CUDA_TRY(launch_after(k_expert_place, tiles, kSortNT, place_smem_bytes(E), stream, route->n_tokens, route->max_tokens, route->top_k, E,
-                             cap, route->align, route->cap_rows, route->place, route->source, route->counts, route->offsets,
-                             d_status, (const int32_t*)tile_counts, (const int32_t*)totals, (const uint32_t*)ranked));
+    HL_CUDA_TRY(launch_cluster(k_expert_rank, tiles, kTileNT, Tile::smem_bytes(E), 0, stream, d_experts, route->n_tokens,
+                               route->max_tokens, route->top_k, E, tile_counts, ranked));
+    HL_CUDA_TRY(launch_after(k_expert_scan, div_up(E + 1, 32), kScanNT, 0, stream, tile_counts, tiles, E, totals));
+    HL_CUDA_TRY(launch_after(k_expert_place, tiles, kTileNT, place_smem_bytes(E), stream, route->n_tokens, route->max_tokens,
+                             route->top_k, E, cap, route->align, route->cap_rows, route->place, route->source, route->counts,
+                             route->offsets, d_status, (const int32_t*)tile_counts, (const int32_t*)totals,
+                             (const uint32_t*)ranked));
     note_launches(3);
     HL_LAUNCH_CHECK();
     return HL_OK;
