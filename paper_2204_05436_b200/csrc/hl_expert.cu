@@ -82,6 +82,7 @@ struct Sort {
     }
 
     // Ranks the CTA's choices [first, first + rounds * NT) below n, of `most` that can be read, and counts them: warp_hist, hist.
+    template <int BITS>
     __device__ __forceinline__ void rank(const int32_t* __restrict__ experts, int first, int rounds, int n, int most,
                                          uint32_t (&packed)[ITEMS]) const {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, seg = first + warp * (rounds * 32) + lane;
@@ -100,11 +101,7 @@ struct Sort {
                 e[i] = -1;
             }
         }
-        uint16_t* h = warp_hist + warp * pitch;
-        if (E <= 16) rank_rounds<4>(e, rounds, h, packed);
-        else if (E <= 64) rank_rounds<6>(e, rounds, h, packed);
-        else if (E <= 256) rank_rounds<8>(e, rounds, h, packed);
-        else rank_rounds<10>(e, rounds, h, packed);
+        rank_rounds<BITS>(e, rounds, warp_hist + warp * pitch, packed);
         if (__any_sync(0xffffffffu, bad) && lane == 0) atomicAdd(&hist[E], 1);
         __syncthreads();
         for (int x = threadIdx.x; x < E; x += NT) {
@@ -191,8 +188,9 @@ struct Sort {
     }
 };
 
-// All of it in one cluster, whose CTAs read each other's counts.
-template <int CTAS, int NT, int ITEMS>
+// All of it in one cluster, whose CTAs read each other's counts.  (A kernel for every two bits of the experts' numbers: what one
+// holds it has to fetch first, and a call alone pays for that -- all four in one: 14.6 us instead of 8.6 where nothing is cached.)
+template <int CTAS, int NT, int ITEMS, int BITS>
 __global__ void __launch_bounds__(NT) k_expert_sort(const int32_t* __restrict__ experts, const int32_t* n_tokens,
                                                     int max_tokens, int top_k, int E, int expert_cap, int align, int cap_rows,
                                                     int32_t* place, int32_t* source, int32_t* counts, int32_t* offsets,
@@ -205,7 +203,7 @@ __global__ void __launch_bounds__(NT) k_expert_sort(const int32_t* __restrict__ 
     const int most = CTAS == 1 ? max_tokens * top_k : n, rounds = (most + CTAS * NT - 1) / (CTAS * NT);
     const int first = (int)blockIdx.x * rounds * NT;
     uint32_t packed[ITEMS];
-    s.rank(experts, first, rounds, n, most, packed);
+    s.template rank<BITS>(experts, first, rounds, n, most, packed);
     if constexpr (CTAS > 1) {
         constexpr int kMine = HL_MAX_EXPERTS / NT + 1;
         cg::cluster_group cluster = cg::this_cluster();
@@ -265,6 +263,7 @@ __device__ __forceinline__ int tile_rounds(int n, int tiles) {
     return (int)(((int64_t)n + (int64_t)tiles * kTileNT - 1) / ((int64_t)tiles * kTileNT));
 }
 
+template <int BITS>
 __global__ void __launch_bounds__(kTileNT) k_expert_rank(const int32_t* __restrict__ experts, const int32_t* n_tokens,
                                                          int max_tokens, int top_k, int E, int32_t* __restrict__ tile_counts,
                                                          uint32_t* __restrict__ ranked) {
@@ -274,7 +273,7 @@ __global__ void __launch_bounds__(kTileNT) k_expert_rank(const int32_t* __restri
     const int n = live_choices(n_tokens, max_tokens, top_k), tiles = gridDim.x, rounds = tile_rounds(n, tiles);
     const int first = min((int64_t)blockIdx.x * rounds * kTileNT, (int64_t)n);
     uint32_t packed[kTileItems];
-    s.rank(experts, first, rounds, n, n, packed);
+    s.rank<BITS>(experts, first, rounds, n, n, packed);
     for (int e = threadIdx.x; e <= E; e += kTileNT) tile_counts[(int64_t)blockIdx.x * (E + 1) + e] = s.hist[e];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -400,177 +399,150 @@ constexpr int kClusterCtas = 8;
 constexpr int64_t kFewChoices = 128 * 4, kSomeChoices = kClusterCtas * 512 * 4, kOneCluster = kClusterCtas * 512 * 16;
 
 // ---- rows -----------------------------------------------------------------------------------------------------------
-// Values move 16 bytes at a time.  Where every row of a call begins at a multiple of 16 bytes (ANY = false), a vector is one
-// load and one store.  Elsewhere a row that is written is cut where its own 16-byte lines begin, so that all its stores but
-// those at its ends are whole lines, and what belongs there is put together from the two lines it lies in (load_any).
+// 16 bytes of a row are moved as one.  Where all rows of a call begin at multiples of 16 bytes and have whole ones, that is a load or
+// a store; other rows are "ragged", below.
 template <typename T>
 struct Vec {
     static constexpr int N = 16 / sizeof(T);
-    union {
-        uint4 raw;
-        T v[N];
-    };
-    __device__ Vec() {}
+    uint4 raw;
+    __device__ __forceinline__ Vec() : raw(make_uint4(0, 0, 0, 0)) {}
+    __device__ __forceinline__ void load(const T* p) { raw = __ldg(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = raw; }
+    // (two values of a word at a time: the conversions to fp32 and back have instructions for that)
+    __device__ __forceinline__ void get(float (&x)[N]) const {
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                x[i] = __uint_as_float(w[i]);
+            } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            } else {
+                const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                x[2 * i] = v.x;
+                x[2 * i + 1] = v.y;
+            }
+        }
+    }
+    __device__ __forceinline__ void set(const float (&x)[N]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                w[i] = __float_as_uint(x[i]);
+            } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+                const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t*>(&v);
+            } else {
+                const __half2 v = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t*>(&v);
+            }
+        }
+        raw = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    // value i, for an i known when this is compiled
+    __device__ __forceinline__ T value(int i) const {
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(w[i]);
+        } else {
+            const uint16_t h = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+            return *reinterpret_cast<const T*>(&h);
+        }
+    }
 };
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
-template <typename T>
-__device__ __forceinline__ T from_f32(float x);
-template <>
-__device__ __forceinline__ float from_f32<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-template <>
-__device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 
-// rows x dim values, ld from one row's begin to the next
+// rows, ld values from one's begin to the next's
 template <typename T>
 struct Rows {
     T* p;
     int ld;
     __device__ __forceinline__ T* at(int r) const { return p + (int64_t)r * ld; }
 };
+
+constexpr int kRowNT = 256;
+
+// Rows that fill experts up: CTA u of units x E takes every units-th of expert u % E's.
 template <typename T>
 __device__ __forceinline__ int in_line(const T* p) {           // values between the 16-byte line's begin and p
     return (int)(reinterpret_cast<uintptr_t>(p) & 15) / (int)sizeof(T);
 }
-
-// 16 bytes from any place of a buffer on; what lies outside of it reads as anything.  In two halves: the two lines they lie in are
-// asked for, into shared memory of the thread's own (registers for them would leave room for half as many threads, and what
-// bounds these kernels is how much is on its way and how many instructions it takes), and what is wanted is put together from them.
-constexpr int kRowNT = 256;
-template <typename T>
-struct Buffer {
-    const T* p;
-    int64_t values;
-    uint64_t most;                     // places N to most + N have two lines inside the buffer, whatever its alignment
-    __device__ __forceinline__ Buffer(const T* p_, int64_t values_)
-        : p(p_), values(values_), most(values_ > 3 * Vec<T>::N ? values_ - 3 * Vec<T>::N : 0) {}
-    // slot: two of the thread's, kRowNT apart.  Returns the bytes of the first line that are not wanted, or -1: to be read value
-    // by value.
-    __device__ __forceinline__ int request(int64_t at, uint4* slot) const {
-        if ((uint64_t)(at - Vec<T>::N) >= most) return -1;
-        const uintptr_t a = reinterpret_cast<uintptr_t>(p + at), line = a & ~(uintptr_t)15;
-        const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot);
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to), "l"(line) : "memory");
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to + kRowNT * 16), "l"(line + 16) : "memory");
-        return (int)(a & 15);
-    }
-    __device__ __forceinline__ Vec<T> take(int s, const uint4* slot, int64_t at) const {
-        Vec<T> r;
-        if (s < 0) {
-            r.raw = make_uint4(0, 0, 0, 0);
-#pragma unroll 1
-            for (int j = 0; j < Vec<T>::N; ++j)
-                if (at + j >= 0 && at + j < values) {
-                    T x = p[at + j];
-#pragma unroll
-                    for (int i = 0; i < Vec<T>::N; ++i)
-                        if (i == j) r.v[i] = x;
-                }
-            return r;
-        }
-        const uint4 a = slot[0], b = slot[kRowNT];
-        const bool far = s & 8, odd = s & 4;
-        const int bits = s * 8;        // (a funnel shift takes it modulo 32)
-        const uint32_t w0 = far ? a.z : a.x, w1 = far ? a.w : a.y, w2 = far ? b.x : a.z, w3 = far ? b.y : a.w,
-                       w4 = far ? b.z : b.x, w5 = far ? b.w : b.y;
-        const uint32_t x0 = odd ? w1 : w0, x1 = odd ? w2 : w1, x2 = odd ? w3 : w2, x3 = odd ? w4 : w3, x4 = odd ? w5 : w4;
-        if constexpr (sizeof(T) == 4)
-            r.raw = make_uint4(x0, x1, x2, x3);
-        else
-            r.raw = make_uint4(__funnelshift_r(x0, x1, bits), __funnelshift_r(x1, x2, bits), __funnelshift_r(x2, x3, bits),
-                               __funnelshift_r(x3, x4, bits));
-        return r;
-    }
-};
-__device__ __forceinline__ void wait_lines() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
-// values [e, e + N) of a row of dim values, as much of them as there is; row + e is a line's begin
-template <typename T>
-__device__ __forceinline__ bool whole_line(int e, int dim) { return e >= 0 && e + Vec<T>::N <= dim; }
+// values [e, e + N) of a row of dim values, as much of them as there is; row + e is where a line begins
 template <typename T>
 __device__ __forceinline__ void store_line(T* row, int e, int dim, const Vec<T>& v) {
     constexpr int N = Vec<T>::N;
-    if (whole_line<T>(e, dim)) {
-        *reinterpret_cast<uint4*>(row + e) = v.raw;
+    if (e >= 0 && e + N <= dim) {
+        v.store(row + e);
         return;
     }
 #pragma unroll
     for (int j = 0; j < N; ++j)
-        if (e + j >= 0 && e + j < dim) row[e + j] = v.v[j];
+        if ((unsigned)(e + j) < (unsigned)dim) row[e + j] = v.value(j);
 }
 
-// Lines that a row of dim values can lie in.
-template <typename T>
-__host__ __device__ constexpr int lines_of(int64_t dim, bool any) {
-    return (int)((dim + (any ? Vec<T>::N - 1 : 0) + Vec<T>::N - 1) / Vec<T>::N);
-}
-
-// Rows that fill experts up: CTA u of units x E takes every units-th of expert u % E's.
 template <typename T>
 __device__ __forceinline__ void zero_pads(int u, int units, int E, const int32_t* __restrict__ counts,
                                           const int32_t* __restrict__ offsets, int cap_rows, Rows<T> y, int dim) {
     const int e = u % E, part = u / E, end = min(__ldg(&offsets[e + 1]), cap_rows);
     const int64_t first = __ldg(&offsets[e]), count = __ldg(&counts[e]);
     if (first < 0 || count < 0) return;
-    Vec<T> zero;
-    zero.raw = make_uint4(0, 0, 0, 0);
+    const Vec<T> zero;
     for (int64_t r = first + count + part; r < end; r += units) {
         T* row = y.at((int)r);
-        for (int e0 = -in_line(row) + (int)threadIdx.x * Vec<T>::N; e0 < dim; e0 += kRowNT * Vec<T>::N) store_line(row, e0, dim, zero);
+        for (int c = (int)threadIdx.x * Vec<T>::N - in_line(row); c < dim; c += kRowNT * Vec<T>::N) store_line(row, c, dim, zero);
     }
 }
 
-// Which token and line a thread's item is: items are dealt out in turn, kRowNT * U to a CTA.  Divisions would be a good part of the
-// kernels' instructions: the host gives 2^64 / lines, rounded up (exact quotients for less than 2^40 items and lines below 2^24), and
-// inside a CTA the token before is followed by at most one more from 512 lines on, below which 2^32 / lines does.
+// Which token and vector a thread's item is: items are dealt out in turn, kRowNT * U to a CTA.  Divisions would be a good part of
+// the kernels' instructions: the host gives 2^64 / vectors, rounded up (exact quotients for less than 2^40 items and rows of less
+// than 2^24 vectors); inside a CTA 2^32 / vectors does for less than 32 768 of them, beyond which one token at most follows the first.
 template <int U>
 struct Items {
     int t0;
     unsigned r0, magic;
-    int lines;
-    __device__ __forceinline__ Items(int lines_, uint64_t inverse) : lines(lines_) {
+    int vectors;
+    __device__ __forceinline__ Items(int vectors_, uint64_t inverse) : vectors(vectors_) {
         const uint64_t first = (uint64_t)blockIdx.x * (kRowNT * U);
-        t0 = lines == 1 ? (int)first : (int)__umul64hi(first, inverse);
-        r0 = (unsigned)(first - (uint64_t)t0 * lines);
+        t0 = vectors == 1 ? (int)first : (int)__umul64hi(first, inverse);
+        r0 = (unsigned)(first - (uint64_t)t0 * vectors);
         magic = (unsigned)((inverse + 0xffffffffu) >> 32);
     }
-    __device__ __forceinline__ void get(int u, int* t, int* line) const {
+    __device__ __forceinline__ void get(int u, int* t, int* vector) const {
         const unsigned i = r0 + u * kRowNT + threadIdx.x;
-        const unsigned q = lines == 1 ? i : lines >= 512 ? i >= (unsigned)lines : __umulhi(i, magic);
+        const unsigned q = vectors == 1 ? i : vectors >= 32768 ? i >= (unsigned)vectors : __umulhi(i, magic);
         *t = t0 + (int)q;
-        *line = (int)(i - q * lines);
+        *vector = (int)(i - q * vectors);
     }
 };
-uint64_t inverse_of(int lines) { return lines == 1 ? 0 : ~uint64_t(0) / lines + 1; }
+uint64_t inverse_of(int vectors) { return vectors == 1 ? 0 : ~uint64_t(0) / vectors + 1; }
 
-// y[place[t, k]] = x[t].  A thread takes a line of a token's row, which it reads once for all of the token's rows.
-template <typename T, bool ANY, int U>
-__global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_dispatch(const T* __restrict__ x_, int ld_x,
-                                                                         const int32_t* n_tokens, int max_tokens, int top_k,
-                                                                         int dim, const int32_t* __restrict__ place,
-                                                                         int cap_rows, T* __restrict__ y_, int ld_y, int lines,
-                                                                         uint64_t inverse, int row_ctas, int E, int pad_units,
-                                                                         const int32_t* __restrict__ counts,
-                                                                         const int32_t* __restrict__ offsets) {
-    constexpr int N = Vec<T>::N, KU = 4;
+// y[place[t, k]] = x[t].  A thread takes two vectors of tokens' rows, which it reads once for all of a token's rows.
+constexpr int kDispatchVectors = 2;
+template <typename T>
+__global__ void __launch_bounds__(kRowNT, 6) k_expert_dispatch(const T* __restrict__ x_, int ld_x, const int32_t* n_tokens,
+                                                               int max_tokens, int top_k, int dim,
+                                                               const int32_t* __restrict__ place, int cap_rows,
+                                                               T* __restrict__ y_, int ld_y, int vectors, uint64_t inverse,
+                                                               int row_ctas, int E, int pad_units,
+                                                               const int32_t* __restrict__ counts,
+                                                               const int32_t* __restrict__ offsets) {
+    constexpr int KU = 4, U = kDispatchVectors, W = Vec<T>::N;
     const Rows<const T> x{x_, ld_x};
     const Rows<T> y{y_, ld_y};
     if ((int)blockIdx.x >= row_ctas) {
-        zero_pads(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, y, dim);
+        zero_pads<T>(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, y, dim);
         return;
     }
     const int tokens = live_choices(n_tokens, max_tokens, 1);
-    const Items<U> items(lines, inverse);
+    const Items<U> items(vectors, inverse);
     Vec<T> v[U];
-    int t[U], line[U];
+    int t[U], c[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        items.get(u, &t[u], &line[u]);
-        if constexpr (!ANY)
-            if (t[u] < tokens) v[u].raw = __ldg(reinterpret_cast<const uint4*>(x.at(t[u]) + line[u] * N));
+        items.get(u, &t[u], &c[u]);
+        c[u] *= W;
+        if (t[u] < tokens) v[u].load(x.at(t[u]) + c[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -579,126 +551,103 @@ __global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_dispatch(const T
         for (int k0 = 0; k0 < top_k; k0 += KU) {
             int row[KU];
 #pragma unroll
-            for (int q = 0; q < KU; ++q) {
-                row[q] = k0 + q < top_k ? __ldg(&at[k0 + q]) : -1;
-                if (row[q] >= cap_rows) row[q] = -1;
-            }
-            if constexpr (!ANY) {
+            for (int q = 0; q < KU; ++q) row[q] = k0 + q < top_k ? __ldg(&at[k0 + q]) : -1;
 #pragma unroll
-                for (int q = 0; q < KU; ++q)
-                    if (row[q] >= 0) *reinterpret_cast<uint4*>(y.at(row[q]) + line[u] * N) = v[u].raw;
-            } else {
-                __shared__ uint4 s_lines[KU][2][kRowNT];
-                const Buffer<T> from(x_, (int64_t)(max_tokens - 1) * ld_x + dim);
-                const int64_t x_at = (int64_t)t[u] * ld_x;
-                int e[KU], s[KU];
-#pragma unroll
-                for (int q = 0; q < KU; ++q) {
-                    e[q] = line[u] * N - in_line(y.at(row[q]));
-                    if (e[q] >= dim) row[q] = -1;
-                    if (row[q] >= 0) s[q] = from.request(x_at + e[q], &s_lines[q][0][threadIdx.x]);
-                }
-                wait_lines();
-#pragma unroll
-                for (int q = 0; q < KU; ++q)
-                    if (row[q] >= 0)
-                        store_line(y.at(row[q]), e[q], dim, from.take(s[q], &s_lines[q][0][threadIdx.x], x_at + e[q]));
-            }
+            for (int q = 0; q < KU; ++q)
+                if ((unsigned)row[q] < (unsigned)cap_rows) v[u].store(y.at(row[q]) + c[u]);
         }
     }
 }
 
 // out[t] = sum over k of w[t, k] * y[place[t, k]], in fp32, in the order of k, rounded once.  (Without weights: the sum.)  A
-// thread takes a line of out, or U of them one after the other, and KU of the token's rows at a time.
-template <typename T, bool ANY, int KU, int U>
-__global__ void __launch_bounds__(kRowNT, ANY ? 5 : 6) k_expert_combine(const T* __restrict__ y_, int ld_y, int cap_rows,
-                                                                        const int32_t* n_tokens, int max_tokens, int top_k,
-                                                                        int dim, const int32_t* __restrict__ place,
-                                                                        const float* __restrict__ weights,
-                                                                        T* __restrict__ out_, int ld_out, int lines,
-                                                                        uint64_t inverse) {
-    constexpr int N = Vec<T>::N;
+// thread takes a vector of out, or U of them one after the other, and KU of the token's rows at a time.
+template <typename T, int KU, int U>
+__global__ void __launch_bounds__(kRowNT, 6) k_expert_combine(const T* __restrict__ y_, int ld_y, int cap_rows,
+                                                              const int32_t* n_tokens, int max_tokens, int top_k,
+                                                              const int32_t* __restrict__ place,
+                                                              const float* __restrict__ weights, T* __restrict__ out_,
+                                                              int ld_out, int vectors, uint64_t inverse) {
+    constexpr int W = Vec<T>::N;
     const Rows<const T> y{y_, ld_y};
     const Rows<T> out{out_, ld_out};
     const int tokens = live_choices(n_tokens, max_tokens, 1);
-    const Items<U> items(lines, inverse);
+    const Items<U> items(vectors, inverse);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        int t, line;
-        items.get(u, &t, &line);
+        int t, c;
+        items.get(u, &t, &c);
         if (t >= tokens) return;
-        T* to = out.at(t);
-        const int e = line * N - (ANY ? in_line(to) : 0);
-        if (ANY && e >= dim) continue;
+        c *= W;
         const int32_t* at = place + t * top_k;
         const float* w_at = weights + t * top_k;
-        float acc[N] = {};
+        float acc[W] = {};
         for (int k0 = 0; k0 < top_k; k0 += KU) {
             int row[KU];
             float w[KU];
+            Vec<T> v[KU];
 #pragma unroll
             for (int q = 0; q < KU; ++q) {
                 row[q] = k0 + q < top_k ? __ldg(&at[k0 + q]) : -1;
-                if (row[q] >= cap_rows) row[q] = -1;
                 w[q] = weights && k0 + q < top_k ? __ldg(&w_at[k0 + q]) : 1.f;
             }
-            if constexpr (ANY) {
-                __shared__ uint4 s_lines[KU][2][kRowNT];
-                const Buffer<T> from(y_, (int64_t)(cap_rows - 1) * ld_y + dim);
-                int s[KU];
 #pragma unroll
-                for (int q = 0; q < KU; ++q)
-                    if (row[q] >= 0) s[q] = from.request((int64_t)row[q] * ld_y + e, &s_lines[q][0][threadIdx.x]);
-                wait_lines();
+            for (int q = 0; q < KU; ++q) {
+                const bool ok = (unsigned)row[q] < (unsigned)cap_rows;
+                if (ok) v[q].load(y.at(row[q]) + c);
+                w[q] = ok ? w[q] : 0.f;
+            }
 #pragma unroll
-                for (int q = 0; q < KU; ++q) {
-                    if (row[q] < 0) continue;
-                    const Vec<T> v = from.take(s[q], &s_lines[q][0][threadIdx.x], (int64_t)row[q] * ld_y + e);
+            for (int q = 0; q < KU; ++q) {
+                float x[W];
+                v[q].get(x);
 #pragma unroll
-                    for (int j = 0; j < N; ++j) acc[j] = fmaf(w[q], to_f32(v.v[j]), acc[j]);
-                }
-            } else {
-                Vec<T> v[KU];
-#pragma unroll
-                for (int q = 0; q < KU; ++q) {
-                    v[q].raw = make_uint4(0, 0, 0, 0);
-                    if (row[q] >= 0) v[q].raw = __ldg(reinterpret_cast<const uint4*>(y.at(row[q]) + e));
-                }
-#pragma unroll
-                for (int q = 0; q < KU; ++q) {
-                    const float f = row[q] >= 0 ? w[q] : 0.f;
-#pragma unroll
-                    for (int j = 0; j < N; ++j) acc[j] = fmaf(f, to_f32(v[q].v[j]), acc[j]);
-                }
+                for (int j = 0; j < W; ++j) acc[j] = fmaf(w[q], x[j], acc[j]);
             }
         }
         Vec<T> r;
-#pragma unroll
-        for (int j = 0; j < N; ++j) r.v[j] = from_f32<T>(acc[j]);
-        if constexpr (ANY) store_line(to, e, dim, r);
-        else *reinterpret_cast<uint4*>(to + e) = r.raw;
+        r.set(acc);
+        r.store(out.at(t) + c);
     }
+}
+
+// The sums of P threads' dot products, in the first of them.  (All threads of the CTA call it.)
+template <int KU>
+__device__ __forceinline__ void sum_dots(float (&dot)[KU], int P, float* s_dot) {
+    for (int d = min(P, 32) / 2; d > 0; d >>= 1)
+#pragma unroll
+        for (int q = 0; q < KU; ++q) dot[q] += __shfl_xor_sync(0xffffffffu, dot[q], d);
+    if (P <= 32) return;
+    const int warp = threadIdx.x >> 5;
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int q = 0; q < KU; ++q) s_dot[warp * KU + q] = dot[q];
+    __syncthreads();
+    if ((threadIdx.x & (P - 1)) == 0)
+        for (int o = 1; o < P / 32; ++o)
+#pragma unroll
+            for (int q = 0; q < KU; ++q) dot[q] += s_dot[(warp + o) * KU + q];
+    __syncthreads();
 }
 
 // grad_y[place[t, k]] = w[t, k] * grad_out[t]; grad_w[t, k] = <grad_out[t], y[place[t, k]]>.  P threads (a power of two) take a
 // token, KU of its rows at a time.
-template <typename T, bool ANY>
+template <typename T>
 __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd(
     const T* __restrict__ go_, int ld_go, const T* __restrict__ y_, int ld_y, int cap_rows, const int32_t* n_tokens,
     int max_tokens, int top_k, int dim, const int32_t* __restrict__ place, const float* __restrict__ weights,
-    T* __restrict__ gy_, int ld_gy, float* __restrict__ grad_w, int P, int lines, int row_ctas, int E, int pad_units,
+    T* __restrict__ gy_, int ld_gy, float* __restrict__ grad_w, int P, int row_ctas, int E, int pad_units,
     const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets) {
-    constexpr int N = Vec<T>::N, KU = ANY ? 2 : 4;
+    constexpr int KU = 4, W = Vec<T>::N;
     const Rows<const T> go{go_, ld_go}, y{y_, ld_y};
     const Rows<T> gy{gy_, ld_gy};
     if ((int)blockIdx.x >= row_ctas) {
-        zero_pads(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, gy, dim);
+        zero_pads<T>(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, gy, dim);
         return;
     }
-    __shared__ float s_dot[kRowNT / 32][KU];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = threadIdx.x & (P - 1);
+    __shared__ float s_dot[kRowNT / 32 * KU];
+    const int sub = threadIdx.x & (P - 1);
     const int tokens = live_choices(n_tokens, max_tokens, 1);
-    const int t = (int)blockIdx.x * (kRowNT / P) + (int)threadIdx.x / P;
+    const int t = (int)((int64_t)blockIdx.x * (kRowNT / P)) + (int)threadIdx.x / P;
     for (int k0 = 0; k0 < top_k; k0 += KU) {
         int row[KU];
         float w[KU], dot[KU];
@@ -709,85 +658,293 @@ __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd(
             w[q] = row[q] >= 0 && weights ? __ldg(&weights[t * top_k + k0 + q]) : 1.f;
             dot[q] = 0.f;
         }
-        for (int l = t < tokens ? sub : lines; l < lines; l += P) {
-            if constexpr (ANY) {
-                __shared__ uint4 s_lines[KU][4][kRowNT];
-                const Buffer<T> from_go(go_, (int64_t)(max_tokens - 1) * ld_go + dim), from_y(y_, (int64_t)(cap_rows - 1) * ld_y + dim);
-                const int64_t go_at = (int64_t)t * ld_go;
-                int e[KU], sg[KU], sy[KU];
+        for (int c = t < tokens ? sub * W : dim; c < dim; c += P * W) {
+            Vec<T> g, v[KU];
+            float x[W];
+            g.load(go.at(t) + c);
 #pragma unroll
-                for (int q = 0; q < KU; ++q) {
-                    e[q] = row[q] < 0 ? dim : l * N - in_line(gy.at(row[q]));
-                    if (e[q] >= dim) continue;
-                    sg[q] = from_go.request(go_at + e[q], &s_lines[q][0][threadIdx.x]);
-                    if (grad_w) sy[q] = from_y.request((int64_t)row[q] * ld_y + e[q], &s_lines[q][2][threadIdx.x]);
+            for (int q = 0; q < KU; ++q)
+                if (row[q] >= 0 && grad_w) v[q].load(y.at(row[q]) + c);
+#pragma unroll
+            for (int q = 0; q < KU; ++q) {
+                if (row[q] < 0) continue;
+                Vec<T> r;
+                float y[W], z[W];
+                g.get(x);
+                v[q].get(y);
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    dot[q] = fmaf(x[j], y[j], dot[q]);
+                    z[j] = w[q] * x[j];
                 }
-                wait_lines();
+                r.set(z);
+                r.store(gy.at(row[q]) + c);
+            }
+        }
+        sum_dots(dot, P, s_dot);
+        if (sub == 0 && t < tokens && grad_w)
 #pragma unroll
-                for (int q = 0; q < KU; ++q) {
-                    if (e[q] >= dim) continue;
-                    const Vec<T> a = from_go.take(sg[q], &s_lines[q][0][threadIdx.x], go_at + e[q]);
-                    float g[N];
+            for (int q = 0; q < KU; ++q)
+                if (k0 + q < top_k) grad_w[t * top_k + k0 + q] = dot[q];
+    }
+}
+
+// ---- ragged rows ----------------------------------------------------------------------------------------------------
+// A row that is written is cut where its own 16-byte lines begin, so that all stores but those at its ends are whole lines; the 16
+// bytes that belong there lie anywhere in the row that is read, and are put together from the two lines that they lie in.  Lines that
+// are not all inside a buffer are not read.
+template <typename T>
+struct Buffer {
+    const T* p;
+    int ld, dim;
+    int64_t values;                    // of all its rows
+    __device__ __forceinline__ Buffer(const T* p_, int ld_, int rows, int dim_)
+        : p(p_), ld(ld_), dim(dim_), values((int64_t)(rows - 1) * ld_ + dim_) {}
+    // whether the lines that a row's values lie in, and one more on either side, are inside
+    __device__ __forceinline__ bool inside(int r) const {
+        const int64_t at = (int64_t)r * ld;
+        return at >= 2 * Vec<T>::N && at + dim + 2 * Vec<T>::N <= values;
+    }
+};
+
+// What is read of a row by lines of another that begin at values -shift, N - shift, ... of it.
+struct Lines {
+    uint4 a, b;
+};
+template <typename T>
+struct Ragged {
+    const uint4* line;                 // the line in which value -shift lies
+    int s;                             // its byte in there
+    __device__ __forceinline__ Ragged() {}
+    __device__ __forceinline__ Ragged(const Buffer<T>& b, int r, int shift) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(b.p + ((int64_t)r * b.ld - shift));
+        line = reinterpret_cast<const uint4*>(a & ~(uintptr_t)15);
+        s = (int)(a & 15);
+    }
+    __device__ __forceinline__ Lines ask(int l) const { return {__ldg(line + l), __ldg(line + l + 1)}; }
+    // what line l of the other begins with; values outside of the row are anything
+    __device__ __forceinline__ Vec<T> take(const Lines& x) const {
+        const bool far = s & 8, odd = s & 4;
+        const uint32_t w0 = far ? x.a.z : x.a.x, w1 = far ? x.a.w : x.a.y, w2 = far ? x.b.x : x.a.z, w3 = far ? x.b.y : x.a.w,
+                       w4 = far ? x.b.z : x.b.x, w5 = far ? x.b.w : x.b.y;
+        const uint32_t y0 = odd ? w1 : w0, y1 = odd ? w2 : w1, y2 = odd ? w3 : w2, y3 = odd ? w4 : w3, y4 = odd ? w5 : w4;
+        const int bits = s * 8;        // (a funnel shift takes it modulo 32)
+        Vec<T> r;
+        r.raw = sizeof(T) == 4 ? make_uint4(y0, y1, y2, y3)
+                               : make_uint4(__funnelshift_r(y0, y1, bits), __funnelshift_r(y1, y2, bits),
+                                            __funnelshift_r(y2, y3, bits), __funnelshift_r(y3, y4, bits));
+        return r;
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ int lines_of(int shift, int dim) { return (shift + dim + Vec<T>::N - 1) / Vec<T>::N; }
+
+__device__ __forceinline__ float value_of(const float* p) { return *p; }
+__device__ __forceinline__ float value_of(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float value_of(const __half* p) { return __half2float(*p); }
+__device__ __forceinline__ void put_value(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put_value(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+__device__ __forceinline__ void put_value(__half* p, float x) { *p = __float2half_rn(x); }
+
+// The forward kernels take a line a thread, as those of whole rows do.  Lines are asked for into shared memory of the thread's own:
+// registers for them would leave room for half as many threads.
+template <typename T>
+__device__ __noinline__ uint4 line_by_value(const T* p, int64_t at, int64_t values) {          // (at a buffer's end)
+    alignas(16) T x[Vec<T>::N] = {};
+    for (int j = 0; j < Vec<T>::N; ++j)
+        if (at + j >= 0 && at + j < values) x[j] = p[at + j];
+    return *reinterpret_cast<const uint4*>(x);
+}
+template <typename T>
+struct LineBuffer {
+    const T* p;
+    int64_t values;
+    uint64_t most;                     // places N to most + N have two lines inside the buffer, whatever its alignment
+    __device__ __forceinline__ LineBuffer(const T* p_, int ld, int rows, int dim)
+        : p(p_), values((int64_t)(rows - 1) * ld + dim), most(values > 3 * Vec<T>::N ? values - 3 * Vec<T>::N : 0) {}
+    // slot: two of the thread's, kRowNT apart.  Returns the bytes of the first line that are not wanted, or -1: by value.
+    __device__ __forceinline__ int ask(int64_t at, uint4* slot) const {
+        if ((uint64_t)(at - Vec<T>::N) >= most) return -1;
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p + at), line = a & ~(uintptr_t)15;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot);
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to), "l"(line) : "memory");
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to + kRowNT * 16), "l"(line + 16) : "memory");
+        return (int)(a & 15);
+    }
+    __device__ __forceinline__ Vec<T> take(int s, const uint4* slot, int64_t at) const {
+        Vec<T> r;
+        if (s < 0) {
+            r.raw = line_by_value(p, at, values);
+            return r;
+        }
+        Ragged<T> x;
+        x.s = s;
+        return x.take({slot[0], slot[kRowNT]});
+    }
+};
+__device__ __forceinline__ void wait_lines() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+template <typename T>
+__global__ void __launch_bounds__(kRowNT, 5) k_expert_dispatch_ragged(const T* __restrict__ x_, int ld_x,
+                                                                      const int32_t* n_tokens, int max_tokens, int top_k,
+                                                                      int dim, const int32_t* __restrict__ place, int cap_rows,
+                                                                      T* __restrict__ y_, int ld_y, int lines, uint64_t inverse,
+                                                                      int row_ctas, int E, int pad_units,
+                                                                      const int32_t* __restrict__ counts,
+                                                                      const int32_t* __restrict__ offsets) {
+    constexpr int N = Vec<T>::N, KU = 4;
+    const Rows<T> y{y_, ld_y};
+    if ((int)blockIdx.x >= row_ctas) {
+        zero_pads<T>(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, y, dim);
+        return;
+    }
+    __shared__ uint4 s_lines[KU][2][kRowNT];
+    const LineBuffer<T> x(x_, ld_x, max_tokens, dim);
+    int t, line;
+    Items<1>(lines, inverse).get(0, &t, &line);
+    if (t >= live_choices(n_tokens, max_tokens, 1)) return;
+    const int32_t* at = place + t * top_k;
+    const int64_t x_at = (int64_t)t * ld_x;
+    for (int k0 = 0; k0 < top_k; k0 += KU) {
+        T* to[KU];
+        int e[KU], s[KU];
 #pragma unroll
-                    for (int j = 0; j < N; ++j) g[j] = to_f32(a.v[j]);
-                    if (grad_w) {
-                        const Vec<T> b = from_y.take(sy[q], &s_lines[q][2][threadIdx.x], (int64_t)row[q] * ld_y + e[q]);
-                        if (whole_line<T>(e[q], dim)) {
+        for (int q = 0; q < KU; ++q) {
+            const int row = k0 + q < top_k ? __ldg(&at[k0 + q]) : -1;
+            to[q] = y.at(row);
+            e[q] = (unsigned)row < (unsigned)cap_rows ? line * N - in_line(to[q]) : dim;
+            if (e[q] < dim) s[q] = x.ask(x_at + e[q], &s_lines[q][0][threadIdx.x]);
+        }
+        wait_lines();
 #pragma unroll
-                            for (int j = 0; j < N; ++j) dot[q] = fmaf(g[j], to_f32(b.v[j]), dot[q]);
-                        } else {
+        for (int q = 0; q < KU; ++q)
+            if (e[q] < dim) store_line(to[q], e[q], dim, x.take(s[q], &s_lines[q][0][threadIdx.x], x_at + e[q]));
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kRowNT, 5) k_expert_combine_ragged(const T* __restrict__ y_, int ld_y, int cap_rows,
+                                                                     const int32_t* n_tokens, int max_tokens, int top_k,
+                                                                     int dim, const int32_t* __restrict__ place,
+                                                                     const float* __restrict__ weights, T* __restrict__ out_,
+                                                                     int ld_out, int lines, uint64_t inverse) {
+    constexpr int N = Vec<T>::N, KU = 4;
+    __shared__ uint4 s_lines[KU][2][kRowNT];
+    const LineBuffer<T> y(y_, ld_y, cap_rows, dim);
+    int t, line;
+    Items<1>(lines, inverse).get(0, &t, &line);
+    if (t >= live_choices(n_tokens, max_tokens, 1)) return;
+    T* to = Rows<T>{out_, ld_out}.at(t);
+    const int e = line * N - in_line(to);
+    if (e >= dim) return;
+    const int32_t* at = place + t * top_k;
+    const float* w_at = weights + t * top_k;
+    float acc[N] = {};
+    for (int k0 = 0; k0 < top_k; k0 += KU) {
+        int row[KU], s[KU];
+        float w[KU];
 #pragma unroll
-                            for (int j = 0; j < N; ++j)
-                                if ((unsigned)(e[q] + j) < (unsigned)dim) dot[q] = fmaf(g[j], to_f32(b.v[j]), dot[q]);
-                        }
+        for (int q = 0; q < KU; ++q) {
+            row[q] = k0 + q < top_k ? __ldg(&at[k0 + q]) : -1;
+            w[q] = weights && k0 + q < top_k ? __ldg(&w_at[k0 + q]) : 1.f;
+        }
+#pragma unroll
+        for (int q = 0; q < KU; ++q)
+            if ((unsigned)row[q] < (unsigned)cap_rows) s[q] = y.ask((int64_t)row[q] * ld_y + e, &s_lines[q][0][threadIdx.x]);
+        wait_lines();
+#pragma unroll
+        for (int q = 0; q < KU; ++q) {
+            if ((unsigned)row[q] >= (unsigned)cap_rows) continue;
+            float x[N];
+            y.take(s[q], &s_lines[q][0][threadIdx.x], (int64_t)row[q] * ld_y + e).get(x);
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[j] = fmaf(w[q], x[j], acc[j]);
+        }
+    }
+    Vec<T> r;
+    r.set(acc);
+    store_line(to, e, dim, r);
+}
+
+// The gradients: P threads (a power of two) take a token, so that where a row lies is found out once for all of its lines; the
+// tokens with rows next to a buffer's ends are done value by value.
+// SAME: y's rows lie in their lines as grad_y's do, so that y needs no putting together.
+template <typename T, bool SAME>
+__global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd_ragged(
+    const T* __restrict__ go_, int ld_go, const T* __restrict__ y_, int ld_y, int cap_rows, const int32_t* n_tokens,
+    int max_tokens, int top_k, int dim, const int32_t* __restrict__ place, const float* __restrict__ weights,
+    T* __restrict__ gy_, int ld_gy, float* __restrict__ grad_w, int P, int row_ctas, int E, int pad_units,
+    const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets) {
+    constexpr int N = Vec<T>::N, L = 3;              // lines of a thread on their way
+    const Rows<T> gy{gy_, ld_gy};
+    if ((int)blockIdx.x >= row_ctas) {
+        zero_pads<T>(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, gy, dim);
+        return;
+    }
+    __shared__ float s_dot[kRowNT / 32];
+    const Buffer<T> go(go_, ld_go, max_tokens, dim), y(grad_w ? y_ : gy_, grad_w ? ld_y : ld_gy, cap_rows, dim);
+    const int sub = threadIdx.x & (P - 1), t = (int)blockIdx.x * (kRowNT / P) + (int)threadIdx.x / P;
+    const bool live = t < live_choices(n_tokens, max_tokens, 1), go_inside = go.inside(t);
+    for (int k = 0; k < top_k; ++k) {
+        const int row = live ? __ldg(&place[t * top_k + k]) : -1;
+        const float w = live && weights ? __ldg(&weights[t * top_k + k]) : 1.f;
+        float dot[1] = {};
+        if ((unsigned)row < (unsigned)cap_rows) {
+            T* to = gy.at(row);
+            if (go_inside && y.inside(row)) {
+                const int shift = in_line(to), lines = lines_of<T>(shift, dim);
+                const Ragged<T> g(go, t, shift), v(y, row, shift);
+                for (int l0 = sub; l0 < lines; l0 += P * L) {
+                    Lines gl[L], vl[L];
+#pragma unroll
+                    for (int i = 0; i < L; ++i) {
+                        if (l0 + i * P >= lines) break;
+                        gl[i] = g.ask(l0 + i * P);
+                        if (!grad_w) continue;
+                        if constexpr (SAME) vl[i].a = __ldg(v.line + l0 + i * P);
+                        else vl[i] = v.ask(l0 + i * P);
                     }
-                    Vec<T> r;
 #pragma unroll
-                    for (int j = 0; j < N; ++j) r.v[j] = from_f32<T>(w[q] * g[j]);
-                    store_line(gy.at(row[q]), e[q], dim, r);
+                    for (int i = 0; i < L; ++i) {
+                        if (l0 + i * P >= lines) break;
+                        const int e = (l0 + i * P) * N - shift;
+                        float x[N], z[N];
+                        g.take(gl[i]).get(x);
+                        if (grad_w) {
+                            Vec<T> b;
+                            float y[N];
+                            if constexpr (SAME) b.raw = vl[i].a;
+                            else b = v.take(vl[i]);
+                            b.get(y);
+                            if (e >= 0 && e + N <= dim) {
+#pragma unroll
+                                for (int j = 0; j < N; ++j) dot[0] = fmaf(x[j], y[j], dot[0]);
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < N; ++j)
+                                    if ((unsigned)(e + j) < (unsigned)dim) dot[0] = fmaf(x[j], y[j], dot[0]);
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < N; ++j) z[j] = w * x[j];
+                        Vec<T> r;
+                        r.set(z);
+                        store_line(to, e, dim, r);
+                    }
                 }
             } else {
-                Vec<T> g, v[KU];
-                g.raw = __ldg(reinterpret_cast<const uint4*>(go.at(t) + l * N));
-#pragma unroll
-                for (int q = 0; q < KU; ++q) {
-                    v[q].raw = make_uint4(0, 0, 0, 0);
-                    if (row[q] >= 0 && grad_w) v[q].raw = __ldg(reinterpret_cast<const uint4*>(y.at(row[q]) + l * N));
-                }
-#pragma unroll
-                for (int q = 0; q < KU; ++q) {
-                    if (row[q] < 0) continue;
-                    Vec<T> r;
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const float x = to_f32(g.v[j]);
-                        dot[q] = fmaf(x, to_f32(v[q].v[j]), dot[q]);
-                        r.v[j] = from_f32<T>(w[q] * x);
-                    }
-                    *reinterpret_cast<uint4*>(gy.at(row[q]) + l * N) = r.raw;
+#pragma unroll 1
+                for (int c = sub; c < dim; c += P) {
+                    const float x = value_of(go.p + (int64_t)t * ld_go + c);
+                    if (grad_w) dot[0] = fmaf(x, value_of(y.p + (int64_t)row * ld_y + c), dot[0]);
+                    put_value(to + c, w * x);
                 }
             }
         }
         if (!grad_w) continue;
-        const int in_warp = min(P, 32);
-        for (int d = in_warp / 2; d > 0; d >>= 1)
-#pragma unroll
-            for (int q = 0; q < KU; ++q) dot[q] += __shfl_xor_sync(0xffffffffu, dot[q], d);
-        if (P > 32) {
-            if (lane == 0)
-#pragma unroll
-                for (int q = 0; q < KU; ++q) s_dot[warp][q] = dot[q];
-            __syncthreads();
-            if (sub == 0)
-                for (int o = 1; o < P / 32; ++o)
-#pragma unroll
-                    for (int q = 0; q < KU; ++q) dot[q] += s_dot[warp + o][q];
-            __syncthreads();
-        }
-        if (sub == 0 && t < tokens)
-#pragma unroll
-            for (int q = 0; q < KU; ++q)
-                if (k0 + q < top_k) grad_w[t * top_k + k0 + q] = dot[q];
+        sum_dots(dot, P, s_dot);
+        if (sub == 0 && live) grad_w[t * top_k + k] = dot[0];
     }
 }
 
@@ -804,12 +961,11 @@ struct Matrix {
     const void* p;
     int64_t ld, rows;
 };
-// Whether all of them can be read and written `bytes` at a time.
-bool aligned_to(int bytes, int size, int64_t dim, std::initializer_list<Matrix> ms) {
-    if (dim * size % bytes) return false;
-    for (const Matrix& m : ms)
-        if (m.p && (reinterpret_cast<uintptr_t>(m.p) % bytes || m.ld * size % bytes)) return false;
-    return true;
+// Whether all of their rows begin at multiples of 16 bytes and have whole ones.
+bool in_lines(int size, int64_t dim, std::initializer_list<Matrix> ms) {
+    bool all = dim * size % 16 == 0;
+    for (const Matrix& m : ms) all = all && reinterpret_cast<uintptr_t>(m.p) % 16 == 0 && m.ld * size % 16 == 0;
+    return all;
 }
 bool matrices_ok(int32_t dtype, int64_t dim, std::initializer_list<Matrix> ms) {
     const int size = size_of(dtype);
@@ -835,55 +991,68 @@ int pad_units(const hl_route* r) {
 // Tiles of at most Tile::kChoices choices: as many CTAs as fill whole rounds of the chip.
 int64_t sort_tiles(int64_t n) { return div_up(div_up(n > 0 ? n : 1, Tile::kChoices), kSMsFallback) * kSMsFallback; }
 
-template <typename T, bool ANY>
-int32_t launch_dispatch(const hl_route* r, int64_t dim, const void* x, int64_t ld_x, void* y, int64_t ld_y, cudaStream_t stream) {
-    constexpr int U = ANY ? 1 : 2;
-    const int lines = lines_of<T>(dim, ANY), units = pad_units(r);
-    const int64_t ctas = div_up(r->max_tokens * lines, kRowNT * U);
-    if (ctas + units == 0) return HL_OK;
-    if (ctas + (int64_t)units * r->n_experts > 0x7fffffff) return HL_EINVAL;
-    HL_CUDA_TRY(launch(k_expert_dispatch<T, ANY, U>, ctas + units * r->n_experts, kRowNT, stream, static_cast<const T*>(x), ld_x,
-                       r->n_tokens, r->max_tokens, r->top_k, dim, r->place, r->cap_rows, static_cast<T*>(y), ld_y, lines,
-                       inverse_of(lines), ctas, r->n_experts, units, r->counts, r->offsets));
-    note_launches(1);
-    HL_LAUNCH_CHECK();
-    return HL_OK;
-}
-
-template <typename T, bool ANY>
-int32_t launch_combine(const hl_route* r, int64_t dim, const void* y, int64_t ld_y, const float* w, void* out, int64_t ld_out,
-                       cudaStream_t stream) {
-    const int lines = lines_of<T>(dim, ANY);
-    const bool few = r->top_k <= 2;
-    const int64_t ctas = div_up(r->max_tokens * lines, kRowNT * (few && !ANY ? 2 : 1));
-    if (ctas > 0x7fffffff) return HL_EINVAL;
-    HL_CUDA_TRY(launch(few ? k_expert_combine<T, ANY, 2, ANY ? 1 : 2> : k_expert_combine<T, ANY, 4, 1>, ctas, kRowNT, stream,
-                       static_cast<const T*>(y), ld_y, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, dim, r->place, w,
-                       static_cast<T*>(out), ld_out, lines, inverse_of(lines)));
-    note_launches(1);
-    HL_LAUNCH_CHECK();
-    return HL_OK;
-}
-
-template <typename T, bool ANY>
-int32_t launch_combine_bwd(const hl_route* r, int64_t dim, const void* go, int64_t ld_go, const void* y, int64_t ld_y,
-                           const float* w, void* gy, int64_t ld_gy, float* gw, cudaStream_t stream) {
-    const int lines = lines_of<T>(dim, ANY), units = pad_units(r);
-    // threads of a token: enough for a line each, but few that find no line in the last round, and at most a warp's, unless
-    // there are few tokens
-    int P = 4;
-    while (P < kRowNT && P < lines) {
+// Threads of a token, a power of two: enough for `each` vectors a thread, few of them without one in the last round, and at most
+// a warp's -- or `most`, for rows that long, where there are few tokens.
+int threads_of(const hl_route* r, int64_t vectors, int each, int most) {
+    int P = 1;
+    while (P < most && P * each < vectors) {
         const bool few = r->max_tokens * P < (int64_t)kSMsFallback * 1024;
-        const int64_t idle = div_up(lines, 2 * P) * 2 * P - lines;
-        if (!few && (P >= 32 || 4 * idle > lines)) break;
+        const int64_t round = 2 * P * each, idle = div_up(vectors, round) * round - vectors;
+        if (!few && (P >= 32 || 4 * idle > vectors)) break;
         P *= 2;
     }
+    return P;
+}
+
+template <typename T>
+int32_t launch_dispatch(const hl_route* r, int64_t dim, const void* x, int64_t ld_x, void* y, int64_t ld_y, bool ragged,
+                        cudaStream_t stream) {
+    const int vectors = (int)div_up(dim + (ragged ? Vec<T>::N - 1 : 0), Vec<T>::N), units = pad_units(r);
+    const int64_t ctas = div_up(r->max_tokens * vectors, kRowNT * (ragged ? 1 : kDispatchVectors));
+    if (ctas + units == 0) return HL_OK;
+    if (ctas + (int64_t)units * r->n_experts > 0x7fffffff) return HL_EINVAL;
+    HL_CUDA_TRY(launch(ragged ? k_expert_dispatch_ragged<T> : k_expert_dispatch<T>, ctas + units * r->n_experts, kRowNT, stream,
+                       static_cast<const T*>(x), ld_x, r->n_tokens, r->max_tokens, r->top_k, dim, r->place, r->cap_rows,
+                       static_cast<T*>(y), ld_y, vectors, inverse_of(vectors), ctas, r->n_experts, units, r->counts, r->offsets));
+    note_launches(1);
+    HL_LAUNCH_CHECK();
+    return HL_OK;
+}
+
+template <typename T>
+int32_t launch_combine(const hl_route* r, int64_t dim, const void* y, int64_t ld_y, const float* w, void* out, int64_t ld_out,
+                       bool ragged, cudaStream_t stream) {
+    const int vectors = (int)div_up(dim + (ragged ? Vec<T>::N - 1 : 0), Vec<T>::N);
+    const bool few = !ragged && r->top_k <= 2;
+    const int64_t ctas = div_up(r->max_tokens * vectors, kRowNT * (few ? 2 : 1));
+    if (ctas > 0x7fffffff) return HL_EINVAL;
+    if (ragged) {
+        HL_CUDA_TRY(launch(k_expert_combine_ragged<T>, ctas, kRowNT, stream, static_cast<const T*>(y), ld_y, r->cap_rows, r->n_tokens,
+                           r->max_tokens, r->top_k, dim, r->place, w, static_cast<T*>(out), ld_out, vectors, inverse_of(vectors)));
+    } else {
+        HL_CUDA_TRY(launch(few ? k_expert_combine<T, 2, 2> : k_expert_combine<T, 4, 1>, ctas, kRowNT, stream,
+                           static_cast<const T*>(y), ld_y, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, r->place, w,
+                           static_cast<T*>(out), ld_out, vectors, inverse_of(vectors)));
+    }
+    note_launches(1);
+    HL_LAUNCH_CHECK();
+    return HL_OK;
+}
+
+template <typename T>
+int32_t launch_combine_bwd(const hl_route* r, int64_t dim, const void* go, int64_t ld_go, const void* y, int64_t ld_y,
+                           const float* w, void* gy, int64_t ld_gy, float* gw, bool ragged, cudaStream_t stream) {
+    const int units = pad_units(r), P = threads_of(r, div_up(dim, Vec<T>::N) + ragged, 1, kRowNT);
     const int64_t ctas = div_up(r->max_tokens, kRowNT / P);
     if (ctas + units == 0) return HL_OK;
     if (ctas + (int64_t)units * r->n_experts > 0x7fffffff) return HL_EINVAL;
-    HL_CUDA_TRY(launch(k_expert_combine_bwd<T, ANY>, ctas + units * r->n_experts, kRowNT, stream, static_cast<const T*>(go), ld_go,
-                       static_cast<const T*>(y), ld_y, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, dim, r->place, w,
-                       static_cast<T*>(gy), ld_gy, gw, P, lines, ctas, r->n_experts, units, r->counts, r->offsets));
+    const bool same = ld_y == ld_gy && (reinterpret_cast<uintptr_t>(y) - reinterpret_cast<uintptr_t>(gy)) % 16 == 0;
+    HL_CUDA_TRY(launch(!ragged ? k_expert_combine_bwd<T>
+                       : same  ? k_expert_combine_bwd_ragged<T, true>
+                               : k_expert_combine_bwd_ragged<T, false>,
+                       ctas + units * r->n_experts, kRowNT, stream, static_cast<const T*>(go), ld_go, static_cast<const T*>(y),
+                       ld_y, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, dim, r->place, w, static_cast<T*>(gy), ld_gy, gw,
+                       P, ctas, r->n_experts, units, r->counts, r->offsets));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
@@ -913,9 +1082,13 @@ extern "C" int32_t hl_expert_sort(const hl_route* route, const int32_t* d_expert
     if (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255)) return HL_EINVAL;
     if (ws_bytes < hl_expert_workspace_bytes(route->max_tokens, route->top_k, E)) return HL_ECAPACITY;
     const int32_t cap = (int32_t)(expert_cap < (int64_t(1) << 30) ? expert_cap : 0);
+    const int bits = E <= 16 ? 0 : E <= 64 ? 1 : E <= 256 ? 2 : 3;
+#define HL_BITS(KERNEL, ...)                                                                        \
+    (bits == 0 ? KERNEL<__VA_ARGS__ 4> : bits == 1 ? KERNEL<__VA_ARGS__ 6> : bits == 2 ? KERNEL<__VA_ARGS__ 8> \
+                                                                                     : KERNEL<__VA_ARGS__ 10>)
     if (n <= kOneCluster) {
 #define HL_SORT(CTAS, NT, ITEMS)                                                                                              \
-    launch_cluster(k_expert_sort<CTAS, NT, ITEMS>, CTAS, NT, (Sort<NT, ITEMS>::smem_bytes(E)), CTAS > 1 ? CTAS : 0, stream,   \
+    launch_cluster(HL_BITS(k_expert_sort, CTAS, NT, ITEMS, ), CTAS, NT, (Sort<NT, ITEMS>::smem_bytes(E)), CTAS > 1 ? CTAS : 0, stream,   \
                    d_experts, route->n_tokens, route->max_tokens, route->top_k, E, cap, route->align, route->cap_rows,         \
                    route->place, route->source, route->counts, route->offsets, d_status)
         HL_CUDA_TRY(n <= kFewChoices    ? HL_SORT(1, 128, 4)
@@ -930,7 +1103,7 @@ extern "C" int32_t hl_expert_sort(const hl_route* route, const int32_t* d_expert
     int32_t* totals = static_cast<int32_t*>(d_workspace);
     int32_t* tile_counts = totals + (E + 1);
     uint32_t* ranked = reinterpret_cast<uint32_t*>(tile_counts + tiles * (E + 1));
-    HL_CUDA_TRY(launch_cluster(k_expert_rank, tiles, kTileNT, Tile::smem_bytes(E), 0, stream, d_experts, route->n_tokens,
+    HL_CUDA_TRY(launch_cluster(HL_BITS(k_expert_rank, ), tiles, kTileNT, Tile::smem_bytes(E), 0, stream, d_experts, route->n_tokens,
                                route->max_tokens, route->top_k, E, tile_counts, ranked));
     HL_CUDA_TRY(launch_after(k_expert_scan, div_up(E + 1, 32), kScanNT, 0, stream, tile_counts, tiles, E, totals));
     HL_CUDA_TRY(launch_after(k_expert_place, tiles, kTileNT, place_smem_bytes(E), stream, route->n_tokens, route->max_tokens,
@@ -942,12 +1115,8 @@ extern "C" int32_t hl_expert_sort(const hl_route* route, const int32_t* d_expert
     return HL_OK;
 }
 
-#define HL_FOR_TYPE(CALL)                                                                   \
-    do {                                                                                    \
-        if (dtype == HL_F32) return wide ? CALL(float, false) : CALL(float, true);          \
-        if (dtype == HL_BF16) return wide ? CALL(__nv_bfloat16, false) : CALL(__nv_bfloat16, true); \
-        return wide ? CALL(__half, false) : CALL(__half, true);                             \
-    } while (0)
+#define HL_FOR_TYPE(CALL) \
+    return dtype == HL_F32 ? CALL(float) : dtype == HL_BF16 ? CALL(__nv_bfloat16) : CALL(__half)
 
 extern "C" int32_t hl_expert_dispatch(const hl_route* route, int32_t dtype, int64_t dim, const void* d_x, int64_t ld_x,
                                       void* d_y, int64_t ld_y, void* stream_) {
@@ -957,8 +1126,8 @@ extern "C" int32_t hl_expert_dispatch(const hl_route* route, int32_t dtype, int6
     const Matrix x{d_x, ld_x, route->max_tokens}, y{d_y, ld_y, route->cap_rows};
     if (!matrices_ok(dtype, dim, {x, y})) return HL_EINVAL;
     if (route->cap_rows == 0) return HL_OK;
-    const bool wide = aligned_to(16, size_of(dtype), dim, {x, y});
-#define HL_DISPATCH(T, ANY) launch_dispatch<T, ANY>(route, dim, d_x, ld_x, d_y, ld_y, stream)
+    const bool ragged = !in_lines(size_of(dtype), dim, {x, y});
+#define HL_DISPATCH(T) launch_dispatch<T>(route, dim, d_x, ld_x, d_y, ld_y, ragged, stream)
     HL_FOR_TYPE(HL_DISPATCH);
 #undef HL_DISPATCH
 }
@@ -970,8 +1139,8 @@ extern "C" int32_t hl_expert_combine(const hl_route* route, int32_t dtype, int64
     const Matrix y{d_y, ld_y, route->cap_rows}, out{d_out, ld_out, route->max_tokens};
     if (!matrices_ok(dtype, dim, {y, out})) return HL_EINVAL;
     if (route->max_tokens == 0) return HL_OK;
-    const bool wide = aligned_to(16, size_of(dtype), dim, {y, out});
-#define HL_COMBINE(T, ANY) launch_combine<T, ANY>(route, dim, d_y, ld_y, d_weights, d_out, ld_out, stream)
+    const bool ragged = !in_lines(size_of(dtype), dim, {y, out});
+#define HL_COMBINE(T) launch_combine<T>(route, dim, d_y, ld_y, d_weights, d_out, ld_out, ragged, stream)
     HL_FOR_TYPE(HL_COMBINE);
 #undef HL_COMBINE
 }
@@ -985,9 +1154,10 @@ extern "C" int32_t hl_expert_combine_bwd(const hl_route* route, int32_t dtype, i
     const Matrix go{d_grad_out, ld_grad_out, route->max_tokens}, gy{d_grad_y, ld_grad_y, route->cap_rows};
     const Matrix y{d_grad_weights ? d_y : d_grad_y, d_grad_weights ? ld_y : ld_grad_y, route->cap_rows};   // (else not read)
     if (!matrices_ok(dtype, dim, {go, y, gy})) return HL_EINVAL;
-    const bool wide = aligned_to(16, size_of(dtype), dim, {go, y, gy});
-#define HL_COMBINE_BWD(T, ANY) \
-    launch_combine_bwd<T, ANY>(route, dim, d_grad_out, ld_grad_out, d_y, ld_y, d_weights, d_grad_y, ld_grad_y, d_grad_weights, stream)
+    const bool ragged = !in_lines(size_of(dtype), dim, {go, y, gy});
+#define HL_COMBINE_BWD(T)                                                                                                      \
+    launch_combine_bwd<T>(route, dim, d_grad_out, ld_grad_out, d_y, ld_y, d_weights, d_grad_y, ld_grad_y, d_grad_weights, ragged, \
+                          stream)
     HL_FOR_TYPE(HL_COMBINE_BWD);
 #undef HL_COMBINE_BWD
 }

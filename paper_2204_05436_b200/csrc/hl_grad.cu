@@ -307,28 +307,32 @@ int32_t in_groups(const hl_tensor* ts, int32_t n, bool norm, int tile_bits, F f)
     return HL_OK;
 }
 
-int64_t tiles_of(const hl_tensor* ts, int32_t n, bool norm, int tile_bits) {
-    int64_t tiles = 0;
-    for (int i = 0; i < n; ++i)
-        if (norm ? !(ts[i].flags & HL_TENSOR_NOT_IN_NORM) : ts[i].dst != nullptr) tiles += div_up(ts[i].n, int64_t(1) << tile_bits);
-    return tiles;
+// The tensors of the norm, or those to write, in tiles: the smallest that leave a CTA one, as near as their number and all their
+// values tell.
+struct Tiling {
+    int bits;
+    int64_t tiles;
+};
+Tiling tiling_of(const hl_tensor* ts, int32_t n, bool norm, int most) {
+    int64_t values = 0, some = 0;
+    for (int i = 0; i < n; ++i) {
+        if (ts[i].n == 0 || (norm ? (ts[i].flags & HL_TENSOR_NOT_IN_NORM) != 0 : ts[i].dst == nullptr)) continue;
+        values += ts[i].n;
+        ++some;
+    }
+    int bits = kMinTileBits;
+    while (bits < kMaxTileBits && (values >> bits) + some > most) ++bits;
+    return {bits, (values >> bits) + some};
 }
 
 template <int N>
 int32_t clip(const hl_tensor* ts, int32_t n, const double* further, int32_t n_further, bool scale, float max_norm, float* norm,
              double* partial, cudaStream_t stream) {
     const int most = grad_grid();
-    // the smallest tiles that leave a CTA one
-    const auto bits = [&](bool of_norm) {
-        int b = kMinTileBits;
-        while (b < kMaxTileBits && tiles_of(ts, n, of_norm, b) > most) ++b;
-        return b;
-    };
-    const int norm_bits = bits(true);
-    const int64_t tiles = tiles_of(ts, n, true, norm_bits);
-    const int n_partials = tiles ? grid_for(tiles, 1, most) : 0;
+    const Tiling of_norm = tiling_of(ts, n, true, most);
+    const int n_partials = of_norm.tiles ? grid_for(of_norm.tiles, 1, most) : 0;
     bool more = false;
-    int32_t st = in_groups<N>(ts, n, true, norm_bits, [&](const TensorPairArgs<N>& a) -> int32_t {
+    int32_t st = in_groups<N>(ts, n, true, of_norm.bits, [&](const TensorPairArgs<N>& a) -> int32_t {
         HL_CUDA_TRY(launch(k_grad_squares<N>, n_partials, kNT, stream, a, more ? 1 : 0, partial));   // (later groups add)
         more = true;
         note_launches(1);
@@ -338,7 +342,7 @@ int32_t clip(const hl_tensor* ts, int32_t n, const double* further, int32_t n_fu
     const int first_after = n_partials ? kAfterLast : 0;       // (of what the caller has on the stream, all has to be over)
     bool said = false;
     if (scale) {
-        st = in_groups<N>(ts, n, false, bits(false), [&](const TensorPairArgs<N>& a) -> int32_t {
+        st = in_groups<N>(ts, n, false, tiling_of(ts, n, false, most).bits, [&](const TensorPairArgs<N>& a) -> int32_t {
             HL_CUDA_TRY(launch_cluster(k_grad_scale<N>, grid_for(a.n_tiles, 1, most), kNT, 0, said ? 0 : first_after, stream, a,
                                        (const double*)partial, n_partials, further, n_further, max_norm, said ? nullptr : norm));
             said = true;
@@ -365,6 +369,7 @@ int32_t clip_call(const hl_tensor* ts, int32_t n, const double* further, int32_t
     if (ws_bytes < hl_grad_workspace_bytes()) return HL_ECAPACITY;
     double* partial = static_cast<double*>(ws);
     if (n <= 32) return clip<32>(ts, n, further, n_further, scale, max_norm, norm, partial, stream);
+    if (n <= 256) return clip<256>(ts, n, further, n_further, scale, max_norm, norm, partial, stream);
     return clip<1000>(ts, n, further, n_further, scale, max_norm, norm, partial, stream);
 }
 
@@ -543,14 +548,18 @@ __global__ void __launch_bounds__(kNT) k_rows_long(const int32_t* slots, const i
     __shared__ int s_first;
     __shared__ bool s_last;
     wait_for_last();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t first = (int64_t)blockIdx.x * kWarps + warp;
+    int start = first < max_windows ? starts[first] : 0;       // (of windows that there are not: not looked at)
     const int64_t n = min((int64_t)max(*d_n, 0), max_n), windows = (n + kWindow - 1) / kWindow;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % G, c = blockIdx.y * G + sub;
+    const int sub = lane % G, c = blockIdx.y * G + sub;
     const bool mine = c < D4;
     double total = 0.0;
     for (int64_t w0 = (int64_t)blockIdx.x * kWarps; w0 < windows; w0 += (int64_t)gridDim.x * kWarps) {
         const int64_t w = w0 + warp;
         bool too_long = false;
-        if (w < windows && starts[w]) {
+        if (w != first && w < windows) start = starts[w];
+        if (w < windows && start) {
             const int32_t slot = slots[(w + 1) * kWindow - 1];
             const int64_t next = (w + 2 + lane) * kWindow;
             const unsigned ends = __ballot_sync(0xffffffffu, next >= n || slots[next] != slot);
@@ -665,9 +674,7 @@ extern "C" int32_t hl_embbag_grad_sumsq(hl_ctx* ctx, const int32_t* d_sorted_slo
         return HL_EINVAL;
     const int D4 = ctx->D / 4;
     if (D4 > 256 || (reinterpret_cast<uintptr_t>(d_grad_out) & 15)) return HL_EINVAL;
-    return as_graph(kept_launches(ctx), [&] {
 #define HL_ROWS(G) rows_squares<G>(ctx, d_sorted_slots, d_sorted_bags, d_n_lookups, d_grad_out, d_sumsq, stream)
-        return D4 <= 4 ? HL_ROWS(4) : D4 <= 8 ? HL_ROWS(8) : D4 <= 16 ? HL_ROWS(16) : HL_ROWS(32);
+    return D4 <= 4 ? HL_ROWS(4) : D4 <= 8 ? HL_ROWS(8) : D4 <= 16 ? HL_ROWS(16) : HL_ROWS(32);
 #undef HL_ROWS
-    });
 }
