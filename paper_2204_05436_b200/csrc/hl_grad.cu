@@ -3,8 +3,6 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include <string.h>
-
 #include "hl_common.cuh"
 
 namespace hl {
@@ -39,7 +37,7 @@ struct TensorPairArgs {
     void* dst[N];
     int64_t n[N];
     int32_t first_tile[N];
-    uint8_t kind[N];                                 // type of src, type of dst
+    uint8_t kind[N];                                 // type of src, type of dst (two bits each)
     int32_t n_tensors, n_tiles, tile_bits, unused;
 };
 
@@ -179,6 +177,48 @@ __device__ __forceinline__ int first_of(const TensorPairArgs<N>& a, unsigned b) 
     return (int)((int64_t)a.n_tiles * b / gridDim.x);
 }
 
+template <int N>
+__device__ __forceinline__ double squares_of(const TensorPairArgs<N>& a, int t, int tile) {
+    const int64_t at = (int64_t)(tile - a.first_tile[t]) << a.tile_bits;
+    const int n = (int)min((int64_t)1 << a.tile_bits, a.n[t] - at), from = a.kind[t] & 3;
+    if (from == HL_F32) return tile_squares(static_cast<const float*>(a.src[t]) + at, n);
+    if (from == HL_BF16) return tile_squares(static_cast<const __nv_bfloat16*>(a.src[t]) + at, n);
+    return tile_squares(static_cast<const __half*>(a.src[t]) + at, n);
+}
+
+// What the tensors are scaled by.
+__device__ __forceinline__ float factor_of(double norm, float max_norm) {
+    const double c = (double)max_norm / (norm + 1e-6);
+    return c > 1.0 ? 1.f : (float)c;                 // (NaN: NaN)
+}
+
+template <int N>
+__device__ __forceinline__ void scale(const TensorPairArgs<N>& a, int t, int tile, float f) {
+    const int64_t at = (int64_t)(tile - a.first_tile[t]) << a.tile_bits;
+    const int n = (int)min((int64_t)1 << a.tile_bits, a.n[t] - at);
+    const void* s = a.src[t];
+    void* d = a.dst[t];
+    const int from = a.kind[t] & 3, to = (a.kind[t] >> 2) & 3;
+    if (d == nullptr || (d == s && f == 1.f)) return;
+    using B = __nv_bfloat16;
+    using H = __half;
+#define HL_SCALE(S, D) tile_scale(static_cast<const S*>(s) + at, static_cast<D*>(d) + at, n, f)
+    if (from == HL_F32) {
+        if (to == HL_F32) HL_SCALE(float, float);
+        else if (to == HL_BF16) HL_SCALE(float, B);
+        else HL_SCALE(float, H);
+    } else if (from == HL_BF16) {
+        if (to == HL_F32) HL_SCALE(B, float);
+        else if (to == HL_BF16) HL_SCALE(B, B);
+        else HL_SCALE(B, H);
+    } else {
+        if (to == HL_F32) HL_SCALE(H, float);
+        else if (to == HL_BF16) HL_SCALE(H, B);
+        else HL_SCALE(H, H);
+    }
+#undef HL_SCALE
+}
+
 // partial[b] (+)= the squares of CTA b's tiles
 template <int N>
 __global__ void __launch_bounds__(kNT) k_grad_squares(const __grid_constant__ TensorPairArgs<N> a, int more,
@@ -189,12 +229,7 @@ __global__ void __launch_bounds__(kNT) k_grad_squares(const __grid_constant__ Te
     int tile = first_of(a, blockIdx.x), t = tensor_of(a, tile);
     for (; tile < end; ++tile) {
         if (t + 1 < a.n_tensors && a.first_tile[t + 1] <= tile) ++t;
-        const int kind = a.kind[t];
-        const int64_t at = (int64_t)(tile - a.first_tile[t]) << a.tile_bits;
-        const int n = (int)min((int64_t)1 << a.tile_bits, a.n[t] - at);
-        if ((kind & 3) == HL_F32) sum += tile_squares(static_cast<const float*>(a.src[t]) + at, n);
-        else if ((kind & 3) == HL_BF16) sum += tile_squares(static_cast<const __nv_bfloat16*>(a.src[t]) + at, n);
-        else sum += tile_squares(static_cast<const __half*>(a.src[t]) + at, n);
+        sum += squares_of(a, t, tile);
     }
     sum = block_sum(sum);
     if (threadIdx.x == 0) partial[blockIdx.x] = more ? partial[blockIdx.x] + sum : sum;
@@ -224,33 +259,10 @@ __global__ void __launch_bounds__(kNT, 4) k_grad_scale(const __grid_constant__ T
     wait_for_last();
     const double total = sqrt(total_squares(partial, n_partials, further, n_further));
     if (blockIdx.x == 0 && threadIdx.x == 0 && norm) *norm = (float)total;
-    const double c = (double)max_norm / (total + 1e-6);
-    const float f = c > 1.0 ? 1.f : (float)c;        // (NaN: NaN)
+    const float f = factor_of(total, max_norm);
     for (; tile >= begin; --tile) {
         if (a.first_tile[t] > tile) --t;
-        const int64_t at = (int64_t)(tile - a.first_tile[t]) << a.tile_bits;
-        const int n = (int)min((int64_t)1 << a.tile_bits, a.n[t] - at);
-        const void* s = a.src[t];
-        void* d = a.dst[t];
-        const int from = a.kind[t] & 3, to = (a.kind[t] >> 2) & 3;
-        if (d == s && f == 1.f) continue;
-        using B = __nv_bfloat16;
-        using H = __half;
-#define HL_SCALE(S, D) tile_scale(static_cast<const S*>(s) + at, static_cast<D*>(d) + at, n, f)
-        if (from == HL_F32) {
-            if (to == HL_F32) HL_SCALE(float, float);
-            else if (to == HL_BF16) HL_SCALE(float, B);
-            else HL_SCALE(float, H);
-        } else if (from == HL_BF16) {
-            if (to == HL_F32) HL_SCALE(B, float);
-            else if (to == HL_BF16) HL_SCALE(B, B);
-            else HL_SCALE(B, H);
-        } else {
-            if (to == HL_F32) HL_SCALE(H, float);
-            else if (to == HL_BF16) HL_SCALE(H, B);
-            else HL_SCALE(H, H);
-        }
-#undef HL_SCALE
+        scale(a, t, tile, f);
     }
 }
 
@@ -277,9 +289,15 @@ int grad_grid() {
     return sms * kGradCtas < kMaxPartials ? sms * kGradCtas : kMaxPartials;
 }
 
-// f(args) for the tensors that count (of the norm, or those to write) in groups of at most N, each a kernel's argument
+// The tensors that count: those of the norm, or those to write.
+enum Which { kOfNorm, kToWrite };
+bool counts(const hl_tensor& t, Which which) {
+    return t.n > 0 && (which == kOfNorm ? !(t.flags & HL_TENSOR_NOT_IN_NORM) : t.dst != nullptr);
+}
+
+// f(args) for them in groups of at most N, each a kernel's argument
 template <int N, typename F>
-int32_t in_groups(const hl_tensor* ts, int32_t n, bool norm, int tile_bits, F f) {
+int32_t in_groups(const hl_tensor* ts, int32_t n, Which which, int tile_bits, F f) {
     TensorPairArgs<N> a;
     int i = 0;
     while (i < n) {
@@ -287,7 +305,7 @@ int32_t in_groups(const hl_tensor* ts, int32_t n, bool norm, int tile_bits, F f)
         int64_t tiles = 0;
         for (; i < n && a.n_tensors < N; ++i) {
             const hl_tensor& t = ts[i];
-            if (t.n == 0 || (norm ? (t.flags & HL_TENSOR_NOT_IN_NORM) != 0 : t.dst == nullptr)) continue;
+            if (!counts(t, which)) continue;
             const int64_t more = div_up(t.n, int64_t(1) << tile_bits);
             if (tiles + more > 0x7fffffff) break;
             const int k = a.n_tensors++;
@@ -313,10 +331,10 @@ struct Tiling {
     int bits;
     int64_t tiles;
 };
-Tiling tiling_of(const hl_tensor* ts, int32_t n, bool norm, int most) {
+Tiling tiling_of(const hl_tensor* ts, int32_t n, Which which, int most) {
     int64_t values = 0, some = 0;
     for (int i = 0; i < n; ++i) {
-        if (ts[i].n == 0 || (norm ? (ts[i].flags & HL_TENSOR_NOT_IN_NORM) != 0 : ts[i].dst == nullptr)) continue;
+        if (!counts(ts[i], which)) continue;
         values += ts[i].n;
         ++some;
     }
@@ -329,10 +347,10 @@ template <int N>
 int32_t clip(const hl_tensor* ts, int32_t n, const double* further, int32_t n_further, bool scale, float max_norm, float* norm,
              double* partial, cudaStream_t stream) {
     const int most = grad_grid();
-    const Tiling of_norm = tiling_of(ts, n, true, most);
+    const Tiling of_norm = tiling_of(ts, n, kOfNorm, most);
     const int n_partials = of_norm.tiles ? grid_for(of_norm.tiles, 1, most) : 0;
     bool more = false;
-    int32_t st = in_groups<N>(ts, n, true, of_norm.bits, [&](const TensorPairArgs<N>& a) -> int32_t {
+    int32_t st = in_groups<N>(ts, n, kOfNorm, of_norm.bits, [&](const TensorPairArgs<N>& a) -> int32_t {
         HL_CUDA_TRY(launch(k_grad_squares<N>, n_partials, kNT, stream, a, more ? 1 : 0, partial));   // (later groups add)
         more = true;
         note_launches(1);
@@ -342,7 +360,7 @@ int32_t clip(const hl_tensor* ts, int32_t n, const double* further, int32_t n_fu
     const int first_after = n_partials ? kAfterLast : 0;       // (of what the caller has on the stream, all has to be over)
     bool said = false;
     if (scale) {
-        st = in_groups<N>(ts, n, false, tiling_of(ts, n, false, most).bits, [&](const TensorPairArgs<N>& a) -> int32_t {
+        st = in_groups<N>(ts, n, kToWrite, tiling_of(ts, n, kToWrite, most).bits, [&](const TensorPairArgs<N>& a) -> int32_t {
             HL_CUDA_TRY(launch_cluster(k_grad_scale<N>, grid_for(a.n_tiles, 1, most), kNT, 0, said ? 0 : first_after, stream, a,
                                        (const double*)partial, n_partials, further, n_further, max_norm, said ? nullptr : norm));
             said = true;
@@ -381,6 +399,7 @@ int32_t clip_call(const hl_tensor* ts, int32_t n, const double* further, int32_t
 template <int G>
 struct RowShape {
     static constexpr int kGroups = kNT / G, kRun = G < 16 ? G : 16, kWindow = kGroups * kRun;
+    static_assert(kWindow <= kNT && kGroups <= 64, "a thread asks for a window's lookup; a bit per group");
 };
 
 __device__ __forceinline__ double square(const double (&a)[4]) { return a[0] * a[0] + a[1] * a[1] + a[2] * a[2] + a[3] * a[3]; }
@@ -390,7 +409,8 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
                                                       const int32_t* __restrict__ d_n, int64_t max_n, int64_t n_slots,
                                                       int64_t n_bags, const float4* __restrict__ grad, int D4,
                                                       double* __restrict__ pieces, int32_t* __restrict__ starts,
-                                                      int64_t max_windows, double* __restrict__ partial) {
+                                                      int64_t max_windows, double* __restrict__ partial,
+                                                      double* __restrict__ sumsq) {
     using Shape = RowShape<G>;
     constexpr int kGroups = Shape::kGroups, kWindow = Shape::kWindow, kRun = Shape::kRun, kRows = kRun < 8 ? kRun : 8;
     __shared__ int32_t s_slot[kWindow + 2], s_bag[kWindow];    // s_slot[0]: the lookup before the window's; s_bag -1: none to add
@@ -515,7 +535,7 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
         if (threadIdx.x == 0 && blockIdx.y == 0) starts[w] = any;
     }
     total = block_sum(mine ? total : 0.0);
-    if (threadIdx.x == 0) partial[blockIdx.y * gridDim.x + blockIdx.x] = total;
+    if (threadIdx.x == 0) *(sumsq ? sumsq : &partial[blockIdx.y * gridDim.x + blockIdx.x]) = total;      // sumsq: of the only CTA
 }
 
 // The sum of a run's pieces: the one in window w, in which it starts, and those of the windows up to `last`, by P threads of which
@@ -638,12 +658,18 @@ int32_t rows_squares(hl_ctx* ctx, const int32_t* slots, const int32_t* bags, con
     double* partial = reinterpret_cast<double*>(ctx->r.bwd_hist[1]);
     int32_t* starts = reinterpret_cast<int32_t*>(partial + n_partials);
     if (2 * n_partials + windows + 1 > sort_hist_words(ctx->max_nnz)) return HL_EINVAL;      // (rows of up to 1 024 fp32: never)
+    const bool only = windows == 1 && cols == 1;     // no run goes on behind it
     HL_CUDA_TRY(launch(k_rows_squares<G>, dim3((unsigned)rows_ctas, (unsigned)cols), kNT, stream, slots, bags, d_n, ctx->max_nnz,
                        ctx->hot_cap + ctx->staging_cap, ctx->max_bags, reinterpret_cast<const float4*>(grad), D4, pieces, starts,
-                       windows, partial));
+                       windows, partial, only ? sumsq : nullptr));
+    note_launches(1);
+    if (only) {
+        HL_LAUNCH_CHECK();
+        return HL_OK;
+    }
     HL_CUDA_TRY(launch_after(k_rows_long<G>, dim3((unsigned)long_ctas, (unsigned)cols), kNT, 0, stream, slots, d_n, ctx->max_nnz,
                              D4, (const double*)pieces, starts, windows, partial, n_partials, sumsq));
-    note_launches(2);
+    note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
 }
