@@ -178,6 +178,32 @@ class Hotline:
     def bwd_non(self, grad: torch.Tensor, lr: float) -> None:
         B.hl_embbag_bwd_sgd(self.ctx, self.cache, self.non, self.counts_non, grad, lr, self.main.cuda_stream)
 
+    def update_clipped(self, grad_all: torch.Tensor, lr: float, max_norm: float, others=()) -> torch.Tensor:
+        """One update of every touched row with the whole mini-batch's gradient (Eq. 5), clipped by the global norm: that of the
+        tables' row gradients, in which the lookups of a row are added up first, together with ``others``, the dense model's
+        gradients ((tensor, tensor) in place, or (src, dst) pairs; see binding.make_tensors).  ``grad_all``: the gradients of O's
+        bags, then X's (X's block begins at row tables * n_pop * steps), scaled in place, as ``others`` are.  Call it when X's
+        slots are known (gather_cold) and both forwards are queued.  Returns the norm (fp32 [1], final in the main stream's
+        order; the next call overwrites it)."""
+        if grad_all.dtype != torch.float32 or grad_all.dim() != 2 or grad_all.shape[1] != self.D or not grad_all.is_contiguous() \
+                or grad_all.shape[0] > self.max_bags or grad_all.device.type != "cuda":
+            raise ValueError(f"grad_all is a contiguous fp32 [bags, {self.D}] tensor on the device, of at most {self.max_bags} bags")
+        if not hasattr(self, "clip_sorted"):
+            i32 = dict(dtype=torch.int32, device=self.device)
+            self.clip_sorted = (torch.zeros(max(1, self.max_nnz), **i32), torch.zeros(max(1, self.max_nnz), **i32),
+                                torch.zeros(4, **i32))
+            self.clip_sumsq = torch.zeros(1, dtype=torch.float64, device=self.device)
+            self.clip_norm = torch.zeros(1, dtype=torch.float32, device=self.device)
+            self.clip_ws = torch.empty(B.hl_grad_workspace_bytes(), dtype=torch.uint8, device=self.device)
+        s = self.main.cuda_stream
+        slots, bags, n = self.clip_sorted
+        tensors = B.make_tensors([(grad_all, grad_all, B.HL_TENSOR_NOT_IN_NORM), *others])
+        B.hl_embbag_bwd_prepare_merged(self.ctx, self.pop, self.counts, self.non, self.counts_non, slots, bags, n, s)
+        B.hl_embbag_grad_sumsq(self.ctx, slots, bags, n[2:], grad_all, self.clip_sumsq, s)
+        B.hl_grad_clip(tensors, self.clip_sumsq, 1, max_norm, self.clip_norm, self.clip_ws, self.clip_ws.numel(), s)
+        B.hl_embbag_bwd_apply(self.ctx, self.cache, slots, bags, n[2:], grad_all, lr, s)
+        return self.clip_norm
+
     def scatter_cold(self) -> None:
         B.hl_scatter_cold(self.ctx, self.cache, self.cold_rows, self.n_cold, self.host_table, self.main.cuda_stream)
 
