@@ -4,6 +4,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "hl_common.cuh"
 
 namespace cg = cooperative_groups;
@@ -289,7 +291,7 @@ constexpr int kScanNT = 1024;
 __global__ void __launch_bounds__(kScanNT) k_expert_scan(int32_t* __restrict__ tile_counts, int tiles, int E,
                                                          int32_t* __restrict__ totals) {
     constexpr int kWarps = kScanNT / 32, kAhead = 16;
-    __shared__ int s_sum[kWarps][32];
+    __shared__ int s_sum[kWarps][33];                // (33: read by rows and by columns)
     let_next_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = (int)blockIdx.x * 32 + lane;
     const int per = (tiles + kWarps - 1) / kWarps, t0 = min(warp * per, tiles), t1 = min(t0 + per, tiles);
@@ -303,9 +305,16 @@ __global__ void __launch_bounds__(kScanNT) k_expert_scan(int32_t* __restrict__ t
     for (int t = t0 + kAhead; t < t1; ++t) sum += column[(int64_t)t * (E + 1)];
     s_sum[warp][lane] = sum;
     __syncthreads();
-    int before = 0;
+    const int v = s_sum[lane][warp];                 // of expert `warp`: the sum of warp `lane`
+    int incl = v;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) before += w < warp ? s_sum[w][lane] : 0;
+    for (int d = 1; d < 32; d <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += x;
+    }
+    s_sum[lane][warp] = incl - v;
+    __syncthreads();
+    int before = s_sum[warp][lane];
     if (e > E) return;
     if (warp == kWarps - 1) totals[e] = before + sum;
 #pragma unroll
@@ -394,9 +403,12 @@ __global__ void __launch_bounds__(kTileNT) k_expert_place(const int32_t* n_token
     }
 }
 
-// Which of them sorts n choices.
-constexpr int kClusterCtas = 8;
-constexpr int64_t kFewChoices = 128 * 4, kSomeChoices = kClusterCtas * 512 * 4, kOneCluster = kClusterCtas * 512 * 16;
+// Which of them sorts n choices, up to kOneCluster.  One CTA for as many as its first loads take; then clusters of 8 CTAs, beyond
+// 8 192 choices of 16, with as few rounds unrolled as there can be.  us each, back to back, 8 / 16 CTAs: 4 096 choices of 64 experts
+// 3.9 / 4.0, of 500 4.8 / 5.7 (every CTA reads all the others' counts); 16 000 of 64 5.2 / 4.4, of 500 6.5 / 6.3; 65 536 of 64 11.0 /
+// 7.7, of 500 13.8 / 10.1.  Three kernels take 11.5 (64 experts) to 12.3 us (500) from 17 000 to 131 072 choices, a cluster 11.7 and
+// 15.1 at 131 072, 9.8 and 12.3 at 90 000.
+constexpr int64_t kFewChoices = 128 * 4, kOneCluster = 16 * 512 * 12;
 
 // ---- rows -----------------------------------------------------------------------------------------------------------
 // 16 bytes of a row are moved as one.  Where all rows of a call begin at multiples of 16 bytes and have whole ones, that is a load or
@@ -463,7 +475,6 @@ struct Rows {
 
 constexpr int kRowNT = 256;
 
-// Rows that fill experts up: CTA u of units x E takes every units-th of expert u % E's.
 template <typename T>
 __device__ __forceinline__ int in_line(const T* p) {           // values between the 16-byte line's begin and p
     return (int)(reinterpret_cast<uintptr_t>(p) & 15) / (int)sizeof(T);
@@ -481,16 +492,21 @@ __device__ __forceinline__ void store_line(T* row, int e, int dim, const Vec<T>&
         if ((unsigned)(e + j) < (unsigned)dim) row[e + j] = v.value(j);
 }
 
+// Rows that fill experts up: CTA u of units x E takes every units-th of expert u % E's, several side by side if they are short.
 template <typename T>
 __device__ __forceinline__ void zero_pads(int u, int units, int E, const int32_t* __restrict__ counts,
                                           const int32_t* __restrict__ offsets, int cap_rows, Rows<T> y, int dim) {
+    constexpr int N = Vec<T>::N;
     const int e = u % E, part = u / E, end = min(__ldg(&offsets[e + 1]), cap_rows);
     const int64_t first = __ldg(&offsets[e]), count = __ldg(&counts[e]);
     if (first < 0 || count < 0) return;
+    int P = 1;                         // threads of a row
+    while (P < kRowNT && P * N < dim) P *= 2;
+    const int sub = threadIdx.x & (P - 1), side = threadIdx.x / P, sides = kRowNT / P;
     const Vec<T> zero;
-    for (int64_t r = first + count + part; r < end; r += units) {
+    for (int64_t r = first + count + part * sides + side; r < end; r += units * sides) {
         T* row = y.at((int)r);
-        for (int c = (int)threadIdx.x * Vec<T>::N - in_line(row); c < dim; c += kRowNT * Vec<T>::N) store_line(row, c, dim, zero);
+        for (int c = sub * N - in_line(row); c < dim; c += P * N) store_line(row, c, dim, zero);
     }
 }
 
@@ -988,6 +1004,40 @@ int pad_units(const hl_route* r) {
     return (int)(u < r->align - 1 ? u : r->align - 1);
 }
 
+// Whether the current device can place clusters of 16 CTAs (a non-portable size) of the sort; asked once per device.
+template <int ITEMS, int BITS>
+bool wide_cluster() {
+    auto* kernel = k_expert_sort<16, 512, ITEMS, BITS>;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 16;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(16);
+    cfg.blockDim = dim3(512);
+    cfg.dynamicSmemBytes = Sort<512, ITEMS>::smem_bytes(HL_MAX_EXPERTS);
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+           cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters >= 1;
+}
+template <int ITEMS>
+bool wide_cluster_of() {
+    return wide_cluster<ITEMS, 4>() && wide_cluster<ITEMS, 6>() && wide_cluster<ITEMS, 8>() && wide_cluster<ITEMS, 10>();
+}
+bool wide_clusters() {
+    static std::atomic<int> known[64];               // 0: not asked yet, 1: no, 2: yes
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+    const int k = known[dev].load(std::memory_order_acquire);
+    if (k) return k == 2;
+    const bool yes = wide_cluster_of<2>() && wide_cluster_of<4>() && wide_cluster_of<8>() && wide_cluster_of<12>();
+    (void)cudaGetLastError();
+    known[dev].store(yes ? 2 : 1, std::memory_order_release);
+    return yes;
+}
+
 // Tiles of at most Tile::kChoices choices: as many CTAs as fill whole rounds of the chip.
 int64_t sort_tiles(int64_t n) { return div_up(div_up(n > 0 ? n : 1, Tile::kChoices), kSMsFallback) * kSMsFallback; }
 
@@ -1068,7 +1118,7 @@ extern "C" size_t hl_expert_workspace_bytes(int64_t max_tokens, int32_t top_k, i
         max_tokens * top_k >= (int64_t(1) << 30))
         return 0;
     const int64_t n = max_tokens * top_k;
-    if (n <= kOneCluster) return 256;
+    if (n <= 8 * 512 * 2) return 256;
     return (((sort_tiles(n) + 1) * (n_experts + 1) + n) * sizeof(int32_t) + 255) & ~size_t(255);
 }
 
@@ -1086,14 +1136,17 @@ extern "C" int32_t hl_expert_sort(const hl_route* route, const int32_t* d_expert
 #define HL_BITS(KERNEL, ...)                                                                        \
     (bits == 0 ? KERNEL<__VA_ARGS__ 4> : bits == 1 ? KERNEL<__VA_ARGS__ 6> : bits == 2 ? KERNEL<__VA_ARGS__ 8> \
                                                                                      : KERNEL<__VA_ARGS__ 10>)
-    if (n <= kOneCluster) {
+    if (n <= 8 * 512 * 2 || (n <= kOneCluster && wide_clusters())) {
 #define HL_SORT(CTAS, NT, ITEMS)                                                                                              \
-    launch_cluster(HL_BITS(k_expert_sort, CTAS, NT, ITEMS, ), CTAS, NT, (Sort<NT, ITEMS>::smem_bytes(E)), CTAS > 1 ? CTAS : 0, stream,   \
-                   d_experts, route->n_tokens, route->max_tokens, route->top_k, E, cap, route->align, route->cap_rows,         \
-                   route->place, route->source, route->counts, route->offsets, d_status)
+    launch_cluster(HL_BITS(k_expert_sort, CTAS, NT, ITEMS, ), CTAS, NT, (Sort<NT, ITEMS>::smem_bytes(E)), CTAS > 1 ? CTAS : 0, \
+                   stream, d_experts, route->n_tokens, route->max_tokens, route->top_k, E, cap, route->align,                  \
+                   route->cap_rows, route->place, route->source, route->counts, route->offsets, d_status)
         HL_CUDA_TRY(n <= kFewChoices    ? HL_SORT(1, 128, 4)
-                    : n <= kSomeChoices ? HL_SORT(kClusterCtas, 512, 4)
-                                        : HL_SORT(kClusterCtas, 512, 16));
+                    : n <= 8 * 512 * 2  ? HL_SORT(8, 512, 2)
+                    : n <= 16 * 512 * 2 ? HL_SORT(16, 512, 2)
+                    : n <= 16 * 512 * 4 ? HL_SORT(16, 512, 4)
+                    : n <= 16 * 512 * 8 ? HL_SORT(16, 512, 8)
+                                        : HL_SORT(16, 512, 12));
 #undef HL_SORT
         note_launches(1);
         HL_LAUNCH_CHECK();

@@ -415,6 +415,7 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
     constexpr int kGroups = Shape::kGroups, kWindow = Shape::kWindow, kRun = Shape::kRun, kRows = kRun < 8 ? kRun : 8;
     __shared__ int32_t s_slot[kWindow + 2], s_bag[kWindow];    // s_slot[0]: the lookup before the window's; s_bag -1: none to add
     __shared__ __align__(16) double s_head[kNT][4];            // of a run that an earlier group began, by lane
+    __shared__ int32_t s_start;
     __shared__ uint32_t s_whole[kGroups / 32 + 1];             // groups whose lookups are all of a run that goes on behind them
     let_next_start();
     const int64_t n = min((int64_t)max(__ldg(d_n), 0), max_n), windows = (n + kWindow - 1) / kWindow;
@@ -445,13 +446,15 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
         }
         if (threadIdx.x < 2) s_slot[threadIdx.x ? kWindow + 1 : 0] = around_ahead;
         if (threadIdx.x <= kGroups / 32) s_whole[threadIdx.x] = 0;
+        if (threadIdx.x == 0) s_start = 0;
         __syncthreads();
         if (w + gridDim.x < windows) ask(w + gridDim.x);
         const int l0 = g * kRun, len = max(0, min(kRun, here - l0));
         double acc[4] = {};
         bool cont = false, whole = false, open = false;
+        int32_t slot = 0;
         if (len > 0) {
-            int32_t slot = s_slot[1 + l0];
+            slot = s_slot[1 + l0];
             cont = begin + l0 > 0 && s_slot[l0] == slot;
             bool head = cont;                            // the run at hand began before this group's lookups
 #pragma unroll 1
@@ -523,16 +526,18 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
 #pragma unroll
                 for (int k = 0; k < 4; ++k) pieces[((w * 2 + 0) * D4 + c) * 4 + k] = a[k];
         }
-        bool out = false;
         if (open) {
-            out = add_from(g + 1, acc);
-            if (!out) total += square(acc);
-            else if (mine)
+            if (!add_from(g + 1, acc)) {
+                total += square(acc);
+            } else {                                         // on into the next window (one run at most)
+                if (sub == 0) s_start = slot + 1;
+                if (mine)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) pieces[((w * 2 + 1) * D4 + c) * 4 + k] = acc[k];
+                    for (int k = 0; k < 4; ++k) pieces[((w * 2 + 1) * D4 + c) * 4 + k] = acc[k];
+            }
         }
-        const int any = __syncthreads_or(out);
-        if (threadIdx.x == 0 && blockIdx.y == 0) starts[w] = any;
+        __syncthreads();
+        if (threadIdx.x == 0 && blockIdx.y == 0) starts[w] = s_start;        // (0: none; the same thread clears it)
     }
     total = block_sum(mine ? total : 0.0);
     if (threadIdx.x == 0) *(sumsq ? sumsq : &partial[blockIdx.y * gridDim.x + blockIdx.x]) = total;      // sumsq: of the only CTA
@@ -580,7 +585,7 @@ __global__ void __launch_bounds__(kNT) k_rows_long(const int32_t* slots, const i
         bool too_long = false;
         if (w != first && w < windows) start = starts[w];
         if (w < windows && start) {
-            const int32_t slot = slots[(w + 1) * kWindow - 1];
+            const int32_t slot = start - 1;
             const int64_t next = (w + 2 + lane) * kWindow;
             const unsigned ends = __ballot_sync(0xffffffffu, next >= n || slots[next] != slot);
             too_long = ends == 0;

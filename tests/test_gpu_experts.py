@@ -110,7 +110,9 @@ def _check_sort(hl, experts, E, align=1, live=None, cap=0, cap_rows=None, source
 
 @pytest.mark.parametrize("T,K,E", [(1, 1, 1), (1, 2, 8), (3, 64, 5), (31, 1, 2), (33, 4, 8), (257, 3, 37), (1000, 8, 1024),
                                    (4096, 2, 64), (4097, 2, 64), (8191, 1, 3), (8193, 1, 1000), (16384, 4, 64), (16385, 4, 257),
-                                   (70001, 1, 1024), (40000, 8, 256), (300_000, 1, 2), (1_000_003, 1, 128)])
+                                   (70001, 1, 1024), (40000, 8, 256), (300_000, 1, 2), (1_000_003, 1, 128),
+                                   (512, 1, 16), (513, 1, 17), (8192, 1, 500), (8193, 1, 64), (32768, 1, 1024), (32769, 1, 65),
+                                   (65536, 1, 16), (65537, 1, 300), (98304, 1, 256), (98305, 1, 257)])
 def test_sort_sizes(hl, T, K, E):
     _check_sort(hl, _choices(T, K, E, T + K, skew=0.8, none=0.05), E)
 
