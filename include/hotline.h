@@ -628,7 +628,8 @@ HL_API int32_t hl_expert_combine_bwd(const hl_route* route, int32_t dtype, int64
                                      void* d_grad_y, int64_t ld_grad_y, float* d_grad_weights, void* stream);
 
 /* One of many gradient tensors: n values at src; hl_grad_clip writes them, scaled, to dst (dst == src: in place, with the
- * same type; NULL: nowhere). */
+ * same type; NULL: nowhere).  Apart from that no dst overlaps a src or another dst.  Any alignment of the type's; src and dst
+ * that lie alike modulo 16 bytes move fastest. */
 typedef struct {
     const void* src;
     void*       dst;
@@ -649,8 +650,8 @@ HL_API int32_t hl_grad_norm(const hl_tensor* tensors, int32_t n_tensors, const d
                             float* d_norm, void* d_workspace, size_t ws_bytes, void* stream);
 
 /* hl_grad_norm, and every tensor scaled by min(1, max_norm / (norm + 1e-6)): dst = factor * src (fp32, rounded once to dst's
- * type).  Tensors in place keep their bits when the factor is 1.  A norm that is infinite makes the factor 0, one that is
- * NaN makes it NaN; *d_norm (may be NULL) shows both. */
+ * type).  Tensors in place keep their bits when the factor is 1.  max_norm >= 0.  A norm that is infinite makes the factor 0
+ * (of a finite max_norm), one that is NaN makes it NaN; *d_norm (may be NULL) shows both. */
 HL_API int32_t hl_grad_clip(const hl_tensor* tensors, int32_t n_tensors, const double* d_further, int32_t n_further,
                             float max_norm, float* d_norm, void* d_workspace, size_t ws_bytes, void* stream);
 

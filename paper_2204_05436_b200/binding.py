@@ -726,14 +726,19 @@ def make_route(max_tokens: int, n_tokens, top_k: int, n_experts: int, align: int
 
 def make_tensors(pairs):
     """The list that hl_grad_norm and hl_grad_clip take, from (src, dst) or (src, dst, flags) of contiguous torch tensors;
-    dst may be None, or src itself (in place).  It keeps their addresses, not the tensors."""
+    dst may be None, or src itself (in place); none is written twice.  It keeps their addresses, not the tensors."""
     arr = (hl_tensor * len(pairs))()
+    written = set()
     for i, pair in enumerate(pairs):
         src, dst, flags = pair if len(pair) == 3 else (*pair, 0)
         if not src.is_contiguous() or (dst is not None and (not dst.is_contiguous() or dst.numel() != src.numel())):
             raise ValueError("gradient tensors are contiguous, and dst has as many values as src")
         if dst is not None and dst.device != src.device:
             raise ValueError("src and dst are on one device")
+        if dst is not None and dst.numel() > 0:
+            if _ptr(dst) in written:
+                raise ValueError("a tensor is written twice")
+            written.add(_ptr(dst))
         arr[i] = hl_tensor(_ptr(src), _ptr(dst), src.numel(), dtype_of(src), dtype_of(src if dst is None else dst),
                            int(flags), 0)
     return arr

@@ -965,8 +965,13 @@ __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd_ragged(
 }
 
 // ---- arguments ------------------------------------------------------------------------------------------------------
+bool words(std::initializer_list<const void*> ps) {            // (NULL, too)
+    for (const void* p : ps)
+        if (reinterpret_cast<uintptr_t>(p) & 3) return false;
+    return true;
+}
 bool route_ok(const hl_route* r) {
-    return r && r->max_tokens >= 0 && r->max_tokens < (int64_t(1) << 30) && r->top_k >= 1 && r->top_k <= HL_MAX_TOP_K && r->n_experts >= 1 &&
+    return r && words({r->n_tokens, r->place, r->source, r->counts, r->offsets}) && r->max_tokens >= 0 && r->max_tokens < (int64_t(1) << 30) && r->top_k >= 1 && r->top_k <= HL_MAX_TOP_K && r->n_experts >= 1 &&
            r->n_experts <= HL_MAX_EXPERTS && r->max_tokens * r->top_k < (int64_t(1) << 30) && r->align >= 1 &&
            r->align <= 65536 && r->cap_rows >= 0 && r->cap_rows < (int64_t(1) << 31) - 65536 &&
            (r->place || r->max_tokens == 0);
@@ -1125,7 +1130,8 @@ extern "C" size_t hl_expert_workspace_bytes(int64_t max_tokens, int32_t top_k, i
 extern "C" int32_t hl_expert_sort(const hl_route* route, const int32_t* d_experts, int64_t expert_cap, int32_t* d_status,
                                   void* d_workspace, size_t ws_bytes, void* stream_) {
     const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if (!route_ok(route) || !route->counts || !route->offsets || (!d_experts && route->max_tokens > 0) || expert_cap < 0)
+    if (!route_ok(route) || !route->counts || !route->offsets || (!d_experts && route->max_tokens > 0) || expert_cap < 0 ||
+        !words({d_experts, d_status}))
         return HL_EINVAL;
     const int64_t n = route->max_tokens * route->top_k;
     const int E = route->n_experts;
@@ -1188,7 +1194,7 @@ extern "C" int32_t hl_expert_dispatch(const hl_route* route, int32_t dtype, int6
 extern "C" int32_t hl_expert_combine(const hl_route* route, int32_t dtype, int64_t dim, const void* d_y, int64_t ld_y,
                                      const float* d_weights, void* d_out, int64_t ld_out, void* stream_) {
     const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if (!route_ok(route)) return HL_EINVAL;
+    if (!route_ok(route) || !words({d_weights})) return HL_EINVAL;
     const Matrix y{d_y, ld_y, route->cap_rows}, out{d_out, ld_out, route->max_tokens};
     if (!matrices_ok(dtype, dim, {y, out})) return HL_EINVAL;
     if (route->max_tokens == 0) return HL_OK;
@@ -1202,7 +1208,7 @@ extern "C" int32_t hl_expert_combine_bwd(const hl_route* route, int32_t dtype, i
                                          int64_t ld_grad_out, const void* d_y, int64_t ld_y, const float* d_weights,
                                          void* d_grad_y, int64_t ld_grad_y, float* d_grad_weights, void* stream_) {
     const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if (!route_ok(route)) return HL_EINVAL;
+    if (!route_ok(route) || !words({d_weights, d_grad_weights})) return HL_EINVAL;
     if (route->align > 1 && (!route->counts || !route->offsets)) return HL_EINVAL;
     const Matrix go{d_grad_out, ld_grad_out, route->max_tokens}, gy{d_grad_y, ld_grad_y, route->cap_rows};
     const Matrix y{d_grad_weights ? d_y : d_grad_y, d_grad_weights ? ld_y : ld_grad_y, route->cap_rows};   // (else not read)

@@ -701,7 +701,7 @@ extern "C" int32_t hl_grad_clip(const hl_tensor* tensors, int32_t n_tensors, con
 extern "C" int32_t hl_embbag_grad_sumsq(hl_ctx* ctx, const int32_t* d_sorted_slots, const int32_t* d_sorted_bags,
                                         const int32_t* d_n_lookups, const float* d_grad_out, double* d_sumsq, void* stream_) {
     const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if (!ctx || !d_n_lookups || !d_sumsq || (ctx->max_nnz > 0 && (!d_sorted_slots || !d_sorted_bags || !d_grad_out)))
+    if (!ctx || !d_n_lookups || !d_sumsq || (reinterpret_cast<uintptr_t>(d_sumsq) & 7) || (ctx->max_nnz > 0 && (!d_sorted_slots || !d_sorted_bags || !d_grad_out)))
         return HL_EINVAL;
     const int D4 = ctx->D / 4;
     if (D4 > 256 || (reinterpret_cast<uintptr_t>(d_grad_out) & 15)) return HL_EINVAL;

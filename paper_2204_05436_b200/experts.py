@@ -81,6 +81,12 @@ class ExpertRoute:
             raise ValueError(f"the values of a row of {name} lie side by side, and rows do not overlap")
         return ld
 
+    @staticmethod
+    def _apart(a: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+        for o in others:
+            if o is not None and o.numel() and a.numel() and o.data_ptr() == a.data_ptr():
+                raise ValueError("what is written is none of what is read")
+
     def sort(self, experts: torch.Tensor, n_tokens: Optional[torch.Tensor] = None, expert_cap: int = 0) -> None:
         """Makes the plan from the router's choices, int32 [tokens, top_k] with at most max_tokens tokens.  ``n_tokens`` (int32 [1],
         on the device): how many of them there are (hl_fragment's counts, say); the tensor is read by all later calls too, and
@@ -113,6 +119,7 @@ class ExpertRoute:
         if out is None:
             out = torch.zeros(self.cap_rows, x.shape[1], dtype=x.dtype, device=x.device)
         ld_out = self._rows("out", out, self.cap_rows, x)
+        self._apart(out, x)
         self._call(B.hl_expert_dispatch, self._route, B.dtype_of(x), x.shape[1], x, ld, out, ld_out)
         return out
 
@@ -128,6 +135,7 @@ class ExpertRoute:
         if out is None:
             out = torch.zeros(self.tokens, y.shape[1], dtype=y.dtype, device=y.device)
         ld_out = self._rows("out", out, self.tokens, y)
+        self._apart(out, y)
         self._call(B.hl_expert_combine, self._route, B.dtype_of(y), y.shape[1], y, ld, weights, out, ld_out)
         return out
 
@@ -142,6 +150,7 @@ class ExpertRoute:
         if grad_y is None:
             grad_y = torch.zeros(self.cap_rows, grad_out.shape[1], dtype=grad_out.dtype, device=grad_out.device)
         ld_gy = self._rows("grad_y", grad_y, self.cap_rows, grad_out)
+        self._apart(grad_y, grad_out, y)
         if y is None:
             if grad_weights is not None:
                 raise ValueError("the gradient of the weights needs y")

@@ -293,9 +293,10 @@ def test_rows_that_begin_anywhere(hl, dtype, shift):
     assert ((gy[:end, :D].double() - e).abs() <= (S + _u(dtype) * (1 + S)) * e.abs() + _tiny(dtype)).all()
 
 
-def test_a_captured_run_replayed_with_other_choices(hl):
+@pytest.mark.parametrize("T", [600, 60_000])
+def test_a_captured_run_replayed_with_other_choices(hl, T):
     """Sort, there, back and the gradients as one graph, beside eager calls with another workspace."""
-    T, K, E, D = 600, 2, 16, 256
+    K, E, D = 2, 16, 256 if T < 1000 else 24
     p, q = _Route(hl, T, K, E, 8), _Route(hl, T, K, E, 8)
     e = torch.from_numpy(_choices(T, K, E, 1)).cuda()
     x, w = _rows(T, D, torch.bfloat16, 0, 1), torch.rand(T, K, device="cuda")
@@ -386,6 +387,39 @@ def test_values_that_are_not_finite_stay_where_they_are(hl):
     hl.hl_expert_combine(p.route, hl.HL_BF16, D, y, D, None, out, D, _stream())
     bad = ~torch.isfinite(out)
     assert bad.sum().item() == 2 and torch.isinf(out[3, 5]) and torch.isnan(out[4, 6])
+
+
+def test_the_first_call_of_all_can_be_captured():
+    """In a process of its own, in which no kernel has been loaded."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch, paper_2204_05436_b200 as hl
+T, K, E, D = 20000, 2, 8, 64
+r = hl.ExpertRoute(T, K, E, align=8)
+e = torch.randint(0, E, (T, K), dtype=torch.int32, device="cuda")
+x = torch.randn(T, D, device="cuda")
+y, out = torch.zeros(r.cap_rows, D, device="cuda"), torch.zeros(T, D, device="cuda")
+ts = hl.make_tensors([(out, out)])
+ws, norm = torch.empty(hl.hl_grad_workspace_bytes(), dtype=torch.uint8, device="cuda"), torch.zeros(1, device="cuda")
+s = torch.cuda.Stream()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g, stream=s):
+    r.sort(e)
+    r.combine(r.dispatch(x, y), None, out)
+    hl.hl_grad_clip(ts, None, 0, 1.0, norm, ws, ws.numel(), torch.cuda.current_stream().cuda_stream)
+g.replay()
+torch.cuda.synchronize()
+n = (2 * x).double().norm()
+assert abs(norm.item() - n.item()) <= 1e-6 * n.item()
+assert (out.double() - 2 * x.double() / (n + 1e-6)).abs().max() <= 1e-6 * (2 * x).abs().max() / n
+print("ok")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0 and out.stdout.strip().endswith("ok"), out.stderr[-2000:]
 
 
 def test_places_outside_the_buffer_are_skipped(hl):

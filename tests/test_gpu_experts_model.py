@@ -178,6 +178,10 @@ def test_what_a_route_refuses(hl):
     with pytest.raises(ValueError):
         r.combine(y, w, out=torch.zeros(8, 16, dtype=torch.bfloat16, device="cuda"))
     with pytest.raises(ValueError):
+        r.combine(y, w, out=y[:8])
+    with pytest.raises(ValueError):
+        r.combine_backward(x, y, w, grad_y=y)
+    with pytest.raises(ValueError):
         r.combine_backward(x, None, w, grad_weights=w)
     with pytest.raises(ValueError):
         r.combine_backward(x, y[:, :8], w)

@@ -27,7 +27,8 @@ def _refused(hl, status, f, *a):
 
 @pytest.mark.parametrize("change", [dict(max_tokens=-1), dict(max_tokens=2 ** 30), dict(max_tokens=2 ** 62), dict(top_k=0), dict(top_k=65),
                                     dict(max_tokens=2 ** 29, top_k=2), dict(n_experts=0), dict(n_experts=1025), dict(align=0),
-                                    dict(align=65537), dict(cap_rows=-1), dict(cap_rows=2 ** 31), dict(place=None)])
+                                    dict(align=65537), dict(cap_rows=-1), dict(cap_rows=2 ** 31), dict(place=None), dict(place=P + 2),
+                                    dict(n_tokens=P + 1), dict(counts=P + 2), dict(offsets=P + 1), dict(source=P + 3)])
 def test_routes(hl, change):
     r = hl.make_route(**{**ROUTE, **change})
     _refused(hl, hl.HL_EINVAL, hl.hl_expert_sort, r, P, 0, None, P, 1 << 40, None)
@@ -41,6 +42,8 @@ def test_sort(hl):
     need = hl.hl_expert_workspace_bytes(100, 2, 8)
     _refused(hl, hl.HL_EINVAL, hl.hl_expert_sort, r, None, 0, None, P, need, None)
     _refused(hl, hl.HL_EINVAL, hl.hl_expert_sort, r, P, -1, None, P, need, None)
+    _refused(hl, hl.HL_EINVAL, hl.hl_expert_sort, r, P + 1, 0, None, P, need, None)
+    _refused(hl, hl.HL_EINVAL, hl.hl_expert_sort, r, P, 0, P + 2, P, need, None)
     _refused(hl, hl.HL_EINVAL, hl.hl_expert_sort, r, P, 0, None, None, need, None)
     _refused(hl, hl.HL_EINVAL, hl.hl_expert_sort, r, P, 0, None, P + 128, need, None)
     _refused(hl, hl.HL_ECAPACITY, hl.hl_expert_sort, r, P, 0, None, P, need - 1, None)
@@ -60,6 +63,9 @@ def test_rows(hl):
         _refused(hl, hl.HL_EINVAL, hl.hl_expert_combine, r, dtype, dim, x, ldx, None, y, ldy, None)
         _refused(hl, hl.HL_EINVAL, hl.hl_expert_combine_bwd, r, dtype, dim, x, ldx, P, max(dim, 1), None, y, ldy, None, None)
     _refused(hl, hl.HL_EINVAL, hl.hl_expert_combine_bwd, r, 0, 16, P, 16, None, 16, None, P, 16, P, None)      # y, for weights' gradient
+    _refused(hl, hl.HL_EINVAL, hl.hl_expert_combine, r, 0, 16, P, 16, P + 2, P, 16, None)
+    _refused(hl, hl.HL_EINVAL, hl.hl_expert_combine_bwd, r, 0, 16, P, 16, P, 16, P + 1, P, 16, P, None)
+    _refused(hl, hl.HL_EINVAL, hl.hl_expert_combine_bwd, r, 0, 16, P, 16, P, 16, P, P, 16, P + 2, None)
     for missing in ("counts", "offsets"):                                      # what fills experts up needs them
         q = hl.make_route(**{**ROUTE, missing: None})
         _refused(hl, hl.HL_EINVAL, hl.hl_expert_dispatch, q, 0, 16, P, 16, P, 16, None)
@@ -94,9 +100,13 @@ def test_gradient_lists(hl):
 def test_lists_from_tensors(hl):
     torch = pytest.importorskip("torch")
     a, b = torch.zeros(6, 4), torch.zeros(24, dtype=torch.bfloat16)
-    ts = hl.make_tensors([(a, None), (a, b), (b, b, hl.HL_TENSOR_NOT_IN_NORM)])
+    c = torch.zeros(24, dtype=torch.bfloat16)
+    ts = hl.make_tensors([(a, None), (a, b), (c, c, hl.HL_TENSOR_NOT_IN_NORM)])
     assert [(t.n, t.src_dtype, t.dst_dtype, t.flags, bool(t.dst)) for t in ts] == [(24, 0, 0, 0, False), (24, 0, 1, 0, True),
                                                                                   (24, 1, 1, 1, True)]
+    with pytest.raises(ValueError):
+        hl.make_tensors([(a, b), (a.half(), b)])
+    hl.make_tensors([(a, None), (a, None), (torch.zeros(0), torch.zeros(0)), (torch.zeros(0), torch.zeros(0))])
     for bad, error in [((a.t(), None), ValueError), ((a, torch.zeros(23)), ValueError), ((a, b[::2]), ValueError),
                        ((a.double(), None), TypeError), ((a, torch.zeros(24, dtype=torch.int32)), TypeError)]:
         with pytest.raises(error):
