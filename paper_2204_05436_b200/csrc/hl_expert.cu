@@ -457,7 +457,7 @@ struct Vec {
     __device__ __forceinline__ T value(int i) const {
         const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
         if constexpr (sizeof(T) == 4) {
-            return __uint_as_float(w[i]);
+            return *reinterpret_cast<const T*>(&w[i]);
         } else {
             const uint16_t h = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
             return *reinterpret_cast<const T*>(&h);
@@ -533,9 +533,11 @@ struct Items {
 };
 uint64_t inverse_of(int vectors) { return vectors == 1 ? 0 : ~uint64_t(0) / vectors + 1; }
 
-// y[place[t, k]] = x[t].  A thread takes two vectors of tokens' rows, which it reads once for all of a token's rows.
-constexpr int kDispatchVectors = 2;
-template <typename T>
+// y[place[t, k]] = x[t], V at a time: 16 bytes, or as many as all rows begin at multiples of and have whole ones of.  A thread takes U
+// of them of tokens' rows, which it reads once for all of a token's rows.  T: what a value is, as far as copying goes.
+template <typename V>
+constexpr int kDispatchVectors = sizeof(V) == 16 ? 2 : 4;
+template <typename T, typename V>
 __global__ void __launch_bounds__(kRowNT, 6) k_expert_dispatch(const T* __restrict__ x_, int ld_x, const int32_t* n_tokens,
                                                                int max_tokens, int top_k, int dim,
                                                                const int32_t* __restrict__ place, int cap_rows,
@@ -543,7 +545,7 @@ __global__ void __launch_bounds__(kRowNT, 6) k_expert_dispatch(const T* __restri
                                                                int row_ctas, int E, int pad_units,
                                                                const int32_t* __restrict__ counts,
                                                                const int32_t* __restrict__ offsets) {
-    constexpr int KU = 4, U = kDispatchVectors, W = Vec<T>::N;
+    constexpr int KU = 4, U = kDispatchVectors<V>, W = sizeof(V) / sizeof(T);
     const Rows<const T> x{x_, ld_x};
     const Rows<T> y{y_, ld_y};
     if ((int)blockIdx.x >= row_ctas) {
@@ -552,13 +554,13 @@ __global__ void __launch_bounds__(kRowNT, 6) k_expert_dispatch(const T* __restri
     }
     const int tokens = live_choices(n_tokens, max_tokens, 1);
     const Items<U> items(vectors, inverse);
-    Vec<T> v[U];
+    V v[U];
     int t[U], c[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         items.get(u, &t[u], &c[u]);
         c[u] *= W;
-        if (t[u] < tokens) v[u].load(x.at(t[u]) + c[u]);
+        if (t[u] < tokens) v[u] = __ldg(reinterpret_cast<const V*>(x.at(t[u]) + c[u]));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -570,7 +572,7 @@ __global__ void __launch_bounds__(kRowNT, 6) k_expert_dispatch(const T* __restri
             for (int q = 0; q < KU; ++q) row[q] = k0 + q < top_k ? __ldg(&at[k0 + q]) : -1;
 #pragma unroll
             for (int q = 0; q < KU; ++q)
-                if ((unsigned)row[q] < (unsigned)cap_rows) v[u].store(y.at(row[q]) + c[u]);
+                if ((unsigned)row[q] < (unsigned)cap_rows) *reinterpret_cast<V*>(y.at(row[q]) + c[u]) = v[u];
         }
     }
 }
@@ -763,7 +765,7 @@ __device__ __forceinline__ void put_value(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put_value(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 __device__ __forceinline__ void put_value(__half* p, float x) { *p = __float2half_rn(x); }
 
-// The forward kernels take a line a thread, as those of whole rows do.  Lines are asked for into shared memory of the thread's own:
+// The forward kernel takes a line a thread, as that of whole rows does.  Lines are asked for into shared memory of the thread's own:
 // registers for them would leave room for half as many threads.
 template <typename T>
 __device__ __noinline__ uint4 line_by_value(const T* p, int64_t at, int64_t values) {          // (at a buffer's end)
@@ -800,44 +802,6 @@ struct LineBuffer {
     }
 };
 __device__ __forceinline__ void wait_lines() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
-template <typename T>
-__global__ void __launch_bounds__(kRowNT, 5) k_expert_dispatch_ragged(const T* __restrict__ x_, int ld_x,
-                                                                      const int32_t* n_tokens, int max_tokens, int top_k,
-                                                                      int dim, const int32_t* __restrict__ place, int cap_rows,
-                                                                      T* __restrict__ y_, int ld_y, int lines, uint64_t inverse,
-                                                                      int row_ctas, int E, int pad_units,
-                                                                      const int32_t* __restrict__ counts,
-                                                                      const int32_t* __restrict__ offsets) {
-    constexpr int N = Vec<T>::N, KU = 4;
-    const Rows<T> y{y_, ld_y};
-    if ((int)blockIdx.x >= row_ctas) {
-        zero_pads<T>(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, y, dim);
-        return;
-    }
-    __shared__ uint4 s_lines[KU][2][kRowNT];
-    const LineBuffer<T> x(x_, ld_x, max_tokens, dim);
-    int t, line;
-    Items<1>(lines, inverse).get(0, &t, &line);
-    if (t >= live_choices(n_tokens, max_tokens, 1)) return;
-    const int32_t* at = place + t * top_k;
-    const int64_t x_at = (int64_t)t * ld_x;
-    for (int k0 = 0; k0 < top_k; k0 += KU) {
-        T* to[KU];
-        int e[KU], s[KU];
-#pragma unroll
-        for (int q = 0; q < KU; ++q) {
-            const int row = k0 + q < top_k ? __ldg(&at[k0 + q]) : -1;
-            to[q] = y.at(row);
-            e[q] = (unsigned)row < (unsigned)cap_rows ? line * N - in_line(to[q]) : dim;
-            if (e[q] < dim) s[q] = x.ask(x_at + e[q], &s_lines[q][0][threadIdx.x]);
-        }
-        wait_lines();
-#pragma unroll
-        for (int q = 0; q < KU; ++q)
-            if (e[q] < dim) store_line(to[q], e[q], dim, x.take(s[q], &s_lines[q][0][threadIdx.x], x_at + e[q]));
-    }
-}
 
 template <typename T>
 __global__ void __launch_bounds__(kRowNT, 5) k_expert_combine_ragged(const T* __restrict__ y_, int ld_y, int cap_rows,
@@ -883,16 +847,16 @@ __global__ void __launch_bounds__(kRowNT, 5) k_expert_combine_ragged(const T* __
     store_line(to, e, dim, r);
 }
 
-// The gradients: P threads (a power of two) take a token, so that where a row lies is found out once for all of its lines; the
-// tokens with rows next to a buffer's ends are done value by value.
-// SAME: y's rows lie in their lines as grad_y's do, so that y needs no putting together.
+// The gradients: P threads (a power of two) take `per` choices one after the other -- a token's, or one where there are few tokens --,
+// so that where a row lies is found out once for all of its lines; rows next to a buffer's ends are done value by value.  SAME: y's rows lie in their lines as grad_y's do, so that y needs no putting
+// together.
 template <typename T, bool SAME>
 __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd_ragged(
     const T* __restrict__ go_, int ld_go, const T* __restrict__ y_, int ld_y, int cap_rows, const int32_t* n_tokens,
     int max_tokens, int top_k, int dim, const int32_t* __restrict__ place, const float* __restrict__ weights,
-    T* __restrict__ gy_, int ld_gy, float* __restrict__ grad_w, int P, int row_ctas, int E, int pad_units,
+    T* __restrict__ gy_, int ld_gy, float* __restrict__ grad_w, int P, int per, int row_ctas, int E, int pad_units,
     const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets) {
-    constexpr int N = Vec<T>::N, L = 3;              // lines of a thread on their way
+    constexpr int N = Vec<T>::N, L = SAME ? 3 : 2;   // lines of a thread on their way
     const Rows<T> gy{gy_, ld_gy};
     if ((int)blockIdx.x >= row_ctas) {
         zero_pads<T>(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, gy, dim);
@@ -900,11 +864,11 @@ __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd_ragged(
     }
     __shared__ float s_dot[kRowNT / 32];
     const Buffer<T> go(go_, ld_go, max_tokens, dim), y(grad_w ? y_ : gy_, grad_w ? ld_y : ld_gy, cap_rows, dim);
-    const int sub = threadIdx.x & (P - 1), t = (int)blockIdx.x * (kRowNT / P) + (int)threadIdx.x / P;
+    const int sub = threadIdx.x & (P - 1), first = ((int)blockIdx.x * (kRowNT / P) + (int)threadIdx.x / P) * per, t = first / top_k;
     const bool live = t < live_choices(n_tokens, max_tokens, 1), go_inside = go.inside(t);
-    for (int k = 0; k < top_k; ++k) {
-        const int row = live ? __ldg(&place[t * top_k + k]) : -1;
-        const float w = live && weights ? __ldg(&weights[t * top_k + k]) : 1.f;
+    for (int a = first; a < first + per; ++a) {
+        const int row = live ? __ldg(&place[a]) : -1;
+        const float w = live && weights ? __ldg(&weights[a]) : 1.f;
         float dot[1] = {};
         if ((unsigned)row < (unsigned)cap_rows) {
             T* to = gy.at(row);
@@ -929,17 +893,16 @@ __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd_ragged(
                         g.take(gl[i]).get(x);
                         if (grad_w) {
                             Vec<T> b;
-                            float y[N];
                             if constexpr (SAME) b.raw = vl[i].a;
                             else b = v.take(vl[i]);
-                            b.get(y);
+                            b.get(z);
                             if (e >= 0 && e + N <= dim) {
 #pragma unroll
-                                for (int j = 0; j < N; ++j) dot[0] = fmaf(x[j], y[j], dot[0]);
+                                for (int j = 0; j < N; ++j) dot[0] = fmaf(x[j], z[j], dot[0]);
                             } else {
 #pragma unroll
                                 for (int j = 0; j < N; ++j)
-                                    if ((unsigned)(e + j) < (unsigned)dim) dot[0] = fmaf(x[j], y[j], dot[0]);
+                                    if ((unsigned)(e + j) < (unsigned)dim) dot[0] = fmaf(x[j], z[j], dot[0]);
                             }
                         }
 #pragma unroll
@@ -960,7 +923,7 @@ __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd_ragged(
         }
         if (!grad_w) continue;
         sum_dots(dot, P, s_dot);
-        if (sub == 0 && live) grad_w[t * top_k + k] = dot[0];
+        if (sub == 0 && live) grad_w[a] = dot[0];
     }
 }
 
@@ -982,10 +945,10 @@ struct Matrix {
     const void* p;
     int64_t ld, rows;
 };
-// Whether all of their rows begin at multiples of 16 bytes and have whole ones.
-bool in_lines(int size, int64_t dim, std::initializer_list<Matrix> ms) {
-    bool all = dim * size % 16 == 0;
-    for (const Matrix& m : ms) all = all && reinterpret_cast<uintptr_t>(m.p) % 16 == 0 && m.ld * size % 16 == 0;
+// Whether all of their rows begin at multiples of `bytes` and have whole ones.
+bool in_lines(int bytes, int size, int64_t dim, std::initializer_list<Matrix> ms) {
+    bool all = dim * size % bytes == 0;
+    for (const Matrix& m : ms) all = all && reinterpret_cast<uintptr_t>(m.p) % bytes == 0 && m.ld * size % bytes == 0;
     return all;
 }
 bool matrices_ok(int32_t dtype, int64_t dim, std::initializer_list<Matrix> ms) {
@@ -1003,9 +966,12 @@ int sms() {
         return kSMsFallback;
     return n;
 }
-int pad_units(const hl_route* r) {
+// CTAs per expert for the rows that fill it up: four a multiprocessor in all, or as many as leave each some 128 KB to write where
+// half of those rows are there (1 000 CTAs with 300 KB each ran in two rounds: 122 us instead of 98).
+int pad_units(const hl_route* r, int64_t row_bytes) {
     if (r->align <= 1 || !r->counts || !r->offsets) return 0;
-    const int64_t u = div_up(4 * kSMsFallback, r->n_experts);
+    const int64_t fill = div_up(4 * kSMsFallback, r->n_experts), work = div_up((r->align - 1) * row_bytes, 256 << 10);
+    const int64_t u = fill > work ? fill : work;
     return (int)(u < r->align - 1 ? u : r->align - 1);
 }
 
@@ -1046,12 +1012,12 @@ bool wide_clusters() {
 // Tiles of at most Tile::kChoices choices: as many CTAs as fill whole rounds of the chip.
 int64_t sort_tiles(int64_t n) { return div_up(div_up(n > 0 ? n : 1, Tile::kChoices), kSMsFallback) * kSMsFallback; }
 
-// Threads of a token, a power of two: enough for `each` vectors a thread, few of them without one in the last round, and at most
-// a warp's -- or `most`, for rows that long, where there are few tokens.
-int threads_of(const hl_route* r, int64_t vectors, int each, int most) {
+// Threads of a row, a power of two: enough for `each` vectors a thread, few of them without one in the last round, and at most a
+// warp's -- or `most`, for rows that long, where there are few rows.
+int threads_of(int64_t rows, int64_t vectors, int each, int most) {
     int P = 1;
     while (P < most && P * each < vectors) {
-        const bool few = r->max_tokens * P < (int64_t)kSMsFallback * 1024;
+        const bool few = rows * P < (int64_t)kSMsFallback * 1024;
         const int64_t round = 2 * P * each, idle = div_up(vectors, round) * round - vectors;
         if (!few && (P >= 32 || 4 * idle > vectors)) break;
         P *= 2;
@@ -1059,16 +1025,15 @@ int threads_of(const hl_route* r, int64_t vectors, int each, int most) {
     return P;
 }
 
-template <typename T>
-int32_t launch_dispatch(const hl_route* r, int64_t dim, const void* x, int64_t ld_x, void* y, int64_t ld_y, bool ragged,
-                        cudaStream_t stream) {
-    const int vectors = (int)div_up(dim + (ragged ? Vec<T>::N - 1 : 0), Vec<T>::N), units = pad_units(r);
-    const int64_t ctas = div_up(r->max_tokens * vectors, kRowNT * (ragged ? 1 : kDispatchVectors));
+template <typename T, typename V>
+int32_t launch_dispatch(const hl_route* r, int64_t dim, const void* x, int64_t ld_x, void* y, int64_t ld_y, cudaStream_t stream) {
+    const int vectors = (int)(dim * sizeof(T) / sizeof(V)), units = pad_units(r, dim * sizeof(T));
+    const int64_t ctas = div_up(r->max_tokens * vectors, kRowNT * kDispatchVectors<V>);
     if (ctas + units == 0) return HL_OK;
     if (ctas + (int64_t)units * r->n_experts > 0x7fffffff) return HL_EINVAL;
-    HL_CUDA_TRY(launch(ragged ? k_expert_dispatch_ragged<T> : k_expert_dispatch<T>, ctas + units * r->n_experts, kRowNT, stream,
-                       static_cast<const T*>(x), ld_x, r->n_tokens, r->max_tokens, r->top_k, dim, r->place, r->cap_rows,
-                       static_cast<T*>(y), ld_y, vectors, inverse_of(vectors), ctas, r->n_experts, units, r->counts, r->offsets));
+    HL_CUDA_TRY(launch(k_expert_dispatch<T, V>, ctas + units * r->n_experts, kRowNT, stream, static_cast<const T*>(x), ld_x,
+                       r->n_tokens, r->max_tokens, r->top_k, dim, r->place, r->cap_rows, static_cast<T*>(y), ld_y, vectors,
+                       inverse_of(vectors), ctas, r->n_experts, units, r->counts, r->offsets));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
@@ -1097,17 +1062,27 @@ int32_t launch_combine(const hl_route* r, int64_t dim, const void* y, int64_t ld
 template <typename T>
 int32_t launch_combine_bwd(const hl_route* r, int64_t dim, const void* go, int64_t ld_go, const void* y, int64_t ld_y,
                            const float* w, void* gy, int64_t ld_gy, float* gw, bool ragged, cudaStream_t stream) {
-    const int units = pad_units(r), P = threads_of(r, div_up(dim, Vec<T>::N) + ragged, 1, kRowNT);
-    const int64_t ctas = div_up(r->max_tokens, kRowNT / P);
+    const int units = pad_units(r, dim * sizeof(T));
+    const int64_t vectors = div_up(dim, Vec<T>::N) + ragged;
+    int P = threads_of(r->max_tokens, vectors, ragged ? 3 : 1, kRowNT);
+    // ragged rows of so few tokens that their threads are less than two rounds of the chip: a choice for itself
+    const bool single = ragged && r->top_k > 1 && r->max_tokens * P < (int64_t)2 * kSMsFallback * 4 * kRowNT;
+    if (single) P = threads_of(r->max_tokens * r->top_k, vectors, 3, kRowNT);
+    const int64_t ctas = div_up(r->max_tokens * (single ? r->top_k : 1), kRowNT / P);
     if (ctas + units == 0) return HL_OK;
     if (ctas + (int64_t)units * r->n_experts > 0x7fffffff) return HL_EINVAL;
     const bool same = ld_y == ld_gy && (reinterpret_cast<uintptr_t>(y) - reinterpret_cast<uintptr_t>(gy)) % 16 == 0;
-    HL_CUDA_TRY(launch(!ragged ? k_expert_combine_bwd<T>
-                       : same  ? k_expert_combine_bwd_ragged<T, true>
-                               : k_expert_combine_bwd_ragged<T, false>,
-                       ctas + units * r->n_experts, kRowNT, stream, static_cast<const T*>(go), ld_go, static_cast<const T*>(y),
-                       ld_y, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, dim, r->place, w, static_cast<T*>(gy), ld_gy, gw,
-                       P, ctas, r->n_experts, units, r->counts, r->offsets));
+    const int grid = (int)(ctas + (int64_t)units * r->n_experts);
+    const T *go_t = static_cast<const T*>(go), *y_t = static_cast<const T*>(y);
+    if (ragged)
+        HL_CUDA_TRY(launch(same ? k_expert_combine_bwd_ragged<T, true> : k_expert_combine_bwd_ragged<T, false>, grid, kRowNT, stream,
+                           go_t, ld_go, y_t, ld_y, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, dim, r->place, w,
+                           static_cast<T*>(gy), ld_gy, gw, P, single ? 1 : r->top_k, ctas, r->n_experts, units, r->counts,
+                           r->offsets));
+    else
+        HL_CUDA_TRY(launch(k_expert_combine_bwd<T>, grid, kRowNT, stream, go_t, ld_go, y_t, ld_y, r->cap_rows, r->n_tokens,
+                           r->max_tokens, r->top_k, dim, r->place, w, static_cast<T*>(gy), ld_gy, gw, P, ctas, r->n_experts, units,
+                           r->counts, r->offsets));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
@@ -1174,9 +1149,6 @@ extern "C" int32_t hl_expert_sort(const hl_route* route, const int32_t* d_expert
     return HL_OK;
 }
 
-#define HL_FOR_TYPE(CALL) \
-    return dtype == HL_F32 ? CALL(float) : dtype == HL_BF16 ? CALL(__nv_bfloat16) : CALL(__half)
-
 extern "C" int32_t hl_expert_dispatch(const hl_route* route, int32_t dtype, int64_t dim, const void* d_x, int64_t ld_x,
                                       void* d_y, int64_t ld_y, void* stream_) {
     const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
@@ -1185,11 +1157,17 @@ extern "C" int32_t hl_expert_dispatch(const hl_route* route, int32_t dtype, int6
     const Matrix x{d_x, ld_x, route->max_tokens}, y{d_y, ld_y, route->cap_rows};
     if (!matrices_ok(dtype, dim, {x, y})) return HL_EINVAL;
     if (route->cap_rows == 0) return HL_OK;
-    const bool ragged = !in_lines(size_of(dtype), dim, {x, y});
-#define HL_DISPATCH(T) launch_dispatch<T>(route, dim, d_x, ld_x, d_y, ld_y, ragged, stream)
-    HL_FOR_TYPE(HL_DISPATCH);
+    const int size = size_of(dtype);
+#define HL_DISPATCH(T, V) launch_dispatch<T, V>(route, dim, d_x, ld_x, d_y, ld_y, stream)
+    if (in_lines(16, size, dim, {x, y})) return size == 4 ? HL_DISPATCH(uint32_t, uint4) : HL_DISPATCH(uint16_t, uint4);
+    if (in_lines(8, size, dim, {x, y})) return size == 4 ? HL_DISPATCH(uint32_t, uint2) : HL_DISPATCH(uint16_t, uint2);
+    if (size == 4) return HL_DISPATCH(uint32_t, uint32_t);
+    return in_lines(4, size, dim, {x, y}) ? HL_DISPATCH(uint16_t, uint32_t) : HL_DISPATCH(uint16_t, uint16_t);
 #undef HL_DISPATCH
 }
+
+#define HL_FOR_TYPE(CALL) \
+    return dtype == HL_F32 ? CALL(float) : dtype == HL_BF16 ? CALL(__nv_bfloat16) : CALL(__half)
 
 extern "C" int32_t hl_expert_combine(const hl_route* route, int32_t dtype, int64_t dim, const void* d_y, int64_t ld_y,
                                      const float* d_weights, void* d_out, int64_t ld_out, void* stream_) {
@@ -1198,7 +1176,7 @@ extern "C" int32_t hl_expert_combine(const hl_route* route, int32_t dtype, int64
     const Matrix y{d_y, ld_y, route->cap_rows}, out{d_out, ld_out, route->max_tokens};
     if (!matrices_ok(dtype, dim, {y, out})) return HL_EINVAL;
     if (route->max_tokens == 0) return HL_OK;
-    const bool ragged = !in_lines(size_of(dtype), dim, {y, out});
+    const bool ragged = !in_lines(16, size_of(dtype), dim, {y, out});
 #define HL_COMBINE(T) launch_combine<T>(route, dim, d_y, ld_y, d_weights, d_out, ld_out, ragged, stream)
     HL_FOR_TYPE(HL_COMBINE);
 #undef HL_COMBINE
@@ -1213,7 +1191,7 @@ extern "C" int32_t hl_expert_combine_bwd(const hl_route* route, int32_t dtype, i
     const Matrix go{d_grad_out, ld_grad_out, route->max_tokens}, gy{d_grad_y, ld_grad_y, route->cap_rows};
     const Matrix y{d_grad_weights ? d_y : d_grad_y, d_grad_weights ? ld_y : ld_grad_y, route->cap_rows};   // (else not read)
     if (!matrices_ok(dtype, dim, {go, y, gy})) return HL_EINVAL;
-    const bool ragged = !in_lines(size_of(dtype), dim, {go, y, gy});
+    const bool ragged = !in_lines(16, size_of(dtype), dim, {go, y, gy});
 #define HL_COMBINE_BWD(T)                                                                                                      \
     launch_combine_bwd<T>(route, dim, d_grad_out, ld_grad_out, d_y, ld_y, d_weights, d_grad_y, ld_grad_y, d_grad_weights, ragged, \
                           stream)

@@ -398,8 +398,9 @@ int32_t clip_call(const hl_tensor* ts, int32_t n, const double* further, int32_t
 // those of a run over several windows go through `pieces` to k_rows_long.
 template <int G>
 struct RowShape {
-    static constexpr int kGroups = kNT / G, kRun = G < 16 ? G : 16, kWindow = kGroups * kRun;
-    static_assert(kWindow <= kNT && kGroups <= 64, "a thread asks for a window's lookup; a bit per group");
+    static constexpr int kGroups = kNT / G, kRun = G < 16 ? 8 : 16, kWindow = kGroups * kRun;
+    static constexpr int kAsk = (kWindow + kNT - 1) / kNT;     // lookups of a window that a thread asks for
+    static_assert(kGroups <= 64, "a bit per group");
 };
 
 __device__ __forceinline__ double square(const double (&a)[4]) { return a[0] * a[0] + a[1] * a[1] + a[2] * a[2] + a[3] * a[3]; }
@@ -425,13 +426,18 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
     double total = 0.0;
     if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) starts[max_windows] = 0;      // (k_rows_long's tally)
     // the next window's pairs are on their way while this one's rows are summed; two threads also take the lookups around it
-    constexpr bool kWhole = kWindow == kNT;
-    int32_t slot_ahead = 0, bag_ahead = 0, around_ahead = 0;
+    constexpr int kAsk = Shape::kAsk;
+    int32_t slot_ahead[kAsk] = {}, bag_ahead[kAsk] = {}, around_ahead = 0;
     const auto ask = [&](int64_t w) {
-        const int64_t at = w * kWindow + threadIdx.x, around = threadIdx.x == 0 ? w * kWindow - 1 : (w + 1) * kWindow;
-        if ((kWhole || threadIdx.x < kWindow) && at < n) {
-            slot_ahead = __ldg(&slots[at]);
-            bag_ahead = __ldg(&bags[at]);
+        const int64_t around = threadIdx.x == 0 ? w * kWindow - 1 : (w + 1) * kWindow;
+#pragma unroll
+        for (int i = 0; i < kAsk; ++i) {
+            const int l = threadIdx.x + i * kNT;
+            const int64_t at = w * kWindow + l;
+            if (l < kWindow && at < n) {
+                slot_ahead[i] = __ldg(&slots[at]);
+                bag_ahead[i] = __ldg(&bags[at]);
+            }
         }
         if (threadIdx.x < 2 && around >= 0 && around < n) around_ahead = __ldg(&slots[around]);
     };
@@ -439,10 +445,13 @@ __global__ void __launch_bounds__(kNT, G < 32 ? 3 : 2) k_rows_squares(const int3
     for (int64_t w = blockIdx.x; w < windows; w += gridDim.x) {
         const int64_t begin = w * kWindow;
         const int here = (int)min((int64_t)kWindow, n - begin);    // lookups of the window
-        if (kWhole || threadIdx.x < kWindow) {
-            s_slot[1 + threadIdx.x] = slot_ahead;
-            const bool adds = (int)threadIdx.x < here && bag_ahead >= 0 && bag_ahead < n_bags && slot_ahead >= 0 && slot_ahead < n_slots;
-            s_bag[threadIdx.x] = adds ? bag_ahead : -1;
+#pragma unroll
+        for (int i = 0; i < kAsk; ++i) {
+            const int l = threadIdx.x + i * kNT;
+            if (l >= kWindow) break;
+            const int32_t slot = slot_ahead[i], bag = bag_ahead[i];
+            s_slot[1 + l] = slot;
+            s_bag[l] = l < here && bag >= 0 && bag < n_bags && slot >= 0 && slot < n_slots ? bag : -1;
         }
         if (threadIdx.x < 2) s_slot[threadIdx.x ? kWindow + 1 : 0] = around_ahead;
         if (threadIdx.x <= kGroups / 32) s_whole[threadIdx.x] = 0;
