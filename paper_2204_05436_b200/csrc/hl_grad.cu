@@ -149,9 +149,9 @@ __device__ __forceinline__ void tile_scale(const S* p, D* d, int n, float f) {
             for (int j = 0; j < W; ++j) x[j] *= f;
             D* to = d + head + (int64_t)(i + u * kNT) * W;
             if constexpr (kOut == 2)
-                *reinterpret_cast<uint2*>(to) = make_uint2(pack<D>(x), pack<D>(x + kPerOut));
+                __stcs(reinterpret_cast<uint2*>(to), make_uint2(pack<D>(x), pack<D>(x + kPerOut)));
             else
-                *reinterpret_cast<uint4*>(to) = make_uint4(pack<D>(x), pack<D>(x + kPerOut), pack<D>(x + 2 * kPerOut), pack<D>(x + 3 * kPerOut));
+                __stcs(reinterpret_cast<uint4*>(to), make_uint4(pack<D>(x), pack<D>(x + kPerOut), pack<D>(x + 2 * kPerOut), pack<D>(x + 3 * kPerOut)));
         }
     }
     for (int i = threadIdx.x; i < head + n - tail; i += kNT) {
