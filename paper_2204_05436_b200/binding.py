@@ -726,15 +726,16 @@ def make_route(max_tokens: int, n_tokens, top_k: int, n_experts: int, align: int
 
 def make_tensors(pairs):
     """The list that hl_grad_norm and hl_grad_clip take, from (src, dst) or (src, dst, flags) of contiguous torch tensors;
-    dst may be None, or src itself (in place); none is written twice.  It keeps their addresses, not the tensors."""
+    dst may be None, or src itself (in place); none is written twice, and all are on one device.  It keeps their addresses, not
+    the tensors."""
     arr = (hl_tensor * len(pairs))()
     written = set()
     for i, pair in enumerate(pairs):
         src, dst, flags = pair if len(pair) == 3 else (*pair, 0)
         if not src.is_contiguous() or (dst is not None and (not dst.is_contiguous() or dst.numel() != src.numel())):
             raise ValueError("gradient tensors are contiguous, and dst has as many values as src")
-        if dst is not None and dst.device != src.device:
-            raise ValueError("src and dst are on one device")
+        if src.device != pairs[0][0].device or (dst is not None and dst.device != src.device):
+            raise ValueError("the tensors are on one device")
         if dst is not None and dst.numel() > 0:
             if _ptr(dst) in written:
                 raise ValueError("a tensor is written twice")

@@ -30,6 +30,7 @@ class Hotline:
         self.max_batch, self.max_nnz = int(max_batch), int(max_nnz)
         self.hot_cap, self.staging_cap = int(hot_cap_rows), int(staging_cap_rows)
         self.max_bags = self.T * self.max_batch * self.S
+        self.bags = 0                            # of the mini-batch that fragment() was last called with
         self.n_dense = int(n_dense)
         # host_table: fp32 [N, D], or a list of one fp32 [rows_t, D] tensor per table (a table too large for one
         # allocation).  It must be memory the device can address: from hl_host_alloc (binding.host_table_tensor),
@@ -160,6 +161,7 @@ class Hotline:
         B.hl_fragment(self.ctx, self._batch(indices, offsets, batch), dense, self.n_dense if dense is not None else 0,
                       self.perm, self.counts, self.pop, self.non, self.dense_out if dense is not None else None,
                       self.main.cuda_stream)
+        self.bags = self.T * batch * self.S
 
     def gather_cold(self, stream: Optional[torch.cuda.Stream] = None) -> None:
         s = stream or self.main
@@ -183,21 +185,25 @@ class Hotline:
         tables' row gradients, in which the lookups of a row are added up first, together with ``others``, the dense model's
         gradients ((tensor, tensor) in place, or (src, dst) pairs; see binding.make_tensors).  ``grad_all``: the gradients of O's
         bags, then X's (X's block begins at row tables * n_pop * steps), scaled in place, as ``others`` are.  Call it when X's
-        slots are known (gather_cold) and both forwards are queued.  Returns the norm (fp32 [1], final in the main stream's
-        order; the next call overwrites it)."""
+        slots are known (gather_cold) and both forwards are queued; all of it is in the main stream's order.  Returns the norm
+        (fp32 [1]; the next call overwrites it)."""
+        if not self.bags:
+            raise ValueError("no mini-batch: fragment() comes first")
         if grad_all.dtype != torch.float32 or grad_all.dim() != 2 or grad_all.shape[1] != self.D or not grad_all.is_contiguous() \
-                or grad_all.shape[0] > self.max_bags or grad_all.device.type != "cuda":
-            raise ValueError(f"grad_all is a contiguous fp32 [bags, {self.D}] tensor on the device, of at most {self.max_bags} bags")
+                or not self.bags <= grad_all.shape[0] <= self.max_bags or grad_all.device != self.cache.device:
+            raise ValueError(f"grad_all is a contiguous fp32 [bags, {self.D}] tensor on {self.cache.device}, of {self.bags} to "
+                             f"{self.max_bags} bags")
+        tensors = B.make_tensors([(grad_all, grad_all, B.HL_TENSOR_NOT_IN_NORM), *others])
         if not hasattr(self, "clip_sorted"):
-            i32 = dict(dtype=torch.int32, device=self.device)
-            self.clip_sorted = (torch.zeros(max(1, self.max_nnz), **i32), torch.zeros(max(1, self.max_nnz), **i32),
-                                torch.zeros(4, **i32))
-            self.clip_sumsq = torch.zeros(1, dtype=torch.float64, device=self.device)
-            self.clip_norm = torch.zeros(1, dtype=torch.float32, device=self.device)
-            self.clip_ws = torch.empty(B.hl_grad_workspace_bytes(), dtype=torch.uint8, device=self.device)
+            with torch.cuda.stream(self.main):
+                i32 = dict(dtype=torch.int32, device=self.device)
+                self.clip_sorted = (torch.zeros(max(1, self.max_nnz), **i32), torch.zeros(max(1, self.max_nnz), **i32),
+                                    torch.zeros(4, **i32))
+                self.clip_sumsq = torch.zeros(1, dtype=torch.float64, device=self.device)
+                self.clip_norm = torch.zeros(1, dtype=torch.float32, device=self.device)
+                self.clip_ws = torch.empty(B.hl_grad_workspace_bytes(), dtype=torch.uint8, device=self.device)
         s = self.main.cuda_stream
         slots, bags, n = self.clip_sorted
-        tensors = B.make_tensors([(grad_all, grad_all, B.HL_TENSOR_NOT_IN_NORM), *others])
         B.hl_embbag_bwd_prepare_merged(self.ctx, self.pop, self.counts, self.non, self.counts_non, slots, bags, n, s)
         B.hl_embbag_grad_sumsq(self.ctx, slots, bags, n[2:], grad_all, self.clip_sumsq, s)
         B.hl_grad_clip(tensors, self.clip_sumsq, 1, max_norm, self.clip_norm, self.clip_ws, self.clip_ws.numel(), s)

@@ -149,6 +149,33 @@ def test_clipping_counts_a_row_once(hl):
             h.update_clipped(grad, 1.0, -1.0)
 
 
+def test_clipping_needs_a_mini_batch_and_all_of_its_gradients(hl):
+    B, D = 50, 16
+    h = hl.Hotline([4], D, 1, B, B, 4, 4, torch.zeros(4, D).pin_memory())
+    grad, dense = torch.ones(B, D, device="cuda"), torch.ones(7, device="cuda")
+    torch.cuda.synchronize()
+    with h:
+        h.set_hot_rows(torch.arange(4).cuda())
+        h.build_remap()
+        with pytest.raises(ValueError):
+            h.update_clipped(grad, 1.0, 1.0)
+        idx, off = torch.full((B,), 2, dtype=torch.int32, device="cuda"), torch.arange(B + 1, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+        h.fragment(idx, off, B)
+        h.gather_cold()
+        for bad, others in [(grad[1:], ()), (grad, [(dense.cpu(), dense.cpu())]), (grad, [(dense, dense), (dense, dense)])]:
+            with pytest.raises(ValueError):
+                h.update_clipped(bad, 1.0, 1.0, others)
+        # (called beside another stream than the main one, which the first call's buffers are not to be filled on)
+        torch.cuda._sleep(20_000_000)
+        norm = h.update_clipped(grad, 1.0, 1.0)
+        h.main.synchronize()
+        e = B * D ** 0.5
+        assert abs(norm.item() - e) <= 1e-6 * e
+        torch.cuda.synchronize()
+        assert abs(norm.item() - e) <= 1e-6 * e
+
+
 def test_what_a_route_refuses(hl):
     for bad in (dict(top_k=0), dict(top_k=65), dict(n_experts=0), dict(n_experts=1025), dict(align=0), dict(max_tokens=-1),
                 dict(max_tokens=2 ** 30), dict(cap_rows=-1)):
