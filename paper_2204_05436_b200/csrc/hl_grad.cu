@@ -24,7 +24,12 @@ __device__ __forceinline__ double block_sum(double v) {        // the same in ev
 }
 
 // ---- many tensors ---------------------------------------------------------------------------------------------------
-// A call's tensors are cut into tiles of 2^tile_bits values, and every CTA takes a run of tiles.
+// A call's tensors are cut into tiles of 2^tile_bits values, and every CTA takes a run of tiles: two kernels, of which the second
+// needs the first's sums, so that tensors beyond the L2's size are read twice.  420 tensors, 153 M values, bf16 scaled into fp32:
+// squares 306 MB in 58 us (5.3 TB/s), scaling 919 MB in 165 us (5.6 TB/s, some of it from the L2); 14 tensors of 0.2 M fp32 in all:
+// 6.9 us a call, two launches.  One cluster of 16 CTAs for both, for few values, took 8.2 to 12.3 instead of 6.8 to 8.4: a CTA's
+// tiles one after the other.  Squares are exact in fp64; the sums' order is the same in every call.  Tried: fp64 made from the bits by shifts instead of
+// conversions 67 us, eight loads ahead 94 (half as many CTAs fit).
 constexpr int kMinTileBits = 10, kMaxTileBits = 13;
 constexpr int kGradCtas = 8;                         // CTAs per multiprocessor
 constexpr int kMaxPartials = 2048;                   // sums of squares, one per CTA
@@ -116,7 +121,8 @@ __device__ __forceinline__ double tile_squares(const T* __restrict__ p, int n) {
     return sum;
 }
 
-// As many values at a time as are 16 bytes in the wider type, so that a warp's stores are whole lines.  (p and d may be the same.)
+// As many values at a time as are 16 bytes in the wider type, so that a warp's stores are whole lines, which the L2 gives up first:
+// what the sums of squares read last stays in it (165 us instead of 177).  (p and d may be the same.)
 template <typename S, typename D>
 __device__ __forceinline__ void tile_scale(const S* p, D* d, int n, float f) {
     constexpr int W = sizeof(S) > sizeof(D) ? kWide<S> : kWide<D>, kIn = W * sizeof(S) / 4, kOut = W * sizeof(D) / 4;   // words
@@ -395,7 +401,10 @@ int32_t clip_call(const hl_tensor* ts, int32_t n, const double* further, int32_t
 // Sum over the distinct slots u of |sum over the lookups j of u of grad[bag(j)]|^2, from the (slot, bag) pairs sorted by slot.
 // A CTA takes windows of consecutive lookups, each of its groups of G lanes a few of them and 4 * G columns; blockIdx.y: which
 // columns.  A group sums its lookups run by run in fp64; the pieces of a run over several groups meet in shared memory, and
-// those of a run over several windows go through `pieces` to k_rows_long.
+// those of a run over several windows go through `pieces` to k_rows_long.  Bound by the latency of rows read in the slots' order:
+// 426 K lookups of 64 fp32, 109 MB in 26.8 us (4.1 TB/s) and 10 for the long runs, a chain of five dependent loads; 129 K of 16
+// fp32: 8 and 8.5.  Windows of a CTA by itself took 62 instead of 44, four CTAs a multiprocessor 26.2, five with half the rows on
+// their way 27.2.
 template <int G>
 struct RowShape {
     static constexpr int kGroups = kNT / G, kRun = G < 16 ? 8 : 16, kWindow = kGroups * kRun;
@@ -710,7 +719,8 @@ extern "C" int32_t hl_grad_clip(const hl_tensor* tensors, int32_t n_tensors, con
 extern "C" int32_t hl_embbag_grad_sumsq(hl_ctx* ctx, const int32_t* d_sorted_slots, const int32_t* d_sorted_bags,
                                         const int32_t* d_n_lookups, const float* d_grad_out, double* d_sumsq, void* stream_) {
     const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if (!ctx || !d_n_lookups || !d_sumsq || (reinterpret_cast<uintptr_t>(d_sumsq) & 7) || (ctx->max_nnz > 0 && (!d_sorted_slots || !d_sorted_bags || !d_grad_out)))
+    if (!ctx || !d_n_lookups || !d_sumsq || (reinterpret_cast<uintptr_t>(d_sumsq) & 7) ||
+        (ctx->max_nnz > 0 && (!d_sorted_slots || !d_sorted_bags || !d_grad_out)))
         return HL_EINVAL;
     const int D4 = ctx->D / 4;
     if (D4 > 256 || (reinterpret_cast<uintptr_t>(d_grad_out) & 15)) return HL_EINVAL;

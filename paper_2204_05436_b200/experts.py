@@ -1,7 +1,9 @@
 """A mixture of experts' routing: buffers and calls around hl_expert_* (plumbing only: torch for memory and streams).
 
 :class:`ExpertRoute` keeps the plan that one router's choices make -- where every token's rows lie among the experts' -- and issues
-the copies there, the weighted sums back and their gradients, on torch's current stream.  No arithmetic happens here.
+the copies there, the weighted sums back and their gradients, on torch's current stream.  No arithmetic happens here.  A route's
+plan and workspace are its own: its calls belong in the order of one stream, and two streams (or two graphs replayed side by side)
+need a route each.
 
     route = ExpertRoute(max_tokens, top_k, n_experts, align=128)
     route.sort(experts)                              # int32 [tokens, top_k], -1: no expert; tokens <= max_tokens
