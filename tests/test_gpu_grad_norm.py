@@ -123,6 +123,32 @@ def test_mixed_tensors_further_sums_and_flags(hl):
     assert torch.equal(db, b.float())
 
 
+@pytest.mark.parametrize("which", ["all", "one not in the norm", "one not written", "one empty"])
+@pytest.mark.parametrize("n", [32, 33, 128, 129, 256, 257, 512, 513, 1000, 1001, 2003])
+def test_as_many_tensors_as_a_list_holds_and_one_more(hl, n, which):
+    """(One launch takes 32, 128, 256, 512 or 1 000 of them; norm and scaling share a list where all tensors count in both.)"""
+    sizes = [1 + (i * 37) % 300 for i in range(n)]
+    odd = n // 2
+    if which == "one empty":
+        sizes[odd] = 0
+    src = [_values(m, torch.float32, i) for i, m in enumerate(sizes)]
+    dst = [torch.full((m,), 7.0, device="cuda") for m in sizes]
+    pairs = [(s, d) for s, d in zip(src, dst)]
+    squares = _squares(src)
+    if which == "one not in the norm":
+        pairs[odd] = (src[odd], dst[odd], hl.HL_TENSOR_NOT_IN_NORM)
+        squares = _squares(src[:odd] + src[odd + 1:])
+    if which == "one not written":
+        pairs[odd] = (src[odd], None)
+    norm = math.sqrt(squares)
+    assert abs(_clip(hl, pairs, 0.5 * norm) - norm) <= 1.01 * S * norm
+    f = _factor(norm, 0.5 * norm)
+    if which == "one not written":
+        assert (dst[odd] == 7).all()
+        del src[odd], dst[odd]
+    _check_scaled(torch.cat(dst), torch.cat(src), f)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_the_range_of_the_types(hl, dtype):
     """Squares beyond fp32's range on either side."""
