@@ -766,9 +766,6 @@ struct Ragged {
     }
 };
 
-template <typename T>
-__device__ __forceinline__ int lines_of(int shift, int dim) { return (shift + dim + Vec<T>::N - 1) / Vec<T>::N; }
-
 __device__ __forceinline__ float value_of(const float* p) { return *p; }
 __device__ __forceinline__ float value_of(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ float value_of(const __half* p) { return __half2float(*p); }
@@ -858,17 +855,18 @@ __global__ void __launch_bounds__(kRowNT, 5) k_expert_combine_ragged(const T* __
     store_line(to, e, dim, r);
 }
 
-// The gradients: P threads (a power of two) take `per` choices one after the other -- a token's, or one where there are few tokens
-// (339 tokens of 8 rows of 176 bf16: 12.8 us a call instead of 19.5) --, so that where a row lies is found out once for all of its
-// lines; rows next to a buffer's ends are done value by value.  SAME: y's rows lie in their lines as grad_y's do, so that y needs no
-// putting together.
+// The gradients: P threads (a power of two) take a choice, so that where its rows lie is found out once for all of their lines: the
+// whole lines of grad_y's row, and the values before and behind them, a thread each.  (A token's choices one after the other, which
+// need no second load of grad_out's row from the caches, took 40 us where this takes 34: a chain of place, rows, stores for each.  32
+// threads a row instead of 8: 42.)  Rows next to a buffer's ends are done value by value.  SAME: y's rows lie in their lines as grad_y's
+// do, so that y needs no putting together.
 template <typename T, bool SAME>
 __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd_ragged(
     const T* __restrict__ go_, int ld_go, const T* __restrict__ y_, int ld_y, int cap_rows, const int32_t* n_tokens,
     int max_tokens, int top_k, int dim, const int32_t* __restrict__ place, const float* __restrict__ weights,
-    T* __restrict__ gy_, int ld_gy, float* __restrict__ grad_w, int P, int per, int row_ctas, int E, int pad_units,
+    T* __restrict__ gy_, int ld_gy, float* __restrict__ grad_w, int P, int row_ctas, int E, int pad_units,
     const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets) {
-    constexpr int N = Vec<T>::N, L = SAME ? 3 : 2;   // lines of a thread on their way
+    constexpr int N = Vec<T>::N, L = 2;              // lines of a thread on their way
     const Rows<T> gy{gy_, ld_gy};
     if ((int)blockIdx.x >= row_ctas) {
         zero_pads<T>(blockIdx.x - row_ctas, pad_units, E, counts, offsets, cap_rows, gy, dim);
@@ -876,67 +874,76 @@ __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd_ragged(
     }
     __shared__ float s_dot[kRowNT / 32];
     const Buffer<T> go(go_, ld_go, max_tokens, dim), y(grad_w ? y_ : gy_, grad_w ? ld_y : ld_gy, cap_rows, dim);
-    const int sub = threadIdx.x & (P - 1), first = ((int)blockIdx.x * (kRowNT / P) + (int)threadIdx.x / P) * per, t = first / top_k;
-    const bool live = t < live_choices(n_tokens, max_tokens, 1), go_inside = go.inside(t);
-    for (int a = first; a < first + per; ++a) {
-        const int row = live ? __ldg(&place[a]) : -1;
-        const float w = live && weights ? __ldg(&weights[a]) : 1.f;
-        float dot[1] = {};
-        if ((unsigned)row < (unsigned)cap_rows) {
-            T* to = gy.at(row);
-            if (go_inside && y.inside(row)) {
-                const int shift = in_line(to), lines = lines_of<T>(shift, dim);
-                const Ragged<T> g(go, t, shift), v(y, row, shift);
-                for (int l0 = sub; l0 < lines; l0 += P * L) {
-                    Lines gl[L], vl[L];
+    const int sub = threadIdx.x & (P - 1), a = (int)((int64_t)blockIdx.x * (kRowNT / P)) + (int)threadIdx.x / P, t = a / top_k;
+    const bool live = t < live_choices(n_tokens, max_tokens, 1);
+    const int row = live ? __ldg(&place[a]) : -1;
+    const float w = live && weights ? __ldg(&weights[a]) : 1.f;
+    float dot[1] = {};
+    if ((unsigned)row < (unsigned)cap_rows) {
+        T* to = gy.at(row);
+        if (go.inside(t) && y.inside(row)) {
+            // whole lines of grad_y's row; then the values before and behind them, a thread each
+            const int in = in_line(to), head = min(in ? N - in : 0, dim), lines = (dim - head) / N;
+            const int tail = head + lines * N, edges = head + dim - tail;
+            const T *x_row = go.p + (int64_t)t * ld_go, *y_row = y.p + (int64_t)row * y.ld;
+            const auto edge = [&](int i) { return i < head ? i : tail + i - head; };
+            float edge_x = 0.f, edge_y = 0.f;
+            if (sub < edges) {
+                edge_x = value_of(x_row + edge(sub));
+                if (grad_w) edge_y = value_of(y_row + edge(sub));
+            }
+            const Ragged<T> g(go, t, -head), v(y, row, -head);
+            T* first_line = to + head;
+            for (int l0 = sub; l0 < lines; l0 += P * L) {
+                Lines gl[L], vl[L];
 #pragma unroll
-                    for (int i = 0; i < L; ++i) {
-                        if (l0 + i * P >= lines) break;
-                        gl[i] = g.ask(l0 + i * P);
-                        if (!grad_w) continue;
-                        if constexpr (SAME) vl[i].a = __ldg(v.line + l0 + i * P);
-                        else vl[i] = v.ask(l0 + i * P);
-                    }
-#pragma unroll
-                    for (int i = 0; i < L; ++i) {
-                        if (l0 + i * P >= lines) break;
-                        const int e = (l0 + i * P) * N - shift;
-                        float x[N], z[N];
-                        g.take(gl[i]).get(x);
-                        if (grad_w) {
-                            Vec<T> b;
-                            if constexpr (SAME) b.raw = vl[i].a;
-                            else b = v.take(vl[i]);
-                            b.get(z);
-                            if (e >= 0 && e + N <= dim) {
-#pragma unroll
-                                for (int j = 0; j < N; ++j) dot[0] = fmaf(x[j], z[j], dot[0]);
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < N; ++j)
-                                    if ((unsigned)(e + j) < (unsigned)dim) dot[0] = fmaf(x[j], z[j], dot[0]);
-                            }
-                        }
-#pragma unroll
-                        for (int j = 0; j < N; ++j) z[j] = w * x[j];
-                        Vec<T> r;
-                        r.set(z);
-                        store_line(to, e, dim, r);
-                    }
+                for (int i = 0; i < L; ++i) {
+                    if (l0 + i * P >= lines) break;
+                    gl[i] = g.ask(l0 + i * P);
+                    if (!grad_w) continue;
+                    if constexpr (SAME) vl[i].a = __ldg(v.line + l0 + i * P);
+                    else vl[i] = v.ask(l0 + i * P);
                 }
-            } else {
-#pragma unroll 1
-                for (int c = sub; c < dim; c += P) {
-                    const float x = value_of(go.p + (int64_t)t * ld_go + c);
-                    if (grad_w) dot[0] = fmaf(x, value_of(y.p + (int64_t)row * ld_y + c), dot[0]);
-                    put_value(to + c, w * x);
+#pragma unroll
+                for (int i = 0; i < L; ++i) {
+                    if (l0 + i * P >= lines) break;
+                    float x[N], z[N];
+                    g.take(gl[i]).get(x);
+                    if (grad_w) {
+                        Vec<T> b;
+                        if constexpr (SAME) b.raw = vl[i].a;
+                        else b = v.take(vl[i]);
+                        b.get(z);
+#pragma unroll
+                        for (int j = 0; j < N; ++j) dot[0] = fmaf(x[j], z[j], dot[0]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < N; ++j) z[j] = w * x[j];
+                    Vec<T> r;
+                    r.set(z);
+                    r.store(first_line + (l0 + i * P) * N);
                 }
             }
+            for (int i = sub; i < edges; i += P) {
+                if (i != sub) {
+                    edge_x = value_of(x_row + edge(i));
+                    if (grad_w) edge_y = value_of(y_row + edge(i));
+                }
+                dot[0] = fmaf(edge_x, edge_y, dot[0]);
+                put_value(to + edge(i), w * edge_x);
+            }
+        } else {
+#pragma unroll 1
+            for (int c = sub; c < dim; c += P) {
+                const float x = value_of(go.p + (int64_t)t * ld_go + c);
+                if (grad_w) dot[0] = fmaf(x, value_of(y.p + (int64_t)row * ld_y + c), dot[0]);
+                put_value(to + c, w * x);
+            }
         }
-        if (!grad_w) continue;
-        sum_dots(dot, P, s_dot);
-        if (sub == 0 && live) grad_w[a] = dot[0];
     }
+    if (!grad_w) return;
+    sum_dots(dot, P, s_dot);
+    if (sub == 0 && live) grad_w[a] = dot[0];
 }
 
 // ---- arguments ------------------------------------------------------------------------------------------------------
@@ -1076,12 +1083,10 @@ template <typename T>
 int32_t launch_combine_bwd(const hl_route* r, int64_t dim, const void* go, int64_t ld_go, const void* y, int64_t ld_y,
                            const float* w, void* gy, int64_t ld_gy, float* gw, bool ragged, cudaStream_t stream) {
     const int units = pad_units(r, dim * sizeof(T));
-    const int64_t vectors = div_up(dim, Vec<T>::N) + ragged;
-    int P = threads_of(r->max_tokens, vectors, ragged ? 3 : 1, kRowNT);
-    // ragged rows of so few tokens that their threads are less than two rounds of the chip: a choice for itself
-    const bool single = ragged && r->top_k > 1 && r->max_tokens * P < (int64_t)2 * kSMsFallback * 4 * kRowNT;
-    if (single) P = threads_of(r->max_tokens * r->top_k, vectors, 3, kRowNT);
-    const int64_t ctas = div_up(r->max_tokens * (single ? r->top_k : 1), kRowNT / P);
+    const int64_t vectors = ragged ? dim / Vec<T>::N : div_up(dim, Vec<T>::N);
+    const int64_t each = r->max_tokens * (ragged ? r->top_k : 1);        // tokens, or choices
+    const int P = threads_of(each, vectors, ragged ? 2 : 1, kRowNT);
+    const int64_t ctas = div_up(each, kRowNT / P);
     if (ctas + units == 0) return HL_OK;
     if (ctas + (int64_t)units * r->n_experts > 0x7fffffff) return HL_EINVAL;
     const bool same = ld_y == ld_gy && (reinterpret_cast<uintptr_t>(y) - reinterpret_cast<uintptr_t>(gy)) % 16 == 0;
@@ -1090,8 +1095,7 @@ int32_t launch_combine_bwd(const hl_route* r, int64_t dim, const void* go, int64
     if (ragged)
         HL_CUDA_TRY(launch(same ? k_expert_combine_bwd_ragged<T, true> : k_expert_combine_bwd_ragged<T, false>, grid, kRowNT, stream,
                            go_t, ld_go, y_t, ld_y, r->cap_rows, r->n_tokens, r->max_tokens, r->top_k, dim, r->place, w,
-                           static_cast<T*>(gy), ld_gy, gw, P, single ? 1 : r->top_k, ctas, r->n_experts, units, r->counts,
-                           r->offsets));
+                           static_cast<T*>(gy), ld_gy, gw, P, ctas, r->n_experts, units, r->counts, r->offsets));
     else
         HL_CUDA_TRY(launch(k_expert_combine_bwd<T>, grid, kRowNT, stream, go_t, ld_go, y_t, ld_y, r->cap_rows, r->n_tokens,
                            r->max_tokens, r->top_k, dim, r->place, w, static_cast<T*>(gy), ld_gy, gw, P, ctas, r->n_experts, units,
