@@ -1032,14 +1032,16 @@ bool wide_clusters() {
 // Tiles of at most Tile::kChoices choices: as many CTAs as fill whole rounds of the chip.
 int64_t sort_tiles(int64_t n) { return div_up(div_up(n > 0 ? n : 1, Tile::kChoices), kSMsFallback) * kSMsFallback; }
 
-// Threads of a row, a power of two: enough for `each` vectors a thread, few of them without one in the last round, and at most a
-// warp's -- or `most`, for rows that long, where there are few rows.
+// Threads of a row, a power of two: enough for `each` vectors a thread, few of them without one in the last round, and at most `most`.
+// More than a warp's only where there are few rows, or for rows of which each still has seven vectors (gradients of 4 000 choices of
+// 16 383 fp32 with 256 threads a row 141 us, with 32 226; of 12 000 of 8 192 bf16 80 and 88; but of 131 072 of 2 050 bf16, two vectors
+// each with 128 threads, 418 instead of 272).
 int threads_of(int64_t rows, int64_t vectors, int each, int most) {
     int P = 1;
     while (P < most && P * each < vectors) {
         const bool few = rows * P < (int64_t)kSMsFallback * 1024;
         const int64_t round = 2 * P * each, idle = div_up(vectors, round) * round - vectors;
-        if (!few && (P >= 32 || 4 * idle > vectors)) break;
+        if (!few && ((P >= 32 && vectors < 14 * P) || 4 * idle > vectors)) break;
         P *= 2;
     }
     return P;
