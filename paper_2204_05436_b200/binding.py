@@ -6,6 +6,7 @@ this module fails and says how to build it.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -726,10 +727,10 @@ def make_route(max_tokens: int, n_tokens, top_k: int, n_experts: int, align: int
 
 def make_tensors(pairs):
     """The list that hl_grad_norm and hl_grad_clip take, from (src, dst) or (src, dst, flags) of contiguous torch tensors;
-    dst may be None, or src itself (in place); none is written twice, and all are on one device.  It keeps their addresses, not
-    the tensors."""
+    dst may be None, or src itself (in place); none is written twice or as another's src, and all are on one device.  It keeps
+    their addresses, not the tensors."""
     arr = (hl_tensor * len(pairs))()
-    written = set()
+    written, read = set(), collections.Counter(_ptr(pair[0]) for pair in pairs if pair[0].numel() > 0)
     for i, pair in enumerate(pairs):
         src, dst, flags = pair if len(pair) == 3 else (*pair, 0)
         if not src.is_contiguous() or (dst is not None and (not dst.is_contiguous() or dst.numel() != src.numel())):
@@ -739,6 +740,8 @@ def make_tensors(pairs):
         if dst is not None and dst.numel() > 0:
             if _ptr(dst) in written:
                 raise ValueError("a tensor is written twice")
+            if read[_ptr(dst)] > (_ptr(dst) == _ptr(src)):
+                raise ValueError("a tensor that is written is read as another's source")
             written.add(_ptr(dst))
         arr[i] = hl_tensor(_ptr(src), _ptr(dst), src.numel(), dtype_of(src), dtype_of(src if dst is None else dst),
                            int(flags), 0)

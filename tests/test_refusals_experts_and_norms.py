@@ -106,6 +106,11 @@ def test_lists_from_tensors(hl):
                                                                                   (24, 1, 1, 1, True)]
     with pytest.raises(ValueError):
         hl.make_tensors([(a, b), (a.half(), b)])
+    d = torch.zeros(6, 4)
+    for bad in ([(a, d), (d, None)], [(d, None), (a, d)], [(a, a), (a, d)], [(a, d), (a, a)], [(a, a), (a, None)]):
+        with pytest.raises(ValueError):
+            hl.make_tensors(bad)
+    hl.make_tensors([(a, d), (a, None), (a, torch.zeros(6, 4))])
     hl.make_tensors([(a, None), (a, None), (torch.zeros(0), torch.zeros(0)), (torch.zeros(0), torch.zeros(0))])
     for bad, error in [((a.t(), None), ValueError), ((a, torch.zeros(23)), ValueError), ((a, b[::2]), ValueError),
                        ((a.double(), None), TypeError), ((a, torch.zeros(24, dtype=torch.int32)), TypeError)]:
