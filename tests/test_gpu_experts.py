@@ -293,6 +293,25 @@ def test_rows_that_begin_anywhere(hl, dtype, shift):
     assert ((gy[:end, :D].double() - e).abs() <= (S + _u(dtype) * (1 + S)) * e.abs() + _tiny(dtype)).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,ld,ld_y", [(1, 1, 1), (3, 4, 5), (7, 9, 9), (8, 11, 9), (9, 9, 10), (23, 25, 25), (41, 43, 41)])
+def test_gradients_of_many_short_rows_that_begin_anywhere(hl, D, ld, ld_y, dtype):
+    """Rows of less than a line to a few, a thread or a few of them each: values before and behind the whole lines, y alike or not."""
+    T, K, E = 60_001, 3, 16
+    p, place, live, end = _case(hl, (T, K, E, D, 0, 4, 60_000, 0.1))
+    ty = hl.dtype_of(torch.empty(0, dtype=dtype))
+    y, go, gy = _rows(p.rows, D, dtype, ld_y - D, 1), _rows(T, D, dtype, ld - D, 2), _filled(p.rows, D, dtype, ld - D)
+    w, gw = torch.rand(T, K, device="cuda"), torch.full((T, K), 5.0, device="cuda")
+    hl.hl_expert_combine_bwd(p.route, ty, D, go, ld, y, ld_y, w, gy, ld, gw, _stream())
+    e = _rows_expected(go, place, w[:live], end)
+    assert ((gy[:end, :D].double() - e).abs() <= (S + _u(dtype) * (1 + S)) * e.abs() + _tiny(dtype)).all()
+    assert (gy[end:] == 5).all() and (gy[:, D:] == 5).all()
+    y0 = torch.where((place >= 0).unsqueeze(2), y[place.clamp(min=0)].double(), 0.0)
+    prod = go[:live].double().unsqueeze(1) * y0
+    assert ((gw[:live].double() - prod.sum(2)).abs() <= (D + 8) * S * prod.abs().sum(2)).all()
+    assert (gw[live:] == 5).all()
+
+
 @pytest.mark.parametrize("T", [600, 60_000])
 def test_a_captured_run_replayed_with_other_choices(hl, T):
     """Sort, there, back and the gradients as one graph, beside eager calls with another workspace."""
