@@ -157,7 +157,7 @@ class ExpertRoute:
             if grad_weights is not None:
                 raise ValueError("the gradient of the weights needs y")
         elif grad_weights is None:
-            grad_weights = torch.zeros(self.tokens, self.top_k, device=grad_out.device)
+            grad_weights = torch.zeros(self.tokens, self.top_k, dtype=torch.float32, device=grad_out.device)
         else:
             self._tensor("grad_weights", grad_weights, (self.tokens, self.top_k), torch.float32)
         self._call(B.hl_expert_combine_bwd, self._route, B.dtype_of(grad_out), grad_out.shape[1], grad_out, ld_go, y, ld_y, weights,
