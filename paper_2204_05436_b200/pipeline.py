@@ -30,7 +30,7 @@ class Hotline:
         self.max_batch, self.max_nnz = int(max_batch), int(max_nnz)
         self.hot_cap, self.staging_cap = int(hot_cap_rows), int(staging_cap_rows)
         self.max_bags = self.T * self.max_batch * self.S
-        self.bags = 0                            # of the mini-batch that fragment() was last called with
+        self.bags = 0                            # of the mini-batch that fragment() or step() was last called with
         self.n_dense = int(n_dense)
         # host_table: fp32 [N, D], or a list of one fp32 [rows_t, D] tensor per table (a table too large for one
         # allocation).  It must be memory the device can address: from hl_host_alloc (binding.host_table_tensor),
@@ -158,6 +158,7 @@ class Hotline:
 
     # ---- acceleration phase: single calls ---------------------------------------------------------------------
     def fragment(self, indices, offsets, batch: int, dense: Optional[torch.Tensor] = None) -> None:
+        self.bags = 0                                # (of a call that fails, what the buffers hold is not known)
         B.hl_fragment(self.ctx, self._batch(indices, offsets, batch), dense, self.n_dense if dense is not None else 0,
                       self.perm, self.counts, self.pop, self.non, self.dense_out if dense is not None else None,
                       self.main.cuda_stream)
@@ -223,9 +224,11 @@ class Hotline:
         that receives, per call name, a list of (start, end) CUDA events recorded on the stream of that call."""
 
         if timers is None:
+            self.bags = 0                            # (of a call that fails, what the buffers hold is not known)
             B.hl_step(self.ctx, self._batch(indices, offsets, batch), dense, self.n_dense if dense is not None else 0,
                       self.step_buffers, self.cache, self.host_table, grad_pop, grad_non, lr, deferred,
                       self.main.cuda_stream, (self.side if overlap else self.main).cuda_stream)
+            self.bags = self.T * batch * self.S
             return
 
         # timed call by call

@@ -46,3 +46,54 @@ def test_gradients_of_weights_are_fp32_whatever_torchs_default(route, rows, defa
     assert grad_w.dtype == torch.float32 and grad_w.shape == (8, 2)
     assert grad_y.dtype == rows and all(t.dtype == rows for t in others)
     assert len(route.calls) == 4
+
+
+@pytest.fixture
+def hotline(hl, monkeypatch):
+    """A Hotline of 3 tables with rows of 8, at most 64 inputs, whose calls go to `calls`."""
+    from types import SimpleNamespace
+
+    from paper_2204_05436_b200 import pipeline
+    h = hl.Hotline.__new__(hl.Hotline)
+    h.ctx, h.calls = None, []
+    for name in ("hl_fragment", "hl_step", "hl_embbag_bwd_prepare_merged", "hl_embbag_grad_sumsq", "hl_grad_clip", "hl_embbag_bwd_apply"):
+        monkeypatch.setattr(pipeline.B, name, lambda *a, name=name: h.calls.append(name))
+    h._batch = lambda indices, offsets, batch: batch
+    h.device = torch.device("cpu")
+    h.T, h.S, h.D, h.max_batch, h.max_nnz, h.n_dense, h.bags = 3, 1, 8, 64, 64 * 3, 0, 0
+    h.max_bags = 64 * 3
+    h.cache, h.host_table = torch.zeros(4, 8), None
+    h.perm = h.counts = h.counts_non = h.pop = h.non = h.dense_out = h.step_buffers = None
+    h.main = h.side = SimpleNamespace(cuda_stream=0)
+    h.clip_sorted = tuple(torch.zeros(192, dtype=torch.int32) for _ in range(3))
+    h.clip_sumsq, h.clip_norm, h.clip_ws = torch.zeros(1, dtype=torch.float64), torch.zeros(1), torch.zeros(256, dtype=torch.uint8)
+    return h
+
+
+def test_clipping_goes_by_the_mini_batch_that_step_put_in_the_buffers(hotline):
+    """step() fills the buffers that fragment() fills: gradients of fewer bags than its mini-batch has are refused."""
+    h = hotline
+    h.fragment(None, None, 16)
+    h.update_clipped(torch.zeros(16 * 3, 8), 0.1, 1.0)
+    h.step(None, None, 50, None, None, 0.1)
+    done = len(h.calls)
+    with pytest.raises(ValueError):
+        h.update_clipped(torch.zeros(16 * 3, 8), 0.1, 1.0)
+    assert len(h.calls) == done
+    h.update_clipped(torch.zeros(50 * 3, 8), 0.1, 1.0)
+    assert len(h.calls) > done
+
+
+def test_clipping_needs_a_mini_batch_after_a_step_that_failed(hotline, monkeypatch):
+    """What the buffers hold then is not known."""
+    from paper_2204_05436_b200 import pipeline
+
+    def failing(*a):
+        raise RuntimeError
+    h = hotline
+    h.fragment(None, None, 16)
+    monkeypatch.setattr(pipeline.B, "hl_step", failing)
+    with pytest.raises(RuntimeError):
+        h.step(None, None, 50, None, None, 0.1)
+    with pytest.raises(ValueError):
+        h.update_clipped(torch.zeros(64 * 3, 8), 0.1, 1.0)
