@@ -659,7 +659,8 @@ HL_API int32_t hl_grad_clip(const hl_tensor* tensors, int32_t n_tensors, const d
  * of d_grad_out's rows over the lookups of u.  d_sorted_slots, d_sorted_bags and *d_n_lookups as made by
  * hl_embbag_bwd_prepare, or by hl_embbag_bwd_prepare_merged (with d_n_lookups + 2); skipped lookups add nothing.  With it as
  * one of d_further, hl_grad_clip clips by the norm of the tables' gradients, which is not that of d_grad_out where several
- * lookups share a row.  Scratch: the backward region (prepare's and apply's). */
+ * lookups share a row.  Rows of up to 1 024 values (HL_EINVAL beyond).  Scratch: the backward region, prepare's and apply's: do
+ * not overlap it with either.  In a pipeline (hl_pipe), where the sort of a later mini-batch may run at any time, it has no place. */
 HL_API int32_t hl_embbag_grad_sumsq(hl_ctx* ctx, const int32_t* d_sorted_slots, const int32_t* d_sorted_bags,
                                     const int32_t* d_n_lookups, const float* d_grad_out, double* d_sumsq, void* stream);
 

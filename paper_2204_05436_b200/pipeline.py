@@ -187,9 +187,12 @@ class Hotline:
         gradients ((tensor, tensor) in place, or (src, dst) pairs; see binding.make_tensors).  ``grad_all``: the gradients of O's
         bags, then X's (X's block begins at row tables * n_pop * steps), scaled in place, as ``others`` are.  Call it when X's
         slots are known (gather_cold) and both forwards are queued; all of it is in the main stream's order.  Returns the norm
-        (fp32 [1]; the next call overwrites it)."""
+        (fp32 [1]; the next call overwrites it).  Rows of up to 1 024 values.  The pipelined schedules update their mini-batches
+        without clipping, and with one of theirs in flight the call is refused: their sorts and updates use its scratch."""
+        if not self.idle:
+            raise ValueError("mini-batches are in the pipeline, whose sorts and updates use the scratch that clipping takes")
         if not self.bags:
-            raise ValueError("no mini-batch: fragment() comes first")
+            raise ValueError("no mini-batch: fragment() comes first (those of a pipeline's start() and step() are not clipped)")
         if grad_all.dtype != torch.float32 or grad_all.dim() != 2 or grad_all.shape[1] != self.D or not grad_all.is_contiguous() \
                 or not self.bags <= grad_all.shape[0] <= self.max_bags or grad_all.device != self.cache.device:
             raise ValueError(f"grad_all is a contiguous fp32 [bags, {self.D}] tensor on {self.cache.device}, of {self.bags} to "
@@ -265,6 +268,11 @@ class Hotline:
     def synchronize(self) -> None:
         self.main.synchronize()
         self.side.synchronize()
+
+    @property
+    def idle(self) -> bool:
+        """Whether no mini-batch is in flight in a pipeline (there is none here)."""
+        return True
 
 
 class _BatchSet:

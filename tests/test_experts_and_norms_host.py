@@ -97,3 +97,24 @@ def test_clipping_needs_a_mini_batch_after_a_step_that_failed(hotline, monkeypat
         h.step(None, None, 50, None, None, 0.1)
     with pytest.raises(ValueError):
         h.update_clipped(torch.zeros(64 * 3, 8), 0.1, 1.0)
+
+
+def test_clipping_is_refused_while_mini_batches_are_in_a_pipeline(hl, hotline):
+    """Their sorts, ahead on other streams, and their updates use the scratch that the call takes."""
+    h = hotline
+    grad = torch.zeros(16 * 3, 8)
+    for cls, in_flight, idle in [(hl.PipelinedHotline, dict(j_submitted=3, j_done=2), dict(j_submitted=3, j_done=3)),
+                                 (hl.NativePipelinedHotline, dict(in_flight=2, pipe=None), dict(in_flight=0, pipe=None))]:
+        p = cls.__new__(cls)
+        p.__dict__.update(h.__dict__, **in_flight)
+        p.fragment(None, None, 16)
+        h.calls.clear()
+        with pytest.raises(ValueError, match="pipeline"):
+            p.update_clipped(grad, 0.1, 1.0)
+        assert not h.calls
+        p.__dict__.update(idle)
+        p.update_clipped(grad, 0.1, 1.0)
+        assert len(h.calls) == 4
+        p.bags = 0                                   # a mini-batch of start() and step() is not one to clip
+        with pytest.raises(ValueError, match="start"):
+            p.update_clipped(grad, 0.1, 1.0)
