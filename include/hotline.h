@@ -605,8 +605,9 @@ HL_API size_t hl_expert_workspace_bytes(int64_t max_tokens, int32_t top_k, int32
 /* Fills route->place, source, counts and offsets from the router's choices d_experts [max_tokens, top_k] (expert ids; -1:
  * none).  An expert's rows hold its choices in ascending order, after those of the experts before it; expert_cap > 0: its
  * first expert_cap choices, the others get no row.  d_status (device, may be NULL) receives HL_OK, HL_EBOUNDS if an id was
- * none of -1 .. n_experts - 1 (it counts as -1), or HL_ECAPACITY if cap_rows was too small (choices that would lie behind
- * it get no row).  The workspace (256-byte aligned) holds nothing between calls; two calls in flight need one each. */
+ * none of -1 .. n_experts - 1 (it counts as -1), or HL_ECAPACITY if cap_rows was too small for the experts' rows, those that
+ * fill them up among them (choices that would lie behind it get no row, offsets end at it).  The workspace (256-byte aligned)
+ * holds nothing between calls; two calls in flight need one each. */
 HL_API int32_t hl_expert_sort(const hl_route* route, const int32_t* d_experts, int64_t expert_cap, int32_t* d_status,
                               void* d_workspace, size_t ws_bytes, void* stream);
 

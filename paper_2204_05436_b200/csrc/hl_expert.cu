@@ -149,7 +149,8 @@ struct Sort {
     }
 
     // count holds every expert's choices: turns them into the rows it gets and their offsets, both inside cap_rows.  Returns
-    // whether some did not fit.  (All rows together, filled up: less than 2^30 + 2^26.)  A thread has kPer experts in a row.
+    // whether some rows did not fit, those that fill experts up among them.  (All together: less than 2^30 + 2^26.)  A thread has
+    // kPer experts in a row.
     __device__ __forceinline__ bool place(const SortOut& o) const {
         int rows[kPer], cnt[kPer], sum = 0, all;
 #pragma unroll
@@ -163,18 +164,17 @@ struct Sort {
             sum += rows[k];
         }
         int at = before(sum, &all);
-        bool mine = false;
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             const int e = kPer * threadIdx.x + k;
             if (e >= E) break;
-            mine = mine || at + cnt[k] > o.cap_rows;
             offset[e] = min(at, o.cap_rows);
             count[e] = min(cnt[k], max(o.cap_rows - at, 0));
             at += rows[k];
         }
         if (threadIdx.x == 0) offset[E] = min(all, o.cap_rows);
-        return __syncthreads_or(mine) != 0;
+        __syncthreads();
+        return all > o.cap_rows;
     }
 
     // The rows that fill an expert up, and the plan's words, by CTA `cta` of `ctas`.

@@ -107,8 +107,8 @@ class ExpertRoute:
         self._call(B.hl_expert_sort, self._route, experts, int(expert_cap), self._status, self._ws, self._ws_bytes)
 
     def status(self, raise_on_error: bool = True) -> int:
-        """Waits for the last sort: HL_OK, HL_EBOUNDS (an id that is no expert's: counted as -1) or HL_ECAPACITY (cap_rows too small:
-        the choices behind it have no row)."""
+        """Waits for the last sort: HL_OK, HL_EBOUNDS (an id that is no expert's: counted as -1) or HL_ECAPACITY (cap_rows too small
+        for the experts' rows, those that fill them up among them: the choices behind it have no row)."""
         st = int(self._status.item())
         if raise_on_error:
             B._check("hl_expert_sort", st)
