@@ -629,8 +629,9 @@ HL_API int32_t hl_expert_combine_bwd(const hl_route* route, int32_t dtype, int64
                                      void* d_grad_y, int64_t ld_grad_y, float* d_grad_weights, void* stream);
 
 /* One of many gradient tensors: n values at src; hl_grad_clip writes them, scaled, to dst (dst == src: in place, with the
- * same type; NULL: nowhere).  Apart from that no dst overlaps a src or another dst.  Any alignment of the type's; src and dst
- * that lie alike modulo 16 bytes move fastest. */
+ * same type; NULL: nowhere).  Apart from that no dst overlaps a src or another dst (HL_EINVAL where it is the tensor's own; that
+ * of several tensors is up to the caller).  Any alignment of the type's; src and dst that lie alike modulo 16 bytes move
+ * fastest. */
 typedef struct {
     const void* src;
     void*       dst;

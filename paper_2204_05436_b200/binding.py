@@ -6,7 +6,6 @@ this module fails and says how to build it.
 """
 from __future__ import annotations
 
-import collections
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -727,24 +726,36 @@ def make_route(max_tokens: int, n_tokens, top_k: int, n_experts: int, align: int
 
 def make_tensors(pairs):
     """The list that hl_grad_norm and hl_grad_clip take, from (src, dst) or (src, dst, flags) of contiguous torch tensors;
-    dst may be None, or src itself (in place); none is written twice or as another's src, and all are on one device.  It keeps
-    their addresses, not the tensors."""
+    dst may be None, or src itself (in place).  What is written shares no byte with what else is read or written, and all
+    tensors are on one device.  It keeps their addresses, not the tensors."""
     arr = (hl_tensor * len(pairs))()
-    written, read = set(), collections.Counter(_ptr(pair[0]) for pair in pairs if pair[0].numel() > 0)
+    spans = []                                       # (first byte, byte behind the last, whether it is written)
     for i, pair in enumerate(pairs):
         src, dst, flags = pair if len(pair) == 3 else (*pair, 0)
-        if not src.is_contiguous() or (dst is not None and (not dst.is_contiguous() or dst.numel() != src.numel())):
+        n = src.numel()
+        if not src.is_contiguous() or (dst is not None and (not dst.is_contiguous() or dst.numel() != n)):
             raise ValueError("gradient tensors are contiguous, and dst has as many values as src")
         if src.device != pairs[0][0].device or (dst is not None and dst.device != src.device):
             raise ValueError("the tensors are on one device")
-        if dst is not None and dst.numel() > 0:
-            if _ptr(dst) in written:
-                raise ValueError("a tensor is written twice")
-            if read[_ptr(dst)] > (_ptr(dst) == _ptr(src)):
-                raise ValueError("a tensor that is written is read as another's source")
-            written.add(_ptr(dst))
-        arr[i] = hl_tensor(_ptr(src), _ptr(dst), src.numel(), dtype_of(src), dtype_of(src if dst is None else dst),
-                           int(flags), 0)
+        p, kind = _ptr(src), dtype_of(src)
+        q, to = (None, kind) if dst is None else (_ptr(dst), dtype_of(dst))
+        arr[i] = hl_tensor(p, q, n, kind, to, int(flags), 0)
+        if n > 0:
+            if q != p or to != kind:
+                spans.append((p, p + n * (4 if kind == HL_F32 else 2), False))
+            if q is not None:
+                spans.append((q, q + n * (4 if to == HL_F32 else 2), True))
+    spans.sort()
+    read = written = 0                               # where those before end
+    for begin, end, writes in spans:
+        if writes and begin < written:
+            raise ValueError("a tensor is written twice")
+        if begin < (read if writes else written):
+            raise ValueError("a tensor that is written overlaps another's source, or a part of its own")
+        if writes:
+            written = max(written, end)
+        else:
+            read = max(read, end)
     return arr
 
 

@@ -294,7 +294,9 @@ bool tensors_ok(const hl_tensor* ts, int32_t n, Count (&count)[2]) {
             return false;
         if (t.n == 0) continue;
         if (!t.src || (reinterpret_cast<uintptr_t>(t.src) & (s - 1)) || (reinterpret_cast<uintptr_t>(t.dst) & (d - 1))) return false;
-        if (t.dst == t.src && t.src_dtype != t.dst_dtype) return false;
+        // (over the whole of itself, with the same type, or over nothing of it; of other tensors nothing is compared here)
+        const uintptr_t from = reinterpret_cast<uintptr_t>(t.src), to = reinterpret_cast<uintptr_t>(t.dst);
+        if (from == to ? t.src_dtype != t.dst_dtype : to && from < to + t.n * d && to < from + t.n * s) return false;
         for (const Which which : {kOfNorm, kToWrite}) {
             if (!counts(t, which)) continue;
             count[which].values += t.n;

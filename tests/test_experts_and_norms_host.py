@@ -118,3 +118,42 @@ def test_clipping_is_refused_while_mini_batches_are_in_a_pipeline(hl, hotline):
         p.bags = 0                                   # a mini-batch of start() and step() is not one to clip
         with pytest.raises(ValueError, match="start"):
             p.update_clipped(grad, 0.1, 1.0)
+
+
+def test_gradient_lists_of_views_that_overlap(hl):
+    """What is written shares no byte with what else is read or written, wherever the two begin; what is only read may."""
+    flat, out = torch.zeros(200), torch.zeros(400)
+    half = torch.zeros(400, dtype=torch.bfloat16)
+    a, b, c = flat[:100], flat[50:150], flat[100:]
+    for bad in ([(a, a), (b, b)],                    # scaled in place, both
+                [(b, b), (a, a)],
+                [(a, out[:100]), (b, out[99:199])],  # written twice
+                [(a, out[10:110]), (out[:11], None)],  # read, and another's dst
+                [(out[109:200], None), (a, out[10:110])],
+                [(a, a), (c, None), (flat[99:101], None)],
+                [(a, b)], [(b, a)],                  # its own src, shifted
+                [(a, half[:100]), (half[99:], None)],
+                [(half[:100], half.view(torch.float32)[:100])],
+                [(half[:100], half.view(torch.float16)[:100])],
+                [(flat, None), (out[:1], flat[199:])],
+                [(flat[:1], flat[:1]), (flat, None)]):
+        with pytest.raises(ValueError):
+            hl.make_tensors(bad)
+    for good in ([(a, a), (c, c)],                   # side by side
+                 [(a, None), (b, None), (flat, out[:200]), (a, out[200:300]), (b, out[300:])],
+                 [(a, c)], [(flat[i:i + 1], flat[i:i + 1]) for i in range(199, -1, -1)],
+                 [(half[:100], half.view(torch.float32)[50:150])],
+                 [(a, a), (flat[50:50], None), (flat[50:50], flat[60:60])]):       # (empty ones, inside)
+        assert len(hl.make_tensors(good)) == len(good)
+
+
+def test_a_tensor_written_over_a_part_of_itself_is_refused_by_the_library(hl):
+    """(Addresses that nothing is read from or written to; a list made by hand.)"""
+    P, need = 0x7000_0000_0000, hl.hl_grad_workspace_bytes()
+    F32, BF16 = hl.HL_F32, hl.HL_BF16
+    for src, dst, n, s, d in [(P, P + 4, 10, F32, F32), (P + 4, P, 10, F32, F32), (P, P + 36, 10, F32, F32), (P, P + 16, 10, BF16, F32),
+                              (P + 36, P, 10, BF16, F32), (P, P + 36, 10, F32, BF16), (P, P, 10, BF16, F32)]:
+        ts = (hl.hl_tensor * 1)(hl.hl_tensor(src, dst, n, s, d, 0, 0))
+        with pytest.raises(hl.HotlineError) as e:
+            hl.hl_grad_clip(ts, None, 0, 1.0, P, P + (1 << 20), need, None)
+        assert e.value.status == hl.HL_EINVAL
