@@ -16,11 +16,39 @@ need a route each.
 """
 from __future__ import annotations
 
+import math
 from typing import Optional, Tuple
 
 import torch
 
 from . import binding as B
+
+
+def _share(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether two matrices, rows of values side by side, have a byte in common."""
+    if not a.numel() or not b.numel():
+        return False
+    if a.shape[0] > b.shape[0]:
+        a, b = b, a
+    (p, w, step, n), (q, v, other, m) = ((t.data_ptr(), t.shape[1] * t.element_size(), t.stride(0) * t.element_size() if t.shape[0] > 1
+                                          else 0, t.shape[0]) for t in (a, b))
+    # columns of one buffer: rows begin in different places of every step
+    g = math.gcd(step, other)
+    if g and w <= (q - p) % g <= g - v:
+        return False
+    # of b's rows, those that a row of a may touch: the last that begins before it or with it, and the next
+    begin = p + step * torch.arange(n, device="cpu")
+    before = torch.div(begin - q, max(other, 1), rounding_mode="floor")
+    rows = (q + other * (before + k).clamp(0, m - 1) for k in (0, 1))
+    return any(bool(((row < begin + w) & (begin < row + v)).any()) for row in rows)
+
+
+def _span(t: Optional[torch.Tensor], rows: int, ld: int):
+    """A matrix with its first byte and the one behind its last (None: none)."""
+    if t is None:
+        return None, 0, 0
+    p = t.data_ptr()
+    return t, p, p + ((rows - 1) * ld + t.shape[1]) * t.element_size()
 
 
 class ExpertRoute:
@@ -84,10 +112,12 @@ class ExpertRoute:
         return ld
 
     @staticmethod
-    def _apart(a: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
-        for o in others:
-            if o is not None and o.numel() and a.numel() and o.data_ptr() == a.data_ptr():
-                raise ValueError("what is written is none of what is read")
+    def _apart(written, *others) -> None:
+        """Of _span()s."""
+        t, begin, end = written
+        for o, p, q in others:
+            if begin < q and p < end and _share(t, o):
+                raise ValueError("what is written shares nothing with what else is read or written")
 
     def sort(self, experts: torch.Tensor, n_tokens: Optional[torch.Tensor] = None, expert_cap: int = 0) -> None:
         """Makes the plan from the router's choices, int32 [tokens, top_k] with at most max_tokens tokens.  ``n_tokens`` (int32 [1],
@@ -103,6 +133,11 @@ class ExpertRoute:
                 raise ValueError("n_tokens is an int32")
         if int(expert_cap) < 0:
             raise ValueError("expert_cap is not negative")
+        begin, size = experts.data_ptr(), 4 * experts.numel()
+        for own in (self.place, self.source):
+            p = own.data_ptr()
+            if begin < p + 4 * own.numel() and p < begin + size:
+                raise ValueError("what is written shares nothing with what else is read or written")
         self._set(experts.shape[0], n_tokens)
         self._call(B.hl_expert_sort, self._route, experts, int(expert_cap), self._status, self._ws, self._ws_bytes)
 
@@ -121,7 +156,7 @@ class ExpertRoute:
         if out is None:
             out = torch.zeros(self.cap_rows, x.shape[1], dtype=x.dtype, device=x.device)
         ld_out = self._rows("out", out, self.cap_rows, x)
-        self._apart(out, x)
+        self._apart(_span(out, self.cap_rows, ld_out), _span(x, self.tokens, ld))
         self._call(B.hl_expert_dispatch, self._route, B.dtype_of(x), x.shape[1], x, ld, out, ld_out)
         return out
 
@@ -137,7 +172,7 @@ class ExpertRoute:
         if out is None:
             out = torch.zeros(self.tokens, y.shape[1], dtype=y.dtype, device=y.device)
         ld_out = self._rows("out", out, self.tokens, y)
-        self._apart(out, y)
+        self._apart(_span(out, self.tokens, ld_out), _span(y, self.cap_rows, ld), _span(weights, self.tokens, self.top_k))
         self._call(B.hl_expert_combine, self._route, B.dtype_of(y), y.shape[1], y, ld, weights, out, ld_out)
         return out
 
@@ -152,7 +187,6 @@ class ExpertRoute:
         if grad_y is None:
             grad_y = torch.zeros(self.cap_rows, grad_out.shape[1], dtype=grad_out.dtype, device=grad_out.device)
         ld_gy = self._rows("grad_y", grad_y, self.cap_rows, grad_out)
-        self._apart(grad_y, grad_out, y)
         if y is None:
             if grad_weights is not None:
                 raise ValueError("the gradient of the weights needs y")
@@ -160,6 +194,10 @@ class ExpertRoute:
             grad_weights = torch.zeros(self.tokens, self.top_k, dtype=torch.float32, device=grad_out.device)
         else:
             self._tensor("grad_weights", grad_weights, (self.tokens, self.top_k), torch.float32)
+        w, gw = _span(weights, self.tokens, self.top_k), _span(grad_weights, self.tokens, self.top_k)
+        read = _span(grad_out, self.tokens, ld_go), _span(y, self.cap_rows, ld_y), w
+        self._apart(_span(grad_y, self.cap_rows, ld_gy), *read, gw)
+        self._apart(gw, *read)
         self._call(B.hl_expert_combine_bwd, self._route, B.dtype_of(grad_out), grad_out.shape[1], grad_out, ld_go, y, ld_y, weights,
                    grad_y, ld_gy, grad_weights)
         return grad_y, grad_weights

@@ -157,3 +157,66 @@ def test_a_tensor_written_over_a_part_of_itself_is_refused_by_the_library(hl):
         with pytest.raises(hl.HotlineError) as e:
             hl.hl_grad_clip(ts, None, 0, 1.0, P, P + (1 << 20), need, None)
         assert e.value.status == hl.HL_EINVAL
+
+
+def _values_of(t):
+    """Where a matrix's values lie in its storage."""
+    return {t.storage_offset() + r * t.stride(0) + c for r in range(t.shape[0]) for c in range(t.shape[1])}
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_what_a_route_writes_shares_nothing_with_the_rows_it_reads(route, dtype):
+    """Views of one buffer: columns side by side and rows between rows are taken, wherever they begin; any value in common is not."""
+    import random
+    r, rng = route, random.Random(1)
+    flat, w = torch.zeros(2000, dtype=dtype), torch.zeros(8, 2)
+
+    def view(rows, begin, ld):
+        return flat[begin:].as_strided((rows, 6), (ld, 1))
+
+    pairs = [((0, 6), (48, 6)), ((0, 6), (47, 6)), ((96, 6), (0, 6)), ((95, 6), (0, 6)), ((0, 20), (6, 20)), ((0, 20), (5, 20)),
+             ((0, 20), (14, 20)), ((0, 20), (15, 20)), ((12, 24), (0, 12)), ((6, 24), (0, 12)), ((0, 6), (0, 6))]
+    pairs += [((rng.randint(0, 150), rng.randint(6, 40)), (rng.randint(0, 150), rng.choice([6, 7, 12, 20, 24, 40]))) for _ in range(600)]
+    pairs += [((rng.randint(0, 60), 12 * rng.randint(1, 4)), (rng.randint(0, 60), 12 * rng.randint(1, 4))) for _ in range(300)]
+    seen = set()
+    for few, many in pairs:
+        a, b = view(8, *few), view(16, *many)
+        shared = bool(_values_of(a) & _values_of(b))
+        seen.add(shared)
+        for call in (lambda: r.dispatch(a, b), lambda: r.combine(b, w, a), lambda: r.combine_backward(a, None, w, b),
+                     lambda: r.dispatch_backward(b, a)):
+            r.calls.clear()
+            if shared:
+                with pytest.raises(ValueError, match="written"):
+                    call()
+                assert not r.calls
+            else:
+                call()
+                assert len(r.calls) == 1
+    assert seen == {True, False}
+
+
+def test_what_a_route_writes_shares_nothing_with_weights_and_choices(route):
+    r = route
+    flat = torch.zeros(400)
+    x, y, w = torch.zeros(8, 6), torch.zeros(16, 6), flat[:16].view(8, 2)
+    grad_w = flat[16:32].view(8, 2)
+    rows = lambda begin, n: flat[begin:begin + 6 * n].view(n, 6)              # noqa: E731
+    r.combine(y, w, rows(16, 8))
+    r.combine_backward(x, y, w, rows(32, 16), grad_w)
+    r.combine_backward(x, y, None, rows(0, 16), flat[96:112].view(8, 2))
+    e = torch.zeros(8, 2, dtype=torch.int32)
+    r._status, r._ws, r._ws_bytes = torch.zeros(1, dtype=torch.int32), None, 0
+    r.sort(e)
+    n = len(r.calls)
+    for bad in (lambda: r.combine(y, w, rows(15, 8)),                          # out, weights
+                lambda: r.combine_backward(x, y, w, rows(15, 16), flat[300:316].view(8, 2)),     # grad_y, weights
+                lambda: r.combine_backward(x, y, w, rows(31, 16), grad_w),     # grad_y, grad_weights
+                lambda: r.combine_backward(x, y, w, rows(32, 16), w),          # grad_weights, weights
+                lambda: r.combine_backward(x, y, w, rows(32, 16), flat[15:31].view(8, 2)),
+                lambda: r.combine_backward(rows(31, 8), y, w, rows(100, 16), grad_w),            # grad_weights, grad_out
+                lambda: r.combine_backward(x, rows(31, 16), w, rows(200, 16), grad_w),           # grad_weights, y
+                lambda: r.sort(r.place), lambda: r.sort(r.source.view(8, 2))):
+        with pytest.raises(ValueError, match="written"):
+            bad()
+    assert len(r.calls) == n
