@@ -76,6 +76,7 @@ class ExpertRoute:
         self.counts = torch.zeros(self.n_experts, **i32)
         self.offsets = torch.zeros(self.n_experts + 1, **i32)
         self._status = torch.zeros(1, **i32)
+        self._sorted_on: Optional[torch.cuda.Stream] = None
         self._ws_bytes = B.hl_expert_workspace_bytes(self.max_tokens, self.top_k, self.n_experts)
         self._ws = torch.empty(self._ws_bytes, dtype=torch.uint8, device=self.device)
         self._set(self.max_tokens, None)
@@ -85,9 +86,11 @@ class ExpertRoute:
         self._route = B.make_route(tokens, n_tokens, self.top_k, self.n_experts, self.align, self.cap_rows, self.place, self.source,
                                    self.counts, self.offsets)
 
-    def _call(self, f, *a) -> None:
+    def _call(self, f, *a) -> torch.cuda.Stream:
         with torch.cuda.device(self.device):
-            f(*a, torch.cuda.current_stream(self.device).cuda_stream)
+            stream = torch.cuda.current_stream(self.device)
+            f(*a, stream.cuda_stream)
+        return stream
 
     def _here(self, name: str, t: torch.Tensor) -> None:
         if t.device != self.device:
@@ -139,11 +142,15 @@ class ExpertRoute:
             if begin < p + 4 * own.numel() and p < begin + size:
                 raise ValueError("what is written shares nothing with what else is read or written")
         self._set(experts.shape[0], n_tokens)
-        self._call(B.hl_expert_sort, self._route, experts, int(expert_cap), self._status, self._ws, self._ws_bytes)
+        self._sorted_on = self._call(B.hl_expert_sort, self._route, experts, int(expert_cap), self._status, self._ws,
+                                     self._ws_bytes)
 
     def status(self, raise_on_error: bool = True) -> int:
         """Waits for the last sort: HL_OK, HL_EBOUNDS (an id that is no expert's: counted as -1) or HL_ECAPACITY (cap_rows too small
-        for the experts' rows, those that fill them up among them: the choices behind it have no row)."""
+        for the experts' rows, those that fill them up among them: the choices behind it have no row).  The sort may have been
+        queued on any stream; one that is replayed with a graph, on the current one."""
+        if self._sorted_on is not None:
+            torch.cuda.current_stream(self.device).wait_stream(self._sorted_on)
         st = int(self._status.item())
         if raise_on_error:
             B._check("hl_expert_sort", st)
