@@ -651,11 +651,12 @@ HL_API size_t hl_grad_workspace_bytes(void);
 HL_API int32_t hl_grad_norm(const hl_tensor* tensors, int32_t n_tensors, const double* d_further, int32_t n_further,
                             float* d_norm, void* d_workspace, size_t ws_bytes, void* stream);
 
-/* hl_grad_norm, and every tensor scaled by min(1, max_norm / (norm + 1e-6)): dst = factor * src (fp32, rounded once to dst's
- * type).  Tensors in place keep their bits when the factor is 1.  max_norm >= 0.  A norm that is infinite makes the factor 0
- * (of a finite max_norm), one that is NaN makes it NaN; *d_norm (may be NULL) shows both. */
+/* hl_grad_norm, and every tensor scaled by min(1, max_norm / (norm + 1e-6)): the factor in fp64, rounded to fp32 once, then
+ * dst = factor * src (fp32, rounded once to dst's type).  Tensors in place keep their bits when the factor is 1.
+ * max_norm >= 0.  A norm that is infinite makes the factor 0 (of a finite max_norm), one that is NaN makes it NaN; *d_norm (may
+ * be NULL) shows both. */
 HL_API int32_t hl_grad_clip(const hl_tensor* tensors, int32_t n_tensors, const double* d_further, int32_t n_further,
-                            float max_norm, float* d_norm, void* d_workspace, size_t ws_bytes, void* stream);
+                            double max_norm, float* d_norm, void* d_workspace, size_t ws_bytes, void* stream);
 
 /* *d_sumsq = sum over the distinct slots u of |G_u|^2, with G_u the row gradients that hl_embbag_bwd_apply applies: the sum
  * of d_grad_out's rows over the lookups of u.  d_sorted_slots, d_sorted_bags and *d_n_lookups as made by

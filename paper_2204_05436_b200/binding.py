@@ -220,7 +220,7 @@ def _load() -> ctypes.CDLL:
     lib.hl_flush_hot.argtypes = [vp, vp, vp, vp, vp, vp]
     lib.hl_embbag_bwd_sgd_static.restype = i32
     lib.hl_embbag_bwd_sgd_static.argtypes = [vp, i64, i32, vp, vp, i32, i64, vp, ctypes.c_float, vp, vp]
-    rt, f32, sz = ctypes.POINTER(hl_route), ctypes.c_float, ctypes.c_size_t
+    rt, sz = ctypes.POINTER(hl_route), ctypes.c_size_t
     lib.hl_expert_workspace_bytes.restype = sz
     lib.hl_expert_workspace_bytes.argtypes = [i64, i32, i32]
     lib.hl_expert_sort.restype = i32
@@ -236,7 +236,7 @@ def _load() -> ctypes.CDLL:
     lib.hl_grad_norm.restype = i32
     lib.hl_grad_norm.argtypes = [ctypes.POINTER(hl_tensor), i32, vp, i32, vp, vp, sz, vp]
     lib.hl_grad_clip.restype = i32
-    lib.hl_grad_clip.argtypes = [ctypes.POINTER(hl_tensor), i32, vp, i32, f32, vp, vp, sz, vp]
+    lib.hl_grad_clip.argtypes = [ctypes.POINTER(hl_tensor), i32, vp, i32, ctypes.c_double, vp, vp, sz, vp]
     lib.hl_embbag_grad_sumsq.restype = i32
     lib.hl_embbag_grad_sumsq.argtypes = [vp, vp, vp, vp, vp, vp, vp]
     return lib

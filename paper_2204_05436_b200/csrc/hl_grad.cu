@@ -193,8 +193,8 @@ __device__ __forceinline__ double squares_of(const TensorPairArgs<N>& a, int t, 
 }
 
 // What the tensors are scaled by.
-__device__ __forceinline__ float factor_of(double norm, float max_norm) {
-    const double c = (double)max_norm / (norm + 1e-6);
+__device__ __forceinline__ float factor_of(double norm, double max_norm) {
+    const double c = max_norm / (norm + 1e-6);
     return c > 1.0 ? 1.f : (float)c;                 // (NaN: NaN)
 }
 
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kNT) k_grad_norm(const double* partial, int n_
 // A CTA takes its tiles from the last to the first: what the sums of squares read last is still in the L2.
 template <int N>
 __global__ void __launch_bounds__(kNT, 4) k_grad_scale(const __grid_constant__ TensorPairArgs<N> a, const double* partial,
-                                                    int n_partials, const double* further, int n_further, float max_norm,
+                                                    int n_partials, const double* further, int n_further, double max_norm,
                                                     float* norm) {
     const int begin = first_of(a, blockIdx.x);
     int tile = first_of(a, blockIdx.x + 1) - 1, t = tensor_of(a, tile);
@@ -356,7 +356,7 @@ Tiling tiling_of(const Count& c, int most) {
 
 template <int N>
 int32_t clip(const hl_tensor* ts, int32_t n, const Count (&count)[2], const double* further, int32_t n_further, bool scale,
-             float max_norm, float* norm, double* partial, cudaStream_t stream) {
+             double max_norm, float* norm, double* partial, cudaStream_t stream) {
     const int most = grad_grid();
     const Tiling of_norm = tiling_of(count[kOfNorm], most);
     const int n_partials = count[kOfNorm].tensors ? grid_for(of_norm.tiles, 1, most) : 0;
@@ -393,10 +393,10 @@ int32_t clip(const hl_tensor* ts, int32_t n, const Count (&count)[2], const doub
     return HL_OK;
 }
 
-int32_t clip_call(const hl_tensor* ts, int32_t n, const double* further, int32_t n_further, bool scale, float max_norm,
+int32_t clip_call(const hl_tensor* ts, int32_t n, const double* further, int32_t n_further, bool scale, double max_norm,
                   float* norm, void* ws, size_t ws_bytes, cudaStream_t stream) {
     Count count[2];
-    if (!tensors_ok(ts, n, count) || n_further < 0 || (n_further > 0 && !further) || !(max_norm >= 0.f) || (!scale && !norm) || !ws ||
+    if (!tensors_ok(ts, n, count) || n_further < 0 || (n_further > 0 && !further) || !(max_norm >= 0.0) || (!scale && !norm) || !ws ||
         (reinterpret_cast<uintptr_t>(further) & 7) || (reinterpret_cast<uintptr_t>(norm) & 3) ||
         (reinterpret_cast<uintptr_t>(ws) & 255))
         return HL_EINVAL;
@@ -718,12 +718,12 @@ extern "C" size_t hl_grad_workspace_bytes(void) { return kMaxPartials * sizeof(d
 
 extern "C" int32_t hl_grad_norm(const hl_tensor* tensors, int32_t n_tensors, const double* d_further, int32_t n_further,
                                 float* d_norm, void* d_workspace, size_t ws_bytes, void* stream) {
-    return clip_call(tensors, n_tensors, d_further, n_further, false, 0.f, d_norm, d_workspace, ws_bytes,
+    return clip_call(tensors, n_tensors, d_further, n_further, false, 0.0, d_norm, d_workspace, ws_bytes,
                      static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int32_t hl_grad_clip(const hl_tensor* tensors, int32_t n_tensors, const double* d_further, int32_t n_further,
-                                float max_norm, float* d_norm, void* d_workspace, size_t ws_bytes, void* stream) {
+                                double max_norm, float* d_norm, void* d_workspace, size_t ws_bytes, void* stream) {
     return clip_call(tensors, n_tensors, d_further, n_further, true, max_norm, d_norm, d_workspace, ws_bytes,
                      static_cast<cudaStream_t>(stream));
 }
