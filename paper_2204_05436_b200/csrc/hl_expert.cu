@@ -981,17 +981,15 @@ bool matrices_ok(int32_t dtype, int64_t dim, std::initializer_list<Matrix> ms) {
     return true;
 }
 
-int sms() {
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-        return kSMsFallback;
-    return n;
-}
+// Grids are made for a B200's multiprocessors, whatever device is current: the sort's workspace, which holds the tiles' counts, may be
+// asked for while another one is.
+constexpr int kSMs = 148;
+
 // CTAs per expert for the rows that fill it up: four a multiprocessor in all, or as many as leave each some 128 KB to write where
 // half of those rows are there (1 000 CTAs with 300 KB each ran in two rounds: 122 us instead of 98).
 int pad_units(const hl_route* r, int64_t row_bytes) {
     if (r->align <= 1 || !r->counts || !r->offsets) return 0;
-    const int64_t fill = div_up(4 * kSMsFallback, r->n_experts), work = div_up((r->align - 1) * row_bytes, 256 << 10);
+    const int64_t fill = div_up(4 * kSMs, r->n_experts), work = div_up((r->align - 1) * row_bytes, 256 << 10);
     const int64_t u = fill > work ? fill : work;
     return (int)(u < r->align - 1 ? u : r->align - 1);
 }
@@ -1031,7 +1029,7 @@ bool wide_clusters() {
 }
 
 // Tiles of at most Tile::kChoices choices: as many CTAs as fill whole rounds of the chip.
-int64_t sort_tiles(int64_t n) { return div_up(div_up(n > 0 ? n : 1, Tile::kChoices), kSMsFallback) * kSMsFallback; }
+int64_t sort_tiles(int64_t n) { return div_up(div_up(n > 0 ? n : 1, Tile::kChoices), kSMs) * kSMs; }
 
 // Threads of a row, a power of two: enough for `each` vectors a thread, few of them without one in the last round, and at most `most`.
 // More than a warp's only where there are few rows, or for rows of which each still has seven vectors (gradients of 4 000 choices of
@@ -1040,7 +1038,7 @@ int64_t sort_tiles(int64_t n) { return div_up(div_up(n > 0 ? n : 1, Tile::kChoic
 int threads_of(int64_t rows, int64_t vectors, int each, int most) {
     int P = 1;
     while (P < most && P * each < vectors) {
-        const bool few = rows * P < (int64_t)kSMsFallback * 1024;
+        const bool few = rows * P < (int64_t)kSMs * 1024;
         const int64_t round = 2 * P * each, idle = div_up(vectors, round) * round - vectors;
         if (!few && ((P >= 32 && vectors < 14 * P) || 4 * idle > vectors)) break;
         P *= 2;
