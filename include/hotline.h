@@ -584,7 +584,8 @@ HL_API int32_t hl_wide_index_cold(hl_wide* w, const int32_t* d_non_offsets, cons
 /* Where every token's rows are among the experts'.  Choice a = t * top_k + k is token t's k-th.  max_tokens * top_k < 2^30. */
 typedef struct {
     const int32_t* n_tokens;         /* device: how many tokens there are, at most max_tokens (NULL: max_tokens).  What
-                                        belongs to the tokens behind them is neither read nor written by any call      */
+                                        belongs to the tokens behind them is not written by any call, and no result
+                                        depends on it (buffers hold max_tokens all the same: parts of it may be read)  */
     int64_t        max_tokens;
     int32_t        top_k;            /* 1 .. HL_MAX_TOP_K                                                               */
     int32_t        n_experts;        /* 1 .. HL_MAX_EXPERTS                                                             */
