@@ -3,6 +3,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <cstring>
+
 #include "hl_common.cuh"
 
 namespace hl {
@@ -255,17 +257,18 @@ __global__ void __launch_bounds__(kNT) k_grad_norm(const double* partial, int n_
     if (threadIdx.x == 0) *norm = (float)sqrt(sum);
 }
 
-// A CTA takes its tiles from the last to the first: what the sums of squares read last is still in the L2.
+// A CTA takes its tiles from the last to the first: what the sums of squares read last is still in the L2.  max_norm: the bits of a
+// double.
 template <int N>
 __global__ void __launch_bounds__(kNT, 4) k_grad_scale(const __grid_constant__ TensorPairArgs<N> a, const double* partial,
-                                                    int n_partials, const double* further, int n_further, double max_norm,
+                                                    int n_partials, const double* further, int n_further, long long max_norm,
                                                     float* norm) {
     const int begin = first_of(a, blockIdx.x);
     int tile = first_of(a, blockIdx.x + 1) - 1, t = tensor_of(a, tile);
     wait_for_last();
     const double total = sqrt(total_squares(partial, n_partials, further, n_further));
     if (blockIdx.x == 0 && threadIdx.x == 0 && norm) *norm = (float)total;
-    const float f = factor_of(total, max_norm);
+    const float f = factor_of(total, __longlong_as_double(max_norm));
     for (; tile >= begin; --tile) {
         if (a.first_tile[t] > tile) --t;
         scale(a, t, tile, f);
@@ -357,6 +360,8 @@ Tiling tiling_of(const Count& c, int most) {
 template <int N>
 int32_t clip(const hl_tensor* ts, int32_t n, const Count (&count)[2], const double* further, int32_t n_further, bool scale,
              double max_norm, float* norm, double* partial, cudaStream_t stream) {
+    long long max_norm_bits;
+    std::memcpy(&max_norm_bits, &max_norm, sizeof max_norm_bits);
     const int most = grad_grid();
     const Tiling of_norm = tiling_of(count[kOfNorm], most);
     const int n_partials = count[kOfNorm].tensors ? grid_for(of_norm.tiles, 1, most) : 0;
@@ -370,7 +375,7 @@ int32_t clip(const hl_tensor* ts, int32_t n, const Count (&count)[2], const doub
     };
     const auto write_scaled = [&](const TensorPairArgs<N>& a) -> int32_t {
         HL_CUDA_TRY(launch_cluster(k_grad_scale<N>, grid_for(a.n_tiles, 1, most), kNT, 0, said ? 0 : first_after, stream, a,
-                                   (const double*)partial, n_partials, further, n_further, max_norm, said ? nullptr : norm));
+                                   (const double*)partial, n_partials, further, n_further, max_norm_bits, said ? nullptr : norm));
         said = true;
         note_launches(1);
         return HL_OK;
