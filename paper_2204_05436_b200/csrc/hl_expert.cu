@@ -722,8 +722,8 @@ __global__ void __launch_bounds__(kRowNT, 4) k_expert_combine_bwd(
 // are not all inside a buffer are not read.  Neither at the memory's rate nor at that of instructions (66 and 53 % of the cycles issue
 // one, a third of them to put lines together): the latency of two loads in a row with half of the warps there, every line that is read
 // asked for twice, by neighbours, and in the sums place, weight and address found out again for every line.  Three rows of 337 fp16 for
-// each of 28 657 tokens, a tenth of them none: sums 71 MB in 22 us, gradients 123 MB in 34: 3.2 and 3.6 TB/s.  Value by value they took 23 to 29 and 64 to 118;
-// a line a thread for both, with the lines in registers, 119 together.
+// each of 28 657 tokens, a tenth of them none: sums 71 MB in 22 us, gradients 123 MB in 34: 3.2 and 3.6 TB/s.  Value by value they took
+// 23 to 29 and 64 to 118; a line a thread for both, with the lines in registers, 119 together.
 template <typename T>
 struct Buffer {
     const T* p;
