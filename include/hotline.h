@@ -668,6 +668,98 @@ HL_API int32_t hl_grad_clip(const hl_tensor* tensors, int32_t n_tensors, const d
 HL_API int32_t hl_embbag_grad_sumsq(hl_ctx* ctx, const int32_t* d_sorted_slots, const int32_t* d_sorted_bags,
                                     const int32_t* d_n_lookups, const float* d_grad_out, double* d_sumsq, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * In front of a mixture of experts, and inside it: a token embedding's rows and their gradient, the router's choices and
+ * theirs, and the experts' product in 4 bits.  As above: no context, rows of any width, `ld_*` values from one row's begin to
+ * the next, and where a call takes d_n_tokens (device, may be NULL: max_tokens) what belongs to tokens behind it is not
+ * written.  d_status (device, may be NULL) receives the first error that a call finds on the device and is left alone otherwise:
+ * the caller sets it to HL_OK.  Buffers of one call must not overlap.
+ * ------------------------------------------------------------------------------------------------------- */
+
+/* out[i, :] = scale * table[tokens[i], :], in fp32, rounded once to out's type.  A token of -1 gives zeros (padding); any other
+ * number that is no row gives zeros too, and HL_EBOUNDS.  n_rows < 2^31. */
+HL_API int32_t hl_token_embed(int32_t table_dtype, int64_t n_rows, int64_t dim, const void* d_table, int64_t ld_table,
+                              const int32_t* d_tokens, int64_t max_tokens, const int32_t* d_n_tokens, float scale,
+                              int32_t out_dtype, void* d_out, int64_t ld_out, int32_t* d_status, void* stream);
+
+/* Bytes of device workspace (256-byte aligned) that hl_token_sort and hl_token_embed_bwd need for at most max_tokens < 2^30
+ * tokens and gradients of `dim` values; it holds nothing between calls, and two calls in flight need one each.  0 on invalid
+ * arguments. */
+HL_API size_t hl_token_workspace_bytes(int64_t max_tokens, int64_t dim);
+
+/* The tokens' places in the order of their rows: d_sorted[0 .. n) the rows, ascending, tokens that are no row behind all others
+ * as n_rows; d_order[0 .. n) where each was, ascending among equal ones.  HL_EBOUNDS as above. */
+HL_API int32_t hl_token_sort(const int32_t* d_tokens, int64_t max_tokens, const int32_t* d_n_tokens, int64_t n_rows,
+                             int32_t* d_sorted, int32_t* d_order, int32_t* d_status, void* d_workspace, size_t ws_bytes,
+                             void* stream);
+
+/* grad_table[u, :] = scale * sum of grad_out[i, :] over the tokens i of row u, rounded once to grad_table's type; zeros in rows
+ * without tokens.  accumulate != 0: that is added to grad_table, whose rows without tokens are left alone.  Sums are the same
+ * in every run: of 32-bit numbers, those of a row's tokens in their order, in runs that the sorted tokens alone decide.
+ * d_sorted and d_order as hl_token_sort made them, with the same d_n_tokens. */
+HL_API int32_t hl_token_embed_bwd(int64_t n_rows, int64_t dim, const int32_t* d_sorted, const int32_t* d_order,
+                                  int64_t max_tokens, const int32_t* d_n_tokens, int32_t grad_dtype, const void* d_grad_out,
+                                  int64_t ld_grad, float scale, int32_t table_dtype, void* d_grad_table, int64_t ld_table,
+                                  int32_t accumulate, void* d_workspace, size_t ws_bytes, void* stream);
+
+#define HL_SCORE_SOFTMAX 0
+#define HL_SCORE_SIGMOID 1
+#define HL_GROUP_MAX     0             /* a group of experts counts with its best one ...                                */
+#define HL_GROUP_TOP2    1             /* ... or with the sum of its two best                                            */
+#define HL_MAX_GROUPS    64
+
+/* How a router chooses: top_k of n_experts experts (1 .. HL_MAX_TOP_K, 1 .. HL_MAX_EXPERTS) out of the top_groups best of n_groups
+ * groups of experts side by side, all of one size (1, 1: no groups; top_k experts have to be in top_groups groups). */
+typedef struct {
+    int32_t score;                     /* HL_SCORE_x */
+    int32_t top_k, n_experts, n_groups, top_groups;
+    int32_t group_score;               /* HL_GROUP_x */
+    int32_t renorm;                    /* 1: the chosen scores are divided by their sum */
+    float   scale;                     /* of the weights, finite */
+} hl_router;
+
+/* s = softmax or sigmoid of the logits [max_tokens, n_experts].  Experts are ranked by s + d_bias[e] (fp32 [n_experts]; NULL: by
+ * s), ties by the lowest number.  Of every token d_experts [max_tokens, top_k] receives the chosen experts, best first, and
+ * d_weights (fp32, alike) scale * s, or scale * s / (the sum of the chosen s): the bias decides who is chosen and has no part in
+ * the weights.  The ranking is that of 64-bit scores (and of the logits themselves where there is no bias).  A group's two best count
+ * by s + bias.  An expert whose logit or bias is -inf is never chosen, nor is one where either is NaN, which says HL_EINVAL
+ * in the status word; where fewer than top_k are left, the rest are -1 with weight 0.  A logit of -inf or NaN has no part in a
+ * softmax. */
+HL_API int32_t hl_expert_choose(const hl_router* router, int32_t dtype, const void* d_logits, int64_t ld, const float* d_bias,
+                                int64_t max_tokens, const int32_t* d_n_tokens, int32_t* d_experts, float* d_weights,
+                                int32_t* d_status, void* stream);
+
+/* The logits' gradient from that of the weights, d_grad_weights (fp32 [max_tokens, top_k]), for the experts that
+ * hl_expert_choose chose; zeros for experts that have no part.  d_grad_logits is of the logits' type. */
+HL_API int32_t hl_expert_choose_bwd(const hl_router* router, int32_t dtype, const void* d_logits, int64_t ld, int64_t max_tokens,
+                                    const int32_t* d_n_tokens, const int32_t* d_experts, const float* d_grad_weights,
+                                    void* d_grad_logits, int64_t ld_grad, void* stream);
+
+/* Matrices in 4 bits.  A block of 32 values side by side in a row (the last may be shorter) has one power of two, 2^e with e =
+ * floor(log2 of the largest absolute value) - 2, at least -127; its values are rounded to 2^e times the nearest of 0, 1/2, 1,
+ * 3/2, 2, 3, 4 and 6 with their sign, ties to the one of even mantissa, larger ones to 6.  A block with an infinity or NaN is NaN.  How such
+ * a matrix lies in memory is the library's affair: hl_mx4_bytes bytes, 16-byte aligned, one matrix behind the other.
+ * `stride`: values from one matrix's begin to the next.  0 bytes on invalid arguments (and for no rows). */
+HL_API size_t hl_mx4_bytes(int64_t rows, int64_t dim);
+HL_API int32_t hl_mx4_quantise(int32_t dtype, int64_t n_matrices, int64_t rows, int64_t dim, const void* d_x, int64_t ld,
+                               int64_t stride, void* d_q, void* stream);
+HL_API int32_t hl_mx4_dequantise(int64_t n_matrices, int64_t rows, int64_t dim, const void* d_q, int32_t dtype, void* d_out,
+                                 int64_t ld, int64_t stride, void* stream);
+
+/* Bytes of device workspace (256-byte aligned) that hl_expert_mx4 needs.  0 on invalid arguments.  It holds nothing between calls,
+ * and two calls in flight need one each; its first int32 is the last call's status: HL_OK, or HL_ETIMEOUT if a wait inside
+ * the product gave up. */
+HL_API size_t hl_expert_mx4_workspace_bytes(int64_t cap_rows, int32_t n_experts, int64_t dim);
+
+/* y[r, :] = x[r, :] * W[e]^T for the rows r of every expert e, both in 4 bits as above, products added in fp32, rounded once to
+ * y's type.  d_weights: n_experts matrices of `outputs` rows and `dim` columns, from hl_mx4_quantise.  d_x, of dtype as y: the rows
+ * by expert [cap_rows, dim], or, with by_token != 0, the tokens' [max_tokens, dim], which go to their experts on the way (no
+ * hl_expert_dispatch is needed then).  Rows of y that fill an expert up become zeros, rows behind the last expert's are left alone.  The
+ * route is hl_expert_sort's; n_tokens and place are read with by_token alone. */
+HL_API int32_t hl_expert_mx4(const hl_route* route, int32_t dtype, int64_t dim, int64_t outputs, const void* d_x, int64_t ld_x,
+                             int32_t by_token, const void* d_weights, void* d_y, int64_t ld_y, void* d_workspace, size_t ws_bytes,
+                             void* stream);
+
 /* No counterpart in the paper: an addition for callers that cannot allocate.
  *
  * Some callers have no way to hand the library a workspace: code that runs where device allocation is forbidden

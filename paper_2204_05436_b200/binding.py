@@ -30,6 +30,8 @@ EXPORTS = (
     "hl_embbag_bwd_prepare_merged", "hl_pipe_set_order", "hl_step", "hl_wide_test_bounded_waits",
     "hl_expert_workspace_bytes", "hl_expert_sort", "hl_expert_dispatch", "hl_expert_combine", "hl_expert_combine_bwd",
     "hl_grad_workspace_bytes", "hl_grad_norm", "hl_grad_clip", "hl_embbag_grad_sumsq",
+    "hl_token_embed", "hl_token_workspace_bytes", "hl_token_sort", "hl_token_embed_bwd", "hl_expert_choose", "hl_expert_choose_bwd",
+    "hl_mx4_bytes", "hl_mx4_quantise", "hl_mx4_dequantise", "hl_expert_mx4_workspace_bytes", "hl_expert_mx4",
 )
 
 
@@ -81,6 +83,12 @@ class hl_route(ctypes.Structure):
                 ("n_experts", ctypes.c_int32), ("align", ctypes.c_int32), ("cap_rows", ctypes.c_int64),
                 ("place", ctypes.c_void_p), ("source", ctypes.c_void_p), ("counts", ctypes.c_void_p),
                 ("offsets", ctypes.c_void_p)]
+
+
+class hl_router(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_int32), ("top_k", ctypes.c_int32), ("n_experts", ctypes.c_int32), ("n_groups", ctypes.c_int32),
+                ("top_groups", ctypes.c_int32), ("group_score", ctypes.c_int32), ("renorm", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
 
 
 class hl_tensor(ctypes.Structure):
@@ -239,6 +247,29 @@ def _load() -> ctypes.CDLL:
     lib.hl_grad_clip.argtypes = [ctypes.POINTER(hl_tensor), i32, vp, i32, ctypes.c_double, vp, vp, sz, vp]
     lib.hl_embbag_grad_sumsq.restype = i32
     lib.hl_embbag_grad_sumsq.argtypes = [vp, vp, vp, vp, vp, vp, vp]
+    f32, ro = ctypes.c_float, ctypes.POINTER(hl_router)
+    lib.hl_token_embed.restype = i32
+    lib.hl_token_embed.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, f32, i32, vp, i64, vp, vp]
+    lib.hl_token_workspace_bytes.restype = sz
+    lib.hl_token_workspace_bytes.argtypes = [i64, i64]
+    lib.hl_token_sort.restype = i32
+    lib.hl_token_sort.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, sz, vp]
+    lib.hl_token_embed_bwd.restype = i32
+    lib.hl_token_embed_bwd.argtypes = [i64, i64, vp, vp, i64, vp, i32, vp, i64, f32, i32, vp, i64, i32, vp, sz, vp]
+    lib.hl_expert_choose.restype = i32
+    lib.hl_expert_choose.argtypes = [ro, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp]
+    lib.hl_expert_choose_bwd.restype = i32
+    lib.hl_expert_choose_bwd.argtypes = [ro, i32, vp, i64, i64, vp, vp, vp, vp, i64, vp]
+    lib.hl_mx4_bytes.restype = sz
+    lib.hl_mx4_bytes.argtypes = [i64, i64]
+    lib.hl_mx4_quantise.restype = i32
+    lib.hl_mx4_quantise.argtypes = [i32, i64, i64, i64, vp, i64, i64, vp, vp]
+    lib.hl_mx4_dequantise.restype = i32
+    lib.hl_mx4_dequantise.argtypes = [i64, i64, i64, vp, i32, vp, i64, i64, vp]
+    lib.hl_expert_mx4_workspace_bytes.restype = sz
+    lib.hl_expert_mx4_workspace_bytes.argtypes = [i64, i32, i64]
+    lib.hl_expert_mx4.restype = i32
+    lib.hl_expert_mx4.argtypes = [rt, i32, i64, i64, vp, i64, i32, vp, vp, i64, vp, sz, vp]
     return lib
 
 
@@ -808,3 +839,83 @@ def hl_grad_clip(tensors, d_further, n_further: int, max_norm: float, d_norm, d_
 def hl_embbag_grad_sumsq(ctx: int, d_sorted_slots, d_sorted_bags, d_n_lookups, d_grad_out, d_sumsq, stream: int) -> None:
     _check("hl_embbag_grad_sumsq", _lib.hl_embbag_grad_sumsq(ctx, _ptr(d_sorted_slots), _ptr(d_sorted_bags),
                                                              _ptr(d_n_lookups), _ptr(d_grad_out), _ptr(d_sumsq), stream))
+
+
+# ---- token embeddings, routing, 4 bits --------------------------------------------------------------------------------------
+HL_SCORE_SOFTMAX, HL_SCORE_SIGMOID = 0, 1
+HL_GROUP_MAX, HL_GROUP_TOP2 = 0, 1
+HL_MAX_GROUPS = 64
+
+
+def make_router(score: int, top_k: int, n_experts: int, n_groups: int = 1, top_groups: int = 1, group_score: int = HL_GROUP_MAX,
+                renorm: bool = True, scale: float = 1.0) -> hl_router:
+    return hl_router(int(score), int(top_k), int(n_experts), int(n_groups), int(top_groups), int(group_score), int(bool(renorm)),
+                     float(scale))
+
+
+def hl_token_embed(table_dtype: int, n_rows: int, dim: int, d_table, ld_table: int, d_tokens, max_tokens: int, d_n_tokens, scale: float,
+                   out_dtype: int, d_out, ld_out: int, d_status, stream: int) -> None:
+    _check("hl_token_embed", _lib.hl_token_embed(table_dtype, n_rows, dim, _ptr(d_table), ld_table, _ptr(d_tokens), max_tokens,
+                                                 _ptr(d_n_tokens), scale, out_dtype, _ptr(d_out), ld_out, _ptr(d_status), stream))
+
+
+def hl_token_workspace_bytes(max_tokens: int, dim: int) -> int:
+    n = _lib.hl_token_workspace_bytes(int(max_tokens), int(dim))
+    if n == 0:
+        raise HotlineError("hl_token_workspace_bytes", HL_EINVAL)
+    return int(n)
+
+
+def hl_token_sort(d_tokens, max_tokens: int, d_n_tokens, n_rows: int, d_sorted, d_order, d_status, d_workspace, ws_bytes: int,
+                  stream: int) -> None:
+    _check("hl_token_sort", _lib.hl_token_sort(_ptr(d_tokens), max_tokens, _ptr(d_n_tokens), n_rows, _ptr(d_sorted), _ptr(d_order),
+                                               _ptr(d_status), _ptr(d_workspace), ws_bytes, stream))
+
+
+def hl_token_embed_bwd(n_rows: int, dim: int, d_sorted, d_order, max_tokens: int, d_n_tokens, grad_dtype: int, d_grad_out, ld_grad: int,
+                       scale: float, table_dtype: int, d_grad_table, ld_table: int, accumulate: bool, d_workspace, ws_bytes: int,
+                       stream: int) -> None:
+    _check("hl_token_embed_bwd", _lib.hl_token_embed_bwd(
+        n_rows, dim, _ptr(d_sorted), _ptr(d_order), max_tokens, _ptr(d_n_tokens), grad_dtype, _ptr(d_grad_out), ld_grad, scale,
+        table_dtype, _ptr(d_grad_table), ld_table, int(bool(accumulate)), _ptr(d_workspace), ws_bytes, stream))
+
+
+def hl_expert_choose(router: hl_router, dtype: int, d_logits, ld: int, d_bias, max_tokens: int, d_n_tokens, d_experts, d_weights,
+                     d_status, stream: int) -> None:
+    _check("hl_expert_choose", _lib.hl_expert_choose(router, dtype, _ptr(d_logits), ld, _ptr(d_bias), max_tokens, _ptr(d_n_tokens),
+                                                     _ptr(d_experts), _ptr(d_weights), _ptr(d_status), stream))
+
+
+def hl_expert_choose_bwd(router: hl_router, dtype: int, d_logits, ld: int, max_tokens: int, d_n_tokens, d_experts, d_grad_weights,
+                         d_grad_logits, ld_grad: int, stream: int) -> None:
+    _check("hl_expert_choose_bwd", _lib.hl_expert_choose_bwd(
+        router, dtype, _ptr(d_logits), ld, max_tokens, _ptr(d_n_tokens), _ptr(d_experts), _ptr(d_grad_weights), _ptr(d_grad_logits),
+        ld_grad, stream))
+
+
+def hl_mx4_bytes(rows: int, dim: int) -> int:
+    n = _lib.hl_mx4_bytes(int(rows), int(dim))
+    if n == 0 and rows != 0:
+        raise HotlineError("hl_mx4_bytes", HL_EINVAL)
+    return int(n)
+
+
+def hl_mx4_quantise(dtype: int, n_matrices: int, rows: int, dim: int, d_x, ld: int, stride: int, d_q, stream: int) -> None:
+    _check("hl_mx4_quantise", _lib.hl_mx4_quantise(dtype, n_matrices, rows, dim, _ptr(d_x), ld, stride, _ptr(d_q), stream))
+
+
+def hl_mx4_dequantise(n_matrices: int, rows: int, dim: int, d_q, dtype: int, d_out, ld: int, stride: int, stream: int) -> None:
+    _check("hl_mx4_dequantise", _lib.hl_mx4_dequantise(n_matrices, rows, dim, _ptr(d_q), dtype, _ptr(d_out), ld, stride, stream))
+
+
+def hl_expert_mx4_workspace_bytes(cap_rows: int, n_experts: int, dim: int) -> int:
+    n = _lib.hl_expert_mx4_workspace_bytes(int(cap_rows), int(n_experts), int(dim))
+    if n == 0:
+        raise HotlineError("hl_expert_mx4_workspace_bytes", HL_EINVAL)
+    return int(n)
+
+
+def hl_expert_mx4(route: hl_route, dtype: int, dim: int, outputs: int, d_x, ld_x: int, by_token: bool, d_weights, d_y, ld_y: int,
+                  d_workspace, ws_bytes: int, stream: int) -> None:
+    _check("hl_expert_mx4", _lib.hl_expert_mx4(route, dtype, dim, outputs, _ptr(d_x), ld_x, int(bool(by_token)), _ptr(d_weights),
+                                               _ptr(d_y), ld_y, _ptr(d_workspace), ws_bytes, stream))

@@ -1,0 +1,619 @@
+// Matrices in 4 bits: blocks of 32 values of a row share a power of two.  Quantisation, the way back, and the experts' product
+// on the tensor cores, which multiply such blocks as they are.
+#include "hl_rows.cuh"
+
+namespace hl {
+namespace {
+
+// ---- how a matrix lies ------------------------------------------------------------------------------------------------
+// In tiles of 128 rows by 256 columns, those of 128 rows side by side, filled up with zeros at both ends; a tile is the 17 408 bytes
+// that a product's step takes as they are, in one copy: 16 KB of values, 128 bytes a row in the 16-byte pieces' order in which the
+// tensor cores read shared memory without bank conflicts (piece p of row r lies at p ^ (r & 7)), and 1 KB of exponents, for each half
+// of the columns 32 pieces of 16 bytes, of which piece r % 32 holds four of each of the rows r % 32, + 32, + 64 and + 96.
+constexpr int kTileRows = 128, kTileCols = 256, kBlock = 32;
+constexpr int kValueBytes = kTileRows * kTileCols / 2, kTileBytes = kValueBytes + kTileRows * kTileCols / kBlock;
+static_assert(kTileBytes == 17408 && kTileBytes % 1024 == 0, "tiles side by side begin where the pieces' order does");
+
+// a lane's eight values among the 256 of a row's part: lanes 4b .. 4b + 3 have block b
+__device__ __forceinline__ int value_at(int row, int lane) { return row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + ((lane & 3) << 2); }
+__device__ __forceinline__ int exponent_at(int row, int block) {
+    return kValueBytes + (block >> 2) * 512 + (row & 31) * 16 + (row >> 5) * 4 + (block & 3);
+}
+
+// Eight values of a row's part in 4 bits, and their block's exponent (in all of its lanes): 2^(E - 127) with E two below the
+// largest value's own, so that this one lies in 4 .. 8, of which what is above 6 becomes 6; values are rounded to the nearest of 0, 1/2, 1,
+// 3/2, 2, 3, 4, 6, ties to the one of even mantissa.  A block with an infinity or NaN is NaN (exponent 255).
+__device__ __forceinline__ uint32_t to_four_bits(const float (&x)[8], uint32_t* exponent) {
+    uint32_t top = 0;                  // (of the bits, so that NaN is the largest)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int e = (int)(top >> 23);
+    const uint32_t E = e == 255 ? 255u : (uint32_t)max(e - 2, 0);
+    const float up = __uint_as_float((254u - min(E, 253u)) << 23);         // 2^(127 - E)
+    uint32_t packed;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(packed)
+        : "f"(x[0] * up), "f"(x[1] * up), "f"(x[2] * up), "f"(x[3] * up), "f"(x[4] * up), "f"(x[5] * up), "f"(x[6] * up),
+          "f"(x[7] * up));
+    *exponent = E;
+    return packed;
+}
+
+// A row's part from column c0 on, eight values a lane; zeros behind its end and where there is no row.
+template <typename T, bool WHOLE>
+struct Part {
+    Pack<T, WHOLE ? 8 : 1> v[WHOLE ? 1 : 8];
+    __device__ __forceinline__ void load(const T* row, int64_t c, int64_t dim) {
+        if constexpr (WHOLE) {
+            v[0].zero();
+            if (row && c < dim) v[0].load(row + c);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i].zero();
+                if (row && c + i < dim) v[i].load(row + c + i);
+            }
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        if constexpr (WHOLE) {
+            v[0].get(x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float one[1];
+                v[i].get(one);
+                x[i] = one[0];
+            }
+        }
+    }
+};
+__device__ __forceinline__ void store_part(uint8_t* tile, int row, int lane, uint32_t packed, uint32_t exponent) {
+    *reinterpret_cast<uint32_t*>(tile + value_at(row, lane)) = packed;
+    if ((lane & 3) == 0) tile[exponent_at(row, lane >> 2)] = (uint8_t)exponent;
+}
+
+constexpr int kRowNT = 256;
+
+// n_matrices of `rows` rows: a warp takes U parts of rows, side by side.  Bound by memory.
+template <typename T, bool WHOLE, int U>
+__global__ void __launch_bounds__(kRowNT) k_mx4_quantise(const T* __restrict__ x, int64_t rows, int64_t dim, int64_t ld, int64_t stride,
+                                                         int64_t row_tiles, int64_t col_tiles, int64_t parts, uint8_t* __restrict__ q) {
+    const int lane = threadIdx.x & 31;
+    const int64_t first = ((int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5)) * U;
+    Part<T, WHOLE> in[U];
+    int64_t tile[U];
+    int r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = min(first + u, parts - 1), row = i / col_tiles, ct = i - row * col_tiles;      // of all, with those that fill up
+        const int64_t m = row / (row_tiles * kTileRows), of = row - m * row_tiles * kTileRows;
+        r[u] = (int)(of & (kTileRows - 1));
+        tile[u] = (m * row_tiles + of / kTileRows) * col_tiles + ct;
+        in[u].load(of < rows ? x + m * stride + of * ld : nullptr, ct * kTileCols + lane * 8, dim);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (first + u >= parts) break;
+        float v[8];
+        uint32_t e;
+        in[u].get(v);
+        const uint32_t packed = to_four_bits(v, &e);
+        store_part(q + tile[u] * kTileBytes, r[u], lane, packed, e);
+    }
+}
+
+__device__ __forceinline__ void from_four_bits(uint32_t packed, uint32_t E, float (&x)[8]) {
+    const float unit = E == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(E ? E << 23 : 0x00400000u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t two;                  // fp16
+        asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\t}" : "=r"(two) : "r"(packed >> (8 * i)));
+        x[2 * i] = __half2float(__ushort_as_half((unsigned short)(two & 0xffffu))) * unit;
+        x[2 * i + 1] = __half2float(__ushort_as_half((unsigned short)(two >> 16))) * unit;
+    }
+}
+
+template <typename T, bool WHOLE, int U>
+__global__ void __launch_bounds__(kRowNT) k_mx4_dequantise(const uint8_t* __restrict__ q, int64_t rows, int64_t dim, int64_t row_tiles,
+                                                           int64_t col_tiles, int64_t parts, T* __restrict__ out, int64_t ld,
+                                                           int64_t stride) {
+    const int lane = threadIdx.x & 31;
+    const int64_t first = ((int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5)) * U;
+    uint32_t packed[U], E[U];
+    int64_t at[U], c[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = min(first + u, parts - 1), row = i / col_tiles, ct = i - row * col_tiles;      // of all rows that there are
+        const int64_t m = row / rows, of = row - m * rows;
+        const int r = (int)(of & (kTileRows - 1));
+        const uint8_t* tile = q + ((m * row_tiles + of / kTileRows) * col_tiles + ct) * kTileBytes;
+        packed[u] = __ldg(reinterpret_cast<const uint32_t*>(tile + value_at(r, lane)));
+        E[u] = __ldg(tile + exponent_at(r, lane >> 2));
+        at[u] = m * stride + of * ld;
+        c[u] = ct * kTileCols + lane * 8;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (first + u >= parts || c[u] >= dim) continue;
+        float x[8];
+        from_four_bits(packed[u], E[u], x);
+        if constexpr (WHOLE) {
+            Pack<T, 8> v;
+            v.set(x);
+            v.store(out + at[u] + c[u]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c[u] + i < dim) out[at[u] + c[u] + i] = from_float<T>(x[i]);
+        }
+    }
+}
+
+// ---- the experts' rows ------------------------------------------------------------------------------------------------
+// Expert e's rows are cut into tiles of 128 of their own, wherever they begin in the expert-ordered buffers: first[e] is its first
+// tile's number, first[E] how many there are (never more than the workspace holds).
+struct Experts {
+    const int32_t *counts, *offsets;
+    int E;
+    int64_t cap_rows;
+    __device__ __forceinline__ int begin(int e) const { return (int)min((int64_t)max(__ldg(&offsets[e]), 0), cap_rows); }
+    __device__ __forceinline__ int rows(int e, int from) const { return (int)min((int64_t)max(__ldg(&counts[e]), 0), cap_rows - from); }
+};
+
+// Fills s_first [E + 1] (and s_begin [E], if there): by all NT threads of a CTA.
+template <int NT>
+__device__ void tile_numbers(const Experts& x, int most, int* s_first, int* s_begin) {
+    constexpr int kPer = (HL_MAX_EXPERTS + NT - 1) / NT;
+    __shared__ int s_warp[NT / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int tiles[kPer], sum = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int e = threadIdx.x * kPer + k;
+        tiles[k] = 0;
+        if (e >= x.E) continue;
+        const int from = x.begin(e);
+        if (s_begin) s_begin[e] = from;
+        tiles[k] = (x.rows(e, from) + kTileRows - 1) / kTileRows;
+        sum += tiles[k];
+    }
+    int incl = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += v;
+    }
+    if (lane == 31) s_warp[warp] = incl;
+    __syncthreads();
+    int at = incl - sum;
+    for (int w = 0; w < warp; ++w) at += s_warp[w];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int e = threadIdx.x * kPer + k;
+        if (e >= x.E) break;
+        s_first[e] = min(at, most);
+        at += tiles[k];
+        if (e == x.E - 1) s_first[x.E] = min(at, most);
+    }
+    __syncthreads();
+}
+// the last e of [0, n) with list[e] <= v (list[0] <= v)
+__device__ __forceinline__ int last_not_above(const int* list, int n, int v) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (list[mid] <= v) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Rows in the experts' order (top_k 0), or the tokens', each to all of its experts' rows: read and converted once.
+template <typename T, bool WHOLE>
+__global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, int64_t ld, int64_t dim, int col_tiles,
+                                                     const int32_t* n_tokens, int64_t max_rows, int top_k,
+                                                     const int32_t* __restrict__ place, const int32_t* __restrict__ counts,
+                                                     const int32_t* __restrict__ offsets, int E, int64_t cap_rows, int max_tiles,
+                                                     uint8_t* __restrict__ q, int32_t* status) {
+    __shared__ int s_first[HL_MAX_EXPERTS + 1], s_begin[HL_MAX_EXPERTS];
+    let_next_start();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *status = HL_OK;
+    const Experts experts{counts, offsets, E, cap_rows};
+    tile_numbers<kRowNT>(experts, max_tiles, s_first, s_begin);
+    const int lane = threadIdx.x & 31;
+    int64_t n = max_rows;
+    if (top_k == 0) n = min(n, (int64_t)max(__ldg(&offsets[E]), 0));
+    else if (n_tokens) n = min(n, (int64_t)max(__ldg(n_tokens), 0));
+    const int64_t parts = n * col_tiles;
+    for (int64_t i = (int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5); i < parts; i += (int64_t)gridDim.x * (kRowNT / 32)) {
+        const int64_t row = i / col_tiles;
+        const int ct = (int)(i - row * col_tiles);
+        Part<T, WHOLE> in;
+        in.load(x + row * ld, (int64_t)ct * kTileCols + lane * 8, dim);
+        float v[8];
+        uint32_t exponent;
+        in.get(v);
+        const uint32_t packed = to_four_bits(v, &exponent);
+        for (int k = 0; k < max(top_k, 1); ++k) {
+            const int at = top_k == 0 ? (int)row : __ldg(&place[row * top_k + k]);
+            if (at < 0 || at >= cap_rows) continue;
+            // (experts without rows begin where the next does: the last that begins there is the one)
+            const int e = last_not_above(s_begin, E, at), r = at - s_begin[e];
+            if (r < 0 || r >= experts.rows(e, s_begin[e])) continue;
+            const int tile = s_first[e] + r / kTileRows;
+            if (tile >= s_first[e + 1]) continue;
+            store_part(q + ((int64_t)tile * col_tiles + ct) * kTileBytes, r & (kTileRows - 1), lane, packed, exponent);
+        }
+    }
+}
+
+// ---- the product --------------------------------------------------------------------------------------------------------
+// y[row, f] = sum over d of x[row, d] * w[e, f, d] for the rows of expert e: 128 outputs f (the lanes of the tensor memory) by up to
+// 128 rows (its columns) at a time, 256 of d a step.  One warp's thread has the tiles of a step copied, one issues the products,
+// four warps take the sums out, those of one tile while the next one's are made.
+constexpr int kStages = 6, kStageBytes = 2 * kTileBytes, kProductNT = 192;
+constexpr int kAccCols = 128;          // tensor-memory columns of a tile's sums (two tiles'), then those of the exponents
+constexpr uint32_t kExponentCols = 2 * kAccCols;
+constexpr int kProductSmem = kStages * kStageBytes + 1024 + (HL_MAX_EXPERTS + 1) * 4 + 256;
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint64_t* b, int n) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(n) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* b) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_done(uint64_t* b, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_u32(b)), "r"(parity)
+        : "memory");
+    return done;
+}
+// Waits for a phase, not for ever: false if it did not come, or somebody else has given up.
+constexpr int kMaxPolls = 1 << 20;
+__device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile int* gave_up) {
+    for (int i = 0; i < kMaxPolls; ++i) {
+        if (bar_done(b, parity)) return true;
+        if (*gave_up) return false;
+    }
+    *gave_up = 1;
+    return false;
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+
+// Where an operand lies in shared memory, as the tensor cores want it said: address, bytes from one group of eight rows to the
+// next, and whether pieces of 16 bytes are in the order of the tiles' values (or of their exponents: as they come).
+__device__ __forceinline__ uint64_t operand(uint32_t address, uint32_t group_bytes, bool ordered) {
+    return (uint64_t)((address & 0x3ffffu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(group_bytes >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)(ordered ? 2 : 0) << 61;
+}
+__device__ __forceinline__ void exponents_to_tmem(uint32_t tmem, uint32_t address) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(operand(address, 128, false)) : "memory");
+}
+// 64 of d: both operands of e2m1 (code 1 in bits 7 and 10), exponents alone as factors (bit 23), 128 by n, the pair of each row's
+// four exponents that counts
+__device__ __forceinline__ void multiply(uint32_t acc, uint64_t a, uint64_t b, uint32_t n, int pair, uint32_t ea, uint32_t eb, bool add) {
+    const uint32_t what = (uint32_t)(2 * pair) << 4 | 1u << 7 | 1u << 10 | (n >> 3) << 17 | 1u << 23 | (128u >> 4) << 24 |
+                          (uint32_t)(2 * pair) << 29;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(acc),
+        "l"(a), "l"(b), "r"(what), "r"(ea), "r"(eb), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+// What a CTA does next: the tile of rows, the expert's, and the tile of outputs.
+struct Item {
+    int e, rows, f;                    // rows: of the tile
+    int64_t row0, tile, pad;           // its first row's number; pad: rows behind the expert's last that fill it up, if it is the last tile
+};
+__device__ __forceinline__ Item item_of(int64_t i, int f_tiles, const Experts& x, const int* s_first) {
+    Item it;
+    it.tile = i / f_tiles;
+    it.f = (int)(i - it.tile * f_tiles);
+    it.e = last_not_above(s_first, x.E, (int)it.tile);
+    const int begin = x.begin(it.e), rows = x.rows(it.e, begin), at = ((int)it.tile - s_first[it.e]) * kTileRows;
+    it.rows = min(rows - at, kTileRows);
+    it.row0 = (int64_t)begin + at;
+    const int64_t end = min((int64_t)max(__ldg(&x.offsets[it.e + 1]), 0), x.cap_rows);
+    it.pad = it.tile + 1 == s_first[it.e + 1] ? max(end - begin - rows, (int64_t)0) : 0;
+    return it;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ wq,
+                                                               const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets,
+                                                               int E, int64_t cap_rows, int max_tiles, int col_tiles, int f_tiles,
+                                                               int64_t outputs, T* __restrict__ y, int64_t ld, int32_t* status) {
+    extern __shared__ uint8_t s_raw[];
+    uint8_t* base = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
+    int* s_first = reinterpret_cast<int*>(base + kStages * kStageBytes);
+    __shared__ uint64_t s_full[kStages], s_empty[kStages], s_sums[2], s_taken[2];
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile int s_gave_up;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(&s_full[s], 1);
+            bar_init(&s_empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            bar_init(&s_sums[b], 1);
+            bar_init(&s_taken[b], 4);
+        }
+        s_gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    }
+    const Experts experts{counts, offsets, E, cap_rows};
+    tile_numbers<kProductNT>(experts, max_tiles, s_first, nullptr);        // (ends with a barrier)
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s_tmem;
+    const int64_t items = (int64_t)s_first[E] * f_tiles;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            wait_for_last();           // (the rows in 4 bits)
+            int stage = 0;
+            uint32_t phase = 1;
+            bool ok = true;
+            for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
+                const Item it = item_of(i, f_tiles, experts, s_first);
+                const uint8_t* a = wq + ((int64_t)it.e * f_tiles + it.f) * col_tiles * kTileBytes;
+                const uint8_t* b = xq + it.tile * col_tiles * kTileBytes;
+                const uint32_t b_bytes = ((it.rows + 15) & ~15) * 128;
+                for (int c = 0; c < col_tiles; ++c, a += kTileBytes, b += kTileBytes) {
+                    if (!(ok = bar_wait(&s_empty[stage], phase, &s_gave_up))) break;
+                    const uint32_t at = smem_u32(base + stage * kStageBytes);
+                    bar_expect(&s_full[stage], kTileBytes + b_bytes + (kTileBytes - kValueBytes));
+                    bulk_load(at, a, kTileBytes, &s_full[stage]);
+                    bulk_load(at + kTileBytes, b, b_bytes, &s_full[stage]);
+                    bulk_load(at + kTileBytes + kValueBytes, b + kValueBytes, kTileBytes - kValueBytes, &s_full[stage]);
+                    if (++stage == kStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+            for (int s = 0; ok && s < kStages; ++s) {            // (nothing may arrive here after this CTA's end)
+                ok = bar_wait(&s_empty[stage], phase, &s_gave_up);
+                if (++stage == kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int stage = 0, buffer = 0;
+            uint32_t phase = 0, taken = 1;
+            bool ok = true;
+            for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
+                const Item it = item_of(i, f_tiles, experts, s_first);
+                const uint32_t n = (it.rows + 15) & ~15, acc = tmem + buffer * kAccCols;
+                if (!(ok = bar_wait(&s_taken[buffer], taken, &s_gave_up))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                for (int c = 0; c < col_tiles; ++c) {
+                    if (!(ok = bar_wait(&s_full[stage], phase, &s_gave_up))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t at = smem_u32(base + stage * kStageBytes);
+                    const uint32_t ea = tmem + kExponentCols + (stage & 1) * 16, eb = ea + 8;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        exponents_to_tmem(ea + 4 * h, at + kValueBytes + 512 * h);
+                        exponents_to_tmem(eb + 4 * h, at + kTileBytes + kValueBytes + 512 * h);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        multiply(acc, operand(at + 32 * k, 1024, true), operand(at + kTileBytes + 32 * k, 1024, true), n, k & 1,
+                                 ea + 4 * (k >> 1), eb + 4 * (k >> 1), c > 0 || k > 0);
+                    commit(&s_empty[stage]);
+                    if (++stage == kStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+                commit(&s_sums[buffer]);
+                buffer ^= 1;
+                taken ^= buffer == 0;
+            }
+        }
+    } else {
+        const int quarter = warp & 3;                            // the lanes of the tensor memory that this warp can read
+        int buffer = 0;
+        uint32_t phase = 0;
+        for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
+            const Item it = item_of(i, f_tiles, experts, s_first);
+            if (!bar_wait(&s_sums[buffer], phase, &s_gave_up)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            __syncwarp();
+            const int64_t f = (int64_t)it.f * kTileRows + quarter * 32 + lane;
+            T* out = y + it.row0 * ld + f;
+            for (int c0 = 0; c0 < it.rows; c0 += 32) {
+                uint32_t v[32];
+                const uint32_t from = tmem + buffer * kAccCols + c0 + ((uint32_t)(quarter * 32) << 16);
+                asm volatile(
+                    "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                    "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                    : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+                      "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+                      "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+                      "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+                    : "r"(from)
+                    : "memory");
+                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                if (f < outputs) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (c0 + k < it.rows) out[(int64_t)(c0 + k) * ld] = from_float<T>(__uint_as_float(v[k]));
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bar_arrive(&s_taken[buffer]);
+            if (f < outputs)
+                for (int64_t p = 0; p < it.pad; ++p) out[(it.rows + p) * ld] = from_float<T>(0.f);
+            buffer ^= 1;
+            phase ^= buffer == 0;
+        }
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (s_gave_up) {
+        // (copies and products that are still on their way get some time to end)
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);
+        if (threadIdx.x == 0) *status = HL_ETIMEOUT;
+        __syncthreads();
+    }
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
+// ---- arguments ------------------------------------------------------------------------------------------------------------
+constexpr int kSMs = 148;              // grids are made for a B200's multiprocessors
+int64_t tiles_of(int64_t n, int per) { return div_up(n, per); }
+bool matrix_dims_ok(int64_t rows, int64_t dim) { return rows >= 0 && rows < (int64_t(1) << 31) && dim >= 1 && dim <= (int64_t(1) << 24); }
+
+constexpr int64_t kWorkspaceHead = 1024;
+int64_t row_tiles_most(int64_t cap_rows, int64_t E) { return cap_rows / kTileRows + (E < cap_rows ? E : cap_rows); }
+
+template <typename T>
+int32_t launch_quantise(int64_t n, int64_t rows, int64_t dim, const void* x, int64_t ld, int64_t stride, void* q, bool whole,
+                        cudaStream_t stream) {
+    constexpr int U = 4;
+    const int64_t rt = tiles_of(rows, kTileRows), ct = tiles_of(dim, kTileCols), parts = n * rt * kTileRows * ct;
+    const int64_t ctas = div_up(parts, kRowNT / 32 * U);
+    if (ctas > 0x7fffffff) return HL_EINVAL;
+    HL_CUDA_TRY(launch(whole ? k_mx4_quantise<T, true, U> : k_mx4_quantise<T, false, U>, (unsigned)ctas, kRowNT, stream,
+                       static_cast<const T*>(x), rows, dim, ld, stride, rt, ct, parts, static_cast<uint8_t*>(q)));
+    note_launches(1);
+    HL_LAUNCH_CHECK();
+    return HL_OK;
+}
+template <typename T>
+int32_t launch_dequantise(int64_t n, int64_t rows, int64_t dim, const void* q, void* out, int64_t ld, int64_t stride, bool whole,
+                          cudaStream_t stream) {
+    constexpr int U = 4;
+    const int64_t rt = tiles_of(rows, kTileRows), ct = tiles_of(dim, kTileCols), parts = n * rows * ct;
+    const int64_t ctas = div_up(parts, kRowNT / 32 * U);
+    if (ctas > 0x7fffffff) return HL_EINVAL;
+    HL_CUDA_TRY(launch(whole ? k_mx4_dequantise<T, true, U> : k_mx4_dequantise<T, false, U>, (unsigned)ctas, kRowNT, stream,
+                       static_cast<const uint8_t*>(q), rows, dim, rt, ct, parts, static_cast<T*>(out), ld, stride));
+    note_launches(1);
+    HL_LAUNCH_CHECK();
+    return HL_OK;
+}
+template <typename T>
+int32_t launch_product(const hl_route* r, int64_t dim, int64_t outputs, const void* x, int64_t ld_x, bool by_token, const void* w,
+                       void* y, int64_t ld_y, void* workspace, bool whole, cudaStream_t stream) {
+    int32_t* status = static_cast<int32_t*>(workspace);
+    uint8_t* q = static_cast<uint8_t*>(workspace) + kWorkspaceHead;
+    const int64_t ct = tiles_of(dim, kTileCols), ft = tiles_of(outputs, kTileRows), rt = row_tiles_most(r->cap_rows, r->n_experts);
+    const int64_t rows = by_token ? r->max_tokens : r->cap_rows;
+    HL_CUDA_TRY(launch(whole ? k_mx4_rows<T, true> : k_mx4_rows<T, false>, grid_for(rows * ct, kRowNT / 32, 8 * kSMs), kRowNT, stream,
+                       static_cast<const T*>(x), ld_x, dim, ct, r->n_tokens, rows, by_token ? r->top_k : 0, r->place, r->counts,
+                       r->offsets, r->n_experts, r->cap_rows, rt, q, status));
+    note_launches(1);
+    const auto kernel = k_mx4_product<T>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem) != cudaSuccess) return HL_ECUDA;
+    HL_CUDA_TRY(launch_after(kernel, grid_for(rt * ft, 1, kSMs), kProductNT, kProductSmem, stream, (const uint8_t*)q,
+                             static_cast<const uint8_t*>(w), r->counts, r->offsets, r->n_experts, r->cap_rows, rt, ct, ft, outputs,
+                             static_cast<T*>(y), ld_y, status));
+    note_launches(1);
+    HL_LAUNCH_CHECK();
+    return HL_OK;
+}
+
+}  // namespace
+}  // namespace hl
+
+using namespace hl;
+
+#define HL_FOR_TYPE(CALL) (dtype == HL_F32 ? CALL(float) : dtype == HL_BF16 ? CALL(__nv_bfloat16) : CALL(__half))
+
+extern "C" size_t hl_mx4_bytes(int64_t rows, int64_t dim) {
+    if (!matrix_dims_ok(rows, dim)) return 0;
+    return (size_t)(tiles_of(rows, kTileRows) * tiles_of(dim, kTileCols) * kTileBytes);
+}
+
+extern "C" int32_t hl_mx4_quantise(int32_t dtype, int64_t n_matrices, int64_t rows, int64_t dim, const void* d_x, int64_t ld,
+                                   int64_t stride, void* d_q, void* stream_) {
+    const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (!matrix_dims_ok(rows, dim) || n_matrices < 0 || n_matrices >= (int64_t(1) << 31) || !row_matrix_ok(dtype, rows * n_matrices, dim, d_x, ld) ||
+        stride < 0 || (!d_q && rows * n_matrices > 0) || !lies_at(d_q, 16))
+        return HL_EINVAL;
+    if (rows == 0 || n_matrices == 0) return HL_OK;
+    if (n_matrices == 1) stride = 0;
+    const bool whole = dim % 8 == 0 && rows_lie_at(dtype, d_x, ld, 16) && rows_lie_at(dtype, d_x, stride, 16);
+#define HL_QUANTISE(T) launch_quantise<T>(n_matrices, rows, dim, d_x, ld, stride, d_q, whole, stream)
+    return HL_FOR_TYPE(HL_QUANTISE);
+#undef HL_QUANTISE
+}
+
+extern "C" int32_t hl_mx4_dequantise(int64_t n_matrices, int64_t rows, int64_t dim, const void* d_q, int32_t dtype, void* d_out,
+                                     int64_t ld, int64_t stride, void* stream_) {
+    const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (!matrix_dims_ok(rows, dim) || n_matrices < 0 || n_matrices >= (int64_t(1) << 31) ||
+        !row_matrix_ok(dtype, rows * n_matrices, dim, d_out, ld) || stride < 0 || (!d_q && rows * n_matrices > 0) || !lies_at(d_q, 16))
+        return HL_EINVAL;
+    if (rows == 0 || n_matrices == 0) return HL_OK;
+    if (n_matrices == 1) stride = 0;
+    const bool whole = dim % 8 == 0 && rows_lie_at(dtype, d_out, ld, 16) && rows_lie_at(dtype, d_out, stride, 16);
+#define HL_DEQUANTISE(T) launch_dequantise<T>(n_matrices, rows, dim, d_q, d_out, ld, stride, whole, stream)
+    return HL_FOR_TYPE(HL_DEQUANTISE);
+#undef HL_DEQUANTISE
+}
+
+extern "C" size_t hl_expert_mx4_workspace_bytes(int64_t cap_rows, int32_t n_experts, int64_t dim) {
+    if (cap_rows < 0 || cap_rows >= (int64_t(1) << 31) - 65536 || n_experts < 1 || n_experts > HL_MAX_EXPERTS || dim < 1 ||
+        dim > (int64_t(1) << 24))
+        return 0;
+    return (size_t)(kWorkspaceHead + row_tiles_most(cap_rows, n_experts) * tiles_of(dim, kTileCols) * kTileBytes);
+}
+
+extern "C" int32_t hl_expert_mx4(const hl_route* route, int32_t dtype, int64_t dim, int64_t outputs, const void* d_x, int64_t ld_x,
+                                 int32_t by_token, const void* d_weights, void* d_y, int64_t ld_y, void* d_workspace, size_t ws_bytes,
+                                 void* stream_) {
+    const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const hl_route* r = route;
+    if (!r || !lies_at(r->n_tokens, 4) || !lies_at(r->place, 4) || !lies_at(r->counts, 4) || !lies_at(r->offsets, 4) ||
+        r->max_tokens < 0 || r->max_tokens >= (int64_t(1) << 30) || r->top_k < 1 || r->top_k > HL_MAX_TOP_K || r->n_experts < 1 ||
+        r->n_experts > HL_MAX_EXPERTS || r->max_tokens * r->top_k >= (int64_t(1) << 30) || r->cap_rows < 0 ||
+        r->cap_rows >= (int64_t(1) << 31) - 65536 || !r->counts || !r->offsets || (by_token && !r->place && r->max_tokens > 0))
+        return HL_EINVAL;
+    if (!row_matrix_ok(dtype, by_token ? r->max_tokens : r->cap_rows, dim, d_x, ld_x) || !row_matrix_ok(dtype, r->cap_rows, outputs, d_y, ld_y) ||
+        !d_weights || !lies_at(d_weights, 16) || !d_workspace || !lies_at(d_workspace, 256))
+        return HL_EINVAL;
+    if (ws_bytes < hl_expert_mx4_workspace_bytes(r->cap_rows, r->n_experts, dim)) return HL_ECAPACITY;
+    if (r->cap_rows == 0) return HL_OK;
+    const bool whole = dim % 8 == 0 && rows_lie_at(dtype, d_x, ld_x, 16);
+#define HL_PRODUCT(T) launch_product<T>(r, dim, outputs, d_x, ld_x, by_token != 0, d_weights, d_y, ld_y, d_workspace, whole, stream)
+    return HL_FOR_TYPE(HL_PRODUCT);
+#undef HL_PRODUCT
+}

@@ -1,0 +1,436 @@
+// A token embedding: the scaled rows of tokens, and the gradient of the table, summed over the tokens of a row.
+#include <math.h>
+
+#include "hl_rows.cuh"
+
+namespace hl {
+namespace {
+
+constexpr int kNT = 256;
+
+__device__ __forceinline__ int64_t live_tokens(const int32_t* n_tokens, int64_t max_tokens) {
+    return n_tokens ? min((int64_t)max(__ldg(n_tokens), 0), max_tokens) : max_tokens;
+}
+
+// ---- rows of tokens ---------------------------------------------------------------------------------------------------
+// out[i] = scale * table[tokens[i]], W values at a time, U of them a thread, dealt out in turn over the rows.  Bound by memory.
+// (item / vectors: by 2^64 / vectors, rounded up; exact for less than 2^40 items and rows of less than 2^24 vectors)
+template <typename TT, typename TO, int W, int U>
+__global__ void __launch_bounds__(kNT) k_token_embed(const TT* __restrict__ table, int64_t ld_table, unsigned n_rows,
+                                                     const int32_t* __restrict__ tokens, int64_t max_tokens, const int32_t* n_tokens,
+                                                     float scale, TO* __restrict__ out, int64_t ld_out, int vectors,
+                                                     unsigned long long inverse, int32_t* status) {
+    const int64_t n = live_tokens(n_tokens, max_tokens), first = (int64_t)blockIdx.x * (kNT * U) + threadIdx.x;
+    int64_t at[U];
+    int column[U], token[U];
+    Pack<TT, W> in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const unsigned long long item = first + u * kNT;
+        at[u] = vectors == 1 ? item : __umul64hi(item, inverse);
+        column[u] = (int)(item - at[u] * vectors) * W;
+        token[u] = at[u] < n ? __ldg(&tokens[at[u]]) : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        in[u].zero();
+        if ((unsigned)token[u] < n_rows) in[u].load(table + token[u] * ld_table + column[u]);
+        else if (token[u] != -1 && status) set_status(status, HL_EBOUNDS);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (at[u] >= n) continue;
+        float x[W];
+        in[u].get(x);
+        const bool there = (unsigned)token[u] < n_rows;
+#pragma unroll
+        for (int i = 0; i < W; ++i) x[i] = there ? x[i] * scale : 0.f;
+        Pack<TO, W> v;
+        v.set(x);
+        v.store(out + at[u] * ld_out + column[u]);
+    }
+}
+
+// ---- the sort -----------------------------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(kNT) k_token_pairs(const int32_t* __restrict__ tokens, int64_t max_tokens, const int32_t* n_tokens,
+                                                     int n_rows, int32_t* __restrict__ keys, int32_t* __restrict__ vals,
+                                                     int32_t* n_out, int32_t* status) {
+    const int64_t n = live_tokens(n_tokens, max_tokens);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *n_out = (int32_t)n;
+    for (int64_t i = (int64_t)blockIdx.x * kNT + threadIdx.x; i < n; i += (int64_t)gridDim.x * kNT) {
+        const int t = __ldg(&tokens[i]);
+        const bool row = (unsigned)t < (unsigned)n_rows;
+        if (!row && t != -1) set_status(status, HL_EBOUNDS);
+        keys[i] = row ? t : n_rows;
+        vals[i] = (int32_t)i;
+    }
+}
+
+// ---- the table's gradient -------------------------------------------------------------------------------------------------
+// The sorted tokens are cut into windows of `window`.  A group of P threads takes one, its columns W * C a thread, and adds up the
+// gradients of each run of equal tokens.  A run inside the window goes to its row; of one that begins before the window or goes on
+// behind it only a piece is known, which goes to memory: piece 2w is that of the run which began before window w, 2w + 1 that of the
+// one that begins in it and goes on.  A second kernel adds the pieces of such a run up, in their order.
+struct Grads {
+    const int32_t *sorted, *order;
+    int64_t n;
+    int n_rows;
+};
+
+// first place in sorted[lo, hi) whose token is not below u
+__device__ __forceinline__ int64_t not_below(const int32_t* __restrict__ sorted, int64_t lo, int64_t hi, int u) {
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (__ldg(&sorted[mid]) < u) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+template <typename TT, int W>
+__device__ __forceinline__ void put(TT* row, const float (&sum)[W], float scale, bool accumulate) {
+    float x[W];
+    Pack<TT, W> v;
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] = scale * sum[i];
+    if (accumulate) {
+        float old[W];
+        v.load(row);
+        v.get(old);
+#pragma unroll
+        for (int i = 0; i < W; ++i) x[i] += old[i];
+    }
+    v.set(x);
+    v.store(row);
+}
+
+// rows [first, last) that no token names become zeros
+template <typename TT, int W>
+__device__ void zero_rows(const Grads& g, int64_t first, int64_t last, int dim, TT* __restrict__ table, int64_t ld) {
+    __shared__ uint32_t s_there[kNT / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Pack<TT, W> zero;
+    zero.zero();
+    const int vectors = dim / W;
+    for (int64_t r0 = first; r0 < last; r0 += kNT) {
+        const int64_t r = r0 + threadIdx.x;
+        bool there = true;
+        if (r < last) {
+            const int64_t at = not_below(g.sorted, 0, g.n, (int)r);
+            there = at < g.n && __ldg(&g.sorted[at]) == (int)r;
+        }
+        const uint32_t word = __ballot_sync(0xffffffffu, there);
+        if (lane == 0) s_there[warp] = word;
+        __syncthreads();
+        const int rows = (int)min((int64_t)kNT, last - r0);
+        if (vectors >= kNT / 2) {
+            for (int k = 0; k < rows; ++k) {
+                if ((s_there[k >> 5] >> (k & 31)) & 1u) continue;
+                for (int c = threadIdx.x; c < vectors; c += kNT) zero.store(table + (r0 + k) * ld + (int64_t)c * W);
+            }
+        } else {
+            for (int k = warp; k < rows; k += kNT / 32) {
+                if ((s_there[k >> 5] >> (k & 31)) & 1u) continue;
+                for (int c = lane; c < vectors; c += 32) zero.store(table + (r0 + k) * ld + (int64_t)c * W);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <typename TG, typename TT, int W, int C, int U>
+__global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ sorted, const int32_t* __restrict__ order,
+                                                    int64_t max_tokens, const int32_t* n_tokens, int n_rows, int dim,
+                                                    const TG* __restrict__ grad, int64_t ld_grad, float scale,
+                                                    TT* __restrict__ table, int64_t ld_table, int accumulate, int window, int P,
+                                                    int sum_ctas, int rows_per_cta, float* __restrict__ pieces) {
+    let_next_start();
+    const Grads g{sorted, order, live_tokens(n_tokens, max_tokens), n_rows};
+    if ((int)blockIdx.x >= sum_ctas) {
+        if (blockIdx.y) return;
+        const int64_t first = (int64_t)(blockIdx.x - sum_ctas) * rows_per_cta;
+        zero_rows<TT, W>(g, first, min(first + rows_per_cta, (int64_t)n_rows), dim, table, ld_table);
+        return;
+    }
+    const int sub = threadIdx.x & (P - 1);
+    const int64_t w = (int64_t)blockIdx.x * (kNT / P) + threadIdx.x / P, begin = w * window, end = min(begin + window, g.n);
+    if (begin >= end) return;
+    const int c0 = (int)blockIdx.y * P * W * C + sub * W;
+    bool col[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) col[c] = c0 + c * P * W < dim;
+    if (!col[0]) return;
+    float sum[C][W] = {};
+    int run = __ldg(&sorted[begin]);
+    bool open = begin > 0 && __ldg(&sorted[begin - 1]) == run;             // began before the window
+    const auto flush = [&](bool goes_on) {
+        if ((unsigned)run < (unsigned)n_rows) {
+            if (open || goes_on) {
+                float* piece = pieces + (2 * w + (open ? 0 : 1)) * (int64_t)dim + c0;
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    if (col[c]) {
+                        Pack<float, W> v;
+                        v.set(sum[c]);
+                        v.store(piece + c * P * W);
+                    }
+            } else {
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    if (col[c]) put<TT, W>(table + run * ld_table + c0 + c * P * W, sum[c], scale, accumulate);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < W; ++i) sum[c][i] = 0.f;
+        open = false;
+    };
+    for (int64_t i0 = begin; i0 < end; i0 += U) {
+        int key[U], at[U];
+        Pack<TG, W> in[U][C];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            key[u] = i0 + u < end ? __ldg(&sorted[i0 + u]) : run;
+            at[u] = i0 + u < end ? __ldg(&order[i0 + u]) : -1;
+            if ((unsigned)key[u] >= (unsigned)n_rows || at[u] >= g.n) at[u] = -1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                in[u][c].zero();
+                if (at[u] >= 0 && col[c]) in[u][c].load(grad + at[u] * ld_grad + c0 + c * P * W);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u >= end) break;
+            if (key[u] != run) {
+                flush(false);
+                run = key[u];
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float x[W];
+                in[u][c].get(x);
+#pragma unroll
+                for (int i = 0; i < W; ++i) sum[c][i] += x[i];
+            }
+        }
+    }
+    flush(end < g.n && __ldg(&sorted[end]) == run);
+}
+
+// Runs over several windows: their pieces, by the CTA of the window where they begin.  Its groups of P threads take a part of the
+// pieces each, in order, and the parts are added up in order.
+template <typename TT, int W, int C>
+__global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__ sorted, int64_t max_tokens, const int32_t* n_tokens,
+                                                     int n_rows, int dim, float scale, TT* __restrict__ table, int64_t ld_table,
+                                                     int accumulate, int window, int P, const float* __restrict__ pieces) {
+    extern __shared__ float s_sum[];                             // [kNT / P][P * W * C]
+    wait_for_last();
+    const int64_t n = live_tokens(n_tokens, max_tokens), w = blockIdx.x, end = (w + 1) * window;
+    if (end >= n) return;
+    const int run = __ldg(&sorted[end]);
+    if (run != __ldg(&sorted[end - 1]) || (unsigned)run >= (unsigned)n_rows) return;
+    const int64_t begin = w * window;
+    if (begin > 0 && __ldg(&sorted[begin - 1]) == run) return;   // (it began before: another CTA's)
+    // the window with the run's last token
+    int64_t lo = end, hi = n;
+    for (int64_t step = window; lo + step < n; step *= 2)
+        if (__ldg(&sorted[lo + step]) == run) lo += step;
+        else {
+            hi = lo + step;
+            break;
+        }
+    const int64_t last = (not_below(sorted, lo, hi, run + 1) - 1) / window;
+    const int sub = threadIdx.x & (P - 1), side = threadIdx.x / P, sides = kNT / P;
+    const int c0 = (int)blockIdx.y * P * W * C + sub * W;
+    const int64_t all = last - w + 1, per = (all + sides - 1) / sides, p0 = min(side * per, all), p1 = min(p0 + per, all);
+    float sum[C][W] = {};
+    constexpr int U = 4;
+    for (int64_t p = p0; p < p1; p += U) {
+        Pack<float, W> in[U][C];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                in[u][c].zero();
+                if (p + u < p1 && c0 + c * P * W < dim)
+                    in[u][c].load(pieces + (2 * (w + p + u) + (p + u == 0 ? 1 : 0)) * (int64_t)dim + c0 + c * P * W);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float x[W];
+                in[u][c].get(x);
+#pragma unroll
+                for (int i = 0; i < W; ++i) sum[c][i] += x[i];
+            }
+    }
+    const int width = P * W * C;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < W; ++i) s_sum[side * width + (c * W + i) * P + sub] = sum[c][i];
+    __syncthreads();
+    if (side) return;
+    for (int s = 1; s < sides && s * per < all; ++s)
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < W; ++i) sum[c][i] += s_sum[s * width + (c * W + i) * P + sub];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (c0 + c * P * W < dim) put<TT, W>(table + run * ld_table + c0 + c * P * W, sum[c], scale, accumulate);
+}
+
+// ---- arguments ------------------------------------------------------------------------------------------------------------
+bool tokens_ok(int64_t max_tokens) { return max_tokens >= 0 && max_tokens < (int64_t(1) << 30); }
+unsigned long long inverse_of(int64_t vectors) { return vectors == 1 ? 0 : ~0ull / vectors + 1; }
+
+// tokens of a window: few enough to give every multiprocessor work, many where there are many, so that few runs are cut
+int window_of(int64_t max_tokens) { return max_tokens <= 65536 ? 32 : 128; }
+
+// the workspace: two words, and then what either call needs
+struct Workspace {
+    int32_t *n, *status, *keys, *vals;
+    uint32_t* hist;
+    float* pieces;
+};
+constexpr int64_t kWorkspaceHead = 256;
+int64_t padded(int64_t words) { return (words + 63) & ~int64_t(63); }
+Workspace layout(void* p, int64_t max_tokens) {
+    int32_t* base = static_cast<int32_t*>(p);
+    int32_t* body = base + kWorkspaceHead / 4;
+    return {base, base + 1, body, body + padded(max_tokens), reinterpret_cast<uint32_t*>(body + 2 * padded(max_tokens)),
+            reinterpret_cast<float*>(body)};
+}
+
+template <typename TT, typename TO>
+int32_t launch_embed(int64_t n_rows, int64_t dim, const void* table, int64_t ld_table, const int32_t* tokens, int64_t max_tokens,
+                     const int32_t* n_tokens, float scale, void* out, int64_t ld_out, int32_t* status, bool whole, cudaStream_t stream) {
+    constexpr int N = 8;               // (the 16 bytes of a 16-bit type)
+    const int64_t vectors = whole ? dim / N : dim, items = max_tokens * vectors, ctas = div_up(items, kNT * (whole ? 2 : 4));
+    if (ctas > 0x7fffffff || items >= (int64_t(1) << 40)) return HL_EINVAL;
+    HL_CUDA_TRY(launch(whole ? k_token_embed<TT, TO, N, 2> : k_token_embed<TT, TO, 1, 4>, (unsigned)ctas, kNT, stream,
+                       static_cast<const TT*>(table), ld_table, (unsigned)n_rows, tokens, max_tokens, n_tokens, scale,
+                       static_cast<TO*>(out), ld_out, (int)vectors, inverse_of(vectors), status));
+    note_launches(1);
+    HL_LAUNCH_CHECK();
+    return HL_OK;
+}
+
+template <typename TG, typename TT, int W, int C, int U>
+int32_t launch_sums(int64_t n_rows, int64_t dim, const int32_t* sorted, const int32_t* order, int64_t max_tokens,
+                    const int32_t* n_tokens, const void* grad, int64_t ld_grad, float scale, void* table, int64_t ld_table,
+                    int accumulate, float* pieces, cudaStream_t stream) {
+    int P = 1;
+    while (P < kNT && P * W * C < dim) P *= 2;
+    const int window = window_of(max_tokens);
+    const int64_t passes = div_up(dim, P * W * C), windows = div_up(max_tokens, window), sums = div_up(windows, kNT / P);
+    // rows without tokens: some 128 KB a CTA
+    int64_t per = (128 << 10) / (dim * (int64_t)sizeof(TT));
+    per = per < 1 ? 1 : per > kNT ? kNT : per;
+    const int64_t zeros = accumulate ? 0 : div_up(n_rows, per);
+    if (sums + zeros > 0x7fffffff || passes > 65535 || windows > 0x7fffffff) return HL_EINVAL;
+    if (sums + zeros == 0) return HL_OK;
+    HL_CUDA_TRY(launch(k_token_sums<TG, TT, W, C, U>, dim3((unsigned)(sums + zeros), (unsigned)passes), kNT, stream, sorted, order,
+                       max_tokens, n_tokens, (int)n_rows, (int)dim, static_cast<const TG*>(grad), ld_grad, scale,
+                       static_cast<TT*>(table), ld_table, accumulate, window, P, (int)sums, (int)per, pieces));
+    note_launches(1);
+    if (windows > 1) {
+        HL_CUDA_TRY(launch_after(k_token_joins<TT, W, C>, dim3((unsigned)(windows - 1), (unsigned)passes), kNT,
+                                 kNT * W * C * sizeof(float), stream, sorted, max_tokens, n_tokens, (int)n_rows, (int)dim, scale,
+                                 static_cast<TT*>(table), ld_table, accumulate, window, P, (const float*)pieces));
+        note_launches(1);
+    }
+    HL_LAUNCH_CHECK();
+    return HL_OK;
+}
+
+}  // namespace
+}  // namespace hl
+
+using namespace hl;
+
+extern "C" int32_t hl_token_embed(int32_t table_dtype, int64_t n_rows, int64_t dim, const void* d_table, int64_t ld_table,
+                                  const int32_t* d_tokens, int64_t max_tokens, const int32_t* d_n_tokens, float scale,
+                                  int32_t out_dtype, void* d_out, int64_t ld_out, int32_t* d_status, void* stream_) {
+    const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (n_rows < 0 || n_rows >= (int64_t(1) << 31) || !tokens_ok(max_tokens) || (!d_tokens && max_tokens > 0) ||
+        !row_matrix_ok(table_dtype, n_rows, dim, d_table, ld_table) || !row_matrix_ok(out_dtype, max_tokens, dim, d_out, ld_out) ||
+        !lies_at(d_tokens, 4) || !lies_at(d_n_tokens, 4) || !lies_at(d_status, 4))
+        return HL_EINVAL;
+    if (max_tokens == 0) return HL_OK;
+    const bool whole = dim % 8 == 0 && rows_lie_at(table_dtype, d_table, ld_table, 16) && rows_lie_at(out_dtype, d_out, ld_out, 16);
+#define HL_EMBED(TT, TO)                                                                                                       \
+    launch_embed<TT, TO>(n_rows, dim, d_table, ld_table, d_tokens, max_tokens, d_n_tokens, scale, d_out, ld_out, d_status, whole, \
+                         stream)
+#define HL_EMBED_TO(TT) (out_dtype == HL_F32 ? HL_EMBED(TT, float) : out_dtype == HL_BF16 ? HL_EMBED(TT, __nv_bfloat16) : HL_EMBED(TT, __half))
+    return table_dtype == HL_F32 ? HL_EMBED_TO(float) : table_dtype == HL_BF16 ? HL_EMBED_TO(__nv_bfloat16) : HL_EMBED_TO(__half);
+#undef HL_EMBED_TO
+#undef HL_EMBED
+}
+
+extern "C" size_t hl_token_workspace_bytes(int64_t max_tokens, int64_t dim) {
+    if (!tokens_ok(max_tokens) || dim < 1 || dim > (int64_t(1) << 24)) return 0;
+    const int64_t sort = (2 * padded(max_tokens) + padded(sort_hist_words(max_tokens))) * 4;
+    const int64_t sums = 2 * div_up(max_tokens, window_of(max_tokens)) * dim * 4;
+    return (size_t)(kWorkspaceHead + ((sort > sums ? sort : sums) + 255) / 256 * 256);
+}
+
+extern "C" int32_t hl_token_sort(const int32_t* d_tokens, int64_t max_tokens, const int32_t* d_n_tokens, int64_t n_rows,
+                                 int32_t* d_sorted, int32_t* d_order, int32_t* d_status, void* d_workspace, size_t ws_bytes,
+                                 void* stream_) {
+    const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (n_rows < 0 || n_rows >= (int64_t(1) << 31) || !tokens_ok(max_tokens) ||
+        (max_tokens > 0 && (!d_tokens || !d_sorted || !d_order)) || !lies_at(d_tokens, 4) || !lies_at(d_n_tokens, 4) ||
+        !lies_at(d_sorted, 4) || !lies_at(d_order, 4) || !lies_at(d_status, 4) || !d_workspace || !lies_at(d_workspace, 256))
+        return HL_EINVAL;
+    if (ws_bytes < hl_token_workspace_bytes(max_tokens, 1)) return HL_ECAPACITY;
+    if (max_tokens == 0) return HL_OK;
+    const Workspace ws = layout(d_workspace, max_tokens);
+    int bits = 1;
+    while ((n_rows >> bits) != 0) ++bits;
+    const int out = ((bits + 7) / 8) & 1;                        // which of the two buffers the sort ends in
+    int32_t *keys[2], *vals[2], *sorted, *order;
+    keys[out] = d_sorted;
+    vals[out] = d_order;
+    keys[out ^ 1] = ws.keys;
+    vals[out ^ 1] = ws.vals;
+    int32_t* status = d_status ? d_status : ws.status;
+    HL_CUDA_TRY(launch(k_token_pairs, grid_for(max_tokens, kNT, 2048), kNT, stream, d_tokens, max_tokens, d_n_tokens, (int)n_rows,
+                       keys[0], vals[0], ws.n, status));
+    note_launches(1);
+    return radix_sort_pairs(keys, vals, ws.n, max_tokens, bits, ws.hist, status, &sorted, &order, stream);
+}
+
+extern "C" int32_t hl_token_embed_bwd(int64_t n_rows, int64_t dim, const int32_t* d_sorted, const int32_t* d_order,
+                                      int64_t max_tokens, const int32_t* d_n_tokens, int32_t grad_dtype, const void* d_grad_out,
+                                      int64_t ld_grad, float scale, int32_t table_dtype, void* d_grad_table, int64_t ld_table,
+                                      int32_t accumulate, void* d_workspace, size_t ws_bytes, void* stream_) {
+    const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (n_rows < 0 || n_rows >= (int64_t(1) << 31) || !tokens_ok(max_tokens) || (max_tokens > 0 && (!d_sorted || !d_order)) ||
+        !row_matrix_ok(grad_dtype, max_tokens, dim, d_grad_out, ld_grad) ||
+        !row_matrix_ok(table_dtype, n_rows, dim, d_grad_table, ld_table) || !lies_at(d_sorted, 4) || !lies_at(d_order, 4) ||
+        !lies_at(d_n_tokens, 4) || !d_workspace || !lies_at(d_workspace, 256))
+        return HL_EINVAL;
+    if (ws_bytes < hl_token_workspace_bytes(max_tokens, dim)) return HL_ECAPACITY;
+    const int N = 16 / dtype_size(grad_dtype);
+    const bool whole = dim % N == 0 && rows_lie_at(grad_dtype, d_grad_out, ld_grad, 16) &&
+                       rows_lie_at(table_dtype, d_grad_table, ld_table, 8) &&
+                       (N * dtype_size(table_dtype) == 8 || rows_lie_at(table_dtype, d_grad_table, ld_table, 16));
+    float* pieces = layout(d_workspace, max_tokens).pieces;
+#define HL_SUMS(TG, TT)                                                                                                         \
+    (whole ? launch_sums<TG, TT, 16 / sizeof(TG), 1, 8>(n_rows, dim, d_sorted, d_order, max_tokens, d_n_tokens, d_grad_out, ld_grad, \
+                                                        scale, d_grad_table, ld_table, accumulate, pieces, stream)              \
+           : launch_sums<TG, TT, 1, 4, 8>(n_rows, dim, d_sorted, d_order, max_tokens, d_n_tokens, d_grad_out, ld_grad, scale,  \
+                                          d_grad_table, ld_table, accumulate, pieces, stream))
+#define HL_SUMS_TO(TG) \
+    (table_dtype == HL_F32 ? HL_SUMS(TG, float) : table_dtype == HL_BF16 ? HL_SUMS(TG, __nv_bfloat16) : HL_SUMS(TG, __half))
+    return grad_dtype == HL_F32 ? HL_SUMS_TO(float) : grad_dtype == HL_BF16 ? HL_SUMS_TO(__nv_bfloat16) : HL_SUMS_TO(__half);
+#undef HL_SUMS_TO
+#undef HL_SUMS
+}
