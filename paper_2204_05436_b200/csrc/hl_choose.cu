@@ -7,11 +7,10 @@ namespace hl {
 namespace {
 
 // ---- who is chosen ----------------------------------------------------------------------------------------------------
-// A token has P lanes of a warp (1 to 32), each of which holds ITEMS of its experts: lane q those with numbers q, q + P, ...
-// The choices are made one after the other: the largest key among a lane's, then over the lanes; a tie goes to the lowest
-// number.  Without a bias the key is the logit itself, which orders as the score does.  With one it is score + bias, and the
-// definition is in 64 bits; what decides is computed in 32, and a token for which it decides by less than 32 bits can tell
-// (kSure) is done again in 64: under one in a hundred of 256 experts whose logits are random.
+// A token has P lanes of a warp (1 to 32), each of which holds ITEMS of its experts side by side.  Without a bias an expert's key is
+// its logit, which orders as the score does.  With one it is score + bias, and the definition is in 64 bits; what decides is
+// computed in 32, and a token for which 32 bits cannot tell (kSure) is done again in 64: some one in a hundred of 256 experts
+// whose logits are random.
 template <int ITEMS, int P>
 struct Shape {
     static constexpr int kNT = 128;
@@ -20,32 +19,34 @@ struct Shape {
     static constexpr int kChosen = kExperts < HL_MAX_TOP_K ? kExperts : HL_MAX_TOP_K;
 };
 
-// |score in 32 bits - score| < 2^-18: exp is off by 2 ulp and by its argument's rounding, |x| e^x 2^-24 < 2^-25, a sum of up to
-// 32 + 5 of them one after the other by 37 * 2^-24 of it and theirs, the quotient by half an ulp; adding the bias rounds by 2^-24
+// |score in 32 bits - score| < 2^-18.  Of a sigmoid: s (1 - s) times the relative error of the exponential (2^-22 of the instruction's,
+// and its argument's roundings, |x| 2^-22; s (1 - s) |x| < 1/4), the sum's rounding and the inverse's 2^-23.  Of a softmax: the same with e^-|x| |x| < 0.37,
+// and the sum, of up to 32 + 5 terms one after the other: 37 * 2^-24 of it and its terms' errors.  Adding the bias rounds by 2^-24
 // of the key.  So keys further apart than 2^-17 (1 + |key|) are in order, and sums of two than twice that.
 constexpr float kSure = 0x1p-17f;
 
-// numbers in the order of the floats (which have no NaN among them, and no -0)
+// numbers in the order of the floats (which have no NaN among them; -0 is 0)
 __device__ __forceinline__ uint32_t ordered(float v) {
-    const uint32_t u = __float_as_uint(v);
+    const uint32_t u = __float_as_uint(v + 0.f);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
 
 constexpr int kNobody = 0x7fffffff;
+constexpr unsigned kAll = 0xffffffffu;
 
 // The largest key over a token's lanes, and the lowest number that has it.
 template <int P, typename Key>
 __device__ __forceinline__ void largest(Key& key, int& e) {
     if constexpr (P == 32 && sizeof(Key) == 4) {
-        const uint32_t u = ordered(key), all = __reduce_max_sync(0xffffffffu, u);
-        e = (int)__reduce_min_sync(0xffffffffu, u == all ? (unsigned)e : (unsigned)kNobody);
+        const uint32_t u = ordered(key), all = __reduce_max_sync(kAll, u);
+        e = (int)__reduce_min_sync(kAll, u == all ? (unsigned)e : (unsigned)kNobody);
         key = unordered(all);
     } else {
 #pragma unroll
         for (int d = P / 2; d > 0; d >>= 1) {
-            const Key k = __shfl_xor_sync(0xffffffffu, key, d);
-            const int x = __shfl_xor_sync(0xffffffffu, e, d);
+            const Key k = __shfl_xor_sync(kAll, key, d);
+            const int x = __shfl_xor_sync(kAll, e, d);
             if (k > key || (k == key && x < e)) {
                 key = k;
                 e = x;
@@ -56,21 +57,38 @@ __device__ __forceinline__ void largest(Key& key, int& e) {
 template <int P, typename V>
 __device__ __forceinline__ V sum_of(V v) {
 #pragma unroll
-    for (int d = P / 2; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    for (int d = P / 2; d > 0; d >>= 1) v += __shfl_xor_sync(kAll, v, d);
     return v;
 }
 template <int P>
 __device__ __forceinline__ float max_of(float v) {
 #pragma unroll
-    for (int d = P / 2; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    for (int d = P / 2; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, d));
     return v;
 }
+// a token's lanes among the warp's, as a mask
+template <int P>
+__device__ __forceinline__ unsigned lanes_of(int lane) { return P == 32 ? kAll : ((1u << (P & 31)) - 1u) << (lane & ~(P - 1) & 31); }
 
 __device__ __forceinline__ float sigmoid(float l) { return 1.f / (1.f + expf(-l)); }
 __device__ __forceinline__ double sigmoid(double l) { return 1.0 / (1.0 + exp(-l)); }
 // e^(l - m) for l <= m, where both may be infinite
 __device__ __forceinline__ float part(float l, float m) { return l == m ? 1.f : expf(l - m); }
 __device__ __forceinline__ double part(double l, double m) { return l == m ? 1.0 : exp(l - m); }
+// the same, as exact as choosing needs it (kSure): 2^x and 1 / x as the hardware has them
+__device__ __forceinline__ float near_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float near_inverse(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float near_sigmoid(float l) { return near_inverse(1.f + near_exp2(-kLog2e * l)); }
+__device__ __forceinline__ float near_part(float l, float m) { return l == m ? 1.f : near_exp2(kLog2e * (l - m)); }
 
 // what a call goes by
 struct Router {
@@ -79,53 +97,91 @@ struct Router {
     bool softmax, pair, renorm;
     __device__ __forceinline__ int group_of(int e) const { return (int)(((uint32_t)e * group_magic) >> 21); }
 };
-enum { kSoftmax = 1, kPair = 2, kRenorm = 4 };
+enum { kSoftmax = 1, kPair = 2, kRenorm = 4, kWholeLanes = 8 };
 
-// Keys of experts outside the groups that are kept become -inf.  `value` is what the groups are compared by, which is -inf for
-// experts that cannot be chosen.  Returns whether it was clear which.
-template <int ITEMS, int P, typename Key>
-__device__ bool keep_groups(const Router& r, const Key (&value)[ITEMS], Key (&key)[ITEMS], int q, Key* s_value, Key* s_group,
-                            Key* s_ranked) {
-    const Key none = -(Key)INFINITY;
-#pragma unroll
-    for (int j = 0; j < ITEMS; ++j)
-        if (j * P + q < r.E) s_value[j * P + q] = value[j];
-    __syncwarp();
-    for (int g = q; g < r.G; g += P) {
-        Key best = none, second = none;
-        int at = g % r.per_group;                                // (each lane begins elsewhere in its group, for the banks' sake)
-        for (int i = 0; i < r.per_group; ++i) {
-            const Key v = s_value[g * r.per_group + at];
-            second = v > best ? best : v > second ? v : second;
-            best = v > best ? v : best;
-            if (++at == r.per_group) at = 0;
-        }
-        if (r.pair && second > none) best += second;
-        s_group[g] = best;
-    }
-    __syncwarp();
-    for (int g = q; g < r.G; g += P) {
-        const Key v = s_group[g];
-        int rank = 0;
-        for (int i = 0; i < r.G; ++i) rank += s_group[i] > v || (s_group[i] == v && i < g);
-        s_ranked[rank] = v;
-        s_value[g] = rank < r.top_groups ? (Key)1 : (Key)0;      // (everybody has read the experts' values)
-    }
-    __syncwarp();
-#pragma unroll
-    for (int j = 0; j < ITEMS; ++j)
-        if (j * P + q < r.E && s_value[r.group_of(j * P + q)] == (Key)0) key[j] = none;
-    bool clear = true;
-    if (r.top_groups < r.G) {
-        const Key in = s_ranked[r.top_groups - 1], out = s_ranked[r.top_groups];
-        clear = out == none || in - out > (Key)(2 * kSure) * ((Key)1 + (in < 0 ? -in : in));
-    }
-    __syncwarp();
-    return clear;
+template <typename Key>
+__device__ __forceinline__ void two_best(Key v, Key& best, Key& second) {
+    second = v > best ? best : v > second ? v : second;
+    best = v > best ? v : best;
 }
 
-// The largest keys, in order: their experts go to s_e (-1: none left).  Where `check`, returns whether their order was clear;
-// same(a, b): two experts whose keys are equal by definition.
+// Keys of experts outside the groups that are kept become -inf.  `value` is what the groups are compared by, which is -inf for
+// experts that cannot be chosen.  Returns whether it was clear which.  whole_lanes: a group is that of 1, 2, 4 ... lanes, which then
+// find its two best between them; other groups go through shared memory (s: [E + 2 G]).
+template <int ITEMS, int P, typename Key>
+__device__ bool keep_groups(const Router& r, bool whole_lanes, const Key (&value)[ITEMS], Key (&key)[ITEMS], int q, Key* s) {
+    const Key none = -(Key)INFINITY;
+    Key in = none, out = none;
+    if (whole_lanes) {
+        const int lanes = r.per_group / ITEMS, lane = threadIdx.x & 31, first = lane & ~(P - 1), mine = q / lanes;
+        Key best = none, second = none;
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j) two_best(value[j], best, second);
+        for (int d = 1; d < lanes; d *= 2) {
+            const Key b = __shfl_xor_sync(kAll, best, d), c = __shfl_xor_sync(kAll, second, d);
+            second = b > best ? (best > c ? best : c) : (b > second ? b : second);
+            best = b > best ? b : best;
+        }
+        if (r.pair && second > none) best += second;
+        int rank = 0;
+        for (int g = 0; g < r.G; ++g) {
+            const Key v = __shfl_sync(kAll, best, first + g * lanes);
+            rank += v > best || (v == best && g < mine);
+        }
+        if (rank >= r.top_groups) {
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) key[j] = none;
+        }
+        if (r.top_groups < r.G) {
+            const unsigned us = lanes_of<P>(lane);
+            const unsigned i = __ballot_sync(kAll, rank == r.top_groups - 1) & us, o = __ballot_sync(kAll, rank == r.top_groups) & us;
+            in = __shfl_sync(kAll, best, __ffs(i) - 1);
+            out = __shfl_sync(kAll, best, __ffs(o) - 1);
+        }
+    } else {
+        Key *s_group = s + r.E, *s_ranked = s_group + r.G;
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j)
+            if (q * ITEMS + j < r.E) s[q * ITEMS + j] = value[j];
+        __syncwarp();
+        for (int g = q; g < r.G; g += P) {
+            Key best = none, second = none;
+            int at = g % r.per_group;                            // (each lane begins elsewhere in its group, for the banks' sake)
+            for (int i = 0; i < r.per_group; ++i) {
+                two_best(s[g * r.per_group + at], best, second);
+                if (++at == r.per_group) at = 0;
+            }
+            if (r.pair && second > none) best += second;
+            s_group[g] = best;
+        }
+        __syncwarp();
+        for (int g = q; g < r.G; g += P) {
+            const Key v = s_group[g];
+            int rank = 0;
+            for (int i = 0; i < r.G; ++i) rank += s_group[i] > v || (s_group[i] == v && i < g);
+            s_ranked[rank] = v;
+            s[g] = rank < r.top_groups ? (Key)1 : (Key)0;        // (everybody has read the experts' values)
+        }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j)
+            if (q * ITEMS + j < r.E && s[r.group_of(q * ITEMS + j)] == (Key)0) key[j] = none;
+        if (r.top_groups < r.G) {
+            in = s_ranked[r.top_groups - 1];
+            out = s_ranked[r.top_groups];
+        }
+        __syncwarp();
+    }
+    return out == none || in - out > (Key)(2 * kSure) * ((Key)1 + (in < 0 ? -in : in));
+}
+
+// Whether keys a >= b are in order for certain; a NaN (of infinite keys) says no.
+template <typename Key>
+__device__ __forceinline__ bool surely(Key a, Key b) { return a - b > (Key)kSure * ((Key)1 + (a < 0 ? -a : a)); }
+
+// The largest keys, in order: their experts go to s_e (-1: none left), one after the other -- the largest of a lane's, then over the
+// lanes; a tie goes to the lowest number.  Where `check`, returns whether their order was clear; same(a, b): two experts whose
+// keys are equal by definition.
 template <int ITEMS, int P, typename Key, typename Same>
 __device__ __forceinline__ bool choose(int top_k, Key (&key)[ITEMS], int q, bool check, int32_t* s_e, Same same) {
     const Key none = -(Key)INFINITY;
@@ -141,23 +197,84 @@ __device__ __forceinline__ bool choose(int top_k, Key (&key)[ITEMS], int q, bool
                 best = key[j];
                 j_best = j;
             }
-        int e = j_best * P + q;
+        int e = q * ITEMS + j_best;
         largest<P>(best, e);
         const bool any = best > none;
-        if (check && k > 0 && any && last_e >= 0 && !(last - best > (Key)kSure * ((Key)1 + (last < 0 ? -last : last))))
-            clear = clear && same(last_e, e);
+        if (check && k > 0 && any && last_e >= 0 && !surely(last, best)) clear = clear && same(last_e, e);
         last = best;
         last_e = any ? e : -1;
         if (k < top_k && q == 0) s_e[k] = last_e;
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j)
-            if (e == j * P + q) key[j] = none;
+            if (e == q * ITEMS + j) key[j] = none;
     }
     return clear;
 }
 
-// Bound by its instructions where there are many tokens: a choice takes a lane some 3 ITEMS of them, and the warp two reductions.
-template <typename T, int ITEMS, int P>
+// The same, all at once, for top_k < P: what is not below the (top_k + 1)-th largest of the lanes' largest keys is all that counts.
+// Those few, a lane each, are ranked by comparing each with all.  Returns false, with nothing done, if there are more than P of
+// them (equal keys, or few lanes with any).
+template <int ITEMS, int P, typename Same>
+__device__ __forceinline__ bool choose_few(int top_k, const float (&key)[ITEMS], int q, bool check, int32_t* s_e, float2* s_few,
+                                           bool* clear, Same same) {
+    const float none = -INFINITY;
+    const int lane = threadIdx.x & 31, first = lane & ~(P - 1);
+    float best = key[0];
+#pragma unroll
+    for (int j = 1; j < ITEMS; ++j) best = fmaxf(best, key[j]);
+    // the lanes' largest, in descending order
+#pragma unroll
+    for (int size = 2; size <= P; size *= 2)
+#pragma unroll
+        for (int d = size / 2; d > 0; d /= 2) {
+            const float other = __shfl_xor_sync(kAll, best, d);
+            const bool upper = ((q & d) != 0) != ((q & size) != 0 && size < P);
+            best = upper ? fminf(best, other) : fmaxf(best, other);
+        }
+    const float least = fmaxf(__shfl_sync(kAll, best, first + top_k), -3.402823466e38f);      // (not those that cannot be chosen)
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) mine += key[j] >= least;
+    int at = mine;
+#pragma unroll
+    for (int d = 1; d < P; d *= 2) {
+        const int v = __shfl_up_sync(kAll, at, d, P);
+        if (q >= d) at += v;
+    }
+    const int few = __shfl_sync(kAll, at, first + P - 1);
+    if (__any_sync(kAll, few > P)) return false;
+    at -= mine;
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j)
+        if (key[j] >= least) s_few[at++] = make_float2(key[j], __int_as_float(q * ITEMS + j));
+    __syncwarp();
+    float2 me = make_float2(none, __int_as_float(-1));
+    if (q < few) me = s_few[q];
+    int rank = 0;                      // (they lie in the order of their numbers)
+    const int most = P == 32 ? few : (int)__reduce_max_sync(kAll, (unsigned)few);
+#pragma unroll 4
+    for (int i = 0; i < most; ++i) {
+        const float v = __shfl_sync(kAll, me.x, first + i);
+        rank += v > me.x || (v == me.x && i < q);
+    }
+    if (q < few && rank < top_k) s_e[rank] = __float_as_int(me.y);
+    if (q >= few && q < top_k) s_e[q] = -1;
+    if (check) {
+        __syncwarp();
+        if (q < few) s_few[rank] = me;
+        __syncwarp();
+        bool mine_clear = true;
+        if (q > 0 && q < few && q <= top_k) {
+            const float2 a = s_few[q - 1], b = s_few[q];
+            if (!surely(a.x, b.x)) mine_clear = same(__float_as_int(a.y), __float_as_int(b.y));
+        }
+        *clear = (__ballot_sync(kAll, !mine_clear) & lanes_of<P>(lane)) == 0;
+    }
+    return true;
+}
+
+// Bound by its instructions where there are many tokens.  WHOLE: rows are read in pieces of 16 bytes.
+template <typename T, int ITEMS, int P, bool WHOLE>
 __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT) k_expert_choose(const T* __restrict__ logits, int64_t ld,
                                                                         const float* __restrict__ bias, const int32_t* n_tokens,
                                                                         int64_t max_tokens, int top_k, int E, int G, int top_groups,
@@ -165,9 +282,11 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT) k_expert_choose(const T*
                                                                         float* __restrict__ weights, int32_t* status) {
     using S = Shape<ITEMS, P>;
     __shared__ int32_t s_chosen[S::kTokens][S::kChosen];
-    extern __shared__ double s_base[];                           // with groups, of every token: [E] values, [2][G] groups
+    __shared__ float2 s_few[P >= 16 ? S::kNT : 1];
+    extern __shared__ double s_base[];                           // with groups that are not whole lanes', of every token: [E + 2 G]
     const Router r{top_k, E, G, E / G, top_groups, ((1u << 21) + E / G - 1) / (unsigned)(E / G), (flags & kSoftmax) != 0,
                    (flags & kPair) != 0, (flags & kRenorm) != 0};
+    const bool whole_lanes = flags & kWholeLanes;
     const int q = threadIdx.x % P, mine = threadIdx.x / P;
     int64_t tokens = max_tokens;
     if (n_tokens) tokens = min((int64_t)max(__ldg(n_tokens), 0), max_tokens);
@@ -176,14 +295,32 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT) k_expert_choose(const T*
     const bool live = t < tokens;
     const T* row = logits + (live ? t : tokens - 1) * ld;
     int32_t* s_e = s_chosen[mine];
-    double* s_value = s_base + mine * (E + 2 * G);
+    double* s_value = s_base + (whole_lanes ? 0 : mine * (E + 2 * G));
     float* s_value32 = reinterpret_cast<float*>(s_value);
     const float none = -INFINITY;
+    const int e0 = q * ITEMS;
 
     float l[ITEMS];
     bool bad = false;
+    if constexpr (WHOLE) {
+        constexpr int N = 16 / sizeof(T);
+        Pack<T, N> in[ITEMS / N];
 #pragma unroll
-    for (int j = 0; j < ITEMS; ++j) l[j] = j * P + q < E ? as_float(row[j * P + q]) + 0.f : none;     // (-0 becomes +0)
+        for (int i = 0; i < ITEMS / N; ++i) {
+            in[i].zero();
+            if (e0 + i * N < E) in[i].load(row + e0 + i * N);
+        }
+#pragma unroll
+        for (int i = 0; i < ITEMS / N; ++i) {
+            float x[N];
+            in[i].get(x);
+#pragma unroll
+            for (int k = 0; k < N; ++k) l[i * N + k] = e0 + i * N < E ? x[k] : none;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j) l[j] = e0 + j < E ? as_float(row[e0 + j]) : none;
+    }
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j)
         if (l[j] != l[j]) {
@@ -209,73 +346,99 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT) k_expert_choose(const T*
         for (int j = 0; j < ITEMS; ++j) key[j] = l[j];
         if (scores) {
             float value[ITEMS];
+            if (r.softmax) {
+                const float per = near_inverse(z);
 #pragma unroll
-            for (int j = 0; j < ITEMS; ++j) {
-                value[j] = none;
-                if (l[j] > none) {
-                    value[j] = r.softmax ? part(l[j], top) / z : sigmoid(l[j]);
-                    if (bias) {
-                        value[j] += __ldg(&bias[j * P + q]) + 0.f;
-                        if (value[j] != value[j]) {
-                            bad = true;
-                            value[j] = none;
-                        }
-                        key[j] = value[j];
+                for (int j = 0; j < ITEMS; ++j) value[j] = near_part(l[j], top) * per;
+            } else {
+#pragma unroll
+                for (int j = 0; j < ITEMS; ++j) value[j] = near_sigmoid(l[j]);
+            }
+            if (bias) {
+                if constexpr (WHOLE) {
+#pragma unroll
+                    for (int i = 0; i < ITEMS / 4; ++i) {
+                        Pack<float, 4> in;
+                        float x[4];
+                        in.zero();
+                        if (e0 + i * 4 < E) in.load(bias + e0 + i * 4);
+                        in.get(x);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) value[4 * i + k] += x[k];
                     }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < ITEMS; ++j)
+                        if (e0 + j < E) value[j] += __ldg(&bias[e0 + j]);
                 }
             }
-            if (G > 1)
-                clear = keep_groups<ITEMS, P>(r, value, key, q, s_value32, s_value32 + E, s_value32 + E + G);
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) {
+                const bool there = l[j] > none;
+                bad = bad || (there && value[j] != value[j]);
+                value[j] = there && value[j] == value[j] ? value[j] : none;
+                if (bias) key[j] = value[j];
+            }
+            if (G > 1) clear = keep_groups<ITEMS, P>(r, whole_lanes, value, key, q, s_value32);
         } else if (G > 1) {
-            keep_groups<ITEMS, P>(r, l, key, q, s_value32, s_value32 + E, s_value32 + E + G);
+            keep_groups<ITEMS, P>(r, whole_lanes, l, key, q, s_value32);
         }
-        clear &= choose<ITEMS, P>(top_k, key, q, bias != nullptr, s_e, [&](int a, int b) {
-            return as_float(row[a]) == as_float(row[b]) && __ldg(&bias[a]) == __ldg(&bias[b]);
-        });
+        const auto same = [&](int a, int b) { return as_float(row[a]) == as_float(row[b]) && __ldg(&bias[a]) == __ldg(&bias[b]); };
+        const bool check = bias != nullptr;
+        bool done = false, in_order = true;
+        if constexpr (P >= 16)
+            if (top_k < P) done = choose_few<ITEMS, P>(top_k, key, q, check, s_e, s_few + mine * P, &in_order, same);
+        if (!done) in_order = choose<ITEMS, P>(top_k, key, q, check, s_e, same);
+        clear = clear && in_order;
     }
-    if (__any_sync(0xffffffffu, scores && live && !clear)) {     // (all tokens of the warp once more)
+    if (__any_sync(kAll, scores && live && !clear)) {            // (all tokens of the warp once more)
         const double none64 = -(double)INFINITY;
-        double key[ITEMS], z64 = 0.0;
+        double key[ITEMS], value[ITEMS], z64 = 0.0;
         if (r.softmax) {
 #pragma unroll
             for (int j = 0; j < ITEMS; ++j) z64 += l[j] > none ? part((double)l[j], (double)top) : 0.0;
             z64 = sum_of<P>(z64);
         }
-        double value[ITEMS];
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j) {
             key[j] = value[j] = none64;
             if (l[j] > none) {
                 value[j] = r.softmax ? part((double)l[j], (double)top) / z64 : sigmoid((double)l[j]);
                 if (bias) {
-                    value[j] += (double)__ldg(&bias[j * P + q]);
+                    value[j] += (double)__ldg(&bias[e0 + j]);
                     if (value[j] != value[j]) value[j] = none64;
                 }
                 key[j] = bias ? value[j] : (double)l[j];
             }
         }
         __syncwarp();
-        if (G > 1) keep_groups<ITEMS, P>(r, value, key, q, s_value, s_value + E, s_value + E + G);
+        if (G > 1) keep_groups<ITEMS, P>(r, whole_lanes, value, key, q, s_value);
         choose<ITEMS, P>(top_k, key, q, false, s_e, [](int, int) { return true; });
     }
-    if (status && __any_sync(0xffffffffu, bad && live) && (threadIdx.x & 31) == 0) set_status(status, HL_EINVAL);
+    if (status && __any_sync(kAll, bad && live) && (threadIdx.x & 31) == 0) set_status(status, HL_EINVAL);
     __syncwarp();
 
     // Weights.  With the sum of the chosen scores below, only their ratios count: all are taken relative to e^m, m the largest of
     // the logits, so that none is lost to underflow (of sigmoids: min(m, 0), as that of a positive logit is 1/2 and more).
-    float m = none, sum = 0.f;
-    for (int k = q; k < top_k; k += P)
-        if (s_e[k] >= 0) m = fmaxf(m, as_float(row[s_e[k]]) + 0.f);
+    float m = none, sum = 0.f, mine_x = none, mine_w = 0.f;      // (of the lane's first choice, which is all it has as a rule)
+    for (int k = q; k < top_k; k += P) {
+        const float x = s_e[k] >= 0 ? as_float(row[s_e[k]]) : none;
+        if (k == q) mine_x = x;
+        m = fmaxf(m, x);
+    }
     m = max_of<P>(m);
     if (!r.softmax) m = r.renorm ? fminf(m, 0.f) : 0.f;
     else if (!r.renorm) m = top;
     const auto weight = [&](float x) {
         if (r.softmax) return part(x, m);
-        return x > 0.f ? sigmoid(x) : part(x, m) / (1.f + expf(x));
+        const float e = expf(x > 0.f ? -x : x);
+        return (x > 0.f ? 1.f : m == 0.f ? e : part(x, m)) / (1.f + e);
     };
+    if (mine_x > none) mine_w = weight(mine_x);
     if (r.renorm) {
-        for (int k = q; k < top_k; k += P)
-            if (s_e[k] >= 0) sum += weight(as_float(row[s_e[k]]) + 0.f);
+        sum = mine_w;
+        for (int k = q + P; k < top_k; k += P)
+            if (s_e[k] >= 0) sum += weight(as_float(row[s_e[k]]));
         sum = sum_of<P>(sum);
     } else {
         sum = r.softmax ? z : 1.f;
@@ -284,49 +447,54 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT) k_expert_choose(const T*
     for (int k = q; k < top_k; k += P) {
         const int e = s_e[k];
         experts[t * top_k + k] = e;
-        weights[t * top_k + k] = e < 0 ? 0.f : scale * (weight(as_float(row[e]) + 0.f) / sum);
+        weights[t * top_k + k] = e < 0 ? 0.f : scale * ((k == q ? mine_w : weight(as_float(row[e]))) / sum);
     }
 }
 
 // ---- the logits' gradient -----------------------------------------------------------------------------------------------
-// Of the scores' sum over a token only what the chosen experts contribute depends on k: every expert's gradient is
-// -c * score of it (softmax without the sum of the chosen below; 0 otherwise), the chosen ones' are written over it.  Bound by
-// writing the rows.
-template <typename T, int ITEMS, int P>
-__global__ void __launch_bounds__(Shape<ITEMS, P>::kNT) k_expert_choose_bwd(const T* __restrict__ logits, int64_t ld,
-                                                                            const int32_t* n_tokens, int64_t max_tokens, int top_k,
-                                                                            int E, int flags, float scale,
-                                                                            const int32_t* __restrict__ experts,
-                                                                            const float* __restrict__ grad_w, T* __restrict__ grad,
-                                                                            int64_t ld_grad) {
-    using S = Shape<ITEMS, P>;
-    __shared__ int32_t s_chosen[S::kTokens][S::kChosen];
-    __shared__ float s_grad[S::kTokens][S::kChosen];
-    const bool softmax = flags & kSoftmax, renorm = flags & kRenorm;
+// Only the chosen experts' gradients depend on the weights' one by one.  Every expert's is -mean * score of it in a softmax without the
+// sum of the chosen below, 0 otherwise; the chosen ones' are written over it.  P lanes of a warp for a token.  Bound by writing
+// the rows.  N values of a row at a time: 16 bytes, or one.
+template <typename T, int P, bool WHOLE>
+__global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__ logits, int64_t ld, const int32_t* n_tokens,
+                                                           int64_t max_tokens, int top_k, int E, int flags, float scale,
+                                                           const int32_t* __restrict__ experts, const float* __restrict__ grad_w,
+                                                           T* __restrict__ grad, int64_t ld_grad) {
+    constexpr int kTokens = 128 / P, N = WHOLE ? 16 / (int)sizeof(T) : 1;
+    constexpr int kChosen = P == 2 ? 16 : HL_MAX_TOP_K;          // (two lanes: of up to 16 experts)
+    __shared__ int32_t s_chosen[kTokens][kChosen];
+    __shared__ float s_grad[kTokens][kChosen];
+    const bool softmax = flags & kSoftmax, renorm = flags & kRenorm, dense = softmax && !renorm;
     const int q = threadIdx.x % P, mine = threadIdx.x / P;
     int64_t tokens = max_tokens;
     if (n_tokens) tokens = min((int64_t)max(__ldg(n_tokens), 0), max_tokens);
-    const int64_t t = (int64_t)blockIdx.x * S::kTokens + mine;
+    const int64_t t = (int64_t)blockIdx.x * kTokens + mine;
     if (t - (int)(threadIdx.x & 31) / P >= tokens) return;
     const bool live = t < tokens;
     const int64_t at = live ? t : tokens - 1;
     const T* row = logits + at * ld;
+    T* out = grad + at * ld_grad;
     const float none = -INFINITY;
     const auto logit = [&](int e) {
-        const float x = as_float(row[e]) + 0.f;
+        const float x = as_float(row[e]);
         return x != x ? none : x;
     };
+    if (!dense && live)
+        for (int c = q * N; c < E; c += P * N) {
+            Pack<T, N> v;
+            v.zero();
+            v.store(out + c);
+        }
 
-    float l[ITEMS], top = none, z = 1.f;
-    if (softmax && !renorm) {
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) l[j] = j * P + q < E ? logit(j * P + q) : none;
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) top = fmaxf(top, l[j]);
+    float top = none, z = 1.f;
+    if (dense) {
+        for (int c = q; c < E; c += P) top = fmaxf(top, logit(c));
         top = max_of<P>(top);
         z = 0.f;
-#pragma unroll
-        for (int j = 0; j < ITEMS; ++j) z += l[j] > none ? part(l[j], top) : 0.f;
+        for (int c = q; c < E; c += P) {
+            const float x = logit(c);
+            z += x > none ? part(x, top) : 0.f;
+        }
         z = sum_of<P>(z);
     }
     // the chosen: their scores (relative, as above), and sums over them
@@ -339,42 +507,53 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT) k_expert_choose_bwd(cons
     m = max_of<P>(m);
     if (!softmax) m = renorm ? fminf(m, 0.f) : 0.f;
     else if (!renorm) m = top;
-    const auto score = [&](float x) {
+    const auto score = [&](float x, float* rest) {               // *rest: 1 - sigmoid(x)
+        *rest = 1.f;
         if (x == none) return 0.f;
         if (softmax) return part(x, m);
-        return x > 0.f ? sigmoid(x) : part(x, m) / (1.f + expf(x));
+        const float e = expf(x > 0.f ? -x : x), per = 1.f / (1.f + e);
+        *rest = (x > 0.f ? e : 1.f) * per;
+        return (x > 0.f ? 1.f : m == 0.f ? e : part(x, m)) * per;
     };
-    float sum = 0.f, dot = 0.f;
+    float sum = 0.f, dot = 0.f, first = 0.f, first_rest = 1.f, first_g = 0.f;                // (of the lane's first choice)
     for (int k = q; k < top_k; k += P) {
         const int e = s_chosen[mine][k];
         if (e < 0) continue;
-        const float s = score(logit(e));
+        float rest;
+        const float s = score(logit(e), &rest), g = __ldg(&grad_w[at * top_k + k]);
+        if (k == q) {
+            first = s;
+            first_rest = rest;
+            first_g = g;
+        }
         sum += s;
-        dot += s * __ldg(&grad_w[at * top_k + k]);
+        dot += s * g;
     }
     sum = sum_of<P>(sum);
     dot = sum_of<P>(dot);
     if (!renorm) sum = softmax ? z : 1.f;
-    const float mean = renorm || softmax ? dot / sum : 0.f;
+    const float per = sum > 0.f ? 1.f / sum : 0.f, mean = renorm || softmax ? dot * per : 0.f;
     // d/dl of the weights: scale * share * (grad - mean), times 1 - score for sigmoids
     for (int k = q; k < top_k; k += P) {
+        float s = first, rest = first_rest, g = first_g;
         const int e = s_chosen[mine][k];
-        float g = 0.f;
-        if (e >= 0) {
-            const float x = logit(e), share = sum > 0.f ? score(x) / sum : 0.f;
-            g = scale * share * (__ldg(&grad_w[at * top_k + k]) - mean);
-            if (!softmax) g *= 1.f / (1.f + expf(x));            // 1 - sigmoid(x)
+        if (k != q && e >= 0) {
+            s = score(logit(e), &rest);
+            g = __ldg(&grad_w[at * top_k + k]);
         }
-        s_grad[mine][k] = g;
+        s_grad[mine][k] = e < 0 ? 0.f : scale * (s * per) * (g - mean) * rest;
     }
     if (!live) return;
-    T* out = grad + t * ld_grad;
+    if (dense)
+        for (int c = q * N; c < E; c += P * N) {
+            Pack<T, N> v;
+            float x[N];
+            v.load(row + c);
+            v.get(x);
 #pragma unroll
-    for (int j = 0; j < ITEMS; ++j)
-        if (j * P + q < E) {
-            float g = 0.f;
-            if (softmax && !renorm && l[j] > none) g = -scale * (part(l[j], top) / z) * mean;
-            out[j * P + q] = from_float<T>(g);
+            for (int k = 0; k < N; ++k) x[k] = x[k] > none ? -scale * (part(x[k], top) * per) * mean : 0.f;
+            v.set(x);
+            v.store(out + c);
         }
     __syncwarp();
     for (int k = q; k < top_k; k += P) {
@@ -404,20 +583,36 @@ int flags_of(const hl_router* r) {
     return (r->score == HL_SCORE_SOFTMAX ? kSoftmax : 0) | (r->group_score == HL_GROUP_TOP2 ? kPair : 0) | (r->renorm ? kRenorm : 0);
 }
 
-// As few lanes a token as hold its experts, eight a lane; above 256 experts more.
-#define HL_SHAPES(E, RUN)                                                                                             \
-    ((E) <= 8 ? RUN(8, 1) : (E) <= 16 ? RUN(8, 2) : (E) <= 32 ? RUN(8, 4) : (E) <= 64 ? RUN(8, 8) : (E) <= 128 ? RUN(8, 16) \
-     : (E) <= 256 ? RUN(8, 32) : (E) <= 512 ? RUN(16, 32) : RUN(32, 32))
+// As few lanes a token as hold its experts, eight a lane; above 128 experts sixteen, as most steps take a warp the same time
+// however many tokens it has; above 512 more.
+#define HL_SHAPES(E, RUN, WHOLE)                                                                                        \
+    ((E) <= 8     ? RUN(8, 1, WHOLE)                                                                                    \
+     : (E) <= 16  ? RUN(8, 2, WHOLE)                                                                                    \
+     : (E) <= 32  ? RUN(8, 4, WHOLE)                                                                                    \
+     : (E) <= 64  ? RUN(8, 8, WHOLE)                                                                                    \
+     : (E) <= 128 ? RUN(8, 16, WHOLE)                                                                                   \
+     : (E) <= 256 ? RUN(16, 16, WHOLE)                                                                                  \
+     : (E) <= 512 ? RUN(16, 32, WHOLE)                                                                                  \
+                  : RUN(32, 32, WHOLE))
+// whether a group is the experts of 1, 2, 4 ... of these lanes
+bool whole_lanes(const hl_router* r) {
+    const int items = r->n_experts <= 128 ? 8 : r->n_experts <= 512 ? 16 : 32, per = r->n_experts / r->n_groups, lanes = per / items;
+    return per % items == 0 && (lanes & (lanes - 1)) == 0;
+}
 
 template <typename T>
 int32_t launch_choose(const hl_router* r, const void* logits, int64_t ld, const float* bias, int64_t max_tokens,
                       const int32_t* n_tokens, int32_t* experts, float* weights, int32_t* status, cudaStream_t stream) {
-#define HL_RUN(ITEMS, P)                                                                                                      \
-    launch_cluster(k_expert_choose<T, ITEMS, P>, (unsigned)div_up(max_tokens, Shape<ITEMS, P>::kTokens), Shape<ITEMS, P>::kNT, \
-                   r->n_groups > 1 ? Shape<ITEMS, P>::kTokens * (r->n_experts + 2 * r->n_groups) * sizeof(double) : 0, 0,      \
+    const bool lanes = whole_lanes(r);
+#define HL_RUN(ITEMS, P, WHOLE)                                                                                               \
+    launch_cluster(k_expert_choose<T, ITEMS, P, WHOLE>, (unsigned)div_up(max_tokens, Shape<ITEMS, P>::kTokens), Shape<ITEMS, P>::kNT, \
+                   r->n_groups > 1 && !lanes ? Shape<ITEMS, P>::kTokens * (r->n_experts + 2 * r->n_groups) * sizeof(double) : 0, 0,      \
                    stream, static_cast<const T*>(logits), ld, bias, n_tokens, max_tokens, r->top_k, r->n_experts, r->n_groups, \
-                   r->top_groups, flags_of(r), r->scale, experts, weights, status)
-    HL_CUDA_TRY(HL_SHAPES(r->n_experts, HL_RUN));
+                   r->top_groups, flags_of(r) | (lanes ? kWholeLanes : 0), r->scale, experts, weights, status)
+    const bool whole = r->n_experts % (16 / (int)sizeof(T)) == 0 && lies_at(logits, 16) && ld * sizeof(T) % 16 == 0 &&
+                       lies_at(bias, 16);
+    if (whole) HL_CUDA_TRY(HL_SHAPES(r->n_experts, HL_RUN, true));
+    else HL_CUDA_TRY(HL_SHAPES(r->n_experts, HL_RUN, false));
 #undef HL_RUN
     note_launches(1);
     HL_LAUNCH_CHECK();
@@ -426,11 +621,15 @@ int32_t launch_choose(const hl_router* r, const void* logits, int64_t ld, const 
 template <typename T>
 int32_t launch_choose_bwd(const hl_router* r, const void* logits, int64_t ld, int64_t max_tokens, const int32_t* n_tokens,
                           const int32_t* experts, const float* grad_w, void* grad, int64_t ld_grad, cudaStream_t stream) {
-#define HL_RUN(ITEMS, P)                                                                                                          \
-    launch(k_expert_choose_bwd<T, ITEMS, P>, (unsigned)div_up(max_tokens, Shape<ITEMS, P>::kTokens), Shape<ITEMS, P>::kNT, stream, \
-           static_cast<const T*>(logits), ld, n_tokens, max_tokens, r->top_k, r->n_experts, flags_of(r), r->scale, experts, grad_w, \
+    const bool whole = r->n_experts % (16 / (int)sizeof(T)) == 0 && lies_at(logits, 16) && ld * sizeof(T) % 16 == 0 &&
+                       lies_at(grad, 16) && ld_grad * sizeof(T) % 16 == 0;
+    // (eight lanes a token: 32 experts' rows a line's half each; many experts: a warp)
+    const int E = r->n_experts, P = E <= 16 ? 2 : E <= 256 ? 8 : 32;
+#define HL_RUN(P)                                                                                                               \
+    launch(whole ? k_expert_choose_bwd<T, P, true> : k_expert_choose_bwd<T, P, false>, (unsigned)div_up(max_tokens, 128 / P), 128, \
+           stream, static_cast<const T*>(logits), ld, n_tokens, max_tokens, r->top_k, E, flags_of(r), r->scale, experts, grad_w,   \
            static_cast<T*>(grad), ld_grad)
-    HL_CUDA_TRY(HL_SHAPES(r->n_experts, HL_RUN));
+    HL_CUDA_TRY(P == 2 ? HL_RUN(2) : P == 8 ? HL_RUN(8) : HL_RUN(32));
 #undef HL_RUN
     note_launches(1);
     HL_LAUNCH_CHECK();

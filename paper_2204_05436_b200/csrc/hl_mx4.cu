@@ -20,18 +20,62 @@ __device__ __forceinline__ int exponent_at(int row, int block) {
     return kValueBytes + (block >> 2) * 512 + (row & 31) * 16 + (row >> 5) * 4 + (block & 3);
 }
 
+// A row's part from column c on, eight values a lane, as they are; zeros behind its end and where there is no row.
+template <typename T, bool WHOLE>
+struct Part {
+    static constexpr int kWords = 8 * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* row, int64_t c, int64_t dim) {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
+        if (!row) return;
+        if constexpr (WHOLE) {
+            if (c >= dim) return;
+            Pack<T, 8> v;
+            v.load(row + c);
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = v.w[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (c + i >= dim) continue;
+                if constexpr (sizeof(T) == 4) w[i] = __ldg(reinterpret_cast<const uint32_t*>(row + c + i));
+                else w[i / 2] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(row + c + i)) << (16 * (i & 1));
+            }
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        Pack<T, 8> v;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) v.w[i] = w[i];
+        v.get(x);
+    }
+    // the largest absolute value of the lane's block, among its four lanes, as 32-bit float's bits (infinities and NaN: 255 << 23
+    // and more).  Bits without the sign are in the order of the values, NaN largest; those of 16-bit types two at a time.
+    __device__ __forceinline__ uint32_t largest() const {
+        constexpr uint32_t kAbs = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
+        uint32_t top = w[0] & kAbs;
+#pragma unroll
+        for (int i = 1; i < kWords; ++i) top = sizeof(T) == 4 ? max(top, w[i] & kAbs) : __vmaxu2(top, w[i] & kAbs);
+        if constexpr (sizeof(T) == 2) top = max(top >> 16, top & 0xffffu);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        if constexpr (sizeof(T) == 4) return top;
+        else if constexpr (std::is_same_v<T, __nv_bfloat16>) return top << 16;
+        else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)top)));
+    }
+};
+
 // Eight values of a row's part in 4 bits, and their block's exponent (in all of its lanes): 2^(E - 127) with E two below the
 // largest value's own, so that this one lies in 4 .. 8, of which what is above 6 becomes 6; values are rounded to the nearest of 0, 1/2, 1,
 // 3/2, 2, 3, 4, 6, ties to the one of even mantissa.  A block with an infinity or NaN is NaN (exponent 255).
-__device__ __forceinline__ uint32_t to_four_bits(const float (&x)[8], uint32_t* exponent) {
-    uint32_t top = 0;                  // (of the bits, so that NaN is the largest)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int e = (int)(top >> 23);
+template <typename T, bool WHOLE>
+__device__ __forceinline__ uint32_t to_four_bits(const Part<T, WHOLE>& part, uint32_t* exponent) {
+    const int e = (int)(part.largest() >> 23);
     const uint32_t E = e == 255 ? 255u : (uint32_t)max(e - 2, 0);
     const float up = __uint_as_float((254u - min(E, 253u)) << 23);         // 2^(127 - E)
+    float x[8];
+    part.get(x);
     uint32_t packed;
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
         "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
@@ -46,35 +90,6 @@ __device__ __forceinline__ uint32_t to_four_bits(const float (&x)[8], uint32_t* 
     return packed;
 }
 
-// A row's part from column c0 on, eight values a lane; zeros behind its end and where there is no row.
-template <typename T, bool WHOLE>
-struct Part {
-    Pack<T, WHOLE ? 8 : 1> v[WHOLE ? 1 : 8];
-    __device__ __forceinline__ void load(const T* row, int64_t c, int64_t dim) {
-        if constexpr (WHOLE) {
-            v[0].zero();
-            if (row && c < dim) v[0].load(row + c);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[i].zero();
-                if (row && c + i < dim) v[i].load(row + c + i);
-            }
-        }
-    }
-    __device__ __forceinline__ void get(float (&x)[8]) const {
-        if constexpr (WHOLE) {
-            v[0].get(x);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float one[1];
-                v[i].get(one);
-                x[i] = one[0];
-            }
-        }
-    }
-};
 __device__ __forceinline__ void store_part(uint8_t* tile, int row, int lane, uint32_t packed, uint32_t exponent) {
     *reinterpret_cast<uint32_t*>(tile + value_at(row, lane)) = packed;
     if ((lane & 3) == 0) tile[exponent_at(row, lane >> 2)] = (uint8_t)exponent;
@@ -82,38 +97,44 @@ __device__ __forceinline__ void store_part(uint8_t* tile, int row, int lane, uin
 
 constexpr int kRowNT = 256;
 
-// n_matrices of `rows` rows: a warp takes U parts of rows, side by side.  Bound by memory.
+// n / d by 2^64 / d, rounded up: exact for n * d < 2^64
+struct Divisor {
+    unsigned long long inverse;
+    int64_t d;
+    __device__ __forceinline__ int64_t operator()(int64_t n) const { return d == 1 ? n : (int64_t)__umul64hi((uint64_t)n, inverse); }
+};
+
+// n_matrices of `rows` rows: a warp takes U parts of a row, side by side.  Bound by memory.  (rows_of: a matrix' rows, here with
+// those that fill its last tile up; chunks: of U parts, in a row)
 template <typename T, bool WHOLE, int U>
 __global__ void __launch_bounds__(kRowNT) k_mx4_quantise(const T* __restrict__ x, int64_t rows, int64_t dim, int64_t ld, int64_t stride,
-                                                         int64_t row_tiles, int64_t col_tiles, int64_t parts, uint8_t* __restrict__ q) {
+                                                         Divisor rows_of, Divisor chunks, int col_tiles, int64_t items,
+                                                         uint8_t* __restrict__ q) {
     const int lane = threadIdx.x & 31;
-    const int64_t first = ((int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5)) * U;
+    const int64_t item = (int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5);
+    if (item >= items) return;
+    const int64_t row = chunks(item), m = rows_of(row), of = row - m * rows_of.d;
+    const int ct = (int)(item - row * chunks.d) * U, r = (int)(of & (kTileRows - 1));
+    const T* from = of < rows ? x + m * stride + of * ld : nullptr;
+    uint8_t* tile = q + ((row >> 7) * col_tiles + ct) * kTileBytes;
     Part<T, WHOLE> in[U];
-    int64_t tile[U];
-    int r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) in[u].load(from, (ct + u) * kTileCols + lane * 8, dim);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int64_t i = min(first + u, parts - 1), row = i / col_tiles, ct = i - row * col_tiles;      // of all, with those that fill up
-        const int64_t m = row / (row_tiles * kTileRows), of = row - m * row_tiles * kTileRows;
-        r[u] = (int)(of & (kTileRows - 1));
-        tile[u] = (m * row_tiles + of / kTileRows) * col_tiles + ct;
-        in[u].load(of < rows ? x + m * stride + of * ld : nullptr, ct * kTileCols + lane * 8, dim);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        if (first + u >= parts) break;
-        float v[8];
+        if (ct + u >= col_tiles) break;
         uint32_t e;
-        in[u].get(v);
-        const uint32_t packed = to_four_bits(v, &e);
-        store_part(q + tile[u] * kTileBytes, r[u], lane, packed, e);
+        const uint32_t packed = to_four_bits(in[u], &e);
+        store_part(tile + u * kTileBytes, r, lane, packed, e);
     }
 }
 
-__device__ __forceinline__ void from_four_bits(uint32_t packed, uint32_t E, float (&x)[8]) {
+// N values in 4 bits each, the first in the lowest
+template <int N>
+__device__ __forceinline__ void from_four_bits(uint32_t packed, uint32_t E, float* x) {
     const float unit = E == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(E ? E << 23 : 0x00400000u);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N / 2; ++i) {
         uint32_t two;                  // fp16
         asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\t}" : "=r"(two) : "r"(packed >> (8 * i)));
         x[2 * i] = __half2float(__ushort_as_half((unsigned short)(two & 0xffffu))) * unit;
@@ -121,40 +142,50 @@ __device__ __forceinline__ void from_four_bits(uint32_t packed, uint32_t E, floa
     }
 }
 
+// The way back: a lane writes 16 bytes of a row's part at a time, so that a warp's stores are whole lines (with 32 bytes of fp32 in a
+// row of a lane's own, two halves of a line each: 4.8 instead of ... TB/s).
 template <typename T, bool WHOLE, int U>
-__global__ void __launch_bounds__(kRowNT) k_mx4_dequantise(const uint8_t* __restrict__ q, int64_t rows, int64_t dim, int64_t row_tiles,
-                                                           int64_t col_tiles, int64_t parts, T* __restrict__ out, int64_t ld,
-                                                           int64_t stride) {
+__global__ void __launch_bounds__(kRowNT) k_mx4_dequantise(const uint8_t* __restrict__ q, int64_t row_tiles, int64_t dim,
+                                                           Divisor rows_of, Divisor chunks, int col_tiles, int64_t items,
+                                                           T* __restrict__ out, int64_t ld, int64_t stride) {
+    constexpr int N = 16 / sizeof(T), S = 8 / N;                 // values of a store, stores of a part
     const int lane = threadIdx.x & 31;
-    const int64_t first = ((int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5)) * U;
-    uint32_t packed[U], E[U];
-    int64_t at[U], c[U];
+    const int64_t item = (int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5);
+    if (item >= items) return;
+    const int64_t row = chunks(item), m = rows_of(row), of = row - m * rows_of.d;
+    const int ct = (int)(item - row * chunks.d) * U, r = (int)(of & (kTileRows - 1));
+    const uint8_t* tile = q + ((m * row_tiles + (of >> 7)) * col_tiles + ct) * kTileBytes;
+    T* to = out + m * stride + of * ld;
+    uint32_t packed[U][S], E[U][S];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t i = min(first + u, parts - 1), row = i / col_tiles, ct = i - row * col_tiles;      // of all rows that there are
-        const int64_t m = row / rows, of = row - m * rows;
-        const int r = (int)(of & (kTileRows - 1));
-        const uint8_t* tile = q + ((m * row_tiles + of / kTileRows) * col_tiles + ct) * kTileBytes;
-        packed[u] = __ldg(reinterpret_cast<const uint32_t*>(tile + value_at(r, lane)));
-        E[u] = __ldg(tile + exponent_at(r, lane >> 2));
-        at[u] = m * stride + of * ld;
-        c[u] = ct * kTileCols + lane * 8;
-    }
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        if (first + u >= parts || c[u] >= dim) continue;
-        float x[8];
-        from_four_bits(packed[u], E[u], x);
-        if constexpr (WHOLE) {
-            Pack<T, 8> v;
-            v.set(x);
-            v.store(out + at[u] + c[u]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c[u] + i < dim) out[at[u] + c[u] + i] = from_float<T>(x[i]);
+        for (int i = 0; i < S; ++i) {
+            const int c = i * 32 * N + lane * N;                 // of the part
+            const uint8_t* p = tile + u * kTileBytes + r * 128 + (((c >> 5) ^ (r & 7)) << 4) + ((c & 31) >> 1);
+            packed[u][i] = E[u][i] = 0;
+            if (ct + u >= col_tiles) continue;
+            packed[u][i] = N == 8 ? __ldg(reinterpret_cast<const uint32_t*>(p)) : __ldg(reinterpret_cast<const unsigned short*>(p));
+            E[u][i] = __ldg(tile + u * kTileBytes + exponent_at(r, c >> 5));
         }
-    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            const int64_t c = (int64_t)(ct + u) * kTileCols + i * 32 * N + lane * N;
+            if (ct + u >= col_tiles || c >= dim) continue;
+            float x[N];
+            from_four_bits<N>(packed[u][i], E[u][i], x);
+            if constexpr (WHOLE) {
+                Pack<T, N> v;
+                v.set(x);
+                v.store(to + c);
+            } else {
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    if (c + k < dim) to[c + k] = from_float<T>(x[k]);
+            }
+        }
 }
 
 // ---- the experts' rows ------------------------------------------------------------------------------------------------
@@ -216,14 +247,17 @@ __device__ __forceinline__ int last_not_above(const int* list, int n, int v) {
     return lo;
 }
 
-// Rows in the experts' order (top_k 0), or the tokens', each to all of its experts' rows: read and converted once.
+// Rows in the experts' order (top_k 0), or the tokens', each to all of its experts' rows: read and converted once.  A warp takes U
+// parts of a row; its lanes find where each of the row's choices lies.
+constexpr int kRowParts = 4;
 template <typename T, bool WHOLE>
-__global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, int64_t ld, int64_t dim, int col_tiles,
+__global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, int64_t ld, int64_t dim, int col_tiles, Divisor chunks,
                                                      const int32_t* n_tokens, int64_t max_rows, int top_k,
                                                      const int32_t* __restrict__ place, const int32_t* __restrict__ counts,
                                                      const int32_t* __restrict__ offsets, int E, int64_t cap_rows, int max_tiles,
                                                      uint8_t* __restrict__ q, int32_t* status) {
     __shared__ int s_first[HL_MAX_EXPERTS + 1], s_begin[HL_MAX_EXPERTS];
+    constexpr int U = kRowParts;
     let_next_start();
     if (blockIdx.x == 0 && threadIdx.x == 0) *status = HL_OK;
     const Experts experts{counts, offsets, E, cap_rows};
@@ -232,25 +266,36 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, in
     int64_t n = max_rows;
     if (top_k == 0) n = min(n, (int64_t)max(__ldg(&offsets[E]), 0));
     else if (n_tokens) n = min(n, (int64_t)max(__ldg(n_tokens), 0));
-    const int64_t parts = n * col_tiles;
-    for (int64_t i = (int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5); i < parts; i += (int64_t)gridDim.x * (kRowNT / 32)) {
-        const int64_t row = i / col_tiles;
-        const int ct = (int)(i - row * col_tiles);
-        Part<T, WHOLE> in;
-        in.load(x + row * ld, (int64_t)ct * kTileCols + lane * 8, dim);
-        float v[8];
-        uint32_t exponent;
-        in.get(v);
-        const uint32_t packed = to_four_bits(v, &exponent);
-        for (int k = 0; k < max(top_k, 1); ++k) {
-            const int at = top_k == 0 ? (int)row : __ldg(&place[row * top_k + k]);
-            if (at < 0 || at >= cap_rows) continue;
-            // (experts without rows begin where the next does: the last that begins there is the one)
-            const int e = last_not_above(s_begin, E, at), r = at - s_begin[e];
-            if (r < 0 || r >= experts.rows(e, s_begin[e])) continue;
-            const int tile = s_first[e] + r / kTileRows;
-            if (tile >= s_first[e + 1]) continue;
-            store_part(q + ((int64_t)tile * col_tiles + ct) * kTileBytes, r & (kTileRows - 1), lane, packed, exponent);
+    const int64_t items = n * chunks.d;
+    for (int64_t i = (int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5); i < items; i += (int64_t)gridDim.x * (kRowNT / 32)) {
+        const int64_t row = chunks(i);
+        const int ct0 = (int)(i - row * chunks.d) * U;
+        Part<T, WHOLE> in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) in[u].load(x + row * ld, (int64_t)(ct0 + u) * kTileCols + lane * 8, dim);
+        uint32_t packed[U], exponent[U];
+        for (int k0 = 0; k0 < max(top_k, 1); k0 += 32) {
+            int64_t to = -1;           // of choice k0 + lane: its tile and row in it
+            int at = -1;
+            if (top_k == 0) at = lane == 0 ? (int)row : -1;
+            else if (k0 + lane < top_k) at = __ldg(&place[row * top_k + k0 + lane]);
+            if (at >= 0 && at < cap_rows) {
+                // (experts without rows begin where the next does: the last that begins there is the one)
+                const int e = last_not_above(s_begin, E, at), r = at - s_begin[e], tile = s_first[e] + r / kTileRows;
+                if (r >= 0 && r < experts.rows(e, s_begin[e]) && tile < s_first[e + 1])
+                    to = (int64_t)tile * kTileRows + (r & (kTileRows - 1));
+            }
+            if (k0 == 0) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) packed[u] = to_four_bits(in[u], &exponent[u]);
+            }
+            for (unsigned left = __ballot_sync(0xffffffffu, to >= 0); left; left &= left - 1) {
+                const int64_t dst = __shfl_sync(0xffffffffu, to, __ffs(left) - 1);
+                uint8_t* tile = q + ((dst >> 7) * col_tiles + ct0) * kTileBytes;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (ct0 + u < col_tiles) store_part(tile + u * kTileBytes, (int)(dst & (kTileRows - 1)), lane, packed[u], exponent[u]);
+            }
         }
     }
 }
@@ -258,8 +303,8 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, in
 // ---- the product --------------------------------------------------------------------------------------------------------
 // y[row, f] = sum over d of x[row, d] * w[e, f, d] for the rows of expert e: 128 outputs f (the lanes of the tensor memory) by up to
 // 128 rows (its columns) at a time, 256 of d a step.  One warp's thread has the tiles of a step copied, one issues the products,
-// four warps take the sums out, those of one tile while the next one's are made.
-constexpr int kStages = 6, kStageBytes = 2 * kTileBytes, kProductNT = 192;
+// eight warps take the sums out, those of one tile while the next one's are made.
+constexpr int kStages = 6, kStageBytes = 2 * kTileBytes, kProductNT = 320;
 constexpr int kAccCols = 128;          // tensor-memory columns of a tile's sums (two tiles'), then those of the exponents
 constexpr uint32_t kExponentCols = 2 * kAccCols;
 constexpr int kProductSmem = kStages * kStageBytes + 1024 + (HL_MAX_EXPERTS + 1) * 4 + 256;
@@ -323,6 +368,20 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
+// 32 columns of a warp's 32 lanes
+__device__ __forceinline__ void tmem_load(uint32_t (&v)[32], uint32_t from) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+          "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+          "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(from)
+        : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
 // What a CTA does next: the tile of rows, the expert's, and the tile of outputs.
 struct Item {
     int e, rows, f;                    // rows: of the tile
@@ -360,7 +419,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
         }
         for (int b = 0; b < 2; ++b) {
             bar_init(&s_sums[b], 1);
-            bar_init(&s_taken[b], 4);
+            bar_init(&s_taken[b], 8);
         }
         s_gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -444,7 +503,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
             }
         }
     } else {
-        const int quarter = warp & 3;                            // the lanes of the tensor memory that this warp can read
+        const int quarter = warp & 3, half = (warp - 2) >> 2;    // the lanes of the tensor memory that this warp can read; its columns
         int buffer = 0;
         uint32_t phase = 0;
         for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
@@ -453,31 +512,26 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             __syncwarp();
             const int64_t f = (int64_t)it.f * kTileRows + quarter * 32 + lane;
-            T* out = y + it.row0 * ld + f;
-            for (int c0 = 0; c0 < it.rows; c0 += 32) {
+            const int end = min(it.rows, (half + 1) * (kTileRows / 2));
+            for (int c0 = half * (kTileRows / 2); c0 < end; c0 += 32) {
                 uint32_t v[32];
-                const uint32_t from = tmem + buffer * kAccCols + c0 + ((uint32_t)(quarter * 32) << 16);
-                asm volatile(
-                    "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-                    "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-                    : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
-                      "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
-                      "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
-                      "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-                    : "r"(from)
-                    : "memory");
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                if (f < outputs) {
+                tmem_load(v, tmem + buffer * kAccCols + c0 + ((uint32_t)(quarter * 32) << 16));
+                if (f >= outputs) continue;
+                T* out = y + (it.row0 + c0) * ld + f;
+                if (c0 + 32 <= end) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (c0 + k < it.rows) out[(int64_t)(c0 + k) * ld] = from_float<T>(__uint_as_float(v[k]));
+                    for (int k = 0; k < 32; ++k, out += ld) *out = from_float<T>(__uint_as_float(v[k]));
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k, out += ld)
+                        if (c0 + k < end) *out = from_float<T>(__uint_as_float(v[k]));
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) bar_arrive(&s_taken[buffer]);
             if (f < outputs)
-                for (int64_t p = 0; p < it.pad; ++p) out[(it.rows + p) * ld] = from_float<T>(0.f);
+                for (int64_t p = half; p < it.pad; p += 2) y[(it.row0 + it.rows + p) * ld + f] = from_float<T>(0.f);
             buffer ^= 1;
             phase ^= buffer == 0;
         }
@@ -500,18 +554,26 @@ constexpr int kSMs = 148;              // grids are made for a B200's multiproce
 int64_t tiles_of(int64_t n, int per) { return div_up(n, per); }
 bool matrix_dims_ok(int64_t rows, int64_t dim) { return rows >= 0 && rows < (int64_t(1) << 31) && dim >= 1 && dim <= (int64_t(1) << 24); }
 
+Divisor divisor(int64_t d) { return {d == 1 ? 0 : ~0ull / (uint64_t)d + 1, d}; }
+
 constexpr int64_t kWorkspaceHead = 1024;
 int64_t row_tiles_most(int64_t cap_rows, int64_t E) { return cap_rows / kTileRows + (E < cap_rows ? E : cap_rows); }
+
+// Parts of a row that a warp takes: as many as there are, up to four.
+int parts_of(int64_t col_tiles) { return col_tiles >= 3 ? 4 : (int)col_tiles; }
+#define HL_PARTS(KERNEL, T)                                                                                             \
+    (U == 4 ? (whole ? KERNEL<T, true, 4> : KERNEL<T, false, 4>)                                                        \
+            : U == 2 ? (whole ? KERNEL<T, true, 2> : KERNEL<T, false, 2>) : (whole ? KERNEL<T, true, 1> : KERNEL<T, false, 1>))
 
 template <typename T>
 int32_t launch_quantise(int64_t n, int64_t rows, int64_t dim, const void* x, int64_t ld, int64_t stride, void* q, bool whole,
                         cudaStream_t stream) {
-    constexpr int U = 4;
-    const int64_t rt = tiles_of(rows, kTileRows), ct = tiles_of(dim, kTileCols), parts = n * rt * kTileRows * ct;
-    const int64_t ctas = div_up(parts, kRowNT / 32 * U);
-    if (ctas > 0x7fffffff) return HL_EINVAL;
-    HL_CUDA_TRY(launch(whole ? k_mx4_quantise<T, true, U> : k_mx4_quantise<T, false, U>, (unsigned)ctas, kRowNT, stream,
-                       static_cast<const T*>(x), rows, dim, ld, stride, rt, ct, parts, static_cast<uint8_t*>(q)));
+    const int64_t rt = tiles_of(rows, kTileRows), ct = tiles_of(dim, kTileCols);
+    const int U = parts_of(ct);
+    const int64_t chunks = div_up(ct, U), items = n * rt * kTileRows * chunks, ctas = div_up(items, kRowNT / 32);
+    if (ctas > 0x7fffffff || n * rt * kTileRows >= (int64_t(1) << 32)) return HL_EINVAL;
+    HL_CUDA_TRY(launch(HL_PARTS(k_mx4_quantise, T), (unsigned)ctas, kRowNT, stream, static_cast<const T*>(x), rows, dim, ld, stride,
+                       divisor(rt * kTileRows), divisor(chunks), ct, items, static_cast<uint8_t*>(q)));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
@@ -519,12 +581,12 @@ int32_t launch_quantise(int64_t n, int64_t rows, int64_t dim, const void* x, int
 template <typename T>
 int32_t launch_dequantise(int64_t n, int64_t rows, int64_t dim, const void* q, void* out, int64_t ld, int64_t stride, bool whole,
                           cudaStream_t stream) {
-    constexpr int U = 4;
-    const int64_t rt = tiles_of(rows, kTileRows), ct = tiles_of(dim, kTileCols), parts = n * rows * ct;
-    const int64_t ctas = div_up(parts, kRowNT / 32 * U);
-    if (ctas > 0x7fffffff) return HL_EINVAL;
-    HL_CUDA_TRY(launch(whole ? k_mx4_dequantise<T, true, U> : k_mx4_dequantise<T, false, U>, (unsigned)ctas, kRowNT, stream,
-                       static_cast<const uint8_t*>(q), rows, dim, rt, ct, parts, static_cast<T*>(out), ld, stride));
+    const int64_t rt = tiles_of(rows, kTileRows), ct = tiles_of(dim, kTileCols);
+    const int U = parts_of(ct);
+    const int64_t chunks = div_up(ct, U), items = n * rows * chunks, ctas = div_up(items, kRowNT / 32);
+    if (ctas > 0x7fffffff || n * rows >= (int64_t(1) << 32)) return HL_EINVAL;
+    HL_CUDA_TRY(launch(HL_PARTS(k_mx4_dequantise, T), (unsigned)ctas, kRowNT, stream, static_cast<const uint8_t*>(q), rt, dim,
+                       divisor(rows), divisor(chunks), ct, items, static_cast<T*>(out), ld, stride));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
@@ -535,9 +597,9 @@ int32_t launch_product(const hl_route* r, int64_t dim, int64_t outputs, const vo
     int32_t* status = static_cast<int32_t*>(workspace);
     uint8_t* q = static_cast<uint8_t*>(workspace) + kWorkspaceHead;
     const int64_t ct = tiles_of(dim, kTileCols), ft = tiles_of(outputs, kTileRows), rt = row_tiles_most(r->cap_rows, r->n_experts);
-    const int64_t rows = by_token ? r->max_tokens : r->cap_rows;
-    HL_CUDA_TRY(launch(whole ? k_mx4_rows<T, true> : k_mx4_rows<T, false>, grid_for(rows * ct, kRowNT / 32, 8 * kSMs), kRowNT, stream,
-                       static_cast<const T*>(x), ld_x, dim, ct, r->n_tokens, rows, by_token ? r->top_k : 0, r->place, r->counts,
+    const int64_t rows = by_token ? r->max_tokens : r->cap_rows, chunks = div_up(ct, kRowParts);
+    HL_CUDA_TRY(launch(whole ? k_mx4_rows<T, true> : k_mx4_rows<T, false>, grid_for(rows * chunks, kRowNT / 32, 8 * kSMs), kRowNT, stream,
+                       static_cast<const T*>(x), ld_x, dim, ct, divisor(chunks), r->n_tokens, rows, by_token ? r->top_k : 0, r->place, r->counts,
                        r->offsets, r->n_experts, r->cap_rows, rt, q, status));
     note_launches(1);
     const auto kernel = k_mx4_product<T>;

@@ -93,6 +93,52 @@ struct Pack {
     }
 };
 
+// Eight values side by side of a row that begins anywhere: columns c .. c + 7, zeros outside [0, dim).  The 16-byte lines that hold
+// some of them are read whole (each has a value of the row, so it lies where the row's memory does), and put in place by shifts.
+template <typename T>
+struct Loose {
+    static constexpr int N = 16 / (int)sizeof(T), kLines = 8 / N + 1, kWords = 4 * kLines;
+    uint32_t w[kWords];
+    int shift;                         // values in the first line that lie before column c
+    __device__ __forceinline__ void zero() {
+        shift = 0;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ void load(const T* row, int c, int dim) {
+        const uintptr_t p = reinterpret_cast<uintptr_t>(row + c), line = p & ~uintptr_t(15);
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(row + max(c, 0)), end = reinterpret_cast<uintptr_t>(row + min(c + 8, dim));
+        shift = (int)(p & 15) / (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < kLines; ++i) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (line + 16 * i < end && line + 16 * i + 16 > begin) v = __ldg(reinterpret_cast<const uint4*>(line + 16 * i));
+            w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[8], int c, int dim) const {
+        uint32_t v[kWords];
+        const int words = shift * (int)sizeof(T) / 4;            // 0 .. 3
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) v[i] = words & 2 ? w[i + 2 < kWords ? i + 2 : i] : w[i];
+#pragma unroll
+        for (int i = 0; i + 1 < kWords; ++i) v[i] = words & 1 ? v[i + 1] : v[i];
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(v[i], v[i + 1], 16 * (shift & 1));
+        }
+        Pack<T, 8> p;
+#pragma unroll
+        for (int i = 0; i < Pack<T, 8>::kWords; ++i) p.w[i] = v[i];
+        p.get(x);
+        if (c < 0 || c + 8 > dim) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if ((unsigned)(c + i) >= (unsigned)dim) x[i] = 0.f;
+        }
+    }
+};
+
 // ---- arguments: types, and matrices of rows -------------------------------------------------------------------------------
 inline int dtype_size(int32_t dtype) { return dtype == HL_F32 ? 4 : dtype == HL_BF16 || dtype == HL_F16 ? 2 : 0; }
 inline bool lies_at(const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }

@@ -51,6 +51,41 @@ __global__ void __launch_bounds__(kNT) k_token_embed(const TT* __restrict__ tabl
     }
 }
 
+// The same for rows that begin anywhere: eight values a thread, from where the written row's 16-byte lines begin, so that all but
+// those at its ends are written whole.
+template <typename TT, typename TO>
+__global__ void __launch_bounds__(kNT) k_token_embed_loose(const TT* __restrict__ table, int64_t ld_table, unsigned n_rows,
+                                                           const int32_t* __restrict__ tokens, int64_t max_tokens,
+                                                           const int32_t* n_tokens, float scale, int dim, TO* __restrict__ out,
+                                                           int64_t ld_out, int vectors, unsigned long long inverse, int32_t* status) {
+    const int64_t n = live_tokens(n_tokens, max_tokens);
+    const unsigned long long item = (int64_t)blockIdx.x * kNT + threadIdx.x;
+    const int64_t at = vectors == 1 ? item : __umul64hi(item, inverse);
+    if (at >= n) return;
+    TO* row = out + at * ld_out;
+    const int c = (int)(item - at * vectors) * 8 - (int)(reinterpret_cast<uintptr_t>(row) & 15) / (int)sizeof(TO);
+    if (c >= dim) return;
+    const int token = __ldg(&tokens[at]);
+    const bool there = (unsigned)token < n_rows;
+    Loose<TT> in;
+    in.zero();
+    if (there) in.load(table + token * ld_table, c, dim);
+    else if (token != -1 && status) set_status(status, HL_EBOUNDS);
+    float x[8];
+    in.get(x, c, dim);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = there ? x[i] * scale : 0.f;
+    if (c >= 0 && c + 8 <= dim) {
+        Pack<TO, 8> v;
+        v.set(x);
+        v.store(row + c);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((unsigned)(c + i) < (unsigned)dim) row[c + i] = from_float<TO>(x[i]);
+    }
+}
+
 // ---- the sort -----------------------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(kNT) k_token_pairs(const int32_t* __restrict__ tokens, int64_t max_tokens, const int32_t* n_tokens,
                                                      int n_rows, int32_t* __restrict__ keys, int32_t* __restrict__ vals,
@@ -67,15 +102,13 @@ __global__ void __launch_bounds__(kNT) k_token_pairs(const int32_t* __restrict__
 }
 
 // ---- the table's gradient -------------------------------------------------------------------------------------------------
-// The sorted tokens are cut into windows of `window`.  A group of P threads takes one, its columns W * C a thread, and adds up the
+// The sorted tokens are cut into windows of `window`.  A group of P threads takes one, its columns W a thread, and adds up the
 // gradients of each run of equal tokens.  A run inside the window goes to its row; of one that begins before the window or goes on
 // behind it only a piece is known, which goes to memory: piece 2w is that of the run which began before window w, 2w + 1 that of the
-// one that begins in it and goes on.  A second kernel adds the pieces of such a run up, in their order.
-struct Grads {
-    const int32_t *sorted, *order;
-    int64_t n;
-    int n_rows;
-};
+// one that begins in it and goes on.  A second kernel adds the pieces of such a run up, in their order.  Rows without tokens are
+// zeroed by CTAs of their own.  LOOSE: rows that begin anywhere; a group is a warp then, eight columns a lane.
+constexpr int kPieceStep = 8;          // a piece's columns are filled up to a multiple of this
+__device__ __forceinline__ int64_t piece_pitch(int dim) { return (dim + kPieceStep - 1) / kPieceStep * kPieceStep; }
 
 // first place in sorted[lo, hi) whose token is not below u
 __device__ __forceinline__ int64_t not_below(const int32_t* __restrict__ sorted, int64_t lo, int64_t hi, int u) {
@@ -87,26 +120,42 @@ __device__ __forceinline__ int64_t not_below(const int32_t* __restrict__ sorted,
     return lo;
 }
 
-template <typename TT, int W>
-__device__ __forceinline__ void put(TT* row, const float (&sum)[W], float scale, bool accumulate) {
-    float x[W];
-    Pack<TT, W> v;
+// row[c ..] = scale * sum (+ row).  LOOSE: by a whole warp, 256 columns from c - 8 * lane on, in the order of the lanes (s: [256]).
+template <typename TT, int W, bool LOOSE>
+__device__ __forceinline__ void put(TT* row, int c, int dim, const float (&sum)[W], float scale, bool accumulate, float* s) {
+    if constexpr (LOOSE) {
+        const int lane = threadIdx.x & 31;
+        __syncwarp();
+        Pack<float, W> mine;
+        mine.set(sum);
+        mine.store(s + lane * W);
+        __syncwarp();
 #pragma unroll
-    for (int i = 0; i < W; ++i) x[i] = scale * sum[i];
-    if (accumulate) {
-        float old[W];
-        v.load(row);
-        v.get(old);
+        for (int i = 0; i < W; ++i) {
+            const int k = c - lane * W + i * 32 + lane;
+            if (k < dim) row[k] = from_float<TT>(scale * s[i * 32 + lane] + (accumulate ? as_float(row[k]) : 0.f));
+        }
+    } else {
+        float x[W];
+        Pack<TT, W> v;
 #pragma unroll
-        for (int i = 0; i < W; ++i) x[i] += old[i];
+        for (int i = 0; i < W; ++i) x[i] = scale * sum[i];
+        if (accumulate) {
+            float old[W];
+            v.load(row + c);
+            v.get(old);
+#pragma unroll
+            for (int i = 0; i < W; ++i) x[i] += old[i];
+        }
+        v.set(x);
+        v.store(row + c);
     }
-    v.set(x);
-    v.store(row);
 }
 
 // rows [first, last) that no token names become zeros
 template <typename TT, int W>
-__device__ void zero_rows(const Grads& g, int64_t first, int64_t last, int dim, TT* __restrict__ table, int64_t ld) {
+__device__ void zero_rows(const int32_t* __restrict__ sorted, int64_t n, int64_t first, int64_t last, int dim, TT* __restrict__ table,
+                          int64_t ld) {
     __shared__ uint32_t s_there[kNT / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Pack<TT, W> zero;
@@ -116,8 +165,8 @@ __device__ void zero_rows(const Grads& g, int64_t first, int64_t last, int dim, 
         const int64_t r = r0 + threadIdx.x;
         bool there = true;
         if (r < last) {
-            const int64_t at = not_below(g.sorted, 0, g.n, (int)r);
-            there = at < g.n && __ldg(&g.sorted[at]) == (int)r;
+            const int64_t at = not_below(sorted, 0, n, (int)r);
+            there = at < n && __ldg(&sorted[at]) == (int)r;
         }
         const uint32_t word = __ballot_sync(0xffffffffu, there);
         if (lane == 0) s_there[warp] = word;
@@ -138,70 +187,75 @@ __device__ void zero_rows(const Grads& g, int64_t first, int64_t last, int dim, 
     }
 }
 
-template <typename TG, typename TT, int W, int C, int U>
+// a thread's W values of a row
+template <typename T, int W, bool LOOSE>
+struct Values {
+    std::conditional_t<LOOSE, Loose<T>, Pack<T, W>> v;
+    __device__ __forceinline__ void load(const T* row, int c, int dim) {
+        if constexpr (LOOSE) v.load(row, c, dim);
+        else v.load(row + c);
+    }
+    __device__ __forceinline__ void get(float (&x)[W], int c, int dim) const {
+        if constexpr (LOOSE) v.get(x, c, dim);
+        else v.get(x);
+    }
+};
+
+template <typename TG, typename TT, int W, int U, bool LOOSE>
 __global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ sorted, const int32_t* __restrict__ order,
                                                     int64_t max_tokens, const int32_t* n_tokens, int n_rows, int dim,
                                                     const TG* __restrict__ grad, int64_t ld_grad, float scale,
                                                     TT* __restrict__ table, int64_t ld_table, int accumulate, int window, int P,
                                                     int sum_ctas, int rows_per_cta, float* __restrict__ pieces) {
+    static_assert(!LOOSE || W == 8, "eight columns a lane");
+    __shared__ __align__(16) float s_put[LOOSE ? kNT * W : 4];
     let_next_start();
-    const Grads g{sorted, order, live_tokens(n_tokens, max_tokens), n_rows};
+    const int64_t n = live_tokens(n_tokens, max_tokens);
     if ((int)blockIdx.x >= sum_ctas) {
         if (blockIdx.y) return;
         const int64_t first = (int64_t)(blockIdx.x - sum_ctas) * rows_per_cta;
-        zero_rows<TT, W>(g, first, min(first + rows_per_cta, (int64_t)n_rows), dim, table, ld_table);
+        zero_rows<TT, LOOSE ? 1 : W>(sorted, n, first, min(first + rows_per_cta, (int64_t)n_rows), dim, table, ld_table);
         return;
     }
     const int sub = threadIdx.x & (P - 1);
-    const int64_t w = (int64_t)blockIdx.x * (kNT / P) + threadIdx.x / P, begin = w * window, end = min(begin + window, g.n);
+    const int64_t w = (int64_t)blockIdx.x * (kNT / P) + threadIdx.x / P, begin = w * window, end = min(begin + window, n);
     if (begin >= end) return;
-    const int c0 = (int)blockIdx.y * P * W * C + sub * W;
-    bool col[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) col[c] = c0 + c * P * W < dim;
-    if (!col[0]) return;
-    float sum[C][W] = {};
+    const int c = ((int)blockIdx.y * P + sub) * W;
+    if (!LOOSE && c >= dim) return;
+    float* s = LOOSE ? s_put + (threadIdx.x & ~31) * W : nullptr;
+    float sum[W] = {};
     int run = __ldg(&sorted[begin]);
     bool open = begin > 0 && __ldg(&sorted[begin - 1]) == run;             // began before the window
     const auto flush = [&](bool goes_on) {
         if ((unsigned)run < (unsigned)n_rows) {
             if (open || goes_on) {
-                float* piece = pieces + (2 * w + (open ? 0 : 1)) * (int64_t)dim + c0;
-#pragma unroll
-                for (int c = 0; c < C; ++c)
-                    if (col[c]) {
-                        Pack<float, W> v;
-                        v.set(sum[c]);
-                        v.store(piece + c * P * W);
-                    }
+                if (c < dim) {
+                    Pack<float, W> v;
+                    v.set(sum);
+                    v.store(pieces + (2 * w + (open ? 0 : 1)) * piece_pitch(dim) + c);
+                }
             } else {
-#pragma unroll
-                for (int c = 0; c < C; ++c)
-                    if (col[c]) put<TT, W>(table + run * ld_table + c0 + c * P * W, sum[c], scale, accumulate);
+                put<TT, W, LOOSE>(table + run * ld_table, c, dim, sum, scale, accumulate, s);
             }
         }
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < W; ++i) sum[c][i] = 0.f;
+        for (int i = 0; i < W; ++i) sum[i] = 0.f;
         open = false;
     };
     for (int64_t i0 = begin; i0 < end; i0 += U) {
         int key[U], at[U];
-        Pack<TG, W> in[U][C];
+        Values<TG, W, LOOSE> in[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             key[u] = i0 + u < end ? __ldg(&sorted[i0 + u]) : run;
             at[u] = i0 + u < end ? __ldg(&order[i0 + u]) : -1;
-            if ((unsigned)key[u] >= (unsigned)n_rows || at[u] >= g.n) at[u] = -1;
+            if ((unsigned)key[u] >= (unsigned)n_rows || at[u] >= n || c >= dim) at[u] = -1;
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                in[u][c].zero();
-                if (at[u] >= 0 && col[c]) in[u][c].load(grad + at[u] * ld_grad + c0 + c * P * W);
-            }
+        for (int u = 0; u < U; ++u) {
+            in[u].v.zero();
+            if (at[u] >= 0) in[u].load(grad + at[u] * ld_grad, c, dim);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (i0 + u >= end) break;
@@ -209,32 +263,29 @@ __global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ 
                 flush(false);
                 run = key[u];
             }
+            float x[W];
+            in[u].get(x, c, dim);
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                float x[W];
-                in[u][c].get(x);
-#pragma unroll
-                for (int i = 0; i < W; ++i) sum[c][i] += x[i];
-            }
+            for (int i = 0; i < W; ++i) sum[i] += x[i];
         }
     }
-    flush(end < g.n && __ldg(&sorted[end]) == run);
+    flush(end < n && __ldg(&sorted[end]) == run);
 }
 
 // Runs over several windows: their pieces, by the CTA of the window where they begin.  Its groups of P threads take a part of the
 // pieces each, in order, and the parts are added up in order.
-template <typename TT, int W, int C>
+template <typename TT, int W, bool LOOSE>
 __global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__ sorted, int64_t max_tokens, const int32_t* n_tokens,
                                                      int n_rows, int dim, float scale, TT* __restrict__ table, int64_t ld_table,
                                                      int accumulate, int window, int P, const float* __restrict__ pieces) {
-    extern __shared__ float s_sum[];                             // [kNT / P][P * W * C]
+    __shared__ __align__(16) float s_sum[kNT * W];               // [kNT / P][P * W]
     wait_for_last();
     const int64_t n = live_tokens(n_tokens, max_tokens), w = blockIdx.x, end = (w + 1) * window;
     if (end >= n) return;
     const int run = __ldg(&sorted[end]);
-    if (run != __ldg(&sorted[end - 1]) || (unsigned)run >= (unsigned)n_rows) return;
     const int64_t begin = w * window;
-    if (begin > 0 && __ldg(&sorted[begin - 1]) == run) return;   // (it began before: another CTA's)
+    const int before = begin > 0 ? __ldg(&sorted[begin - 1]) : -1;
+    if (run != __ldg(&sorted[end - 1]) || (unsigned)run >= (unsigned)n_rows || before == run) return;      // (or it began before)
     // the window with the run's last token
     int64_t lo = end, hi = n;
     for (int64_t step = window; lo + step < n; step *= 2)
@@ -245,45 +296,34 @@ __global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__
         }
     const int64_t last = (not_below(sorted, lo, hi, run + 1) - 1) / window;
     const int sub = threadIdx.x & (P - 1), side = threadIdx.x / P, sides = kNT / P;
-    const int c0 = (int)blockIdx.y * P * W * C + sub * W;
+    const int c = ((int)blockIdx.y * P + sub) * W;
     const int64_t all = last - w + 1, per = (all + sides - 1) / sides, p0 = min(side * per, all), p1 = min(p0 + per, all);
-    float sum[C][W] = {};
-    constexpr int U = 4;
+    const int64_t pitch = piece_pitch(dim);
+    float sum[W] = {};
+    constexpr int U = 8;
     for (int64_t p = p0; p < p1; p += U) {
-        Pack<float, W> in[U][C];
+        Pack<float, W> in[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            in[u].zero();
+            if (p + u < p1 && c < dim) in[u].load(pieces + (2 * (w + p + u) + (p + u == 0 ? 1 : 0)) * pitch + c);
+        }
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                in[u][c].zero();
-                if (p + u < p1 && c0 + c * P * W < dim)
-                    in[u][c].load(pieces + (2 * (w + p + u) + (p + u == 0 ? 1 : 0)) * (int64_t)dim + c0 + c * P * W);
-            }
+        for (int u = 0; u < U; ++u) {
+            float x[W];
+            in[u].get(x);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                float x[W];
-                in[u][c].get(x);
-#pragma unroll
-                for (int i = 0; i < W; ++i) sum[c][i] += x[i];
-            }
+            for (int i = 0; i < W; ++i) sum[i] += x[i];
+        }
     }
-    const int width = P * W * C;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < W; ++i) s_sum[side * width + (c * W + i) * P + sub] = sum[c][i];
+    for (int i = 0; i < W; ++i) s_sum[side * P * W + i * P + sub] = sum[i];
     __syncthreads();
     if (side) return;
     for (int s = 1; s < sides && s * per < all; ++s)
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < W; ++i) sum[c][i] += s_sum[s * width + (c * W + i) * P + sub];
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-        if (c0 + c * P * W < dim) put<TT, W>(table + run * ld_table + c0 + c * P * W, sum[c], scale, accumulate);
+        for (int i = 0; i < W; ++i) sum[i] += s_sum[s * P * W + i * P + sub];
+    if (LOOSE || c < dim) put<TT, W, LOOSE>(table + run * ld_table, c, dim, sum, scale, accumulate, s_sum);
 }
 
 // ---- arguments ------------------------------------------------------------------------------------------------------------
@@ -311,39 +351,45 @@ Workspace layout(void* p, int64_t max_tokens) {
 template <typename TT, typename TO>
 int32_t launch_embed(int64_t n_rows, int64_t dim, const void* table, int64_t ld_table, const int32_t* tokens, int64_t max_tokens,
                      const int32_t* n_tokens, float scale, void* out, int64_t ld_out, int32_t* status, bool whole, cudaStream_t stream) {
-    constexpr int N = 8;               // (the 16 bytes of a 16-bit type)
-    const int64_t vectors = whole ? dim / N : dim, items = max_tokens * vectors, ctas = div_up(items, kNT * (whole ? 2 : 4));
+    constexpr int N = 8, U = 2;        // (the 16 bytes of a 16-bit type)
+    const int64_t vectors = whole ? dim / N : (dim + 16 / (int)sizeof(TO) - 1 + N - 1) / N, items = max_tokens * vectors;
+    const int64_t ctas = div_up(items, kNT * (whole ? U : 1));
     if (ctas > 0x7fffffff || items >= (int64_t(1) << 40)) return HL_EINVAL;
-    HL_CUDA_TRY(launch(whole ? k_token_embed<TT, TO, N, 2> : k_token_embed<TT, TO, 1, 4>, (unsigned)ctas, kNT, stream,
-                       static_cast<const TT*>(table), ld_table, (unsigned)n_rows, tokens, max_tokens, n_tokens, scale,
-                       static_cast<TO*>(out), ld_out, (int)vectors, inverse_of(vectors), status));
+    const TT* t = static_cast<const TT*>(table);
+    TO* o = static_cast<TO*>(out);
+    if (whole)
+        HL_CUDA_TRY(launch(k_token_embed<TT, TO, N, U>, (unsigned)ctas, kNT, stream, t, ld_table, (unsigned)n_rows, tokens, max_tokens,
+                           n_tokens, scale, o, ld_out, (int)vectors, inverse_of(vectors), status));
+    else
+        HL_CUDA_TRY(launch(k_token_embed_loose<TT, TO>, (unsigned)ctas, kNT, stream, t, ld_table, (unsigned)n_rows, tokens, max_tokens,
+                           n_tokens, scale, (int)dim, o, ld_out, (int)vectors, inverse_of(vectors), status));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
 }
 
-template <typename TG, typename TT, int W, int C, int U>
+template <typename TG, typename TT, int W, int U, bool LOOSE>
 int32_t launch_sums(int64_t n_rows, int64_t dim, const int32_t* sorted, const int32_t* order, int64_t max_tokens,
                     const int32_t* n_tokens, const void* grad, int64_t ld_grad, float scale, void* table, int64_t ld_table,
                     int accumulate, float* pieces, cudaStream_t stream) {
-    int P = 1;
-    while (P < kNT && P * W * C < dim) P *= 2;
-    const int window = window_of(max_tokens);
-    const int64_t passes = div_up(dim, P * W * C), windows = div_up(max_tokens, window), sums = div_up(windows, kNT / P);
+    int P = LOOSE ? 32 : 1;
+    while (!LOOSE && P < kNT && P * W < dim) P *= 2;
+    const int window = window_of(max_tokens), Q = P < 32 ? P : 32;         // Q: of the joins, eight warps of which share a run's pieces
+    const int64_t windows = div_up(max_tokens, window), sums = div_up(windows, kNT / P);
     // rows without tokens: some 128 KB a CTA
     int64_t per = (128 << 10) / (dim * (int64_t)sizeof(TT));
     per = per < 1 ? 1 : per > kNT ? kNT : per;
     const int64_t zeros = accumulate ? 0 : div_up(n_rows, per);
-    if (sums + zeros > 0x7fffffff || passes > 65535 || windows > 0x7fffffff) return HL_EINVAL;
+    if (sums + zeros > 0x7fffffff || div_up(dim, Q * W) > 65535 || windows > 0x7fffffff) return HL_EINVAL;
     if (sums + zeros == 0) return HL_OK;
-    HL_CUDA_TRY(launch(k_token_sums<TG, TT, W, C, U>, dim3((unsigned)(sums + zeros), (unsigned)passes), kNT, stream, sorted, order,
-                       max_tokens, n_tokens, (int)n_rows, (int)dim, static_cast<const TG*>(grad), ld_grad, scale,
+    HL_CUDA_TRY(launch(k_token_sums<TG, TT, W, U, LOOSE>, dim3((unsigned)(sums + zeros), (unsigned)div_up(dim, P * W)), kNT, stream,
+                       sorted, order, max_tokens, n_tokens, (int)n_rows, (int)dim, static_cast<const TG*>(grad), ld_grad, scale,
                        static_cast<TT*>(table), ld_table, accumulate, window, P, (int)sums, (int)per, pieces));
     note_launches(1);
     if (windows > 1) {
-        HL_CUDA_TRY(launch_after(k_token_joins<TT, W, C>, dim3((unsigned)(windows - 1), (unsigned)passes), kNT,
-                                 kNT * W * C * sizeof(float), stream, sorted, max_tokens, n_tokens, (int)n_rows, (int)dim, scale,
-                                 static_cast<TT*>(table), ld_table, accumulate, window, P, (const float*)pieces));
+        HL_CUDA_TRY(launch_after(k_token_joins<TT, W, LOOSE>, dim3((unsigned)(windows - 1), (unsigned)div_up(dim, Q * W)), kNT, 0, stream,
+                                 sorted, max_tokens, n_tokens, (int)n_rows, (int)dim, scale, static_cast<TT*>(table), ld_table, accumulate,
+                                 window, Q, (const float*)pieces));
         note_launches(1);
     }
     HL_LAUNCH_CHECK();
@@ -377,7 +423,7 @@ extern "C" int32_t hl_token_embed(int32_t table_dtype, int64_t n_rows, int64_t d
 extern "C" size_t hl_token_workspace_bytes(int64_t max_tokens, int64_t dim) {
     if (!tokens_ok(max_tokens) || dim < 1 || dim > (int64_t(1) << 24)) return 0;
     const int64_t sort = (2 * padded(max_tokens) + padded(sort_hist_words(max_tokens))) * 4;
-    const int64_t sums = 2 * div_up(max_tokens, window_of(max_tokens)) * dim * 4;
+    const int64_t sums = 2 * div_up(max_tokens, window_of(max_tokens)) * (div_up(dim, kPieceStep) * kPieceStep) * 4;
     return (size_t)(kWorkspaceHead + ((sort > sums ? sort : sums) + 255) / 256 * 256);
 }
 
@@ -423,11 +469,11 @@ extern "C" int32_t hl_token_embed_bwd(int64_t n_rows, int64_t dim, const int32_t
                        rows_lie_at(table_dtype, d_grad_table, ld_table, 8) &&
                        (N * dtype_size(table_dtype) == 8 || rows_lie_at(table_dtype, d_grad_table, ld_table, 16));
     float* pieces = layout(d_workspace, max_tokens).pieces;
-#define HL_SUMS(TG, TT)                                                                                                         \
-    (whole ? launch_sums<TG, TT, 16 / sizeof(TG), 1, 8>(n_rows, dim, d_sorted, d_order, max_tokens, d_n_tokens, d_grad_out, ld_grad, \
-                                                        scale, d_grad_table, ld_table, accumulate, pieces, stream)              \
-           : launch_sums<TG, TT, 1, 4, 8>(n_rows, dim, d_sorted, d_order, max_tokens, d_n_tokens, d_grad_out, ld_grad, scale,  \
-                                          d_grad_table, ld_table, accumulate, pieces, stream))
+#define HL_SUMS(TG, TT)                                                                                                           \
+    (whole ? launch_sums<TG, TT, 16 / sizeof(TG), 8, false>(n_rows, dim, d_sorted, d_order, max_tokens, d_n_tokens, d_grad_out,  \
+                                                            ld_grad, scale, d_grad_table, ld_table, accumulate, pieces, stream)  \
+           : launch_sums<TG, TT, 8, 4, true>(n_rows, dim, d_sorted, d_order, max_tokens, d_n_tokens, d_grad_out, ld_grad, scale, \
+                                             d_grad_table, ld_table, accumulate, pieces, stream))
 #define HL_SUMS_TO(TG) \
     (table_dtype == HL_F32 ? HL_SUMS(TG, float) : table_dtype == HL_BF16 ? HL_SUMS(TG, __nv_bfloat16) : HL_SUMS(TG, __half))
     return grad_dtype == HL_F32 ? HL_SUMS_TO(float) : grad_dtype == HL_BF16 ? HL_SUMS_TO(__nv_bfloat16) : HL_SUMS_TO(__half);
