@@ -13,7 +13,7 @@ namespace {
 // whose logits are random.
 template <int ITEMS, int P>
 struct Shape {
-    static constexpr int kNT = 128;
+    static constexpr int kNT = 128, kCtas = ITEMS == 8 ? 8 : ITEMS == 16 ? 5 : 1;       // threads; CTAs of a multiprocessor
     static constexpr int kTokens = kNT / P;                      // of a CTA
     static constexpr int kExperts = ITEMS * P;                   // at most
     static constexpr int kChosen = kExperts < HL_MAX_TOP_K ? kExperts : HL_MAX_TOP_K;
@@ -70,7 +70,6 @@ __device__ __forceinline__ float max_of(float v) {
 template <int P>
 __device__ __forceinline__ unsigned lanes_of(int lane) { return P == 32 ? kAll : ((1u << (P & 31)) - 1u) << (lane & ~(P - 1) & 31); }
 
-__device__ __forceinline__ float sigmoid(float l) { return 1.f / (1.f + expf(-l)); }
 __device__ __forceinline__ double sigmoid(double l) { return 1.0 / (1.0 + exp(-l)); }
 // e^(l - m) for l <= m, where both may be infinite
 __device__ __forceinline__ float part(float l, float m) { return l == m ? 1.f : expf(l - m); }
@@ -275,17 +274,17 @@ __device__ __forceinline__ bool choose_few(int top_k, const float (&key)[ITEMS],
 
 // Bound by its instructions where there are many tokens.  WHOLE: rows are read in pieces of 16 bytes.
 template <typename T, int ITEMS, int P, bool WHOLE>
-__global__ void __launch_bounds__(Shape<ITEMS, P>::kNT) k_expert_choose(const T* __restrict__ logits, int64_t ld,
+__global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) k_expert_choose(const T* __restrict__ logits, int64_t ld,
                                                                         const float* __restrict__ bias, const int32_t* n_tokens,
-                                                                        int64_t max_tokens, int top_k, int E, int G, int top_groups,
-                                                                        int flags, float scale, int32_t* __restrict__ experts,
+                                                                        int64_t max_tokens, int top_k, int E, int G, int per_group,
+                                                                        unsigned group_magic, int top_groups, int flags,
+                                                                        float scale, int32_t* __restrict__ experts,
                                                                         float* __restrict__ weights, int32_t* status) {
     using S = Shape<ITEMS, P>;
     __shared__ int32_t s_chosen[S::kTokens][S::kChosen];
     __shared__ float2 s_few[P >= 16 ? S::kNT : 1];
     extern __shared__ double s_base[];                           // with groups that are not whole lanes', of every token: [E + 2 G]
-    const Router r{top_k, E, G, E / G, top_groups, ((1u << 21) + E / G - 1) / (unsigned)(E / G), (flags & kSoftmax) != 0,
-                   (flags & kPair) != 0, (flags & kRenorm) != 0};
+    const Router r{top_k, E, G, per_group, top_groups, group_magic, (flags & kSoftmax) != 0, (flags & kPair) != 0, (flags & kRenorm) != 0};
     const bool whole_lanes = flags & kWholeLanes;
     const int q = threadIdx.x % P, mine = threadIdx.x / P;
     int64_t tokens = max_tokens;
@@ -583,20 +582,19 @@ int flags_of(const hl_router* r) {
     return (r->score == HL_SCORE_SOFTMAX ? kSoftmax : 0) | (r->group_score == HL_GROUP_TOP2 ? kPair : 0) | (r->renorm ? kRenorm : 0);
 }
 
-// As few lanes a token as hold its experts, eight a lane; above 128 experts sixteen, as most steps take a warp the same time
-// however many tokens it has; above 512 more.
+// As few lanes a token as hold its experts, eight a lane; above 256 experts more.
 #define HL_SHAPES(E, RUN, WHOLE)                                                                                        \
     ((E) <= 8     ? RUN(8, 1, WHOLE)                                                                                    \
      : (E) <= 16  ? RUN(8, 2, WHOLE)                                                                                    \
      : (E) <= 32  ? RUN(8, 4, WHOLE)                                                                                    \
      : (E) <= 64  ? RUN(8, 8, WHOLE)                                                                                    \
      : (E) <= 128 ? RUN(8, 16, WHOLE)                                                                                   \
-     : (E) <= 256 ? RUN(16, 16, WHOLE)                                                                                  \
+     : (E) <= 256 ? RUN(8, 32, WHOLE)                                                                                   \
      : (E) <= 512 ? RUN(16, 32, WHOLE)                                                                                  \
                   : RUN(32, 32, WHOLE))
 // whether a group is the experts of 1, 2, 4 ... of these lanes
 bool whole_lanes(const hl_router* r) {
-    const int items = r->n_experts <= 128 ? 8 : r->n_experts <= 512 ? 16 : 32, per = r->n_experts / r->n_groups, lanes = per / items;
+    const int items = r->n_experts <= 256 ? 8 : r->n_experts <= 512 ? 16 : 32, per = r->n_experts / r->n_groups, lanes = per / items;
     return per % items == 0 && (lanes & (lanes - 1)) == 0;
 }
 
@@ -604,11 +602,12 @@ template <typename T>
 int32_t launch_choose(const hl_router* r, const void* logits, int64_t ld, const float* bias, int64_t max_tokens,
                       const int32_t* n_tokens, int32_t* experts, float* weights, int32_t* status, cudaStream_t stream) {
     const bool lanes = whole_lanes(r);
+    const int per = r->n_experts / r->n_groups;
 #define HL_RUN(ITEMS, P, WHOLE)                                                                                               \
     launch_cluster(k_expert_choose<T, ITEMS, P, WHOLE>, (unsigned)div_up(max_tokens, Shape<ITEMS, P>::kTokens), Shape<ITEMS, P>::kNT, \
                    r->n_groups > 1 && !lanes ? Shape<ITEMS, P>::kTokens * (r->n_experts + 2 * r->n_groups) * sizeof(double) : 0, 0,      \
                    stream, static_cast<const T*>(logits), ld, bias, n_tokens, max_tokens, r->top_k, r->n_experts, r->n_groups, \
-                   r->top_groups, flags_of(r) | (lanes ? kWholeLanes : 0), r->scale, experts, weights, status)
+                   per, ((1u << 21) + per - 1) / (unsigned)per, r->top_groups, flags_of(r) | (lanes ? kWholeLanes : 0), r->scale, experts, weights, status)
     const bool whole = r->n_experts % (16 / (int)sizeof(T)) == 0 && lies_at(logits, 16) && ld * sizeof(T) % 16 == 0 &&
                        lies_at(bias, 16);
     if (whole) HL_CUDA_TRY(HL_SHAPES(r->n_experts, HL_RUN, true));

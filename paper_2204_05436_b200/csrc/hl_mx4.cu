@@ -344,28 +344,43 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                  : "memory");
 }
 
-// Where an operand lies in shared memory, as the tensor cores want it said: address, bytes from one group of eight rows to the
-// next, and whether pieces of 16 bytes are in the order of the tiles' values (or of their exponents: as they come).
-__device__ __forceinline__ uint64_t operand(uint32_t address, uint32_t group_bytes, bool ordered) {
-    return (uint64_t)((address & 0x3ffffu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(group_bytes >> 4) << 32 | (uint64_t)1 << 46 |
-           (uint64_t)(ordered ? 2 : 0) << 61;
-}
-__device__ __forceinline__ void exponents_to_tmem(uint32_t tmem, uint32_t address) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(operand(address, 128, false)) : "memory");
+// Where an operand lies in shared memory, as the tensor cores want it said: the address in 16 bytes (the lower half, which alone
+// changes from one to the next), bytes from one group of eight rows to the next, and whether pieces of 16 bytes are in the order of
+// the tiles' values (or of their exponents: as they come).
+constexpr uint32_t kOrderedHigh = (1024u >> 4) | 1u << 14 | 2u << 29, kPlainHigh = (128u >> 4) | 1u << 14;
+__device__ __forceinline__ uint32_t operand_low(uint32_t address) { return (address & 0x3ffffu) >> 4 | 1u << 16; }
+__device__ __forceinline__ uint64_t operand(uint32_t low, uint32_t high) { return (uint64_t)high << 32 | low; }
+
+// These are for one thread: `one` says who.  (The warp's threads go through the loop together, so that what is the same in all of them
+// stays in the registers that the tensor cores' instructions take; with the loop in one thread alone each of them took some 200
+// cycles to put together.)
+__device__ __forceinline__ void exponents_to_tmem(bool one, uint32_t tmem, uint32_t low) {
+    asm volatile("{\n\t.reg .pred o;\n\tsetp.ne.b32 o, %2, 0;\n\t@o tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(tmem),
+                 "l"(operand(low, kPlainHigh)), "r"((uint32_t)one)
+                 : "memory");
 }
 // 64 of d: both operands of e2m1 (code 1 in bits 7 and 10), exponents alone as factors (bit 23), 128 by n, the pair of each row's
 // four exponents that counts
-__device__ __forceinline__ void multiply(uint32_t acc, uint64_t a, uint64_t b, uint32_t n, int pair, uint32_t ea, uint32_t eb, bool add) {
-    const uint32_t what = (uint32_t)(2 * pair) << 4 | 1u << 7 | 1u << 10 | (n >> 3) << 17 | 1u << 23 | (128u >> 4) << 24 |
-                          (uint32_t)(2 * pair) << 29;
+__device__ __forceinline__ uint32_t multiplication(uint32_t n, int pair) {
+    return (uint32_t)(2 * pair) << 4 | 1u << 7 | 1u << 10 | (n >> 3) << 17 | 1u << 23 | (128u >> 4) << 24 | (uint32_t)(2 * pair) << 29;
+}
+__device__ __forceinline__ void multiply(bool one, uint32_t acc, uint32_t a, uint32_t b, uint32_t what, uint32_t ea, uint32_t eb, bool add) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(acc),
-        "l"(a), "l"(b), "r"(what), "r"(ea), "r"(eb), "r"((uint32_t)add)
+        "{\n\t.reg .pred p, o;\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 o, %7, 0;\n\t"
+        "@o tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(acc),
+        "l"(operand(a, kOrderedHigh)), "l"(operand(b, kOrderedHigh)), "r"(what), "r"(ea), "r"(eb), "r"((uint32_t)add), "r"((uint32_t)one)
         : "memory");
 }
-__device__ __forceinline__ void commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+__device__ __forceinline__ void commit(bool one, uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .pred o;\n\tsetp.ne.b32 o, %1, 0;\n\t"
+        "@o tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)), "r"((uint32_t)one)
+        : "memory");
+}
+__device__ __forceinline__ bool elected() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one;
 }
 
 // 32 columns of a warp's 32 lanes
@@ -468,39 +483,38 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            int stage = 0, buffer = 0;
-            uint32_t phase = 0, taken = 1;
-            bool ok = true;
-            for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-                const Item it = item_of(i, f_tiles, experts, s_first);
-                const uint32_t n = (it.rows + 15) & ~15, acc = tmem + buffer * kAccCols;
-                if (!(ok = bar_wait(&s_taken[buffer], taken, &s_gave_up))) break;
+        const bool one = elected();
+        const uint32_t base_low = operand_low(__shfl_sync(0xffffffffu, smem_u32(base), 0)), d = __shfl_sync(0xffffffffu, tmem, 0);
+        int stage = 0, buffer = 0;
+        uint32_t phase = 0, taken = 1;
+        bool ok = true;
+        for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
+            const uint32_t n = __shfl_sync(0xffffffffu, (item_of(i, f_tiles, experts, s_first).rows + 15) & ~15, 0);
+            const uint32_t acc = d + buffer * kAccCols, what0 = multiplication(n, 0), what1 = multiplication(n, 1);
+            if (!(ok = bar_wait(&s_taken[buffer], taken, &s_gave_up))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            for (int c = 0; c < col_tiles; ++c) {
+                if (!(ok = bar_wait(&s_full[stage], phase, &s_gave_up))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int c = 0; c < col_tiles; ++c) {
-                    if (!(ok = bar_wait(&s_full[stage], phase, &s_gave_up))) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t at = smem_u32(base + stage * kStageBytes);
-                    const uint32_t ea = tmem + kExponentCols + (stage & 1) * 16, eb = ea + 8;
+                const uint32_t a = base_low + stage * (kStageBytes >> 4), b = a + (kTileBytes >> 4);
+                const uint32_t ea = d + kExponentCols + (stage & 1) * 16, eb = ea + 8;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        exponents_to_tmem(ea + 4 * h, at + kValueBytes + 512 * h);
-                        exponents_to_tmem(eb + 4 * h, at + kTileBytes + kValueBytes + 512 * h);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        multiply(acc, operand(at + 32 * k, 1024, true), operand(at + kTileBytes + 32 * k, 1024, true), n, k & 1,
-                                 ea + 4 * (k >> 1), eb + 4 * (k >> 1), c > 0 || k > 0);
-                    commit(&s_empty[stage]);
-                    if (++stage == kStages) {
-                        stage = 0;
-                        phase ^= 1;
-                    }
+                for (int h = 0; h < 2; ++h) {
+                    exponents_to_tmem(one, ea + 4 * h, a + ((kValueBytes + 512 * h) >> 4));
+                    exponents_to_tmem(one, eb + 4 * h, b + ((kValueBytes + 512 * h) >> 4));
                 }
-                commit(&s_sums[buffer]);
-                buffer ^= 1;
-                taken ^= buffer == 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    multiply(one, acc, a + 2 * k, b + 2 * k, k & 1 ? what1 : what0, ea + 4 * (k >> 1), eb + 4 * (k >> 1), c > 0 || k > 0);
+                commit(one, &s_empty[stage]);
+                if (++stage == kStages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
             }
+            commit(one, &s_sums[buffer]);
+            buffer ^= 1;
+            taken ^= buffer == 0;
         }
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;    // the lanes of the tensor memory that this warp can read; its columns
