@@ -16,9 +16,15 @@ static_assert(kTileBytes == 17408 && kTileBytes % 1024 == 0, "tiles side by side
 
 // a lane's eight values among the 256 of a row's part: lanes 4b .. 4b + 3 have block b
 __device__ __forceinline__ int value_at(int row, int lane) { return row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + ((lane & 3) << 2); }
+// a block's exponent, behind the values
 __device__ __forceinline__ int exponent_at(int row, int block) {
-    return kValueBytes + (block >> 2) * 512 + (row & 31) * 16 + (row >> 5) * 4 + (block & 3);
+    return (row >> 7) * 1024 + (block >> 2) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
 }
+
+// The rows that experts get lie in tiles of 240: as many columns as the tensor memory has room for twice, next to the exponents.  The
+// exponents of rows 128 to 239 lie behind those of the first 128.
+constexpr int kPanelRows = 240, kPanelValueBytes = kPanelRows * kTileCols / 2, kPanelBytes = kPanelValueBytes + 2048;
+static_assert(kPanelBytes == 32768 && kPanelValueBytes % 1024 == 0, "as above");
 
 // A row's part from column c on, eight values a lane, as they are; zeros behind its end and where there is no row.
 template <typename T, bool WHOLE>
@@ -90,9 +96,9 @@ __device__ __forceinline__ uint32_t to_four_bits(const Part<T, WHOLE>& part, uin
     return packed;
 }
 
-__device__ __forceinline__ void store_part(uint8_t* tile, int row, int lane, uint32_t packed, uint32_t exponent) {
+__device__ __forceinline__ void store_part(uint8_t* tile, int row, int lane, uint32_t packed, uint32_t exponent, int exponents_from) {
     *reinterpret_cast<uint32_t*>(tile + value_at(row, lane)) = packed;
-    if ((lane & 3) == 0) tile[exponent_at(row, lane >> 2)] = (uint8_t)exponent;
+    if ((lane & 3) == 0) tile[exponents_from + exponent_at(row, lane >> 2)] = (uint8_t)exponent;
 }
 
 constexpr int kRowNT = 256;
@@ -125,7 +131,7 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_quantise(const T* __restrict__ x
         if (ct + u >= col_tiles) break;
         uint32_t e;
         const uint32_t packed = to_four_bits(in[u], &e);
-        store_part(tile + u * kTileBytes, r, lane, packed, e);
+        store_part(tile + u * kTileBytes, r, lane, packed, e, kValueBytes);
     }
 }
 
@@ -166,7 +172,7 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_dequantise(const uint8_t* __rest
             packed[u][i] = E[u][i] = 0;
             if (ct + u >= col_tiles) continue;
             packed[u][i] = N == 8 ? __ldg(reinterpret_cast<const uint32_t*>(p)) : __ldg(reinterpret_cast<const unsigned short*>(p));
-            E[u][i] = __ldg(tile + u * kTileBytes + exponent_at(r, c >> 5));
+            E[u][i] = __ldg(tile + u * kTileBytes + kValueBytes + exponent_at(r, c >> 5));
         }
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -189,7 +195,7 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_dequantise(const uint8_t* __rest
 }
 
 // ---- the experts' rows ------------------------------------------------------------------------------------------------
-// Expert e's rows are cut into tiles of 128 of their own, wherever they begin in the expert-ordered buffers: first[e] is its first
+// Expert e's rows are cut into tiles of 240 of their own, wherever they begin in the expert-ordered buffers: first[e] is its first
 // tile's number, first[E] how many there are (never more than the workspace holds).
 struct Experts {
     const int32_t *counts, *offsets;
@@ -213,7 +219,7 @@ __device__ void tile_numbers(const Experts& x, int most, int* s_first, int* s_be
         if (e >= x.E) continue;
         const int from = x.begin(e);
         if (s_begin) s_begin[e] = from;
-        tiles[k] = (x.rows(e, from) + kTileRows - 1) / kTileRows;
+        tiles[k] = (x.rows(e, from) + kPanelRows - 1) / kPanelRows;
         sum += tiles[k];
     }
     int incl = sum;
@@ -281,9 +287,9 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, in
             else if (k0 + lane < top_k) at = __ldg(&place[row * top_k + k0 + lane]);
             if (at >= 0 && at < cap_rows) {
                 // (experts without rows begin where the next does: the last that begins there is the one)
-                const int e = last_not_above(s_begin, E, at), r = at - s_begin[e], tile = s_first[e] + r / kTileRows;
+                const int e = last_not_above(s_begin, E, at), r = at - s_begin[e], tile = s_first[e] + r / kPanelRows;
                 if (r >= 0 && r < experts.rows(e, s_begin[e]) && tile < s_first[e + 1])
-                    to = (int64_t)tile * kTileRows + (r & (kTileRows - 1));
+                    to = (int64_t)tile << 8 | (r - r / kPanelRows * kPanelRows);
             }
             if (k0 == 0) {
 #pragma unroll
@@ -291,10 +297,11 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, in
             }
             for (unsigned left = __ballot_sync(0xffffffffu, to >= 0); left; left &= left - 1) {
                 const int64_t dst = __shfl_sync(0xffffffffu, to, __ffs(left) - 1);
-                uint8_t* tile = q + ((dst >> 7) * col_tiles + ct0) * kTileBytes;
+                uint8_t* tile = q + ((dst >> 8) * col_tiles + ct0) * kPanelBytes;
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-                    if (ct0 + u < col_tiles) store_part(tile + u * kTileBytes, (int)(dst & (kTileRows - 1)), lane, packed[u], exponent[u]);
+                    if (ct0 + u < col_tiles)
+                        store_part(tile + u * kPanelBytes, (int)(dst & 255), lane, packed[u], exponent[u], kPanelValueBytes);
             }
         }
     }
@@ -302,11 +309,10 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, in
 
 // ---- the product --------------------------------------------------------------------------------------------------------
 // y[row, f] = sum over d of x[row, d] * w[e, f, d] for the rows of expert e: 128 outputs f (the lanes of the tensor memory) by up to
-// 128 rows (its columns) at a time, 256 of d a step.  One warp's thread has the tiles of a step copied, one issues the products,
+// 240 rows (its columns) at a time, 256 of d a step.  One warp's thread has the tiles of a step copied, one issues the products,
 // eight warps take the sums out, those of one tile while the next one's are made.
-constexpr int kStages = 6, kStageBytes = 2 * kTileBytes, kProductNT = 320;
-constexpr int kAccCols = 128;          // tensor-memory columns of a tile's sums (two tiles'), then those of the exponents
-constexpr uint32_t kExponentCols = 2 * kAccCols;
+constexpr int kStages = 4, kStageBytes = kTileBytes + kPanelBytes, kProductNT = 320;
+constexpr uint32_t kExponentCols = 2 * kPanelRows;               // tensor-memory columns: two tiles' sums, 8 of w's exponents, 16 of x'
 constexpr int kProductSmem = kStages * kStageBytes + 1024 + (HL_MAX_EXPERTS + 1) * 4 + 256;
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -407,8 +413,8 @@ __device__ __forceinline__ Item item_of(int64_t i, int f_tiles, const Experts& x
     it.tile = i / f_tiles;
     it.f = (int)(i - it.tile * f_tiles);
     it.e = last_not_above(s_first, x.E, (int)it.tile);
-    const int begin = x.begin(it.e), rows = x.rows(it.e, begin), at = ((int)it.tile - s_first[it.e]) * kTileRows;
-    it.rows = min(rows - at, kTileRows);
+    const int begin = x.begin(it.e), rows = x.rows(it.e, begin), at = ((int)it.tile - s_first[it.e]) * kPanelRows;
+    it.rows = min(rows - at, kPanelRows);
     it.row0 = (int64_t)begin + at;
     const int64_t end = min((int64_t)max(__ldg(&x.offsets[it.e + 1]), 0), x.cap_rows);
     it.pad = it.tile + 1 == s_first[it.e + 1] ? max(end - begin - rows, (int64_t)0) : 0;
@@ -459,15 +465,15 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
             for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
                 const Item it = item_of(i, f_tiles, experts, s_first);
                 const uint8_t* a = wq + ((int64_t)it.e * f_tiles + it.f) * col_tiles * kTileBytes;
-                const uint8_t* b = xq + it.tile * col_tiles * kTileBytes;
-                const uint32_t b_bytes = ((it.rows + 15) & ~15) * 128;
-                for (int c = 0; c < col_tiles; ++c, a += kTileBytes, b += kTileBytes) {
+                const uint8_t* b = xq + it.tile * col_tiles * kPanelBytes;
+                const uint32_t b_bytes = ((it.rows + 15) & ~15) * 128, e_bytes = it.rows > kTileRows ? 2048 : 1024;
+                for (int c = 0; c < col_tiles; ++c, a += kTileBytes, b += kPanelBytes) {
                     if (!(ok = bar_wait(&s_empty[stage], phase, &s_gave_up))) break;
                     const uint32_t at = smem_u32(base + stage * kStageBytes);
-                    bar_expect(&s_full[stage], kTileBytes + b_bytes + (kTileBytes - kValueBytes));
+                    bar_expect(&s_full[stage], kTileBytes + b_bytes + e_bytes);
                     bulk_load(at, a, kTileBytes, &s_full[stage]);
                     bulk_load(at + kTileBytes, b, b_bytes, &s_full[stage]);
-                    bulk_load(at + kTileBytes + kValueBytes, b + kValueBytes, kTileBytes - kValueBytes, &s_full[stage]);
+                    bulk_load(at + kTileBytes + kPanelValueBytes, b + kPanelValueBytes, e_bytes, &s_full[stage]);
                     if (++stage == kStages) {
                         stage = 0;
                         phase ^= 1;
@@ -490,22 +496,24 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
         bool ok = true;
         for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
             const uint32_t n = __shfl_sync(0xffffffffu, (item_of(i, f_tiles, experts, s_first).rows + 15) & ~15, 0);
-            const uint32_t acc = d + buffer * kAccCols, what0 = multiplication(n, 0), what1 = multiplication(n, 1);
+            const uint32_t acc = d + buffer * kPanelRows, what0 = multiplication(n, 0), what1 = multiplication(n, 1);
             if (!(ok = bar_wait(&s_taken[buffer], taken, &s_gave_up))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             for (int c = 0; c < col_tiles; ++c) {
                 if (!(ok = bar_wait(&s_full[stage], phase, &s_gave_up))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t a = base_low + stage * (kStageBytes >> 4), b = a + (kTileBytes >> 4);
-                const uint32_t ea = d + kExponentCols + (stage & 1) * 16, eb = ea + 8;
+                // (copies and products run in the order in which they are issued)
+                const uint32_t ea = d + kExponentCols, eb = ea + 8;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     exponents_to_tmem(one, ea + 4 * h, a + ((kValueBytes + 512 * h) >> 4));
-                    exponents_to_tmem(one, eb + 4 * h, b + ((kValueBytes + 512 * h) >> 4));
+                    exponents_to_tmem(one, eb + 8 * h, b + ((kPanelValueBytes + 512 * h) >> 4));
+                    if (n > kTileRows) exponents_to_tmem(one, eb + 8 * h + 4, b + ((kPanelValueBytes + 1024 + 512 * h) >> 4));
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    multiply(one, acc, a + 2 * k, b + 2 * k, k & 1 ? what1 : what0, ea + 4 * (k >> 1), eb + 4 * (k >> 1), c > 0 || k > 0);
+                    multiply(one, acc, a + 2 * k, b + 2 * k, k & 1 ? what1 : what0, ea + 4 * (k >> 1), eb + 8 * (k >> 1), c > 0 || k > 0);
                 commit(one, &s_empty[stage]);
                 if (++stage == kStages) {
                     stage = 0;
@@ -526,10 +534,10 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             __syncwarp();
             const int64_t f = (int64_t)it.f * kTileRows + quarter * 32 + lane;
-            const int end = min(it.rows, (half + 1) * (kTileRows / 2));
-            for (int c0 = half * (kTileRows / 2); c0 < end; c0 += 32) {
+            const int middle = min((it.rows + 31) / 32 * 16, it.rows), end = half ? it.rows : middle;
+            for (int c0 = half ? middle : 0; c0 < end; c0 += 32) {
                 uint32_t v[32];
-                tmem_load(v, tmem + buffer * kAccCols + c0 + ((uint32_t)(quarter * 32) << 16));
+                tmem_load(v, tmem + buffer * kPanelRows + c0 + ((uint32_t)(quarter * 32) << 16));
                 if (f >= outputs) continue;
                 T* out = y + (it.row0 + c0) * ld + f;
                 if (c0 + 32 <= end) {
@@ -571,7 +579,7 @@ bool matrix_dims_ok(int64_t rows, int64_t dim) { return rows >= 0 && rows < (int
 Divisor divisor(int64_t d) { return {d == 1 ? 0 : ~0ull / (uint64_t)d + 1, d}; }
 
 constexpr int64_t kWorkspaceHead = 1024;
-int64_t row_tiles_most(int64_t cap_rows, int64_t E) { return cap_rows / kTileRows + (E < cap_rows ? E : cap_rows); }
+int64_t row_tiles_most(int64_t cap_rows, int64_t E) { return cap_rows / kPanelRows + (E < cap_rows ? E : cap_rows); }
 
 // Parts of a row that a warp takes: as many as there are, up to four.
 int parts_of(int64_t col_tiles) { return col_tiles >= 3 ? 4 : (int)col_tiles; }
@@ -670,7 +678,7 @@ extern "C" size_t hl_expert_mx4_workspace_bytes(int64_t cap_rows, int32_t n_expe
     if (cap_rows < 0 || cap_rows >= (int64_t(1) << 31) - 65536 || n_experts < 1 || n_experts > HL_MAX_EXPERTS || dim < 1 ||
         dim > (int64_t(1) << 24))
         return 0;
-    return (size_t)(kWorkspaceHead + row_tiles_most(cap_rows, n_experts) * tiles_of(dim, kTileCols) * kTileBytes);
+    return (size_t)(kWorkspaceHead + row_tiles_most(cap_rows, n_experts) * tiles_of(dim, kTileCols) * kPanelBytes);
 }
 
 extern "C" int32_t hl_expert_mx4(const hl_route* route, int32_t dtype, int64_t dim, int64_t outputs, const void* d_x, int64_t ld_x,
