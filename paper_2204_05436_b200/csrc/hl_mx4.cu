@@ -31,7 +31,7 @@ template <typename T, bool WHOLE>
 struct Part {
     static constexpr int kWords = 8 * (int)sizeof(T) / 4;
     uint32_t w[kWords];
-    __device__ __forceinline__ void load(const T* row, int64_t c, int64_t dim) {
+    __device__ __forceinline__ void load(const T* row, int c, int dim) {
 #pragma unroll
         for (int i = 0; i < kWords; ++i) w[i] = 0;
         if (!row) return;
@@ -96,10 +96,6 @@ __device__ __forceinline__ uint32_t to_four_bits(const Part<T, WHOLE>& part, uin
     return packed;
 }
 
-__device__ __forceinline__ void store_part(uint8_t* tile, int row, int lane, uint32_t packed, uint32_t exponent, int exponents_from) {
-    *reinterpret_cast<uint32_t*>(tile + value_at(row, lane)) = packed;
-    if ((lane & 3) == 0) tile[exponents_from + exponent_at(row, lane >> 2)] = (uint8_t)exponent;
-}
 
 constexpr int kRowNT = 256;
 
@@ -125,13 +121,14 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_quantise(const T* __restrict__ x
     uint8_t* tile = q + ((row >> 7) * col_tiles + ct) * kTileBytes;
     Part<T, WHOLE> in[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) in[u].load(from, (ct + u) * kTileCols + lane * 8, dim);
+    for (int u = 0; u < U; ++u) in[u].load(from, (ct + u) * kTileCols + lane * 8, (int)dim);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (ct + u >= col_tiles) break;
         uint32_t e;
         const uint32_t packed = to_four_bits(in[u], &e);
-        store_part(tile + u * kTileBytes, r, lane, packed, e, kValueBytes);
+        *reinterpret_cast<uint32_t*>(tile + u * kTileBytes + value_at(r, lane)) = packed;
+        if ((lane & 3) == 0) tile[u * kTileBytes + kValueBytes + exponent_at(r, lane >> 2)] = (uint8_t)e;
     }
 }
 
@@ -253,15 +250,15 @@ __device__ __forceinline__ int last_not_above(const int* list, int n, int v) {
     return lo;
 }
 
-// Rows in the experts' order (top_k 0), or the tokens', each to all of its experts' rows: read and converted once.  A warp takes U
-// parts of a row; its lanes find where each of the row's choices lies.
+// Rows in the experts' order (top_k 0), or the tokens', each to all of its experts' rows: read and converted once.  A warp takes `span`
+// times U parts of a row; its lanes find where each of the row's choices lies.
 constexpr int kRowParts = 4;
 template <typename T, bool WHOLE>
-__global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, int64_t ld, int64_t dim, int col_tiles, Divisor chunks,
-                                                     const int32_t* n_tokens, int64_t max_rows, int top_k,
-                                                     const int32_t* __restrict__ place, const int32_t* __restrict__ counts,
-                                                     const int32_t* __restrict__ offsets, int E, int64_t cap_rows, int max_tiles,
-                                                     uint8_t* __restrict__ q, int32_t* status) {
+__global__ void __launch_bounds__(kRowNT, 4) k_mx4_rows(const T* __restrict__ x, int64_t ld, int dim, int col_tiles, int span, Divisor items_of,
+                                                        const int32_t* n_tokens, int64_t max_rows, int top_k,
+                                                        const int32_t* __restrict__ place, const int32_t* __restrict__ counts,
+                                                        const int32_t* __restrict__ offsets, int E, int64_t cap_rows, int max_tiles,
+                                                        uint8_t* __restrict__ q, int32_t* status) {
     __shared__ int s_first[HL_MAX_EXPERTS + 1], s_begin[HL_MAX_EXPERTS];
     constexpr int U = kRowParts;
     let_next_start();
@@ -272,16 +269,13 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, in
     int64_t n = max_rows;
     if (top_k == 0) n = min(n, (int64_t)max(__ldg(&offsets[E]), 0));
     else if (n_tokens) n = min(n, (int64_t)max(__ldg(n_tokens), 0));
-    const int64_t items = n * chunks.d;
+    const int64_t items = n * items_of.d;
     for (int64_t i = (int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5); i < items; i += (int64_t)gridDim.x * (kRowNT / 32)) {
-        const int64_t row = chunks(i);
-        const int ct0 = (int)(i - row * chunks.d) * U;
-        Part<T, WHOLE> in[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) in[u].load(x + row * ld, (int64_t)(ct0 + u) * kTileCols + lane * 8, dim);
-        uint32_t packed[U], exponent[U];
+        const int64_t row = items_of(i);
+        const int begin = (int)(i - row * items_of.d) * span * U, end = min(begin + span * U, col_tiles);
+        const T* from = x + row * ld;
         for (int k0 = 0; k0 < max(top_k, 1); k0 += 32) {
-            int64_t to = -1;           // of choice k0 + lane: its tile and row in it
+            int64_t to = -1;           // of choice k0 + lane: its tile's number times 256, and its row in it
             int at = -1;
             if (top_k == 0) at = lane == 0 ? (int)row : -1;
             else if (k0 + lane < top_k) at = __ldg(&place[row * top_k + k0 + lane]);
@@ -291,17 +285,27 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, in
                 if (r >= 0 && r < experts.rows(e, s_begin[e]) && tile < s_first[e + 1])
                     to = (int64_t)tile << 8 | (r - r / kPanelRows * kPanelRows);
             }
-            if (k0 == 0) {
+            const unsigned there = __ballot_sync(0xffffffffu, to >= 0);
+            if (!there) continue;
+            for (int ct = begin; ct < end; ct += U) {
+                Part<T, WHOLE> in[U];
+                uint32_t packed[U], exponent[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) in[u].load(from, (ct + u) * kTileCols + lane * 8, dim);
 #pragma unroll
                 for (int u = 0; u < U; ++u) packed[u] = to_four_bits(in[u], &exponent[u]);
-            }
-            for (unsigned left = __ballot_sync(0xffffffffu, to >= 0); left; left &= left - 1) {
-                const int64_t dst = __shfl_sync(0xffffffffu, to, __ffs(left) - 1);
-                uint8_t* tile = q + ((dst >> 8) * col_tiles + ct0) * kPanelBytes;
+                for (unsigned left = there; left; left &= left - 1) {
+                    const int64_t dst = __shfl_sync(0xffffffffu, to, __ffs(left) - 1);
+                    const int r = (int)(dst & 255);
+                    uint8_t* tile = q + ((dst >> 8) * col_tiles + ct) * kPanelBytes;
+                    uint8_t *values = tile + value_at(r, lane), *exponents = tile + kPanelValueBytes + exponent_at(r, lane >> 2);
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (ct0 + u < col_tiles)
-                        store_part(tile + u * kPanelBytes, (int)(dst & 255), lane, packed[u], exponent[u], kPanelValueBytes);
+                    for (int u = 0; u < U; ++u) {
+                        if (ct + u >= end) break;
+                        *reinterpret_cast<uint32_t*>(values + u * kPanelBytes) = packed[u];
+                        if ((lane & 3) == 0) exponents[u * kPanelBytes] = (uint8_t)exponent[u];
+                    }
+                }
             }
         }
     }
@@ -311,9 +315,11 @@ __global__ void __launch_bounds__(kRowNT) k_mx4_rows(const T* __restrict__ x, in
 // y[row, f] = sum over d of x[row, d] * w[e, f, d] for the rows of expert e: 128 outputs f (the lanes of the tensor memory) by up to
 // 240 rows (its columns) at a time, 256 of d a step.  One warp's thread has the tiles of a step copied, one issues the products,
 // eight warps take the sums out, those of one tile while the next one's are made.
-constexpr int kStages = 4, kStageBytes = kTileBytes + kPanelBytes, kProductNT = 320;
+constexpr int kProductNT = 320;
 constexpr uint32_t kExponentCols = 2 * kPanelRows;               // tensor-memory columns: two tiles' sums, 8 of w's exponents, 16 of x'
-constexpr int kProductSmem = kStages * kStageBytes + 1024 + (HL_MAX_EXPERTS + 1) * 4 + 256;
+// A stage is a step's tile of w and as many of x' rows as an expert can have: few rows leave room for more steps on their way.
+constexpr int kMostStages = 10, kStagesBytes = 4 * (kTileBytes + kPanelBytes);
+constexpr int kProductSmem = kStagesBytes + 1024 + (HL_MAX_EXPERTS + 1) * 4 + 256;
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint64_t* b, int n) {
@@ -408,13 +414,13 @@ struct Item {
     int e, rows, f;                    // rows: of the tile
     int64_t row0, tile, pad;           // its first row's number; pad: rows behind the expert's last that fill it up, if it is the last tile
 };
-__device__ __forceinline__ Item item_of(int64_t i, int f_tiles, const Experts& x, const int* s_first) {
+__device__ __forceinline__ Item item_of(int64_t i, int f_tiles, const Experts& x, const int* s_first, int panel_rows) {
     Item it;
     it.tile = i / f_tiles;
     it.f = (int)(i - it.tile * f_tiles);
     it.e = last_not_above(s_first, x.E, (int)it.tile);
     const int begin = x.begin(it.e), rows = x.rows(it.e, begin), at = ((int)it.tile - s_first[it.e]) * kPanelRows;
-    it.rows = min(rows - at, kPanelRows);
+    it.rows = min(rows - at, panel_rows);
     it.row0 = (int64_t)begin + at;
     const int64_t end = min((int64_t)max(__ldg(&x.offsets[it.e + 1]), 0), x.cap_rows);
     it.pad = it.tile + 1 == s_first[it.e + 1] ? max(end - begin - rows, (int64_t)0) : 0;
@@ -425,16 +431,18 @@ template <typename T>
 __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ wq,
                                                                const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets,
                                                                int E, int64_t cap_rows, int max_tiles, int col_tiles, int f_tiles,
-                                                               int64_t outputs, T* __restrict__ y, int64_t ld, int32_t* status) {
+                                                               int64_t outputs, T* __restrict__ y, int64_t ld, int stages,
+                                                               int panel_rows, int32_t* status) {
     extern __shared__ uint8_t s_raw[];
     uint8_t* base = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
-    int* s_first = reinterpret_cast<int*>(base + kStages * kStageBytes);
-    __shared__ uint64_t s_full[kStages], s_empty[kStages], s_sums[2], s_taken[2];
+    int* s_first = reinterpret_cast<int*>(base + kStagesBytes);
+    const int panel_bytes = panel_rows * 128, stage_bytes = kTileBytes + panel_bytes + (panel_rows > kTileRows ? 2048 : 1024);
+    __shared__ uint64_t s_full[kMostStages], s_empty[kMostStages], s_sums[2], s_taken[2];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_gave_up;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < stages; ++s) {
             bar_init(&s_full[s], 1);
             bar_init(&s_empty[s], 1);
         }
@@ -458,34 +466,53 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
 
     if (warp == 0) {
         if (lane == 0) {
-            wait_for_last();           // (the rows in 4 bits)
             int stage = 0;
             uint32_t phase = 1;
             bool ok = true;
+            // the weights of the first steps, while the rows are still being put into 4 bits
+            const auto ask = [&](const uint8_t* a, uint32_t b_bytes, uint32_t e_bytes) {
+                bar_expect(&s_full[stage], kTileBytes + b_bytes + e_bytes);
+                bulk_load(smem_u32(base + stage * stage_bytes), a, kTileBytes, &s_full[stage]);
+            };
+            const auto next = [&]() {
+                if (++stage == stages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            };
+            int early = 0;
+            if (blockIdx.x < items) {
+                const Item it = item_of(blockIdx.x, f_tiles, experts, s_first, panel_rows);
+                const uint8_t* a = wq + ((int64_t)it.e * f_tiles + it.f) * col_tiles * kTileBytes;
+                for (; early < min(stages, col_tiles); ++early, a += kTileBytes) {
+                    ask(a, ((it.rows + 15) & ~15) * 128, it.rows > kTileRows ? 2048 : 1024);
+                    next();
+                }
+            }
+            wait_for_last();
+            stage = 0;
+            phase = 1;
             for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-                const Item it = item_of(i, f_tiles, experts, s_first);
+                const Item it = item_of(i, f_tiles, experts, s_first, panel_rows);
                 const uint8_t* a = wq + ((int64_t)it.e * f_tiles + it.f) * col_tiles * kTileBytes;
                 const uint8_t* b = xq + it.tile * col_tiles * kPanelBytes;
                 const uint32_t b_bytes = ((it.rows + 15) & ~15) * 128, e_bytes = it.rows > kTileRows ? 2048 : 1024;
                 for (int c = 0; c < col_tiles; ++c, a += kTileBytes, b += kPanelBytes) {
-                    if (!(ok = bar_wait(&s_empty[stage], phase, &s_gave_up))) break;
-                    const uint32_t at = smem_u32(base + stage * kStageBytes);
-                    bar_expect(&s_full[stage], kTileBytes + b_bytes + e_bytes);
-                    bulk_load(at, a, kTileBytes, &s_full[stage]);
-                    bulk_load(at + kTileBytes, b, b_bytes, &s_full[stage]);
-                    bulk_load(at + kTileBytes + kPanelValueBytes, b + kPanelValueBytes, e_bytes, &s_full[stage]);
-                    if (++stage == kStages) {
-                        stage = 0;
-                        phase ^= 1;
+                    if (early > 0) {
+                        --early;
+                    } else {
+                        if (!(ok = bar_wait(&s_empty[stage], phase, &s_gave_up))) break;
+                        ask(a, b_bytes, e_bytes);
                     }
+                    const uint32_t at = smem_u32(base + stage * stage_bytes) + kTileBytes;
+                    bulk_load(at, b, b_bytes, &s_full[stage]);
+                    bulk_load(at + panel_bytes, b + kPanelValueBytes, e_bytes, &s_full[stage]);
+                    next();
                 }
             }
-            for (int s = 0; ok && s < kStages; ++s) {            // (nothing may arrive here after this CTA's end)
+            for (int s = 0; ok && s < stages; ++s) {             // (nothing may arrive here after this CTA's end)
                 ok = bar_wait(&s_empty[stage], phase, &s_gave_up);
-                if (++stage == kStages) {
-                    stage = 0;
-                    phase ^= 1;
-                }
+                next();
             }
         }
     } else if (warp == 1) {
@@ -495,27 +522,27 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
         uint32_t phase = 0, taken = 1;
         bool ok = true;
         for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-            const uint32_t n = __shfl_sync(0xffffffffu, (item_of(i, f_tiles, experts, s_first).rows + 15) & ~15, 0);
+            const uint32_t n = __shfl_sync(0xffffffffu, (item_of(i, f_tiles, experts, s_first, panel_rows).rows + 15) & ~15, 0);
             const uint32_t acc = d + buffer * kPanelRows, what0 = multiplication(n, 0), what1 = multiplication(n, 1);
             if (!(ok = bar_wait(&s_taken[buffer], taken, &s_gave_up))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             for (int c = 0; c < col_tiles; ++c) {
                 if (!(ok = bar_wait(&s_full[stage], phase, &s_gave_up))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t a = base_low + stage * (kStageBytes >> 4), b = a + (kTileBytes >> 4);
+                const uint32_t a = base_low + stage * (stage_bytes >> 4), b = a + (kTileBytes >> 4), eb_at = b + (panel_bytes >> 4);
                 // (copies and products run in the order in which they are issued)
                 const uint32_t ea = d + kExponentCols, eb = ea + 8;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     exponents_to_tmem(one, ea + 4 * h, a + ((kValueBytes + 512 * h) >> 4));
-                    exponents_to_tmem(one, eb + 8 * h, b + ((kPanelValueBytes + 512 * h) >> 4));
-                    if (n > kTileRows) exponents_to_tmem(one, eb + 8 * h + 4, b + ((kPanelValueBytes + 1024 + 512 * h) >> 4));
+                    exponents_to_tmem(one, eb + 8 * h, eb_at + ((512 * h) >> 4));
+                    if (n > kTileRows) exponents_to_tmem(one, eb + 8 * h + 4, eb_at + ((1024 + 512 * h) >> 4));
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     multiply(one, acc, a + 2 * k, b + 2 * k, k & 1 ? what1 : what0, ea + 4 * (k >> 1), eb + 8 * (k >> 1), c > 0 || k > 0);
                 commit(one, &s_empty[stage]);
-                if (++stage == kStages) {
+                if (++stage == stages) {
                     stage = 0;
                     phase ^= 1;
                 }
@@ -529,7 +556,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
         int buffer = 0;
         uint32_t phase = 0;
         for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
-            const Item it = item_of(i, f_tiles, experts, s_first);
+            const Item it = item_of(i, f_tiles, experts, s_first, panel_rows);
             if (!bar_wait(&s_sums[buffer], phase, &s_gave_up)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             __syncwarp();
@@ -620,15 +647,24 @@ int32_t launch_product(const hl_route* r, int64_t dim, int64_t outputs, const vo
     uint8_t* q = static_cast<uint8_t*>(workspace) + kWorkspaceHead;
     const int64_t ct = tiles_of(dim, kTileCols), ft = tiles_of(outputs, kTileRows), rt = row_tiles_most(r->cap_rows, r->n_experts);
     const int64_t rows = by_token ? r->max_tokens : r->cap_rows, chunks = div_up(ct, kRowParts);
-    HL_CUDA_TRY(launch(whole ? k_mx4_rows<T, true> : k_mx4_rows<T, false>, grid_for(rows * chunks, kRowNT / 32, 8 * kSMs), kRowNT, stream,
-                       static_cast<const T*>(x), ld_x, dim, ct, divisor(chunks), r->n_tokens, rows, by_token ? r->top_k : 0, r->place, r->counts,
+    // (up to four times four parts a warp where there are enough rows for four rounds of the chip's warps all the same)
+    int64_t span = rows * chunks / (4 * 32 * kSMs);
+    span = span < 1 ? 1 : span > 4 ? 4 : span;
+    const int64_t per_row = div_up(chunks, span);
+    HL_CUDA_TRY(launch(whole ? k_mx4_rows<T, true> : k_mx4_rows<T, false>, grid_for(rows * per_row, kRowNT / 32, 4 * kSMs), kRowNT, stream,
+                       static_cast<const T*>(x), ld_x, dim, ct, span, divisor(per_row), r->n_tokens, rows, by_token ? r->top_k : 0, r->place, r->counts,
                        r->offsets, r->n_experts, r->cap_rows, rt, q, status));
     note_launches(1);
+    // (an expert can have all rows that there are)
+    const int64_t all = r->cap_rows < r->max_tokens * r->top_k ? r->cap_rows : r->max_tokens * r->top_k;
+    const int64_t most_rows = by_token ? all : r->cap_rows, panel = most_rows < kPanelRows ? (most_rows + 15) / 16 * 16 : kPanelRows;
+    const int64_t stage = kTileBytes + panel * 128 + (panel > kTileRows ? 2048 : 1024);
+    const int64_t stages = kStagesBytes / stage < kMostStages ? kStagesBytes / stage : kMostStages;
     const auto kernel = k_mx4_product<T>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem) != cudaSuccess) return HL_ECUDA;
     HL_CUDA_TRY(launch_after(kernel, grid_for(rt * ft, 1, kSMs), kProductNT, kProductSmem, stream, (const uint8_t*)q,
                              static_cast<const uint8_t*>(w), r->counts, r->offsets, r->n_experts, r->cap_rows, rt, ct, ft, outputs,
-                             static_cast<T*>(y), ld_y, status));
+                             static_cast<T*>(y), ld_y, stages, panel, status));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
