@@ -152,26 +152,52 @@ __device__ __forceinline__ void put(TT* row, int c, int dim, const float (&sum)[
     }
 }
 
+// The same by a whole warp, 32 places a step.
+__device__ __forceinline__ int64_t not_below_by_warp(const int32_t* __restrict__ sorted, int64_t n, int u) {
+    const int lane = threadIdx.x & 31;
+    int64_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int64_t step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step - 1;           // the last of the lane's part
+        const unsigned below = __ballot_sync(0xffffffffu, at < hi && __ldg(&sorted[min(at, n - 1)]) < u);
+        const int parts = __popc(below);                         // (the first so many are wholly below)
+        lo += parts * step;
+        hi = min(hi, lo + step - 1);
+    }
+    return lo;
+}
+
 // rows [first, last) that no token names become zeros
 template <typename TT, int W>
 __device__ void zero_rows(const int32_t* __restrict__ sorted, int64_t n, int64_t first, int64_t last, int dim, TT* __restrict__ table,
                           int64_t ld) {
     __shared__ uint32_t s_there[kNT / 32];
+    __shared__ int64_t s_range[2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Pack<TT, W> zero;
     zero.zero();
     const int vectors = dim / W;
     for (int64_t r0 = first; r0 < last; r0 += kNT) {
-        const int64_t r = r0 + threadIdx.x;
-        bool there = true;
-        if (r < last) {
-            const int64_t at = not_below(sorted, 0, n, (int)r);
-            there = at < n && __ldg(&sorted[at]) == (int)r;
+        const int64_t r1 = min(r0 + kNT, last);
+        if (warp < 2) {
+            const int64_t at = not_below_by_warp(sorted, n, (int)(warp ? r1 - 1 : r0));
+            if (lane == 0) s_range[warp] = at;
         }
-        const uint32_t word = __ballot_sync(0xffffffffu, there);
-        if (lane == 0) s_there[warp] = word;
+        if (threadIdx.x < kNT / 32) s_there[threadIdx.x] = 0;
         __syncthreads();
-        const int rows = (int)min((int64_t)kNT, last - r0);
+        const int64_t lo = s_range[0], hi = s_range[1];          // those of row r1 - 1 begin at hi
+        if (hi - lo <= 4 * kNT) {
+            for (int64_t i = lo + threadIdx.x; i < hi; i += kNT) {
+                const unsigned r = (unsigned)(__ldg(&sorted[i]) - (int)r0);
+                if (r < (unsigned)kNT) atomicOr(&s_there[r >> 5], 1u << (r & 31));
+            }
+        } else if (r0 + threadIdx.x < r1 - 1) {                  // (many tokens of few rows: a row a thread)
+            const int64_t at = not_below(sorted, lo, hi, (int)(r0 + threadIdx.x));
+            if (at < hi && __ldg(&sorted[at]) == (int)(r0 + threadIdx.x)) atomicOr(&s_there[warp], 1u << lane);
+        }
+        if (threadIdx.x == 0 && hi < n && __ldg(&sorted[hi]) == (int)(r1 - 1))
+            atomicOr(&s_there[(r1 - 1 - r0) >> 5], 1u << ((r1 - 1 - r0) & 31));
+        __syncthreads();
+        const int rows = (int)(r1 - r0);
         if (vectors >= kNT / 2) {
             for (int k = 0; k < rows; ++k) {
                 if ((s_there[k >> 5] >> (k & 31)) & 1u) continue;
@@ -211,14 +237,17 @@ __global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ 
     __shared__ __align__(16) float s_put[LOOSE ? kNT * W : 4];
     let_next_start();
     const int64_t n = live_tokens(n_tokens, max_tokens);
-    if ((int)blockIdx.x >= sum_ctas) {
+    // (CTAs of the two kinds alternate, evenly, so that the ones' stores go along with the others' loads)
+    const unsigned zeros = gridDim.x - sum_ctas;
+    const unsigned zeros_before = zeros ? (unsigned)((unsigned long long)blockIdx.x * zeros / gridDim.x) : 0;
+    if (zeros && (unsigned)((unsigned long long)(blockIdx.x + 1) * zeros / gridDim.x) > zeros_before) {
         if (blockIdx.y) return;
-        const int64_t first = (int64_t)(blockIdx.x - sum_ctas) * rows_per_cta;
+        const int64_t first = (int64_t)zeros_before * rows_per_cta;
         zero_rows<TT, LOOSE ? 1 : W>(sorted, n, first, min(first + rows_per_cta, (int64_t)n_rows), dim, table, ld_table);
         return;
     }
     const int sub = threadIdx.x & (P - 1);
-    const int64_t w = (int64_t)blockIdx.x * (kNT / P) + threadIdx.x / P, begin = w * window, end = min(begin + window, n);
+    const int64_t w = (int64_t)(blockIdx.x - zeros_before) * (kNT / P) + threadIdx.x / P, begin = w * window, end = min(begin + window, n);
     if (begin >= end) return;
     const int c = ((int)blockIdx.y * P + sub) * W;
     if (!LOOSE && c >= dim) return;
@@ -272,34 +301,14 @@ __global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ 
     flush(end < n && __ldg(&sorted[end]) == run);
 }
 
-// Runs over several windows: their pieces, by the CTA of the window where they begin.  Its groups of P threads take a part of the
-// pieces each, in order, and the parts are added up in order.
-template <typename TT, int W, bool LOOSE>
-__global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__ sorted, int64_t max_tokens, const int32_t* n_tokens,
-                                                     int n_rows, int dim, float scale, TT* __restrict__ table, int64_t ld_table,
-                                                     int accumulate, int window, int P, const float* __restrict__ pieces) {
-    __shared__ __align__(16) float s_sum[kNT * W];               // [kNT / P][P * W]
-    wait_for_last();
-    const int64_t n = live_tokens(n_tokens, max_tokens), w = blockIdx.x, end = (w + 1) * window;
-    if (end >= n) return;
-    const int run = __ldg(&sorted[end]);
-    const int64_t begin = w * window;
-    const int before = begin > 0 ? __ldg(&sorted[begin - 1]) : -1;
-    if (run != __ldg(&sorted[end - 1]) || (unsigned)run >= (unsigned)n_rows || before == run) return;      // (or it began before)
-    // the window with the run's last token
-    int64_t lo = end, hi = n;
-    for (int64_t step = window; lo + step < n; step *= 2)
-        if (__ldg(&sorted[lo + step]) == run) lo += step;
-        else {
-            hi = lo + step;
-            break;
-        }
-    const int64_t last = (not_below(sorted, lo, hi, run + 1) - 1) / window;
-    const int sub = threadIdx.x & (P - 1), side = threadIdx.x / P, sides = kNT / P;
-    const int c = ((int)blockIdx.y * P + sub) * W;
-    const int64_t all = last - w + 1, per = (all + sides - 1) / sides, p0 = min(side * per, all), p1 = min(p0 + per, all);
-    const int64_t pitch = piece_pitch(dim);
-    float sum[W] = {};
+// Runs over several windows: their pieces.  A warp looks at one window, of which a run may begin there and go on, and adds up the run's
+// pieces in order if it is short; what reaches over more than kShort windows is left to the CTA, whose warps take a part of the
+// pieces each, in order, and add the parts up in order.  32 W columns a CTA.  (A CTA a window, most of which end at once: 24 us
+// instead of ... for 512 windows of 2 048 columns.)
+constexpr int kShort = 16;
+template <int W>
+__device__ __forceinline__ void add_pieces(const float* __restrict__ pieces, int64_t pitch, int64_t w, int64_t p0, int64_t p1, int c, int dim,
+                                           float (&sum)[W]) {
     constexpr int U = 8;
     for (int64_t p = p0; p < p1; p += U) {
         Pack<float, W> in[U];
@@ -316,22 +325,78 @@ __global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__
             for (int i = 0; i < W; ++i) sum[i] += x[i];
         }
     }
+}
+
+template <typename TT, int W, bool LOOSE>
+__global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__ sorted, int64_t max_tokens, const int32_t* n_tokens,
+                                                     int n_rows, int dim, float scale, TT* __restrict__ table, int64_t ld_table,
+                                                     int accumulate, int window, const float* __restrict__ pieces) {
+    constexpr int kWarps = kNT / 32;
+    __shared__ __align__(16) float s_sum[kNT * W];               // of each warp: [32 W]
+    __shared__ int s_long[kWarps];                               // the run of a warp's window, if it is long
+    wait_for_last();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t n = live_tokens(n_tokens, max_tokens), first = (int64_t)blockIdx.x * kWarps, pitch = piece_pitch(dim);
+    const int c = ((int)blockIdx.y * 32 + lane) * W;
+    const int64_t w = first + warp, end = (w + 1) * window;
+    int begins = -1;                                             // the run that begins in the window and goes on
+    if (end < n) {
+        // (lanes: before the window, its last token, the first behind it, and those of the windows behind that)
+        const int64_t at = lane == 0 ? w * window - 1 : lane == 1 ? end - 1 : (w + lane - 1) * window;
+        const int v = at >= 0 && at < n ? __ldg(&sorted[at]) : -1;
+        const int run = __shfl_sync(0xffffffffu, v, 2);
+        const unsigned same = __ballot_sync(0xffffffffu, v == run);
+        const int more = __ffs(~(same >> 2)) - 1;                // windows behind that begin with it; at most 30
+        if ((unsigned)run < (unsigned)n_rows && (same & 3) == 2) {
+            begins = run;
+            if (more < kShort) {
+                float sum[W] = {};
+                add_pieces<W>(pieces, pitch, w, 0, more + 1, c, dim, sum);
+                if (LOOSE || c < dim) put<TT, W, LOOSE>(table + run * ld_table, c, dim, sum, scale, accumulate, s_sum + warp * 32 * W);
+                begins = -1;
+            }
+        }
+    }
+    if (lane == 0) s_long[warp] = begins;
+    if (!__syncthreads_or(begins >= 0)) return;
+    for (int k = 0; k < kWarps; ++k) {
+        const int run = s_long[k];
+        if (run < 0) continue;
+        int64_t all = 1;                                         // its pieces
+        for (int64_t v = first + k + 1; v * window < n; v += kNT) {
+            const int64_t at = (v + threadIdx.x) * window;
+            const int more = __syncthreads_count(at < n && __ldg(&sorted[min(at, n - 1)]) == run);
+            all += more;
+            if (more < kNT) break;
+        }
+        const int64_t per = (all + kWarps - 1) / kWarps, p0 = min(warp * per, all), p1 = min(p0 + per, all);
+        float sum[W] = {};
+        add_pieces<W>(pieces, pitch, first + k, p0, p1, c, dim, sum);
 #pragma unroll
-    for (int i = 0; i < W; ++i) s_sum[side * P * W + i * P + sub] = sum[i];
-    __syncthreads();
-    if (side) return;
-    for (int s = 1; s < sides && s * per < all; ++s)
+        for (int i = 0; i < W; ++i) s_sum[(warp * W + i) * 32 + lane] = sum[i];
+        __syncthreads();
+        if (warp == 0) {
+            for (int s = 1; s < kWarps; ++s)
 #pragma unroll
-        for (int i = 0; i < W; ++i) sum[i] += s_sum[s * P * W + i * P + sub];
-    if (LOOSE || c < dim) put<TT, W, LOOSE>(table + run * ld_table, c, dim, sum, scale, accumulate, s_sum);
+                for (int i = 0; i < W; ++i) sum[i] += s_sum[(s * W + i) * 32 + lane];
+            if (LOOSE || c < dim) put<TT, W, LOOSE>(table + run * ld_table, c, dim, sum, scale, accumulate, s_sum);
+        }
+        __syncthreads();
+    }
 }
 
 // ---- arguments ------------------------------------------------------------------------------------------------------------
 bool tokens_ok(int64_t max_tokens) { return max_tokens >= 0 && max_tokens < (int64_t(1) << 30); }
 unsigned long long inverse_of(int64_t vectors) { return vectors == 1 ? 0 : ~0ull / vectors + 1; }
 
-// tokens of a window: few enough to give every multiprocessor work, many where there are many, so that few runs are cut
-int window_of(int64_t max_tokens) { return max_tokens <= 65536 ? 32 : 128; }
+// Tokens of a window, a power of two from 16 to 128: so many that the windows' threads, of eight columns, fill the chip once, but not
+// more than 8 192 windows where 128 tokens each make fewer of them.
+constexpr int64_t kChipThreads = 148 * 2048;
+int window_of(int64_t max_tokens, int64_t dim) {
+    int w = 16;
+    while (w < 128 && (max_tokens * div_up(dim, 8) > w * kChipThreads || max_tokens > w * int64_t(8192))) w *= 2;
+    return w;
+}
 
 // the workspace: two words, and then what either call needs
 struct Workspace {
@@ -374,22 +439,22 @@ int32_t launch_sums(int64_t n_rows, int64_t dim, const int32_t* sorted, const in
                     int accumulate, float* pieces, cudaStream_t stream) {
     int P = LOOSE ? 32 : 1;
     while (!LOOSE && P < kNT && P * W < dim) P *= 2;
-    const int window = window_of(max_tokens), Q = P < 32 ? P : 32;         // Q: of the joins, eight warps of which share a run's pieces
+    const int window = window_of(max_tokens, dim);
     const int64_t windows = div_up(max_tokens, window), sums = div_up(windows, kNT / P);
     // rows without tokens: some 128 KB a CTA
     int64_t per = (128 << 10) / (dim * (int64_t)sizeof(TT));
     per = per < 1 ? 1 : per > kNT ? kNT : per;
     const int64_t zeros = accumulate ? 0 : div_up(n_rows, per);
-    if (sums + zeros > 0x7fffffff || div_up(dim, Q * W) > 65535 || windows > 0x7fffffff) return HL_EINVAL;
+    if (sums + zeros > 0x7fffffff || div_up(dim, 32 * W) > 65535 || windows > 0x7fffffff) return HL_EINVAL;
     if (sums + zeros == 0) return HL_OK;
     HL_CUDA_TRY(launch(k_token_sums<TG, TT, W, U, LOOSE>, dim3((unsigned)(sums + zeros), (unsigned)div_up(dim, P * W)), kNT, stream,
                        sorted, order, max_tokens, n_tokens, (int)n_rows, (int)dim, static_cast<const TG*>(grad), ld_grad, scale,
                        static_cast<TT*>(table), ld_table, accumulate, window, P, (int)sums, (int)per, pieces));
     note_launches(1);
     if (windows > 1) {
-        HL_CUDA_TRY(launch_after(k_token_joins<TT, W, LOOSE>, dim3((unsigned)(windows - 1), (unsigned)div_up(dim, Q * W)), kNT, 0, stream,
-                                 sorted, max_tokens, n_tokens, (int)n_rows, (int)dim, scale, static_cast<TT*>(table), ld_table, accumulate,
-                                 window, Q, (const float*)pieces));
+        HL_CUDA_TRY(launch_after(k_token_joins<TT, W, LOOSE>, dim3((unsigned)div_up(windows - 1, kNT / 32), (unsigned)div_up(dim, 32 * W)),
+                                 kNT, 0, stream, sorted, max_tokens, n_tokens, (int)n_rows, (int)dim, scale, static_cast<TT*>(table),
+                                 ld_table, accumulate, window, (const float*)pieces));
         note_launches(1);
     }
     HL_LAUNCH_CHECK();
@@ -423,7 +488,7 @@ extern "C" int32_t hl_token_embed(int32_t table_dtype, int64_t n_rows, int64_t d
 extern "C" size_t hl_token_workspace_bytes(int64_t max_tokens, int64_t dim) {
     if (!tokens_ok(max_tokens) || dim < 1 || dim > (int64_t(1) << 24)) return 0;
     const int64_t sort = (2 * padded(max_tokens) + padded(sort_hist_words(max_tokens))) * 4;
-    const int64_t sums = 2 * div_up(max_tokens, window_of(max_tokens)) * (div_up(dim, kPieceStep) * kPieceStep) * 4;
+    const int64_t sums = 2 * div_up(max_tokens, window_of(max_tokens, dim)) * (div_up(dim, kPieceStep) * kPieceStep) * 4;
     return (size_t)(kWorkspaceHead + ((sort > sums ? sort : sums) + 255) / 256 * 256);
 }
 
