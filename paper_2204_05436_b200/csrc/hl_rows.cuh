@@ -93,8 +93,9 @@ struct Pack {
     }
 };
 
-// Eight values side by side of a row that begins anywhere: columns c .. c + 7, zeros outside [0, dim).  The 16-byte lines that hold
-// some of them are read whole (each has a value of the row, so it lies where the row's memory does), and put in place by shifts.
+// Eight values side by side of a row that begins anywhere: columns c .. c + 7; what lies outside [0, dim) may be anything.  The 16-byte
+// lines that hold some of them are read whole (each has a value of the row, so it lies where the row's memory does), and put in place
+// by shifts.
 template <typename T>
 struct Loose {
     static constexpr int N = 16 / (int)sizeof(T), kLines = 8 / N + 1, kWords = 4 * kLines;
@@ -106,17 +107,19 @@ struct Loose {
         for (int i = 0; i < kWords; ++i) w[i] = 0;
     }
     __device__ __forceinline__ void load(const T* row, int c, int dim) {
-        const uintptr_t p = reinterpret_cast<uintptr_t>(row + c), line = p & ~uintptr_t(15);
-        const uintptr_t begin = reinterpret_cast<uintptr_t>(row + max(c, 0)), end = reinterpret_cast<uintptr_t>(row + min(c + 8, dim));
-        shift = (int)(p & 15) / (int)sizeof(T);
+        constexpr int kSize = (int)sizeof(T);
+        const int in_line = (int)(reinterpret_cast<uintptr_t>(row) & 15), at = c * kSize + in_line;
+        const int first = (at & ~15) - in_line, end = min(c + 8, dim) * kSize;         // bytes from the row's begin
+        const char* p = reinterpret_cast<const char*>(row) + first;
+        shift = (at & 15) / kSize;
 #pragma unroll
         for (int i = 0; i < kLines; ++i) {
             uint4 v = make_uint4(0, 0, 0, 0);
-            if (line + 16 * i < end && line + 16 * i + 16 > begin) v = __ldg(reinterpret_cast<const uint4*>(line + 16 * i));
+            if (first + 16 * i < end && first + 16 * i > -16) v = __ldg(reinterpret_cast<const uint4*>(p + 16 * i));
             w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
         }
     }
-    __device__ __forceinline__ void get(float (&x)[8], int c, int dim) const {
+    __device__ __forceinline__ void get(float (&x)[8]) const {
         uint32_t v[kWords];
         const int words = shift * (int)sizeof(T) / 4;            // 0 .. 3
 #pragma unroll
@@ -131,13 +134,30 @@ struct Loose {
 #pragma unroll
         for (int i = 0; i < Pack<T, 8>::kWords; ++i) p.w[i] = v[i];
         p.get(x);
-        if (c < 0 || c + 8 > dim) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if ((unsigned)(c + i) >= (unsigned)dim) x[i] = 0.f;
-        }
     }
 };
+
+// v[i] for the columns c + i of a row, those outside [0, dim) left out
+template <typename T>
+__device__ __forceinline__ void store_some(T* row, int c, int dim, const Pack<T, 8>& v) {
+    T* p = row + c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if ((unsigned)(c + i) >= (unsigned)dim) continue;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(p + i) = v.w[i];
+        else *reinterpret_cast<unsigned short*>(p + i) = (unsigned short)(v.w[i / 2] >> (16 * (i & 1)));
+    }
+}
+// zeros in a row that begins anywhere, by a whole warp: whole lines, and what lies before and behind them
+template <typename T>
+__device__ __forceinline__ void zero_row(T* row, int dim) {
+    constexpr int N = 16 / (int)sizeof(T);
+    const int lane = threadIdx.x & 31, before = min((int)(-(reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (N - 1)), dim);
+    const int lines = (dim - before) / N, behind = before + lines * N;
+    if (lane < before) row[lane] = from_float<T>(0.f);
+    for (int i = lane; i < lines; i += 32) reinterpret_cast<uint4*>(row + before)[i] = make_uint4(0, 0, 0, 0);
+    if (behind + lane < dim) row[behind + lane] = from_float<T>(0.f);
+}
 
 // ---- arguments: types, and matrices of rows -------------------------------------------------------------------------------
 inline int dtype_size(int32_t dtype) { return dtype == HL_F32 ? 4 : dtype == HL_BF16 || dtype == HL_F16 ? 2 : 0; }

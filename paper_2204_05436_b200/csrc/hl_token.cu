@@ -72,18 +72,13 @@ __global__ void __launch_bounds__(kNT) k_token_embed_loose(const TT* __restrict_
     if (there) in.load(table + token * ld_table, c, dim);
     else if (token != -1 && status) set_status(status, HL_EBOUNDS);
     float x[8];
-    in.get(x, c, dim);
+    in.get(x);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = there ? x[i] * scale : 0.f;
-    if (c >= 0 && c + 8 <= dim) {
-        Pack<TO, 8> v;
-        v.set(x);
-        v.store(row + c);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if ((unsigned)(c + i) < (unsigned)dim) row[c + i] = from_float<TO>(x[i]);
-    }
+    Pack<TO, 8> v;
+    v.set(x);
+    if (c >= 0 && c + 8 <= dim) v.store(row + c);
+    else store_some(row, c, dim, v);
 }
 
 // ---- the sort -----------------------------------------------------------------------------------------------------------
@@ -167,7 +162,7 @@ __device__ __forceinline__ int64_t not_below_by_warp(const int32_t* __restrict__
 }
 
 // rows [first, last) that no token names become zeros
-template <typename TT, int W>
+template <typename TT, int W, bool LOOSE>
 __device__ void zero_rows(const int32_t* __restrict__ sorted, int64_t n, int64_t first, int64_t last, int dim, TT* __restrict__ table,
                           int64_t ld) {
     __shared__ uint32_t s_there[kNT / 32];
@@ -198,7 +193,10 @@ __device__ void zero_rows(const int32_t* __restrict__ sorted, int64_t n, int64_t
             atomicOr(&s_there[(r1 - 1 - r0) >> 5], 1u << ((r1 - 1 - r0) & 31));
         __syncthreads();
         const int rows = (int)(r1 - r0);
-        if (vectors >= kNT / 2) {
+        if (LOOSE) {
+            for (int k = warp; k < rows; k += kNT / 32)
+                if (!((s_there[k >> 5] >> (k & 31)) & 1u)) zero_row(table + (r0 + k) * ld, dim);
+        } else if (vectors >= kNT / 2) {
             for (int k = 0; k < rows; ++k) {
                 if ((s_there[k >> 5] >> (k & 31)) & 1u) continue;
                 for (int c = threadIdx.x; c < vectors; c += kNT) zero.store(table + (r0 + k) * ld + (int64_t)c * W);
@@ -221,10 +219,7 @@ struct Values {
         if constexpr (LOOSE) v.load(row, c, dim);
         else v.load(row + c);
     }
-    __device__ __forceinline__ void get(float (&x)[W], int c, int dim) const {
-        if constexpr (LOOSE) v.get(x, c, dim);
-        else v.get(x);
-    }
+    __device__ __forceinline__ void get(float (&x)[W]) const { v.get(x); }
 };
 
 template <typename TG, typename TT, int W, int U, bool LOOSE>
@@ -243,12 +238,13 @@ __global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ 
     if (zeros && (unsigned)((unsigned long long)(blockIdx.x + 1) * zeros / gridDim.x) > zeros_before) {
         if (blockIdx.y) return;
         const int64_t first = (int64_t)zeros_before * rows_per_cta;
-        zero_rows<TT, LOOSE ? 1 : W>(sorted, n, first, min(first + rows_per_cta, (int64_t)n_rows), dim, table, ld_table);
+        zero_rows<TT, W, LOOSE>(sorted, n, first, min(first + rows_per_cta, (int64_t)n_rows), dim, table, ld_table);
         return;
     }
     const int sub = threadIdx.x & (P - 1);
-    const int64_t w = (int64_t)(blockIdx.x - zeros_before) * (kNT / P) + threadIdx.x / P, begin = w * window, end = min(begin + window, n);
-    if (begin >= end) return;
+    const int64_t w = (int64_t)(blockIdx.x - zeros_before) * (kNT / P) + threadIdx.x / P, first = w * window;
+    if (first >= n) return;
+    const int begin = (int)first, end = (int)min(first + window, n);       // (there are less than 2^30 tokens)
     const int c = ((int)blockIdx.y * P + sub) * W;
     if (!LOOSE && c >= dim) return;
     float* s = LOOSE ? s_put + (threadIdx.x & ~31) * W : nullptr;
@@ -271,19 +267,19 @@ __global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ 
         for (int i = 0; i < W; ++i) sum[i] = 0.f;
         open = false;
     };
-    for (int64_t i0 = begin; i0 < end; i0 += U) {
+    for (int i0 = begin; i0 < end; i0 += U) {
         int key[U], at[U];
         Values<TG, W, LOOSE> in[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             key[u] = i0 + u < end ? __ldg(&sorted[i0 + u]) : run;
             at[u] = i0 + u < end ? __ldg(&order[i0 + u]) : -1;
-            if ((unsigned)key[u] >= (unsigned)n_rows || at[u] >= n || c >= dim) at[u] = -1;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             in[u].v.zero();
-            if (at[u] >= 0) in[u].load(grad + at[u] * ld_grad, c, dim);
+            if ((unsigned)key[u] < (unsigned)n_rows && (unsigned)at[u] < (unsigned)n && c < dim)
+                in[u].load(grad + at[u] * ld_grad, c, dim);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -293,7 +289,7 @@ __global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ 
                 run = key[u];
             }
             float x[W];
-            in[u].get(x, c, dim);
+            in[u].get(x);
 #pragma unroll
             for (int i = 0; i < W; ++i) sum[i] += x[i];
         }
