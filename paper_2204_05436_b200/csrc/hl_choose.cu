@@ -9,7 +9,7 @@ namespace {
 // ---- who is chosen ----------------------------------------------------------------------------------------------------
 // A token has P lanes of a warp (1 to 32), each of which holds ITEMS of its experts side by side.  Without a bias an expert's key is
 // its logit, which orders as the score does.  With one it is score + bias, and the definition is in 64 bits; what decides is
-// computed in 32, and a token for which 32 bits cannot tell (kSure) is done again in 64: some one in a hundred of 256 experts
+// computed in 32, and a token for which 32 bits cannot tell is done again in 64: with sigmoids two or three in a thousand of 256 experts
 // whose logits are random.
 template <int ITEMS, int P>
 struct Shape {
@@ -19,11 +19,12 @@ struct Shape {
     static constexpr int kChosen = kExperts < HL_MAX_TOP_K ? kExperts : HL_MAX_TOP_K;
 };
 
-// |score in 32 bits - score| < 2^-18.  Of a sigmoid: s (1 - s) times the relative error of the exponential (2^-22 of the instruction's,
-// and its argument's roundings, |x| 2^-22; s (1 - s) |x| < 1/4), the sum's rounding and the inverse's 2^-23.  Of a softmax: the same with e^-|x| |x| < 0.37,
-// and the sum, of up to 32 + 5 terms one after the other: 37 * 2^-24 of it and its terms' errors.  Adding the bias rounds by 2^-24
-// of the key.  So keys further apart than 2^-17 (1 + |key|) are in order, and sums of two than twice that.
-constexpr float kSure = 0x1p-17f;
+// How far scores of 32 bits may be off.  A sigmoid s: s (1 - s) times the relative error of the exponential (2^-22 of the instruction's,
+// and its argument's roundings, |x| 2^-22; s (1 - s) |x| < 1/4), the sum's rounding and the inverse's 2^-23: less than 2^-21 in
+// all.  A softmax: the same with e^-|x| (1 + |x|) 2^-22 < 2^-21, and the sum of up to 32 + 5 terms one after the other, 37 * 2^-24 of
+// it, and the inverse: less than 2^-18.  Adding the bias rounds by 2^-24 of the key.  So keys further apart than this times 1 +
+// |key| are in order, and sums of two than twice that.
+constexpr float kSureSigmoid = 0x1p-19f, kSureSoftmax = 0x1p-17f;
 
 // numbers in the order of the floats (which have no NaN among them; -0 is 0)
 __device__ __forceinline__ uint32_t ordered(float v) {
@@ -74,7 +75,7 @@ __device__ __forceinline__ double sigmoid(double l) { return 1.0 / (1.0 + exp(-l
 // e^(l - m) for l <= m, where both may be infinite
 __device__ __forceinline__ float part(float l, float m) { return l == m ? 1.f : expf(l - m); }
 __device__ __forceinline__ double part(double l, double m) { return l == m ? 1.0 : exp(l - m); }
-// the same, as exact as choosing needs it (kSure): 2^x and 1 / x as the hardware has them
+// the same, as exact as choosing needs it: 2^x and 1 / x as the hardware has them
 __device__ __forceinline__ float near_exp2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -93,6 +94,7 @@ __device__ __forceinline__ float near_part(float l, float m) { return l == m ? 1
 struct Router {
     int top_k, E, G, per_group, top_groups;
     uint32_t group_magic;              // 2^21 / per_group, rounded up: exact for numbers and sizes of at most 1 024
+    float sure;                        // kSure...
     bool softmax, pair, renorm;
     __device__ __forceinline__ int group_of(int e) const { return (int)(((uint32_t)e * group_magic) >> 21); }
 };
@@ -100,8 +102,13 @@ enum { kSoftmax = 1, kPair = 2, kRenorm = 4, kWholeLanes = 8 };
 
 template <typename Key>
 __device__ __forceinline__ void two_best(Key v, Key& best, Key& second) {
-    second = v > best ? best : v > second ? v : second;
-    best = v > best ? v : best;
+    if constexpr (sizeof(Key) == 4) {
+        second = fmaxf(second, fminf(best, v));
+        best = fmaxf(best, v);
+    } else {
+        second = fmax(second, fmin(best, v));
+        best = fmax(best, v);
+    }
 }
 
 // Keys of experts outside the groups that are kept become -inf.  `value` is what the groups are compared by, which is -inf for
@@ -118,14 +125,15 @@ __device__ bool keep_groups(const Router& r, bool whole_lanes, const Key (&value
         for (int j = 0; j < ITEMS; ++j) two_best(value[j], best, second);
         for (int d = 1; d < lanes; d *= 2) {
             const Key b = __shfl_xor_sync(kAll, best, d), c = __shfl_xor_sync(kAll, second, d);
-            second = b > best ? (best > c ? best : c) : (b > second ? b : second);
-            best = b > best ? b : best;
+            two_best(b, best, second);
+            second = c > second ? c : second;
         }
         if (r.pair && second > none) best += second;
         int rank = 0;
+#pragma unroll 4
         for (int g = 0; g < r.G; ++g) {
             const Key v = __shfl_sync(kAll, best, first + g * lanes);
-            rank += v > best || (v == best && g < mine);
+            rank += g < mine ? v >= best : v > best;
         }
         if (rank >= r.top_groups) {
 #pragma unroll
@@ -171,18 +179,18 @@ __device__ bool keep_groups(const Router& r, bool whole_lanes, const Key (&value
         }
         __syncwarp();
     }
-    return out == none || in - out > (Key)(2 * kSure) * ((Key)1 + (in < 0 ? -in : in));
+    return out == none || in - out > (Key)(2 * r.sure) * ((Key)1 + (in < 0 ? -in : in));
 }
 
 // Whether keys a >= b are in order for certain; a NaN (of infinite keys) says no.
 template <typename Key>
-__device__ __forceinline__ bool surely(Key a, Key b) { return a - b > (Key)kSure * ((Key)1 + (a < 0 ? -a : a)); }
+__device__ __forceinline__ bool surely(Key a, Key b, float sure) { return a - b > (Key)sure * ((Key)1 + (a < 0 ? -a : a)); }
 
 // The largest keys, in order: their experts go to s_e (-1: none left), one after the other -- the largest of a lane's, then over the
 // lanes; a tie goes to the lowest number.  Where `check`, returns whether their order was clear; same(a, b): two experts whose
 // keys are equal by definition.
 template <int ITEMS, int P, typename Key, typename Same>
-__device__ __forceinline__ bool choose(int top_k, Key (&key)[ITEMS], int q, bool check, int32_t* s_e, Same same) {
+__device__ __forceinline__ bool choose(int top_k, Key (&key)[ITEMS], int q, bool check, float sure, int32_t* s_e, Same same) {
     const Key none = -(Key)INFINITY;
     bool clear = true;
     Key last = 0;
@@ -199,7 +207,7 @@ __device__ __forceinline__ bool choose(int top_k, Key (&key)[ITEMS], int q, bool
         int e = q * ITEMS + j_best;
         largest<P>(best, e);
         const bool any = best > none;
-        if (check && k > 0 && any && last_e >= 0 && !surely(last, best)) clear = clear && same(last_e, e);
+        if (check && k > 0 && any && last_e >= 0 && !surely(last, best, sure)) clear = clear && same(last_e, e);
         last = best;
         last_e = any ? e : -1;
         if (k < top_k && q == 0) s_e[k] = last_e;
@@ -214,7 +222,7 @@ __device__ __forceinline__ bool choose(int top_k, Key (&key)[ITEMS], int q, bool
 // Those few, a lane each, are ranked by comparing each with all.  Returns false, with nothing done, if there are more than P of
 // them (equal keys, or few lanes with any).
 template <int ITEMS, int P, typename Same>
-__device__ __forceinline__ bool choose_few(int top_k, const float (&key)[ITEMS], int q, bool check, int32_t* s_e, float2* s_few,
+__device__ __forceinline__ bool choose_few(int top_k, const float (&key)[ITEMS], int q, bool check, float sure, int32_t* s_e, float2* s_few,
                                            bool* clear, Same same) {
     const float none = -INFINITY;
     const int lane = threadIdx.x & 31, first = lane & ~(P - 1);
@@ -254,7 +262,7 @@ __device__ __forceinline__ bool choose_few(int top_k, const float (&key)[ITEMS],
 #pragma unroll 4
     for (int i = 0; i < most; ++i) {
         const float v = __shfl_sync(kAll, me.x, first + i);
-        rank += v > me.x || (v == me.x && i < q);
+        rank += i < q ? v >= me.x : v > me.x;
     }
     if (q < few && rank < top_k) s_e[rank] = __float_as_int(me.y);
     if (q >= few && q < top_k) s_e[q] = -1;
@@ -265,7 +273,7 @@ __device__ __forceinline__ bool choose_few(int top_k, const float (&key)[ITEMS],
         bool mine_clear = true;
         if (q > 0 && q < few && q <= top_k) {
             const float2 a = s_few[q - 1], b = s_few[q];
-            if (!surely(a.x, b.x)) mine_clear = same(__float_as_int(a.y), __float_as_int(b.y));
+            if (!surely(a.x, b.x, sure)) mine_clear = same(__float_as_int(a.y), __float_as_int(b.y));
         }
         *clear = (__ballot_sync(kAll, !mine_clear) & lanes_of<P>(lane)) == 0;
     }
@@ -284,7 +292,7 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
     __shared__ int32_t s_chosen[S::kTokens][S::kChosen];
     __shared__ float2 s_few[P >= 16 ? S::kNT : 1];
     extern __shared__ double s_base[];                           // with groups that are not whole lanes', of every token: [E + 2 G]
-    const Router r{top_k, E, G, per_group, top_groups, group_magic, (flags & kSoftmax) != 0, (flags & kPair) != 0, (flags & kRenorm) != 0};
+    const Router r{top_k, E, G, per_group, top_groups, group_magic, flags & kSoftmax ? kSureSoftmax : kSureSigmoid, (flags & kSoftmax) != 0, (flags & kPair) != 0, (flags & kRenorm) != 0};
     const bool whole_lanes = flags & kWholeLanes;
     const int q = threadIdx.x % P, mine = threadIdx.x / P;
     int64_t tokens = max_tokens;
@@ -320,12 +328,17 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j) l[j] = e0 + j < E ? as_float(row[e0 + j]) : none;
     }
+    float any_nan = 0.f;                                         // (infinities make one, too)
 #pragma unroll
-    for (int j = 0; j < ITEMS; ++j)
-        if (l[j] != l[j]) {
-            bad = true;
-            l[j] = none;
-        }
+    for (int j = 0; j < ITEMS; ++j) any_nan = fmaf(l[j], 0.f, any_nan);
+    if (any_nan != 0.f) {
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j)
+            if (l[j] != l[j]) {
+                bad = true;
+                l[j] = none;
+            }
+    }
     // of all scores, where they are needed: the largest logit and the sum of e^(l - largest)
     const bool scores = bias || (G > 1 && r.pair);
     float top = none, z = 1.f;
@@ -386,8 +399,8 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
         const bool check = bias != nullptr;
         bool done = false, in_order = true;
         if constexpr (P >= 16)
-            if (top_k < P) done = choose_few<ITEMS, P>(top_k, key, q, check, s_e, s_few + mine * P, &in_order, same);
-        if (!done) in_order = choose<ITEMS, P>(top_k, key, q, check, s_e, same);
+            if (top_k < P) done = choose_few<ITEMS, P>(top_k, key, q, check, r.sure, s_e, s_few + mine * P, &in_order, same);
+        if (!done) in_order = choose<ITEMS, P>(top_k, key, q, check, r.sure, s_e, same);
         clear = clear && in_order;
     }
     if (__any_sync(kAll, scores && live && !clear)) {            // (all tokens of the warp once more)
@@ -412,7 +425,7 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
         }
         __syncwarp();
         if (G > 1) keep_groups<ITEMS, P>(r, whole_lanes, value, key, q, s_value);
-        choose<ITEMS, P>(top_k, key, q, false, s_e, [](int, int) { return true; });
+        choose<ITEMS, P>(top_k, key, q, false, 0.f, s_e, [](int, int) { return true; });
     }
     if (status && __any_sync(kAll, bad && live) && (threadIdx.x & 31) == 0) set_status(status, HL_EINVAL);
     __syncwarp();
