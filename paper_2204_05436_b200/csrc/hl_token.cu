@@ -394,6 +394,15 @@ int window_of(int64_t max_tokens, int64_t dim) {
     return w;
 }
 
+// The windows that at most so many tokens can make: fewer tokens may have shorter windows, but of those that fill the chip.
+int64_t most_windows(int64_t max_tokens, int64_t dim) {
+    const int64_t now = div_up(max_tokens, window_of(max_tokens, dim)), shortest = div_up(max_tokens, 16);
+    int64_t filled = kChipThreads / div_up(dim, 8) + 1;
+    filled = filled < 8192 ? filled : 8192;
+    filled = filled < shortest ? filled : shortest;
+    return now > filled ? now : filled;
+}
+
 // the workspace: two words, and then what either call needs
 struct Workspace {
     int32_t *n, *status, *keys, *vals;
@@ -484,7 +493,7 @@ extern "C" int32_t hl_token_embed(int32_t table_dtype, int64_t n_rows, int64_t d
 extern "C" size_t hl_token_workspace_bytes(int64_t max_tokens, int64_t dim) {
     if (!tokens_ok(max_tokens) || dim < 1 || dim > (int64_t(1) << 24)) return 0;
     const int64_t sort = (2 * padded(max_tokens) + padded(sort_hist_words(max_tokens))) * 4;
-    const int64_t sums = 2 * div_up(max_tokens, window_of(max_tokens, dim)) * (div_up(dim, kPieceStep) * kPieceStep) * 4;
+    const int64_t sums = 2 * most_windows(max_tokens, dim) * (div_up(dim, kPieceStep) * kPieceStep) * 4;
     return (size_t)(kWorkspaceHead + ((sort > sums ? sort : sums) + 255) / 256 * 256);
 }
 

@@ -208,3 +208,177 @@ class ExpertRoute:
         self._call(B.hl_expert_combine_bwd, self._route, B.dtype_of(grad_out), grad_out.shape[1], grad_out, ld_go, y, ld_y, weights,
                    grad_y, ld_gy, grad_weights)
         return grad_y, grad_weights
+
+
+def _count(name: str, n_tokens: Optional[torch.Tensor], device: torch.device) -> None:
+    if n_tokens is not None and (n_tokens.device != device or n_tokens.dtype != torch.int32 or n_tokens.numel() < 1):
+        raise ValueError(f"{name} is an int32 on {device}")
+
+
+def _matrix(name: str, t: torch.Tensor, device: torch.device, rows: Optional[int] = None, dim: Optional[int] = None, dtype=None) -> int:
+    """Checks a matrix of rows whose values lie side by side; returns the values from one row's begin to the next."""
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    B.dtype_of(t)
+    if t.dim() != 2 or t.shape[1] < 1 or (rows is not None and t.shape[0] != rows) or (dim is not None and t.shape[1] != dim) or (
+            dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} is [{'rows' if rows is None else rows}, {'dim' if dim is None else dim}]"
+                         f"{'' if dtype is None else f' of {dtype}'}, not {tuple(t.shape)} of {t.dtype}")
+    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    if (t.shape[1] > 1 and t.stride(1) != 1) or ld < t.shape[1]:
+        raise ValueError(f"the values of a row of {name} lie side by side, and rows do not overlap")
+    return ld
+
+
+def _side_by_side(name: str, t: torch.Tensor, device: torch.device, shape, dtype) -> None:
+    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} is a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+
+
+def _written(written: torch.Tensor, ld: int, *read: Optional[torch.Tensor]) -> None:
+    """What is written (a matrix) shares no byte with what is read."""
+    t = written if written.dim() == 2 else written.view(1, -1)
+    for r in read:
+        if r is not None:
+            m = r if r.dim() == 2 else r.reshape(1, -1)
+            ExpertRoute._apart(_span(t, t.shape[0], ld), _span(m, m.shape[0], m.stride(0) if m.shape[0] > 1 else m.shape[1]))
+
+
+class ExpertRouter:
+    """A router's choice: logits -> (experts, weights), as :class:`ExpertRoute` takes them, and the logits' gradient.
+
+        router = ExpertRouter(top_k=8, n_experts=256, score="sigmoid", n_groups=8, top_groups=4, group_score="top2", scale=2.5)
+        experts, weights = router.choose(logits, bias)       # int32, fp32 [tokens, top_k]
+        route.sort(experts); ...; grad_y, grad_weights = route.combine_backward(grad_out, y, weights)
+        grad_logits = router.backward(logits, experts, grad_weights)
+
+    ``score``: "softmax" or "sigmoid"; ``n_groups`` groups of experts side by side, of which the ``top_groups`` best are kept (a group
+    counts with its best expert, "max", or with the sum of its two best, "top2"); ``renorm``: the chosen scores are divided by their
+    sum; ``scale``: of the weights.  A router has no buffers of its own but a status word: its calls may be made on any streams."""
+
+    def __init__(self, top_k: int, n_experts: int, score: str = "softmax", n_groups: int = 1, top_groups: int = 1,
+                 group_score: str = "max", renorm: bool = True, scale: float = 1.0, device: str = "cuda:0"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("the Hotline library needs a CUDA device (there is no CPU fallback)")
+        scores, groups = {"softmax": B.HL_SCORE_SOFTMAX, "sigmoid": B.HL_SCORE_SIGMOID}, {"max": B.HL_GROUP_MAX, "top2": B.HL_GROUP_TOP2}
+        if score not in scores or group_score not in groups:
+            raise ValueError("score is softmax or sigmoid, group_score max or top2")
+        if not (1 <= n_experts <= B.HL_MAX_EXPERTS and 1 <= top_k <= min(n_experts, B.HL_MAX_TOP_K) and 1 <= n_groups <= B.HL_MAX_GROUPS
+                and n_experts % n_groups == 0 and 1 <= top_groups <= n_groups and top_k <= n_experts // n_groups * top_groups
+                and math.isfinite(scale)):
+            raise ValueError(f"1 to {B.HL_MAX_TOP_K} of 1 to {B.HL_MAX_EXPERTS} experts, in 1 to {B.HL_MAX_GROUPS} groups of one size, "
+                             "the kept ones of which have top_k; a finite scale")
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.top_k, self.n_experts = int(top_k), int(n_experts)
+        self._router = B.make_router(scores[score], top_k, n_experts, n_groups, top_groups, groups[group_score], renorm, scale)
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)
+
+    def choose(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, n_tokens: Optional[torch.Tensor] = None,
+               out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """``bias`` (fp32 [n_experts]): added to the scores for the choice, not to the weights.  ``n_tokens`` (int32 [1], on the device):
+        how many tokens there are; those behind them are left as they are in ``out`` (-1 and 0 without it)."""
+        ld, tokens = _matrix("logits", logits, self.device, dim=self.n_experts), logits.shape[0]
+        _count("n_tokens", n_tokens, self.device)
+        if bias is not None:
+            _side_by_side("bias", bias, self.device, (self.n_experts,), torch.float32)
+        if out is None:
+            experts = torch.full((tokens, self.top_k), -1, dtype=torch.int32, device=self.device)
+            weights = torch.zeros(tokens, self.top_k, dtype=torch.float32, device=self.device)
+        else:
+            experts, weights = out
+            _side_by_side("experts", experts, self.device, (tokens, self.top_k), torch.int32)
+            _side_by_side("weights", weights, self.device, (tokens, self.top_k), torch.float32)
+            _written(experts, self.top_k, logits, bias, weights, n_tokens)
+            _written(weights, self.top_k, logits, bias, n_tokens)
+        with torch.cuda.device(self.device):
+            B.hl_expert_choose(self._router, B.dtype_of(logits), logits, ld, bias, tokens, n_tokens, experts, weights, self._status,
+                               torch.cuda.current_stream(self.device).cuda_stream)
+        return experts, weights
+
+    def backward(self, logits: torch.Tensor, experts: torch.Tensor, grad_weights: torch.Tensor,
+                 n_tokens: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The logits' gradient, from choose's logits and experts (rows behind the last token: as in ``out``, or zeros)."""
+        ld, tokens = _matrix("logits", logits, self.device, dim=self.n_experts), logits.shape[0]
+        _count("n_tokens", n_tokens, self.device)
+        _side_by_side("experts", experts, self.device, (tokens, self.top_k), torch.int32)
+        _side_by_side("grad_weights", grad_weights, self.device, (tokens, self.top_k), torch.float32)
+        if out is None:
+            out = torch.zeros(tokens, self.n_experts, dtype=logits.dtype, device=self.device)
+        ld_out = _matrix("out", out, self.device, tokens, self.n_experts, logits.dtype)
+        _written(out, ld_out, logits, experts, grad_weights, n_tokens)
+        with torch.cuda.device(self.device):
+            B.hl_expert_choose_bwd(self._router, B.dtype_of(logits), logits, ld, tokens, n_tokens, experts, grad_weights, out, ld_out,
+                                   torch.cuda.current_stream(self.device).cuda_stream)
+        return out
+
+    def status(self, raise_on_error: bool = True) -> int:
+        """Waits for the device: HL_OK, or HL_EINVAL if a logit or a bias was NaN (that expert was not chosen) since the last call."""
+        torch.cuda.synchronize(self.device)
+        st = int(self._status.item())
+        self._status.zero_()
+        if raise_on_error:
+            B._check("hl_expert_choose", st)
+        return st
+
+
+class Mx4Weights:
+    """The weights of experts, [n_experts, outputs, dim], in 4 bits (blocks of 32 values of a row share a power of two), and the
+    product with them.  For serving: there is no gradient.
+
+        w = Mx4Weights(weights)                              # laid out once
+        y = w.product(route, x)                              # x: the tokens' rows; y by expert, as route.dispatch would lay them out
+        z = w2.product(route, act(y), by_token=False)        # rows by expert
+        out = route.combine(z, weights)
+
+    A product takes the workspace of its own matrix: products with one Mx4Weights belong in the order of one stream."""
+
+    def __init__(self, weights: torch.Tensor):
+        if not torch.cuda.is_available():
+            raise RuntimeError("the Hotline library needs a CUDA device (there is no CPU fallback)")
+        if weights.dim() != 3 or not weights.is_cuda or not 1 <= weights.shape[0] <= B.HL_MAX_EXPERTS or not weights.is_contiguous() or (
+                weights.shape[1] < 1 or weights.shape[2] < 1):
+            raise ValueError(f"weights is a contiguous [experts, outputs, dim] on a CUDA device, of 1 to {B.HL_MAX_EXPERTS} experts")
+        self.device = weights.device
+        self.n_experts, self.outputs, self.dim = weights.shape
+        self._q = torch.empty(self.n_experts * B.hl_mx4_bytes(self.outputs, self.dim), dtype=torch.uint8, device=self.device)
+        self._ws: list = []                                  # the last is the largest; a captured graph may hold on to any
+        self._call(B.hl_mx4_quantise, B.dtype_of(weights), self.n_experts, self.outputs, self.dim, weights, self.dim,
+                   self.outputs * self.dim, self._q)
+
+    def _call(self, f, *a) -> None:
+        with torch.cuda.device(self.device):
+            f(*a, torch.cuda.current_stream(self.device).cuda_stream)
+
+    def dequantise(self, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+        out = torch.empty(self.n_experts, self.outputs, self.dim, dtype=dtype, device=self.device)
+        self._call(B.hl_mx4_dequantise, self.n_experts, self.outputs, self.dim, self._q, B.dtype_of(out), out, self.dim,
+                   self.outputs * self.dim)
+        return out
+
+    def product(self, route: ExpertRoute, x: torch.Tensor, by_token: bool = True, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Rows by expert times their expert's weights, both in 4 bits, added up in fp32.  ``by_token``: x has the rows of the route's
+        tokens, which go to their experts on the way; else the experts' rows.  Rows that fill an expert up become zeros, rows
+        behind the last expert's stay as they are in ``out`` (zeros without it)."""
+        if route.device != self.device or route.n_experts != self.n_experts:
+            raise ValueError(f"the route is of {route.n_experts} experts on {route.device}, the weights of {self.n_experts} on {self.device}")
+        ld = _matrix("x", x, self.device, route.tokens if by_token else route.cap_rows, self.dim)
+        if out is None:
+            out = torch.zeros(route.cap_rows, self.outputs, dtype=x.dtype, device=self.device)
+        ld_out = _matrix("out", out, self.device, route.cap_rows, self.outputs, x.dtype)
+        _written(out, ld_out, x)
+        need = B.hl_expert_mx4_workspace_bytes(route.cap_rows, self.n_experts, self.dim)
+        if not self._ws or self._ws[-1].numel() < need:
+            self._ws.append(torch.zeros(need, dtype=torch.uint8, device=self.device))
+        self._call(B.hl_expert_mx4, route._route, B.dtype_of(x), self.dim, self.outputs, x, ld, by_token, self._q, out, ld_out,
+                   self._ws[-1], self._ws[-1].numel())
+        return out
+
+    def status(self, raise_on_error: bool = True) -> int:
+        """Waits for the device: HL_OK, or HL_ETIMEOUT if a wait inside the last product gave up."""
+        torch.cuda.synchronize(self.device)
+        st = int(self._ws[-1][:4].view(torch.int32).item()) if self._ws else B.HL_OK
+        if raise_on_error:
+            B._check("hl_expert_mx4", st)
+        return st
