@@ -545,6 +545,7 @@ __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__
     dot = sum_of<P>(dot);
     if (!renorm) sum = softmax ? z : 1.f;
     const float per = sum > 0.f ? 1.f / sum : 0.f, mean = renorm || softmax ? dot * per : 0.f;
+    __syncwarp();
     // d/dl of the weights: scale * share * (grad - mean), times 1 - score for sigmoids
     for (int k = q; k < top_k; k += P) {
         float s = first, rest = first_rest, g = first_g;
@@ -553,7 +554,11 @@ __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__
             s = score(logit(e), &rest);
             g = __ldg(&grad_w[at * top_k + k]);
         }
-        s_grad[mine][k] = e < 0 ? 0.f : scale * (s * per) * (g - mean) * rest;
+        // (the mean is of all experts' softmax: once for an expert, however often it is there)
+        bool again = false;
+        if (dense)
+            for (int i = 0; i < k; ++i) again = again || s_chosen[mine][i] == e;
+        s_grad[mine][k] = e < 0 ? 0.f : scale * (s * per) * (again ? g : g - mean) * rest;
     }
     if (!live) return;
     if (dense)

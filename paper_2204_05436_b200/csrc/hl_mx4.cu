@@ -731,7 +731,10 @@ extern "C" int32_t hl_expert_mx4(const hl_route* route, int32_t dtype, int64_t d
         !d_weights || !lies_at(d_weights, 16) || !d_workspace || !lies_at(d_workspace, 256))
         return HL_EINVAL;
     if (ws_bytes < hl_expert_mx4_workspace_bytes(r->cap_rows, r->n_experts, dim)) return HL_ECAPACITY;
-    if (r->cap_rows == 0) return HL_OK;
+    if (r->cap_rows == 0) {                                      // (no more than the status)
+        HL_CUDA_TRY(clear_words(static_cast<uint32_t*>(d_workspace), 4, stream));
+        return HL_OK;
+    }
     const bool whole = dim % 8 == 0 && rows_lie_at(dtype, d_x, ld_x, 16);
 #define HL_PRODUCT(T) launch_product<T>(r, dim, outputs, d_x, ld_x, by_token != 0, d_weights, d_y, ld_y, d_workspace, whole, stream)
     return HL_FOR_TYPE(HL_PRODUCT);
