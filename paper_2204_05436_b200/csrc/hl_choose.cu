@@ -88,7 +88,6 @@ __device__ __forceinline__ float near_inverse(float x) {
 }
 constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float near_sigmoid(float l) { return near_inverse(1.f + near_exp2(-kLog2e * l)); }
-__device__ __forceinline__ float near_part(float l, float m) { return l == m ? 1.f : near_exp2(kLog2e * (l - m)); }
 
 // what a call goes by
 struct Router {
@@ -341,14 +340,21 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
     }
     // of all scores, where they are needed: the largest logit and the sum of e^(l - largest)
     const bool scores = bias || (G > 1 && r.pair);
-    float top = none, z = 1.f;
+    float top = none, z = 1.f, value[ITEMS];
     if (r.softmax && (scores || !r.renorm)) {
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j) top = fmaxf(top, l[j]);
         top = max_of<P>(top);
         z = 0.f;
+        if (fabsf(top) < INFINITY) {
 #pragma unroll
-        for (int j = 0; j < ITEMS; ++j) z += l[j] > none ? part(l[j], top) : 0.f;
+            for (int j = 0; j < ITEMS; ++j) value[j] = near_exp2(kLog2e * (l[j] - top));      // (0 of -inf)
+        } else {
+#pragma unroll
+            for (int j = 0; j < ITEMS; ++j) value[j] = l[j] > none && l[j] == top ? 1.f : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < ITEMS; ++j) z += value[j];
         z = sum_of<P>(z);
     }
     bool clear = true;
@@ -357,11 +363,10 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j) key[j] = l[j];
         if (scores) {
-            float value[ITEMS];
             if (r.softmax) {
                 const float per = near_inverse(z);
 #pragma unroll
-                for (int j = 0; j < ITEMS; ++j) value[j] = near_part(l[j], top) * per;
+                for (int j = 0; j < ITEMS; ++j) value[j] *= per;
             } else {
 #pragma unroll
                 for (int j = 0; j < ITEMS; ++j) value[j] = near_sigmoid(l[j]);
@@ -500,12 +505,24 @@ __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__
 
     float top = none, z = 1.f;
     if (dense) {
-        for (int c = q; c < E; c += P) top = fmaxf(top, logit(c));
+        // (the row stays in the L1 for the next two rounds)
+        for (int c = q * N; c < E; c += P * N) {
+            Pack<T, N> v;
+            float x[N];
+            v.load(row + c);
+            v.get(x);
+#pragma unroll
+            for (int k = 0; k < N; ++k) top = fmaxf(top, x[k]);  // (which is not NaN where one of the two is)
+        }
         top = max_of<P>(top);
         z = 0.f;
-        for (int c = q; c < E; c += P) {
-            const float x = logit(c);
-            z += x > none ? part(x, top) : 0.f;
+        for (int c = q * N; c < E; c += P * N) {
+            Pack<T, N> v;
+            float x[N];
+            v.load(row + c);
+            v.get(x);
+#pragma unroll
+            for (int k = 0; k < N; ++k) z += x[k] > none ? part(x[k], top) : 0.f;
         }
         z = sum_of<P>(z);
     }

@@ -431,7 +431,7 @@ template <typename T>
 __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ wq,
                                                                const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets,
                                                                int E, int64_t cap_rows, int max_tiles, int col_tiles, int f_tiles,
-                                                               int64_t outputs, T* __restrict__ y, int64_t ld, int stages,
+                                                               int64_t outputs, T* __restrict__ y, int64_t ld, bool lines, int stages,
                                                                int panel_rows, int32_t* status) {
     extern __shared__ uint8_t s_raw[];
     uint8_t* base = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
@@ -579,8 +579,20 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) bar_arrive(&s_taken[buffer]);
-            if (f < outputs)
-                for (int64_t p = half; p < it.pad; p += 2) y[(it.row0 + it.rows + p) * ld + f] = from_float<T>(0.f);
+            if (it.pad) {
+                const int64_t f0 = (int64_t)it.f * kTileRows;
+                const int width = (int)min((int64_t)kTileRows, outputs - f0), tid = threadIdx.x - 64;
+                T* pads = y + (it.row0 + it.rows) * ld + f0;
+                constexpr int N = 16 / sizeof(T);
+                if (lines) {           // (all rows of y, and their tiles of outputs, begin at multiples of 16 bytes, and are whole ones)
+                    const int per = width / N;
+                    for (int64_t p = tid / (kTileRows / N); p < it.pad; p += 256 / (kTileRows / N))
+                        if (tid % (kTileRows / N) < per) reinterpret_cast<uint4*>(pads + p * ld)[tid % (kTileRows / N)] = make_uint4(0, 0, 0, 0);
+                } else {
+                    for (int64_t p = tid / kTileRows; p < it.pad; p += 256 / kTileRows)
+                        if (tid % kTileRows < width) pads[p * ld + tid % kTileRows] = from_float<T>(0.f);
+                }
+            }
             buffer ^= 1;
             phase ^= buffer == 0;
         }
@@ -664,7 +676,7 @@ int32_t launch_product(const hl_route* r, int64_t dim, int64_t outputs, const vo
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem) != cudaSuccess) return HL_ECUDA;
     HL_CUDA_TRY(launch_after(kernel, grid_for(rt * ft, 1, kSMs), kProductNT, kProductSmem, stream, (const uint8_t*)q,
                              static_cast<const uint8_t*>(w), r->counts, r->offsets, r->n_experts, r->cap_rows, rt, ct, ft, outputs,
-                             static_cast<T*>(y), ld_y, stages, panel, status));
+                             static_cast<T*>(y), ld_y, outputs * sizeof(T) % 16 == 0 && ld_y * sizeof(T) % 16 == 0 && lies_at(y, 16), stages, panel, status));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;

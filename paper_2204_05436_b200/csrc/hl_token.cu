@@ -82,18 +82,63 @@ __global__ void __launch_bounds__(kNT) k_token_embed_loose(const TT* __restrict_
 }
 
 // ---- the sort -----------------------------------------------------------------------------------------------------------
+// Few tokens: a token's place is how many are below it, and equal ones in front of it; each is compared with all.  (Some 4 us of one
+// kernel for 2 048, where making pairs and sorting them takes two kernels and 15 us, whatever their number.)
+constexpr int kFewTokens = 2048, kFewNT = 128;
+__global__ void __launch_bounds__(kFewNT) k_token_rank(const int32_t* __restrict__ tokens, int max_tokens, const int32_t* n_tokens,
+                                                       int n_rows, int32_t* __restrict__ sorted, int32_t* __restrict__ order,
+                                                       int32_t* status) {
+    __shared__ __align__(16) int32_t s_key[kFewTokens + 4];
+    const int n = (int)live_tokens(n_tokens, max_tokens), me = blockIdx.x * kFewNT + threadIdx.x;
+    if ((int)blockIdx.x * kFewNT >= n) return;
+    for (int i = threadIdx.x; i < (n + 3) / 4 * 4; i += kFewNT) {
+        const int t = i < n ? __ldg(&tokens[i]) : n_rows;        // (those that fill the last four up are behind all)
+        const bool row = (unsigned)t < (unsigned)n_rows;
+        if (!row && t != -1 && i == me && i < n && status) set_status(status, HL_EBOUNDS);
+        s_key[i] = row ? t : n_rows;
+    }
+    __syncthreads();
+    if (me >= n) return;
+    const int key = s_key[me];
+    int rank = 0;
+    // keys in front of mine count if they are not above it, those behind if they are below it
+    const int quads = me / 4;
+#pragma unroll 4
+    for (int i = 0; i < quads; ++i) {
+        const int4 k = reinterpret_cast<const int4*>(s_key)[i];
+        rank += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
+    }
+    for (int i = quads * 4; i < quads * 4 + 4; ++i) rank += i < me ? s_key[i] <= key : s_key[i] < key;
+#pragma unroll 4
+    for (int i = quads + 1; i < (n + 3) / 4; ++i) {
+        const int4 k = reinterpret_cast<const int4*>(s_key)[i];
+        rank += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+    }
+    sorted[rank] = key;
+    order[rank] = me;
+}
+
+// Many: pairs of row and place, for the sort by digits, whose counts are made here too.
 __global__ void __launch_bounds__(kNT) k_token_pairs(const int32_t* __restrict__ tokens, int64_t max_tokens, const int32_t* n_tokens,
                                                      int n_rows, int32_t* __restrict__ keys, int32_t* __restrict__ vals,
-                                                     int32_t* n_out, int32_t* status) {
+                                                     int32_t* n_out, int passes, uint32_t* __restrict__ counts, int32_t* status) {
+    __shared__ uint32_t s_counts[4 * 256];
     const int64_t n = live_tokens(n_tokens, max_tokens);
     if (blockIdx.x == 0 && threadIdx.x == 0) *n_out = (int32_t)n;
+    for (int i = threadIdx.x; i < passes * 256; i += kNT) s_counts[i] = 0;
+    __syncthreads();
     for (int64_t i = (int64_t)blockIdx.x * kNT + threadIdx.x; i < n; i += (int64_t)gridDim.x * kNT) {
         const int t = __ldg(&tokens[i]);
         const bool row = (unsigned)t < (unsigned)n_rows;
         if (!row && t != -1) set_status(status, HL_EBOUNDS);
-        keys[i] = row ? t : n_rows;
+        const int key = row ? t : n_rows;
+        keys[i] = key;
         vals[i] = (int32_t)i;
+        for (int p = 0; p < passes; ++p) atomicAdd(&s_counts[p * 256 + ((key >> (8 * p)) & 255)], 1u);
     }
+    __syncthreads();
+    for (int i = threadIdx.x; i < passes * 256; i += kNT)
+        if (s_counts[i]) atomicAdd(&counts[i], s_counts[i]);
 }
 
 // ---- the table's gradient -------------------------------------------------------------------------------------------------
@@ -101,7 +146,7 @@ __global__ void __launch_bounds__(kNT) k_token_pairs(const int32_t* __restrict__
 // gradients of each run of equal tokens.  A run inside the window goes to its row; of one that begins before the window or goes on
 // behind it only a piece is known, which goes to memory: piece 2w is that of the run which began before window w, 2w + 1 that of the
 // one that begins in it and goes on.  A second kernel adds the pieces of such a run up, in their order.  Rows without tokens are
-// zeroed by CTAs of their own.  LOOSE: rows that begin anywhere; a group is a warp then, eight columns a lane.
+// zeroed by CTAs of their own.  LOOSE: rows that begin anywhere; a group is a warp at most then, eight columns a lane.
 constexpr int kPieceStep = 8;          // a piece's columns are filled up to a multiple of this
 __device__ __forceinline__ int64_t piece_pitch(int dim) { return (dim + kPieceStep - 1) / kPieceStep * kPieceStep; }
 
@@ -115,10 +160,15 @@ __device__ __forceinline__ int64_t not_below(const int32_t* __restrict__ sorted,
     return lo;
 }
 
-// row[c ..] = scale * sum (+ row).  LOOSE: by a whole warp, 256 columns from c - 8 * lane on, in the order of the lanes (s: [256]).
+// row[c ..] = scale * sum (+ row).  LOOSE: by a whole warp, 256 columns from c - 8 * lane on, in the order of the lanes (s: [256]), or,
+// without s, each thread by itself.
 template <typename TT, int W, bool LOOSE>
 __device__ __forceinline__ void put(TT* row, int c, int dim, const float (&sum)[W], float scale, bool accumulate, float* s) {
-    if constexpr (LOOSE) {
+    if (LOOSE && !s) {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (c + i < dim) row[c + i] = from_float<TT>(scale * sum[i] + (accumulate ? as_float(row[c + i]) : 0.f));
+    } else if constexpr (LOOSE) {
         const int lane = threadIdx.x & 31;
         __syncwarp();
         Pack<float, W> mine;
@@ -246,8 +296,8 @@ __global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ 
     if (first >= n) return;
     const int begin = (int)first, end = (int)min(first + window, n);       // (there are less than 2^30 tokens)
     const int c = ((int)blockIdx.y * P + sub) * W;
-    if (!LOOSE && c >= dim) return;
-    float* s = LOOSE ? s_put + (threadIdx.x & ~31) * W : nullptr;
+    if (c >= dim && !(LOOSE && P == 32)) return;                 // (a warp that writes together stays together)
+    float* s = LOOSE && P == 32 ? s_put + (threadIdx.x & ~31) * W : nullptr;
     float sum[W] = {};
     int run = __ldg(&sorted[begin]);
     bool open = begin > 0 && __ldg(&sorted[begin - 1]) == run;             // began before the window
@@ -302,38 +352,47 @@ __global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ 
 // pieces each, in order, and add the parts up in order.  32 W columns a CTA.  (A CTA a window, most of which end at once: 24 us
 // instead of ... for 512 windows of 2 048 columns.)
 constexpr int kShort = 16;
+// Pieces p0 .. p1 of the run that begins in window w.  A warp's groups of P lanes, which have all columns, take every so many of them
+// and are added up by halves.
 template <int W>
-__device__ __forceinline__ void add_pieces(const float* __restrict__ pieces, int64_t pitch, int64_t w, int64_t p0, int64_t p1, int c, int dim,
+__device__ __forceinline__ void add_pieces(const float* __restrict__ pieces, int64_t pitch, int64_t w, int p0, int p1, int c, int dim, int P,
                                            float (&sum)[W]) {
     constexpr int U = 8;
-    for (int64_t p = p0; p < p1; p += U) {
-        Pack<float, W> in[U];
+    const int groups = 32 / P;
+    const float* column = pieces + (c < dim ? c : 0);
+    for (int p = p0 + (threadIdx.x & 31) / P; p < p1; p += U * groups) {
+        Pack<float, W> in[U];          // (asked for without a condition, so that all are on their way before the first is added)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            in[u].zero();
-            if (p + u < p1 && c < dim) in[u].load(pieces + (2 * (w + p + u) + (p + u == 0 ? 1 : 0)) * pitch + c);
+            const int at = min(p + u * groups, p1 - 1);
+            in[u].load(column + (2 * (w + at) + (at == 0 ? 1 : 0)) * pitch);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float x[W];
             in[u].get(x);
 #pragma unroll
-            for (int i = 0; i < W; ++i) sum[i] += x[i];
+            for (int i = 0; i < W; ++i) sum[i] += p + u * groups < p1 ? x[i] : 0.f;
         }
     }
+    __syncwarp();
+    for (int d = P; d < 32; d *= 2)
+#pragma unroll
+        for (int i = 0; i < W; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], d);
 }
 
 template <typename TT, int W, bool LOOSE>
 __global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__ sorted, int64_t max_tokens, const int32_t* n_tokens,
                                                      int n_rows, int dim, float scale, TT* __restrict__ table, int64_t ld_table,
-                                                     int accumulate, int window, const float* __restrict__ pieces) {
+                                                     int accumulate, int window, int P, const float* __restrict__ pieces) {
     constexpr int kWarps = kNT / 32;
     __shared__ __align__(16) float s_sum[kNT * W];               // of each warp: [32 W]
     __shared__ int s_long[kWarps];                               // the run of a warp's window, if it is long
     wait_for_last();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t n = live_tokens(n_tokens, max_tokens), first = (int64_t)blockIdx.x * kWarps, pitch = piece_pitch(dim);
-    const int c = ((int)blockIdx.y * 32 + lane) * W;
+    const int c = ((int)blockIdx.y * P + lane % P) * W;          // (P lanes: 32, or as many as have all columns)
+    const bool writes = lane < P;
     const int64_t w = first + warp, end = (w + 1) * window;
     int begins = -1;                                             // the run that begins in the window and goes on
     if (end < n) {
@@ -347,8 +406,9 @@ __global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__
             begins = run;
             if (more < kShort) {
                 float sum[W] = {};
-                add_pieces<W>(pieces, pitch, w, 0, more + 1, c, dim, sum);
-                if (LOOSE || c < dim) put<TT, W, LOOSE>(table + run * ld_table, c, dim, sum, scale, accumulate, s_sum + warp * 32 * W);
+                add_pieces<W>(pieces, pitch, w, 0, more + 1, c, dim, P, sum);
+                if (writes && (LOOSE || c < dim))
+                    put<TT, W, LOOSE>(table + run * ld_table, c, dim, sum, scale, accumulate, P == 32 ? s_sum + warp * 32 * W : nullptr);
                 begins = -1;
             }
         }
@@ -358,16 +418,16 @@ __global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__
     for (int k = 0; k < kWarps; ++k) {
         const int run = s_long[k];
         if (run < 0) continue;
-        int64_t all = 1;                                         // its pieces
+        int all = 1;                                             // its pieces
         for (int64_t v = first + k + 1; v * window < n; v += kNT) {
             const int64_t at = (v + threadIdx.x) * window;
             const int more = __syncthreads_count(at < n && __ldg(&sorted[min(at, n - 1)]) == run);
             all += more;
             if (more < kNT) break;
         }
-        const int64_t per = (all + kWarps - 1) / kWarps, p0 = min(warp * per, all), p1 = min(p0 + per, all);
+        const int per = (all + kWarps - 1) / kWarps, p0 = min(warp * per, all), p1 = min(p0 + per, all);
         float sum[W] = {};
-        add_pieces<W>(pieces, pitch, first + k, p0, p1, c, dim, sum);
+        add_pieces<W>(pieces, pitch, first + k, p0, p1, c, dim, P, sum);
 #pragma unroll
         for (int i = 0; i < W; ++i) s_sum[(warp * W + i) * 32 + lane] = sum[i];
         __syncthreads();
@@ -375,7 +435,8 @@ __global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__
             for (int s = 1; s < kWarps; ++s)
 #pragma unroll
                 for (int i = 0; i < W; ++i) sum[i] += s_sum[(s * W + i) * 32 + lane];
-            if (LOOSE || c < dim) put<TT, W, LOOSE>(table + run * ld_table, c, dim, sum, scale, accumulate, s_sum);
+            if (writes && (LOOSE || c < dim))
+                put<TT, W, LOOSE>(table + run * ld_table, c, dim, sum, scale, accumulate, P == 32 ? s_sum : nullptr);
         }
         __syncthreads();
     }
@@ -442,8 +503,8 @@ template <typename TG, typename TT, int W, int U, bool LOOSE>
 int32_t launch_sums(int64_t n_rows, int64_t dim, const int32_t* sorted, const int32_t* order, int64_t max_tokens,
                     const int32_t* n_tokens, const void* grad, int64_t ld_grad, float scale, void* table, int64_t ld_table,
                     int accumulate, float* pieces, cudaStream_t stream) {
-    int P = LOOSE ? 32 : 1;
-    while (!LOOSE && P < kNT && P * W < dim) P *= 2;
+    int P = 1;
+    while (P < (LOOSE ? 32 : kNT) && P * W < dim) P *= 2;
     const int window = window_of(max_tokens, dim);
     const int64_t windows = div_up(max_tokens, window), sums = div_up(windows, kNT / P);
     // rows without tokens: some 128 KB a CTA
@@ -457,9 +518,10 @@ int32_t launch_sums(int64_t n_rows, int64_t dim, const int32_t* sorted, const in
                        static_cast<TT*>(table), ld_table, accumulate, window, P, (int)sums, (int)per, pieces));
     note_launches(1);
     if (windows > 1) {
-        HL_CUDA_TRY(launch_after(k_token_joins<TT, W, LOOSE>, dim3((unsigned)div_up(windows - 1, kNT / 32), (unsigned)div_up(dim, 32 * W)),
+        const int Q = P < 32 ? P : 32;
+        HL_CUDA_TRY(launch_after(k_token_joins<TT, W, LOOSE>, dim3((unsigned)div_up(windows - 1, kNT / 32), (unsigned)div_up(dim, Q * W)),
                                  kNT, 0, stream, sorted, max_tokens, n_tokens, (int)n_rows, (int)dim, scale, static_cast<TT*>(table),
-                                 ld_table, accumulate, window, (const float*)pieces));
+                                 ld_table, accumulate, window, Q, (const float*)pieces));
         note_launches(1);
     }
     HL_LAUNCH_CHECK();
@@ -508,6 +570,13 @@ extern "C" int32_t hl_token_sort(const int32_t* d_tokens, int64_t max_tokens, co
     if (ws_bytes < hl_token_workspace_bytes(max_tokens, 1)) return HL_ECAPACITY;
     if (max_tokens == 0) return HL_OK;
     const Workspace ws = layout(d_workspace, max_tokens);
+    if (max_tokens <= kFewTokens) {
+        HL_CUDA_TRY(launch(k_token_rank, (unsigned)div_up(max_tokens, kFewNT), kFewNT, stream, d_tokens, (int)max_tokens, d_n_tokens,
+                           (int)n_rows, d_sorted, d_order, d_status));
+        note_launches(1);
+        HL_LAUNCH_CHECK();
+        return HL_OK;
+    }
     int bits = 1;
     while ((n_rows >> bits) != 0) ++bits;
     const int out = ((bits + 7) / 8) & 1;                        // which of the two buffers the sort ends in
@@ -517,10 +586,13 @@ extern "C" int32_t hl_token_sort(const int32_t* d_tokens, int64_t max_tokens, co
     keys[out ^ 1] = ws.keys;
     vals[out ^ 1] = ws.vals;
     int32_t* status = d_status ? d_status : ws.status;
-    HL_CUDA_TRY(launch(k_token_pairs, grid_for(max_tokens, kNT, 2048), kNT, stream, d_tokens, max_tokens, d_n_tokens, (int)n_rows,
-                       keys[0], vals[0], ws.n, status));
+    // (a sort that counts no digits, in one cluster, has none to clear either)
+    const int64_t clear = sort_clear_words(max_tokens, bits, WaitCfg());
+    if (clear) HL_CUDA_TRY(clear_words(ws.hist, clear, stream));
+    HL_CUDA_TRY(launch(k_token_pairs, grid_for(max_tokens, kNT * (clear ? 8 : 1), 2048), kNT, stream, d_tokens, max_tokens, d_n_tokens,
+                       (int)n_rows, keys[0], vals[0], ws.n, clear ? (bits + 7) / 8 : 0, ws.hist, status));
     note_launches(1);
-    return radix_sort_pairs(keys, vals, ws.n, max_tokens, bits, ws.hist, status, &sorted, &order, stream);
+    return radix_sort_pairs(keys, vals, ws.n, max_tokens, bits, ws.hist, status, &sorted, &order, stream, WaitCfg(), clear != 0);
 }
 
 extern "C" int32_t hl_token_embed_bwd(int64_t n_rows, int64_t dim, const int32_t* d_sorted, const int32_t* d_order,
