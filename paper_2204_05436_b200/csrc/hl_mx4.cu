@@ -101,7 +101,7 @@ constexpr int kRowNT = 256;
 
 // n / d by 2^64 / d, rounded up: exact for n * d < 2^64
 struct Divisor {
-    unsigned long long inverse;
+    uint64_t inverse;
     int64_t d;
     __device__ __forceinline__ int64_t operator()(int64_t n) const { return d == 1 ? n : (int64_t)__umul64hi((uint64_t)n, inverse); }
 };
@@ -110,8 +110,9 @@ struct Divisor {
 // those that fill its last tile up; chunks: of U parts, in a row)
 template <typename T, bool WHOLE, int U>
 __global__ void __launch_bounds__(kRowNT) k_mx4_quantise(const T* __restrict__ x, int64_t rows, int64_t dim, int64_t ld, int64_t stride,
-                                                         Divisor rows_of, Divisor chunks, int col_tiles, int64_t items,
-                                                         uint8_t* __restrict__ q) {
+                                                         uint64_t rows_inverse, int64_t rows_d, uint64_t chunks_inverse,
+                                                         int64_t chunks_d, int col_tiles, int64_t items, uint8_t* __restrict__ q) {
+    const Divisor rows_of{rows_inverse, rows_d}, chunks{chunks_inverse, chunks_d};
     const int lane = threadIdx.x & 31;
     const int64_t item = (int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5);
     if (item >= items) return;
@@ -149,8 +150,10 @@ __device__ __forceinline__ void from_four_bits(uint32_t packed, uint32_t E, floa
 // row of a lane's own, two halves of a line each: 4.8 instead of ... TB/s).
 template <typename T, bool WHOLE, int U>
 __global__ void __launch_bounds__(kRowNT) k_mx4_dequantise(const uint8_t* __restrict__ q, int64_t row_tiles, int64_t dim,
-                                                           Divisor rows_of, Divisor chunks, int col_tiles, int64_t items,
-                                                           T* __restrict__ out, int64_t ld, int64_t stride) {
+                                                           uint64_t rows_inverse, int64_t rows_d, uint64_t chunks_inverse,
+                                                           int64_t chunks_d, int col_tiles, int64_t items, T* __restrict__ out,
+                                                           int64_t ld, int64_t stride) {
+    const Divisor rows_of{rows_inverse, rows_d}, chunks{chunks_inverse, chunks_d};
     constexpr int N = 16 / sizeof(T), S = 8 / N;                 // values of a store, stores of a part
     const int lane = threadIdx.x & 31;
     const int64_t item = (int64_t)blockIdx.x * (kRowNT / 32) + (threadIdx.x >> 5);
@@ -254,13 +257,14 @@ __device__ __forceinline__ int last_not_above(const int* list, int n, int v) {
 // times U parts of a row; its lanes find where each of the row's choices lies.
 constexpr int kRowParts = 4;
 template <typename T, bool WHOLE>
-__global__ void __launch_bounds__(kRowNT, 4) k_mx4_rows(const T* __restrict__ x, int64_t ld, int dim, int col_tiles, int span, Divisor items_of,
-                                                        const int32_t* n_tokens, int64_t max_rows, int top_k,
+__global__ void __launch_bounds__(kRowNT, 4) k_mx4_rows(const T* __restrict__ x, int64_t ld, int dim, int col_tiles, int span,
+                                                        uint64_t items_inverse, int64_t items_d, const int32_t* n_tokens, int64_t max_rows, int top_k,
                                                         const int32_t* __restrict__ place, const int32_t* __restrict__ counts,
                                                         const int32_t* __restrict__ offsets, int E, int64_t cap_rows, int max_tiles,
                                                         uint8_t* __restrict__ q, int32_t* status) {
     __shared__ int s_first[HL_MAX_EXPERTS + 1], s_begin[HL_MAX_EXPERTS];
     constexpr int U = kRowParts;
+    const Divisor items_of{items_inverse, items_d};
     let_next_start();
     if (blockIdx.x == 0 && threadIdx.x == 0) *status = HL_OK;
     const Experts experts{counts, offsets, E, cap_rows};
@@ -312,6 +316,21 @@ __global__ void __launch_bounds__(kRowNT, 4) k_mx4_rows(const T* __restrict__ x,
 }
 
 // ---- the product --------------------------------------------------------------------------------------------------------
+// Few rows, 16 in all at most (a token or two that are being served): the product's CTAs put them into 4 bits themselves, each those of
+// its tile, straight into shared memory -- one kernel instead of two, one behind the other.
+constexpr int kFewRows = 16;
+// The row of x that expert-ordered row `at` gets (-1: none), asked by a whole warp; place: of x's rows by token, NULL: they are in the
+// experts' order.
+__device__ __forceinline__ int64_t row_of(int64_t at, const int32_t* __restrict__ place, const int32_t* n_tokens, int64_t max_tokens, int top_k) {
+    if (!place) return at;
+    const int lane = threadIdx.x & 31;
+    int64_t tokens = max_tokens;
+    if (n_tokens) tokens = min(tokens, (int64_t)max(__ldg(n_tokens), 0));
+    const int choices = (int)tokens * top_k;                     // (kFewRows at most)
+    const unsigned here = __ballot_sync(0xffffffffu, lane < choices && __ldg(&place[min(lane, max(choices - 1, 0))]) == at);
+    return here ? (__ffs(here) - 1) / top_k : -1;
+}
+
 // y[row, f] = sum over d of x[row, d] * w[e, f, d] for the rows of expert e: 128 outputs f (the lanes of the tensor memory) by up to
 // 240 rows (its columns) at a time, 256 of d a step.  One warp's thread has the tiles of a step copied, one issues the products,
 // eight warps take the sums out, those of one tile while the next one's are made.
@@ -427,8 +446,10 @@ __device__ __forceinline__ Item item_of(int64_t i, int f_tiles, const Experts& x
     return it;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __restrict__ xq, const uint8_t* __restrict__ wq,
+template <typename T, bool DIRECT, bool WHOLE>
+__global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restrict__ few_x, int64_t few_ld, const int32_t* n_tokens,
+                                                               const int32_t* __restrict__ few_place, int64_t max_tokens, int top_k,
+                                                               int dim, const uint8_t* __restrict__ xq, const uint8_t* __restrict__ wq,
                                                                const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets,
                                                                int E, int64_t cap_rows, int max_tiles, int col_tiles, int f_tiles,
                                                                int64_t outputs, T* __restrict__ y, int64_t ld, bool lines, int stages,
@@ -443,7 +464,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) {
-            bar_init(&s_full[s], 1);
+            bar_init(&s_full[s], DIRECT ? 1 + 8 : 1);            // (and the warps that put x' rows into 4 bits)
             bar_init(&s_empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -451,6 +472,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
             bar_init(&s_taken[b], 8);
         }
         s_gave_up = 0;
+        if (DIRECT && blockIdx.x == 0) *status = HL_OK;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -485,7 +507,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
                 const Item it = item_of(blockIdx.x, f_tiles, experts, s_first, panel_rows);
                 const uint8_t* a = wq + ((int64_t)it.e * f_tiles + it.f) * col_tiles * kTileBytes;
                 for (; early < min(stages, col_tiles); ++early, a += kTileBytes) {
-                    ask(a, ((it.rows + 15) & ~15) * 128, it.rows > kTileRows ? 2048 : 1024);
+                    ask(a, DIRECT ? 0 : ((it.rows + 15) & ~15) * 128, DIRECT ? 0 : it.rows > kTileRows ? 2048 : 1024);
                     next();
                 }
             }
@@ -496,7 +518,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
                 const Item it = item_of(i, f_tiles, experts, s_first, panel_rows);
                 const uint8_t* a = wq + ((int64_t)it.e * f_tiles + it.f) * col_tiles * kTileBytes;
                 const uint8_t* b = xq + it.tile * col_tiles * kPanelBytes;
-                const uint32_t b_bytes = ((it.rows + 15) & ~15) * 128, e_bytes = it.rows > kTileRows ? 2048 : 1024;
+                const uint32_t b_bytes = DIRECT ? 0 : ((it.rows + 15) & ~15) * 128, e_bytes = DIRECT ? 0 : it.rows > kTileRows ? 2048 : 1024;
                 for (int c = 0; c < col_tiles; ++c, a += kTileBytes, b += kPanelBytes) {
                     if (early > 0) {
                         --early;
@@ -504,9 +526,11 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
                         if (!(ok = bar_wait(&s_empty[stage], phase, &s_gave_up))) break;
                         ask(a, b_bytes, e_bytes);
                     }
-                    const uint32_t at = smem_u32(base + stage * stage_bytes) + kTileBytes;
-                    bulk_load(at, b, b_bytes, &s_full[stage]);
-                    bulk_load(at + panel_bytes, b + kPanelValueBytes, e_bytes, &s_full[stage]);
+                    if (!DIRECT) {
+                        const uint32_t at = smem_u32(base + stage * stage_bytes) + kTileBytes;
+                        bulk_load(at, b, b_bytes, &s_full[stage]);
+                        bulk_load(at + panel_bytes, b + kPanelValueBytes, e_bytes, &s_full[stage]);
+                    }
                     next();
                 }
             }
@@ -553,10 +577,38 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const uint8_t* __
         }
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;    // the lanes of the tensor memory that this warp can read; its columns
-        int buffer = 0;
-        uint32_t phase = 0;
+        int buffer = 0, stage = 0;
+        uint32_t phase = 0, empty = 1;
         for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
             const Item it = item_of(i, f_tiles, experts, s_first, panel_rows);
+            if constexpr (DIRECT) {
+                // x' rows step by step, each row's part by one of the warps in turn.  (As a rule an expert has one row or two here; several
+                // parts of a warp on their way at a time: 10.8 us instead of 8.8 a call of one token, 20 instead of 23 for twelve rows
+                // of one expert.)
+                bool ok = true;
+                for (int c = 0, part = 0; ok && c < col_tiles; ++c) {
+                    ok = bar_wait(&s_empty[stage], empty, &s_gave_up);
+                    for (int r = 0; ok && r < it.rows; ++r, ++part) {
+                        if ((part & 7) != warp - 2) continue;
+                        const int64_t from = row_of(it.row0 + r, few_place, n_tokens, max_tokens, top_k);
+                        Part<T, WHOLE> in;
+                        in.load(from < 0 ? nullptr : few_x + from * few_ld, c * kTileCols + lane * 8, dim);
+                        uint32_t e;
+                        const uint32_t packed = to_four_bits(in, &e);
+                        uint8_t* panel = base + stage * stage_bytes + kTileBytes;
+                        *reinterpret_cast<uint32_t*>(panel + value_at(r, lane)) = packed;
+                        if ((lane & 3) == 0) panel[panel_bytes + exponent_at(r, lane >> 2)] = (uint8_t)e;
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                    __syncwarp();
+                    if (ok && lane == 0) bar_arrive(&s_full[stage]);
+                    if (++stage == stages) {
+                        stage = 0;
+                        empty ^= 1;
+                    }
+                }
+                if (!ok) break;
+            }
             if (!bar_wait(&s_sums[buffer], phase, &s_gave_up)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             __syncwarp();
@@ -615,7 +667,7 @@ constexpr int kSMs = 148;              // grids are made for a B200's multiproce
 int64_t tiles_of(int64_t n, int per) { return div_up(n, per); }
 bool matrix_dims_ok(int64_t rows, int64_t dim) { return rows >= 0 && rows < (int64_t(1) << 31) && dim >= 1 && dim <= (int64_t(1) << 24); }
 
-Divisor divisor(int64_t d) { return {d == 1 ? 0 : ~0ull / (uint64_t)d + 1, d}; }
+uint64_t inverse_of(int64_t d) { return d == 1 ? 0 : ~uint64_t(0) / (uint64_t)d + 1; }
 
 constexpr int64_t kWorkspaceHead = 1024;
 int64_t row_tiles_most(int64_t cap_rows, int64_t E) { return cap_rows / kPanelRows + (E < cap_rows ? E : cap_rows); }
@@ -634,7 +686,7 @@ int32_t launch_quantise(int64_t n, int64_t rows, int64_t dim, const void* x, int
     const int64_t chunks = div_up(ct, U), items = n * rt * kTileRows * chunks, ctas = div_up(items, kRowNT / 32);
     if (ctas > 0x7fffffff || n * rt * kTileRows >= (int64_t(1) << 32)) return HL_EINVAL;
     HL_CUDA_TRY(launch(HL_PARTS(k_mx4_quantise, T), (unsigned)ctas, kRowNT, stream, static_cast<const T*>(x), rows, dim, ld, stride,
-                       divisor(rt * kTileRows), divisor(chunks), ct, items, static_cast<uint8_t*>(q)));
+                       inverse_of(rt * kTileRows), rt * kTileRows, inverse_of(chunks), chunks, ct, items, static_cast<uint8_t*>(q)));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
@@ -647,7 +699,7 @@ int32_t launch_dequantise(int64_t n, int64_t rows, int64_t dim, const void* q, v
     const int64_t chunks = div_up(ct, U), items = n * rows * chunks, ctas = div_up(items, kRowNT / 32);
     if (ctas > 0x7fffffff || n * rows >= (int64_t(1) << 32)) return HL_EINVAL;
     HL_CUDA_TRY(launch(HL_PARTS(k_mx4_dequantise, T), (unsigned)ctas, kRowNT, stream, static_cast<const uint8_t*>(q), rt, dim,
-                       divisor(rows), divisor(chunks), ct, items, static_cast<T*>(out), ld, stride));
+                       inverse_of(rows), rows, inverse_of(chunks), chunks, ct, items, static_cast<T*>(out), ld, stride));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
@@ -658,25 +710,30 @@ int32_t launch_product(const hl_route* r, int64_t dim, int64_t outputs, const vo
     int32_t* status = static_cast<int32_t*>(workspace);
     uint8_t* q = static_cast<uint8_t*>(workspace) + kWorkspaceHead;
     const int64_t ct = tiles_of(dim, kTileCols), ft = tiles_of(outputs, kTileRows), rt = row_tiles_most(r->cap_rows, r->n_experts);
-    const int64_t rows = by_token ? r->max_tokens : r->cap_rows, chunks = div_up(ct, kRowParts);
-    // (up to four times four parts a warp where there are enough rows for four rounds of the chip's warps all the same)
-    int64_t span = rows * chunks / (4 * 32 * kSMs);
-    span = span < 1 ? 1 : span > 4 ? 4 : span;
-    const int64_t per_row = div_up(chunks, span);
-    HL_CUDA_TRY(launch(whole ? k_mx4_rows<T, true> : k_mx4_rows<T, false>, grid_for(rows * per_row, kRowNT / 32, 4 * kSMs), kRowNT, stream,
-                       static_cast<const T*>(x), ld_x, dim, ct, span, divisor(per_row), r->n_tokens, rows, by_token ? r->top_k : 0, r->place, r->counts,
-                       r->offsets, r->n_experts, r->cap_rows, rt, q, status));
-    note_launches(1);
     // (an expert can have all rows that there are)
-    const int64_t all = r->cap_rows < r->max_tokens * r->top_k ? r->cap_rows : r->max_tokens * r->top_k;
-    const int64_t most_rows = by_token ? all : r->cap_rows, panel = most_rows < kPanelRows ? (most_rows + 15) / 16 * 16 : kPanelRows;
+    const int64_t choices = r->max_tokens * r->top_k, most_rows = by_token && choices < r->cap_rows ? choices : r->cap_rows;
+    const bool direct = most_rows <= kFewRows && (!by_token || choices <= kFewRows);
+    if (!direct) {
+        const int64_t rows = by_token ? r->max_tokens : r->cap_rows, chunks = div_up(ct, kRowParts);
+        // (up to four times four parts a warp where there are enough rows for four rounds of the chip's warps all the same)
+        int64_t span = rows * chunks / (4 * 32 * kSMs);
+        span = span < 1 ? 1 : span > 4 ? 4 : span;
+        const int64_t per_row = div_up(chunks, span);
+        HL_CUDA_TRY(launch(whole ? k_mx4_rows<T, true> : k_mx4_rows<T, false>, grid_for(rows * per_row, kRowNT / 32, 4 * kSMs), kRowNT,
+                           stream, static_cast<const T*>(x), ld_x, dim, ct, span, inverse_of(per_row), per_row, r->n_tokens, rows,
+                           by_token ? r->top_k : 0, r->place, r->counts, r->offsets, r->n_experts, r->cap_rows, rt, q, status));
+        note_launches(1);
+    }
+    const int64_t panel = most_rows < kPanelRows ? (most_rows + 15) / 16 * 16 : kPanelRows;
     const int64_t stage = kTileBytes + panel * 128 + (panel > kTileRows ? 2048 : 1024);
     const int64_t stages = kStagesBytes / stage < kMostStages ? kStagesBytes / stage : kMostStages;
-    const auto kernel = k_mx4_product<T>;
+    const auto kernel = !direct ? k_mx4_product<T, false, true> : whole ? k_mx4_product<T, true, true> : k_mx4_product<T, true, false>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProductSmem) != cudaSuccess) return HL_ECUDA;
-    HL_CUDA_TRY(launch_after(kernel, grid_for(rt * ft, 1, kSMs), kProductNT, kProductSmem, stream, (const uint8_t*)q,
-                             static_cast<const uint8_t*>(w), r->counts, r->offsets, r->n_experts, r->cap_rows, rt, ct, ft, outputs,
-                             static_cast<T*>(y), ld_y, outputs * sizeof(T) % 16 == 0 && ld_y * sizeof(T) % 16 == 0 && lies_at(y, 16), stages, panel, status));
+    HL_CUDA_TRY(launch_cluster(kernel, grid_for(rt * ft, 1, kSMs), kProductNT, kProductSmem, direct ? 0 : kAfterLast, stream,
+                               static_cast<const T*>(direct ? x : nullptr), ld_x, r->n_tokens, by_token ? r->place : nullptr,
+                               r->max_tokens, r->top_k, dim, (const uint8_t*)q, static_cast<const uint8_t*>(w), r->counts, r->offsets, r->n_experts, r->cap_rows, rt, ct,
+                               ft, outputs, static_cast<T*>(y), ld_y,
+                               outputs * sizeof(T) % 16 == 0 && ld_y * sizeof(T) % 16 == 0 && lies_at(y, 16), stages, panel, status));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;

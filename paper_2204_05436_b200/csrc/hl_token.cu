@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(kNT) k_token_embed_loose(const TT* __restrict_
 }
 
 // ---- the sort -----------------------------------------------------------------------------------------------------------
-// Few tokens: a token's place is how many are below it, and equal ones in front of it; each is compared with all.  (Some 4 us of one
+// Few tokens: a token's place is how many are below it, and equal ones in front of it; each is compared with all.  (Some 5 us of one
 // kernel for 2 048, where making pairs and sorting them takes two kernels and 15 us, whatever their number.)
 constexpr int kFewTokens = 2048, kFewNT = 128;
 __global__ void __launch_bounds__(kFewNT) k_token_rank(const int32_t* __restrict__ tokens, int max_tokens, const int32_t* n_tokens,
@@ -446,10 +446,11 @@ __global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__
 bool tokens_ok(int64_t max_tokens) { return max_tokens >= 0 && max_tokens < (int64_t(1) << 30); }
 unsigned long long inverse_of(int64_t vectors) { return vectors == 1 ? 0 : ~0ull / vectors + 1; }
 
-// Tokens of a window, a power of two from 16 to 128: so many that the windows' threads, of eight columns, fill the chip once, but not
+// Tokens of a window: up to 32 tokens are one, so that no run is cut.  Else a power of two from 16 to 128: so many that the windows' threads, of eight columns, fill the chip once, but not
 // more than 8 192 windows where 128 tokens each make fewer of them.
 constexpr int64_t kChipThreads = 148 * 2048;
 int window_of(int64_t max_tokens, int64_t dim) {
+    if (max_tokens <= 32) return 32;
     int w = 16;
     while (w < 128 && (max_tokens * div_up(dim, 8) > w * kChipThreads || max_tokens > w * int64_t(8192))) w *= 2;
     return w;
