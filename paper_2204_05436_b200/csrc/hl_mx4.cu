@@ -26,62 +26,62 @@ __device__ __forceinline__ int exponent_at(int row, int block) {
 constexpr int kPanelRows = 240, kPanelValueBytes = kPanelRows * kTileCols / 2, kPanelBytes = kPanelValueBytes + 2048;
 static_assert(kPanelBytes == 32768 && kPanelValueBytes % 1024 == 0, "as above");
 
-// A row's part from column c on, eight values a lane, as they are; zeros behind its end and where there is no row.
+// A row's part from column c on, eight values a lane, as they are; zeros behind its end and where there is no row.  WHOLE: rows begin
+// at multiples of 16 bytes and have a multiple of eight values.
 template <typename T, bool WHOLE>
 struct Part {
-    static constexpr int kWords = 8 * (int)sizeof(T) / 4;
-    uint32_t w[kWords];
+    std::conditional_t<WHOLE, Pack<T, 8>, Loose<T>> v;
+    int there;                         // values of the eight that there are (!WHOLE)
     __device__ __forceinline__ void load(const T* row, int c, int dim) {
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) w[i] = 0;
-        if (!row) return;
+        v.zero();
+        there = row ? dim - c : 0;
+        if (there <= 0) return;
+        if constexpr (WHOLE) v.load(row + c);
+        else v.load(row, c, dim);
+    }
+    __device__ __forceinline__ Pack<T, 8> values() const {
         if constexpr (WHOLE) {
-            if (c >= dim) return;
-            Pack<T, 8> v;
-            v.load(row + c);
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) w[i] = v.w[i];
+            return v;
         } else {
+            Pack<T, 8> p = v.values();
+            if (there < 8) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (c + i >= dim) continue;
-                if constexpr (sizeof(T) == 4) w[i] = __ldg(reinterpret_cast<const uint32_t*>(row + c + i));
-                else w[i / 2] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(row + c + i)) << (16 * (i & 1));
+                for (int i = 0; i < Pack<T, 8>::kWords; ++i) {
+                    if constexpr (sizeof(T) == 4) p.w[i] = i < there ? p.w[i] : 0u;
+                    else p.w[i] &= (2 * i < there ? 0xffffu : 0u) | (2 * i + 1 < there ? 0xffff0000u : 0u);
+                }
             }
+            return p;
         }
     }
-    __device__ __forceinline__ void get(float (&x)[8]) const {
-        Pack<T, 8> v;
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) v.w[i] = w[i];
-        v.get(x);
-    }
-    // the largest absolute value of the lane's block, among its four lanes, as 32-bit float's bits (infinities and NaN: 255 << 23
-    // and more).  Bits without the sign are in the order of the values, NaN largest; those of 16-bit types two at a time.
-    __device__ __forceinline__ uint32_t largest() const {
-        constexpr uint32_t kAbs = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
-        uint32_t top = w[0] & kAbs;
-#pragma unroll
-        for (int i = 1; i < kWords; ++i) top = sizeof(T) == 4 ? max(top, w[i] & kAbs) : __vmaxu2(top, w[i] & kAbs);
-        if constexpr (sizeof(T) == 2) top = max(top >> 16, top & 0xffffu);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        if constexpr (sizeof(T) == 4) return top;
-        else if constexpr (std::is_same_v<T, __nv_bfloat16>) return top << 16;
-        else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)top)));
-    }
 };
+// The largest absolute value of the lane's block, among its four lanes, as a 32-bit float's bits (infinities and NaN: 255 << 23 and
+// more).  Bits without the sign are in the order of the values, NaN largest; those of 16-bit types two at a time.
+template <typename T>
+__device__ __forceinline__ uint32_t largest(const Pack<T, 8>& p) {
+    constexpr uint32_t kAbs = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
+    uint32_t top = p.w[0] & kAbs;
+#pragma unroll
+    for (int i = 1; i < Pack<T, 8>::kWords; ++i) top = sizeof(T) == 4 ? max(top, p.w[i] & kAbs) : __vmaxu2(top, p.w[i] & kAbs);
+    if constexpr (sizeof(T) == 2) top = max(top >> 16, top & 0xffffu);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    if constexpr (sizeof(T) == 4) return top;
+    else if constexpr (std::is_same_v<T, __nv_bfloat16>) return top << 16;
+    else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)top)));
+}
 
 // Eight values of a row's part in 4 bits, and their block's exponent (in all of its lanes): 2^(E - 127) with E two below the
 // largest value's own, so that this one lies in 4 .. 8, of which what is above 6 becomes 6; values are rounded to the nearest of 0, 1/2, 1,
 // 3/2, 2, 3, 4, 6, ties to the one of even mantissa.  A block with an infinity or NaN is NaN (exponent 255).
 template <typename T, bool WHOLE>
 __device__ __forceinline__ uint32_t to_four_bits(const Part<T, WHOLE>& part, uint32_t* exponent) {
-    const int e = (int)(part.largest() >> 23);
+    const Pack<T, 8> p = part.values();
+    const int e = (int)(largest(p) >> 23);
     const uint32_t E = e == 255 ? 255u : (uint32_t)max(e - 2, 0);
     const float up = __uint_as_float((254u - min(E, 253u)) << 23);         // 2^(127 - E)
     float x[8];
-    part.get(x);
+    p.get(x);
     uint32_t packed;
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
         "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
@@ -369,6 +369,10 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, uint32_t parity, volatile 
     *gave_up = 1;
     return false;
 }
+// The same by a whole warp, which goes on together, or gives up together.
+__device__ __forceinline__ bool bar_wait_all(uint64_t* b, uint32_t parity, volatile int* gave_up) {
+    return __all_sync(0xffffffffu, bar_wait(b, parity, gave_up));
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
                  "r"(bytes), "r"(smem_u32(bar))
@@ -548,10 +552,10 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
         for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
             const uint32_t n = __shfl_sync(0xffffffffu, (item_of(i, f_tiles, experts, s_first, panel_rows).rows + 15) & ~15, 0);
             const uint32_t acc = d + buffer * kPanelRows, what0 = multiplication(n, 0), what1 = multiplication(n, 1);
-            if (!(ok = bar_wait(&s_taken[buffer], taken, &s_gave_up))) break;
+            if (!(ok = bar_wait_all(&s_taken[buffer], taken, &s_gave_up))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             for (int c = 0; c < col_tiles; ++c) {
-                if (!(ok = bar_wait(&s_full[stage], phase, &s_gave_up))) break;
+                if (!(ok = bar_wait_all(&s_full[stage], phase, &s_gave_up))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t a = base_low + stage * (stage_bytes >> 4), b = a + (kTileBytes >> 4), eb_at = b + (panel_bytes >> 4);
                 // (copies and products run in the order in which they are issued)
@@ -587,7 +591,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
                 // of one expert.)
                 bool ok = true;
                 for (int c = 0, part = 0; ok && c < col_tiles; ++c) {
-                    ok = bar_wait(&s_empty[stage], empty, &s_gave_up);
+                    ok = bar_wait_all(&s_empty[stage], empty, &s_gave_up);
                     for (int r = 0; ok && r < it.rows; ++r, ++part) {
                         if ((part & 7) != warp - 2) continue;
                         const int64_t from = row_of(it.row0 + r, few_place, n_tokens, max_tokens, top_k);
@@ -609,7 +613,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
                 }
                 if (!ok) break;
             }
-            if (!bar_wait(&s_sums[buffer], phase, &s_gave_up)) break;
+            if (!bar_wait_all(&s_sums[buffer], phase, &s_gave_up)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             __syncwarp();
             const int64_t f = (int64_t)it.f * kTileRows + quarter * 32 + lane;

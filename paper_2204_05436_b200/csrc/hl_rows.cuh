@@ -119,7 +119,8 @@ struct Loose {
             w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
         }
     }
-    __device__ __forceinline__ void get(float (&x)[8]) const {
+    // the eight, as they are
+    __device__ __forceinline__ Pack<T, 8> values() const {
         uint32_t v[kWords];
         const int words = shift * (int)sizeof(T) / 4;            // 0 .. 3
 #pragma unroll
@@ -133,8 +134,9 @@ struct Loose {
         Pack<T, 8> p;
 #pragma unroll
         for (int i = 0; i < Pack<T, 8>::kWords; ++i) p.w[i] = v[i];
-        p.get(x);
+        return p;
     }
+    __device__ __forceinline__ void get(float (&x)[8]) const { values().get(x); }
 };
 
 // v[i] for the columns c + i of a row, those outside [0, dim) left out
