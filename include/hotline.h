@@ -683,7 +683,7 @@ HL_API int32_t hl_token_embed(int32_t table_dtype, int64_t n_rows, int64_t dim, 
                               int32_t out_dtype, void* d_out, int64_t ld_out, int32_t* d_status, void* stream);
 
 /* Bytes of device workspace (256-byte aligned) that hl_token_sort and hl_token_embed_bwd need for at most max_tokens < 2^30
- * tokens and gradients of `dim` values; it holds nothing between calls, and two calls in flight need one each.  0 on invalid
+ * tokens and gradients of `dim` values, at most 2^22 (HL_EINVAL beyond); it holds nothing between calls, and two calls in flight need one each.  0 on invalid
  * arguments. */
 HL_API size_t hl_token_workspace_bytes(int64_t max_tokens, int64_t dim);
 
@@ -739,7 +739,8 @@ HL_API int32_t hl_expert_choose_bwd(const hl_router* router, int32_t dtype, cons
  * floor(log2 of the largest absolute value) - 2, at least -127; its values are rounded to 2^e times the nearest of 0, 1/2, 1,
  * 3/2, 2, 3, 4 and 6 with their sign, ties to the one of even mantissa, larger ones to 6.  A block with an infinity or NaN is NaN.  How such
  * a matrix lies in memory is the library's affair: hl_mx4_bytes bytes, 16-byte aligned, one matrix behind the other.
- * `stride`: values from one matrix's begin to the next.  0 bytes on invalid arguments (and for no rows). */
+ * `stride`: values from one matrix's begin to the next.  All rows together, each matrix' filled up to a multiple of 128: less than
+ * 2^32 (HL_EINVAL beyond).  0 bytes on invalid arguments (and for no rows). */
 HL_API size_t hl_mx4_bytes(int64_t rows, int64_t dim);
 HL_API int32_t hl_mx4_quantise(int32_t dtype, int64_t n_matrices, int64_t rows, int64_t dim, const void* d_x, int64_t ld,
                                int64_t stride, void* d_q, void* stream);
@@ -748,7 +749,7 @@ HL_API int32_t hl_mx4_dequantise(int64_t n_matrices, int64_t rows, int64_t dim, 
 
 /* Bytes of device workspace (256-byte aligned) that hl_expert_mx4 needs.  0 on invalid arguments.  It holds nothing between calls,
  * and two calls in flight need one each; its first int32 is the last call's status: HL_OK, or HL_ETIMEOUT if a wait inside
- * the product gave up. */
+ * the product gave up (what y holds is then of no use). */
 HL_API size_t hl_expert_mx4_workspace_bytes(int64_t cap_rows, int32_t n_experts, int64_t dim);
 
 /* y[r, :] = x[r, :] * W[e]^T for the rows r of every expert e, both in 4 bits as above, products added in fp32, rounded once to

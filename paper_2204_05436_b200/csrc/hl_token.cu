@@ -349,8 +349,8 @@ __global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ 
 
 // Runs over several windows: their pieces.  A warp looks at one window, of which a run may begin there and go on, and adds up the run's
 // pieces in order if it is short; what reaches over more than kShort windows is left to the CTA, whose warps take a part of the
-// pieces each, in order, and add the parts up in order.  32 W columns a CTA.  (A CTA a window, most of which end at once: 24 us
-// instead of ... for 512 windows of 2 048 columns.)
+// pieces each, in order, and add the parts up in order.  32 W columns a CTA.  (A CTA a window, most of which end at once: 30 us
+// instead of 12 for 1 024 windows of 2 048 columns.)
 constexpr int kShort = 16;
 // Pieces p0 .. p1 of the run that begins in window w.  A warp's groups of P lanes, which have all columns, take every so many of them
 // and are added up by halves.
@@ -443,6 +443,7 @@ __global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__
 }
 
 // ---- arguments ------------------------------------------------------------------------------------------------------------
+constexpr int64_t kMostDim = 1 << 22;  // (of a gradient: columns are a grid's second dimension)
 bool tokens_ok(int64_t max_tokens) { return max_tokens >= 0 && max_tokens < (int64_t(1) << 30); }
 unsigned long long inverse_of(int64_t vectors) { return vectors == 1 ? 0 : ~0ull / vectors + 1; }
 
@@ -554,7 +555,7 @@ extern "C" int32_t hl_token_embed(int32_t table_dtype, int64_t n_rows, int64_t d
 }
 
 extern "C" size_t hl_token_workspace_bytes(int64_t max_tokens, int64_t dim) {
-    if (!tokens_ok(max_tokens) || dim < 1 || dim > (int64_t(1) << 24)) return 0;
+    if (!tokens_ok(max_tokens) || dim < 1 || dim > kMostDim) return 0;
     const int64_t sort = (2 * padded(max_tokens) + padded(sort_hist_words(max_tokens))) * 4;
     const int64_t sums = 2 * most_windows(max_tokens, dim) * (div_up(dim, kPieceStep) * kPieceStep) * 4;
     return (size_t)(kWorkspaceHead + ((sort > sums ? sort : sums) + 255) / 256 * 256);
@@ -601,7 +602,8 @@ extern "C" int32_t hl_token_embed_bwd(int64_t n_rows, int64_t dim, const int32_t
                                       int64_t ld_grad, float scale, int32_t table_dtype, void* d_grad_table, int64_t ld_table,
                                       int32_t accumulate, void* d_workspace, size_t ws_bytes, void* stream_) {
     const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if (n_rows < 0 || n_rows >= (int64_t(1) << 31) || !tokens_ok(max_tokens) || (max_tokens > 0 && (!d_sorted || !d_order)) ||
+    if (n_rows < 0 || n_rows >= (int64_t(1) << 31) || dim > kMostDim || !tokens_ok(max_tokens) ||
+        (max_tokens > 0 && (!d_sorted || !d_order)) ||
         !row_matrix_ok(grad_dtype, max_tokens, dim, d_grad_out, ld_grad) ||
         !row_matrix_ok(table_dtype, n_rows, dim, d_grad_table, ld_table) || !lies_at(d_sorted, 4) || !lies_at(d_order, 4) ||
         !lies_at(d_n_tokens, 4) || !d_workspace || !lies_at(d_workspace, 256))

@@ -28,8 +28,8 @@ class TokenEmbedding:
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.max_tokens, self.n_rows, self.dim = int(max_tokens), int(n_rows), int(dim)
-        if not (0 <= self.max_tokens < 2 ** 30 and 0 <= self.n_rows < 2 ** 31 and 1 <= self.dim <= 2 ** 24):
-            raise ValueError("less than 2^30 tokens, less than 2^31 rows, of 1 to 2^24 values")
+        if not (0 <= self.max_tokens < 2 ** 30 and 0 <= self.n_rows < 2 ** 31 and 1 <= self.dim <= 2 ** 22):
+            raise ValueError("less than 2^30 tokens, less than 2^31 rows, of 1 to 2^22 values")
         i32 = dict(dtype=torch.int32, device=self.device)
         self.sorted, self.order = torch.zeros(self.max_tokens, **i32), torch.zeros(self.max_tokens, **i32)
         self._status = torch.zeros(1, **i32)

@@ -268,6 +268,26 @@ def test_plans_from_elsewhere_stay_inside_the_buffers(hl):
             assert (c.wide[c.cap:] == -7).all() and (c.wide[:, c.F:] == -7).all()
 
 
+def test_no_tokens_and_a_plan_of_some(hl):
+    """Tokens' rows of which there are none, whatever counts the plan has."""
+    c = _Case(hl, 3, 2, 4, 64, 32)
+    place, counts, offsets = c.route.place, c.route.counts, c.route.offsets
+    counts.fill_(2)
+    offsets.copy_(torch.arange(5, dtype=torch.int32) * 2)
+    route = hl.make_route(0, None, 2, 4, 1, 6, None, None, counts, offsets)
+    c.wide.fill_(-7.0)
+    c.ws[: c.ws_bytes] = 0xFF
+    hl.hl_expert_mx4(route, hl.HL_BF16, 64, 32, None, 64, True, c.q, c.y, c.wide.stride(0), c.ws, c.ws_bytes, _stream())
+    torch.cuda.synchronize()
+    assert int(c.ws[:4].view(torch.int32)) == hl.HL_OK and (c.wide == -7).all()
+    # some, of which the device says there are none: no row of x is read
+    route = hl.make_route(3, torch.zeros(1, dtype=torch.int32, device="cuda"), 2, 4, 1, 6, place, None, counts, offsets)
+    c.x.fill_(float("nan"))
+    hl.hl_expert_mx4(route, hl.HL_BF16, 64, 32, c.x, c.x.stride(0), True, c.q, c.y, c.wide.stride(0), c.ws, c.ws_bytes, _stream())
+    torch.cuda.synchronize()
+    assert int(c.ws[:4].view(torch.int32)) == hl.HL_OK and (c.wide[6:] == -7).all()
+
+
 def test_class(hl):
     E, F, dim, T, K = 6, 96, 160, 70, 2
     w = torch.randn(E, F, dim, device="cuda").to(BF16)
