@@ -255,15 +255,15 @@ __device__ __forceinline__ int last_not_above(const int* list, int n, int v) {
 
 // Rows in the experts' order (top_k 0), or the tokens', each to all of its experts' rows: read and converted once.  A warp takes `span`
 // times U parts of a row; its lanes find where each of the row's choices lies.
-constexpr int kRowParts = 4;
-template <typename T, bool WHOLE>
-__global__ void __launch_bounds__(kRowNT, 4) k_mx4_rows(const T* __restrict__ x, int64_t ld, int dim, int col_tiles, int span,
+template <int U>
+constexpr int kRowCtas = U == 8 ? 3 : U == 4 ? 4 : 6;            // CTAs of a multiprocessor
+template <typename T, bool WHOLE, int U>
+__global__ void __launch_bounds__(kRowNT, kRowCtas<U>) k_mx4_rows(const T* __restrict__ x, int64_t ld, int dim, int col_tiles, int span,
                                                         uint64_t items_inverse, int64_t items_d, const int32_t* n_tokens, int64_t max_rows, int top_k,
                                                         const int32_t* __restrict__ place, const int32_t* __restrict__ counts,
                                                         const int32_t* __restrict__ offsets, int E, int64_t cap_rows, int max_tiles,
                                                         uint8_t* __restrict__ q, int32_t* status) {
     __shared__ int s_first[HL_MAX_EXPERTS + 1], s_begin[HL_MAX_EXPERTS];
-    constexpr int U = kRowParts;
     const Divisor items_of{items_inverse, items_d};
     let_next_start();
     if (blockIdx.x == 0 && threadIdx.x == 0) *status = HL_OK;
@@ -718,13 +718,17 @@ int32_t launch_product(const hl_route* r, int64_t dim, int64_t outputs, const vo
     const int64_t choices = r->max_tokens * r->top_k, most_rows = by_token && choices < r->cap_rows ? choices : r->cap_rows;
     const bool direct = most_rows <= kFewRows && (!by_token || choices <= kFewRows);
     if (!direct) {
-        const int64_t rows = by_token ? r->max_tokens : r->cap_rows, chunks = div_up(ct, kRowParts);
-        // (up to four times four parts a warp where there are enough rows for four rounds of the chip's warps all the same)
-        int64_t span = rows * chunks / (4 * 32 * kSMs);
-        span = span < 1 ? 1 : span > 4 ? 4 : span;
-        const int64_t per_row = div_up(chunks, span);
-        HL_CUDA_TRY(launch(whole ? k_mx4_rows<T, true> : k_mx4_rows<T, false>, grid_for(rows * per_row, kRowNT / 32, 4 * kSMs), kRowNT,
-                           stream, static_cast<const T*>(x), ld_x, dim, ct, span, inverse_of(per_row), per_row, r->n_tokens, rows,
+        // Parts of a row that a warp has on their way at a time: as many as there are, up to four, or eight where there are enough rows
+        // for the chip's warps all the same; twice that one after the other where that leaves them eight rounds.
+        const int64_t rows = by_token ? r->max_tokens : r->cap_rows;
+        const int U = ct <= 2 ? (int)ct : ct >= 7 && rows * div_up(ct, 8) >= 8 * kRowCtas<8> * kSMs ? 8 : 4;
+        const int ctas = U == 8 ? kRowCtas<8> : U == 4 ? kRowCtas<4> : kRowCtas<1>;
+        const int64_t chunks = div_up(ct, U), span = U == 8 && rows * chunks >= 8 * 8 * ctas * kSMs ? 2 : 1, per_row = div_up(chunks, span);
+#define HL_ROWS(U) (whole ? k_mx4_rows<T, true, U> : k_mx4_rows<T, false, U>)
+        const auto convert = U == 8 ? HL_ROWS(8) : U == 4 ? HL_ROWS(4) : U == 2 ? HL_ROWS(2) : HL_ROWS(1);
+#undef HL_ROWS
+        HL_CUDA_TRY(launch(convert, grid_for(rows * per_row, kRowNT / 32, ctas * kSMs), kRowNT, stream,
+                           static_cast<const T*>(x), ld_x, dim, ct, span, inverse_of(per_row), per_row, r->n_tokens, rows,
                            by_token ? r->top_k : 0, r->place, r->counts, r->offsets, r->n_experts, r->cap_rows, rt, q, status));
         note_launches(1);
     }
