@@ -9,8 +9,8 @@ namespace {
 // ---- who is chosen ----------------------------------------------------------------------------------------------------
 // A token has P lanes of a warp (1 to 32), each of which holds ITEMS of its experts side by side.  Without a bias an expert's key is
 // its logit, which orders as the score does.  With one it is score + bias, and the definition is in 64 bits; what decides is
-// computed in 32, and a token for which 32 bits cannot tell is done again in 64: with sigmoids two or three in a thousand of 256 experts
-// whose logits are random.
+// computed in 32, and a token for which 32 bits cannot tell is done again in 64: one or two in a thousand of 256 experts whose
+// logits are random.
 template <int ITEMS, int P>
 struct Shape {
     static constexpr int kNT = 128, kCtas = ITEMS == 8 ? 8 : ITEMS == 16 ? 5 : 1;       // threads; CTAs of a multiprocessor
@@ -19,12 +19,14 @@ struct Shape {
     static constexpr int kChosen = kExperts < HL_MAX_TOP_K ? kExperts : HL_MAX_TOP_K;
 };
 
-// How far scores of 32 bits may be off.  A sigmoid s: s (1 - s) times the relative error of the exponential (2^-22 of the instruction's,
-// and its argument's roundings, |x| 2^-22; s (1 - s) |x| < 1/4), the sum's rounding and the inverse's 2^-23: less than 2^-21 in
-// all.  A softmax: the same with e^-|x| (1 + |x|) 2^-22 < 2^-21, and the sum of up to 32 + 5 terms one after the other, 37 * 2^-24 of
-// it, and the inverse: less than 2^-18.  Adding the bias rounds by 2^-24 of the key.  So keys further apart than this times 1 +
-// |key| are in order, and sums of two than twice that.
-constexpr float kSureSigmoid = 0x1p-19f, kSureSoftmax = 0x1p-17f;
+// How far scores of 32 bits may be off, in steps of 2^-24.  A sigmoid s: s (1 - s) times the relative error of the exponential -- 4 of
+// the instruction's, and its argument's roundings, 1.5 |x|, where s (1 - s) |x| < 0.23 --, 1 for the sum and 2 for the inverse:
+// less than 4.5.  A softmax: s times the exponential's 4 + 2 |x|, where s |x| < 0.37, the same of the sum's terms on average
+// (less than 4 + 14), up to 32 + 5 roundings of the sum and 2 of the inverse: less than 61 s + 1, and s is at most 1 / z, z the sum of
+// e^(x - largest).  Adding the bias rounds by 1 of the key.  So keys further apart than twice that, times 1 + |key| with room for the
+// rounding, are in order, and sums of two than four times.
+constexpr float kSureSigmoid = 0x1p-20f;
+__device__ __forceinline__ float sure_of_softmax(float z) { return 0x1p-23f * (64.f / z + 2.f); }
 
 // numbers in the order of the floats (which have no NaN among them; -0 is 0)
 __device__ __forceinline__ uint32_t ordered(float v) {
@@ -93,7 +95,7 @@ __device__ __forceinline__ float near_sigmoid(float l) { return near_inverse(1.f
 struct Router {
     int top_k, E, G, per_group, top_groups;
     uint32_t group_magic;              // 2^21 / per_group, rounded up: exact for numbers and sizes of at most 1 024
-    float sure;                        // kSure...
+    float sure;                        // how far keys have to be apart (in 32 bits)
     bool softmax, pair, renorm;
     __device__ __forceinline__ int group_of(int e) const { return (int)(((uint32_t)e * group_magic) >> 21); }
 };
@@ -217,27 +219,49 @@ __device__ __forceinline__ bool choose(int top_k, Key (&key)[ITEMS], int q, bool
     return clear;
 }
 
-// The same, all at once, for top_k < P: what is not below the (top_k + 1)-th largest of the lanes' largest keys is all that counts.
-// Those few, a lane each, are ranked by comparing each with all.  Returns false, with nothing done, if there are more than P of
-// them (equal keys, or few lanes with any).
+// v over a token's lanes, in descending order
+template <int P>
+__device__ __forceinline__ float in_descending_order(float v, int q) {
+#pragma unroll
+    for (int size = 2; size <= P; size *= 2)
+#pragma unroll
+        for (int d = size / 2; d > 0; d /= 2) {
+            const float other = __shfl_xor_sync(kAll, v, d);
+            const bool upper = ((q & d) != 0) != ((q & size) != 0 && size < P);
+            v = upper ? fminf(v, other) : fmaxf(v, other);
+        }
+    return v;
+}
+
+// The same, all at once, for top_k < P: top_k + 1 keys are known that are among the largest of eight side by side, and what is below the
+// least of them does not count.  Those few that do, a lane each, are ranked by comparing each with all.  Returns false, with nothing
+// done, if there are more than P of them (equal keys, or few lanes with any).
 template <int ITEMS, int P, typename Same>
 __device__ __forceinline__ bool choose_few(int top_k, const float (&key)[ITEMS], int q, bool check, float sure, int32_t* s_e, float2* s_few,
                                            bool* clear, Same same) {
     const float none = -INFINITY;
     const int lane = threadIdx.x & 31, first = lane & ~(P - 1);
-    float best = key[0];
+    float least;
+    if constexpr (ITEMS == 16) {
+        // of a lane's two largest of eight, the larger ones h and the smaller ones l of all lanes, each in order: i of l's first and
+        // top_k + 1 - i of h's first are top_k + 1 keys, whatever i is
+        float a = key[0], b = key[8];
 #pragma unroll
-    for (int j = 1; j < ITEMS; ++j) best = fmaxf(best, key[j]);
-    // the lanes' largest, in descending order
-#pragma unroll
-    for (int size = 2; size <= P; size *= 2)
-#pragma unroll
-        for (int d = size / 2; d > 0; d /= 2) {
-            const float other = __shfl_xor_sync(kAll, best, d);
-            const bool upper = ((q & d) != 0) != ((q & size) != 0 && size < P);
-            best = upper ? fminf(best, other) : fmaxf(best, other);
+        for (int j = 1; j < 8; ++j) {
+            a = fmaxf(a, key[j]);
+            b = fmaxf(b, key[8 + j]);
         }
-    const float least = fmaxf(__shfl_sync(kAll, best, first + top_k), -3.402823466e38f);      // (not those that cannot be chosen)
+        const float h = in_descending_order<P>(fmaxf(a, b), q), l = in_descending_order<P>(fminf(a, b), q);
+        const float other = __shfl_sync(kAll, h, first + max(top_k - 1 - q, 0));
+        least = max_of<P>(q < top_k ? fminf(l, other) : q == top_k ? h : none);
+    } else {
+        float best = key[0];
+#pragma unroll
+        for (int j = 1; j < ITEMS; ++j) best = fmaxf(best, key[j]);
+        best = in_descending_order<P>(best, q);
+        least = __shfl_sync(kAll, best, first + top_k);
+    }
+    least = fmaxf(least, -3.402823466e38f);                      // (not those that cannot be chosen)
     int mine = 0;
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) mine += key[j] >= least;
@@ -291,7 +315,7 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
     __shared__ int32_t s_chosen[S::kTokens][S::kChosen];
     __shared__ float2 s_few[P >= 16 ? S::kNT : 1];
     extern __shared__ double s_base[];                           // with groups that are not whole lanes', of every token: [E + 2 G]
-    const Router r{top_k, E, G, per_group, top_groups, group_magic, flags & kSoftmax ? kSureSoftmax : kSureSigmoid, (flags & kSoftmax) != 0, (flags & kPair) != 0, (flags & kRenorm) != 0};
+    Router r{top_k, E, G, per_group, top_groups, group_magic, kSureSigmoid, (flags & kSoftmax) != 0, (flags & kPair) != 0, (flags & kRenorm) != 0};
     const bool whole_lanes = flags & kWholeLanes;
     const int q = threadIdx.x % P, mine = threadIdx.x / P;
     int64_t tokens = max_tokens;
@@ -356,6 +380,7 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j) z += value[j];
         z = sum_of<P>(z);
+        r.sure = sure_of_softmax(z);
     }
     bool clear = true;
     {
@@ -617,19 +642,20 @@ int flags_of(const hl_router* r) {
     return (r->score == HL_SCORE_SOFTMAX ? kSoftmax : 0) | (r->group_score == HL_GROUP_TOP2 ? kPair : 0) | (r->renorm ? kRenorm : 0);
 }
 
-// As few lanes a token as hold its experts, eight a lane; above 256 experts more.
+// As few lanes a token as hold its experts, eight a lane, above 128 experts sixteen (two tokens of 256 experts a warp, for which most steps
+// take the time of one: 69 us instead of 82 for 65 536), above 512 more.
 #define HL_SHAPES(E, RUN, WHOLE)                                                                                        \
     ((E) <= 8     ? RUN(8, 1, WHOLE)                                                                                    \
      : (E) <= 16  ? RUN(8, 2, WHOLE)                                                                                    \
      : (E) <= 32  ? RUN(8, 4, WHOLE)                                                                                    \
      : (E) <= 64  ? RUN(8, 8, WHOLE)                                                                                    \
      : (E) <= 128 ? RUN(8, 16, WHOLE)                                                                                   \
-     : (E) <= 256 ? RUN(8, 32, WHOLE)                                                                                   \
+     : (E) <= 256 ? RUN(16, 16, WHOLE)                                                                                  \
      : (E) <= 512 ? RUN(16, 32, WHOLE)                                                                                  \
                   : RUN(32, 32, WHOLE))
 // whether a group is the experts of 1, 2, 4 ... of these lanes
 bool whole_lanes(const hl_router* r) {
-    const int items = r->n_experts <= 256 ? 8 : r->n_experts <= 512 ? 16 : 32, per = r->n_experts / r->n_groups, lanes = per / items;
+    const int items = r->n_experts <= 128 ? 8 : r->n_experts <= 512 ? 16 : 32, per = r->n_experts / r->n_groups, lanes = per / items;
     return per % items == 0 && (lanes & (lanes - 1)) == 0;
 }
 
