@@ -150,15 +150,16 @@ __device__ __forceinline__ void store_some(T* row, int c, int dim, const Pack<T,
         else *reinterpret_cast<unsigned short*>(p + i) = (unsigned short)(v.w[i / 2] >> (16 * (i & 1)));
     }
 }
-// zeros in a row that begins anywhere, by a whole warp: whole lines, and what lies before and behind them
+// zeros in a row that begins anywhere, by `threads` threads (at least 8): whole lines, and what lies before and behind them
 template <typename T>
-__device__ __forceinline__ void zero_row(T* row, int dim) {
+__device__ __forceinline__ void zero_row(T* row, int dim, int thread, int threads) {
     constexpr int N = 16 / (int)sizeof(T);
-    const int lane = threadIdx.x & 31, before = min((int)(-(reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (N - 1)), dim);
+    const int before = min((int)(-(reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (N - 1)), dim);
     const int lines = (dim - before) / N, behind = before + lines * N;
-    if (lane < before) row[lane] = from_float<T>(0.f);
-    for (int i = lane; i < lines; i += 32) reinterpret_cast<uint4*>(row + before)[i] = make_uint4(0, 0, 0, 0);
-    if (behind + lane < dim) row[behind + lane] = from_float<T>(0.f);
+    if (thread < before) row[thread] = from_float<T>(0.f);
+    uint4* line = reinterpret_cast<uint4*>(row + before);
+    for (int i = thread; i < lines; i += threads) line[i] = make_uint4(0, 0, 0, 0);
+    if (behind + thread < dim) row[behind + thread] = from_float<T>(0.f);
 }
 
 // ---- arguments: types, and matrices of rows -------------------------------------------------------------------------------

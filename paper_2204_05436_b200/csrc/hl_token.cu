@@ -212,15 +212,12 @@ __device__ __forceinline__ int64_t not_below_by_warp(const int32_t* __restrict__
 }
 
 // rows [first, last) that no token names become zeros
-template <typename TT, int W, bool LOOSE>
+template <typename TT>
 __device__ void zero_rows(const int32_t* __restrict__ sorted, int64_t n, int64_t first, int64_t last, int dim, TT* __restrict__ table,
                           int64_t ld) {
     __shared__ uint32_t s_there[kNT / 32];
     __shared__ int64_t s_range[2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    Pack<TT, W> zero;
-    zero.zero();
-    const int vectors = dim / W;
     for (int64_t r0 = first; r0 < last; r0 += kNT) {
         const int64_t r1 = min(r0 + kNT, last);
         if (warp < 2) {
@@ -243,19 +240,13 @@ __device__ void zero_rows(const int32_t* __restrict__ sorted, int64_t n, int64_t
             atomicOr(&s_there[(r1 - 1 - r0) >> 5], 1u << ((r1 - 1 - r0) & 31));
         __syncthreads();
         const int rows = (int)(r1 - r0);
-        if (LOOSE) {
-            for (int k = warp; k < rows; k += kNT / 32)
-                if (!((s_there[k >> 5] >> (k & 31)) & 1u)) zero_row(table + (r0 + k) * ld, dim);
-        } else if (vectors >= kNT / 2) {
-            for (int k = 0; k < rows; ++k) {
-                if ((s_there[k >> 5] >> (k & 31)) & 1u) continue;
-                for (int c = threadIdx.x; c < vectors; c += kNT) zero.store(table + (r0 + k) * ld + (int64_t)c * W);
-            }
+        if (dim * (int)sizeof(TT) >= 8192) {                     // (a row that gives the whole CTA something to do)
+            for (int k = 0; k < rows; ++k)
+                if (!((s_there[k >> 5] >> (k & 31)) & 1u)) zero_row(table + (r0 + k) * ld, dim, threadIdx.x, kNT);
         } else {
-            for (int k = warp; k < rows; k += kNT / 32) {
-                if ((s_there[k >> 5] >> (k & 31)) & 1u) continue;
-                for (int c = lane; c < vectors; c += 32) zero.store(table + (r0 + k) * ld + (int64_t)c * W);
-            }
+            const int L = dim * (int)sizeof(TT) <= 512 ? 8 : 32;                     // (lanes of a short row)
+            for (int k = threadIdx.x / L; k < rows; k += kNT / L)
+                if (!((s_there[k >> 5] >> (k & 31)) & 1u)) zero_row(table + (r0 + k) * ld, dim, threadIdx.x % L, L);
         }
         __syncthreads();
     }
@@ -273,11 +264,11 @@ struct Values {
 };
 
 template <typename TG, typename TT, int W, int U, bool LOOSE>
-__global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ sorted, const int32_t* __restrict__ order,
+__global__ void __launch_bounds__(kNT, LOOSE ? 3 : 2) k_token_sums(const int32_t* __restrict__ sorted, const int32_t* __restrict__ order,
                                                     int64_t max_tokens, const int32_t* n_tokens, int n_rows, int dim,
                                                     const TG* __restrict__ grad, int64_t ld_grad, float scale,
                                                     TT* __restrict__ table, int64_t ld_table, int accumulate, int window, int P,
-                                                    int sum_ctas, int rows_per_cta, float* __restrict__ pieces) {
+                                                    int passes, int sum_ctas, int rows_per_cta, float* __restrict__ pieces) {
     static_assert(!LOOSE || W == 8, "eight columns a lane");
     __shared__ __align__(16) float s_put[LOOSE ? kNT * W : 4];
     let_next_start();
@@ -286,16 +277,16 @@ __global__ void __launch_bounds__(kNT) k_token_sums(const int32_t* __restrict__ 
     const unsigned zeros = gridDim.x - sum_ctas;
     const unsigned zeros_before = zeros ? (unsigned)((unsigned long long)blockIdx.x * zeros / gridDim.x) : 0;
     if (zeros && (unsigned)((unsigned long long)(blockIdx.x + 1) * zeros / gridDim.x) > zeros_before) {
-        if (blockIdx.y) return;
         const int64_t first = (int64_t)zeros_before * rows_per_cta;
-        zero_rows<TT, W, LOOSE>(sorted, n, first, min(first + rows_per_cta, (int64_t)n_rows), dim, table, ld_table);
+        zero_rows<TT>(sorted, n, first, min(first + rows_per_cta, (int64_t)n_rows), dim, table, ld_table);
         return;
     }
     const int sub = threadIdx.x & (P - 1);
-    const int64_t w = (int64_t)(blockIdx.x - zeros_before) * (kNT / P) + threadIdx.x / P, first = w * window;
+    const unsigned mine = blockIdx.x - zeros_before, group = mine / (unsigned)passes;       // (all columns of some windows, one pass after the other)
+    const int64_t w = (int64_t)group * (kNT / P) + threadIdx.x / P, first = w * window;
     if (first >= n) return;
     const int begin = (int)first, end = (int)min(first + window, n);       // (there are less than 2^30 tokens)
-    const int c = ((int)blockIdx.y * P + sub) * W;
+    const int c = ((int)(mine - group * passes) * P + sub) * W;
     if (c >= dim && !(LOOSE && P == 32)) return;                 // (a warp that writes together stays together)
     float* s = LOOSE && P == 32 ? s_put + (threadIdx.x & ~31) * W : nullptr;
     float sum[W] = {};
@@ -508,16 +499,16 @@ int32_t launch_sums(int64_t n_rows, int64_t dim, const int32_t* sorted, const in
     int P = 1;
     while (P < (LOOSE ? 32 : kNT) && P * W < dim) P *= 2;
     const int window = window_of(max_tokens, dim);
-    const int64_t windows = div_up(max_tokens, window), sums = div_up(windows, kNT / P);
-    // rows without tokens: some 128 KB a CTA
-    int64_t per = (128 << 10) / (dim * (int64_t)sizeof(TT));
-    per = per < 1 ? 1 : per > kNT ? kNT : per;
+    const int64_t windows = div_up(max_tokens, window), passes = div_up(dim, P * W), sums = div_up(windows, kNT / P) * passes;
+    // rows without tokens: some 128 KB a CTA, as many for each of its warps
+    int64_t per = (128 << 10) / (dim * (int64_t)sizeof(TT)) / (kNT / 32) * (kNT / 32);
+    per = per < kNT / 32 ? kNT / 32 : per > kNT ? kNT : per;
     const int64_t zeros = accumulate ? 0 : div_up(n_rows, per);
     if (sums + zeros > 0x7fffffff || div_up(dim, 32 * W) > 65535 || windows > 0x7fffffff) return HL_EINVAL;
     if (sums + zeros == 0) return HL_OK;
-    HL_CUDA_TRY(launch(k_token_sums<TG, TT, W, U, LOOSE>, dim3((unsigned)(sums + zeros), (unsigned)div_up(dim, P * W)), kNT, stream,
-                       sorted, order, max_tokens, n_tokens, (int)n_rows, (int)dim, static_cast<const TG*>(grad), ld_grad, scale,
-                       static_cast<TT*>(table), ld_table, accumulate, window, P, (int)sums, (int)per, pieces));
+    HL_CUDA_TRY(launch(k_token_sums<TG, TT, W, U, LOOSE>, (unsigned)(sums + zeros), kNT, stream, sorted, order, max_tokens, n_tokens,
+                       (int)n_rows, (int)dim, static_cast<const TG*>(grad), ld_grad, scale, static_cast<TT*>(table), ld_table, accumulate,
+                       window, P, (int)passes, (int)sums, (int)per, pieces));
     note_launches(1);
     if (windows > 1) {
         const int Q = P < 32 ? P : 32;
@@ -591,7 +582,7 @@ extern "C" int32_t hl_token_sort(const int32_t* d_tokens, int64_t max_tokens, co
     // (a sort that counts no digits, in one cluster, has none to clear either)
     const int64_t clear = sort_clear_words(max_tokens, bits, WaitCfg());
     if (clear) HL_CUDA_TRY(clear_words(ws.hist, clear, stream));
-    HL_CUDA_TRY(launch(k_token_pairs, grid_for(max_tokens, kNT * (clear ? 8 : 1), 2048), kNT, stream, d_tokens, max_tokens, d_n_tokens,
+    HL_CUDA_TRY(launch(k_token_pairs, grid_for(max_tokens, kNT * (clear ? 2 : 1), 1024), kNT, stream, d_tokens, max_tokens, d_n_tokens,
                        (int)n_rows, keys[0], vals[0], ws.n, clear ? (bits + 7) / 8 : 0, ws.hist, status));
     note_launches(1);
     return radix_sort_pairs(keys, vals, ws.n, max_tokens, bits, ws.hist, status, &sorted, &order, stream, WaitCfg(), clear != 0);
