@@ -13,7 +13,8 @@ __device__ __forceinline__ int64_t live_tokens(const int32_t* n_tokens, int64_t 
 }
 
 // ---- rows of tokens ---------------------------------------------------------------------------------------------------
-// out[i] = scale * table[tokens[i]], W values at a time, U of them a thread, dealt out in turn over the rows.  Bound by memory.
+// out[i] = scale * table[tokens[i]], W values at a time, U of them a thread, dealt out in turn over the rows.  Bound by memory: 16 384 rows
+// of 2 048 bf16 17 us (67 MB written), 131 072 of 512 fp32 to bf16 34.6 (134 MB written, 70 read: 5.9 TB/s).
 // (item / vectors: by 2^64 / vectors, rounded up; exact for less than 2^40 items and rows of less than 2^24 vectors)
 template <typename TT, typename TO, int W, int U>
 __global__ void __launch_bounds__(kNT) k_token_embed(const TT* __restrict__ table, int64_t ld_table, unsigned n_rows,
@@ -52,7 +53,8 @@ __global__ void __launch_bounds__(kNT) k_token_embed(const TT* __restrict__ tabl
 }
 
 // The same for rows that begin anywhere: eight values a thread, from where the written row's 16-byte lines begin, so that all but
-// those at its ends are written whole.
+// those at its ends are written whole.  28 657 rows of 337 fp16, 339 apart: 11 us, 22 MB; two of three cycles issue an instruction (a value
+// a thread: 23).
 template <typename TT, typename TO>
 __global__ void __launch_bounds__(kNT) k_token_embed_loose(const TT* __restrict__ table, int64_t ld_table, unsigned n_rows,
                                                            const int32_t* __restrict__ tokens, int64_t max_tokens,
@@ -146,7 +148,9 @@ __global__ void __launch_bounds__(kNT) k_token_pairs(const int32_t* __restrict__
 // gradients of each run of equal tokens.  A run inside the window goes to its row; of one that begins before the window or goes on
 // behind it only a piece is known, which goes to memory: piece 2w is that of the run which began before window w, 2w + 1 that of the
 // one that begins in it and goes on.  A second kernel adds the pieces of such a run up, in their order.  Rows without tokens are
-// zeroed by CTAs of their own.  LOOSE: rows that begin anywhere; a group is a warp at most then, eight columns a lane.
+// zeroed by CTAs of their own.  Bound by memory: 16 384 gradients of 2 048 bf16, summed into 32 000 rows of fp32, 58 us (67 MB in, 262 out:
+// 5.7 TB/s) and 12 for the joined ones; 131 072 of 512 into 200 000 rows 95 (544 MB) and 19.  28 657 of 337 fp16, 339 apart: 20, where
+// instructions and the latency of order, then row, are what bounds it, and 16.  LOOSE: rows that begin anywhere; a group is a warp at most then, eight columns a lane.
 constexpr int kPieceStep = 8;          // a piece's columns are filled up to a multiple of this
 __device__ __forceinline__ int64_t piece_pitch(int dim) { return (dim + kPieceStep - 1) / kPieceStep * kPieceStep; }
 
