@@ -356,19 +356,22 @@ __device__ __forceinline__ void add_pieces(const float* __restrict__ pieces, int
     const int groups = 32 / P;
     const float* column = pieces + (c < dim ? c : 0);
     for (int p = p0 + (threadIdx.x & 31) / P; p < p1; p += U * groups) {
-        Pack<float, W> in[U];          // (asked for without a condition, so that all are on their way before the first is added)
+        float in[U][W];                // (asked for without a condition and in this order, so that all are on their way before one is added)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = min(p + u * groups, p1 - 1);
-            in[u].load(column + (2 * (w + at) + (at == 0 ? 1 : 0)) * pitch);
+            const float* from = column + (2 * (w + at) + (at == 0 ? 1 : 0)) * pitch;
+#pragma unroll
+            for (int i = 0; i < W; i += 4)
+                asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(in[u][i]), "=f"(in[u][i + 1]), "=f"(in[u][i + 2]), "=f"(in[u][i + 3])
+                             : "l"(from + i)
+                             : "memory");
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float x[W];
-            in[u].get(x);
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < W; ++i) sum[i] += p + u * groups < p1 ? x[i] : 0.f;
-        }
+            for (int i = 0; i < W; ++i) sum[i] += p + u * groups < p1 ? in[u][i] : 0.f;
     }
     __syncwarp();
     for (int d = P; d < 32; d *= 2)
@@ -377,7 +380,7 @@ __device__ __forceinline__ void add_pieces(const float* __restrict__ pieces, int
 }
 
 template <typename TT, int W, bool LOOSE>
-__global__ void __launch_bounds__(kNT) k_token_joins(const int32_t* __restrict__ sorted, int64_t max_tokens, const int32_t* n_tokens,
+__global__ void __launch_bounds__(kNT, 2) k_token_joins(const int32_t* __restrict__ sorted, int64_t max_tokens, const int32_t* n_tokens,
                                                      int n_rows, int dim, float scale, TT* __restrict__ table, int64_t ld_table,
                                                      int accumulate, int window, int P, const float* __restrict__ pieces) {
     constexpr int kWarps = kNT / 32;
