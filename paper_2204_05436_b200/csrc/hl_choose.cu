@@ -7,7 +7,8 @@ namespace hl {
 namespace {
 
 // ---- who is chosen ----------------------------------------------------------------------------------------------------
-// A token has P lanes of a warp (1 to 32), each of which holds ITEMS of its experts side by side.  Without a bias an expert's key is
+// A token has P lanes of a warp (1 to 32), each of which holds up to ITEMS of its experts side by side: `per_lane`, so that a group is
+// that of whole lanes if that can be.  Without a bias an expert's key is
 // its logit, which orders as the score does.  With one it is score + bias, and the definition is in 64 bits; what decides is
 // computed in 32, and a token for which 32 bits cannot tell is done again in 64: one or two in a thousand of 256 experts whose
 // logits are random.
@@ -93,13 +94,14 @@ __device__ __forceinline__ float near_sigmoid(float l) { return near_inverse(1.f
 
 // what a call goes by
 struct Router {
-    int top_k, E, G, per_group, top_groups;
+    int top_k, E, G, per_group, top_groups, per_lane;
+    int group_lanes;                   // lanes of a group; 0: groups are not of whole lanes
     uint32_t group_magic;              // 2^21 / per_group, rounded up: exact for numbers and sizes of at most 1 024
     float sure;                        // how far keys have to be apart (in 32 bits)
     bool softmax, pair, renorm;
     __device__ __forceinline__ int group_of(int e) const { return (int)(((uint32_t)e * group_magic) >> 21); }
 };
-enum { kSoftmax = 1, kPair = 2, kRenorm = 4, kWholeLanes = 8 };
+enum { kSoftmax = 1, kPair = 2, kRenorm = 4 };
 
 template <typename Key>
 __device__ __forceinline__ void two_best(Key v, Key& best, Key& second) {
@@ -113,19 +115,22 @@ __device__ __forceinline__ void two_best(Key v, Key& best, Key& second) {
 }
 
 // Keys of experts outside the groups that are kept become -inf.  `value` is what the groups are compared by, which is -inf for
-// experts that cannot be chosen.  Returns whether it was clear which.  whole_lanes: a group is that of 1, 2, 4 ... lanes, which then
-// find its two best between them; other groups go through shared memory (s: [E + 2 G]).
+// experts that cannot be chosen.  Returns whether it was clear which.  Groups of whole lanes find their two best between those;
+// others go through shared memory (s: [E + 2 G]).
 template <int ITEMS, int P, typename Key>
-__device__ bool keep_groups(const Router& r, bool whole_lanes, const Key (&value)[ITEMS], Key (&key)[ITEMS], int q, Key* s) {
+__device__ bool keep_groups(const Router& r, const Key (&value)[ITEMS], Key (&key)[ITEMS], int q, Key* s) {
     const Key none = -(Key)INFINITY;
     Key in = none, out = none;
-    if (whole_lanes) {
-        const int lanes = r.per_group / ITEMS, lane = threadIdx.x & 31, first = lane & ~(P - 1), mine = q / lanes;
+    if (r.group_lanes) {
+        const int lanes = r.group_lanes, lane = threadIdx.x & 31, first = lane & ~(P - 1), mine = q / lanes;
         Key best = none, second = none;
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j) two_best(value[j], best, second);
-        for (int d = 1; d < lanes; d *= 2) {
-            const Key b = __shfl_xor_sync(kAll, best, d), c = __shfl_xor_sync(kAll, second, d);
+        const Key my_best = best, my_second = second;
+        const int from = first + min(mine, r.G - 1) * lanes;
+        for (int d = 1, at = q - mine * lanes; d < lanes; ++d) {         // (the group's other lanes, one after the other)
+            at = at + 1 < lanes ? at + 1 : 0;
+            const Key b = __shfl_sync(kAll, my_best, from + at), c = __shfl_sync(kAll, my_second, from + at);
             two_best(b, best, second);
             second = c > second ? c : second;
         }
@@ -150,7 +155,7 @@ __device__ bool keep_groups(const Router& r, bool whole_lanes, const Key (&value
         Key *s_group = s + r.E, *s_ranked = s_group + r.G;
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j)
-            if (q * ITEMS + j < r.E) s[q * ITEMS + j] = value[j];
+            if (j < r.per_lane && q * r.per_lane + j < r.E) s[q * r.per_lane + j] = value[j];
         __syncwarp();
         for (int g = q; g < r.G; g += P) {
             Key best = none, second = none;
@@ -173,7 +178,7 @@ __device__ bool keep_groups(const Router& r, bool whole_lanes, const Key (&value
         __syncwarp();
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j)
-            if (q * ITEMS + j < r.E && s[r.group_of(q * ITEMS + j)] == (Key)0) key[j] = none;
+            if (j < r.per_lane && q * r.per_lane + j < r.E && s[r.group_of(q * r.per_lane + j)] == (Key)0) key[j] = none;
         if (r.top_groups < r.G) {
             in = s_ranked[r.top_groups - 1];
             out = s_ranked[r.top_groups];
@@ -191,7 +196,7 @@ __device__ __forceinline__ bool surely(Key a, Key b, float sure) { return a - b 
 // lanes; a tie goes to the lowest number.  Where `check`, returns whether their order was clear; same(a, b): two experts whose
 // keys are equal by definition.
 template <int ITEMS, int P, typename Key, typename Same>
-__device__ __forceinline__ bool choose(int top_k, Key (&key)[ITEMS], int q, bool check, float sure, int32_t* s_e, Same same) {
+__device__ __forceinline__ bool choose(int top_k, Key (&key)[ITEMS], int e0, int q, bool check, float sure, int32_t* s_e, Same same) {
     const Key none = -(Key)INFINITY;
     bool clear = true;
     Key last = 0;
@@ -205,7 +210,7 @@ __device__ __forceinline__ bool choose(int top_k, Key (&key)[ITEMS], int q, bool
                 best = key[j];
                 j_best = j;
             }
-        int e = q * ITEMS + j_best;
+        int e = e0 + j_best;
         largest<P>(best, e);
         const bool any = best > none;
         if (check && k > 0 && any && last_e >= 0 && !surely(last, best, sure)) clear = clear && same(last_e, e);
@@ -214,7 +219,7 @@ __device__ __forceinline__ bool choose(int top_k, Key (&key)[ITEMS], int q, bool
         if (k < top_k && q == 0) s_e[k] = last_e;
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j)
-            if (e == q * ITEMS + j) key[j] = none;
+            if (e == e0 + j) key[j] = none;                      // (behind the lane's own: -inf already)
     }
     return clear;
 }
@@ -237,7 +242,7 @@ __device__ __forceinline__ float in_descending_order(float v, int q) {
 // least of them does not count.  Those few that do, a lane each, are ranked by comparing each with all.  Returns false, with nothing
 // done, if there are more than P of them (equal keys, or few lanes with any).
 template <int ITEMS, int P, typename Same>
-__device__ __forceinline__ bool choose_few(int top_k, const float (&key)[ITEMS], int q, bool check, float sure, int32_t* s_e, float2* s_few,
+__device__ __forceinline__ bool choose_few(int top_k, const float (&key)[ITEMS], int e0, int q, bool check, float sure, int32_t* s_e, float2* s_few,
                                            bool* clear, Same same) {
     const float none = -INFINITY;
     const int lane = threadIdx.x & 31, first = lane & ~(P - 1);
@@ -276,7 +281,7 @@ __device__ __forceinline__ bool choose_few(int top_k, const float (&key)[ITEMS],
     at -= mine;
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j)
-        if (key[j] >= least) s_few[at++] = make_float2(key[j], __int_as_float(q * ITEMS + j));
+        if (key[j] >= least) s_few[at++] = make_float2(key[j], __int_as_float(e0 + j));
     __syncwarp();
     float2 me = make_float2(none, __int_as_float(-1));
     if (q < few) me = s_few[q];
@@ -310,15 +315,15 @@ template <typename T, int ITEMS, int P, bool WHOLE>
 __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) k_expert_choose(const T* __restrict__ logits, int64_t ld,
                                                                         const float* __restrict__ bias, const int32_t* n_tokens,
                                                                         int64_t max_tokens, int top_k, int E, int G, int per_group,
-                                                                        unsigned group_magic, int top_groups, int flags,
+                                                                        unsigned group_magic, int top_groups, int per_lane,
+                                                                        int group_lanes, int flags,
                                                                         float scale, int32_t* __restrict__ experts,
                                                                         float* __restrict__ weights, int32_t* status) {
     using S = Shape<ITEMS, P>;
     __shared__ int32_t s_chosen[S::kTokens][S::kChosen];
     __shared__ float2 s_few[P >= 16 ? S::kNT : 1];
     extern __shared__ double s_base[];                           // with groups that are not whole lanes', of every token: [E + 2 G]
-    Router r{top_k, E, G, per_group, top_groups, group_magic, kSureSigmoid, (flags & kSoftmax) != 0, (flags & kPair) != 0, (flags & kRenorm) != 0};
-    const bool whole_lanes = flags & kWholeLanes;
+    Router r{top_k, E, G, per_group, top_groups, per_lane, group_lanes, group_magic, kSureSigmoid, (flags & kSoftmax) != 0, (flags & kPair) != 0, (flags & kRenorm) != 0};
     const int q = threadIdx.x % P, mine = threadIdx.x / P;
     int64_t tokens = max_tokens;
     if (n_tokens) tokens = min((int64_t)max(__ldg(n_tokens), 0), max_tokens);
@@ -327,12 +332,12 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
     const bool live = t < tokens;
     const T* row = logits + (live ? t : tokens - 1) * ld;
     int32_t* s_e = s_chosen[mine];
-    double* s_value = s_base + (whole_lanes ? 0 : mine * (E + 2 * G));
+    double* s_value = s_base + (group_lanes ? 0 : mine * (E + 2 * G));
     float* s_value32 = reinterpret_cast<float*>(s_value);
     const float none = -INFINITY;
-    const int e0 = q * ITEMS;
+    const int e0 = q * per_lane, e1 = min(e0 + per_lane, E);     // the lane's experts
 
-    float l[ITEMS];
+    float l[ITEMS], any_nan = 0.f;                               // (0 * an infinity makes a NaN, too)
     bool bad = false;
     if constexpr (WHOLE) {
         constexpr int N = 16 / sizeof(T);
@@ -340,22 +345,26 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
 #pragma unroll
         for (int i = 0; i < ITEMS / N; ++i) {
             in[i].zero();
-            if (e0 + i * N < E) in[i].load(row + e0 + i * N);
+            if (e0 + i * N < e1) in[i].load(row + e0 + i * N);
         }
 #pragma unroll
         for (int i = 0; i < ITEMS / N; ++i) {
             float x[N];
             in[i].get(x);
 #pragma unroll
-            for (int k = 0; k < N; ++k) l[i * N + k] = e0 + i * N < E ? x[k] : none;
+            for (int k = 0; k < N; ++k) {
+                any_nan = fmaf(x[k], 0.f, any_nan);
+                l[i * N + k] = e0 + i * N < e1 ? x[k] : none;
+            }
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < ITEMS; ++j) l[j] = e0 + j < E ? as_float(row[e0 + j]) : none;
+        for (int j = 0; j < ITEMS; ++j) {
+            const float x = e0 + j < e1 ? as_float(row[e0 + j]) : 0.f;
+            any_nan = fmaf(x, 0.f, any_nan);
+            l[j] = e0 + j < e1 ? x : none;
+        }
     }
-    float any_nan = 0.f;                                         // (infinities make one, too)
-#pragma unroll
-    for (int j = 0; j < ITEMS; ++j) any_nan = fmaf(l[j], 0.f, any_nan);
     if (any_nan != 0.f) {
 #pragma unroll
         for (int j = 0; j < ITEMS; ++j)
@@ -405,7 +414,7 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
                         Pack<float, 4> in;
                         float x[4];
                         in.zero();
-                        if (e0 + i * 4 < E) in.load(bias + e0 + i * 4);
+                        if (e0 + i * 4 < e1) in.load(bias + e0 + i * 4);
                         in.get(x);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) value[4 * i + k] += x[k];
@@ -413,7 +422,7 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
                 } else {
 #pragma unroll
                     for (int j = 0; j < ITEMS; ++j)
-                        if (e0 + j < E) value[j] += __ldg(&bias[e0 + j]);
+                        if (e0 + j < e1) value[j] += __ldg(&bias[e0 + j]);
                 }
             }
 #pragma unroll
@@ -423,16 +432,16 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
                 value[j] = there && value[j] == value[j] ? value[j] : none;
                 if (bias) key[j] = value[j];
             }
-            if (G > 1) clear = keep_groups<ITEMS, P>(r, whole_lanes, value, key, q, s_value32);
+            if (G > 1) clear = keep_groups<ITEMS, P>(r, value, key, q, s_value32);
         } else if (G > 1) {
-            keep_groups<ITEMS, P>(r, whole_lanes, l, key, q, s_value32);
+            keep_groups<ITEMS, P>(r, l, key, q, s_value32);
         }
         const auto same = [&](int a, int b) { return as_float(row[a]) == as_float(row[b]) && __ldg(&bias[a]) == __ldg(&bias[b]); };
         const bool check = bias != nullptr;
         bool done = false, in_order = true;
         if constexpr (P >= 16)
-            if (top_k < P) done = choose_few<ITEMS, P>(top_k, key, q, check, r.sure, s_e, s_few + mine * P, &in_order, same);
-        if (!done) in_order = choose<ITEMS, P>(top_k, key, q, check, r.sure, s_e, same);
+            if (top_k < P) done = choose_few<ITEMS, P>(top_k, key, e0, q, check, r.sure, s_e, s_few + mine * P, &in_order, same);
+        if (!done) in_order = choose<ITEMS, P>(top_k, key, e0, q, check, r.sure, s_e, same);
         clear = clear && in_order;
     }
     if (__any_sync(kAll, scores && live && !clear)) {            // (all tokens of the warp once more)
@@ -456,8 +465,8 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
             }
         }
         __syncwarp();
-        if (G > 1) keep_groups<ITEMS, P>(r, whole_lanes, value, key, q, s_value);
-        choose<ITEMS, P>(top_k, key, q, false, 0.f, s_e, [](int, int) { return true; });
+        if (G > 1) keep_groups<ITEMS, P>(r, value, key, q, s_value);
+        choose<ITEMS, P>(top_k, key, e0, q, false, 0.f, s_e, [](int, int) { return true; });
     }
     if (status && __any_sync(kAll, bad && live) && (threadIdx.x & 31) == 0) set_status(status, HL_EINVAL);
     __syncwarp();
@@ -645,37 +654,50 @@ int flags_of(const hl_router* r) {
     return (r->score == HL_SCORE_SOFTMAX ? kSoftmax : 0) | (r->group_score == HL_GROUP_TOP2 ? kPair : 0) | (r->renorm ? kRenorm : 0);
 }
 
-// As few lanes a token as hold its experts, eight a lane, above 128 experts sixteen (two tokens of 256 experts a warp, for which most steps
-// take the time of one: 69 us instead of 82 for 65 536), above 512 more.
-#define HL_SHAPES(E, RUN, WHOLE)                                                                                        \
-    ((E) <= 8     ? RUN(8, 1, WHOLE)                                                                                    \
-     : (E) <= 16  ? RUN(8, 2, WHOLE)                                                                                    \
-     : (E) <= 32  ? RUN(8, 4, WHOLE)                                                                                    \
-     : (E) <= 64  ? RUN(8, 8, WHOLE)                                                                                    \
-     : (E) <= 128 ? RUN(8, 16, WHOLE)                                                                                   \
-     : (E) <= 256 ? RUN(16, 16, WHOLE)                                                                                  \
-     : (E) <= 512 ? RUN(16, 32, WHOLE)                                                                                  \
-                  : RUN(32, 32, WHOLE))
-// whether a group is the experts of 1, 2, 4 ... of these lanes
-bool whole_lanes(const hl_router* r) {
-    const int items = r->n_experts <= 128 ? 8 : r->n_experts <= 512 ? 16 : 32, per = r->n_experts / r->n_groups, lanes = per / items;
-    return per % items == 0 && (lanes & (lanes - 1)) == 0;
+// Lanes of a token and how many experts each holds at most: as few lanes as hold all, eight a lane, above 128 experts sixteen (two
+// tokens of 256 experts a warp, for which most steps take the time of one: 69 us instead of 82 for 65 536), above 512 more.  With
+// groups, one in which a group is that of whole lanes, of as many experts each as divide it: that one, or a wider one of less than 16 lanes
+// (16 lanes for 60 experts in five groups: 54 us instead of 33 through shared memory, 45 282 tokens; 384 in eight: 115 instead of
+// 190 for 65 536).
+#define HL_SHAPES(S, RUN, WHOLE)                                                                                        \
+    ((S) == 0   ? RUN(8, 1, WHOLE)                                                                                      \
+     : (S) == 1 ? RUN(8, 2, WHOLE)                                                                                      \
+     : (S) == 2 ? RUN(8, 4, WHOLE)                                                                                      \
+     : (S) == 3 ? RUN(8, 8, WHOLE)                                                                                      \
+     : (S) == 4 ? RUN(8, 16, WHOLE)                                                                                     \
+     : (S) == 5 ? RUN(16, 16, WHOLE)                                                                                    \
+     : (S) == 6 ? RUN(16, 32, WHOLE)                                                                                    \
+                : RUN(32, 32, WHOLE))
+constexpr int kShapes = 8, kShapeItems[kShapes] = {8, 8, 8, 8, 8, 16, 16, 32}, kShapeLanes[kShapes] = {1, 2, 4, 8, 16, 16, 32, 32};
+struct Layout {
+    int shape, per_lane, group_lanes;
+};
+Layout layout_of(const hl_router* r) {
+    const int E = r->n_experts, per = E / r->n_groups;
+    int first = 0;
+    while (kShapeItems[first] * kShapeLanes[first] < E) ++first;
+    if (r->n_groups > 1)
+        for (int s = first; s == first || (s < kShapes && kShapeLanes[s] < 16); ++s)
+            for (int d = kShapeItems[s]; 2 * d >= kShapeItems[s]; --d)     // (at least half of what a lane can hold)
+                if (per % d == 0 && E / d <= kShapeLanes[s]) return {s, d, per / d};
+    return {first, kShapeItems[first], 0};
 }
 
 template <typename T>
 int32_t launch_choose(const hl_router* r, const void* logits, int64_t ld, const float* bias, int64_t max_tokens,
                       const int32_t* n_tokens, int32_t* experts, float* weights, int32_t* status, cudaStream_t stream) {
-    const bool lanes = whole_lanes(r);
+    const Layout at = layout_of(r);
     const int per = r->n_experts / r->n_groups;
 #define HL_RUN(ITEMS, P, WHOLE)                                                                                               \
     launch_cluster(k_expert_choose<T, ITEMS, P, WHOLE>, (unsigned)div_up(max_tokens, Shape<ITEMS, P>::kTokens), Shape<ITEMS, P>::kNT, \
-                   r->n_groups > 1 && !lanes ? Shape<ITEMS, P>::kTokens * (r->n_experts + 2 * r->n_groups) * sizeof(double) : 0, 0,      \
+                   r->n_groups > 1 && !at.group_lanes ? Shape<ITEMS, P>::kTokens * (r->n_experts + 2 * r->n_groups) * sizeof(double) : 0, 0,      \
                    stream, static_cast<const T*>(logits), ld, bias, n_tokens, max_tokens, r->top_k, r->n_experts, r->n_groups, \
-                   per, ((1u << 21) + per - 1) / (unsigned)per, r->top_groups, flags_of(r) | (lanes ? kWholeLanes : 0), r->scale, experts, weights, status)
-    const bool whole = r->n_experts % (16 / (int)sizeof(T)) == 0 && lies_at(logits, 16) && ld * sizeof(T) % 16 == 0 &&
-                       lies_at(bias, 16);
-    if (whole) HL_CUDA_TRY(HL_SHAPES(r->n_experts, HL_RUN, true));
-    else HL_CUDA_TRY(HL_SHAPES(r->n_experts, HL_RUN, false));
+                   per, ((1u << 21) + per - 1) / (unsigned)per, r->top_groups, at.per_lane, at.group_lanes, flags_of(r), r->scale,    \
+                   experts, weights, status)
+    constexpr int N = 16 / (int)sizeof(T);
+    const bool whole = r->n_experts % N == 0 && at.per_lane % N == 0 && lies_at(logits, 16) && ld * sizeof(T) % 16 == 0 && lies_at(bias, 16);
+    if (whole) HL_CUDA_TRY(HL_SHAPES(at.shape, HL_RUN, true));
+    else HL_CUDA_TRY(HL_SHAPES(at.shape, HL_RUN, false));
 #undef HL_RUN
     note_launches(1);
     HL_LAUNCH_CHECK();

@@ -141,7 +141,8 @@ def test_choices(hl, K, E, score):
 
 @pytest.mark.parametrize("E,G,TG,K", [(8, 2, 1, 3), (8, 8, 3, 2), (16, 4, 2, 8), (60, 5, 3, 6), (64, 8, 3, 8), (64, 2, 1, 4), (64, 64, 9, 9),
                                       (128, 16, 5, 8), (160, 8, 3, 6), (256, 8, 4, 8), (256, 8, 2, 8), (256, 8, 1, 32), (256, 2, 1, 8),
-                                      (256, 16, 16, 8), (500, 4, 2, 8), (512, 8, 2, 16), (1024, 32, 4, 8), (1000, 50, 7, 64)])
+                                      (256, 16, 16, 8), (500, 4, 2, 8), (512, 8, 2, 16), (1024, 32, 4, 8), (1000, 50, 7, 64),
+                                      (32, 8, 3, 4), (96, 8, 3, 4), (192, 4, 2, 8), (384, 8, 4, 8), (480, 10, 4, 8), (800, 25, 5, 20)])
 @pytest.mark.parametrize("score", [0, 1])
 @pytest.mark.parametrize("pair", [False, True])
 def test_groups(hl, E, G, TG, K, score, pair):
