@@ -597,6 +597,12 @@ int32_t radix_sort_pairs(int32_t* keys[2], int32_t* vals[2], const int32_t* d_n,
                          uint32_t* hist, int32_t* status, int32_t** out_keys, int32_t** out_vals,
                          cudaStream_t stream, WaitCfg w = WaitCfg(), bool counted = false);
 
+// The places of tokens in the order of their rows, for at most as many as one cluster holds (sorts_tokens): tokens that are no row
+// of n_rows < 2^key_bits behind all others, as n_rows; HL_EBOUNDS in status (may be null) for any that is not -1 either.
+bool sorts_tokens(int64_t max_tokens);
+int32_t sort_tokens(const int32_t* tokens, const int32_t* n_tokens, int64_t max_tokens, int n_rows, int key_bits, int32_t* sorted,
+                    int32_t* order, int32_t* status, cudaStream_t stream);
+
 // Words at the start of `hist` that must be zero before the sort's digits are counted; 0 if the sort that will be used
 // counts none.  A caller that clears them and then counts the keys' digits itself (hist[pass * 256 + digit]) passes
 // counted = true.

@@ -300,12 +300,10 @@ __global__ void __launch_bounds__(kThreads, ORDER ? 4 : 1) k_sort_pass(const int
 // sends each pair to the CTA that owns its new position (the last pass: to its place in the output).  CTA c owns
 // positions [c * per, (c + 1) * per).  One launch instead of a memset, the digit counts and a kernel per pass, and nothing
 // but the pairs themselves goes through the L2 (8 K pairs, three passes: 12.5 us, against 23 us in four kernels).
-template <int CTAS, int NT, int ITEMS>
-__global__ void __launch_bounds__(NT) k_sort_cluster(const int32_t* __restrict__ keys_in,
-                                                               const int32_t* __restrict__ vals_in,
-                                                               int32_t* __restrict__ keys_out,
-                                                               int32_t* __restrict__ vals_out, const int32_t* d_n,
-                                                               int64_t n_max, int passes) {
+// pair_at(i, key, val): the i-th of n > 0 pairs.
+template <int CTAS, int NT, int ITEMS, typename PairAt>
+__device__ __forceinline__ void sort_by_cluster(PairAt pair_at, int32_t* __restrict__ keys_out, int32_t* __restrict__ vals_out, int n,
+                                                int passes) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     constexpr int PD = NT / 256;                  // threads per digit
@@ -314,8 +312,6 @@ __global__ void __launch_bounds__(NT) k_sort_cluster(const int32_t* __restrict__
     __shared__ uint32_t cta_hist[256];            // this CTA's digit counts, read by the other CTAs
     __shared__ uint32_t digit_base[256];
     __shared__ int scan_smem[40];
-    const int n = (int)clamp_n(d_n, n_max);
-    if (n == 0) return;                           // the same in all CTAs
     const int cta = (int)cluster.block_rank();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per = max(2, (n + CTAS - 1) / CTAS);        // pairs per CTA (two at least: inv_per has 32 bits)
@@ -328,10 +324,7 @@ __global__ void __launch_bounds__(NT) k_sort_cluster(const int32_t* __restrict__
 #pragma unroll
     for (int r = 0; r < ITEMS; ++r) {
         key[r] = val[r] = 0u;
-        if (r < rounds && r * 32 + lane < n_mine) {
-            key[r] = (uint32_t)keys_in[cta * per + first + r * 32 + lane];
-            val[r] = (uint32_t)vals_in[cta * per + first + r * 32 + lane];
-        }
+        if (r < rounds && r * 32 + lane < n_mine) pair_at(cta * per + first + r * 32 + lane, key[r], val[r]);
     }
     for (int p = 0; p < passes; ++p) {
         const int shift = 8 * p;
@@ -388,6 +381,38 @@ __global__ void __launch_bounds__(NT) k_sort_cluster(const int32_t* __restrict__
             }
         }
     }
+}
+
+template <int CTAS, int NT, int ITEMS>
+__global__ void __launch_bounds__(NT) k_sort_cluster(const int32_t* __restrict__ keys_in,
+                                                               const int32_t* __restrict__ vals_in,
+                                                               int32_t* __restrict__ keys_out,
+                                                               int32_t* __restrict__ vals_out, const int32_t* d_n,
+                                                               int64_t n_max, int passes) {
+    const int n = (int)clamp_n(d_n, n_max);
+    if (n == 0) return;                           // the same in all CTAs
+    const auto pair_at = [&](int i, uint32_t& key, uint32_t& val) {
+        key = (uint32_t)keys_in[i];
+        val = (uint32_t)vals_in[i];
+    };
+    sort_by_cluster<CTAS, NT, ITEMS>(pair_at, keys_out, vals_out, n, passes);
+}
+
+// The same of tokens and their places: a token that is no row counts as n_rows.
+template <int CTAS, int NT, int ITEMS>
+__global__ void __launch_bounds__(NT) k_sort_tokens(const int32_t* __restrict__ tokens, int32_t* __restrict__ sorted,
+                                                    int32_t* __restrict__ order, const int32_t* n_tokens, int64_t max_tokens,
+                                                    int n_rows, int passes, int32_t* status) {
+    const int n = n_tokens ? (int)clamp_n(n_tokens, max_tokens) : (int)max_tokens;
+    if (n == 0) return;
+    const auto pair_at = [&](int i, uint32_t& key, uint32_t& val) {
+        const int t = __ldg(&tokens[i]);
+        const bool row = (unsigned)t < (unsigned)n_rows;
+        if (!row && t != -1 && status) set_status(status, HL_EBOUNDS);
+        key = row ? (uint32_t)t : (uint32_t)n_rows;
+        val = (uint32_t)i;
+    };
+    sort_by_cluster<CTAS, NT, ITEMS>(pair_at, sorted, order, n, passes);
 }
 
 // ---- pairs that are grouped by table already ---------------------------------------------------------------------
@@ -601,9 +626,13 @@ int sort_cluster_ctas() {
                cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters >= 1;
     };
     const int ctas = can(k_sort_cluster<16, kClusterNT, kClusterItems>, 16, kClusterNT, kClusterItems) &&
+                             can(k_sort_tokens<16, kClusterNT, kClusterItems>, 16, kClusterNT, kClusterItems) &&
                              can(k_sort_segments<16, 256, 8>, 16, 256, 8) && can(k_sort_segments<16, 512, 8>, 16, 512, 8)
                          ? 16
-                         : (can(k_sort_cluster<8, kClusterNT, kClusterItems>, 8, kClusterNT, kClusterItems) ? 8 : 0);
+                         : (can(k_sort_cluster<8, kClusterNT, kClusterItems>, 8, kClusterNT, kClusterItems) &&
+                                    can(k_sort_tokens<8, kClusterNT, kClusterItems>, 8, kClusterNT, kClusterItems)
+                                ? 8
+                                : 0);
     (void)cudaGetLastError();
     known[dev].store(ctas + 1, std::memory_order_release);
     return ctas;
@@ -669,6 +698,19 @@ int32_t sort_segments(const SegmentArgs& a, cudaStream_t stream) {
 int64_t sort_clear_words(int64_t n_max, int key_bits, WaitCfg w) {
     if (n_max <= 0 || sort_in_cluster(n_max, w)) return 0;
     return 4 * 256 + (int64_t)((key_bits + 7) / 8) * div_up(n_max, kSortTile) * 256;
+}
+
+bool sorts_tokens(int64_t max_tokens) { return sort_in_cluster(max_tokens, WaitCfg()); }
+
+int32_t sort_tokens(const int32_t* tokens, const int32_t* n_tokens, int64_t max_tokens, int n_rows, int key_bits, int32_t* sorted,
+                    int32_t* order, int32_t* status, cudaStream_t stream) {
+    const int ctas = sort_cluster_ctas();
+    HL_CUDA_TRY(launch_cluster(ctas == 16 ? k_sort_tokens<16, kClusterNT, kClusterItems> : k_sort_tokens<8, kClusterNT, kClusterItems>,
+                               ctas, kClusterNT, sizeof(SortSmem<kClusterNT, kClusterItems>), ctas, stream, tokens, sorted, order,
+                               n_tokens, max_tokens, n_rows, (key_bits + 7) / 8, status));
+    note_launches(1);
+    HL_LAUNCH_CHECK();
+    return HL_OK;
 }
 
 int32_t radix_sort_pairs(int32_t* keys[2], int32_t* vals[2], const int32_t* d_n, int64_t n_max, int key_bits,

@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kNT) k_token_embed_loose(const TT* __restrict_
 
 // ---- the sort -----------------------------------------------------------------------------------------------------------
 // Few tokens: a token's place is how many are below it, and equal ones in front of it; each is compared with all.  (Some 5 us of one
-// kernel for 2 048, where making pairs and sorting them takes two kernels and 15 us, whatever their number.)
+// kernel for 2 048, where a cluster's sort takes 12 whatever their number.)
 constexpr int kFewTokens = 2048, kFewNT = 128;
 __global__ void __launch_bounds__(kFewNT) k_token_rank(const int32_t* __restrict__ tokens, int max_tokens, const int32_t* n_tokens,
                                                        int n_rows, int32_t* __restrict__ sorted, int32_t* __restrict__ order,
@@ -579,20 +579,20 @@ extern "C" int32_t hl_token_sort(const int32_t* d_tokens, int64_t max_tokens, co
     }
     int bits = 1;
     while ((n_rows >> bits) != 0) ++bits;
-    const int out = ((bits + 7) / 8) & 1;                        // which of the two buffers the sort ends in
+    if (sorts_tokens(max_tokens))
+        return sort_tokens(d_tokens, d_n_tokens, max_tokens, (int)n_rows, bits, d_sorted, d_order, d_status, stream);
+    const int passes = (bits + 7) / 8, out = passes & 1;         // (which of the two buffers the sort ends in)
     int32_t *keys[2], *vals[2], *sorted, *order;
     keys[out] = d_sorted;
     vals[out] = d_order;
     keys[out ^ 1] = ws.keys;
     vals[out ^ 1] = ws.vals;
     int32_t* status = d_status ? d_status : ws.status;
-    // (a sort that counts no digits, in one cluster, has none to clear either)
-    const int64_t clear = sort_clear_words(max_tokens, bits, WaitCfg());
-    if (clear) HL_CUDA_TRY(clear_words(ws.hist, clear, stream));
-    HL_CUDA_TRY(launch(k_token_pairs, grid_for(max_tokens, kNT * (clear ? 2 : 1), 1024), kNT, stream, d_tokens, max_tokens, d_n_tokens,
-                       (int)n_rows, keys[0], vals[0], ws.n, clear ? (bits + 7) / 8 : 0, ws.hist, status));
+    HL_CUDA_TRY(clear_words(ws.hist, sort_clear_words(max_tokens, bits, WaitCfg()), stream));
+    HL_CUDA_TRY(launch(k_token_pairs, grid_for(max_tokens, kNT * 2, 1024), kNT, stream, d_tokens, max_tokens, d_n_tokens, (int)n_rows,
+                       keys[0], vals[0], ws.n, passes, ws.hist, status));
     note_launches(1);
-    return radix_sort_pairs(keys, vals, ws.n, max_tokens, bits, ws.hist, status, &sorted, &order, stream, WaitCfg(), clear != 0);
+    return radix_sort_pairs(keys, vals, ws.n, max_tokens, bits, ws.hist, status, &sorted, &order, stream, WaitCfg(), true);
 }
 
 extern "C" int32_t hl_token_embed_bwd(int64_t n_rows, int64_t dim, const int32_t* d_sorted, const int32_t* d_order,
