@@ -205,10 +205,9 @@ struct Experts {
     __device__ __forceinline__ int rows(int e, int from) const { return (int)min((int64_t)max(__ldg(&counts[e]), 0), cap_rows - from); }
 };
 
-// Fills s_first [E + 1] and s_begin [E], and, if it is there, s_rows [E] with how many rows each has (s_begin [E + 1] then): by all NT
-// threads of a CTA.
+// Fills s_first [E + 1] (and s_begin [E], if there): by all NT threads of a CTA.
 template <int NT>
-__device__ void tile_numbers(const Experts& x, int most, int* s_first, int* s_begin, int* s_rows) {
+__device__ void tile_numbers(const Experts& x, int most, int* s_first, int* s_begin) {
     constexpr int kPer = (HL_MAX_EXPERTS + NT - 1) / NT;
     __shared__ int s_warp[NT / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -219,13 +218,8 @@ __device__ void tile_numbers(const Experts& x, int most, int* s_first, int* s_be
         tiles[k] = 0;
         if (e >= x.E) continue;
         const int from = x.begin(e);
-        const int rows = x.rows(e, from);
-        s_begin[e] = from;
-        if (s_rows) {
-            s_rows[e] = rows;
-            if (e == x.E - 1) s_begin[e + 1] = x.begin(e + 1);
-        }
-        tiles[k] = (rows + kPanelRows - 1) / kPanelRows;
+        if (s_begin) s_begin[e] = from;
+        tiles[k] = (x.rows(e, from) + kPanelRows - 1) / kPanelRows;
         sum += tiles[k];
     }
     int incl = sum;
@@ -275,7 +269,7 @@ __global__ void __launch_bounds__(kRowNT, kRowCtas<U>) k_mx4_rows(const T* __res
     let_next_start();
     if (blockIdx.x == 0 && threadIdx.x == 0) *status = HL_OK;
     const Experts experts{counts, offsets, E, cap_rows};
-    tile_numbers<kRowNT>(experts, max_tiles, s_first, s_begin, nullptr);
+    tile_numbers<kRowNT>(experts, max_tiles, s_first, s_begin);
     const int lane = threadIdx.x & 31;
     int64_t n = max_rows;
     if (top_k == 0) n = min(n, (int64_t)max(__ldg(&offsets[E]), 0));
@@ -348,7 +342,7 @@ constexpr int kProductNT = 320;
 constexpr uint32_t kExponentCols = 2 * kPanelRows;               // tensor-memory columns: two tiles' sums, 8 of w's exponents, 16 of x'
 // A stage is a step's tile of w and as many of x' rows as an expert can have: few rows leave room for more steps on their way.
 constexpr int kMostStages = 10, kStagesBytes = 4 * (kTileBytes + kPanelBytes);
-constexpr int kProductSmem = kStagesBytes + 1024 + 3 * (HL_MAX_EXPERTS + 1) * 4;
+constexpr int kProductSmem = kStagesBytes + 1024 + (HL_MAX_EXPERTS + 1) * 4 + 256;
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint64_t* b, int n) {
@@ -447,20 +441,16 @@ struct Item {
     int e, rows, f;                    // rows: of the tile
     int64_t row0, tile, pad;           // its first row's number; pad: rows behind the expert's last that fill it up, if it is the last tile
 };
-// the experts as the CTA has them in shared memory (tile_numbers)
-struct Tiles {
-    int E, f_tiles, panel_rows;
-    const int *first, *begin, *rows;
-};
-__device__ __forceinline__ Item item_of(int64_t i, const Tiles& x) {
+__device__ __forceinline__ Item item_of(int64_t i, int f_tiles, const Experts& x, const int* s_first, int panel_rows) {
     Item it;
-    it.tile = i / x.f_tiles;
-    it.f = (int)(i - it.tile * x.f_tiles);
-    it.e = last_not_above(x.first, x.E, (int)it.tile);
-    const int begin = x.begin[it.e], rows = x.rows[it.e], at = ((int)it.tile - x.first[it.e]) * kPanelRows;
-    it.rows = min(rows - at, x.panel_rows);
+    it.tile = i / f_tiles;
+    it.f = (int)(i - it.tile * f_tiles);
+    it.e = last_not_above(s_first, x.E, (int)it.tile);
+    const int begin = x.begin(it.e), rows = x.rows(it.e, begin), at = ((int)it.tile - s_first[it.e]) * kPanelRows;
+    it.rows = min(rows - at, panel_rows);
     it.row0 = (int64_t)begin + at;
-    it.pad = it.tile + 1 == x.first[it.e + 1] ? max(x.begin[it.e + 1] - begin - rows, 0) : 0;
+    const int64_t end = min((int64_t)max(__ldg(&x.offsets[it.e + 1]), 0), x.cap_rows);
+    it.pad = it.tile + 1 == s_first[it.e + 1] ? max(end - begin - rows, (int64_t)0) : 0;
     return it;
 }
 
@@ -474,7 +464,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
                                                                int panel_rows, int32_t* status) {
     extern __shared__ uint8_t s_raw[];
     uint8_t* base = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
-    int *s_first = reinterpret_cast<int*>(base + kStagesBytes), *s_begin = s_first + E + 1, *s_rows = s_begin + E + 1;
+    int* s_first = reinterpret_cast<int*>(base + kStagesBytes);
     const int panel_bytes = panel_rows * 128, stage_bytes = kTileBytes + panel_bytes + (panel_rows > kTileRows ? 2048 : 1024);
     __shared__ uint64_t s_full[kMostStages], s_empty[kMostStages], s_sums[2], s_taken[2];
     __shared__ uint32_t s_tmem;
@@ -499,10 +489,9 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }
     const Experts experts{counts, offsets, E, cap_rows};
-    tile_numbers<kProductNT>(experts, max_tiles, s_first, s_begin, s_rows);          // (ends with a barrier)
+    tile_numbers<kProductNT>(experts, max_tiles, s_first, nullptr);        // (ends with a barrier)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
-    const Tiles tiles{E, f_tiles, panel_rows, s_first, s_begin, s_rows};
     const int64_t items = (int64_t)s_first[E] * f_tiles;
 
     if (warp == 0) {
@@ -523,7 +512,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
             };
             int early = 0;
             if (blockIdx.x < items) {
-                const Item it = item_of(blockIdx.x, tiles);
+                const Item it = item_of(blockIdx.x, f_tiles, experts, s_first, panel_rows);
                 const uint8_t* a = wq + ((int64_t)it.e * f_tiles + it.f) * col_tiles * kTileBytes;
                 for (; early < min(stages, col_tiles); ++early, a += kTileBytes) {
                     ask(a, DIRECT ? 0 : ((it.rows + 15) & ~15) * 128, DIRECT ? 0 : it.rows > kTileRows ? 2048 : 1024);
@@ -534,7 +523,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
             stage = 0;
             phase = 1;
             for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-                const Item it = item_of(i, tiles);
+                const Item it = item_of(i, f_tiles, experts, s_first, panel_rows);
                 const uint8_t* a = wq + ((int64_t)it.e * f_tiles + it.f) * col_tiles * kTileBytes;
                 const uint8_t* b = xq + it.tile * col_tiles * kPanelBytes;
                 const uint32_t b_bytes = DIRECT ? 0 : ((it.rows + 15) & ~15) * 128, e_bytes = DIRECT ? 0 : it.rows > kTileRows ? 2048 : 1024;
@@ -565,7 +554,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
         uint32_t phase = 0, taken = 1;
         bool ok = true;
         for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-            const uint32_t n = __shfl_sync(0xffffffffu, (item_of(i, tiles).rows + 15) & ~15, 0);
+            const uint32_t n = __shfl_sync(0xffffffffu, (item_of(i, f_tiles, experts, s_first, panel_rows).rows + 15) & ~15, 0);
             const uint32_t acc = d + buffer * kPanelRows, what0 = multiplication(n, 0), what1 = multiplication(n, 1);
             if (!(ok = bar_wait_all(&s_taken[buffer], taken, &s_gave_up))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -599,7 +588,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
         int buffer = 0, stage = 0;
         uint32_t phase = 0, empty = 1;
         for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
-            const Item it = item_of(i, tiles);
+            const Item it = item_of(i, f_tiles, experts, s_first, panel_rows);
             if constexpr (DIRECT) {
                 // x' rows step by step, each row's part by one of the warps in turn.  (As a rule an expert has one row or two here; several
                 // parts of a warp on their way at a time: 10.8 us instead of 8.8 a call of one token, 20 instead of 23 for twelve rows
