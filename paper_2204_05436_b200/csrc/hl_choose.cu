@@ -564,13 +564,19 @@ __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__
         z = sum_of<P>(z);
     }
     // the chosen: their scores (relative, as above), and sums over them
-    float m = none;
+    float m = none, base = none;
     for (int k = q; k < top_k; k += P) {
         const int e = __ldg(&experts[at * top_k + k]);
         s_chosen[mine][k] = (unsigned)e < (unsigned)E ? e : -1;
-        if ((unsigned)e < (unsigned)E) m = fmaxf(m, logit(e));
+        if ((unsigned)e >= (unsigned)E) continue;
+        m = fmaxf(m, logit(e));
+        if (renorm) base = fmaxf(base, __ldg(&grad_w[at * top_k + k]));
     }
     m = max_of<P>(m);
+    // Shares do not change with what all gradients have in common: without the largest of them, nothing is left where they are alike,
+    // or there is one alone, whatever the shares' roundings.
+    if (renorm) base = max_of<P>(base);
+    if (!renorm || !isfinite(base)) base = 0.f;
     if (!softmax) m = renorm ? fminf(m, 0.f) : 0.f;
     else if (!renorm) m = top;
     const auto score = [&](float x, float* rest) {               // *rest: 1 - sigmoid(x)
@@ -586,7 +592,7 @@ __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__
         const int e = s_chosen[mine][k];
         if (e < 0) continue;
         float rest;
-        const float s = score(logit(e), &rest), g = __ldg(&grad_w[at * top_k + k]);
+        const float s = score(logit(e), &rest), g = __ldg(&grad_w[at * top_k + k]) - base;
         if (k == q) {
             first = s;
             first_rest = rest;
@@ -606,7 +612,7 @@ __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__
         const int e = s_chosen[mine][k];
         if (k != q && e >= 0) {
             s = score(logit(e), &rest);
-            g = __ldg(&grad_w[at * top_k + k]);
+            g = __ldg(&grad_w[at * top_k + k]) - base;
         }
         // (the mean is of all experts' softmax: once for an expert, however often it is there)
         bool again = false;

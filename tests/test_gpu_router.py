@@ -300,6 +300,22 @@ def test_gradient(hl, K, E, score, renorm, dtype):
 
 
 @pytest.mark.parametrize("score", [0, 1])
+@pytest.mark.parametrize("K,E", [(1, 8), (1, 64), (1, 300), (4, 37), (8, 256), (20, 64)])
+def test_shares_that_cannot_change(hl, K, E, score):
+    """A share of one alone is 1, and gradients that are all alike (here and there infinite) change no share: exactly 0."""
+    l = _logits(500, E, torch.float32, E + K)
+    gw = torch.randn(500, K, generator=torch.Generator().manual_seed(K)).cuda()
+    if K > 1:
+        l[::2, 1:] = -INF
+        gw[::2, 1:] = INF                                        # (of choices that are not there)
+        gw[1::2] = gw[1::2, :1]
+    router, e, _ = _check(hl, l, top_k=K, score=score, renorm=True, scale=2.5)
+    out = torch.full((500, E), -7.0, device="cuda")
+    hl.hl_expert_choose_bwd(router, hl.HL_F32, l, E, 500, None, e, gw, out, E, torch.cuda.current_stream().cuda_stream)
+    assert (out == 0).all(), float(out.abs().max())
+
+
+@pytest.mark.parametrize("score", [0, 1])
 @pytest.mark.parametrize("renorm", [False, True])
 def test_gradient_against_differences(hl, score, renorm):
     """Of the sum of grad_w * weights, by central differences of the 64-bit definition (the choice stays the same)."""
