@@ -165,6 +165,20 @@ def test_runs(hl, kind, n, V, dim):
     b.check(grad_out, 2.0, table, accumulate=True)
 
 
+@pytest.mark.parametrize("n", [2047, 2048, 2049, 4095, 16_384, 16_385, 32_767, 32_768, 32_769, 33_000])
+@pytest.mark.parametrize("V", [1, 200, 255, 256, 70_000, 20_000_000])
+def test_orders_around_the_sorts_sizes(hl, n, V):
+    """Tokens in all numbers of digits, also fewer than there is room for: _Backward compares the order with a stable sort's."""
+    for live in (None, n - 1, 2049, 1, 0):
+        live = live if live is None else min(live, n)
+        tokens = _tokens(n, V, n + V, "power")
+        tokens[::7] = -1
+        assert int(_Backward(hl, tokens, V, 4, live).status) == hl.HL_OK
+        if live is None or live > 5:
+            tokens[5] = V
+            assert int(_Backward(hl, tokens, V, 4, live).status) == hl.HL_EBOUNDS
+
+
 def test_runs_of_every_length_around_the_windows(hl):
     """Rows of 1, 2, 3 ... 70 and of 15, 16, 17 times 16, 32 and 64 tokens, one behind the other."""
     lengths = list(range(1, 71)) + [w * k + d for w in (16, 32, 64) for k in (1, 15, 16, 17) for d in (-1, 0, 1)]
