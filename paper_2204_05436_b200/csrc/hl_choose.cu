@@ -308,7 +308,7 @@ __device__ __forceinline__ bool choose_few(int top_k, const float (&key)[ITEMS],
     return true;
 }
 
-// Bound by its instructions where there are many tokens: 65 536 tokens, 8 of 256 experts in 8 groups, sigmoids with a bias: 69 us, 34 MB
+// Bound by its instructions where there are many tokens: 65 536 tokens, 8 of 256 experts in 8 groups, sigmoids with a bias: 73 us, 34 MB
 // that memory gives in 6; an instruction is issued in two of three cycles.  Of that some 15 the rows and what is done once a
 // token, 11 scores and bias, 15 the groups, 20 the choice, 8 the weights.  WHOLE: rows are read in pieces of 16 bytes.
 template <typename T, int ITEMS, int P, bool WHOLE>
@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
 // ---- the logits' gradient -----------------------------------------------------------------------------------------------
 // Only the chosen experts' gradients depend on the weights' one by one.  Every expert's is -mean * score of it in a softmax without the
 // sum of the chosen below, 0 otherwise; the chosen ones' are written over it.  P lanes of a warp for a token: the chosen ones' loads,
-// one behind the other, are what a token takes, and many tokens are on their way so.  65 536 tokens, 8 of 256 bf16: 15 us, 38 MB
+// one behind the other, are what a token takes, and many tokens are on their way so.  65 536 tokens, 8 of 256 bf16: 14 us, 38 MB
 // (37 us with a warp a token).  N values of a row at a time: 16 bytes, or one.
 template <typename T, int P, bool WHOLE>
 __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__ logits, int64_t ld, const int32_t* n_tokens,

@@ -335,8 +335,8 @@ __device__ __forceinline__ int64_t row_of(int64_t at, const int32_t* __restrict_
 // y[row, f] = sum over d of x[row, d] * w[e, f, d] for the rows of expert e: 128 outputs f (the lanes of the tensor memory) by up to
 // 240 rows (its columns) at a time, 256 of d a step.  One warp's thread has the tiles of a step copied, one issues the products,
 // eight warps take the sums out, those of one tile while the next one's are made.
-// Bound by what the multiprocessors can read of the L2, for many rows: 32 768 rows by 4 096 outputs of 4 096: 225 us, 4.9 PFLOP/s, 3.7 GB of
-// tiles at 16 TB/s.  (With the copies left out it was 215 us at tiles of 128 rows, with the products left out 290; w' and x' tiles
+// Bound by what the multiprocessors can read of the L2, for many rows: 32 768 rows by 4 096 outputs of 4 096: 211 to 225 us, 5 PFLOP/s, 3.7 GB
+// of tiles at 17 TB/s.  (With the copies left out it was 215 us at tiles of 128 rows, with the products left out 290; w' and x' tiles
 // go to each multiprocessor anew, and wider ones would need two of them for a tile.)  Few rows: latency of a copy and a launch.
 constexpr int kProductNT = 320;
 constexpr uint32_t kExponentCols = 2 * kPanelRows;               // tensor-memory columns: two tiles' sums, 8 of w's exponents, 16 of x'

@@ -398,7 +398,8 @@ __global__ void __launch_bounds__(NT) k_sort_cluster(const int32_t* __restrict__
     sort_by_cluster<CTAS, NT, ITEMS>(pair_at, keys_out, vals_out, n, passes);
 }
 
-// The same of tokens and their places: a token that is no row counts as n_rows.
+// The same of tokens and their places: a token that is no row counts as n_rows.  Bound by latency: 13 us for 16 384 tokens as for
+// 28 657 (two passes; pairs in a kernel of their own first: 4 us more).
 template <int CTAS, int NT, int ITEMS>
 __global__ void __launch_bounds__(NT) k_sort_tokens(const int32_t* __restrict__ tokens, int32_t* __restrict__ sorted,
                                                     int32_t* __restrict__ order, const int32_t* n_tokens, int64_t max_tokens,

@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(kNT, LOOSE ? 3 : 2) k_token_sums(const int32_t
 // Runs over several windows: their pieces.  A warp looks at one window, of which a run may begin there and go on, and adds up the run's
 // pieces in order if it is short; what reaches over more than kShort windows is left to the CTA, whose warps take a part of the
 // pieces each, in order, and add the parts up in order.  32 W columns a CTA.  (A CTA a window, most of which end at once: 30 us
-// instead of 12 for 1 024 windows of 2 048 columns.)
+// instead of 12 for 1 024 windows of 2 048 columns.)  Bound by latency: those 13 us, 1 876 windows of 337 ragged columns 9.5.
 constexpr int kShort = 16;
 // Pieces p0 .. p1 of the run that begins in window w.  A warp's groups of P lanes, which have all columns, take every so many of them
 // and are added up by halves.
