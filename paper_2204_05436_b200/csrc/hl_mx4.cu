@@ -619,21 +619,22 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
             }
             if (!bar_wait_all(&s_sums[buffer], phase, &s_gave_up)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            __syncwarp();
             const int64_t f = (int64_t)it.f * kTileRows + quarter * 32 + lane;
             const int middle = min((it.rows + 31) / 32 * 16, it.rows), end = half ? it.rows : middle;
             for (int c0 = half ? middle : 0; c0 < end; c0 += 32) {
                 uint32_t v[32];
+                __syncwarp();          // (the whole warp reads tensor memory together; lanes behind the last output skipped the stores)
                 tmem_load(v, tmem + buffer * kPanelRows + c0 + ((uint32_t)(quarter * 32) << 16));
-                if (f >= outputs) continue;
-                T* out = y + (it.row0 + c0) * ld + f;
-                if (c0 + 32 <= end) {
+                if (f < outputs) {
+                    T* out = y + (it.row0 + c0) * ld + f;
+                    if (c0 + 32 <= end) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k, out += ld) *out = from_float<T>(__uint_as_float(v[k]));
-                } else {
+                        for (int k = 0; k < 32; ++k, out += ld) *out = from_float<T>(__uint_as_float(v[k]));
+                    } else {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k, out += ld)
-                        if (c0 + k < end) *out = from_float<T>(__uint_as_float(v[k]));
+                        for (int k = 0; k < 32; ++k, out += ld)
+                            if (c0 + k < end) *out = from_float<T>(__uint_as_float(v[k]));
+                    }
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
