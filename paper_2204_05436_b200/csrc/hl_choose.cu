@@ -114,6 +114,14 @@ __device__ __forceinline__ void two_best(Key v, Key& best, Key& second) {
     }
 }
 
+// The sum of a group's two best.  Of numbers it may be below the lowest of 32 bits, and -inf would say that nobody can be chosen there: the
+// lowest itself, then, as any other such sum, and who comes first is not clear.  (Above the largest, infinities are not clear either.)
+template <typename Key>
+__device__ __forceinline__ Key both(Key best, Key second) {
+    if constexpr (sizeof(Key) == 4) return fmaxf(best + second, -3.402823466e38f);
+    else return best + second;
+}
+
 // Keys of experts outside the groups that are kept become -inf.  `value` is what the groups are compared by, which is -inf for
 // experts that cannot be chosen.  Returns whether it was clear which.  Groups of whole lanes find their two best between those;
 // others go through shared memory (s: [E + 2 G]).
@@ -134,7 +142,7 @@ __device__ bool keep_groups(const Router& r, const Key (&value)[ITEMS], Key (&ke
             two_best(b, best, second);
             second = c > second ? c : second;
         }
-        if (r.pair && second > none) best += second;
+        if (r.pair && second > none) best = both(best, second);
         int rank = 0;
 #pragma unroll 4
         for (int g = 0; g < r.G; ++g) {
@@ -164,7 +172,7 @@ __device__ bool keep_groups(const Router& r, const Key (&value)[ITEMS], Key (&ke
                 two_best(s[g * r.per_group + at], best, second);
                 if (++at == r.per_group) at = 0;
             }
-            if (r.pair && second > none) best += second;
+            if (r.pair && second > none) best = both(best, second);
             s_group[g] = best;
         }
         __syncwarp();
