@@ -425,18 +425,23 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
                         if (e0 + i * 4 < e1) in.load(bias + e0 + i * 4);
                         in.get(x);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) value[4 * i + k] += x[k];
+                        for (int k = 0; k < 4; ++k) {
+                            value[4 * i + k] += x[k];
+                            bad = bad || x[k] != x[k];
+                        }
                     }
                 } else {
 #pragma unroll
-                    for (int j = 0; j < ITEMS; ++j)
-                        if (e0 + j < e1) value[j] += __ldg(&bias[e0 + j]);
+                    for (int j = 0; j < ITEMS; ++j) {
+                        const float x = e0 + j < e1 ? __ldg(&bias[e0 + j]) : 0.f;
+                        value[j] += x;
+                        bad = bad || x != x;
+                    }
                 }
             }
 #pragma unroll
             for (int j = 0; j < ITEMS; ++j) {
                 const bool there = l[j] > none;
-                bad = bad || (there && value[j] != value[j]);
                 value[j] = there && value[j] == value[j] ? value[j] : none;
                 if (bias) key[j] = value[j];
             }
