@@ -577,19 +577,27 @@ __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__
         z = sum_of<P>(z);
     }
     // the chosen: their scores (relative, as above), and sums over them
-    float m = none, base = none;
+    float m = none, base = 0.f;
     for (int k = q; k < top_k; k += P) {
         const int e = __ldg(&experts[at * top_k + k]);
         s_chosen[mine][k] = (unsigned)e < (unsigned)E ? e : -1;
         if ((unsigned)e >= (unsigned)E) continue;
-        m = fmaxf(m, logit(e));
-        if (renorm) base = fmaxf(base, __ldg(&grad_w[at * top_k + k]));
+        const float x = logit(e), g = renorm ? __ldg(&grad_w[at * top_k + k]) : 0.f;
+        if (x > m) {
+            m = x;
+            base = g;
+        }
     }
+    const float mine_m = m;
     m = max_of<P>(m);
-    // Shares do not change with what all gradients have in common: without the largest of them, nothing is left where they are alike,
-    // or there is one alone, whatever the shares' roundings.
-    if (renorm) base = max_of<P>(base);
-    if (!renorm || !isfinite(base)) base = 0.f;
+    // Shares do not change with what all gradients have in common.  Without the gradient of the one with the largest share, what is
+    // left of that one is the others' mean, which is small where they have little, and of the others the differences that count: nothing
+    // is lost between large numbers (with one share all but 1, that would be all digits), and nothing at all is left where gradients
+    // are alike, or there is one alone.
+    if (renorm) {
+        base = __shfl_sync(kAll, base, __ffs(__ballot_sync(kAll, mine_m == m) & lanes_of<P>(threadIdx.x & 31)) - 1);
+        if (!isfinite(base)) base = 0.f;
+    }
     if (!softmax) m = renorm ? fminf(m, 0.f) : 0.f;
     else if (!renorm) m = top;
     const auto score = [&](float x, float* rest) {               // *rest: 1 - sigmoid(x)
