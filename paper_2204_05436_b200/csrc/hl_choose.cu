@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(Shape<ITEMS, P>::kNT, Shape<ITEMS, P>::kCtas) 
 // sum of the chosen below, 0 otherwise; the chosen ones' are written over it.  P lanes of a warp for a token: the chosen ones' loads,
 // one behind the other, are what a token takes, and many tokens are on their way so.  65 536 tokens, 8 of 256 bf16: 14 us, 38 MB
 // (37 us with a warp a token).  N values of a row at a time: 16 bytes, or one.
-template <typename T, int P, bool WHOLE>
+template <typename T, int P, bool WHOLE, bool DENSE>
 __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__ logits, int64_t ld, const int32_t* n_tokens,
                                                            int64_t max_tokens, int top_k, int E, int flags, float scale,
                                                            const int32_t* __restrict__ experts, const float* __restrict__ grad_w,
@@ -531,7 +531,9 @@ __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__
     constexpr int kChosen = P == 2 ? 16 : HL_MAX_TOP_K;          // (two lanes: of up to 16 experts)
     __shared__ int32_t s_chosen[kTokens][kChosen];
     __shared__ float s_grad[kTokens][kChosen];
-    const bool softmax = flags & kSoftmax, renorm = flags & kRenorm, dense = softmax && !renorm;
+    constexpr int kWords = P == 2 ? 1 : P;                       // (two lanes: of up to 16 experts, eight: of up to 256)
+    __shared__ uint32_t s_there[DENSE ? kTokens : 1][kWords];    // a bit for each that is chosen
+    const bool softmax = DENSE || (flags & kSoftmax), renorm = !DENSE && (flags & kRenorm);
     const int q = threadIdx.x % P, mine = threadIdx.x / P;
     int64_t tokens = max_tokens;
     if (n_tokens) tokens = min((int64_t)max(__ldg(n_tokens), 0), max_tokens);
@@ -546,15 +548,16 @@ __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__
         const float x = as_float(row[e]);
         return x != x ? none : x;
     };
-    if (!dense && live)
+    if (!DENSE && live)
         for (int c = q * N; c < E; c += P * N) {
             Pack<T, N> v;
             v.zero();
             v.store(out + c);
         }
 
-    float top = none, z = 1.f;
-    if (dense) {
+    float top = none;
+    if constexpr (DENSE) {
+        if (q < kWords) s_there[mine][q] = 0;
         // (the row stays in the L1 for the next two rounds)
         for (int c = q * N; c < E; c += P * N) {
             Pack<T, N> v;
@@ -565,16 +568,7 @@ __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__
             for (int k = 0; k < N; ++k) top = fmaxf(top, x[k]);  // (which is not NaN where one of the two is)
         }
         top = max_of<P>(top);
-        z = 0.f;
-        for (int c = q * N; c < E; c += P * N) {
-            Pack<T, N> v;
-            float x[N];
-            v.load(row + c);
-            v.get(x);
-#pragma unroll
-            for (int k = 0; k < N; ++k) z += x[k] > none ? part(x[k], top) : 0.f;
-        }
-        z = sum_of<P>(z);
+        __syncwarp();
     }
     // the chosen: their scores (relative, as above), and sums over them
     float m = none, base = 0.f;
@@ -582,74 +576,103 @@ __global__ void __launch_bounds__(128) k_expert_choose_bwd(const T* __restrict__
         const int e = __ldg(&experts[at * top_k + k]);
         s_chosen[mine][k] = (unsigned)e < (unsigned)E ? e : -1;
         if ((unsigned)e >= (unsigned)E) continue;
-        const float x = logit(e), g = renorm ? __ldg(&grad_w[at * top_k + k]) : 0.f;
+        const float x = logit(e), g = renorm || DENSE ? __ldg(&grad_w[at * top_k + k]) : 0.f;
         if (x > m) {
             m = x;
             base = g;
         }
+        if constexpr (DENSE) atomicOr(&s_there[mine][e >> 5], 1u << (e & 31));
     }
     const float mine_m = m;
     m = max_of<P>(m);
     // Shares do not change with what all gradients have in common.  Without the gradient of the one with the largest share, what is
     // left of that one is the others' mean, which is small where they have little, and of the others the differences that count: nothing
     // is lost between large numbers (with one share all but 1, that would be all digits), and nothing at all is left where gradients
-    // are alike, or there is one alone.
-    if (renorm) {
+    // are alike, or there is one alone.  In a softmax over all, those that were not chosen have a gradient of 0: -base is left of it.
+    if (renorm || DENSE) {
         base = __shfl_sync(kAll, base, __ffs(__ballot_sync(kAll, mine_m == m) & lanes_of<P>(threadIdx.x & 31)) - 1);
         if (!isfinite(base)) base = 0.f;
     }
+    float z = 1.f, rest = 0.f;                                   // rest: of z, what those have that were not chosen
+    if constexpr (DENSE) {
+        if (m != top) base = 0.f;                                // (the one with the largest share was not chosen)
+        __syncwarp();
+        z = 0.f;
+        for (int c = q * N; c < E; c += P * N) {
+            Pack<T, N> v;
+            float x[N];
+            v.load(row + c);
+            v.get(x);
+            const uint32_t there = s_there[mine][c >> 5] >> (c & 31);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const float s = x[k] > none ? part(x[k], top) : 0.f;
+                z += s;
+                rest += (there >> k) & 1u ? 0.f : s;
+            }
+        }
+        z = sum_of<P>(z);
+        rest = sum_of<P>(rest);
+    }
     if (!softmax) m = renorm ? fminf(m, 0.f) : 0.f;
     else if (!renorm) m = top;
-    const auto score = [&](float x, float* rest) {               // *rest: 1 - sigmoid(x)
-        *rest = 1.f;
+    const auto score = [&](float x, float* other) {              // *other: 1 - sigmoid(x)
+        *other = 1.f;
         if (x == none) return 0.f;
         if (softmax) return part(x, m);
         const float e = expf(x > 0.f ? -x : x), per = 1.f / (1.f + e);
-        *rest = (x > 0.f ? e : 1.f) * per;
+        *other = (x > 0.f ? e : 1.f) * per;
         return (x > 0.f ? 1.f : m == 0.f ? e : part(x, m)) * per;
     };
-    float sum = 0.f, dot = 0.f, first = 0.f, first_rest = 1.f, first_g = 0.f;                // (of the lane's first choice)
+    // (in a softmax over all an expert counts once, however often it is there: at its first place)
+    const auto gradient = [&](int k, int e, bool* again) {
+        *again = false;
+        if constexpr (DENSE)
+            for (int i = 0; i < k; ++i) *again = *again || s_chosen[mine][i] == e;
+        return __ldg(&grad_w[at * top_k + k]) - (*again ? 0.f : base);
+    };
+    float sum = 0.f, dot = 0.f, first = 0.f, first_other = 1.f, first_g = 0.f;               // (of the lane's first choice)
+    bool first_again = false;
     for (int k = q; k < top_k; k += P) {
         const int e = s_chosen[mine][k];
         if (e < 0) continue;
-        float rest;
-        const float s = score(logit(e), &rest), g = __ldg(&grad_w[at * top_k + k]) - base;
+        float other;
+        bool again;
+        const float s = score(logit(e), &other), g = gradient(k, e, &again);
         if (k == q) {
             first = s;
-            first_rest = rest;
+            first_other = other;
             first_g = g;
+            first_again = again;
         }
         sum += s;
         dot += s * g;
     }
     sum = sum_of<P>(sum);
     dot = sum_of<P>(dot);
+    if constexpr (DENSE) dot -= base * rest;
     if (!renorm) sum = softmax ? z : 1.f;
     const float per = sum > 0.f ? 1.f / sum : 0.f, mean = renorm || softmax ? dot * per : 0.f;
-    __syncwarp();
     // d/dl of the weights: scale * share * (grad - mean), times 1 - score for sigmoids
     for (int k = q; k < top_k; k += P) {
-        float s = first, rest = first_rest, g = first_g;
+        float s = first, other = first_other, g = first_g;
+        bool again = first_again;
         const int e = s_chosen[mine][k];
         if (k != q && e >= 0) {
-            s = score(logit(e), &rest);
-            g = __ldg(&grad_w[at * top_k + k]) - base;
+            s = score(logit(e), &other);
+            g = gradient(k, e, &again);
         }
-        // (the mean is of all experts' softmax: once for an expert, however often it is there)
-        bool again = false;
-        if (dense)
-            for (int i = 0; i < k; ++i) again = again || s_chosen[mine][i] == e;
-        s_grad[mine][k] = e < 0 ? 0.f : scale * (s * per) * (again ? g : g - mean) * rest;
+        s_grad[mine][k] = e < 0 ? 0.f : scale * (s * per) * (again ? g : g - mean) * other;
     }
     if (!live) return;
-    if (dense)
+    if constexpr (DENSE)
         for (int c = q * N; c < E; c += P * N) {
             Pack<T, N> v;
             float x[N];
             v.load(row + c);
             v.get(x);
 #pragma unroll
-            for (int k = 0; k < N; ++k) x[k] = x[k] > none ? -scale * (part(x[k], top) * per) * mean : 0.f;
+            for (int k = 0; k < N; ++k) x[k] = x[k] > none ? -scale * (part(x[k], top) * per) * (base + mean) : 0.f;
             v.set(x);
             v.store(out + c);
         }
@@ -737,9 +760,11 @@ int32_t launch_choose_bwd(const hl_router* r, const void* logits, int64_t ld, in
                        lies_at(grad, 16) && ld_grad * sizeof(T) % 16 == 0;
     // (eight lanes a token: 32 experts' rows a line's half each; many experts: a warp)
     const int E = r->n_experts, P = E <= 16 ? 2 : E <= 256 ? 8 : 32;
+    const bool dense = r->score == HL_SCORE_SOFTMAX && !r->renorm;                 // (every expert's has a part)
 #define HL_RUN(P)                                                                                                               \
-    launch(whole ? k_expert_choose_bwd<T, P, true> : k_expert_choose_bwd<T, P, false>, (unsigned)div_up(max_tokens, 128 / P), 128, \
-           stream, static_cast<const T*>(logits), ld, n_tokens, max_tokens, r->top_k, E, flags_of(r), r->scale, experts, grad_w,   \
+    launch(dense ? (whole ? k_expert_choose_bwd<T, P, true, true> : k_expert_choose_bwd<T, P, false, true>)                       \
+                 : (whole ? k_expert_choose_bwd<T, P, true, false> : k_expert_choose_bwd<T, P, false, false>),                    \
+           (unsigned)div_up(max_tokens, 128 / P), 128, stream, static_cast<const T*>(logits), ld, n_tokens, max_tokens, r->top_k, E, flags_of(r), r->scale, experts, grad_w,   \
            static_cast<T*>(grad), ld_grad)
     HL_CUDA_TRY(P == 2 ? HL_RUN(2) : P == 8 ? HL_RUN(8) : HL_RUN(32));
 #undef HL_RUN
