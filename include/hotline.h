@@ -761,6 +761,12 @@ HL_API int32_t hl_expert_mx4(const hl_route* route, int32_t dtype, int64_t dim, 
                              int32_t by_token, const void* d_weights, void* d_y, int64_t ld_y, void* d_workspace, size_t ws_bytes,
                              void* stream);
 
+/* The same, with a status word as the other calls have one: d_status (device, may be NULL) receives HL_ETIMEOUT and is left alone
+ * otherwise, so that it tells of any of the products since the caller set it to HL_OK, whatever workspaces they took. */
+HL_API int32_t hl_expert_mx4_checked(const hl_route* route, int32_t dtype, int64_t dim, int64_t outputs, const void* d_x, int64_t ld_x,
+                                     int32_t by_token, const void* d_weights, void* d_y, int64_t ld_y, void* d_workspace,
+                                     size_t ws_bytes, int32_t* d_status, void* stream);
+
 /* No counterpart in the paper: an addition for callers that cannot allocate.
  *
  * Some callers have no way to hand the library a workspace: code that runs where device allocation is forbidden

@@ -31,7 +31,7 @@ EXPORTS = (
     "hl_expert_workspace_bytes", "hl_expert_sort", "hl_expert_dispatch", "hl_expert_combine", "hl_expert_combine_bwd",
     "hl_grad_workspace_bytes", "hl_grad_norm", "hl_grad_clip", "hl_embbag_grad_sumsq",
     "hl_token_embed", "hl_token_workspace_bytes", "hl_token_sort", "hl_token_embed_bwd", "hl_expert_choose", "hl_expert_choose_bwd",
-    "hl_mx4_bytes", "hl_mx4_quantise", "hl_mx4_dequantise", "hl_expert_mx4_workspace_bytes", "hl_expert_mx4",
+    "hl_mx4_bytes", "hl_mx4_quantise", "hl_mx4_dequantise", "hl_expert_mx4_workspace_bytes", "hl_expert_mx4", "hl_expert_mx4_checked",
 )
 
 
@@ -270,6 +270,8 @@ def _load() -> ctypes.CDLL:
     lib.hl_expert_mx4_workspace_bytes.argtypes = [i64, i32, i64]
     lib.hl_expert_mx4.restype = i32
     lib.hl_expert_mx4.argtypes = [rt, i32, i64, i64, vp, i64, i32, vp, vp, i64, vp, sz, vp]
+    lib.hl_expert_mx4_checked.restype = i32
+    lib.hl_expert_mx4_checked.argtypes = [rt, i32, i64, i64, vp, i64, i32, vp, vp, i64, vp, sz, vp, vp]
     return lib
 
 
@@ -919,3 +921,10 @@ def hl_expert_mx4(route: hl_route, dtype: int, dim: int, outputs: int, d_x, ld_x
                   d_workspace, ws_bytes: int, stream: int) -> None:
     _check("hl_expert_mx4", _lib.hl_expert_mx4(route, dtype, dim, outputs, _ptr(d_x), ld_x, int(bool(by_token)), _ptr(d_weights),
                                                _ptr(d_y), ld_y, _ptr(d_workspace), ws_bytes, stream))
+
+
+def hl_expert_mx4_checked(route: hl_route, dtype: int, dim: int, outputs: int, d_x, ld_x: int, by_token: bool, d_weights, d_y, ld_y: int,
+                          d_workspace, ws_bytes: int, d_status, stream: int) -> None:
+    _check("hl_expert_mx4_checked", _lib.hl_expert_mx4_checked(
+        route, dtype, dim, outputs, _ptr(d_x), ld_x, int(bool(by_token)), _ptr(d_weights), _ptr(d_y), ld_y, _ptr(d_workspace), ws_bytes,
+        _ptr(d_status), stream))

@@ -461,7 +461,7 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
                                                                const int32_t* __restrict__ counts, const int32_t* __restrict__ offsets,
                                                                int E, int64_t cap_rows, int max_tiles, int col_tiles, int f_tiles,
                                                                int64_t outputs, T* __restrict__ y, int64_t ld, bool lines, int stages,
-                                                               int panel_rows, int32_t* status) {
+                                                               int panel_rows, int32_t* status, int32_t* first_error) {
     extern __shared__ uint8_t s_raw[];
     uint8_t* base = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
     int* s_first = reinterpret_cast<int*>(base + kStagesBytes);
@@ -665,7 +665,10 @@ __global__ void __launch_bounds__(kProductNT, 1) k_mx4_product(const T* __restri
     if (s_gave_up) {
         // (copies and products that are still on their way get some time to end)
         for (int i = 0; i < 64; ++i) __nanosleep(1000);
-        if (threadIdx.x == 0) *status = HL_ETIMEOUT;
+        if (threadIdx.x == 0) {
+            *status = HL_ETIMEOUT;
+            if (first_error) set_status(first_error, HL_ETIMEOUT);
+        }
         __syncthreads();
     }
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
@@ -715,7 +718,7 @@ int32_t launch_dequantise(int64_t n, int64_t rows, int64_t dim, const void* q, v
 }
 template <typename T>
 int32_t launch_product(const hl_route* r, int64_t dim, int64_t outputs, const void* x, int64_t ld_x, bool by_token, const void* w,
-                       void* y, int64_t ld_y, void* workspace, bool whole, cudaStream_t stream) {
+                       void* y, int64_t ld_y, void* workspace, bool whole, int32_t* first_error, cudaStream_t stream) {
     int32_t* status = static_cast<int32_t*>(workspace);
     uint8_t* q = static_cast<uint8_t*>(workspace) + kWorkspaceHead;
     const int64_t ct = tiles_of(dim, kTileCols), ft = tiles_of(outputs, kTileRows), rt = row_tiles_most(r->cap_rows, r->n_experts);
@@ -746,7 +749,7 @@ int32_t launch_product(const hl_route* r, int64_t dim, int64_t outputs, const vo
                                static_cast<const T*>(direct ? x : nullptr), ld_x, r->n_tokens, by_token ? r->place : nullptr,
                                r->max_tokens, r->top_k, dim, (const uint8_t*)q, static_cast<const uint8_t*>(w), r->counts, r->offsets, r->n_experts, r->cap_rows, rt, ct,
                                ft, outputs, static_cast<T*>(y), ld_y,
-                               outputs * sizeof(T) % 16 == 0 && ld_y * sizeof(T) % 16 == 0 && lies_at(y, 16), stages, panel, status));
+                               outputs * sizeof(T) % 16 == 0 && ld_y * sizeof(T) % 16 == 0 && lies_at(y, 16), stages, panel, status, first_error));
     note_launches(1);
     HL_LAUNCH_CHECK();
     return HL_OK;
@@ -799,9 +802,9 @@ extern "C" size_t hl_expert_mx4_workspace_bytes(int64_t cap_rows, int32_t n_expe
     return (size_t)(kWorkspaceHead + row_tiles_most(cap_rows, n_experts) * tiles_of(dim, kTileCols) * kPanelBytes);
 }
 
-extern "C" int32_t hl_expert_mx4(const hl_route* route, int32_t dtype, int64_t dim, int64_t outputs, const void* d_x, int64_t ld_x,
-                                 int32_t by_token, const void* d_weights, void* d_y, int64_t ld_y, void* d_workspace, size_t ws_bytes,
-                                 void* stream_) {
+extern "C" int32_t hl_expert_mx4_checked(const hl_route* route, int32_t dtype, int64_t dim, int64_t outputs, const void* d_x, int64_t ld_x,
+                                         int32_t by_token, const void* d_weights, void* d_y, int64_t ld_y, void* d_workspace,
+                                         size_t ws_bytes, int32_t* d_status, void* stream_) {
     const cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     const hl_route* r = route;
     if (!r || !lies_at(r->n_tokens, 4) || !lies_at(r->place, 4) || !lies_at(r->counts, 4) || !lies_at(r->offsets, 4) ||
@@ -810,7 +813,7 @@ extern "C" int32_t hl_expert_mx4(const hl_route* route, int32_t dtype, int64_t d
         r->cap_rows >= (int64_t(1) << 31) - 65536 || !r->counts || !r->offsets || (by_token && !r->place && r->max_tokens > 0))
         return HL_EINVAL;
     if (!row_matrix_ok(dtype, by_token ? r->max_tokens : r->cap_rows, dim, d_x, ld_x) || !row_matrix_ok(dtype, r->cap_rows, outputs, d_y, ld_y) ||
-        !d_weights || !lies_at(d_weights, 16) || !d_workspace || !lies_at(d_workspace, 256))
+        !d_weights || !lies_at(d_weights, 16) || !d_workspace || !lies_at(d_workspace, 256) || !lies_at(d_status, 4))
         return HL_EINVAL;
     if (ws_bytes < hl_expert_mx4_workspace_bytes(r->cap_rows, r->n_experts, dim)) return HL_ECAPACITY;
     if (r->cap_rows == 0 || (by_token && r->max_tokens == 0)) {  // (no more than the status)
@@ -818,7 +821,13 @@ extern "C" int32_t hl_expert_mx4(const hl_route* route, int32_t dtype, int64_t d
         return HL_OK;
     }
     const bool whole = dim % 8 == 0 && rows_lie_at(dtype, d_x, ld_x, 16);
-#define HL_PRODUCT(T) launch_product<T>(r, dim, outputs, d_x, ld_x, by_token != 0, d_weights, d_y, ld_y, d_workspace, whole, stream)
+#define HL_PRODUCT(T) launch_product<T>(r, dim, outputs, d_x, ld_x, by_token != 0, d_weights, d_y, ld_y, d_workspace, whole, d_status, stream)
     return HL_FOR_TYPE(HL_PRODUCT);
 #undef HL_PRODUCT
+}
+
+extern "C" int32_t hl_expert_mx4(const hl_route* route, int32_t dtype, int64_t dim, int64_t outputs, const void* d_x, int64_t ld_x,
+                                 int32_t by_token, const void* d_weights, void* d_y, int64_t ld_y, void* d_workspace, size_t ws_bytes,
+                                 void* stream) {
+    return hl_expert_mx4_checked(route, dtype, dim, outputs, d_x, ld_x, by_token, d_weights, d_y, ld_y, d_workspace, ws_bytes, nullptr, stream);
 }

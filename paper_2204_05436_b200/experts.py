@@ -344,6 +344,7 @@ class Mx4Weights:
         self.n_experts, self.outputs, self.dim = weights.shape
         self._q = torch.empty(self.n_experts * B.hl_mx4_bytes(self.outputs, self.dim), dtype=torch.uint8, device=self.device)
         self._ws: list = []                                  # the last is the largest; a captured graph may hold on to any
+        self._status = torch.zeros(1, dtype=torch.int32, device=self.device)       # of all products, with any of them
         self._call(B.hl_mx4_quantise, B.dtype_of(weights), self.n_experts, self.outputs, self.dim, weights, self.dim,
                    self.outputs * self.dim, self._q)
 
@@ -371,14 +372,15 @@ class Mx4Weights:
         need = B.hl_expert_mx4_workspace_bytes(route.cap_rows, self.n_experts, self.dim)
         if not self._ws or self._ws[-1].numel() < need:
             self._ws.append(torch.zeros(need, dtype=torch.uint8, device=self.device))
-        self._call(B.hl_expert_mx4, route._route, B.dtype_of(x), self.dim, self.outputs, x, ld, by_token, self._q, out, ld_out,
-                   self._ws[-1], self._ws[-1].numel())
+        self._call(B.hl_expert_mx4_checked, route._route, B.dtype_of(x), self.dim, self.outputs, x, ld, by_token, self._q, out, ld_out,
+                   self._ws[-1], self._ws[-1].numel(), self._status)
         return out
 
     def status(self, raise_on_error: bool = True) -> int:
-        """Waits for the device: HL_OK, or HL_ETIMEOUT if a wait inside the last product gave up."""
+        """Waits for the device: HL_OK, or HL_ETIMEOUT if a wait inside any product since the last call gave up."""
         torch.cuda.synchronize(self.device)
-        st = int(self._ws[-1][:4].view(torch.int32).item()) if self._ws else B.HL_OK
+        st = int(self._status.item())
+        self._status.zero_()
         if raise_on_error:
             B._check("hl_expert_mx4", st)
         return st
