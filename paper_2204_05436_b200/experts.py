@@ -318,6 +318,7 @@ class ExpertRouter:
         torch.cuda.synchronize(self.device)
         st = int(self._status.item())
         self._status.zero_()
+        torch.cuda.current_stream(self.device).synchronize()     # (before a call on another stream may set it)
         if raise_on_error:
             B._check("hl_expert_choose", st)
         return st
@@ -381,6 +382,7 @@ class Mx4Weights:
         torch.cuda.synchronize(self.device)
         st = int(self._status.item())
         self._status.zero_()
+        torch.cuda.current_stream(self.device).synchronize()     # (before a call on another stream may set it)
         if raise_on_error:
             B._check("hl_expert_mx4", st)
         return st

@@ -94,6 +94,7 @@ class TokenEmbedding:
         torch.cuda.synchronize(self.device)
         st = int(self._status.item())
         self._status.zero_()
+        torch.cuda.current_stream(self.device).synchronize()     # (before a call on another stream may set it)
         if raise_on_error:
             B._check("hl_token_embed", st)
         return st
