@@ -67,7 +67,7 @@ class TokenEmbedding:
         """Puts the tokens in the order of their rows, for backward() (which reads ``n_tokens`` too)."""
         self._tokens(tokens, n_tokens, self.max_tokens)
         for own in (self.sorted, self.order):
-            _written(own, own.numel(), tokens)
+            _written(own, own.numel(), tokens, n_tokens)
         self.tokens, self.n_tokens = tokens.numel(), n_tokens
         self._call(B.hl_token_sort, tokens, self.tokens, n_tokens, self.n_rows, self.sorted, self.order, self._status, self._ws,
                    self._ws_bytes)
@@ -84,7 +84,7 @@ class TokenEmbedding:
                 raise ValueError("accumulate needs the grad_table to add to")
             grad_table = torch.empty(self.n_rows, self.dim, dtype=dtype, device=self.device)
         ld_table = _matrix("grad_table", grad_table, self.device, self.n_rows, self.dim)
-        _written(grad_table, ld_table, grad_out, self.n_tokens)
+        _written(grad_table, ld_table, grad_out, self.n_tokens, self.sorted, self.order)
         self._call(B.hl_token_embed_bwd, self.n_rows, self.dim, self.sorted, self.order, self.tokens, self.n_tokens, B.dtype_of(grad_out),
                    grad_out, ld, scale, B.dtype_of(grad_table), grad_table, ld_table, accumulate, self._ws, self._ws_bytes)
         return grad_table
