@@ -726,14 +726,17 @@ int32_t launch_product(const hl_route* r, int64_t dim, int64_t outputs, const vo
     const int64_t choices = r->max_tokens * r->top_k, most_rows = by_token && choices < r->cap_rows ? choices : r->cap_rows;
     const bool direct = most_rows <= kFewRows && (!by_token || choices <= kFewRows);
     if (!direct) {
-        // Parts of a row that a warp has on their way at a time: as many as there are, up to four, or eight where there are enough rows
-        // for the chip's warps all the same; twice that one after the other where that leaves them eight rounds.
+        // Parts of a row that a warp has on their way at a time: as many as there are, up to four, or eight of 16-bit types where there are
+        // enough rows for the chip's warps all the same; twice that one after the other where that leaves them eight rounds.  Eight / four, a whole call
+        // of 32 outputs: 16 384 rows of 4 096 bf16 to two experts each 57 / 69 us, that begin anywhere 77 / 83, by expert 82 / 101 and 118 / 132; fp32,
+        // whose eight do not fit the registers, 76 / 74, 129 / 107, 118 / 110 and 213 / 174.
+        constexpr int kMost = sizeof(T) == 2 ? 8 : 4;
         const int64_t rows = by_token ? r->max_tokens : r->cap_rows;
-        const int U = ct <= 2 ? (int)ct : ct >= 7 && rows * div_up(ct, 8) >= 8 * kRowCtas<8> * kSMs ? 8 : 4;
+        const int U = ct <= 2 ? (int)ct : kMost == 8 && ct >= 7 && rows * div_up(ct, 8) >= 8 * kRowCtas<8> * kSMs ? 8 : 4;
         const int ctas = U == 8 ? kRowCtas<8> : U == 4 ? kRowCtas<4> : kRowCtas<1>;
         const int64_t chunks = div_up(ct, U), span = U == 8 && rows * chunks >= 8 * 8 * ctas * kSMs ? 2 : 1, per_row = div_up(chunks, span);
 #define HL_ROWS(U) (whole ? k_mx4_rows<T, true, U> : k_mx4_rows<T, false, U>)
-        const auto convert = U == 8 ? HL_ROWS(8) : U == 4 ? HL_ROWS(4) : U == 2 ? HL_ROWS(2) : HL_ROWS(1);
+        const auto convert = U == kMost ? HL_ROWS(kMost) : U == 4 ? HL_ROWS(4) : U == 2 ? HL_ROWS(2) : HL_ROWS(1);
 #undef HL_ROWS
         HL_CUDA_TRY(launch(convert, grid_for(rows * per_row, kRowNT / 32, ctas * kSMs), kRowNT, stream,
                            static_cast<const T*>(x), ld_x, dim, ct, span, inverse_of(per_row), per_row, r->n_tokens, rows,
