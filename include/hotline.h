@@ -695,7 +695,7 @@ HL_API int32_t hl_token_sort(const int32_t* d_tokens, int64_t max_tokens, const 
 
 /* grad_table[u, :] = scale * sum of grad_out[i, :] over the tokens i of row u, rounded once to grad_table's type; zeros in rows
  * without tokens.  accumulate != 0: that is added to grad_table, whose rows without tokens are left alone.  Sums are the same
- * in every run: of 32-bit numbers, those of a row's tokens in their order, in runs that the sorted tokens alone decide.
+ * in every run: of 32-bit numbers, those of a row's tokens in their order, in pieces that max_tokens, dim and the sorted tokens decide.
  * d_sorted and d_order as hl_token_sort made them, with the same d_n_tokens. */
 HL_API int32_t hl_token_embed_bwd(int64_t n_rows, int64_t dim, const int32_t* d_sorted, const int32_t* d_order,
                                   int64_t max_tokens, const int32_t* d_n_tokens, int32_t grad_dtype, const void* d_grad_out,

@@ -147,7 +147,8 @@ __device__ __forceinline__ void from_four_bits(uint32_t packed, uint32_t E, floa
 }
 
 // The way back: a lane writes 16 bytes of a row's part at a time, so that a warp's stores are whole lines (with 32 bytes of fp32 in a
-// row of a lane's own, two halves of a line each: 127 us instead of 92 for 134 M values).
+// row of a lane's own, two halves of a line each: 127 us instead of 92 for 134 M values).  Rows that begin anywhere are written value by
+// value: 40 000 of 2 500 values 102 us in fp32 and 275 in 16 bits, where such of 2 496 that begin at 16 bytes take 74 and 45.
 template <typename T, bool WHOLE, int U>
 __global__ void __launch_bounds__(kRowNT) k_mx4_dequantise(const uint8_t* __restrict__ q, int64_t row_tiles, int64_t dim,
                                                            uint64_t rows_inverse, int64_t rows_d, uint64_t chunks_inverse,
